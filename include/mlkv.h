@@ -227,6 +227,114 @@ int mlkv_prefill(mlkv_cache_t c, int layer, const void *Q, const void *K, const 
                  const int *prompt_lens, int s_max, void *cuda_stream);
 
 /*
+ * mlkv_decode_attention_window - mlkv_decode_attention with a sliding window and a few first tokens
+ * that stay visible (sinks): the newest token, at position L - 1 (L = seq_lens[beta]), attends to
+ * positions u < L with u < sinks or u >= L - window.  Only tiles with visible positions are read; the
+ * cache keeps the others.  The paper's layers attend to every position: this bounds what a step of a
+ * long sequence reads, whatever the map of owners.
+ *
+ *   window   >= 0 positions, the newest included; 0 = every position (sinks ignored)
+ *   sinks    >= 0
+ * The other arguments as for mlkv_decode_attention (an owner layer's new token is stored before, with
+ * mlkv_append).  Option "tile_tokens" applies; "tc" does not.  Errors: as mlkv_decode_attention, and
+ * MLKV_ERR_INVALID_ARG for a negative window or sinks.
+ */
+int mlkv_decode_attention_window(mlkv_cache_t c, int layer, const void *Q, void *out,
+                                 const int *seq_lens, int window, int sinks, void *cuda_stream);
+
+/*
+ * mlkv_prefill_window - mlkv_prefill with a sliding window and sinks: prompt position t attends to
+ * positions u <= t with u < sinks or u > t - window (mlkv_decode_attention_window's rule at every
+ * position; window 0 = every u <= t).  Key tiles that no query of a block sees are never read.  An
+ * owner layer stores all of the prompt's keys and values.  As in mlkv_prefill a key that is masked for
+ * one query but shares a tile of 128 with one of its visible keys must hold a finite value.
+ * Arguments and errors as for mlkv_prefill, and MLKV_ERR_INVALID_ARG for a negative window or sinks.
+ */
+int mlkv_prefill_window(mlkv_cache_t c, int layer, const void *Q, const void *K, const void *V,
+                        void *out, const int *prompt_lens, int s_max, int window, int sinks,
+                        void *cuda_stream);
+
+/*
+ * mlkv_qk_norm_rope - queries, keys and values as a projection leaves them, made ready for the calls of
+ * this library: RMS norm of every query and key head with a learned gain, rotary position encoding,
+ * and the keys and values moved to the cache's head-major order, in one pass.
+ * The paper's models encode positions rotarily; its cache takes keys that are encoded already.
+ *
+ *   y = x / sqrt(mean(x^2) + eps) * gain, per head; then on channels [0, rot_dim) of y each pair (a, b)
+ *   becomes (a cos - b sin, b cos + a sin), with cos and sin of row positions[token], column i.
+ *
+ *   Q          device bf16, batch * s tokens of n_q_heads heads of head_dim; token k at Q + k q_stride
+ *   K, V       the same with kv_heads heads and their strides (the three may be parts of one fused
+ *              projection); V and V_out may both be NULL, else values are copied unchanged
+ *   *_stride   elements between tokens, >= 0, a multiple of 8
+ *   q_gain, k_gain   device bf16 [head_dim], or NULL: gain 1
+ *   cos_table, sin_table   device fp32 [n_pos][rot_dim / 2]
+ *   rot_dim    0 (no encoding) to head_dim, a multiple of 16
+ *   interleaved   0: pair i is channels i and i + rot_dim / 2; else channels 2 i and 2 i + 1
+ *   positions  device int32 [batch * s]; a token whose position lies outside [0, n_pos) gets NaN in
+ *              its rotated channels, nothing outside the tables is read
+ *   eps        finite, >= 0
+ *   Q_out      device bf16 [batch][s][n_q_heads][head_dim]
+ *   K_out, V_out   device bf16 [batch][kv_heads][s][head_dim] (one token: [batch][kv_heads][head_dim])
+ * Every tensor 16-byte aligned (positions 4).  An output may be its own input where every head keeps its
+ * place (dense tokens; for K and V, s = 1), and otherwise overlaps no input and no other output.
+ * Arithmetic: fp32, each output rounded once.  Runs on the calling thread's current device.
+ * Errors: MLKV_ERR_INVALID_ARG, MLKV_ERR_UNSUPPORTED (head_dim not 64 or 128, rot_dim not a multiple of
+ * 16), MLKV_ERR_CUDA.
+ */
+int mlkv_qk_norm_rope(const void *Q, const void *K, const void *V, int64_t q_stride, int64_t k_stride,
+                      int64_t v_stride, const void *q_gain, const void *k_gain,
+                      const float *cos_table, const float *sin_table, int n_pos, int rot_dim,
+                      int interleaved, const int *positions, float eps, int batch, int s,
+                      int n_q_heads, int kv_heads, int head_dim, void *Q_out, void *K_out,
+                      void *V_out, void *cuda_stream);
+
+/*
+ * The 4-bit cache: the m owner layers' keys and values (Sec. 3) in 4 bits a channel, for contexts or
+ * batches whose bf16 cache is too large or too slow to read; 0.28 of its bytes.
+ *
+ * 32 consecutive channels of one position of one KV head share a scale, the bf16 nearest to their
+ * largest magnitude / 7.  A channel is held as the whole number in [-7, 7] nearest to its value / scale
+ * (halves away from zero) and stands for that number times the scale.  A group with a NaN or an
+ * infinity holds NaN throughout; one whose scale would be below 2^-126 holds zeros.
+ *
+ * The calls mirror those of the bf16 cache: the same maps, layouts, checks, errors and stream rules.
+ *   mlkv_q4_create            as mlkv_cache_create; the cache starts as zeros
+ *   mlkv_q4_destroy           as mlkv_cache_destroy
+ *   mlkv_q4_bytes             bytes of the cache, 2.25 * b * g * m * head_dim / 2 a position, positions
+ *                             rounded up to a multiple of 64
+ *   mlkv_q4_append            as mlkv_append
+ *   mlkv_q4_load_prefix       as mlkv_load_prefix (K and V in the device's memory, 16-byte aligned);
+ *                             positions from len on keep what they hold
+ *   mlkv_q4_read              positions [start, start + len) of the layer's owner as bf16 K and V
+ *                             [batch][g][len][d]: each value rounded to nearest even
+ *   mlkv_q4_decode_attention  as mlkv_decode_attention over what the cache holds, with the window and
+ *                             sinks of mlkv_decode_attention_window (window 0 = every position)
+ *   mlkv_q4_prefill           as mlkv_prefill_window, over the prompt's own K and V (bf16, so that a
+ *                             prompt's outputs do not depend on the cache's precision): every layer is
+ *                             given its owner's K and V, and an owner layer stores them; out overlaps
+ *                             none of Q, K and V
+ *   mlkv_q4_sync_status       as mlkv_sync_status
+ */
+typedef struct mlkv_q4cache *mlkv_q4cache_t;
+
+int mlkv_q4_create(mlkv_q4cache_t *out, int n_layers, int n_q_heads, int head_dim,
+                   const int *layer_owner, int kv_heads_per_owner, int batch, int max_seq);
+int mlkv_q4_destroy(mlkv_q4cache_t c);
+int64_t mlkv_q4_bytes(mlkv_q4cache_t c);
+int mlkv_q4_append(mlkv_q4cache_t c, int layer, const void *K, const void *V, const int *seq_lens,
+                   void *cuda_stream);
+int mlkv_q4_load_prefix(mlkv_q4cache_t c, int layer, const void *K, const void *V, int len,
+                        void *cuda_stream);
+int mlkv_q4_read(mlkv_q4cache_t c, int layer, void *K, void *V, int start, int len,
+                 void *cuda_stream);
+int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *out,
+                             const int *seq_lens, int window, int sinks, void *cuda_stream);
+int mlkv_q4_prefill(mlkv_q4cache_t c, int layer, const void *Q, const void *K, const void *V, void *out,
+                    const int *prompt_lens, int s_max, int window, int sinks, void *cuda_stream);
+int mlkv_q4_sync_status(mlkv_q4cache_t c);
+
+/*
  * mlkv_load_prefix - bulk-stores positions [0, len) of an owner layer's keys and values
  * (prefill).  K, V: device bf16 [batch][g][len][d].  No-op (MLKV_OK) for a non-owner layer.
  * A kernel copies them; if K or V lies in another GPU's memory or the host's, or off the 16-byte

@@ -223,12 +223,36 @@ __device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v 
 
 // With one length for every sequence (uniform_len > 0) the walk is arithmetic; otherwise it reads
 // the per-sequence tables, which the kernel copies from its parameters into shared memory.
-template <int T>
+template <int T, bool kWin = false>
 struct TileWalk {
     int beta, j, tt, nt, L, seg_first, layer, item;
     int kk;    // multi-layer launch: index of the current item among the CTA's
     int t0;    // first tile of the current piece's chunk (0 unless segments are chunked)
     int rec;   // multi-layer launch with chunks: the piece's partial-record index
+    int ns, skip, sinks;   // sliding window: see VisibleTiles (unset without one)
+
+    // Tiles of the current sequence, whose L positions are set.
+    __device__ __forceinline__ void set_tiles(const DecodeWindow<kWin> &win)
+    {
+        if constexpr (kWin) {
+            const VisibleTiles v = visible_tiles(L, win.window, win.sinks, T, 1);
+            nt = v.nt;
+            ns = v.ns;
+            skip = v.skip;
+            sinks = win.sinks;
+        } else {
+            nt = (L + T - 1) / T;
+        }
+    }
+    // First position of the current tile, and the visible positions from there on (T or more: all).
+    __device__ __forceinline__ int pos() const
+    {
+        return kWin && tt >= ns ? tt * T + skip : tt * T;
+    }
+    __device__ __forceinline__ int left() const
+    {
+        return kWin && tt < ns ? sinks - tt * T : L - pos();
+    }
 
     // Multi-layer launch: the rank of this CTA's k-th item, or -1 past its last: round k of the
     // deal gives CTA c rank k P + c, or k P + P - 1 - c in odd rounds of a snake deal.
@@ -301,7 +325,8 @@ struct TileWalk {
     // `tile`: the flattened tile of a single-layer launch, or the CTA's own tile count in a
     // multi-layer launch (its k-th item is item blockIdx.x + k gridDim.x).
     __device__ __forceinline__ void init(const DecodeParams &p, const int *s_len,
-                                         const int *s_start, int tile)
+                                         const int *s_start, int tile,
+                                         const DecodeWindow<kWin> &win = {})
     {
         if (p.ml_layers > 0) {
             // only ever started at the CTA's first tile (tile_lo = 0)
@@ -318,7 +343,7 @@ struct TileWalk {
         rec = 0;
         if (p.uniform_len > 0) {
             L = p.uniform_len;
-            nt = (L + T - 1) / T;
+            set_tiles(win);
             const int seg = tile / nt;
             tt = tile - seg * nt;
             beta = seg / p.g;
@@ -336,7 +361,7 @@ struct TileWalk {
         }
         beta = lo;
         L = s_len[beta];
-        nt = (L + T - 1) / T;
+        set_tiles(win);
         const int rel = tile - s_start[beta];
         j = rel / nt;
         tt = rel - j * nt;
@@ -344,7 +369,7 @@ struct TileWalk {
     }
 
     __device__ __forceinline__ void next(const DecodeParams &p, const int *s_len,
-                                         const int *s_start)
+                                         const int *s_start, const DecodeWindow<kWin> &win = {})
     {
         if (++tt < nt)
             return;
@@ -371,7 +396,7 @@ struct TileWalk {
             j = 0;
             if (++beta < p.b) {
                 L = s_len[beta];
-                nt = (L + T - 1) / T;
+                set_tiles(win);
             }
         }
         seg_first = (beta < p.b) ? s_start[beta] + j * nt : p.num_tiles;

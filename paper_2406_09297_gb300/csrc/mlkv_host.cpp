@@ -17,80 +17,22 @@
 #include <vector>
 
 #include "mlkv.h"
+#include "mlkv_host.h"
 #include "mlkv_internal.h"
+
+using mlkv::aligned16;
+using mlkv::current_device;
+using mlkv::DeviceGuard;
+using mlkv::driver_entry;
+using mlkv::EncodeTiledFn;
+using mlkv::fail;
+using mlkv::fail_cuda;
+using mlkv::overlap;
+using mlkv::validate_map;
 
 namespace {
 
 thread_local std::string g_last_error;
-
-int fail(int code, const char *fmt, ...)
-{
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof(buf), fmt, ap);
-    va_end(ap);
-    g_last_error = buf;
-    return code;
-}
-
-int fail_cuda(cudaError_t e, const char *what)
-{
-    return fail(MLKV_ERR_CUDA, "%s: %s (%s)", what, cudaGetErrorName(e), cudaGetErrorString(e));
-}
-
-using EncodeTiledFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
-                                   const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                                   const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-using CtxGetCurrentFn = CUresult (*)(CUcontext *);
-using CtxGetDeviceFn = CUresult (*)(CUdevice *);
-
-template <typename Fn>
-Fn driver_entry(const char *name)
-{
-    void *fn = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion(name, &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess)
-        return nullptr;
-    return reinterpret_cast<Fn>(fn);
-}
-
-// The device of the CUDA context current on this thread (e.g. the one PyTorch made current);
-// falls back to this runtime's current device.
-int current_device()
-{
-    static CtxGetCurrentFn get_ctx = driver_entry<CtxGetCurrentFn>("cuCtxGetCurrent");
-    static CtxGetDeviceFn get_dev = driver_entry<CtxGetDeviceFn>("cuCtxGetDevice");
-    CUcontext ctx = nullptr;
-    if (get_ctx != nullptr && get_dev != nullptr && get_ctx(&ctx) == CUDA_SUCCESS && ctx) {
-        CUdevice dev;
-        if (get_dev(&dev) == CUDA_SUCCESS)
-            return static_cast<int>(dev);
-    }
-    int d = 0;
-    cudaGetDevice(&d);
-    return d;
-}
-
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev)
-    {
-        if (cudaGetDevice(&prev) != cudaSuccess)
-            prev = -1;
-        if (prev != dev)
-            ok = cudaSetDevice(dev) == cudaSuccess;
-    }
-    ~DeviceGuard()
-    {
-        int now = -1;
-        if (prev >= 0 && cudaGetDevice(&now) == cudaSuccess && now != prev)
-            cudaSetDevice(prev);
-    }
-};
 
 }  // namespace
 
@@ -124,7 +66,7 @@ struct mlkv_cache {
     int pdl = 1;                // programmatic dependent launch
     int early_fetch = 1;        // per-layer step: later layers read Q and tiles before the wait
     int tc = 0;                 // 1: the tcgen05 kernel where a variant exists (slower here)
-    int prefill_ready = 0;      // the prefill kernel's shared-memory limit is set
+    int prefill_ready = 0;      // the prefill kernels' shared-memory limits are set (1 all, 2 windowed)
     int fused_ready = 0;        // the same for the fused-decode forms (bit 1 << form)
     int fused_deep = 1;         // fused decode: the deep one-tile form where one unit per SM
     // Context-chunk partials of the fused decode.  A buffer that was outgrown lives until the cache
@@ -192,8 +134,6 @@ int check_seq_lens(const mlkv_cache *c, const int *seq_lens)
     }
     return MLKV_OK;
 }
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 mlkv_cache::Variant *pick_variant(mlkv_cache *c, double mean_len = -1.0, int force_T = 0)
 {
@@ -269,7 +209,11 @@ void assign_map(mlkv_cache *c, int l, int h, int d, const int *owner, int g, int
     }
 }
 
-int validate_map(int l, int h, int d, const int *owner, int g, int b, int max_seq)
+}  // namespace
+
+void mlkv::set_last_error(const char *msg) { g_last_error = msg; }
+
+int mlkv::validate_map(int l, int h, int d, const int *owner, int g, int b, int max_seq)
 {
     if (l < 1 || h < 1 || g < 1 || b < 1 || max_seq < 1 || d < 1)
         return fail(MLKV_ERR_INVALID_ARG,
@@ -297,10 +241,6 @@ int validate_map(int l, int h, int d, const int *owner, int g, int b, int max_se
         return fail(MLKV_ERR_UNSUPPORTED, "batch %d exceeds %d", b, MLKV_MAX_BATCH);
     return MLKV_OK;
 }
-
-}  // namespace
-
-void mlkv::set_last_error(const char *msg) { g_last_error = msg; }
 
 extern "C" {
 
@@ -496,7 +436,8 @@ int mlkv_append(mlkv_cache_t c, int layer, const void *K, const void *V, const i
 static int decode_impl(mlkv_cache_t c, int layer, const void *K_new, const void *V_new,
                        const void *Q, void *out, const int *seq_lens, void *cuda_stream,
                        int early_fetch = 0, const void *Q_next = nullptr,
-                       int newest_ready = 0, int store_new = 1, int in_step = 0)
+                       int newest_ready = 0, int store_new = 1, int in_step = 0, int window = 0,
+                       int sinks = 0)
 {
     if (c == nullptr)
         return fail(MLKV_ERR_INVALID_ARG, "null cache handle");
@@ -514,9 +455,11 @@ static int decode_impl(mlkv_cache_t c, int layer, const void *K_new, const void 
     int rc = check_seq_lens(c, seq_lens);
     if (rc != MLKV_OK)
         return rc;
+    // What a sliding window leaves of a length, in positions (the tiles' count follows below).
+    auto seen = [&](int L) { return window > 0 && L - window > sinks ? window + sinks : L; };
     double mean_len = 0.0;
     for (int beta = 0; beta < c->b; ++beta)
-        mean_len += seq_lens[beta];
+        mean_len += seen(seq_lens[beta]);
     mean_len /= c->b;
     // Inside a decode step, a layer that is one long segment (d = 64) runs on the 128-position
     // tile (two CTAs per SM) over 64 CTAs, so the next layers' grids stream beside it (measured,
@@ -526,7 +469,11 @@ static int decode_impl(mlkv_cache_t c, int layer, const void *K_new, const void 
     const bool single_long = in_step && c->tile_tokens == 0 && c->grid <= 0 && c->d == 64 &&
                              c->b * c->g == 1 && seq_lens[0] >= 16384;
     mlkv_cache::Variant *var = pick_variant(c, mean_len, single_long ? 128 : 0);
-    if (var == nullptr)
+    if (var != nullptr && window > 0 && var->v->win_fn == nullptr)   // the tcgen05 kernel has none
+        for (auto &v : c->variants)
+            if (v.v->win_fn != nullptr && v.v->tile_tokens == var->v->tile_tokens)
+                var = &v;
+    if (var == nullptr || (window > 0 && var->v->win_fn == nullptr))
         return fail(MLKV_ERR_UNSUPPORTED, "no decode variant for d=%d tile_tokens=%d", c->d,
                     c->tile_tokens);
     bool uniform = true;
@@ -552,9 +499,23 @@ static int decode_impl(mlkv_cache_t c, int layer, const void *K_new, const void 
     for (int beta = 0; beta < c->b; ++beta) {
         p.tile_start[beta] = static_cast<int>(tiles);
         p.seq_len[beta] = seq_lens[beta];
-        tiles += static_cast<long long>(c->g) * ((seq_lens[beta] + T - 1) / T);
+        tiles += static_cast<long long>(c->g) *
+                 (window > 0 ? mlkv::visible_tiles(seq_lens[beta], window, sinks, T, 1).nt
+                             : (seq_lens[beta] + T - 1) / T);
     }
     p.uniform_len = uniform ? seq_lens[0] : 0;
+    // With a window the kernel sees the sequences' own lengths, the merges of pieces those whose plain
+    // tiling gives the same tiles.
+    auto window_lens = [&](bool own) {
+        for (int beta = 0; beta < c->b; ++beta)
+            p.seq_len[beta] =
+                own ? seq_lens[beta]
+                    : mlkv::visible_len(seq_lens[beta],
+                                        mlkv::visible_tiles(seq_lens[beta], window, sinks, T, 1));
+        p.uniform_len = uniform ? p.seq_len[0] : 0;
+    };
+    if (window > 0)
+        window_lens(false);
     if (tiles > 0x7fffffffLL)
         return fail(MLKV_ERR_UNSUPPORTED, "%lld tiles exceed the int32 tile index", tiles);
     p.tile_start[c->b] = static_cast<int>(tiles);
@@ -602,7 +563,7 @@ static int decode_impl(mlkv_cache_t c, int layer, const void *K_new, const void 
     } else {
         grid = static_cast<int>((tiles + per_wave - 1) / per_wave);
         if (uniform) {
-            const long long nt = (seq_lens[0] + T - 1) / T;
+            const long long nt = tiles / S_all;
             const long long S = static_cast<long long>(c->b) * c->g;
             const long long per = tiles / grid;
             const long long pieces = per > 0 ? (nt - 1 + per - 1) / per + 1 : grid;
@@ -714,8 +675,14 @@ static int decode_impl(mlkv_cache_t c, int layer, const void *K_new, const void 
     DeviceGuard guard(c->device);
     if (cluster_k > 1)   // one length only
         smem += (cluster_k - 1) * var->v->res_bytes;
+    const mlkv::DecodeWindow<true> sliding = {window, sinks};
+    if (window > 0)
+        window_lens(true);
     cudaError_t e = mlkv::launch_decode(*var->v, grid, smem, static_cast<cudaStream_t>(cuda_stream),
-                                        &var->tmap, &var->tmap_rows, p, winp, c->pdl != 0);
+                                        &var->tmap, &var->tmap_rows, p, winp, c->pdl != 0,
+                                        window > 0 ? &sliding : nullptr);
+    if (window > 0)
+        window_lens(false);
     if (e != cudaSuccess)
         return fail_cuda(e, "decode launch");
     if (p.deferred_merge) {
@@ -736,6 +703,18 @@ int mlkv_decode_attention(mlkv_cache_t c, int layer, const void *Q, void *out,
                           const int *seq_lens, void *cuda_stream)
 {
     return decode_impl(c, layer, nullptr, nullptr, Q, out, seq_lens, cuda_stream);
+}
+
+int mlkv_decode_attention_window(mlkv_cache_t c, int layer, const void *Q, void *out,
+                                 const int *seq_lens, int window, int sinks, void *cuda_stream)
+{
+    const int rc = mlkv::check_window(window, sinks);
+    if (rc != MLKV_OK)
+        return rc;
+    if (c != nullptr)
+        mlkv::clamp_window(c->max_seq, &window, &sinks);
+    return decode_impl(c, layer, nullptr, nullptr, Q, out, seq_lens, cuda_stream, 0, nullptr, 0, 1, 0,
+                       window, sinks);
 }
 
 int mlkv_append_decode_attention(mlkv_cache_t c, int layer, const void *K, const void *V,
@@ -1823,34 +1802,151 @@ int mlkv_load_prefix(mlkv_cache_t c, int layer, const void *K, const void *V, in
                         false);
 }
 
-int mlkv_prefill(mlkv_cache_t c, int layer, const void *Q, const void *K, const void *V, void *out,
-                 const int *prompt_lens, int s_max, void *cuda_stream)
+}  // extern "C"
+
+// One layer's causal prefill: see PrefillCall.
+int mlkv::issue_prefill(const PrefillCall &a, cudaStream_t stream)
+{
+    // The queries, position-major [b][s_max][h][d]: boxes of 64 channels x 1 head x 128 positions.
+    static EncodeTiledFn encode = driver_entry<EncodeTiledFn>("cuTensorMapEncodeTiled");
+    if (encode == nullptr)
+        return fail(MLKV_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable from the driver");
+    cudaError_t e;
+    CUtensorMap tmap_q;
+    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(a.d), static_cast<cuuint64_t>(a.h),
+                                static_cast<cuuint64_t>(a.s_max), static_cast<cuuint64_t>(a.b)};
+    const cuuint64_t strides[3] = {static_cast<cuuint64_t>(a.d) * 2,
+                                   static_cast<cuuint64_t>(a.h) * a.d * 2,
+                                   static_cast<cuuint64_t>(a.s_max) * a.h * a.d * 2};
+    const cuuint32_t box[4] = {64u, 1u, 128u, 1u};
+    const cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
+    CUresult r = encode(&tmap_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(a.Q), dims,
+                        strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS)
+        return fail(MLKV_ERR_CUDA, "cuTensorMapEncodeTiled(Q) failed (CUresult %d)",
+                    static_cast<int>(r));
+    // K and V in boxes of 128 positions: an owner layer's prompt where it is, [b][g][s_max][d]; else
+    // the cache (the map of the 128-position decode variant).
+    CUtensorMap tmap_in[2];
+    if (a.direct) {
+        const cuuint64_t kdims[3] = {static_cast<cuuint64_t>(a.d), static_cast<cuuint64_t>(a.s_max),
+                                     static_cast<cuuint64_t>(a.b) * a.g};
+        const cuuint64_t kstrides[2] = {static_cast<cuuint64_t>(a.d) * 2,
+                                        static_cast<cuuint64_t>(a.s_max) * a.d * 2};
+        const cuuint32_t kbox[3] = {64u, 128u, 1u};
+        const void *kv[2] = {a.K, a.V};
+        for (int i = 0; i < 2; ++i) {
+            r = encode(&tmap_in[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(kv[i]),
+                       kdims, kstrides, kbox, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+            if (r != CUDA_SUCCESS)
+                return fail(MLKV_ERR_CUDA, "cuTensorMapEncodeTiled(prompt K/V) failed (CUresult %d)",
+                            static_cast<int>(r));
+        }
+    }
+    static thread_local mlkv::PrefillParams p;
+    p.out = static_cast<__nv_bfloat16 *>(a.out);
+    p.err = a.err;
+    p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(a.d)));
+    p.b = a.b;
+    p.h = a.h;
+    p.g = a.g;
+    p.G = a.h / a.g;
+    p.s_max = a.s_max;
+    p.slot = a.slot;
+    p.window = a.window;
+    p.sinks = a.sinks;
+    p.sm_count = a.sm_count;
+    p.kv_direct = a.direct ? 1 : 0;
+    p.fused_L = p.fused_L1 = 0;
+    const CUtensorMap *tmap_k = a.direct ? &tmap_in[0] : a.tmap_kv;
+    const CUtensorMap *tmap_v = a.direct ? &tmap_in[1] : a.tmap_kv;
+    int max_len = 0;
+    for (int beta = 0; beta < a.b; ++beta) {
+        p.prompt_len[beta] = a.prompt_lens[beta];
+        max_len = std::max(max_len, a.prompt_lens[beta]);
+    }
+    // Work units, those that see the most keys first.  head_dim 64: one query block of one head
+    // per CTA (two CTAs per SM).  head_dim 128: two heads of a group at the same block when the
+    // group size is even, else the blocks 2p and 2p+1 of one head (the unit of block 2p+1).
+    const bool one_tile = a.d == 64;
+    p.head_pairs = (!one_tile && p.G % 2 == 0) ? 1 : 0;
+    const int sels = p.head_pairs ? a.h / 2 : a.h;
+    const int max_blocks = (max_len + 127) / 128;
+    int n = 0;
+    for (int qb = max_blocks - 1; qb >= 0; --qb) {
+        for (int beta = 0; beta < a.b; ++beta) {
+            const int nb = (a.prompt_lens[beta] + 127) / 128;
+            if (qb >= nb || (!one_tile && !p.head_pairs && qb % 2 == 0 && qb != nb - 1))
+                continue;
+            for (int sel = 0; sel < sels; ++sel) {
+                p.units[n] = static_cast<uint32_t>(beta) | (static_cast<uint32_t>(qb) << 10) |
+                             (static_cast<uint32_t>(sel) << 24);
+                if (++n == mlkv::kPrefillMaxUnits) {
+                    p.n_units = n;
+                    if ((e = mlkv::launch_prefill(a.d, &tmap_q, tmap_k, tmap_v, p, stream)) !=
+                        cudaSuccess)
+                        return fail_cuda(e, "prefill launch");
+                    n = 0;
+                }
+            }
+        }
+    }
+    if (n > 0) {
+        p.n_units = n;
+        if ((e = mlkv::launch_prefill(a.d, &tmap_q, tmap_k, tmap_v, p, stream)) != cudaSuccess)
+            return fail_cuda(e, "prefill launch");
+    }
+    return MLKV_OK;
+}
+
+int mlkv::check_prefill_args(const void *Q, const void *out, const int *prompt_lens, int b, int h, int d,
+                             int s_max, int max_seq)
+{
+    if (s_max < 1 || s_max > max_seq)
+        return fail(MLKV_ERR_RANGE, "s_max %d outside [1, %d]", s_max, max_seq);
+    if (Q == nullptr || out == nullptr || !aligned16(Q) || !aligned16(out))
+        return fail(MLKV_ERR_INVALID_ARG, "Q and out must be non-NULL and 16-byte aligned");
+    if (prompt_lens == nullptr)
+        return fail(MLKV_ERR_INVALID_ARG, "prompt_lens must be non-NULL");
+    if (h > kPrefillMaxHeads || s_max > kPrefillMaxBlocks * 128)
+        return fail(MLKV_ERR_UNSUPPORTED, "prefill handles at most %d query heads and %d positions",
+                    kPrefillMaxHeads, kPrefillMaxBlocks * 128);
+    for (int beta = 0; beta < b; ++beta)
+        if (prompt_lens[beta] < 1 || prompt_lens[beta] > s_max)
+            return fail(MLKV_ERR_RANGE, "prompt length %d of sequence %d outside [1, %d]",
+                        prompt_lens[beta], beta, s_max);
+    const size_t qbytes = static_cast<size_t>(b) * s_max * h * d * 2;
+    if (overlap(Q, qbytes, out, qbytes))
+        return fail(MLKV_ERR_INVALID_ARG, "out overlaps Q");
+    return MLKV_OK;
+}
+
+int mlkv::check_window(int window, int sinks)
+{
+    if (window < 0 || sinks < 0)
+        return fail(MLKV_ERR_INVALID_ARG, "window %d and sinks %d must not be negative", window, sinks);
+    return MLKV_OK;
+}
+
+extern "C" {
+
+static int prefill_impl(mlkv_cache_t c, int layer, const void *Q, const void *K, const void *V,
+                        void *out, const int *prompt_lens, int s_max, int window, int sinks,
+                        void *cuda_stream)
 {
     if (c == nullptr)
         return fail(MLKV_ERR_INVALID_ARG, "null cache handle");
     if (layer < 0 || layer >= c->l)
         return fail(MLKV_ERR_INVALID_ARG, "layer %d outside [0, %d)", layer, c->l);
-    if (s_max < 1 || s_max > c->max_seq)
-        return fail(MLKV_ERR_RANGE, "s_max %d outside [1, %d]", s_max, c->max_seq);
-    if (Q == nullptr || out == nullptr || !aligned16(Q) || !aligned16(out))
-        return fail(MLKV_ERR_INVALID_ARG, "Q and out must be non-NULL and 16-byte aligned");
-    if (prompt_lens == nullptr)
-        return fail(MLKV_ERR_INVALID_ARG, "prompt_lens must be non-NULL");
-    if (c->h > mlkv::kPrefillMaxHeads || s_max > mlkv::kPrefillMaxBlocks * 128)
-        return fail(MLKV_ERR_UNSUPPORTED, "prefill handles at most %d query heads and %d positions",
-                    mlkv::kPrefillMaxHeads, mlkv::kPrefillMaxBlocks * 128);
-    int max_len = 0;
-    for (int beta = 0; beta < c->b; ++beta) {
-        if (prompt_lens[beta] < 1 || prompt_lens[beta] > s_max)
-            return fail(MLKV_ERR_RANGE, "prompt length %d of sequence %d outside [1, %d]",
-                        prompt_lens[beta], beta, s_max);
-        max_len = std::max(max_len, prompt_lens[beta]);
-    }
+    int rc = mlkv::check_prefill_args(Q, out, prompt_lens, c->b, c->h, c->d, s_max, c->max_seq);
+    if (rc != MLKV_OK || (rc = mlkv::check_window(window, sinks)) != MLKV_OK)
+        return rc;
+    mlkv::clamp_window(s_max, &window, &sinks);
     const size_t qbytes = static_cast<size_t>(c->b) * s_max * c->h * c->d * 2;
-    const char *qs = static_cast<const char *>(Q);
-    const char *os = static_cast<const char *>(out);
-    if (os < qs + qbytes && qs < os + qbytes)
-        return fail(MLKV_ERR_INVALID_ARG, "out overlaps Q");
     const bool owner = c->owner[layer] == layer;
     if (owner && (K == nullptr || V == nullptr || !aligned16(K) || !aligned16(V)))
         return fail(MLKV_ERR_INVALID_ARG, "K and V must be non-NULL and 16-byte aligned");
@@ -1864,123 +1960,62 @@ int mlkv_prefill(mlkv_cache_t c, int layer, const void *Q, const void *K, const 
         const bool local = on_device(c, K) && on_device(c, V);
         direct = local;
         const size_t kvbytes = static_cast<size_t>(c->b) * c->g * s_max * c->d * 2;
-        auto overlap = [](const void *a, size_t na, const void *b, size_t nb) {
-            const char *x = static_cast<const char *>(a), *y = static_cast<const char *>(b);
-            return x < y + nb && y < x + na;
-        };
         for (const void *kv : {K, V})
             if (overlap(kv, kvbytes, out, qbytes) || overlap(kv, kvbytes, c->cache, c->cache_bytes))
                 direct = false;
         if (overlap(Q, qbytes, c->cache, c->cache_bytes))
             direct = false;
         if (!direct) {
-            const int rc = store_prefix(c, layer, K, V, s_max, stream, local, false);
-            if (rc != MLKV_OK)
+            if ((rc = store_prefix(c, layer, K, V, s_max, stream, local, false)) != MLKV_OK)
                 return rc;
         }
     }
-    cudaError_t e;
-    if (!c->prefill_ready) {
-        if ((e = mlkv::prepare_prefill(c->d)) != cudaSuccess)
+    const int ready = window > 0 ? 2 : 1;   // the two kernels' bits
+    if (!(c->prefill_ready & ready)) {
+        const cudaError_t e = mlkv::prepare_prefill(c->d, window > 0);
+        if (e != cudaSuccess)
             return fail_cuda(e, "cudaFuncSetAttribute(prefill)");
-        c->prefill_ready = 1;
+        c->prefill_ready |= ready;
     }
-    // The queries, position-major [b][s_max][h][d]: boxes of 64 channels x 1 head x 128 positions.
-    static EncodeTiledFn encode = driver_entry<EncodeTiledFn>("cuTensorMapEncodeTiled");
-    if (encode == nullptr)
-        return fail(MLKV_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable from the driver");
-    CUtensorMap tmap_q;
-    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(c->d), static_cast<cuuint64_t>(c->h),
-                                static_cast<cuuint64_t>(s_max), static_cast<cuuint64_t>(c->b)};
-    const cuuint64_t strides[3] = {static_cast<cuuint64_t>(c->d) * 2,
-                                   static_cast<cuuint64_t>(c->h) * c->d * 2,
-                                   static_cast<cuuint64_t>(s_max) * c->h * c->d * 2};
-    const cuuint32_t box[4] = {64u, 1u, 128u, 1u};
-    const cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
-    CUresult r = encode(&tmap_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(Q), dims,
-                        strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS)
-        return fail(MLKV_ERR_CUDA, "cuTensorMapEncodeTiled(Q) failed (CUresult %d)",
-                    static_cast<int>(r));
-    // K and V in boxes of 128 positions: an owner layer's prompt where it is, [b][g][s_max][d]; else
-    // the cache (the map of the 128-position decode variant).
-    CUtensorMap tmap_in[2];
-    if (direct) {
-        const cuuint64_t kdims[3] = {static_cast<cuuint64_t>(c->d), static_cast<cuuint64_t>(s_max),
-                                     static_cast<cuuint64_t>(c->b) * c->g};
-        const cuuint64_t kstrides[2] = {static_cast<cuuint64_t>(c->d) * 2,
-                                        static_cast<cuuint64_t>(s_max) * c->d * 2};
-        const cuuint32_t kbox[3] = {64u, 128u, 1u};
-        const void *kv[2] = {K, V};
-        for (int i = 0; i < 2; ++i) {
-            r = encode(&tmap_in[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(kv[i]),
-                       kdims, kstrides, kbox, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-            if (r != CUDA_SUCCESS)
-                return fail(MLKV_ERR_CUDA, "cuTensorMapEncodeTiled(prompt K/V) failed (CUresult %d)",
-                            static_cast<int>(r));
-        }
-    }
-    const CUtensorMap *tmap_kv = nullptr;
+    mlkv::PrefillCall a = {};
     for (auto &v : c->variants)
         if (v.v->tile_tokens == 128)
-            tmap_kv = &v.tmap;
-    if (tmap_kv == nullptr)
+            a.tmap_kv = &v.tmap;
+    if (a.tmap_kv == nullptr)
         return fail(MLKV_ERR_UNSUPPORTED, "no 128-position cache map for d=%d", c->d);
-
-    static thread_local mlkv::PrefillParams p;
-    p.out = static_cast<__nv_bfloat16 *>(out);
-    p.err = c->err;
-    p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(c->d)));
-    p.b = c->b;
-    p.h = c->h;
-    p.g = c->g;
-    p.G = c->G;
-    p.s_max = s_max;
-    p.slot = c->slot[layer];
-    p.sm_count = c->sm_count;
-    p.kv_direct = direct ? 1 : 0;
-    p.fused_L = p.fused_L1 = 0;
-    const CUtensorMap *tmap_k = direct ? &tmap_in[0] : tmap_kv;
-    const CUtensorMap *tmap_v = direct ? &tmap_in[1] : tmap_kv;
-    for (int beta = 0; beta < c->b; ++beta)
-        p.prompt_len[beta] = prompt_lens[beta];
-    // Work units, those that see the most keys first.  head_dim 64: one query block of one head
-    // per CTA (two CTAs per SM).  head_dim 128: two heads of a group at the same block when the
-    // group size is even, else the blocks 2p and 2p+1 of one head (the unit of block 2p+1).
-    const bool one_tile = c->d == 64;
-    p.head_pairs = (!one_tile && c->G % 2 == 0) ? 1 : 0;
-    const int sels = p.head_pairs ? c->h / 2 : c->h;
-    const int max_blocks = (max_len + 127) / 128;
-    int n = 0;
-    for (int qb = max_blocks - 1; qb >= 0; --qb) {
-        for (int beta = 0; beta < c->b; ++beta) {
-            const int nb = (prompt_lens[beta] + 127) / 128;
-            if (qb >= nb || (!one_tile && !p.head_pairs && qb % 2 == 0 && qb != nb - 1))
-                continue;
-            for (int sel = 0; sel < sels; ++sel) {
-                p.units[n] = static_cast<uint32_t>(beta) | (static_cast<uint32_t>(qb) << 10) |
-                             (static_cast<uint32_t>(sel) << 24);
-                if (++n == mlkv::kPrefillMaxUnits) {
-                    p.n_units = n;
-                    if ((e = mlkv::launch_prefill(c->d, &tmap_q, tmap_k, tmap_v, p, stream)) !=
-                        cudaSuccess)
-                        return fail_cuda(e, "prefill launch");
-                    n = 0;
-                }
-            }
-        }
-    }
-    if (n > 0) {
-        p.n_units = n;
-        if ((e = mlkv::launch_prefill(c->d, &tmap_q, tmap_k, tmap_v, p, stream)) != cudaSuccess)
-            return fail_cuda(e, "prefill launch");
-    }
+    a.Q = Q;
+    a.K = K;
+    a.V = V;
+    a.out = out;
+    a.prompt_lens = prompt_lens;
+    a.err = c->err;
+    a.b = c->b;
+    a.h = c->h;
+    a.g = c->g;
+    a.d = c->d;
+    a.s_max = s_max;
+    a.slot = c->slot[layer];
+    a.sm_count = c->sm_count;
+    a.direct = direct;
+    a.window = window;
+    a.sinks = sinks;
+    if ((rc = mlkv::issue_prefill(a, stream)) != MLKV_OK)
+        return rc;
     // Sec. 3: only an owner layer stores K/V -- the prompt's, at positions [0, s_max).
     return direct ? store_prefix(c, layer, K, V, s_max, stream, true, true) : MLKV_OK;
+}
+
+int mlkv_prefill(mlkv_cache_t c, int layer, const void *Q, const void *K, const void *V, void *out,
+                 const int *prompt_lens, int s_max, void *cuda_stream)
+{
+    return prefill_impl(c, layer, Q, K, V, out, prompt_lens, s_max, 0, 0, cuda_stream);
+}
+
+int mlkv_prefill_window(mlkv_cache_t c, int layer, const void *Q, const void *K, const void *V,
+                        void *out, const int *prompt_lens, int s_max, int window, int sinks,
+                        void *cuda_stream)
+{
+    return prefill_impl(c, layer, Q, K, V, out, prompt_lens, s_max, window, sinks, cuda_stream);
 }
 
 int mlkv_decode_block_fused(mlkv_cache_t c, int owner_layer, const void *Q, void *out,

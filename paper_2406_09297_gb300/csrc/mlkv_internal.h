@@ -21,6 +21,40 @@ enum : int {
 // Layers one multi-layer decode launch can cover (DecodeParams::ml_layers).
 constexpr int kMaxStepLayers = 128;
 
+// What one sequence of L positions shows its newest query, in tiles of T positions: all of it, or (a
+// window that leaves a gap behind the sinks) ns tiles from position 0 on, of which the first `sinks`
+// positions are visible, and then tiles from the window's first position, rounded down to `align`, on.
+// Tile tt covers positions from tt T (+ skip from tile ns on).
+struct VisibleTiles {
+    int nt, ns, skip, first;   // first: the window's first position (0 without a gap)
+};
+__host__ __device__ inline VisibleTiles visible_tiles(int L, int window, int sinks, int T, int align)
+{
+    VisibleTiles v;
+    v.ns = v.skip = v.first = 0;
+    int len = L;
+    if (window > 0 && L - window > sinks) {
+        v.first = L - window;
+        v.ns = (sinks + T - 1) / T;
+        v.skip = v.first / align * align - v.ns * T;
+        len = L - v.skip;
+    }
+    v.nt = (len + T - 1) / T;
+    return v;
+}
+// The length whose plain tiling has the same number of tiles (combine_kernel's view).
+__host__ __device__ inline int visible_len(int L, const VisibleTiles &v) { return L - v.skip; }
+
+// Sliding window of a decode launch (window > 0), for the kernel's windowed instantiations; the others
+// take the empty one.
+template <bool kWin>
+struct DecodeWindow {
+    int window, sinks;
+};
+template <>
+struct DecodeWindow<false> {
+};
+
 // Split-KV decode of one layer.  Passed by value (__grid_constant__), so a launch needs no
 // device-side metadata and is stream-ordered and graph-capturable by construction.
 struct DecodeParams {
@@ -111,6 +145,8 @@ struct PrefillParams {
     float scale_log2;         // log2(e) / sqrt(D)
     int b, h, g, G, s_max, slot, n_units, head_pairs;
     int sm_count;             // the launch's persistent CTAs: one or two per SM, at most n_units
+    // Prefill: a query at position t sees u <= t with u < sinks or u > t - window (0: every u <= t).
+    int window, sinks;
     int kv_direct;            // prefill: K and V are the prompt's own tensors (an owner layer), each
                               // under a map of its own; 0: the cache slot's, under one map
     // Cross-layer fused decode (mlkv_decode_block_fused, and mlkv_decode_step's fused form): every
@@ -140,7 +176,7 @@ struct PrefillParams {
 // Dynamic shared memory of the prefill kernel; sets its limit (once per device); launches it with
 // programmatic dependent launch on `stream`.
 size_t prefill_smem_bytes(int head_dim);
-cudaError_t prepare_prefill(int head_dim);
+cudaError_t prepare_prefill(int head_dim, bool windowed);
 cudaError_t launch_prefill(int head_dim, const CUtensorMap *tmap_q, const CUtensorMap *tmap_k,
                            const CUtensorMap *tmap_v, const PrefillParams &p, cudaStream_t stream);
 // Fused decode forms (head_dim 64 with L * G <= 128 may take either one-tile form; otherwise the
@@ -196,6 +232,7 @@ struct DecodeVariant {
     int tc = 0;               // 1: decode_tc_kernel (tcgen05, TMEM), 0: decode_kernel (mma.sync)
     size_t raw2_bytes = 0;    // of smem_bytes: the second raw-sum buffer, which a launch may do without
     int min_blocks = 1;       // CTAs per SM the variant is built for
+    const void *win_fn = nullptr;   // the kernel with a sliding window (same resources), if built
 };
 
 // The tcgen05 variants (mlkv_decode_tc.cu).
@@ -226,12 +263,14 @@ cudaError_t prepare_decode_variant(const DecodeVariant &v, size_t max_smem);
 
 // pdl: launch with programmatic stream serialization (the kernel's prologue may overlap the
 // previous kernel of the stream; it waits on griddepcontrol.wait before touching global memory).
+// win: the sliding window of v.win_fn, which then runs (p's lengths are the sequences' own, its tiles
+// those of visible_tiles).
 // tmap: the cache with boxes of {64 channels, tile_tokens positions}; tmap_rows: the same tensor
 // with boxes of 64 positions, used for a segment's last tile when it is only partly visible.
 cudaError_t launch_decode(const DecodeVariant &v, int grid, size_t smem, cudaStream_t stream,
                           const CUtensorMap *tmap, const CUtensorMap *tmap_rows,
                           const DecodeParams &p, const cudaAccessPolicyWindow *window,
-                          bool pdl = true);
+                          bool pdl = true, const DecodeWindow<true> *win = nullptr);
 
 // Default positions per tile of the mma.sync decode kernel for a launch over `segments`
 // (sequence, KV head) pairs of mean length mean_len.  Longer tiles move more bytes per TMA

@@ -167,12 +167,13 @@ constexpr uint32_t kOnesBf16x2 = 0x3f803f80u;
 // Measured on GB300 (layer calls, 16-row form -> this one): 32 layers of 8 uneven sequences, 8 KV
 // heads of 128 with 4 heads each 413 -> 404 us; 12 layers of 128 uneven sequences, 4 KV heads of 64
 // with 3 heads each 602 -> 579 us.
-template <int D, int T, int STAGES, int NCW, bool kT>
+template <int D, int T, int STAGES, int NCW, bool kT, bool kWin = false>
 __global__ void __launch_bounds__(Plan<D, T, STAGES, NCW, kT>::kThreads,
                                   Plan<D, T, STAGES, NCW, kT>::kMinBlocks)
     decode_kernel(const __grid_constant__ CUtensorMap tmap,
                   const __grid_constant__ CUtensorMap tmap_rows,
-                  const __grid_constant__ DecodeParams p)
+                  const __grid_constant__ DecodeParams p,
+                  const __grid_constant__ DecodeWindow<kWin> win)
 {
     using PL = Plan<D, T, STAGES, NCW, kT>;
     constexpr int TW = PL::kTW;
@@ -212,15 +213,15 @@ __global__ void __launch_bounds__(Plan<D, T, STAGES, NCW, kT>::kThreads,
         tile_lo = 0;
         tile_hi = 0;
         for (int k = 0;; ++k) {
-            const int r = TileWalk<T>::ml_rank(p, k);
+            const int r = TileWalk<T, kWin>::ml_rank(p, k);
             if (r < 0)
                 break;
             const int L = p.uniform_len > 0
                               ? p.uniform_len
-                              : p.seq_len[p.tile_start[TileWalk<T>::ml_seq_pos(p, r)]];
+                              : p.seq_len[p.tile_start[TileWalk<T, kWin>::ml_seq_pos(p, r)]];
             if (p.ml_chunks > 1) {
                 int a, b;
-                TileWalk<T>::ml_chunk(p, (L + T - 1) / T, r % p.ml_chunks, a, b);
+                TileWalk<T, kWin>::ml_chunk(p, (L + T - 1) / T, r % p.ml_chunks, a, b);
                 tile_hi += b - a;
             } else {
                 tile_hi += (L + T - 1) / T;
@@ -247,13 +248,13 @@ __global__ void __launch_bounds__(Plan<D, T, STAGES, NCW, kT>::kThreads,
     // or HBM, 2 to 8 copies outstanding), while copies from different lanes proceed side by side;
     // so the copies of a tile -- K and V boxes, query rows -- go out from different lanes, and
     // successive stages from different groups of lanes.  Lane 0 first announces the stage's bytes.
-    auto issue_tile = [&](const TileWalk<T> &w, int s, bool with_q) {
+    auto issue_tile = [&](const TileWalk<T, kWin> &w, int s, bool with_q) {
         const uint32_t fb = bar_full + 8 * s;
         const uint32_t qbytes = static_cast<uint32_t>(p.G) * D * 2;
         // A segment's last tile may be partly visible: only its boxes of 64 positions that
         // hold visible rows are fetched (the rest of the stage keeps stale rows, which the
         // consumers mask in S and zero in V).
-        const int vis = w.L - w.tt * T;
+        const int vis = w.left();
         const int nbox = vis < T ? (vis + 63) / 64 : 0;
         const uint32_t kv_bytes =
             nbox > 0 ? static_cast<uint32_t>(nbox) * 64u * D * 2u * 2u : PL::kStageBytes;
@@ -265,7 +266,7 @@ __global__ void __launch_bounds__(Plan<D, T, STAGES, NCW, kT>::kThreads,
         const int mine = (lane - s * 2 * PL::kSub) & 31;
         const int zk = ((slot_of(w.layer) * 2 + 0) * p.b + w.beta) * p.g + w.j;
         const int zv = zk + p.b * p.g;
-        const int y = w.tt * T;
+        const int y = w.pos();
         const uint32_t kdst = sbase + s * PL::kStageBytes;
         const uint32_t vdst = kdst + PL::kTileBytes;
         if (mine < per_tile) {
@@ -311,8 +312,8 @@ __global__ void __launch_bounds__(Plan<D, T, STAGES, NCW, kT>::kThreads,
         }
         __syncwarp();
         if (pre_tile && p.uniform_len > 0 && tile_lo < tile_hi) {
-            TileWalk<T> w0;
-            w0.init(p, s_len, s_start, tile_lo);
+            TileWalk<T, kWin> w0;
+            w0.init(p, s_len, s_start, tile_lo, win);
             if (w0.tt != w0.nt - 1 || p.newest_ready) {   // not a newest row still to wait for
                 issue_tile(w0, 0, false);
                 pre_issued = true;
@@ -345,9 +346,9 @@ __global__ void __launch_bounds__(Plan<D, T, STAGES, NCW, kT>::kThreads,
     if (p.cluster_k > 1)
         cluster_arrive();   // this CTA's barriers exist; waited on before any remote access
     // The tile walk reads only the parameters and the shared tables: set it up before the wait.
-    TileWalk<T> wk;
+    TileWalk<T, kWin> wk;
     if (tile_lo < tile_hi)
-        wk.init(p, s_len, s_start, tile_lo);
+        wk.init(p, s_len, s_start, tile_lo, win);
     // Everything above overlaps the previous kernels' tails.  Normally global memory is touched
     // only after the dependency wait.  When the previous kernels still running are this library's
     // decodes of the preceding layers (p.early_fetch, inside mlkv_decode_step), they write nothing
@@ -383,7 +384,7 @@ __global__ void __launch_bounds__(Plan<D, T, STAGES, NCW, kT>::kThreads,
         int issued = pre_issued ? 1 : 0;
         int tile = tile_lo + issued;
         if (pre_issued)
-            wk.next(p, s_len, s_start);
+            wk.next(p, s_len, s_start, win);
         bool waited = !early;
         if (!early)
             grid_dependency_wait();
@@ -419,7 +420,7 @@ __global__ void __launch_bounds__(Plan<D, T, STAGES, NCW, kT>::kThreads,
             // A later piece starts here: its query rows come with the tile.
             issue_tile(wk, s, wk.tt == wk.t0 && tile != tile_lo);
             ++issued;
-            wk.next(p, s_len, s_start);
+            wk.next(p, s_len, s_start, win);
         }
         // No copy may still be in flight when the CTA exits.
         if (lane == 0) {
@@ -695,7 +696,7 @@ __global__ void __launch_bounds__(Plan<D, T, STAGES, NCW, kT>::kThreads,
                 atomicOr(p.err, kErrWaitFull);
             }
             const int row0 = warp * TW;                 // this warp's first row in the tile
-            const int valid = L - (wk.tt * T + row0);   // visible rows in this warp's slice
+            const int valid = wk.left() - row0;   // visible rows in this warp's slice
             if (!flags[0] && valid > 0) {
                 const uint32_t kt = sbase + s * PL::kStageBytes;
                 const uint32_t vt = kt + PL::kTileBytes;
@@ -906,7 +907,7 @@ __global__ void __launch_bounds__(Plan<D, T, STAGES, NCW, kT>::kThreads,
             __syncwarp();
             if (lane == 0)
                 mbar_arrive(bar_empty + 8 * s);
-            wk.next(p, s_len, s_start);
+            wk.next(p, s_len, s_start, win);
         }
 
         // ---------------- end of piece: every warp's raw sums to the piece's buffer -------------
@@ -1335,7 +1336,8 @@ constexpr DecodeVariant make_variant()
     return DecodeVariant{D, T, STAGES, PL::kThreads, static_cast<size_t>(PL::kAlloc),
                          PL::kClusterInRaw ? 0 : static_cast<size_t>(PL::kResBytes),
                          reinterpret_cast<const void *>(&decode_kernel<D, T, STAGES, NCW, kT>), 0,
-                         static_cast<size_t>((PL::kMaxRawBufs - 1) * PL::kRawBytes), PL::kMinBlocks};
+                         static_cast<size_t>((PL::kMaxRawBufs - 1) * PL::kRawBytes), PL::kMinBlocks,
+                         reinterpret_cast<const void *>(&decode_kernel<D, T, STAGES, NCW, kT, true>)};
 }
 
 // (head_dim, positions per tile, ring stages, consumer warps) for groups of more than 8 heads, and
@@ -1376,13 +1378,20 @@ cudaError_t prepare_decode_variant(const DecodeVariant &v, size_t max_smem)
         want = max_smem;
     if (v.smem_bytes > want)
         return cudaErrorInvalidValue;
+    if (v.win_fn != nullptr) {
+        const cudaError_t e = cudaFuncSetAttribute(
+            v.win_fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(want));
+        if (e != cudaSuccess)
+            return e;
+    }
     return cudaFuncSetAttribute(v.fn, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 static_cast<int>(want));
 }
 
 cudaError_t launch_decode(const DecodeVariant &v, int grid, size_t smem, cudaStream_t stream,
                           const CUtensorMap *tmap, const CUtensorMap *tmap_rows,
-                          const DecodeParams &p, const cudaAccessPolicyWindow *window, bool pdl)
+                          const DecodeParams &p, const cudaAccessPolicyWindow *window, bool pdl,
+                          const DecodeWindow<true> *win)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(grid));
@@ -1410,9 +1419,12 @@ cudaError_t launch_decode(const DecodeVariant &v, int grid, size_t smem, cudaStr
     }
     cfg.attrs = attr;
     cfg.numAttrs = na;
+    DecodeWindow<false> none;
     void *args[] = {const_cast<CUtensorMap *>(tmap), const_cast<CUtensorMap *>(tmap_rows),
-                    const_cast<DecodeParams *>(&p)};
-    return cudaLaunchKernelExC(&cfg, v.fn, args);
+                    const_cast<DecodeParams *>(&p),
+                    win != nullptr ? static_cast<void *>(const_cast<DecodeWindow<true> *>(win))
+                                   : static_cast<void *>(&none)};
+    return cudaLaunchKernelExC(&cfg, win != nullptr ? v.win_fn : v.fn, args);
 }
 
 int max_pieces_per_segment(const DecodeParams &p, int T, int grid)

@@ -59,6 +59,10 @@
 //   4 x 2048 x 32 heads, head_dim 128             313.8   240.6   215 us
 //   32 prompts of 1 to 777 positions, head_dim 64 103.7    83.0    54.2 us
 //
+// Sliding window with sinks (kWin): a unit's key tiles are the sinks' and those from the first one its
+// first query's window reaches on; the rest is never loaded.  Rows mask what lies before their own
+// window in the one or two tiles of its edge.
+//
 // The diagonal tile masks keys after the query; keys past the prompt's end only meet such masked
 // scores, and their V rows are zeroed in shared memory so that 0 * V stays 0.
 //
@@ -176,11 +180,19 @@ struct Unit {
     int n_a, n_b;         // key tiles of query tiles A (0: no tile A) and B, n_a <= n_b
     int qb_b;             // prefill: tile B's query block
     int head_a, head_b, j;
+    int ns, skip;         // sliding window: key tiles of the sinks, and blocks left out behind them
     int zk, zv;           // rows of the K and V tensor maps: (slot, sequence, KV head)
     bool has_end;         // the unit holds the sequence's last key tile
 };
 
-template <bool kFused, int kTiles>
+// Block of 128 positions that the unit's key tile t covers.
+template <bool kWin>
+__device__ __forceinline__ int key_block(const Unit &x, int t)
+{
+    return x.kt0 + t + (kWin && t >= x.ns ? x.skip : 0);
+}
+
+template <bool kFused, int kTiles, bool kWin>
 __device__ __forceinline__ Unit unit_of(const PrefillParams &p, int i)
 {
     Unit x;
@@ -188,6 +200,7 @@ __device__ __forceinline__ Unit unit_of(const PrefillParams &p, int i)
     x.beta = static_cast<int>(u & 0x3FFu);
     const int sel = static_cast<int>(u >> 24);
     x.S = p.prompt_len[x.beta];
+    x.ns = x.skip = 0;
     if (kFused) {
         // every query row sees positions [0, S); the unit takes key tiles [kt0, kt0 + n_b)
         const int n_kt = (x.S + 127) / 128;
@@ -204,8 +217,16 @@ __device__ __forceinline__ Unit unit_of(const PrefillParams &p, int i)
         x.chunk = x.blk = x.kt0 = 0;
         x.has_end = true;
         x.qb_b = static_cast<int>((u >> 10) & 0x3FFFu);
-        x.n_b = x.qb_b + 1;
-        x.n_a = kTiles == 1 ? 0 : p.head_pairs ? x.n_b : ((x.qb_b & 1) ? x.qb_b : 0);
+        if (kWin) {
+            // The sinks' blocks, then those from the first one that the unit's first query sees
+            // (tile A's where there is one: tile B may find its first block masked throughout).
+            const bool pair = kTiles == 2 && !p.head_pairs && (x.qb_b & 1);
+            const int q_first = (x.qb_b - (pair ? 1 : 0)) * 128;
+            x.ns = (p.sinks + 127) / 128;
+            x.skip = max(0, max(0, q_first - p.window + 1) / 128 - x.ns);
+        }
+        x.n_b = x.qb_b + 1 - x.skip;
+        x.n_a = kTiles == 1 ? 0 : p.head_pairs ? x.n_b : ((x.qb_b & 1) ? x.qb_b - x.skip : 0);
         x.head_a = p.head_pairs ? 2 * sel : sel;
         x.head_b = p.head_pairs ? 2 * sel + 1 : sel;
         x.j = x.head_b / p.G;   // Eq. 15
@@ -228,7 +249,7 @@ __device__ __forceinline__ int unit_index(const PrefillParams &p, int k)
     return i < p.n_units ? i : -1;
 }
 
-template <int D, bool kFused, int kForm>
+template <int D, bool kFused, int kForm, bool kWin>
 __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                                   PrefillPlan<D, kForm>::kMinBlocks)
     prefill_kernel(const __grid_constant__ CUtensorMap tmap_q,
@@ -397,7 +418,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
 #pragma unroll
             for (int sub = 0; sub < PL::kSub; ++sub)
                 tma_load_3d(sbase + PL::kRing + s * PL::kTileBytes + sub * 16384,
-                            (k & 1) ? &tmap_v : &tmap_k, fb, sub * 64, ((k >> 1) + x.kt0) * 128,
+                            (k & 1) ? &tmap_v : &tmap_k, fb, sub * 64, key_block<kWin>(x, k >> 1) * 128,
                             (k & 1) ? x.zv : x.zk);
             ++idx;
             return true;
@@ -433,7 +454,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                                     x.blk * p.fused_L + (g ? 0 : p.fused_L1));
                     else
                         tma_load_4d(d, &tmap_q, qbar, sub * 64, g ? x.head_b : x.head_a,
-                                    (g ? x.qb_b : x.n_a - 1) * 128, x.beta);
+                                    (g ? x.qb_b : x.n_a - 1 + x.skip) * 128, x.beta);
                 }
             ++uc;
             return true;
@@ -444,7 +465,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                 const int i = unit_index(p, n);
                 if (i < 0)
                     break;
-                const Unit x = unit_of<kFused, PL::kTiles>(p, i);
+                const Unit x = unit_of<kFused, PL::kTiles, kWin>(p, i);
                 const int n_idx = 2 * x.n_b;
                 int k = 0;
                 if (n == 0 && early && !q_early) {
@@ -546,7 +567,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                 const int i = unit_index(p, n);
                 if (i < 0)
                     break;
-                const Unit x = unit_of<kFused, PL::kTiles>(p, i);
+                const Unit x = unit_of<kFused, PL::kTiles, kWin>(p, i);
                 const int qb = n % NQ;
                 const uint64_t dq = dq0 + static_cast<uint32_t>(qb * PL::kTiles) * kSlot;
                 if (PL::kPSep && do_s) {
@@ -676,7 +697,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
             // The CTA's only unit: nothing to compute before its queries, so every softmax warp
             // loads, one round trip over the link (by the last warp alone, two: 64 sequences of
             // 2,048 tokens end to end 34.5 us a step, now 32.9).
-            load_q_host(unit_of<kFused, PL::kTiles>(p, unit_index(p, 0)), 0, threadIdx.x,
+            load_q_host(unit_of<kFused, PL::kTiles, kWin>(p, unit_index(p, 0)), 0, threadIdx.x,
                         std::integral_constant<int, 32 * PL::kSoftWarps>{},
                         std::integral_constant<int, 4>{});
             fence_proxy_async_smem();
@@ -691,13 +712,13 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
             const int i = unit_index(p, n);
             if (i < 0 || (!kSplit && __any_sync(0xffffffffu, flags[0])))
                 break;
-            const Unit x = unit_of<kFused, PL::kTiles>(p, i);
+            const Unit x = unit_of<kFused, PL::kTiles, kWin>(p, i);
             const int qb = n % NQ;
             const int n_g = grp ? x.n_b : x.n_a;
-            const int q0 = (x.kt0 + n_g - 1) * 128;       // first position of the unit's last tile
+            const int q0 = (x.kt0 + n_g - 1 + x.skip) * 128;   // first position of the unit's last tile
             // The prompt's last block holds keys past its end; the first tile to reach it zeroes
             // them.
-            const bool zero_v = n_g > 0 && (kFused ? x.has_end : n_g == (x.S + 127) / 128) &&
+            const bool zero_v = n_g > 0 && (kFused ? x.has_end : n_g + x.skip == (x.S + 127) / 128) &&
                                 (grp == 0 || x.n_a != x.n_b);
             uint8_t *q_slot = smem + PL::kQ + (qb * PL::kTiles + sg) * PL::kTileBytes;
             float m_run = NEG_INF, l_run = 0.f;
@@ -709,6 +730,10 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                         mbar_arrive(bar_empty + 8 * ((2 * (kb + t) - 1) % R));   // V_{t-1}
                 }
                 const bool diag = t == n_g - 1 && x.has_end;
+                // Sliding window: some of the tile's keys, past the sinks, lie before some row's
+                // window.
+                const int k0 = kWin ? key_block<kWin>(x, t) * 128 : 0;
+                const bool behind = kWin && k0 + 128 > p.sinks && k0 <= q0 + 127 - p.window;
                 // This tile's scores and the row's maximum, which the load returns with them.
                 float sv[4][32], mx[4];
                 uint32_t w[2][32];
@@ -736,7 +761,24 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                                                    (((c & 7) ^ (r & 7)) << 4)) = make_uint4(0, 0, 0, 0);
                     fence_proxy_async_smem();
                 }
-                if (diag) {
+                if (kWin && (diag || behind)) {
+                    // Keys [0, hi) of the tile that are sinks (below lo_s) or in the window (from
+                    // lo_w on) are visible; a row may see none of a tile.
+                    const int hi = diag ? r + 1 : 128;
+                    const int lo_s = p.sinks - k0, lo_w = q0 + r + 1 - p.window - k0;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        mx[c] = NEG_INF;
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) {
+                            const int key = c * 32 + k;
+                            if (key >= hi || (key >= lo_s && key < lo_w))
+                                sv[c][k] = NEG_INF;
+                            mx[c] = fmaxf(mx[c], sv[c][k]);
+                        }
+                    }
+                }
+                if (!kWin && diag) {
                     // Keys [0, lim) of the tile are visible: up to the sequence's end (fused
                     // decode) or to the query's own position (causal mask); the maximum is
                     // taken again over those.
@@ -758,7 +800,9 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                 const bool raise = (m_run == NEG_INF) || (m_tile > m_run + 8.f);
                 if (__any_sync(0xffffffffu, raise)) {
                     const float m_new = raise ? fmaxf(m_run, m_tile) : m_run;
-                    const float alpha = fast_exp2(m_run - m_new);   // 0 while nothing is summed
+                    // 0 while nothing is summed; a row without a visible key yet keeps its zeros
+                    const float alpha =
+                        kWin && m_new == NEG_INF ? 1.f : fast_exp2(m_run - m_new);
                     if (t > wg) {
                         // Rescale this row of O once the previous tile's product has landed.
                         if (PL::kPSep)
@@ -837,7 +881,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
             // during the loop.
             int i_out = i;
             asm volatile("" : "+r"(i_out));
-            const Unit y = unit_of<kFused, PL::kTiles>(p, i_out);
+            const Unit y = unit_of<kFused, PL::kTiles, kWin>(p, i_out);
             // The unit's last product, and with it the last reader of its last V.
             const int n_mine = kSplit ? (n_g - wg + 1) / 2 : n_g;   // this warpgroup's tiles
             if (n_mine > 0) {
@@ -1000,7 +1044,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                 const int i = unit_index(p, n);
                 if (i < 0)
                     break;
-                const Unit x = unit_of<kFused, PL::kTiles>(p, i);
+                const Unit x = unit_of<kFused, PL::kTiles, kWin>(p, i);
                 const int qb = n % NQ;
                 int ok = 1;
                 if (lane == 0 && n >= NQ && !flags[0] &&
@@ -1156,10 +1200,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 3) combine_fused_kernel(con
             pack_bf16x2(acc[e] * inv, acc[e + 1] * inv);
 }
 
-template <int D, bool kFused, int kForm>
+template <int D, bool kFused, int kForm, bool kWin = false>
 const void *prefill_fn()
 {
-    return reinterpret_cast<const void *>(&prefill_kernel<D, kFused, kForm>);
+    return reinterpret_cast<const void *>(&prefill_kernel<D, kFused, kForm, kWin>);
 }
 
 // The forms built: prefill at head_dim 64 with one query tile per CTA, at 128 with two; the fused
@@ -1188,8 +1232,11 @@ size_t smem_of(int head_dim, int form)
                       [](auto pl) { return static_cast<size_t>(decltype(pl)::kAlloc); });
 }
 
-const void *kernel_fn(int head_dim, bool fused, int form)
+const void *kernel_fn(int head_dim, bool fused, int form, bool windowed)
 {
+    if (windowed)
+        return head_dim == 64 ? prefill_fn<64, false, kOneTile, true>()
+                              : prefill_fn<128, false, kTwoTiles, true>();
     if (fused) {
         if (head_dim == 64)
             return form == kOneDeep   ? prefill_fn<64, true, kOneDeep>()
@@ -1218,7 +1265,7 @@ cudaError_t launch(int head_dim, bool fused, int form, const CUtensorMap *tmap_q
     cfg.numAttrs = 1;
     void *args[] = {const_cast<CUtensorMap *>(tmap_q), const_cast<CUtensorMap *>(tmap_k),
                     const_cast<CUtensorMap *>(tmap_v), const_cast<PrefillParams *>(&p)};
-    return cudaLaunchKernelExC(&cfg, kernel_fn(head_dim, fused, form), args);
+    return cudaLaunchKernelExC(&cfg, kernel_fn(head_dim, fused, form, !fused && p.window > 0), args);
 }
 
 // The prefill form of a head_dim; a fused-decode form valid for the head_dim.
@@ -1232,10 +1279,10 @@ size_t prefill_smem_bytes(int head_dim) { return smem_of(head_dim, prefill_form(
 // The warpgroups' register split (setmaxnreg) adds up to the registers the block is launched with;
 // a kernel built with another per-thread count would wait forever in setmaxnreg.inc, so it is
 // refused here instead of launched.
-cudaError_t prepare(int head_dim, bool fused, int form)
+cudaError_t prepare(int head_dim, bool fused, int form, bool windowed)
 {
     cudaFuncAttributes fa;
-    const void *fn = kernel_fn(head_dim, fused, form);
+    const void *fn = kernel_fn(head_dim, fused, form, windowed);
     cudaError_t e = cudaFuncGetAttributes(&fa, fn);
     if (e != cudaSuccess)
         return e;
@@ -1245,14 +1292,14 @@ cudaError_t prepare(int head_dim, bool fused, int form)
                                 static_cast<int>(smem_of(head_dim, form)));
 }
 
-cudaError_t prepare_prefill(int head_dim)
+cudaError_t prepare_prefill(int head_dim, bool windowed)
 {
-    return prepare(head_dim, false, prefill_form(head_dim));
+    return prepare(head_dim, false, prefill_form(head_dim), windowed);
 }
 
 cudaError_t prepare_fused(int head_dim, int form)
 {
-    return prepare(head_dim, true, fused_form(head_dim, form));
+    return prepare(head_dim, true, fused_form(head_dim, form), false);
 }
 
 cudaError_t launch_prefill(int head_dim, const CUtensorMap *tmap_q, const CUtensorMap *tmap_k,

@@ -1,0 +1,313 @@
+// Storing into and reading back the 4-bit KV cache (layout and values: mlkv_q4.h).
+//
+//   s = bf16(max |x| / 7) over 32 channels, q = the whole number nearest to x / s, halves away from
+//   zero.
+//
+// x and s have 8-bit significands, so x / s is a half exactly or at least 2^-10 away from one (their
+// quotient's distance from n + 1/2 is a multiple of 1 / (2 S), S the scale's significand, shifted by
+// at most the quotient's own exponent).  x times the approximate reciprocal of s, raised by 2^-16 of
+// itself, is therefore on the right side of every half; the sum with 1.5 2^23 + 8 rounds it and leaves
+// the code in the low bits: one multiply-add a channel.  Likewise max |x| times fp32(1/7) rounds to the
+// same bf16 as the exact quotient, which is at least 2^-12 of itself away from a bf16 midpoint unless
+// it is a bf16.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "mlkv_q4.h"
+
+#include "mlkv_device.cuh"
+
+namespace mlkv {
+namespace {
+
+__device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b)
+{
+    const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162 *>(&a);
+    const __nv_bfloat162 y = *reinterpret_cast<const __nv_bfloat162 *>(&b);
+    const __nv_bfloat162 m = __hmax2_nan(__habs2(x), __habs2(y));
+    return *reinterpret_cast<const uint32_t *>(&m);
+}
+
+// Eight channels of a group whose four lanes are neighbours (lane % 4): the sum of code << 4 i over
+// the channels' nibbles, and the scale's bits.
+struct Coded {
+    uint32_t even, odd;   // channels 0, 2, 4, 6 and 1, 3, 5, 7, a nibble each (low 16 bits)
+    uint32_t quad[2];     // channels 0 .. 3 and 4 .. 7
+    uint32_t scale;       // bf16 bits
+};
+
+__device__ __forceinline__ Coded quantise8(uint4 x)
+{
+    uint32_t m = max_abs2(max_abs2(x.x, x.y), max_abs2(x.z, x.w));
+    m = max_abs2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    m = max_abs2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    m = max_abs2(m, m >> 16);
+    const float amax = bf16_lo(m);
+    Coded c;
+    const float s = __uint_as_float(pack_bf16x2(0.f, amax * (1.f / 7.f)) & 0xffff0000u);
+    float r = 0.f;
+    if (!(amax < __int_as_float(0x7f800000))) {
+        c.scale = 0x7fffu;
+    } else if (s < 1.17549435e-38f) {
+        c.scale = 0u;
+    } else {
+        c.scale = __float_as_uint(s) >> 16;
+        r = fast_rcp(s) * (1.f + 1.f / 65536.f);
+    }
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t n[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        // a group with a NaN or an infinity takes code 8 (0) everywhere
+        const float v = (i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
+        n[i] = __float_as_uint(fmaf(r == 0.f ? 0.f : v, r, 12582912.f + 8.f)) & 15u;
+    }
+    c.even = n[0] | n[2] << 4 | n[4] << 8 | n[6] << 12;
+    c.odd = n[1] | n[3] << 4 | n[5] << 8 | n[7] << 12;
+    c.quad[0] = n[0] | n[1] << 4 | n[2] << 8 | n[3] << 12;
+    c.quad[1] = n[4] | n[5] << 4 | n[6] << 8 | n[7] << 12;
+    return c;
+}
+
+// One position's octet of a row, straight to its places in the row's block.
+template <int D>
+__device__ __forceinline__ void store_octet(uint8_t *row, int pos, int oct, bool is_v, const Coded &c)
+{
+    using LY = Q4Layout<D>;
+    uint8_t *blk = row + static_cast<size_t>(pos / kQ4Block) * LY::kBytes;
+    const int r = pos % kQ4Block, grp = oct >> 2, t = oct & 3;
+    if (is_v) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            *reinterpret_cast<uint16_t *>(blk + LY::v_word(r, grp, 2 * t + q) + 2 * (r & 1)) =
+                static_cast<uint16_t>(c.quad[q]);
+    } else {
+        *reinterpret_cast<uint32_t *>(blk + LY::k_word(r, grp, t)) = c.even | c.odd << 16;
+    }
+    if (t == 0)
+        *reinterpret_cast<uint16_t *>(blk + (is_v ? LY::v_scale(r, grp) : LY::k_scale(r, grp))) =
+            static_cast<uint16_t>(c.scale);
+}
+
+// The new token of every (sequence, KV head): a thread per 8 channels.
+template <int D>
+__global__ void __launch_bounds__(128) q4_append_kernel(const __grid_constant__ Q4StoreParams p)
+{
+    grid_dependency_wait();
+    grid_dependents_launch();
+    constexpr int kOct = D / 8;
+    const int total = 2 * p.b * p.g * kOct;
+    const int idx = blockIdx.x * blockDim.x + threadIdx.x;
+    // whole groups of lanes are in or out: total is a multiple of 8
+    const bool in = idx < total;
+    const int oct = idx % kOct;
+    int row = in ? idx / kOct : 0;
+    const int bg = p.b * p.g;
+    const bool is_v = row >= bg;
+    row -= is_v ? bg : 0;
+    const uint4 x = *reinterpret_cast<const uint4 *>((is_v ? p.V : p.K) +
+                                                     static_cast<size_t>(row) * D + oct * 8);
+    const Coded c = quantise8(x);
+    if (in)
+        store_octet<D>(p.slot + row * p.row_bytes, p.seq_len[row / p.g] - 1, oct, is_v, c);
+}
+
+constexpr int kTile = kQ4RowAlign;   // positions of one CTA of the store and of the read
+
+// A CTA turns 64 positions of one (sequence, KV head) into the image of their four blocks in shared
+// memory and writes it out in 16-byte pieces (the last, partly filled tile: each position to its own
+// places, so that positions past it keep their contents).  HBM-bound: 2 bytes a channel in, 0.5625 out.
+template <int D>
+__global__ void __launch_bounds__(256) q4_store_kernel(const __grid_constant__ Q4StoreParams p)
+{
+    using LY = Q4Layout<D>;
+    constexpr int kOct = D / 8;
+    constexpr int kTasks = kTile * kOct / 256;   // octets of K (and of V) a thread
+    __shared__ __align__(16) uint8_t img[4 * LY::kBytes];
+    grid_dependency_wait();
+    grid_dependents_launch();
+    const int tiles = (p.len + kTile - 1) / kTile;
+    const int row = static_cast<int>(blockIdx.x) / tiles;
+    const int tile = static_cast<int>(blockIdx.x) - row * tiles;
+    const int n = min(kTile, p.len - tile * kTile);
+    const size_t src = (static_cast<size_t>(row) * p.len + static_cast<size_t>(tile) * kTile) * D;
+    uint8_t *dst = p.slot + row * p.row_bytes + static_cast<size_t>(tile) * 4 * LY::kBytes;
+    const int tid = threadIdx.x;
+    uint4 x[2][kTasks];
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+        for (int u = 0; u < kTasks; ++u) {
+            const int i = u * 256 + tid;
+            x[kv][u] = i / kOct < n ? __ldcs(reinterpret_cast<const uint4 *>((kv ? p.V : p.K) + src) + i)
+                                    : make_uint4(0, 0, 0, 0);
+        }
+    if (n < kTile) {
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+            for (int u = 0; u < kTasks; ++u) {
+                const int i = u * 256 + tid;
+                const Coded c = quantise8(x[kv][u]);
+                if (i / kOct < n)
+                    store_octet<D>(dst, i / kOct, i % kOct, kv == 1, c);
+            }
+        return;
+    }
+#pragma unroll
+    for (int u = 0; u < kTasks; ++u) {
+        const int i = u * 256 + tid;
+        const int pos = i / kOct, oct = i % kOct, grp = oct >> 2, t = oct & 3;
+        uint8_t *blk = img + pos / kQ4Block * LY::kBytes;
+        const int r = pos % kQ4Block;
+        Coded c = quantise8(x[0][u]);
+        *reinterpret_cast<uint32_t *>(blk + LY::k_word(r, grp, t)) = c.even | c.odd << 16;
+        if (t == 0)
+            *reinterpret_cast<uint16_t *>(blk + LY::k_scale(r, grp)) = static_cast<uint16_t>(c.scale);
+        c = quantise8(x[1][u]);
+        // the positions of a pair swap a quad: the even one stores words 2 t, the odd one 2 t + 1
+        const bool odd = r & 1;
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? c.quad[0] : c.quad[1], kOct);
+        const uint32_t word = odd ? other | c.quad[1] << 16 : c.quad[0] | other << 16;
+        *reinterpret_cast<uint32_t *>(blk + LY::v_word(r, grp, 2 * t + (odd ? 1 : 0))) = word;
+        if (t == 0)
+            *reinterpret_cast<uint16_t *>(blk + LY::v_scale(r, grp)) = static_cast<uint16_t>(c.scale);
+    }
+    __syncthreads();
+    for (int i = tid; i < 4 * LY::kBytes / 16; i += 256)
+        reinterpret_cast<uint4 *>(dst)[i] = reinterpret_cast<const uint4 *>(img)[i];
+}
+
+// Nibbles i and i + 4 of a word as a bf16 pair: the code's bits in the mantissa of 128, less 136.
+__device__ __forceinline__ uint32_t codes2(uint32_t w, int i)
+{
+    const uint32_t v = ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u;
+    const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162 *>(&v);
+    const __nv_bfloat162 y = __hsub2(x, __floats2bfloat162_rn(136.f, 136.f));
+    return *reinterpret_cast<const uint32_t *>(&y);
+}
+
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b)
+{
+    const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162 *>(&a);
+    const __nv_bfloat162 y = *reinterpret_cast<const __nv_bfloat162 *>(&b);
+    const __nv_bfloat162 z = __hmul2(x, y);   // 4 x 8 significant bits: rounded once, as in fp32
+    return *reinterpret_cast<const uint32_t *>(&z);
+}
+
+// A CTA brings the blocks of 64 positions of one (sequence, KV head) into shared memory and writes the
+// values of those of [start, start + len), a thread 8 channels of a pair of positions at a time.
+template <int D>
+__global__ void __launch_bounds__(256) q4_read_kernel(const __grid_constant__ Q4ReadParams p)
+{
+    using LY = Q4Layout<D>;
+    constexpr int kOct = D / 8;
+    __shared__ __align__(16) uint8_t img[4 * LY::kBytes];
+    grid_dependency_wait();
+    grid_dependents_launch();
+    const int tile0 = p.start / kTile;
+    const int tiles = (p.start + p.len - 1) / kTile - tile0 + 1;
+    const int row = static_cast<int>(blockIdx.x) / tiles;
+    const int pos0 = (tile0 + static_cast<int>(blockIdx.x) - row * tiles) * kTile;
+    // the tile's positions [lo, hi) that are asked for, and their blocks
+    const int lo = max(p.start - pos0, 0), hi = min(p.start + p.len - pos0, kTile);
+    const uint8_t *src =
+        p.slot + row * p.row_bytes + static_cast<size_t>(pos0 / kQ4Block) * LY::kBytes;
+    const int tid = threadIdx.x;
+    const int i1 = ((hi + kQ4Block - 1) / kQ4Block) * LY::kBytes / 16;
+    for (int i = lo / kQ4Block * LY::kBytes / 16 + tid; i < i1; i += 256)
+        reinterpret_cast<uint4 *>(img)[i] = reinterpret_cast<const uint4 *>(src)[i];
+    __syncthreads();
+    // pairs [lo / 2, (hi + 1) / 2)
+    const int first = lo / 2 * kOct;
+    const int n = ((hi + 1) / 2 - lo / 2) * kOct;
+    for (int k = tid; k < 2 * n; k += 256) {
+        const bool is_v = k >= n;
+        const int i = first + (is_v ? k - n : k);
+        const int pos = i / kOct * 2, oct = i % kOct, grp = oct >> 2, t = oct & 3;
+        const uint8_t *blk = img + pos / kQ4Block * LY::kBytes;
+        const int r = pos % kQ4Block;
+        uint32_t v[2][4];   // [position][channel pair]
+        if (is_v) {
+            const uint32_t s = *reinterpret_cast<const uint32_t *>(blk + LY::v_scale(r, grp));
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const uint32_t w =
+                    *reinterpret_cast<const uint32_t *>(blk + LY::v_word(r, grp, 2 * t + q));
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const uint32_t a = mul2(codes2(w, 2 * c), s), b = mul2(codes2(w, 2 * c + 1), s);
+                    v[0][2 * q + c] = __byte_perm(a, b, 0x5410);
+                    v[1][2 * q + c] = __byte_perm(a, b, 0x7632);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+                const uint32_t s =
+                    *reinterpret_cast<const uint16_t *>(blk + LY::k_scale(r + o, grp)) * 0x10001u;
+                const uint32_t w =
+                    *reinterpret_cast<const uint32_t *>(blk + LY::k_word(r + o, grp, t));
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    v[o][c] = mul2(codes2(w, c), s);
+            }
+        }
+        __nv_bfloat16 *dst = (is_v ? p.V : p.K) +
+                             (static_cast<long long>(row) * p.len + (pos0 + pos - p.start)) * D +
+                             oct * 8;
+        if (pos >= lo)
+            *reinterpret_cast<uint4 *>(dst) = make_uint4(v[0][0], v[0][1], v[0][2], v[0][3]);
+        if (pos + 1 < hi)
+            *reinterpret_cast<uint4 *>(dst + D) = make_uint4(v[1][0], v[1][1], v[1][2], v[1][3]);
+    }
+}
+
+template <typename P>
+cudaError_t launch(const void *fn, long long blocks, int threads, const P &p, cudaStream_t stream)
+{
+    if (blocks > 0x7FFFFFFFLL)
+        return cudaErrorInvalidConfiguration;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    void *args[] = {const_cast<P *>(&p)};
+    return cudaLaunchKernelExC(&cfg, fn, args);
+}
+
+template <typename F64, typename F128>
+const void *pick(int d, F64 *f64, F128 *f128)
+{
+    return d == 64 ? reinterpret_cast<const void *>(f64) : reinterpret_cast<const void *>(f128);
+}
+
+}  // namespace
+
+cudaError_t launch_q4_append(int d, const Q4StoreParams &p, cudaStream_t stream)
+{
+    const long long total = 2LL * p.b * p.g * (d / 8);
+    return launch(pick(d, &q4_append_kernel<64>, &q4_append_kernel<128>), (total + 127) / 128, 128, p,
+                  stream);
+}
+
+cudaError_t launch_q4_store(int d, const Q4StoreParams &p, cudaStream_t stream)
+{
+    const long long tiles = (p.len + kTile - 1) / kTile;
+    return launch(pick(d, &q4_store_kernel<64>, &q4_store_kernel<128>), tiles * p.b * p.g, 256, p,
+                  stream);
+}
+
+cudaError_t launch_q4_read(int d, const Q4ReadParams &p, cudaStream_t stream)
+{
+    const long long tiles = (p.start + p.len - 1) / kTile - p.start / kTile + 1;
+    return launch(pick(d, &q4_read_kernel<64>, &q4_read_kernel<128>), tiles * p.b * p.g, 256, p, stream);
+}
+
+}  // namespace mlkv

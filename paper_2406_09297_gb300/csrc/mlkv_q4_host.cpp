@@ -1,0 +1,391 @@
+// Host side of the 4-bit KV cache: argument checks, allocation and the mlkv_q4_* calls of mlkv.h.
+//
+// The cache of an MLKV model's m owner layers (arXiv 2406.09297, Sec. 3) as one allocation of
+// [m][b][g] rows of blocks (mlkv_q4.h).  The decode kernel splits its work as the bf16 decode kernel
+// does and shares its merge of many records (combine_kernel).
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "mlkv_host.h"
+#include "mlkv_q4.h"
+
+using mlkv::aligned16;
+using mlkv::DeviceGuard;
+using mlkv::fail;
+using mlkv::fail_cuda;
+using mlkv::overlap;
+
+struct mlkv_q4cache {
+    int l = 0, h = 0, d = 0, g = 0, G = 0, b = 0, max_seq = 0, m = 0;
+    std::vector<int> owner, slot;
+    int device = 0;
+    int sm_count = 0;
+    int ctas_per_sm = 0;
+    uint8_t *cache = nullptr;   // [m][b][g] rows
+    long long row_bytes = 0;
+    size_t cache_bytes = 0;
+    float *part_o = nullptr;    // [records][G][d]
+    float *part_lse = nullptr;  // [records][G]
+    unsigned *counters = nullptr;
+    int *err = nullptr;
+};
+
+namespace {
+
+void free_all(mlkv_q4cache *c)
+{
+    cudaFree(c->cache);
+    cudaFree(c->part_o);
+    cudaFree(c->part_lse);
+    cudaFree(c->counters);
+    cudaFree(c->err);
+}
+
+int check_layer(const mlkv_q4cache *c, int layer)
+{
+    if (c == nullptr)
+        return fail(MLKV_ERR_INVALID_ARG, "null cache handle");
+    if (layer < 0 || layer >= c->l)
+        return fail(MLKV_ERR_INVALID_ARG, "layer %d outside [0, %d)", layer, c->l);
+    return MLKV_OK;
+}
+
+int check_lens(const mlkv_q4cache *c, const int *seq_lens)
+{
+    if (seq_lens == nullptr)
+        return fail(MLKV_ERR_INVALID_ARG, "seq_lens is NULL");
+    for (int beta = 0; beta < c->b; ++beta)
+        if (seq_lens[beta] < 1 || seq_lens[beta] > c->max_seq)
+            return fail(MLKV_ERR_RANGE, "seq_lens[%d] = %d outside [1, %d]", beta, seq_lens[beta],
+                        c->max_seq);
+    return MLKV_OK;
+}
+
+uint8_t *slot_base(const mlkv_q4cache *c, int layer)
+{
+    return c->cache + c->cache_bytes / c->m * c->slot[layer];
+}
+
+int store(mlkv_q4cache *c, int layer, const void *K, const void *V, int len, const int *seq_lens,
+          cudaStream_t stream)
+{
+    static thread_local mlkv::Q4StoreParams p;
+    p.K = static_cast<const __nv_bfloat16 *>(K);
+    p.V = static_cast<const __nv_bfloat16 *>(V);
+    p.slot = slot_base(c, layer);
+    p.row_bytes = c->row_bytes;
+    p.b = c->b;
+    p.g = c->g;
+    p.len = len;
+    if (seq_lens != nullptr)
+        std::memcpy(p.seq_len, seq_lens, sizeof(int) * c->b);
+    const cudaError_t e = seq_lens != nullptr ? mlkv::launch_q4_append(c->d, p, stream)
+                                              : mlkv::launch_q4_store(c->d, p, stream);
+    return e == cudaSuccess ? MLKV_OK : fail_cuda(e, "4-bit store launch");
+}
+
+}  // namespace
+
+extern "C" {
+
+int mlkv_q4_create(mlkv_q4cache_t *out, int n_layers, int n_q_heads, int head_dim,
+                   const int *layer_owner, int kv_heads_per_owner, int batch, int max_seq)
+{
+    if (out == nullptr)
+        return fail(MLKV_ERR_INVALID_ARG, "out is NULL");
+    const int rc = mlkv::validate_map(n_layers, n_q_heads, head_dim, layer_owner, kv_heads_per_owner,
+                                      batch, max_seq);
+    if (rc != MLKV_OK)
+        return rc;
+    if (static_cast<long long>(batch) * kv_heads_per_owner > (1 << 24) || max_seq > (1 << 30))
+        return fail(MLKV_ERR_UNSUPPORTED, "%d sequences of %d KV heads and %d positions exceed the "
+                    "int32 indices", batch, kv_heads_per_owner, max_seq);
+    mlkv_q4cache *c = new (std::nothrow) mlkv_q4cache();
+    if (c == nullptr)
+        return fail(MLKV_ERR_OOM, "out of host memory");
+    c->l = n_layers;
+    c->h = n_q_heads;
+    c->d = head_dim;
+    c->g = kv_heads_per_owner;
+    c->G = n_q_heads / kv_heads_per_owner;
+    c->b = batch;
+    c->max_seq = max_seq;
+    c->owner.assign(layer_owner, layer_owner + n_layers);
+    c->slot.resize(n_layers);
+    for (int n = 0; n < n_layers; ++n)   // an owner comes before its readers
+        c->slot[n] = c->owner[n] == n ? c->m++ : c->slot[c->owner[n]];
+    c->device = mlkv::current_device();
+    DeviceGuard guard(c->device);
+    cudaError_t e = cudaDeviceGetAttribute(&c->sm_count, cudaDevAttrMultiProcessorCount, c->device);
+    if (e == cudaSuccess)
+        e = mlkv::prepare_q4_decode(c->d, c->G, &c->ctas_per_sm);
+    for (const bool windowed : {false, true})
+        if (e == cudaSuccess)
+            e = mlkv::prepare_prefill(c->d, windowed);
+    if (e != cudaSuccess || c->ctas_per_sm < 1) {
+        delete c;
+        return e != cudaSuccess ? fail_cuda(e, "preparing the 4-bit cache's kernels")
+                                : fail(MLKV_ERR_CUDA, "the 4-bit decode kernel cannot be resident");
+    }
+    c->row_bytes = mlkv::q4_row_bytes(max_seq, c->d);
+    const size_t rows = static_cast<size_t>(c->b) * c->g;
+    c->cache_bytes = rows * c->m * c->row_bytes;
+    // a record for each segment and each CTA of a launch's runs
+    const size_t records = rows + static_cast<size_t>(c->ctas_per_sm) * c->sm_count;
+    auto alloc = [&](void **ptr, size_t n) {
+        if (e == cudaSuccess)
+            e = cudaMalloc(ptr, n);
+        if (e == cudaSuccess && ptr != reinterpret_cast<void **>(&c->part_o) &&
+            ptr != reinterpret_cast<void **>(&c->part_lse))
+            e = cudaMemset(*ptr, 0, n);
+    };
+    alloc(reinterpret_cast<void **>(&c->cache), c->cache_bytes);
+    alloc(reinterpret_cast<void **>(&c->part_o), records * c->G * c->d * sizeof(float));
+    alloc(reinterpret_cast<void **>(&c->part_lse), records * c->G * sizeof(float));
+    alloc(reinterpret_cast<void **>(&c->counters), rows * sizeof(unsigned));
+    alloc(reinterpret_cast<void **>(&c->err), sizeof(int));
+    if (e == cudaSuccess)
+        e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        const size_t need = c->cache_bytes;
+        free_all(c);
+        delete c;
+        return fail(e == cudaErrorMemoryAllocation ? MLKV_ERR_OOM : MLKV_ERR_CUDA,
+                    "allocating a %zu-byte 4-bit cache: %s", need, cudaGetErrorString(e));
+    }
+    *out = c;
+    return MLKV_OK;
+}
+
+int mlkv_q4_destroy(mlkv_q4cache_t c)
+{
+    if (c == nullptr)
+        return MLKV_OK;
+    DeviceGuard guard(c->device);
+    cudaDeviceSynchronize();
+    free_all(c);
+    delete c;
+    return MLKV_OK;
+}
+
+int64_t mlkv_q4_bytes(mlkv_q4cache_t c)
+{
+    if (c == nullptr)
+        return fail(MLKV_ERR_INVALID_ARG, "null cache handle");
+    return static_cast<int64_t>(c->cache_bytes);
+}
+
+int mlkv_q4_append(mlkv_q4cache_t c, int layer, const void *K, const void *V, const int *seq_lens,
+                   void *cuda_stream)
+{
+    int rc = check_layer(c, layer);
+    if (rc != MLKV_OK)
+        return rc;
+    if (c->owner[layer] != layer)
+        return MLKV_OK;   // Sec. 3: a layer without KV heads of its own stores nothing
+    if (K == nullptr || V == nullptr || !aligned16(K) || !aligned16(V))
+        return fail(MLKV_ERR_INVALID_ARG, "K and V must be non-NULL and 16-byte aligned");
+    if ((rc = check_lens(c, seq_lens)) != MLKV_OK)
+        return rc;
+    DeviceGuard guard(c->device);
+    return store(c, layer, K, V, 1, seq_lens, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int mlkv_q4_load_prefix(mlkv_q4cache_t c, int layer, const void *K, const void *V, int len,
+                        void *cuda_stream)
+{
+    const int rc = check_layer(c, layer);
+    if (rc != MLKV_OK)
+        return rc;
+    if (c->owner[layer] != layer)
+        return MLKV_OK;
+    if (len < 0 || len > c->max_seq)
+        return fail(MLKV_ERR_RANGE, "prefix length %d outside [0, %d]", len, c->max_seq);
+    if (len == 0)
+        return MLKV_OK;
+    if (K == nullptr || V == nullptr || !aligned16(K) || !aligned16(V))
+        return fail(MLKV_ERR_INVALID_ARG, "K and V must be non-NULL and 16-byte aligned");
+    DeviceGuard guard(c->device);
+    return store(c, layer, K, V, len, nullptr, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int mlkv_q4_read(mlkv_q4cache_t c, int layer, void *K, void *V, int start, int len, void *cuda_stream)
+{
+    const int rc = check_layer(c, layer);
+    if (rc != MLKV_OK)
+        return rc;
+    if (start < 0 || len < 0 || start > c->max_seq - len)
+        return fail(MLKV_ERR_RANGE, "positions [%d, %d + %d) outside [0, %d)", start, start, len,
+                    c->max_seq);
+    if (len == 0)
+        return MLKV_OK;
+    if (K == nullptr || V == nullptr || !aligned16(K) || !aligned16(V))
+        return fail(MLKV_ERR_INVALID_ARG, "K and V must be non-NULL and 16-byte aligned");
+    const size_t bytes = static_cast<size_t>(c->b) * c->g * len * c->d * 2;
+    if (overlap(K, bytes, V, bytes))
+        return fail(MLKV_ERR_INVALID_ARG, "K and V overlap");
+    DeviceGuard guard(c->device);
+    mlkv::Q4ReadParams p;
+    p.K = static_cast<__nv_bfloat16 *>(K);
+    p.V = static_cast<__nv_bfloat16 *>(V);
+    p.slot = slot_base(c, layer);
+    p.row_bytes = c->row_bytes;
+    p.b = c->b;
+    p.g = c->g;
+    p.start = start;
+    p.len = len;
+    const cudaError_t e = mlkv::launch_q4_read(c->d, p, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? MLKV_OK : fail_cuda(e, "4-bit read launch");
+}
+
+int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *out,
+                             const int *seq_lens, int window, int sinks, void *cuda_stream)
+{
+    int rc = check_layer(c, layer);
+    if (rc != MLKV_OK)
+        return rc;
+    if (Q == nullptr || out == nullptr || !aligned16(Q) || !aligned16(out))
+        return fail(MLKV_ERR_INVALID_ARG, "Q and out must be non-NULL and 16-byte aligned");
+    const size_t qbytes = static_cast<size_t>(c->b) * c->h * c->d * 2;
+    if (overlap(Q, qbytes, out, qbytes))
+        return fail(MLKV_ERR_INVALID_ARG, "out overlaps Q");
+    if ((rc = check_lens(c, seq_lens)) != MLKV_OK || (rc = mlkv::check_window(window, sinks)) != MLKV_OK)
+        return rc;
+    mlkv::clamp_window(c->max_seq, &window, &sinks);
+    static thread_local mlkv::Q4DecodeParams p;
+    const int T = mlkv::q4_tile_tokens(c->d);
+    bool uniform = true;
+    long long tiles = 0;
+    for (int beta = 0; beta < c->b; ++beta) {
+        const int L = seq_lens[beta];
+        uniform = uniform && L == seq_lens[0];
+        p.seq_len[beta] = L;
+        p.tile_start[beta] = static_cast<int>(tiles);
+        tiles += static_cast<long long>(c->g) *
+                 mlkv::visible_tiles(L, window, sinks, T, mlkv::kQ4Block).nt;
+        if (tiles > 0x7fffffffLL)
+            return fail(MLKV_ERR_UNSUPPORTED, "the tiles exceed the int32 tile index");
+    }
+    p.tile_start[c->b] = static_cast<int>(tiles);
+    p.uniform_len = uniform ? seq_lens[0] : 0;
+    // One wave of resident CTAs, each with at least a tile for every warp.
+    const long long slots = std::min<long long>(static_cast<long long>(c->ctas_per_sm) * c->sm_count,
+                                                mlkv::kCombineMaxPiecesHost);
+    const int grid = static_cast<int>(std::max(1LL, std::min(slots, (tiles + 7) / 8)));
+    p.Q = static_cast<const __nv_bfloat16 *>(Q);
+    p.out = static_cast<__nv_bfloat16 *>(out);
+    p.slot = slot_base(c, layer);
+    p.row_bytes = c->row_bytes;
+    p.part_o = c->part_o;
+    p.part_lse = c->part_lse;
+    p.counters = c->counters;
+    p.err = c->err;
+    p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(c->d)));
+    p.b = c->b;
+    p.h = c->h;
+    p.g = c->g;
+    p.G = c->G;
+    p.window = window;
+    p.sinks = sinks;
+    p.num_tiles = static_cast<int>(tiles);
+    // What the merges see: lengths whose plain tiling gives these tiles.
+    static thread_local mlkv::DecodeParams m;
+    m.b = c->b;
+    m.h = c->h;
+    m.g = c->g;
+    m.G = c->G;
+    m.num_tiles = p.num_tiles;
+    m.ml_layers = 0;
+    for (int beta = 0; beta < c->b; ++beta) {
+        m.tile_start[beta] = p.tile_start[beta];
+        m.seq_len[beta] = mlkv::visible_len(
+            p.seq_len[beta],
+            mlkv::visible_tiles(p.seq_len[beta], window, sinks, T, mlkv::kQ4Block));
+    }
+    m.uniform_len = uniform ? m.seq_len[0] : 0;
+    p.deferred_merge = mlkv::max_pieces_per_segment(m, T, grid) > mlkv::inline_merge_pieces(c->G, c->d);
+    DeviceGuard guard(c->device);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    cudaError_t e = mlkv::launch_q4_decode(c->d, grid, p, stream);
+    if (e != cudaSuccess)
+        return fail_cuda(e, "4-bit decode launch");
+    if (p.deferred_merge) {
+        m.out = p.out;
+        m.part_o = p.part_o;
+        m.part_lse = p.part_lse;
+        m.tile_tokens = T;
+        m.decode_grid = grid;
+        if ((e = mlkv::launch_combine(m, c->d, stream)) != cudaSuccess)
+            return fail_cuda(e, "combine launch");
+    }
+    return MLKV_OK;
+}
+
+int mlkv_q4_prefill(mlkv_q4cache_t c, int layer, const void *Q, const void *K, const void *V, void *out,
+                    const int *prompt_lens, int s_max, int window, int sinks, void *cuda_stream)
+{
+    int rc = check_layer(c, layer);
+    if (rc != MLKV_OK)
+        return rc;
+    if ((rc = mlkv::check_prefill_args(Q, out, prompt_lens, c->b, c->h, c->d, s_max, c->max_seq)) !=
+            MLKV_OK ||
+        (rc = mlkv::check_window(window, sinks)) != MLKV_OK)
+        return rc;
+    if (K == nullptr || V == nullptr || !aligned16(K) || !aligned16(V))
+        return fail(MLKV_ERR_INVALID_ARG, "K and V must be non-NULL and 16-byte aligned");
+    const size_t qbytes = static_cast<size_t>(c->b) * s_max * c->h * c->d * 2;
+    const size_t kvbytes = static_cast<size_t>(c->b) * c->g * s_max * c->d * 2;
+    if (overlap(K, kvbytes, out, qbytes) || overlap(V, kvbytes, out, qbytes))
+        return fail(MLKV_ERR_INVALID_ARG, "out overlaps K or V");
+    mlkv::clamp_window(s_max, &window, &sinks);
+    DeviceGuard guard(c->device);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    mlkv::PrefillCall a = {};
+    a.Q = Q;
+    a.K = K;
+    a.V = V;
+    a.out = out;
+    a.prompt_lens = prompt_lens;
+    a.err = c->err;
+    a.b = c->b;
+    a.h = c->h;
+    a.g = c->g;
+    a.d = c->d;
+    a.s_max = s_max;
+    a.sm_count = c->sm_count;
+    a.direct = true;
+    a.window = window;
+    a.sinks = sinks;
+    if ((rc = mlkv::issue_prefill(a, stream)) != MLKV_OK)
+        return rc;
+    return c->owner[layer] == layer ? store(c, layer, K, V, s_max, nullptr, stream) : MLKV_OK;
+}
+
+int mlkv_q4_sync_status(mlkv_q4cache_t c)
+{
+    if (c == nullptr)
+        return fail(MLKV_ERR_INVALID_ARG, "null cache handle");
+    DeviceGuard guard(c->device);
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e != cudaSuccess)
+        return fail_cuda(e, "cudaDeviceSynchronize");
+    int word = 0;
+    if ((e = cudaMemcpy(&word, c->err, sizeof(int), cudaMemcpyDeviceToHost)) != cudaSuccess)
+        return fail_cuda(e, "reading the device error word");
+    if (word != 0) {
+        // A kernel stopped early: clear the word and the merge counters it may have left behind.
+        cudaMemset(c->err, 0, sizeof(int));
+        cudaMemset(c->counters, 0, static_cast<size_t>(c->b) * c->g * sizeof(unsigned));
+        cudaDeviceSynchronize();
+        return fail(MLKV_ERR_DEVICE, "a kernel reported device error bits 0x%x", word);
+    }
+    return MLKV_OK;
+}
+
+}  // extern "C"

@@ -32,6 +32,9 @@ EXPORTED = [
     "mlkv_block_owner_map", "mlkv_version", "mlkv_decode_attention_static", "mlkv_prefill",
     "mlkv_merge_kv_weights", "mlkv_decode_block_fused", "mlkv_decode_step_host",
     "mlkv_static_status", "mlkv_read_bandwidth_probe", "mlkv_plan_step",
+    "mlkv_decode_attention_window", "mlkv_prefill_window", "mlkv_qk_norm_rope", "mlkv_q4_create",
+    "mlkv_q4_destroy", "mlkv_q4_bytes", "mlkv_q4_append", "mlkv_q4_load_prefix", "mlkv_q4_read",
+    "mlkv_q4_decode_attention", "mlkv_q4_prefill", "mlkv_q4_sync_status",
 ]
 
 
@@ -78,6 +81,20 @@ def _load():
     L.mlkv_decode_block_fused.argtypes = [vp, ci, vp, vp, vp, vp]
     L.mlkv_plan_step.argtypes = [ci, ci, ci, ip, ci, ci, ci, vp, ci, ci, ci, ci,
                                  ctypes.POINTER(i64)]
+    L.mlkv_decode_attention_window.argtypes = [vp, ci, vp, vp, vp, ci, ci, vp]
+    L.mlkv_prefill_window.argtypes = [vp, ci, vp, vp, vp, vp, vp, ci, ci, ci, vp]
+    L.mlkv_qk_norm_rope.argtypes = ([vp] * 3 + [i64] * 3 + [vp] * 4 + [ci] * 3 + [vp, ctypes.c_float] +
+                                    [ci] * 5 + [vp] * 4)
+    L.mlkv_q4_create.argtypes = L.mlkv_cache_create.argtypes
+    L.mlkv_q4_destroy.argtypes = [vp]
+    L.mlkv_q4_bytes.argtypes = [vp]
+    L.mlkv_q4_bytes.restype = i64
+    L.mlkv_q4_append.argtypes = [vp, ci, vp, vp, vp, vp]
+    L.mlkv_q4_load_prefix.argtypes = [vp, ci, vp, vp, ci, vp]
+    L.mlkv_q4_read.argtypes = [vp, ci, vp, vp, ci, ci, vp]
+    L.mlkv_q4_decode_attention.argtypes = [vp, ci, vp, vp, vp, ci, ci, vp]
+    L.mlkv_q4_prefill.argtypes = [vp, ci, vp, vp, vp, vp, vp, ci, ci, ci, vp]
+    L.mlkv_q4_sync_status.argtypes = [vp]
     return L
 
 
@@ -135,16 +152,20 @@ def _lens_ptr(seq_lens):
         return a, a.ctypes.data
 
 
-def mlkv_cache_create(n_layers, n_q_heads, head_dim, layer_owner, kv_heads_per_owner, batch,
-                      max_seq):
+def _create(fn, n_layers, n_q_heads, head_dim, layer_owner, kv_heads_per_owner, batch, max_seq):
     owner = np.ascontiguousarray(np.asarray(layer_owner, dtype=np.int32))
     if len(owner) != n_layers:
         raise MLKVError(MLKV_ERR_INVALID_ARG, "layer_owner must have n_layers entries")
     h = ctypes.c_void_p()
-    _check(lib.mlkv_cache_create(ctypes.byref(h), n_layers, n_q_heads, head_dim,
-                                 owner.ctypes.data_as(ctypes.POINTER(ctypes.c_int)),
-                                 kv_heads_per_owner, batch, max_seq))
+    _check(fn(ctypes.byref(h), n_layers, n_q_heads, head_dim,
+              owner.ctypes.data_as(ctypes.POINTER(ctypes.c_int)), kv_heads_per_owner, batch, max_seq))
     return h
+
+
+def mlkv_cache_create(n_layers, n_q_heads, head_dim, layer_owner, kv_heads_per_owner, batch,
+                      max_seq):
+    return _create(lib.mlkv_cache_create, n_layers, n_q_heads, head_dim, layer_owner,
+                   kv_heads_per_owner, batch, max_seq)
 
 
 def mlkv_cache_destroy(handle):
@@ -294,6 +315,104 @@ def mlkv_merge_kv_weights(layer_owner, n_q_heads, n_kv_heads, W, out, stream=Non
         row, _ptr(W), _ptr(out), _stream(stream)))
 
 
+def mlkv_decode_attention_window(handle, layer, Q, out, seq_lens, window, sinks, stream=None):
+    a, p = _lens_ptr(seq_lens)
+    return _check(lib.mlkv_decode_attention_window(handle, layer, _ptr(Q), _ptr(out), p, window,
+                                                   sinks, _stream(stream)))
+
+
+def mlkv_prefill_window(handle, layer, Q, K, V, out, prompt_lens, s_max, window, sinks, stream=None):
+    a, p = _lens_ptr(prompt_lens)
+    return _check(lib.mlkv_prefill_window(handle, layer, _ptr(Q), _ptr(K), _ptr(V), _ptr(out), p,
+                                          s_max, window, sinks, _stream(stream)))
+
+
+def _token_stride(x, name, batch, s, d):
+    """Elements between the tokens of x [batch][s][heads][d], whose heads are dense."""
+    if x is None:
+        return 0
+    st = x.stride()
+    if x.dim() != 4 or tuple(x.shape[:2]) != (batch, s) or x.shape[3] != d:
+        raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must be [{batch}][{s}][heads][{d}]")
+    if st[3] != 1 or (x.shape[2] > 1 and st[2] != d) or (batch > 1 and s > 1 and st[0] != s * st[1]):
+        raise MLKVError(MLKV_ERR_INVALID_ARG,
+                        f"{name}'s heads must be dense and its tokens one stride apart")
+    return st[1] if s > 1 else st[0]
+
+
+def mlkv_qk_norm_rope(Q, K, V, q_gain, k_gain, cos, sin, positions, Q_out, K_out, V_out, eps=1e-6,
+                      interleaved=False, stream=None):
+    """Q [b][s][h][d], K and V [b][s][g][d] (views of a fused projection will do; V and V_out may be
+    None), gains [d] or None, cos and sin fp32 [n_pos][rot / 2] and positions int32 [b][s] (None: no
+    rotary encoding) -> Q_out [b][s][h][d], K_out and V_out [b][g][s][d], all bf16."""
+    b, s, h, d = Q.shape
+    g = K.shape[2]
+    strides = [_token_stride(x, n, b, s, d) for x, n in ((Q, "Q"), (K, "K"), (V, "V"))]
+    if V is not None and V.shape[2] != g:
+        raise MLKVError(MLKV_ERR_INVALID_ARG, "K and V must have the same heads")
+    for x, n, heads in ((Q_out, "Q_out", h), (K_out, "K_out", g), (V_out, "V_out", g)):
+        if x is not None and (x.numel() != b * s * heads * d or not x.is_contiguous()):
+            raise MLKVError(MLKV_ERR_INVALID_ARG, f"{n} must be dense and hold every head")
+    for x, n in ((q_gain, "q_gain"), (k_gain, "k_gain")):
+        if x is not None and (x.numel() != d or not x.is_contiguous()):
+            raise MLKVError(MLKV_ERR_INVALID_ARG, f"{n} must be dense and hold {d} channels")
+    n_pos, half = (0, 0) if cos is None else cos.shape
+    if cos is not None and (sin is None or sin.shape != cos.shape or positions is None or
+                            not (cos.is_contiguous() and sin.is_contiguous() and
+                                 positions.is_contiguous()) or positions.numel() != b * s or
+                            cos.element_size() != 4 or sin.element_size() != 4 or
+                            positions.element_size() != 4):
+        raise MLKVError(MLKV_ERR_INVALID_ARG,
+                        "cos and sin must be dense fp32 of one shape, positions dense int32 [b][s]")
+    return _check(lib.mlkv_qk_norm_rope(
+        _ptr(Q), _ptr(K), _ptr(V), *strides, _ptr(q_gain), _ptr(k_gain), _ptr(cos), _ptr(sin), n_pos,
+        2 * half, int(interleaved), _ptr(positions), eps, b, s, h, g, d, _ptr(Q_out), _ptr(K_out),
+        _ptr(V_out), _stream(stream)))
+
+
+def mlkv_q4_create(n_layers, n_q_heads, head_dim, layer_owner, kv_heads_per_owner, batch, max_seq):
+    return _create(lib.mlkv_q4_create, n_layers, n_q_heads, head_dim, layer_owner,
+                   kv_heads_per_owner, batch, max_seq)
+
+
+def mlkv_q4_destroy(handle):
+    return _check(lib.mlkv_q4_destroy(handle))
+
+
+def mlkv_q4_bytes(handle):
+    return _check(lib.mlkv_q4_bytes(handle))
+
+
+def mlkv_q4_append(handle, layer, K, V, seq_lens, stream=None):
+    a, p = _lens_ptr(seq_lens)
+    return _check(lib.mlkv_q4_append(handle, layer, _ptr(K), _ptr(V), p, _stream(stream)))
+
+
+def mlkv_q4_load_prefix(handle, layer, K, V, length, stream=None):
+    return _check(lib.mlkv_q4_load_prefix(handle, layer, _ptr(K), _ptr(V), length, _stream(stream)))
+
+
+def mlkv_q4_read(handle, layer, K, V, start, length, stream=None):
+    """Positions [start, start + length) as the cache holds them: bf16 K, V [b][g][length][d]."""
+    return _check(lib.mlkv_q4_read(handle, layer, _ptr(K), _ptr(V), start, length, _stream(stream)))
+
+
+def mlkv_q4_decode_attention(handle, layer, Q, out, seq_lens, window=0, sinks=0, stream=None):
+    a, p = _lens_ptr(seq_lens)
+    return _check(lib.mlkv_q4_decode_attention(handle, layer, _ptr(Q), _ptr(out), p, window, sinks,
+                                               _stream(stream)))
+
+
+def mlkv_q4_prefill(handle, layer, Q, K, V, out, prompt_lens, s_max, window=0, sinks=0, stream=None):
+    a, p = _lens_ptr(prompt_lens)
+    return _check(lib.mlkv_q4_prefill(handle, layer, _ptr(Q), _ptr(K), _ptr(V), _ptr(out), p, s_max,
+                                      window, sinks, _stream(stream)))
+
+
+def mlkv_q4_sync_status(handle):
+    return _check(lib.mlkv_q4_sync_status(handle))
+
+
 class MLKVCache:
     """Owning wrapper around an mlkv_cache_t handle."""
 
@@ -338,6 +457,14 @@ class MLKVCache:
         """Causal prefill of one layer; Q / out [b][s_max][h][d], K / V [b][g][s_max][d]."""
         return mlkv_prefill(self.handle, layer, Q, K, V, out, prompt_lens, int(Q.shape[1]), stream)
 
+    def decode_attention_window(self, layer, Q, out, seq_lens, window, sinks=0, stream=None):
+        return mlkv_decode_attention_window(self.handle, layer, Q, out, seq_lens, window, sinks, stream)
+
+    def prefill_window(self, layer, Q, K, V, out, prompt_lens, window, sinks=0, stream=None):
+        """prefill with a sliding window and sinks."""
+        return mlkv_prefill_window(self.handle, layer, Q, K, V, out, prompt_lens, int(Q.shape[1]),
+                                   window, sinks, stream)
+
     def decode_step_host(self, Q, K, V, out, seq_lens, stream=None):
         return mlkv_decode_step_host(self.handle, Q, K, V, out, seq_lens, stream)
 
@@ -367,3 +494,57 @@ class MLKVCache:
 
     def sync_status(self):
         return mlkv_sync_status(self.handle)
+
+
+class MLKVQ4Cache:
+    """Owning wrapper around an mlkv_q4cache_t handle: keys and values in 4 bits."""
+
+    def __init__(self, n_layers, n_q_heads, head_dim, layer_owner, kv_heads_per_owner, batch,
+                 max_seq):
+        self.l, self.h, self.d = n_layers, n_q_heads, head_dim
+        self.owner = [int(o) for o in layer_owner]
+        self.g, self.b, self.max_seq = kv_heads_per_owner, batch, max_seq
+        self.handle = None
+        self.handle = mlkv_q4_create(n_layers, n_q_heads, head_dim, layer_owner, kv_heads_per_owner,
+                                     batch, max_seq)
+
+    def close(self):
+        if self.handle is not None:
+            mlkv_q4_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def append(self, layer, K, V, seq_lens, stream=None):
+        return mlkv_q4_append(self.handle, layer, K, V, seq_lens, stream)
+
+    def load_prefix(self, layer, K, V, length, stream=None):
+        return mlkv_q4_load_prefix(self.handle, layer, K, V, length, stream)
+
+    def read(self, layer, K, V, start, length, stream=None):
+        return mlkv_q4_read(self.handle, layer, K, V, start, length, stream)
+
+    def decode_attention(self, layer, Q, out, seq_lens, window=0, sinks=0, stream=None):
+        return mlkv_q4_decode_attention(self.handle, layer, Q, out, seq_lens, window, sinks, stream)
+
+    def prefill(self, layer, Q, K, V, out, prompt_lens, window=0, sinks=0, stream=None):
+        """Causal prefill of one layer over its owner's prompt K / V [b][g][s_max][d]; Q / out
+        [b][s_max][h][d].  An owner layer stores K and V."""
+        return mlkv_q4_prefill(self.handle, layer, Q, K, V, out, prompt_lens, int(Q.shape[1]), window,
+                               sinks, stream)
+
+    def cache_bytes(self):
+        return mlkv_q4_bytes(self.handle)
+
+    def sync_status(self):
+        return mlkv_q4_sync_status(self.handle)
