@@ -6,11 +6,12 @@
 // x and s have 8-bit significands, so x / s is a half exactly or at least 2^-10 away from one (their
 // quotient's distance from n + 1/2 is a multiple of 1 / (2 S), S the scale's significand, shifted by
 // at most the quotient's own exponent).  x times the approximate reciprocal of s, raised by 2^-16 of
-// itself, is therefore on the right side of every half; the sum with 1.5 2^23 + 8 rounds it and leaves
-// the code in the low bits: one multiply-add a channel.  Likewise max |x| times fp32(1/7) rounds to the
+// itself, is therefore on the right side of every half; the sum of its magnitude and 1.5 2^23 rounds it
+// and leaves the code's magnitude in the low bits: one multiply-add a channel.  Likewise max |x| times fp32(1/7) rounds to the
 // same bf16 as the exact quotient, which is at least 2^-12 of itself away from a bf16 midpoint unless
 // it is a bf16.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -29,14 +30,16 @@ __device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b)
     return *reinterpret_cast<const uint32_t *>(&m);
 }
 
-// Eight channels of a group whose four lanes are neighbours (lane % 4): the sum of code << 4 i over
-// the channels' nibbles, and the scale's bits.
+// Eight channels of a group whose four lanes are neighbours (lane % 4).
 struct Coded {
-    uint32_t even, odd;   // channels 0, 2, 4, 6 and 1, 3, 5, 7, a nibble each (low 16 bits)
-    uint32_t quad[2];     // channels 0 .. 3 and 4 .. 7
-    uint32_t scale;       // bf16 bits
+    uint32_t k;        // as a K word
+    uint32_t v[2];     // as the even position's bits of the two V words (channels 0 .. 3, 4 .. 7)
+    uint32_t scale;    // bf16 bits
 };
 
+__device__ __forceinline__ uint32_t rotl(uint32_t w, int n) { return __funnelshift_l(w, w, n); }
+
+template <bool kK, bool kV>
 __device__ __forceinline__ Coded quantise8(uint4 x)
 {
     uint32_t m = max_abs2(max_abs2(x.x, x.y), max_abs2(x.z, x.w));
@@ -59,34 +62,44 @@ __device__ __forceinline__ Coded quantise8(uint4 x)
     uint32_t n[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        // a group with a NaN or an infinity takes code 8 (0) everywhere
+        // a group with a NaN or an infinity takes magnitude 0 everywhere
         const float v = (i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
-        n[i] = __float_as_uint(fmaf(r == 0.f ? 0.f : v, r, 12582912.f + 8.f)) & 15u;
+        n[i] = __float_as_uint(fmaf(r == 0.f ? 0.f : fabsf(v), r, 12582912.f)) & 7u;
     }
-    c.even = n[0] | n[2] << 4 | n[4] << 8 | n[6] << 12;
-    c.odd = n[1] | n[3] << 4 | n[5] << 8 | n[7] << 12;
-    c.quad[0] = n[0] | n[1] << 4 | n[2] << 8 | n[3] << 12;
-    c.quad[1] = n[4] | n[5] << 4 | n[6] << 8 | n[7] << 12;
+    c.k = 0u;
+    c.v[0] = c.v[1] = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t sign = (i & 1) ? w[i >> 1] & 0x80000000u : w[i >> 1] << 16 & 0x80000000u;
+        if (kK)
+            c.k |= n[i] << q4_mag(i >> 1, i & 1) | sign >> (31 - q4_sign(i >> 1, i & 1));
+        if (kV)
+            c.v[i >> 2] |= n[i] << q4_mag(i & 3, 0) | sign >> (31 - q4_sign(i & 3, 0));
+    }
     return c;
 }
 
-// One position's octet of a row, straight to its places in the row's block.
-template <int D>
-__device__ __forceinline__ void store_octet(uint8_t *row, int pos, int oct, bool is_v, const Coded &c)
+// One position's octet of a row, straight to its places in the row's block.  The V words it shares with
+// the other position of its pair are read, and belong to this thread alone in their kernel.
+template <int D, bool kIsV>
+__device__ __forceinline__ void store_octet(uint8_t *row, int pos, int oct, const Coded &c)
 {
     using LY = Q4Layout<D>;
     uint8_t *blk = row + static_cast<size_t>(pos / kQ4Block) * LY::kBytes;
     const int r = pos % kQ4Block, grp = oct >> 2, t = oct & 3;
-    if (is_v) {
+    if (kIsV) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
-            *reinterpret_cast<uint16_t *>(blk + LY::v_word(r, grp, 2 * t + q) + 2 * (r & 1)) =
-                static_cast<uint16_t>(c.quad[q]);
+        for (int q = 0; q < 2; ++q) {
+            uint32_t *at = reinterpret_cast<uint32_t *>(blk + LY::v_word(r, grp, 2 * t + q));
+            // the odd position's bits are the even one's rotated by half a word
+            const uint32_t mine = (r & 1) ? rotl(c.v[q], 16) : c.v[q];
+            *at = (*at & ~q4_bits(r & 1)) | mine;
+        }
     } else {
-        *reinterpret_cast<uint32_t *>(blk + LY::k_word(r, grp, t)) = c.even | c.odd << 16;
+        *reinterpret_cast<uint32_t *>(blk + LY::k_word(r, grp, t)) = c.k;
     }
     if (t == 0)
-        *reinterpret_cast<uint16_t *>(blk + (is_v ? LY::v_scale(r, grp) : LY::k_scale(r, grp))) =
+        *reinterpret_cast<uint16_t *>(blk + (kIsV ? LY::v_scale(r, grp) : LY::k_scale(r, grp))) =
             static_cast<uint16_t>(c.scale);
 }
 
@@ -108,9 +121,13 @@ __global__ void __launch_bounds__(128) q4_append_kernel(const __grid_constant__ 
     row -= is_v ? bg : 0;
     const uint4 x = *reinterpret_cast<const uint4 *>((is_v ? p.V : p.K) +
                                                      static_cast<size_t>(row) * D + oct * 8);
-    const Coded c = quantise8(x);
-    if (in)
-        store_octet<D>(p.slot + row * p.row_bytes, p.seq_len[row / p.g] - 1, oct, is_v, c);
+    uint8_t *dst = p.slot + row * p.row_bytes;
+    const int pos = p.seq_len[row / p.g] - 1;
+    const Coded c = quantise8<true, true>(x);
+    if (in && is_v)
+        store_octet<D, true>(dst, pos, oct, c);
+    else if (in)
+        store_octet<D, false>(dst, pos, oct, c);
 }
 
 constexpr int kTile = kQ4RowAlign;   // positions of one CTA of the store and of the read
@@ -143,57 +160,53 @@ __global__ void __launch_bounds__(256) q4_store_kernel(const __grid_constant__ Q
             x[kv][u] = i / kOct < n ? __ldcs(reinterpret_cast<const uint4 *>((kv ? p.V : p.K) + src) + i)
                                     : make_uint4(0, 0, 0, 0);
         }
-    if (n < kTile) {
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-            for (int u = 0; u < kTasks; ++u) {
-                const int i = u * 256 + tid;
-                const Coded c = quantise8(x[kv][u]);
-                if (i / kOct < n)
-                    store_octet<D>(dst, i / kOct, i % kOct, kv == 1, c);
-            }
-        return;
-    }
+    constexpr int kStep = 256 / kOct;   // a thread's positions: a step apart, in its own pair's place
+    const int oct = tid % kOct, grp = oct >> 2, t = oct & 3;
 #pragma unroll
     for (int u = 0; u < kTasks; ++u) {
-        const int i = u * 256 + tid;
-        const int pos = i / kOct, oct = i % kOct, grp = oct >> 2, t = oct & 3;
-        uint8_t *blk = img + pos / kQ4Block * LY::kBytes;
+        const int pos = u * kStep + tid / kOct;
+        uint8_t *blk = (n < kTile ? dst : img) + pos / kQ4Block * LY::kBytes;
         const int r = pos % kQ4Block;
-        Coded c = quantise8(x[0][u]);
-        *reinterpret_cast<uint32_t *>(blk + LY::k_word(r, grp, t)) = c.even | c.odd << 16;
-        if (t == 0)
-            *reinterpret_cast<uint16_t *>(blk + LY::k_scale(r, grp)) = static_cast<uint16_t>(c.scale);
-        c = quantise8(x[1][u]);
-        // the positions of a pair swap a quad: the even one stores words 2 t, the odd one 2 t + 1
+        const bool in = pos < n;
+        const Coded k = quantise8<true, false>(x[0][u]);
+        const Coded v = quantise8<false, true>(x[1][u]);
+        // The positions of a pair swap words: the even one stores word 2 t, the odd one 2 t + 1.
         const bool odd = r & 1;
-        const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? c.quad[0] : c.quad[1], kOct);
-        const uint32_t word = odd ? other | c.quad[1] << 16 : c.quad[0] | other << 16;
-        *reinterpret_cast<uint32_t *>(blk + LY::v_word(r, grp, 2 * t + (odd ? 1 : 0))) = word;
-        if (t == 0)
-            *reinterpret_cast<uint16_t *>(blk + LY::v_scale(r, grp)) = static_cast<uint16_t>(c.scale);
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? v.v[0] : v.v[1], kOct);
+        uint32_t word = odd ? other | rotl(v.v[1], 16) : v.v[0] | rotl(other, 16);
+        uint32_t *at = reinterpret_cast<uint32_t *>(blk + LY::v_word(r, grp, 2 * t + (odd ? 1 : 0)));
+        if (n < kTile) {
+            // the prefix ends inside the tile: what lies behind it keeps its bits
+            const bool even_in = (pos & ~1) < n, odd_in = (pos | 1) < n;
+            const uint32_t keep = (even_in ? 0u : q4_bits(0)) | (odd_in ? 0u : q4_bits(1));
+            if (even_in)
+                *at = (word & ~keep) | (keep != 0u ? *at & keep : 0u);
+        } else {
+            *at = word;
+        }
+        if (in) {
+            *reinterpret_cast<uint32_t *>(blk + LY::k_word(r, grp, t)) = k.k;
+            if (t == 0) {
+                *reinterpret_cast<uint16_t *>(blk + LY::k_scale(r, grp)) =
+                    static_cast<uint16_t>(k.scale);
+                *reinterpret_cast<uint16_t *>(blk + LY::v_scale(r, grp)) =
+                    static_cast<uint16_t>(v.scale);
+            }
+        }
     }
+    if (n < kTile)
+        return;
     __syncthreads();
     for (int i = tid; i < 4 * LY::kBytes / 16; i += 256)
         reinterpret_cast<uint4 *>(dst)[i] = reinterpret_cast<const uint4 *>(img)[i];
 }
 
-// Nibbles i and i + 4 of a word as a bf16 pair: the code's bits in the mantissa of 128, less 136.
-__device__ __forceinline__ uint32_t codes2(uint32_t w, int i)
+// Pair j of a word, times a scale each, as bf16: 3 x 8 significant bits, rounded once.
+__device__ __forceinline__ uint32_t values2(uint32_t w, int j, float s0, float s1)
 {
-    const uint32_t v = ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u;
-    const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162 *>(&v);
-    const __nv_bfloat162 y = __hsub2(x, __floats2bfloat162_rn(136.f, 136.f));
-    return *reinterpret_cast<const uint32_t *>(&y);
-}
-
-__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b)
-{
-    const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162 *>(&a);
-    const __nv_bfloat162 y = *reinterpret_cast<const __nv_bfloat162 *>(&b);
-    const __nv_bfloat162 z = __hmul2(x, y);   // 4 x 8 significant bits: rounded once, as in fp32
-    return *reinterpret_cast<const uint32_t *>(&z);
+    const uint32_t h = q4_pair(w, j);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+    return pack_bf16x2(f.x * kQ4Unit * s0, f.y * kQ4Unit * s1);
 }
 
 // A CTA brings the blocks of 64 positions of one (sequence, KV head) into shared memory and writes the
@@ -237,7 +250,8 @@ __global__ void __launch_bounds__(256) q4_read_kernel(const __grid_constant__ Q4
                     *reinterpret_cast<const uint32_t *>(blk + LY::v_word(r, grp, 2 * t + q));
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const uint32_t a = mul2(codes2(w, 2 * c), s), b = mul2(codes2(w, 2 * c + 1), s);
+                    const uint32_t a = values2(w, 2 * c, bf16_lo(s), bf16_hi(s));
+                    const uint32_t b = values2(w, 2 * c + 1, bf16_lo(s), bf16_hi(s));
                     v[0][2 * q + c] = __byte_perm(a, b, 0x5410);
                     v[1][2 * q + c] = __byte_perm(a, b, 0x7632);
                 }
@@ -245,13 +259,15 @@ __global__ void __launch_bounds__(256) q4_read_kernel(const __grid_constant__ Q4
         } else {
 #pragma unroll
             for (int o = 0; o < 2; ++o) {
-                const uint32_t s =
-                    *reinterpret_cast<const uint16_t *>(blk + LY::k_scale(r + o, grp)) * 0x10001u;
+                const float s = __uint_as_float(
+                    static_cast<uint32_t>(
+                        *reinterpret_cast<const uint16_t *>(blk + LY::k_scale(r + o, grp)))
+                    << 16);
                 const uint32_t w =
                     *reinterpret_cast<const uint32_t *>(blk + LY::k_word(r + o, grp, t));
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
-                    v[o][c] = mul2(codes2(w, c), s);
+                    v[o][c] = values2(w, c, s, s);
             }
         }
         __nv_bfloat16 *dst = (is_v ? p.V : p.K) +

@@ -2,20 +2,22 @@
 // kernels (mlkv_q4.cu, mlkv_q4_decode.cu).  Internal; not part of the public ABI.
 //
 // Value.  32 consecutive channels of one position of one KV head share a scale, s = bf16(max |x| / 7);
-// a channel is held as the whole number q in [-7, 7] nearest to x / s (halves away from zero), code
-// q + 8, and stands for q s.  A group with a NaN or an infinity holds NaN; one whose scale would be
-// below 2^-126 holds zeros.
+// a channel is held as the whole number q in [-7, 7] nearest to x / s (halves away from zero), as sign
+// and magnitude in 4 bits, and stands for q s.  A group with a NaN or an infinity holds NaN; one whose
+// scale would be below 2^-126 holds zeros.
 //
 // Layout.  [m slots][b][g] rows, each a run of blocks of 16 positions, 18 D bytes a block: the codes
 // of K (8 D), the codes of V (8 D), the scales of K (D), the scales of V (D).  Inside a block the codes
-// lie as the lanes of a warp want them for mma.m16n8k16, lane = 4 gid + tig, one 32-bit word a lane
-// holding four bf16 pairs once its nibbles i and i + 4 (bits 4 i and 16 + 4 i) are set apart:
-//   K, positions as the rows of A (gid, gid + 8): word (position, group, tig) holds the group's
-//     channels 8 tig .. 8 tig + 7, channel 8 tig + e in nibble e / 2 of half e % 2.
-//   V, channels as the rows of A, positions along k: word (position pair, group, gid) holds channels
-//     4 gid .. 4 gid + 3 of the group, channel 4 gid + i in nibble i, of the even position in the low
-//     half and of the odd one in the high half.  So one position owns whole 16-bit halves, and storing
-//     it reads nothing.
+// lie as the lanes of a warp (lane = 4 gid + tig) want them for the A operand of mma.m16n8k16, a 32-bit
+// word of 8 codes at a time.  A word as it is, rotated right by 4, shifted left by 8 and by 4, masked with
+// 0x87008700, is its pairs j = 0 .. 3 of fp16 numbers, the sign in the sign bit and the magnitude m in
+// bits 8 to 10: the top two mantissa bits and the lowest exponent bit, where subnormals and the first
+// binade make one scale of m 2^-16.  (The masks, moved back, tile the word.  Left shifts go to the
+// multiply-add pipe: the integer pipe, at half rate, is what bounds the unpacking.)
+//   K, positions as rows: word (position, group, tig) holds the group's channels 8 tig + e, pair j =
+//     e / 2, low half first.
+//   V, channels as rows: word (position pair, group, gid) holds channels 4 gid + j of the group, pair j
+//     the even position (low half) and the odd one (high half): their bits interleave in the word.
 // A lane's words of one 16-byte load are its groups (D = 128), or its two groups of both halves of the
 // block (D = 64).
 #pragma once
@@ -63,6 +65,25 @@ struct Q4Layout {
         return kVs + 2 * ((((((r & 7) >> 1) * 2 + (r >> 3)) * kGroups) + grp) * 2 + (r & 1));
     }
 };
+
+// A word's pair j, half o: mask, lowest bit of the magnitude, sign bit; the bits of half o of all pairs.
+constexpr uint32_t kQ4Mask = 0x87008700u;
+constexpr float kQ4Unit = 65536.f;   // what makes a magnitude whole
+__host__ __device__ constexpr int q4_mag(int j, int o)
+{
+    return 16 * o + (j == 0 ? 8 : j == 1 ? 12 : j == 2 ? 0 : 4);
+}
+__host__ __device__ constexpr int q4_sign(int j, int o) { return (q4_mag(j, o) + 7) & 31; }
+__host__ __device__ constexpr uint32_t q4_bits(int o) { return o ? 0xfff70008u : 0x0008fff7u; }
+
+#ifdef __CUDACC__
+// Pair j of a code word as fp16 in units of 2^-16.
+__device__ __forceinline__ uint32_t q4_pair(uint32_t w, int j)
+{
+    const uint32_t x = j == 0 ? w : j == 1 ? __funnelshift_r(w, w, 4) : j == 2 ? w * 256u : w * 16u;
+    return x & kQ4Mask;
+}
+#endif
 
 // Stores positions of K and V [b][g][len][D] (store) or of one new token [b][g][D] at seq_len - 1
 // (append) into one slot.

@@ -1,25 +1,27 @@
 // Single-token decode attention over the 4-bit KV cache (layout and values: mlkv_q4.h), with an
 // optional sliding window and sinks (MLKV, arXiv 2406.09297, Sec. 3; attention of Eqs. 2-3).
 //
-//   out = sum_t p_t v_t / sum_t p_t,  p_t = 2^(log2(e) q.k_t / sqrt(D) - m),  k_t = s_t (c_t - 8)
+//   out = sum_t p_t v_t / sum_t p_t,  p_t = 2^(log2(e) q.k_t / sqrt(D) - m)
 //
-// per group of 32 channels.  K and V are never widened: a word's nibbles become bf16 128 + c by one
-// mask-or each (the code's bits in the mantissa), which mma.m16n8k16 takes as its A operand straight
-// from registers (16 positions or 16 channels by 8 query heads).  The surplus of 136 a channel goes
-// into the accumulator it starts from:
-//   S:  acc = -136 sum_c q_c + sum_c (128 + c_tc) q_c, exact products, at most 32 terms; the group's
-//       scale multiplies the finished sum in fp32.
-//   O:  P'_t = bf16(p_t s_t) per group is the B operand; acc = -136 sum_t P'_t (an MMA with -136s for
-//       A, the same rounded P') + sum_t (128 + c_tc) P'_t over one tile, then added to O in fp32.
-// p is rounded to bf16 once for the transposition and the sum of weights, and once more with the
-// scale; both errors are relative, independent from position to position, and average out as the
-// bf16 weights of the other decode kernel do.
+// What bounds it: at 0.5625 bytes a channel HBM delivers ~42 channels per SM and clock, so unpacking is
+// the work to be saved.  K and V are never widened: one shift and one AND turn a quarter of a word of
+// 8 codes into a register of the A operand, fp16 with the code's magnitude in units of 2^-16 (mlkv_q4.h).
+//   S = K Q^T, 16 positions by 8 heads a group of 32 channels: exact codes, queries as fp16 scaled by a
+//       power of two per head to at most 2^15 (bf16's 8 bits fit; below 2^-29 of the head's largest
+//       magnitude bits are lost); fp32 sums, times the group's scale in fp32.
+//   O = V^T P^T, 16 channels by 8 heads.  The group's scale goes into P: P' = fp16(fp16(p) s / f), f a
+//       power of two that bounds the scales the warp has met (raised with a rescaled O, like the
+//       running maximum), so that fp16's range holds whatever the values' magnitude.
+// (Tried before.  Codes as bf16 128 + c, the surplus cancelled in the accumulators, P in bf16: as fast,
+// outputs 0.0024 to 0.0029 from the 64-bit ones instead of 0.0017.  K in e4m3: mma.sync takes 8-bit
+// operands apart again, 385 instructions per 16 positions of 128 channels and 8 heads.)
 //
 // Work split as in decode_kernel: the tiles of all (sequence, KV head) segments end to end, an equal run
 // of them for each persistent CTA; a CTA's warps take its tiles in turn, each through a ring of its own
 // (one bulk copy a tile: a block's codes and scales lie together), so nothing but the ends of
 // segments makes warps wait for one another.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -46,16 +48,24 @@ struct Q4Plan {
     static constexpr int kRow = D + 4;
     static constexpr int kRaw = kRing + kWarps * kStages * kTileBytes;
     static constexpr int kStat = kRaw + kWarps * 8 * kRow * 4;  // m, l [8 NB heads][kWarps] each
-    // The piece's queries, rows padded so that a quarter warp's 16-byte loads fall in distinct
-    // banks, and -136 times their group sums [group][16 heads].
-    static constexpr int kQRow = D * 2 + 64;
+    // The piece's queries as fp16, a lane's 8 channels of a group 16 bytes, the odd heads' halves of 128
+    // bytes swapped so that a quarter warp's loads fall in distinct banks; and what a head's products
+    // are to be multiplied with.
+    static constexpr int kQRow = 2 * D;
     static constexpr int kQ = kStat + 2 * 8 * NB * kWarps * 4;
-    static constexpr int kBias = kQ + 8 * NB * kQRow;
-    static constexpr int kFlags = kBias + LY::kGroups * 16 * 4;
+    static constexpr int kMul = kQ + 8 * NB * kQRow;
+    static constexpr int kVs = kMul + 8 * NB * 4;               // [kWarps][64] V scales, fp16 pairs
+    static constexpr int kFlags = kVs + kWarps * 256;
     static constexpr int kBars = kFlags + 16;
     static constexpr int kBytes = kBars + kWarps * kStages * 8;
+    static_assert(kSub * 8 * LY::kGroups == 64, "two words of V scales a lane");
     static_assert(kMinBlocks * (kBytes + 1024) <= 228 * 1024, "shared memory of the resident CTAs");
-    static_assert(kTileBytes % 128 == 0 && kRaw % 16 == 0 && kQ % 16 == 0 && kBars % 8 == 0, "");
+    static_assert(kTileBytes % 128 == 0 && kRaw % 16 == 0 && kQ % 16 == 0 && kVs % 16 == 0 &&
+                      kBars % 8 == 0, "");
+    __device__ static constexpr int q_at(int head, int group, int tig)
+    {
+        return kQ + head * kQRow + (((group * 4 + tig) ^ ((head & 1) * 4)) * 16);
+    }
 };
 
 // A (sequence, KV head) segment as the walk sees it.
@@ -120,35 +130,31 @@ __device__ __forceinline__ void tile_range(const Segment &s, int sinks, int tt, 
     end = sink ? sinks : s.L;
 }
 
-// D = A B + C with its own registers for D.
-__device__ __forceinline__ void mma_from(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
-                                         uint32_t a3, uint32_t b0, uint32_t b1, float c0, float c1,
-                                         float c2, float c3)
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                        uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 "
-        "{%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
-        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 "
+        "{%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ uint32_t hmul2_bf16(uint32_t a, uint32_t b)
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
 {
-    const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162 *>(&a);
-    const __nv_bfloat162 y = *reinterpret_cast<const __nv_bfloat162 *>(&b);
-    const __nv_bfloat162 z = __hmul2(x, y);
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+__device__ __forceinline__ uint32_t hmul2_f16(uint32_t a, uint32_t b)
+{
+    const __half2 x = *reinterpret_cast<const __half2 *>(&a);
+    const __half2 y = *reinterpret_cast<const __half2 *>(&b);
+    const __half2 z = __hmul2(x, y);
     return *reinterpret_cast<const uint32_t *>(&z);
-}
-
-// Nibbles i and i + 4 of a word as the bf16 pair 128 + code.
-__device__ __forceinline__ uint32_t codes_at(uint32_t w, int i)
-{
-    return ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u;
 }
 
 // Reference maxima move when a score exceeds them by more than this (log2 units): weights stay <= 2^8.
 constexpr float kQ4LazyMax = 8.f;
-constexpr uint32_t kOnes2 = 0x3f803f80u;
-constexpr uint32_t kMinus136 = 0xc308c308u;
 
 template <int D, int NB>
 __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBlocks)
@@ -200,11 +206,12 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
         f_tile += NW;
         ++f_it;
     };
-    // Queries of a segment: 16 bytes a thread; and the sums of their groups (four neighbours each).
-    constexpr int kQThreads = 8 * NB * (D / 8);
+    // Queries of a segment: 16 bytes (8 channels) a thread, a head's threads neighbours in a warp.
+    constexpr int kOct = D / 8;
+    constexpr int kQThreads = 8 * NB * kOct;
     static_assert(kQThreads <= PL::kThreads, "one load a thread");
     auto load_q = [&](const Segment &s) {
-        const int head = tid / (D / 8);
+        const int head = tid / kOct;
         uint4 v = make_uint4(0, 0, 0, 0);
         if (tid < kQThreads && head < p.G)
             v = *reinterpret_cast<const uint4 *>(
@@ -213,16 +220,32 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
         return v;
     };
     auto store_q = [&](const uint4 &v) {
-        const int head = tid / (D / 8), oct = tid % (D / 8);
-        float sum = (bf16_lo(v.x) + bf16_hi(v.x)) + (bf16_lo(v.y) + bf16_hi(v.y)) +
-                    ((bf16_lo(v.z) + bf16_hi(v.z)) + (bf16_lo(v.w) + bf16_hi(v.w)));
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        if (tid < kQThreads) {
-            *reinterpret_cast<uint4 *>(smem + PL::kQ + head * PL::kQRow + oct * 16) = v;
-            if ((oct & 3) == 0)
-                reinterpret_cast<float *>(smem + PL::kBias)[(oct >> 2) * 16 + head] = -136.f * sum;
+        if (tid >= kQThreads)   // whole warps
+            return;
+        const int head = tid / kOct, oct = tid % kOct;
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        // a row with a NaN or an infinity becomes NaN
+        auto bad_row = [](float m) { return !(m < __int_as_float(0x7f800000)); };
+        float x[8], mx = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] = (i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
+            mx = fmaxf(mx, bad_row(fabsf(x[i])) ? __int_as_float(0x7f800000) : fabsf(x[i]));
         }
+#pragma unroll
+        for (int m = 1; m < kOct; m <<= 1)
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, m));
+        // 2^e, the largest with mx 2^e < 2^15 (within limits that keep every factor finite)
+        const int e = max(-100, min(100, 14 - (static_cast<int>(__float_as_uint(mx) >> 23) - 127)));
+        const float up = __int_as_float((127 + e) << 23), down = __int_as_float((127 - e) << 23);
+        uint32_t y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            y[i] = bad_row(mx) ? 0x7fff7fffu : pack_f16x2(x[2 * i] * up, x[2 * i + 1] * up);
+        *reinterpret_cast<uint4 *>(smem + PL::q_at(head, oct >> 2, oct & 3)) =
+            make_uint4(y[0], y[1], y[2], y[3]);
+        if (oct == 0)
+            reinterpret_cast<float *>(smem + PL::kMul)[head] = p.scale_log2 * kQ4Unit * down;
     };
 
     grid_dependency_wait();
@@ -249,16 +272,24 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
             next_segment<T>(p, ns);
             q_next = load_q(ns);
         }
+        // A thread's statistics are those of heads 2 tig and 2 tig + 1 (la: over its own positions);
+        // O is in units of 2^-16 times the scales' bound.
         float o[NB][2 * NG][4];
-        float la[NB][4], m_run[NB][2];
+        float la[NB][2], m_run[NB][2], mul[NB][2];
+        float bound = 0x1p-100f, inv_bound = 0x1p100f;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
             for (int n = 0; n < 2 * NG; ++n)
                 o[nb][n][0] = o[nb][n][1] = o[nb][n][2] = o[nb][n][3] = 0.f;
-            la[nb][0] = la[nb][1] = la[nb][2] = la[nb][3] = 0.f;
+            la[nb][0] = la[nb][1] = 0.f;
             m_run[nb][0] = m_run[nb][1] = NEG_INF;
+            const float2 f =
+                *reinterpret_cast<const float2 *>(smem + PL::kMul + (8 * nb + 2 * tig) * 4);
+            mul[nb][0] = f.x;
+            mul[nb][1] = f.y;
         }
+        uint32_t *vscale = reinterpret_cast<uint32_t *>(smem + PL::kVs) + warp * 64;
         for (; tile < piece_end; tile += NW, ++it) {
             const int s = it % R;
             int ok = 1;
@@ -274,6 +305,45 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
             const int vis1 = end - pos0;
             const bool edge = vis0 > 0 || vis1 < T;
             if (__all_sync(0xffffffffu, ok)) {
+                // ---- the scales of V as fp16, over their bound: two pairs a lane ----
+                float2 vf[2];
+                float top = 0.f;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int k = lane + 32 * i, blk = k / (8 * NG), at = k % (8 * NG);
+                    const uint32_t w = *reinterpret_cast<const uint32_t *>(st + blk * LY::kBytes +
+                                                                           LY::kVs + at * 4);
+                    vf[i] = make_float2(bf16_lo(w), bf16_hi(w));
+                    if (edge) {
+                        // positions outside [vis0, vis1) hold anything, NaN scales among it
+                        const int r = 16 * blk + 8 * (at / NG & 1) + 2 * (at / (2 * NG));
+                        if (r < vis0 || r >= vis1)
+                            vf[i].x = 0.f;
+                        if (r + 1 < vis0 || r + 1 >= vis1)
+                            vf[i].y = 0.f;
+                    }
+                    top = fmaxf(top, fmaxf(vf[i].x, vf[i].y));
+                }
+                if (__any_sync(0xffffffffu, top > bound)) {
+#pragma unroll
+                    for (int m = 1; m < 32; m <<= 1)
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+                    // the power of two above it (scales are below 2^126)
+                    const uint32_t eb = (__float_as_uint(top) >> 23) + 1;
+                    const float down = bound * __uint_as_float((254u - eb) << 23);
+                    bound = __uint_as_float(eb << 23);
+                    inv_bound = __uint_as_float((254u - eb) << 23);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int n = 0; n < 2 * NG; ++n)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c)
+                                o[nb][n][c] *= down;
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    vscale[lane + 32 * i] = pack_f16x2(vf[i].x * inv_bound, vf[i].y * inv_bound);
                 // ---- S = K Q^T, 16 positions by 8 heads a block ----
                 float sc[NS][NB][4];
                 uint32_t kw[NS][2 * NG];       // [hi][group]
@@ -300,44 +370,35 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
                             kss[b][hi] = *reinterpret_cast<const uint32_t *>(ks);
                         }
                     }
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
-                        sc[b][nb][0] = sc[b][nb][1] = sc[b][nb][2] = sc[b][nb][3] = 0.f;
                 }
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
                     uint4 q[NB];
-                    float2 bias[NB];
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) {
-                        q[nb] = *reinterpret_cast<const uint4 *>(
-                            smem + PL::kQ + (8 * nb + gid) * PL::kQRow + g * 64 + tig * 16);
-                        bias[nb] = *reinterpret_cast<const float2 *>(
-                            smem + PL::kBias + (g * 16 + 8 * nb + 2 * tig) * 4);
-                    }
+                    for (int nb = 0; nb < NB; ++nb)
+                        q[nb] =
+                            *reinterpret_cast<const uint4 *>(smem + PL::q_at(8 * nb + gid, g, tig));
 #pragma unroll
                     for (int b = 0; b < NS; ++b) {
                         const uint32_t w0 = kw[b][g], w1 = kw[b][NG + g];
+                        const uint32_t a[8] = {q4_pair(w0, 0), q4_pair(w1, 0), q4_pair(w0, 1), q4_pair(w1, 1),
+                                               q4_pair(w0, 2), q4_pair(w1, 2), q4_pair(w0, 3), q4_pair(w1, 3)};
                         const uint32_t s0 = kss[b][g / 2], s1 = kss[b][NG / 2 + g / 2];
                         const float f0 = (g & 1) ? bf16_hi(s0) : bf16_lo(s0);
                         const float f1 = (g & 1) ? bf16_hi(s1) : bf16_lo(s1);
 #pragma unroll
                         for (int nb = 0; nb < NB; ++nb) {
-                            float t[4];
-                            mma_from(t, codes_at(w0, 0), codes_at(w1, 0), codes_at(w0, 1),
-                                     codes_at(w1, 1), q[nb].x, q[nb].y, bias[nb].x, bias[nb].y,
-                                     bias[nb].x, bias[nb].y);
-                            mma_from(t, codes_at(w0, 2), codes_at(w1, 2), codes_at(w0, 3),
-                                     codes_at(w1, 3), q[nb].z, q[nb].w, t[0], t[1], t[2], t[3]);
-                            sc[b][nb][0] = fmaf(t[0], f0, sc[b][nb][0]);
-                            sc[b][nb][1] = fmaf(t[1], f0, sc[b][nb][1]);
-                            sc[b][nb][2] = fmaf(t[2], f1, sc[b][nb][2]);
-                            sc[b][nb][3] = fmaf(t[3], f1, sc[b][nb][3]);
+                            float t[4] = {0.f, 0.f, 0.f, 0.f};
+                            mma_f16(t, a[0], a[1], a[2], a[3], q[nb].x, q[nb].y);
+                            mma_f16(t, a[4], a[5], a[6], a[7], q[nb].z, q[nb].w);
+                            sc[b][nb][0] = g == 0 ? t[0] * f0 : fmaf(t[0], f0, sc[b][nb][0]);
+                            sc[b][nb][1] = g == 0 ? t[1] * f0 : fmaf(t[1], f0, sc[b][nb][1]);
+                            sc[b][nb][2] = g == 0 ? t[2] * f1 : fmaf(t[2], f1, sc[b][nb][2]);
+                            sc[b][nb][3] = g == 0 ? t[3] * f1 : fmaf(t[3], f1, sc[b][nb][3]);
                         }
                     }
                 }
                 if (edge) {
-                    // Positions outside [vis0, vis1) hold anything, NaN scales among it.
 #pragma unroll
                     for (int b = 0; b < NS; ++b)
 #pragma unroll
@@ -360,8 +421,8 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
                         mx[0] = fmaxf(mx[0], fmaxf(sc[b][nb][0], sc[b][nb][2]));
                         mx[1] = fmaxf(mx[1], fmaxf(sc[b][nb][1], sc[b][nb][3]));
                     }
-                    const bool raise = mx[0] * p.scale_log2 > m_run[nb][0] + kQ4LazyMax ||
-                                       mx[1] * p.scale_log2 > m_run[nb][1] + kQ4LazyMax;
+                    const bool raise = mx[0] * mul[nb][0] > m_run[nb][0] + kQ4LazyMax ||
+                                       mx[1] * mul[nb][1] > m_run[nb][1] + kQ4LazyMax;
                     if (__any_sync(0xffffffffu, raise)) {
                         float alpha[2];
 #pragma unroll
@@ -369,9 +430,10 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
                             mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 4));
                             mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 8));
                             mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 16));
-                            const float m_new = fmaxf(m_run[nb][i], mx[i] * p.scale_log2);
+                            const float m_new = fmaxf(m_run[nb][i], mx[i] * mul[nb][i]);
                             alpha[i] = m_new == NEG_INF ? 1.f : fast_exp2(m_run[nb][i] - m_new);
                             m_run[nb][i] = m_new;
+                            la[nb][i] *= alpha[i];
                         }
 #pragma unroll
                         for (int n = 0; n < 2 * NG; ++n) {
@@ -380,85 +442,54 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
                             o[nb][n][2] *= alpha[0];
                             o[nb][n][3] *= alpha[1];
                         }
-                        la[nb][0] *= alpha[0];
-                        la[nb][1] *= alpha[1];
                     }
                     const float m0 = m_run[nb][0] == NEG_INF ? 0.f : m_run[nb][0];
                     const float m1 = m_run[nb][1] == NEG_INF ? 0.f : m_run[nb][1];
 #pragma unroll
                     for (int b = 0; b < NS; ++b) {
-                        const float p0 = fast_exp2(fmaf(sc[b][nb][0], p.scale_log2, -m0));
-                        const float p1 = fast_exp2(fmaf(sc[b][nb][1], p.scale_log2, -m1));
-                        const float p2 = fast_exp2(fmaf(sc[b][nb][2], p.scale_log2, -m0));
-                        const float p3 = fast_exp2(fmaf(sc[b][nb][3], p.scale_log2, -m1));
-                        pb[b][nb][0] = movmatrix_trans(pack_bf16x2(p0, p1));
-                        pb[b][nb][1] = movmatrix_trans(pack_bf16x2(p2, p3));
-                        mma_from(la[nb], kOnes2, kOnes2, kOnes2, kOnes2, pb[b][nb][0], pb[b][nb][1],
-                                 la[nb][0], la[nb][1], la[nb][2], la[nb][3]);
+                        const float p0 = fast_exp2(fmaf(sc[b][nb][0], mul[nb][0], -m0));
+                        const float p1 = fast_exp2(fmaf(sc[b][nb][1], mul[nb][1], -m1));
+                        const float p2 = fast_exp2(fmaf(sc[b][nb][2], mul[nb][0], -m0));
+                        const float p3 = fast_exp2(fmaf(sc[b][nb][3], mul[nb][1], -m1));
+                        la[nb][0] += p0 + p2;
+                        la[nb][1] += p1 + p3;
+                        pb[b][nb][0] = movmatrix_trans(pack_f16x2(p0, p1));
+                        pb[b][nb][1] = movmatrix_trans(pack_f16x2(p2, p3));
                     }
                 }
+                __syncwarp();   // the scales of V are in place
                 // ---- O += V^T (s P)^T ----
-                uint32_t vw[NS][2 * NG], vs[NS][2 * NG];   // [th][group]
 #pragma unroll
                 for (int b = 0; b < NS; ++b) {
                     const uint8_t *blk = st + b * LY::kBytes;
+                    uint32_t vw[2 * NG], vs[2 * NG];   // [th][group]
 #pragma unroll
                     for (int q = 0; q < 2 * NG / 4; ++q) {
                         const uint4 w =
                             *reinterpret_cast<const uint4 *>(blk + LY::kV + q * 512 + lane * 16);
-                        vw[b][4 * q] = w.x;
-                        vw[b][4 * q + 1] = w.y;
-                        vw[b][4 * q + 2] = w.z;
-                        vw[b][4 * q + 3] = w.w;
+                        vw[4 * q] = w.x;
+                        vw[4 * q + 1] = w.y;
+                        vw[4 * q + 2] = w.z;
+                        vw[4 * q + 3] = w.w;
                         const uint4 f = *reinterpret_cast<const uint4 *>(
-                            blk + LY::kVs + tig * NG * 8 + q * 16);
-                        vs[b][4 * q] = f.x;
-                        vs[b][4 * q + 1] = f.y;
-                        vs[b][4 * q + 2] = f.z;
-                        vs[b][4 * q + 3] = f.w;
+                            vscale + b * 8 * NG + tig * 2 * NG + q * 4);
+                        vs[4 * q] = f.x;
+                        vs[4 * q + 1] = f.y;
+                        vs[4 * q + 2] = f.z;
+                        vs[4 * q + 3] = f.w;
                     }
-                    if (edge) {
 #pragma unroll
-                        for (int th = 0; th < 2; ++th) {
-                            const int r = 16 * b + 8 * th + 2 * tig;
-                            const uint32_t keep = (r >= vis0 && r < vis1 ? 0x0000ffffu : 0u) |
-                                                  (r + 1 >= vis0 && r + 1 < vis1 ? 0xffff0000u : 0u);
+                    for (int g = 0; g < NG; ++g) {
+                        const uint32_t w0 = vw[g], w1 = vw[NG + g];
+                        const uint32_t a[8] = {q4_pair(w0, 0), q4_pair(w0, 1), q4_pair(w1, 0),
+                                               q4_pair(w1, 1), q4_pair(w0, 2), q4_pair(w0, 3),
+                                               q4_pair(w1, 2), q4_pair(w1, 3)};
 #pragma unroll
-                            for (int g = 0; g < NG; ++g)
-                                vs[b][th * NG + g] &= keep;
-                        }
-                    }
-                }
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    uint32_t pv[NS][NB][2];
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) {
-                        float t0[4] = {0.f, 0.f, 0.f, 0.f}, t1[4];
-#pragma unroll
-                        for (int b = 0; b < NS; ++b) {
-                            pv[b][nb][0] = hmul2_bf16(pb[b][nb][0], vs[b][g]);
-                            pv[b][nb][1] = hmul2_bf16(pb[b][nb][1], vs[b][NG + g]);
-                            mma_from(t0, kMinus136, kMinus136, kMinus136, kMinus136, pv[b][nb][0],
-                                     pv[b][nb][1], t0[0], t0[1], t0[2], t0[3]);
-                        }
-#pragma unroll
-                        for (int c = 0; c < 4; ++c)
-                            t1[c] = t0[c];
-#pragma unroll
-                        for (int b = 0; b < NS; ++b) {
-                            const uint32_t w0 = vw[b][g], w1 = vw[b][NG + g];
-                            mma_from(t0, codes_at(w0, 0), codes_at(w0, 1), codes_at(w1, 0),
-                                     codes_at(w1, 1), pv[b][nb][0], pv[b][nb][1], t0[0], t0[1], t0[2],
-                                     t0[3]);
-                            mma_from(t1, codes_at(w0, 2), codes_at(w0, 3), codes_at(w1, 2),
-                                     codes_at(w1, 3), pv[b][nb][0], pv[b][nb][1], t1[0], t1[1], t1[2],
-                                     t1[3]);
-                        }
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            o[nb][2 * g][c] += t0[c];
-                            o[nb][2 * g + 1][c] += t1[c];
+                        for (int nb = 0; nb < NB; ++nb) {
+                            const uint32_t b0 = hmul2_f16(pb[b][nb][0], vs[g]);
+                            const uint32_t b1 = hmul2_f16(pb[b][nb][1], vs[NG + g]);
+                            mma_f16(o[nb][2 * g], a[0], a[1], a[2], a[3], b0, b1);
+                            mma_f16(o[nb][2 * g + 1], a[4], a[5], a[6], a[7], b0, b1);
                         }
                     }
                 }
@@ -476,8 +507,16 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
         const size_t rec = static_cast<size_t>(seg) + cta;
         __nv_bfloat16 *ob =
             p.out + (static_cast<size_t>(cs.beta) * p.h + static_cast<size_t>(cs.j) * G) * D;
+        // out of the units of the codes and of the scales' bound (whose product may pass fp32's range)
+        auto whole_units = [&](float x) { return x * kQ4Unit * bound; };
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                la[nb][i] += __shfl_xor_sync(0xffffffffu, la[nb][i], 4);
+                la[nb][i] += __shfl_xor_sync(0xffffffffu, la[nb][i], 8);
+                la[nb][i] += __shfl_xor_sync(0xffffffffu, la[nb][i], 16);
+            }
             if (nb > 0 && G <= 8 * nb)
                 break;
             if (nb > 0)
@@ -488,8 +527,9 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
 #pragma unroll
                 for (int g = 0; g < NG; ++g)
                     *reinterpret_cast<float4 *>(dst + g * 32) =
-                        make_float4(o[nb][2 * g][i], o[nb][2 * g][2 + i], o[nb][2 * g + 1][i],
-                                    o[nb][2 * g + 1][2 + i]);
+                        make_float4(whole_units(o[nb][2 * g][i]), whole_units(o[nb][2 * g][2 + i]),
+                                    whole_units(o[nb][2 * g + 1][i]),
+                                    whole_units(o[nb][2 * g + 1][2 + i]));
                 if (gid == 0) {
                     st_m[(8 * nb + 2 * tig + i) * NW + warp] = m_run[nb][i];
                     st_l[(8 * nb + 2 * tig + i) * NW + warp] = la[nb][i];
