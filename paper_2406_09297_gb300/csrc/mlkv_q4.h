@@ -119,6 +119,7 @@ struct Q4DecodeParams {
     int b, h, g, G;
     int window, sinks;
     int num_tiles;
+    int empty_tiles;           // of the tiles: empty ones behind every segment's, its ends' cost
     int uniform_len;           // the common length, or 0
     int deferred_merge;        // 1: combine_kernel merges the records
     int seq_len[MLKV_MAX_BATCH];
@@ -127,6 +128,9 @@ struct Q4DecodeParams {
 // Positions per tile of the decode kernel, and its launch.
 constexpr int q4_tile_tokens(int d) { return d == 128 ? 32 : 64; }
 cudaError_t prepare_q4_decode(int d, int group, int *ctas_per_sm);
-cudaError_t launch_q4_decode(int d, int grid, const Q4DecodeParams &p, cudaStream_t stream);
+constexpr int q4_warps(int group) { return group <= 8 ? 8 : 6; }   // of a CTA
+// warp_runs: P = grid x warps runs of tiles, a warp each; else P = grid, a CTA each (see the kernel).
+cudaError_t launch_q4_decode(int d, int grid, bool warp_runs, const Q4DecodeParams &p,
+                             cudaStream_t stream);
 
 }  // namespace mlkv

@@ -17,9 +17,11 @@
 // operands apart again, 385 instructions per 16 positions of 128 channels and 8 heads.)
 //
 // Work split as in decode_kernel: the tiles of all (sequence, KV head) segments end to end, an equal run
-// of them for each persistent CTA; a CTA's warps take its tiles in turn, each through a ring of its own
-// (one bulk copy a tile: a block's codes and scales lie together), so nothing but the ends of
-// segments makes warps wait for one another.
+// of them for each persistent worker, the part of a segment in one run a piece.  Every warp has a ring of
+// its own (one bulk copy a tile: a block's codes and scales lie together).  With many tiles a worker is
+// a warp, which meets no other until it stores its pieces: no barrier, and a piece of a few tiles costs
+// its warp a round trip or two while the others stream.  With few, a CTA is, whose warps take its tiles
+// in turn and merge their sums at the ends of pieces: fewer records for long segments.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -32,10 +34,12 @@
 namespace mlkv {
 namespace {
 
-template <int D, int NB>
+// kWarpRuns: every warp has a run of tiles, and the queries of its segment, of its own; else a CTA's warps
+// share both.
+template <int D, int NB, bool kWarpRuns>
 struct Q4Plan {
     using LY = Q4Layout<D>;
-    static constexpr int kWarps = 8;
+    static constexpr int kWarps = q4_warps(8 * NB);
     static constexpr int kThreads = kWarps * 32;
     static constexpr int kT = q4_tile_tokens(D);
     static constexpr int kSub = kT / kQ4Block;                  // blocks of a tile
@@ -43,25 +47,27 @@ struct Q4Plan {
     static constexpr int kTileBytes = kSub * LY::kBytes;
     static constexpr int kMinBlocks = 2;
     static constexpr int kRing = 0;                             // [kWarps][kStages]
-    // A piece's sums of 8 heads from every warp; rows padded so that the fragments' 16-byte stores
-    // fall in distinct banks.
-    static constexpr int kRow = D + 4;
-    static constexpr int kRaw = kRing + kWarps * kStages * kTileBytes;
-    static constexpr int kStat = kRaw + kWarps * 8 * kRow * 4;  // m, l [8 NB heads][kWarps] each
-    // The piece's queries as fp16, a lane's 8 channels of a group 16 bytes, the odd heads' halves of 128
-    // bytes swapped so that a quarter warp's loads fall in distinct banks; and what a head's products
-    // are to be multiplied with.
+    // The queries as fp16, a lane's 8 channels of a group 16 bytes, the odd heads' halves of 128 bytes
+    // swapped so that a quarter warp's loads fall in distinct banks; and what a head's products are to
+    // be multiplied with.
+    static constexpr int kQSets = kWarpRuns ? kWarps : 1;
     static constexpr int kQRow = 2 * D;
-    static constexpr int kQ = kStat + 2 * 8 * NB * kWarps * 4;
-    static constexpr int kMul = kQ + 8 * NB * kQRow;
-    static constexpr int kVs = kMul + 8 * NB * 4;               // [kWarps][64] V scales, fp16 pairs
-    static constexpr int kFlags = kVs + kWarps * 256;
-    static constexpr int kBars = kFlags + 16;
-    static constexpr int kBytes = kBars + kWarps * kStages * 8;
+    static constexpr int kQ = kRing + kWarps * kStages * kTileBytes;
+    static constexpr int kQSet = 8 * NB * kQRow;
+    static constexpr int kMul = kQ + kQSets * kQSet;
+    static constexpr int kVs = kMul + kQSets * 8 * NB * 4;      // [kWarps][64] V scales, fp16 pairs
+    static constexpr int kBars = kVs + kWarps * 256;
+    static constexpr int kFlags = kBars + kWarps * kStages * 8;
+    // Shared runs: a piece's sums of 8 heads from every warp, rows padded so that the fragments' 16-byte
+    // stores fall in distinct banks, and m, l [8 NB heads][kWarps].
+    static constexpr int kRow = D + 4;
+    static constexpr int kRaw = kFlags + 16;
+    static constexpr int kStat = kRaw + (kWarpRuns ? 0 : kWarps * 8 * kRow * 4);
+    static constexpr int kBytes = kStat + (kWarpRuns ? 0 : 2 * 8 * NB * kWarps * 4);
     static_assert(kSub * 8 * LY::kGroups == 64, "two words of V scales a lane");
     static_assert(kMinBlocks * (kBytes + 1024) <= 228 * 1024, "shared memory of the resident CTAs");
-    static_assert(kTileBytes % 128 == 0 && kRaw % 16 == 0 && kQ % 16 == 0 && kVs % 16 == 0 &&
-                      kBars % 8 == 0, "");
+    static_assert(kTileBytes % 128 == 0 && kQ % 16 == 0 && kVs % 16 == 0 && kBars % 8 == 0 &&
+                      kRaw % 16 == 0, "");
     __device__ static constexpr int q_at(int head, int group, int tig)
     {
         return kQ + head * kQRow + (((group * 4 + tig) ^ ((head & 1) * 4)) * 16);
@@ -71,7 +77,7 @@ struct Q4Plan {
 // A (sequence, KV head) segment as the walk sees it.
 struct Segment {
     int beta, j, L;
-    int first;            // its first tile in the flattened list
+    int first, nt;        // its first tile in the flattened list, its tiles with the empty ones behind
     VisibleTiles v;
 };
 
@@ -80,6 +86,7 @@ __device__ __forceinline__ void load_segment(const Q4DecodeParams &p, Segment &s
 {
     s.L = p.uniform_len > 0 ? p.uniform_len : p.seq_len[s.beta];
     s.v = visible_tiles(s.L, p.window, p.sinks, T, kQ4Block);
+    s.nt = s.v.nt + p.empty_tiles;
 }
 
 template <int T>
@@ -89,10 +96,10 @@ __device__ __forceinline__ Segment segment_of_tile(const Q4DecodeParams &p, int 
     if (p.uniform_len > 0) {
         s.beta = 0;
         load_segment<T>(p, s);
-        const int seg = tile / s.v.nt;
+        const int seg = tile / s.nt;
         s.beta = seg / p.g;
         s.j = seg - s.beta * p.g;
-        s.first = seg * s.v.nt;
+        s.first = seg * s.nt;
         return s;
     }
     int lo = 0, hi = p.b - 1;
@@ -105,15 +112,15 @@ __device__ __forceinline__ Segment segment_of_tile(const Q4DecodeParams &p, int 
     }
     s.beta = lo;
     load_segment<T>(p, s);
-    s.j = (tile - p.tile_start[lo]) / s.v.nt;
-    s.first = p.tile_start[lo] + s.j * s.v.nt;
+    s.j = (tile - p.tile_start[lo]) / s.nt;
+    s.first = p.tile_start[lo] + s.j * s.nt;
     return s;
 }
 
 template <int T>
 __device__ __forceinline__ void next_segment(const Q4DecodeParams &p, Segment &s)
 {
-    s.first += s.v.nt;
+    s.first += s.nt;
     if (++s.j == p.g) {
         s.j = 0;
         if (++s.beta < p.b && p.uniform_len <= 0)
@@ -156,11 +163,12 @@ __device__ __forceinline__ uint32_t hmul2_f16(uint32_t a, uint32_t b)
 // Reference maxima move when a score exceeds them by more than this (log2 units): weights stay <= 2^8.
 constexpr float kQ4LazyMax = 8.f;
 
-template <int D, int NB>
-__global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBlocks)
+template <int D, int NB, bool kWarpRuns>
+__global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
+                                  Q4Plan<D, NB, kWarpRuns>::kMinBlocks)
     q4_decode_kernel(const __grid_constant__ Q4DecodeParams p)
 {
-    using PL = Q4Plan<D, NB>;
+    using PL = Q4Plan<D, NB, kWarpRuns>;
     using LY = Q4Layout<D>;
     constexpr int NW = PL::kWarps, T = PL::kT, NS = PL::kSub, NG = LY::kGroups, R = PL::kStages;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -168,61 +176,70 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
     volatile int *flags = reinterpret_cast<volatile int *>(smem + PL::kFlags);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int gid = lane >> 2, tig = lane & 3;
-    const int P = gridDim.x, cta = blockIdx.x, N = p.num_tiles;
-    const int tile_lo = static_cast<int>(static_cast<long long>(cta) * N / P);
-    const int tile_hi = static_cast<int>(static_cast<long long>(cta + 1) * N / P);
+    // run `run` of P: tiles [tile_lo, tile_hi), of which this warp takes every kStep-th
+    const int P = gridDim.x * (kWarpRuns ? NW : 1), N = p.num_tiles;
+    const int run = kWarpRuns ? blockIdx.x * NW + warp : blockIdx.x;
+    const int tile_lo = static_cast<int>(static_cast<long long>(run) * N / P);
+    const int tile_hi = static_cast<int>(static_cast<long long>(run + 1) * N / P);
+    constexpr int kStep = kWarpRuns ? 1 : NW;
+    const int tile_first = tile_lo + (kWarpRuns ? 0 : warp);
     const uint32_t ring = sbase + PL::kRing + warp * R * PL::kTileBytes;
     const uint32_t bar_full = sbase + PL::kBars + warp * R * 8;
+    // this warp's queries and their factors
+    const uint8_t *q_set = smem + (kWarpRuns ? warp * PL::kQSet : 0);
+    float *q_mul = reinterpret_cast<float *>(smem + PL::kMul) + (kWarpRuns ? warp * 8 * NB : 0);
+    bool expired = false;   // a wait gave up
     const float NEG_INF = -__int_as_float(0x7f800000);
     if (lane == 0) {
         for (int s = 0; s < R; ++s)
             mbar_init(bar_full + 8 * s, 1);
-        if (warp == 0)
-            flags[0] = 0;
         fence_barrier_init();
     }
     __syncwarp();
 
-    // The warp's tiles: tile_lo + warp, + NW, ...  Lane 0 sends each tile's copy R tiles ahead.
+    // Lane 0 sends the copies of the warp's tiles R ahead.
     Segment fs = segment_of_tile<T>(p, tile_lo < N ? tile_lo : N - 1);
-    int f_tile = tile_lo + warp, f_it = 0;
+    int f_tile = tile_first, f_it = 0;
     auto fetch = [&]() {
-        if (f_tile >= tile_hi)
+        if (lane != 0)
             return;
-        while (f_tile >= fs.first + fs.v.nt)
-            next_segment<T>(p, fs);
-        if (lane == 0) {
+        for (; f_tile < tile_hi; f_tile += kStep) {
+            while (f_tile >= fs.first + fs.nt)
+                next_segment<T>(p, fs);
+            const int tt = f_tile - fs.first;
+            if (tt >= fs.v.nt)
+                continue;   // an empty tile
             int pos0, end;
-            tile_range<T>(fs, p.sinks, f_tile - fs.first, pos0, end);
+            tile_range<T>(fs, p.sinks, tt, pos0, end);
             const int n = min(NS, (end - pos0 + kQ4Block - 1) / kQ4Block);
             const uint32_t bytes = static_cast<uint32_t>(n) * LY::kBytes;
-            const uint32_t bar = bar_full + 8 * (f_it % R);
-            mbar_arrive_expect_tx(bar, bytes);
-            bulk_load(ring + (f_it % R) * PL::kTileBytes,
+            const int s = f_it % R;
+            mbar_arrive_expect_tx(bar_full + 8 * s, bytes);
+            bulk_load(ring + s * PL::kTileBytes,
                       p.slot + (static_cast<long long>(fs.beta) * p.g + fs.j) * p.row_bytes +
                           static_cast<long long>(pos0 / kQ4Block) * LY::kBytes,
-                      bytes, bar);
+                      bytes, bar_full + 8 * s);
+            f_tile += kStep;
+            ++f_it;
+            return;
         }
-        f_tile += NW;
-        ++f_it;
     };
-    // Queries of a segment: 16 bytes (8 channels) a thread, a head's threads neighbours in a warp.
+    // Queries of a segment: 16 bytes (8 channels) `i` of them, a head's in neighbouring lanes.
     constexpr int kOct = D / 8;
-    constexpr int kQThreads = 8 * NB * kOct;
-    static_assert(kQThreads <= PL::kThreads, "one load a thread");
-    auto load_q = [&](const Segment &s) {
-        const int head = tid / kOct;
+    constexpr int kQLoads = 8 * NB * kOct;
+    constexpr int kQPer = (kQLoads + PL::kThreads - 1) / PL::kThreads;   // shared runs: a thread's
+    auto load_q = [&](const Segment &s, int i) {
         uint4 v = make_uint4(0, 0, 0, 0);
-        if (tid < kQThreads && head < p.G)
+        if (i < kQLoads && i / kOct < p.G)
             v = *reinterpret_cast<const uint4 *>(
                 p.Q + (static_cast<size_t>(s.beta) * p.h + static_cast<size_t>(s.j) * p.G) * D +
-                tid * 8);
+                i * 8);
         return v;
     };
-    auto store_q = [&](const uint4 &v) {
-        if (tid >= kQThreads)   // whole warps
+    auto store_q = [&](const uint4 &v, int i) {
+        const int head = i / kOct, oct = i % kOct;
+        if (i >= kQLoads || head >= p.G)   // whole heads
             return;
-        const int head = tid / kOct, oct = tid % kOct;
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
         // a row with a NaN or an infinity becomes NaN
         auto bad_row = [](float m) { return !(m < __int_as_float(0x7f800000)); };
@@ -232,9 +249,11 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
             x[i] = (i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
             mx = fmaxf(mx, bad_row(fabsf(x[i])) ? __int_as_float(0x7f800000) : fabsf(x[i]));
         }
+        // a head's kOct lanes
+        const uint32_t peers = (kOct == 16 ? 0xffffu : 0xffu) << (lane & ~(kOct - 1));
 #pragma unroll
         for (int m = 1; m < kOct; m <<= 1)
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, m));
+            mx = fmaxf(mx, __shfl_xor_sync(peers, mx, m));
         // 2^e, the largest with mx 2^e < 2^15 (within limits that keep every factor finite)
         const int e = max(-100, min(100, 14 - (static_cast<int>(__float_as_uint(mx) >> 23) - 127)));
         const float up = __int_as_float((127 + e) << 23), down = __int_as_float((127 - e) << 23);
@@ -242,40 +261,98 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             y[i] = bad_row(mx) ? 0x7fff7fffu : pack_f16x2(x[2 * i] * up, x[2 * i + 1] * up);
-        *reinterpret_cast<uint4 *>(smem + PL::q_at(head, oct >> 2, oct & 3)) =
+        *reinterpret_cast<uint4 *>(const_cast<uint8_t *>(q_set) + PL::q_at(head, oct >> 2, oct & 3)) =
             make_uint4(y[0], y[1], y[2], y[3]);
         if (oct == 0)
-            reinterpret_cast<float *>(smem + PL::kMul)[head] = p.scale_log2 * kQ4Unit * down;
+            q_mul[head] = p.scale_log2 * kQ4Unit * down;
     };
+    // A warp's own queries: all its loads, then their conversion.
+    struct WarpQ {
+        uint4 v[kQLoads / 32];
+    };
+    const int q_n = (p.G * kOct + 31) / 32;
+    auto load_warp_q = [&](const Segment &s, WarpQ &q) {
+#pragma unroll
+        for (int i = 0; i < kQLoads / 32; ++i)
+            if (i < q_n)
+                q.v[i] = load_q(s, 32 * i + lane);
+    };
+    auto store_warp_q = [&](const WarpQ &q) {
+#pragma unroll
+        for (int i = 0; i < kQLoads / 32; ++i)
+            if (i < q_n)
+                store_q(q.v[i], 32 * i + lane);
+        __syncwarp();
+    };
+    // The heads past the group's: zeros once.
+    {
+        const int n = kWarpRuns ? 32 : PL::kThreads;
+        for (int i = (kWarpRuns ? lane : tid) + p.G * kOct; i < kQLoads; i += n) {
+            const int head = i / kOct, oct = i % kOct;
+            *reinterpret_cast<uint4 *>(const_cast<uint8_t *>(q_set) +
+                                       PL::q_at(head, oct >> 2, oct & 3)) = make_uint4(0, 0, 0, 0);
+            if (oct == 0)
+                q_mul[head] = 1.f;
+        }
+    }
 
     grid_dependency_wait();
     grid_dependents_launch();
     if (tile_lo >= tile_hi)
         return;
+    // The first queries before the first tiles: behind the whole GPU's first tiles they took 4 us.
     Segment cs = segment_of_tile<T>(p, tile_lo);
+    if constexpr (kWarpRuns) {
+        WarpQ q;
+        load_warp_q(cs, q);
 #pragma unroll
-    for (int s = 0; s < R; ++s)
-        fetch();
-    store_q(load_q(cs));
-    __syncthreads();
+        for (int s = 0; s < R; ++s)
+            fetch();
+        store_warp_q(q);
+    } else {
+        uint4 q[kQPer];
+#pragma unroll
+        for (int i = 0; i < kQPer; ++i)
+            q[i] = load_q(cs, tid + i * PL::kThreads);
+#pragma unroll
+        for (int s = 0; s < R; ++s)
+            fetch();
+#pragma unroll
+        for (int i = 0; i < kQPer; ++i)
+            store_q(q[i], tid + i * PL::kThreads);
+        __syncthreads();
+    }
 
     int it = 0;                       // this warp's tiles so far
-    int tile = tile_lo + warp;
+    int tile = tile_first;
     for (int piece = tile_lo; piece < tile_hi;) {
-        const int seg_end = cs.first + cs.v.nt;
+        const int seg_end = cs.first + cs.nt;
         const int piece_end = min(seg_end, tile_hi);
         const bool last = piece_end == tile_hi;
-        // the next piece's queries travel while this one is computed
         Segment ns = cs;
-        uint4 q_next = make_uint4(0, 0, 0, 0);
-        if (!last) {
+        if (!last)
             next_segment<T>(p, ns);
-            q_next = load_q(ns);
+        // (shared runs: the next piece's queries travel while this one is computed)
+        uint4 q_next[kQPer] = {};
+        if (!last) {
+            if constexpr (kWarpRuns) {
+                // the next piece's queries to L2
+                if (lane * 64 < p.G * D)
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(
+                        p.Q + (static_cast<size_t>(ns.beta) * p.h + static_cast<size_t>(ns.j) * p.G) * D +
+                        lane * 64));
+            } else {
+#pragma unroll
+                for (int i = 0; i < kQPer; ++i)
+                    q_next[i] = load_q(ns, tid + i * PL::kThreads);
+            }
         }
         // A thread's statistics are those of heads 2 tig and 2 tig + 1 (la: over its own positions);
         // O is in units of 2^-16 times the scales' bound.
         float o[NB][2 * NG][4];
-        float la[NB][2], m_run[NB][2], mul[NB][2];
+        // A head's reference maximum is -nm, in log2 units; it moves when a product exceeds `top`
+        // (products times mul are log2 units).  Without one yet top is -inf and nm 0.
+        float la[NB][2], nm[NB][2], top[NB][2], mul[NB][2];
         float bound = 0x1p-100f, inv_bound = 0x1p100f;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -283,19 +360,21 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
             for (int n = 0; n < 2 * NG; ++n)
                 o[nb][n][0] = o[nb][n][1] = o[nb][n][2] = o[nb][n][3] = 0.f;
             la[nb][0] = la[nb][1] = 0.f;
-            m_run[nb][0] = m_run[nb][1] = NEG_INF;
-            const float2 f =
-                *reinterpret_cast<const float2 *>(smem + PL::kMul + (8 * nb + 2 * tig) * 4);
+            nm[nb][0] = nm[nb][1] = 0.f;
+            top[nb][0] = top[nb][1] = NEG_INF;
+            const float2 f = *reinterpret_cast<const float2 *>(q_mul + 8 * nb + 2 * tig);
             mul[nb][0] = f.x;
             mul[nb][1] = f.y;
         }
         uint32_t *vscale = reinterpret_cast<uint32_t *>(smem + PL::kVs) + warp * 64;
-        for (; tile < piece_end; tile += NW, ++it) {
+        for (; tile < piece_end; tile += kStep, ++it) {
             const int s = it % R;
-            int ok = 1;
-            if (!mbar_wait(bar_full + 8 * s, (it / R) & 1)) {
-                ok = 0;
-                flags[0] = 1;
+            if (tile - cs.first >= cs.v.nt) {
+                --it;
+                continue;   // an empty tile
+            }
+            if (!expired && !mbar_wait(bar_full + 8 * s, (it / R) & 1)) {
+                expired = true;   // the status says so; what follows is whatever the ring holds
                 atomicOr(p.err, kErrWaitFull);
             }
             const uint8_t *st = smem + PL::kRing + (warp * R + s) * PL::kTileBytes;
@@ -304,10 +383,10 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
             const int vis0 = (tile - cs.first < cs.v.ns ? 0 : cs.v.first) - pos0;   // visible: [vis0, vis1)
             const int vis1 = end - pos0;
             const bool edge = vis0 > 0 || vis1 < T;
-            if (__all_sync(0xffffffffu, ok)) {
+            {
                 // ---- the scales of V as fp16, over their bound: two pairs a lane ----
                 float2 vf[2];
-                float top = 0.f;
+                float peak = 0.f;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int k = lane + 32 * i, blk = k / (8 * NG), at = k % (8 * NG);
@@ -322,14 +401,14 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
                         if (r + 1 < vis0 || r + 1 >= vis1)
                             vf[i].y = 0.f;
                     }
-                    top = fmaxf(top, fmaxf(vf[i].x, vf[i].y));
+                    peak = fmaxf(peak, fmaxf(vf[i].x, vf[i].y));
                 }
-                if (__any_sync(0xffffffffu, top > bound)) {
+                if (__any_sync(0xffffffffu, peak > bound)) {
 #pragma unroll
                     for (int m = 1; m < 32; m <<= 1)
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+                        peak = fmaxf(peak, __shfl_xor_sync(0xffffffffu, peak, m));
                     // the power of two above it (scales are below 2^126)
-                    const uint32_t eb = (__float_as_uint(top) >> 23) + 1;
+                    const uint32_t eb = (__float_as_uint(peak) >> 23) + 1;
                     const float down = bound * __uint_as_float((254u - eb) << 23);
                     bound = __uint_as_float(eb << 23);
                     inv_bound = __uint_as_float((254u - eb) << 23);
@@ -377,7 +456,7 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb)
                         q[nb] =
-                            *reinterpret_cast<const uint4 *>(smem + PL::q_at(8 * nb + gid, g, tig));
+                            *reinterpret_cast<const uint4 *>(q_set + PL::q_at(8 * nb + gid, g, tig));
 #pragma unroll
                     for (int b = 0; b < NS; ++b) {
                         const uint32_t w0 = kw[b][g], w1 = kw[b][NG + g];
@@ -421,8 +500,7 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
                         mx[0] = fmaxf(mx[0], fmaxf(sc[b][nb][0], sc[b][nb][2]));
                         mx[1] = fmaxf(mx[1], fmaxf(sc[b][nb][1], sc[b][nb][3]));
                     }
-                    const bool raise = mx[0] * mul[nb][0] > m_run[nb][0] + kQ4LazyMax ||
-                                       mx[1] * mul[nb][1] > m_run[nb][1] + kQ4LazyMax;
+                    const bool raise = mx[0] > top[nb][0] || mx[1] > top[nb][1];
                     if (__any_sync(0xffffffffu, raise)) {
                         float alpha[2];
 #pragma unroll
@@ -430,9 +508,14 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
                             mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 4));
                             mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 8));
                             mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 16));
-                            const float m_new = fmaxf(m_run[nb][i], mx[i] * mul[nb][i]);
-                            alpha[i] = m_new == NEG_INF ? 1.f : fast_exp2(m_run[nb][i] - m_new);
-                            m_run[nb][i] = m_new;
+                            const float m_old = top[nb][i] == NEG_INF ? NEG_INF : -nm[nb][i];
+                            const float m_new = fmaxf(m_old, mx[i] * mul[nb][i]);
+                            alpha[i] = 1.f;
+                            if (m_new != NEG_INF) {
+                                alpha[i] = fast_exp2(m_old - m_new);
+                                nm[nb][i] = -m_new;
+                                top[nb][i] = (m_new + kQ4LazyMax) * fast_rcp(mul[nb][i]);
+                            }
                             la[nb][i] *= alpha[i];
                         }
 #pragma unroll
@@ -443,14 +526,12 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
                             o[nb][n][3] *= alpha[1];
                         }
                     }
-                    const float m0 = m_run[nb][0] == NEG_INF ? 0.f : m_run[nb][0];
-                    const float m1 = m_run[nb][1] == NEG_INF ? 0.f : m_run[nb][1];
 #pragma unroll
                     for (int b = 0; b < NS; ++b) {
-                        const float p0 = fast_exp2(fmaf(sc[b][nb][0], mul[nb][0], -m0));
-                        const float p1 = fast_exp2(fmaf(sc[b][nb][1], mul[nb][1], -m1));
-                        const float p2 = fast_exp2(fmaf(sc[b][nb][2], mul[nb][0], -m0));
-                        const float p3 = fast_exp2(fmaf(sc[b][nb][3], mul[nb][1], -m1));
+                        const float p0 = fast_exp2(fmaf(sc[b][nb][0], mul[nb][0], nm[nb][0]));
+                        const float p1 = fast_exp2(fmaf(sc[b][nb][1], mul[nb][1], nm[nb][1]));
+                        const float p2 = fast_exp2(fmaf(sc[b][nb][2], mul[nb][0], nm[nb][0]));
+                        const float p3 = fast_exp2(fmaf(sc[b][nb][3], mul[nb][1], nm[nb][1]));
                         la[nb][0] += p0 + p2;
                         la[nb][1] += p1 + p3;
                         pb[b][nb][0] = movmatrix_trans(pack_f16x2(p0, p1));
@@ -498,25 +579,117 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
             fetch();   // into the stage just read
         }
 
-        // ---- end of the piece: the warps' sums are merged, 8 heads at a time ----
-        float *raw = reinterpret_cast<float *>(smem + PL::kRaw);          // [kWarps][8][kRow]
-        float *st_m = reinterpret_cast<float *>(smem + PL::kStat);        // [8 NB][kWarps]
-        float *st_l = st_m + 8 * NB * NW;
+        // ---- end of the piece ----
         const int G = p.G, seg = cs.beta * p.g + cs.j;
         const bool whole = piece == cs.first && piece_end == seg_end;
-        const size_t rec = static_cast<size_t>(seg) + cta;
+        const size_t rec = static_cast<size_t>(seg) + run;
         __nv_bfloat16 *ob =
             p.out + (static_cast<size_t>(cs.beta) * p.h + static_cast<size_t>(cs.j) * G) * D;
+        // the runs that hold the segment
+        const int c0 = cta_of_tile(cs.first, N, P), c1 = cta_of_tile(seg_end - 1, N, P);
         // out of the units of the codes and of the scales' bound (whose product may pass fp32's range)
         auto whole_units = [&](float x) { return x * kQ4Unit * bound; };
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 la[nb][i] += __shfl_xor_sync(0xffffffffu, la[nb][i], 4);
                 la[nb][i] += __shfl_xor_sync(0xffffffffu, la[nb][i], 8);
                 la[nb][i] += __shfl_xor_sync(0xffffffffu, la[nb][i], 16);
             }
+        // Merges the segment's records (at most kInlineMergeMaxPieces), in their order, by the threads
+        // t of n.
+        auto merge = [&](int t, int n) {
+            const int np = c1 - c0 + 1;
+            const size_t rec0 = static_cast<size_t>(seg) + c0;
+            for (int i = 4 * t; i < G * D; i += 4 * n) {
+                const int row = i / D;
+                float l[kInlineMergeMaxPieces];
+                float4 x[kInlineMergeMaxPieces];
+                float mx = NEG_INF;
+#pragma unroll
+                for (int k = 0; k < kInlineMergeMaxPieces; ++k) {
+                    l[k] = NEG_INF;
+                    x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (k < np) {
+                        l[k] = __ldcg(&p.part_lse[(rec0 + k) * G + row]);
+                        x[k] = __ldcg(
+                            reinterpret_cast<const float4 *>(p.part_o + (rec0 + k) * G * D + i));
+                    }
+                    mx = fmaxf(mx, l[k]);
+                }
+                float tot = 0.f;
+                float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int k = 0; k < kInlineMergeMaxPieces; ++k) {
+                    const float f = fast_exp2(l[k] - mx);   // 0 past the records
+                    tot += f;
+                    a.x = fmaf(f, x[k].x, a.x);
+                    a.y = fmaf(f, x[k].y, a.y);
+                    a.z = fmaf(f, x[k].z, a.z);
+                    a.w = fmaf(f, x[k].w, a.w);
+                }
+                const float inv = fast_rcp(tot);
+                *reinterpret_cast<uint2 *>(ob + i) =
+                    make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
+            }
+        };
+        if constexpr (kWarpRuns) {
+            // The warp holds the piece's sums: four channels of a head and group a lane.
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int head = 8 * nb + 2 * tig + i;
+                    if (head < G) {
+                        // (a piece of empty tiles: zeros, with the weight 2^-inf)
+                        const float inv = la[nb][i] == 0.f ? 0.f : fast_rcp(la[nb][i]);
+                        const size_t at = static_cast<size_t>(head) * D + gid * 4;
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) {
+                            const float4 v = make_float4(whole_units(o[nb][2 * g][i]) * inv,
+                                                         whole_units(o[nb][2 * g][2 + i]) * inv,
+                                                         whole_units(o[nb][2 * g + 1][i]) * inv,
+                                                         whole_units(o[nb][2 * g + 1][2 + i]) * inv);
+                            if (whole)
+                                *reinterpret_cast<uint2 *>(ob + at + 32 * g) =
+                                    make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+                            else
+                                *reinterpret_cast<float4 *>(p.part_o + rec * G * D + at + 32 * g) = v;
+                        }
+                        if (!whole && gid == 0)
+                            p.part_lse[rec * G + head] = fast_log2(la[nb][i]) - nm[nb][i];
+                    }
+                }
+            if (!whole && !p.deferred_merge) {
+                // The warp that finishes a segment last merges its records.
+                __syncwarp();
+                unsigned prev = 0;
+                if (lane == 0)
+                    prev = atomic_add_acq_rel_gpu(&p.counters[seg], 1u);
+                prev = __shfl_sync(0xffffffffu, prev, 0);
+                __syncwarp();
+                if (prev == static_cast<unsigned>(c1 - c0)) {
+                    merge(lane, 32);
+                    if (lane == 0)
+                        p.counters[seg] = 0u;
+                }
+            }
+            piece = piece_end;
+            cs = ns;
+            if (!last) {
+                WarpQ q;
+                load_warp_q(cs, q);
+                store_warp_q(q);
+            }
+            continue;
+        }
+        // Shared runs: the warps' sums are merged, 8 heads at a time.
+        float *raw = reinterpret_cast<float *>(smem + PL::kRaw);          // [kWarps][8][kRow]
+        float *st_m = reinterpret_cast<float *>(smem + PL::kStat);        // [8 NB][kWarps]
+        float *st_l = st_m + 8 * NB * NW;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
             if (nb > 0 && G <= 8 * nb)
                 break;
             if (nb > 0)
@@ -531,7 +704,8 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
                                     whole_units(o[nb][2 * g + 1][i]),
                                     whole_units(o[nb][2 * g + 1][2 + i]));
                 if (gid == 0) {
-                    st_m[(8 * nb + 2 * tig + i) * NW + warp] = m_run[nb][i];
+                    st_m[(8 * nb + 2 * tig + i) * NW + warp] =
+                        top[nb][i] == NEG_INF ? NEG_INF : -nm[nb][i];
                     st_l[(8 * nb + 2 * tig + i) * NW + warp] = la[nb][i];
                 }
             }
@@ -572,50 +746,20 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
                 }
             }
         }
-        if (!last)
-            store_q(q_next);   // every warp has passed this piece's last use of the queries
+        if (!last) {   // every warp has passed this piece's last use of the queries
+#pragma unroll
+            for (int i = 0; i < kQPer; ++i)
+                store_q(q_next[i], tid + i * PL::kThreads);
+        }
         if (!whole && !p.deferred_merge) {
-            // The CTA that finishes a segment last merges its records, in their order.
-            const int c0 = cta_of_tile(cs.first, N, P), c1 = cta_of_tile(seg_end - 1, N, P);
+            // The CTA that finishes a segment last merges its records.
             __syncthreads();
             if (tid == 0)
-                flags[1] = atomic_add_acq_rel_gpu(&p.counters[seg], 1u) ==
+                flags[0] = atomic_add_acq_rel_gpu(&p.counters[seg], 1u) ==
                            static_cast<unsigned>(c1 - c0);
             __syncthreads();
-            if (flags[1]) {
-                const int np = c1 - c0 + 1;
-                const size_t rec0 = static_cast<size_t>(seg) + c0;
-                for (int i = 4 * tid; i < G * D; i += 4 * PL::kThreads) {
-                    const int row = i / D;
-                    float l[kInlineMergeMaxPieces];
-                    float4 x[kInlineMergeMaxPieces];
-                    float mx = NEG_INF;
-#pragma unroll
-                    for (int k = 0; k < kInlineMergeMaxPieces; ++k) {
-                        l[k] = NEG_INF;
-                        x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (k < np) {
-                            l[k] = __ldcg(&p.part_lse[(rec0 + k) * G + row]);
-                            x[k] = __ldcg(reinterpret_cast<const float4 *>(
-                                p.part_o + (rec0 + k) * G * D + i));
-                        }
-                        mx = fmaxf(mx, l[k]);
-                    }
-                    float tot = 0.f;
-                    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                    for (int k = 0; k < kInlineMergeMaxPieces; ++k) {
-                        const float f = fast_exp2(l[k] - mx);   // 0 past the records
-                        tot += f;
-                        a.x = fmaf(f, x[k].x, a.x);
-                        a.y = fmaf(f, x[k].y, a.y);
-                        a.z = fmaf(f, x[k].z, a.z);
-                        a.w = fmaf(f, x[k].w, a.w);
-                    }
-                    const float inv = fast_rcp(tot);
-                    *reinterpret_cast<uint2 *>(ob + i) =
-                        make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
-                }
+            if (flags[0]) {
+                merge(tid, PL::kThreads);
                 if (tid == 0)
                     p.counters[seg] = 0u;
             }
@@ -625,53 +769,66 @@ __global__ void __launch_bounds__(Q4Plan<D, NB>::kThreads, Q4Plan<D, NB>::kMinBl
         cs = ns;
     }
     // No copy may still be in flight when the CTA exits (after an expired wait).
-    if (lane == 0 && flags[0]) {
+    if (lane == 0 && expired) {
         for (int k = f_it > R ? f_it - R : 0; k < f_it; ++k)
             if (!mbar_wait(bar_full + 8 * (k % R), (k / R) & 1))
                 atomicOr(p.err, kErrDrain);
     }
 }
 
-template <int D, int NB>
-struct Launch {
-    static const void *fn() { return reinterpret_cast<const void *>(&q4_decode_kernel<D, NB>); }
+struct Variant {
+    const void *fn;
+    size_t smem;
 };
 
-const void *decode_fn(int d, int group, int *threads, size_t *smem)
+template <int D, int NB, bool kWarpRuns>
+Variant variant()
 {
-    if (d == 64) {
-        *threads = Q4Plan<64, 1>::kThreads;
-        *smem = group <= 8 ? Q4Plan<64, 1>::kBytes : Q4Plan<64, 2>::kBytes;
-        return group <= 8 ? Launch<64, 1>::fn() : Launch<64, 2>::fn();
-    }
-    *threads = Q4Plan<128, 1>::kThreads;
-    *smem = group <= 8 ? Q4Plan<128, 1>::kBytes : Q4Plan<128, 2>::kBytes;
-    return group <= 8 ? Launch<128, 1>::fn() : Launch<128, 2>::fn();
+    return {reinterpret_cast<const void *>(&q4_decode_kernel<D, NB, kWarpRuns>),
+            static_cast<size_t>(Q4Plan<D, NB, kWarpRuns>::kBytes)};
+}
+
+template <int D, int NB>
+Variant variant(bool warp_runs)
+{
+    return warp_runs ? variant<D, NB, true>() : variant<D, NB, false>();
+}
+
+Variant find_variant(int d, int group, bool warp_runs)
+{
+    if (d == 64)
+        return group <= 8 ? variant<64, 1>(warp_runs) : variant<64, 2>(warp_runs);
+    return group <= 8 ? variant<128, 1>(warp_runs) : variant<128, 2>(warp_runs);
 }
 
 }  // namespace
 
 cudaError_t prepare_q4_decode(int d, int group, int *ctas_per_sm)
 {
-    int threads;
-    size_t smem;
-    const void *fn = decode_fn(d, group, &threads, &smem);
-    cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         static_cast<int>(smem));
-    if (e != cudaSuccess)
-        return e;
-    return cudaOccupancyMaxActiveBlocksPerMultiprocessor(ctas_per_sm, fn, threads, smem);
+    *ctas_per_sm = 1 << 30;
+    for (const bool warp_runs : {false, true}) {
+        const Variant v = find_variant(d, group, warp_runs);
+        cudaError_t e = cudaFuncSetAttribute(v.fn, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             static_cast<int>(v.smem));
+        int n = 0;
+        if (e == cudaSuccess)
+            e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, v.fn, q4_warps(group) * 32,
+                                                              v.smem);
+        if (e != cudaSuccess)
+            return e;
+        *ctas_per_sm = n < *ctas_per_sm ? n : *ctas_per_sm;
+    }
+    return cudaSuccess;
 }
 
-cudaError_t launch_q4_decode(int d, int grid, const Q4DecodeParams &p, cudaStream_t stream)
+cudaError_t launch_q4_decode(int d, int grid, bool warp_runs, const Q4DecodeParams &p,
+                             cudaStream_t stream)
 {
-    int threads;
-    size_t smem;
-    const void *fn = decode_fn(d, p.G, &threads, &smem);
+    const Variant v = find_variant(d, p.G, warp_runs);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(grid));
-    cfg.blockDim = dim3(static_cast<unsigned>(threads));
-    cfg.dynamicSmemBytes = smem;
+    cfg.blockDim = dim3(static_cast<unsigned>(q4_warps(p.G) * 32));
+    cfg.dynamicSmemBytes = v.smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -679,7 +836,7 @@ cudaError_t launch_q4_decode(int d, int grid, const Q4DecodeParams &p, cudaStrea
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     void *args[] = {const_cast<Q4DecodeParams *>(&p)};
-    return cudaLaunchKernelExC(&cfg, fn, args);
+    return cudaLaunchKernelExC(&cfg, v.fn, args);
 }
 
 }  // namespace mlkv

@@ -135,8 +135,9 @@ int mlkv_q4_create(mlkv_q4cache_t *out, int n_layers, int n_q_heads, int head_di
     c->row_bytes = mlkv::q4_row_bytes(max_seq, c->d);
     const size_t rows = static_cast<size_t>(c->b) * c->g;
     c->cache_bytes = rows * c->m * c->row_bytes;
-    // a record for each segment and each CTA of a launch's runs
-    const size_t records = rows + static_cast<size_t>(c->ctas_per_sm) * c->sm_count;
+    // a record for each segment and each run of a launch
+    const size_t records =
+        rows + static_cast<size_t>(c->ctas_per_sm) * c->sm_count * mlkv::q4_warps(c->G);
     auto alloc = [&](void **ptr, size_t n) {
         if (e == cudaSuccess)
             e = cudaMalloc(ptr, n);
@@ -259,25 +260,52 @@ int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *o
         return rc;
     mlkv::clamp_window(c->max_seq, &window, &sinks);
     static thread_local mlkv::Q4DecodeParams p;
-    const int T = mlkv::q4_tile_tokens(c->d);
-    bool uniform = true;
-    long long tiles = 0;
-    for (int beta = 0; beta < c->b; ++beta) {
-        const int L = seq_lens[beta];
-        uniform = uniform && L == seq_lens[0];
-        p.seq_len[beta] = L;
-        p.tile_start[beta] = static_cast<int>(tiles);
-        tiles += static_cast<long long>(c->g) *
-                 mlkv::visible_tiles(L, window, sinks, T, mlkv::kQ4Block).nt;
-        if (tiles > 0x7fffffffLL)
-            return fail(MLKV_ERR_UNSUPPORTED, "the tiles exceed the int32 tile index");
-    }
-    p.tile_start[c->b] = static_cast<int>(tiles);
-    p.uniform_len = uniform ? seq_lens[0] : 0;
-    // One wave of resident CTAs, each with at least a tile for every warp.
+    static thread_local mlkv::DecodeParams m;   // what the merges see
+    const int T = mlkv::q4_tile_tokens(c->d), W = mlkv::q4_warps(c->G);
     const long long slots = std::min<long long>(static_cast<long long>(c->ctas_per_sm) * c->sm_count,
                                                 mlkv::kCombineMaxPiecesHost);
-    const int grid = static_cast<int>(std::max(1LL, std::min(slots, (tiles + 7) / 8)));
+    m.b = c->b;
+    m.h = c->h;
+    m.g = c->g;
+    m.G = c->G;
+    m.ml_layers = 0;
+    // Every segment's tiles and `empty` more; the merges see lengths whose plain tiling gives them.
+    long long tiles = 0;
+    auto lay_tiles = [&](int empty) {
+        tiles = 0;
+        bool uniform = true;
+        for (int beta = 0; beta < c->b; ++beta) {
+            const int L = seq_lens[beta];
+            uniform = uniform && L == seq_lens[0];
+            const int nt = mlkv::visible_tiles(L, window, sinks, T, mlkv::kQ4Block).nt + empty;
+            p.seq_len[beta] = L;
+            m.seq_len[beta] = nt * T;
+            p.tile_start[beta] = m.tile_start[beta] = static_cast<int>(tiles);
+            tiles += static_cast<long long>(c->g) * nt;
+            if (tiles > 0x7fffffffLL)
+                return false;
+        }
+        p.tile_start[c->b] = m.tile_start[c->b] = static_cast<int>(tiles);
+        p.num_tiles = m.num_tiles = static_cast<int>(tiles);
+        p.empty_tiles = empty;
+        p.uniform_len = uniform ? seq_lens[0] : 0;
+        m.uniform_len = uniform ? m.seq_len[0] : 0;
+        return true;
+    };
+    // One wave of resident CTAs.  A warp a run where each gets at least 8 tiles (and no segment more
+    // records than one merge takes), else a CTA a run, with at least a tile for every warp.  A segment's
+    // start and end cost a warp about as much as a tile (measured: 2.2 us against 1.75).
+    if (!lay_tiles(1))
+        return fail(MLKV_ERR_UNSUPPORTED, "the tiles exceed the int32 tile index");
+    int grid = static_cast<int>(slots);
+    int pieces = mlkv::max_pieces_per_segment(m, T, grid * W);
+    const bool warp_runs = tiles >= 8 * slots * W && pieces <= mlkv::kCombineMaxPiecesHost;
+    if (!warp_runs) {
+        lay_tiles(0);
+        grid = static_cast<int>(std::max(1LL, std::min(slots, (tiles + W - 1) / W)));
+        pieces = mlkv::max_pieces_per_segment(m, T, grid);
+    }
+    p.deferred_merge = pieces > mlkv::inline_merge_pieces(c->G, c->d) ? 1 : 0;
     p.Q = static_cast<const __nv_bfloat16 *>(Q);
     p.out = static_cast<__nv_bfloat16 *>(out);
     p.slot = slot_base(c, layer);
@@ -293,26 +321,9 @@ int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *o
     p.G = c->G;
     p.window = window;
     p.sinks = sinks;
-    p.num_tiles = static_cast<int>(tiles);
-    // What the merges see: lengths whose plain tiling gives these tiles.
-    static thread_local mlkv::DecodeParams m;
-    m.b = c->b;
-    m.h = c->h;
-    m.g = c->g;
-    m.G = c->G;
-    m.num_tiles = p.num_tiles;
-    m.ml_layers = 0;
-    for (int beta = 0; beta < c->b; ++beta) {
-        m.tile_start[beta] = p.tile_start[beta];
-        m.seq_len[beta] = mlkv::visible_len(
-            p.seq_len[beta],
-            mlkv::visible_tiles(p.seq_len[beta], window, sinks, T, mlkv::kQ4Block));
-    }
-    m.uniform_len = uniform ? m.seq_len[0] : 0;
-    p.deferred_merge = mlkv::max_pieces_per_segment(m, T, grid) > mlkv::inline_merge_pieces(c->G, c->d);
     DeviceGuard guard(c->device);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    cudaError_t e = mlkv::launch_q4_decode(c->d, grid, p, stream);
+    cudaError_t e = mlkv::launch_q4_decode(c->d, grid, warp_runs, p, stream);
     if (e != cudaSuccess)
         return fail_cuda(e, "4-bit decode launch");
     if (p.deferred_merge) {
@@ -320,7 +331,7 @@ int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *o
         m.part_o = p.part_o;
         m.part_lse = p.part_lse;
         m.tile_tokens = T;
-        m.decode_grid = grid;
+        m.decode_grid = grid * (warp_runs ? W : 1);
         if ((e = mlkv::launch_combine(m, c->d, stream)) != cudaSuccess)
             return fail_cuda(e, "combine launch");
     }

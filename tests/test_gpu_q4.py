@@ -172,6 +172,23 @@ def test_decode_splits(d, h, g, lens, window, sinks):
     assert torch.equal(out, _decode(d, h, g, lens, window, sinks))
 
 
+def _uneven(n, most):
+    return [1 + (7919 * i * i + 13 * i) % most for i in range(n)]
+
+
+@pytest.mark.parametrize("d,h,g,lens,window,sinks", [
+    (64, 12, 4, [5000] * 80, 0, 0),              # the smallest launches in which every warp has a run
+    (64, 12, 1, _uneven(90, 60000), 0, 0),
+    (128, 32, 8, _uneven(64, 8000), 0, 0),
+    (128, 32, 2, _uneven(100, 16000), 0, 0),     # groups of 16
+    (128, 8, 2, _uneven(300, 9000), 3000, 70),
+    (64, 16, 1, [131072] * 10, 0, 0),            # hundreds of runs a segment
+])
+def test_decode_warp_runs(d, h, g, lens, window, sinks):
+    out = _decode(d, h, g, lens, window, sinks)
+    assert torch.equal(out, _decode(d, h, g, lens, window, sinks))
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_decode_sharp_scores(d):
     """Scores that differ by hundreds: the running maximum moves all the time."""
