@@ -129,6 +129,8 @@ struct Q4DecodeParams {
 constexpr int q4_tile_tokens(int d) { return d == 128 ? 32 : 64; }
 cudaError_t prepare_q4_decode(int d, int group, int *ctas_per_sm);
 constexpr int q4_warps(int group) { return group <= 8 ? 8 : 6; }   // of a CTA
+// Records of a segment up to which the launch merges them itself.
+constexpr int kQ4InlineMergePieces = 16;
 // warp_runs: P = grid x warps runs of tiles, a warp each; else P = grid, a CTA each (see the kernel).
 cudaError_t launch_q4_decode(int d, int grid, bool warp_runs, const Q4DecodeParams &p,
                              cudaStream_t stream);

@@ -27,6 +27,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "mlkv_q4.h"
 
 #include "mlkv_device.cuh"
@@ -146,6 +148,16 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// The first product of a sum.
+__device__ __forceinline__ void mma_f16_zero(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                             uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 "
+        "{%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
 {
     const __half2 v = __floats2half2_rn(lo, hi);
@@ -197,12 +209,26 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
     }
     __syncwarp();
 
-    // Lane 0 sends the copies of the warp's tiles R ahead.
+    // Lane 0 sends the copies of the warp's tiles R ahead; f_run of them follow one another at f_src.
     Segment fs = segment_of_tile<T>(p, tile_lo < N ? tile_lo : N - 1);
-    int f_tile = tile_first, f_it = 0;
+    int f_tile = tile_first, f_it = 0, f_run = 0;
+    const uint8_t *f_src = nullptr;
+    auto send = [&](uint32_t bytes) {
+        const int s = f_it % R;
+        mbar_arrive_expect_tx(bar_full + 8 * s, bytes);
+        bulk_load(ring + s * PL::kTileBytes, f_src, bytes, bar_full + 8 * s);
+        f_tile += kStep;
+        ++f_it;
+    };
     auto fetch = [&]() {
         if (lane != 0)
             return;
+        if (f_run > 0) {
+            send(PL::kTileBytes);
+            f_src += kStep * PL::kTileBytes;
+            --f_run;
+            return;
+        }
         for (; f_tile < tile_hi; f_tile += kStep) {
             while (f_tile >= fs.first + fs.nt)
                 next_segment<T>(p, fs);
@@ -212,15 +238,13 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
             int pos0, end;
             tile_range<T>(fs, p.sinks, tt, pos0, end);
             const int n = min(NS, (end - pos0 + kQ4Block - 1) / kQ4Block);
-            const uint32_t bytes = static_cast<uint32_t>(n) * LY::kBytes;
-            const int s = f_it % R;
-            mbar_arrive_expect_tx(bar_full + 8 * s, bytes);
-            bulk_load(ring + s * PL::kTileBytes,
-                      p.slot + (static_cast<long long>(fs.beta) * p.g + fs.j) * p.row_bytes +
-                          static_cast<long long>(pos0 / kQ4Block) * LY::kBytes,
-                      bytes, bar_full + 8 * s);
-            f_tile += kStep;
-            ++f_it;
+            f_src = p.slot + (static_cast<long long>(fs.beta) * p.g + fs.j) * p.row_bytes +
+                    static_cast<long long>(pos0 / kQ4Block) * LY::kBytes;
+            send(static_cast<uint32_t>(n) * LY::kBytes);
+            // the whole tiles behind it, of the same part of the segment and this run
+            const int stop = min(tile_hi, fs.first + (tt < fs.v.ns ? fs.v.ns : fs.v.nt)) - 1;
+            f_run = f_tile < stop ? (stop - f_tile + kStep - 1) / kStep : 0;
+            f_src += kStep * PL::kTileBytes;
             return;
         }
     };
@@ -467,8 +491,8 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
                         const float f1 = (g & 1) ? bf16_hi(s1) : bf16_lo(s1);
 #pragma unroll
                         for (int nb = 0; nb < NB; ++nb) {
-                            float t[4] = {0.f, 0.f, 0.f, 0.f};
-                            mma_f16(t, a[0], a[1], a[2], a[3], q[nb].x, q[nb].y);
+                            float t[4];
+                            mma_f16_zero(t, a[0], a[1], a[2], a[3], q[nb].x, q[nb].y);
                             mma_f16(t, a[4], a[5], a[6], a[7], q[nb].z, q[nb].w);
                             sc[b][nb][0] = g == 0 ? t[0] * f0 : fmaf(t[0], f0, sc[b][nb][0]);
                             sc[b][nb][1] = g == 0 ? t[1] * f0 : fmaf(t[1], f0, sc[b][nb][1]);
@@ -597,41 +621,73 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
                 la[nb][i] += __shfl_xor_sync(0xffffffffu, la[nb][i], 8);
                 la[nb][i] += __shfl_xor_sync(0xffffffffu, la[nb][i], 16);
             }
-        // Merges the segment's records (at most kInlineMergeMaxPieces), in their order, by the threads
-        // t of n.
-        auto merge = [&](int t, int n) {
+        // Merges the segment's records, in their order, by the threads t of n: C times four columns of K
+        // records a thread in flight (one round trip to L2 after another otherwise: 6 us at the end of
+        // a launch).
+        auto merge = [&](int t, int n, auto c_, auto k_) {
+            constexpr int C = decltype(c_)::value, K = decltype(k_)::value;
             const int np = c1 - c0 + 1;
             const size_t rec0 = static_cast<size_t>(seg) + c0;
-            for (int i = 4 * t; i < G * D; i += 4 * n) {
-                const int row = i / D;
-                float l[kInlineMergeMaxPieces];
-                float4 x[kInlineMergeMaxPieces];
-                float mx = NEG_INF;
+            for (int i0 = 4 * t; i0 < G * D; i0 += 4 * n * C) {
+                float mx[C], tot[C];
+                float4 a[C];
 #pragma unroll
-                for (int k = 0; k < kInlineMergeMaxPieces; ++k) {
-                    l[k] = NEG_INF;
-                    x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (k < np) {
-                        l[k] = __ldcg(&p.part_lse[(rec0 + k) * G + row]);
-                        x[k] = __ldcg(
-                            reinterpret_cast<const float4 *>(p.part_o + (rec0 + k) * G * D + i));
+                for (int c = 0; c < C; ++c) {
+                    mx[c] = NEG_INF;
+                    tot[c] = 0.f;
+                    a[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+                for (int k0 = 0; k0 < np; k0 += K) {
+                    float l[K][C];
+                    float4 x[K][C];
+#pragma unroll
+                    for (int k = 0; k < K; ++k)
+#pragma unroll
+                        for (int c = 0; c < C; ++c) {
+                            const int i = i0 + 4 * n * c;
+                            l[k][c] = NEG_INF;
+                            x[k][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (k0 + k < np && i < G * D) {
+                                l[k][c] = __ldcg(&p.part_lse[(rec0 + k0 + k) * G + i / D]);
+                                x[k][c] = __ldcg(reinterpret_cast<const float4 *>(
+                                    p.part_o + (rec0 + k0 + k) * G * D + i));
+                            }
+                        }
+#pragma unroll
+                    for (int c = 0; c < C; ++c) {
+                        float m_new = mx[c];
+#pragma unroll
+                        for (int k = 0; k < K; ++k)
+                            m_new = fmaxf(m_new, l[k][c]);
+                        // (a run may hold empty tiles of the segment alone: no weight at all yet)
+                        const float base = m_new == NEG_INF ? 0.f : m_new;
+                        const float down = fast_exp2(mx[c] - base);   // 0 before the first weight
+                        mx[c] = m_new;
+                        tot[c] *= down;
+                        a[c].x *= down;
+                        a[c].y *= down;
+                        a[c].z *= down;
+                        a[c].w *= down;
+#pragma unroll
+                        for (int k = 0; k < K; ++k) {
+                            const float f = fast_exp2(l[k][c] - base);   // 0 past the records
+                            tot[c] += f;
+                            a[c].x = fmaf(f, x[k][c].x, a[c].x);
+                            a[c].y = fmaf(f, x[k][c].y, a[c].y);
+                            a[c].z = fmaf(f, x[k][c].z, a[c].z);
+                            a[c].w = fmaf(f, x[k][c].w, a[c].w);
+                        }
                     }
-                    mx = fmaxf(mx, l[k]);
                 }
-                float tot = 0.f;
-                float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int k = 0; k < kInlineMergeMaxPieces; ++k) {
-                    const float f = fast_exp2(l[k] - mx);   // 0 past the records
-                    tot += f;
-                    a.x = fmaf(f, x[k].x, a.x);
-                    a.y = fmaf(f, x[k].y, a.y);
-                    a.z = fmaf(f, x[k].z, a.z);
-                    a.w = fmaf(f, x[k].w, a.w);
+                for (int c = 0; c < C; ++c) {
+                    const int i = i0 + 4 * n * c;
+                    const float inv = fast_rcp(tot[c]);
+                    if (i < G * D)
+                        *reinterpret_cast<uint2 *>(ob + i) =
+                            make_uint2(pack_bf16x2(a[c].x * inv, a[c].y * inv),
+                                       pack_bf16x2(a[c].z * inv, a[c].w * inv));
                 }
-                const float inv = fast_rcp(tot);
-                *reinterpret_cast<uint2 *>(ob + i) =
-                    make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
             }
         };
         if constexpr (kWarpRuns) {
@@ -670,7 +726,8 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
                 prev = __shfl_sync(0xffffffffu, prev, 0);
                 __syncwarp();
                 if (prev == static_cast<unsigned>(c1 - c0)) {
-                    merge(lane, 32);
+                    merge(lane, 32, std::integral_constant<int, 4>{},
+                          std::integral_constant<int, 4>{});
                     if (lane == 0)
                         p.counters[seg] = 0u;
                 }
@@ -759,7 +816,8 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
                            static_cast<unsigned>(c1 - c0);
             __syncthreads();
             if (flags[0]) {
-                merge(tid, PL::kThreads);
+                merge(tid, PL::kThreads, std::integral_constant<int, 1>{},
+                      std::integral_constant<int, 8>{});
                 if (tid == 0)
                     p.counters[seg] = 0u;
             }

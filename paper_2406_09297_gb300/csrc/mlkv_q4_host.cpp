@@ -293,9 +293,10 @@ int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *o
         return true;
     };
     // One wave of resident CTAs.  A warp a run where each gets at least 8 tiles (and no segment more
-    // records than one merge takes), else a CTA a run, with at least a tile for every warp.  A segment's
-    // start and end cost a warp about as much as a tile (measured: 2.2 us against 1.75).
-    if (!lay_tiles(1))
+    // records than one merge takes), else a CTA a run, with at least a tile for every warp.  The start and
+    // end of a segment's part cost a warp ~2 us and more, a tile 1.75: three empty tiles a segment (64
+    // uneven sequences of up to 8192 positions, 8 KV heads of 128: 58.8, 57.5, 56.6 us with 1, 2, 3).
+    if (!lay_tiles(3))
         return fail(MLKV_ERR_UNSUPPORTED, "the tiles exceed the int32 tile index");
     int grid = static_cast<int>(slots);
     int pieces = mlkv::max_pieces_per_segment(m, T, grid * W);
@@ -305,7 +306,7 @@ int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *o
         grid = static_cast<int>(std::max(1LL, std::min(slots, (tiles + W - 1) / W)));
         pieces = mlkv::max_pieces_per_segment(m, T, grid);
     }
-    p.deferred_merge = pieces > mlkv::inline_merge_pieces(c->G, c->d) ? 1 : 0;
+    p.deferred_merge = pieces > mlkv::kQ4InlineMergePieces ? 1 : 0;
     p.Q = static_cast<const __nv_bfloat16 *>(Q);
     p.out = static_cast<__nv_bfloat16 *>(out);
     p.slot = slot_base(c, layer);

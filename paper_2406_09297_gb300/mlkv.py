@@ -327,17 +327,21 @@ def mlkv_prefill_window(handle, layer, Q, K, V, out, prompt_lens, s_max, window,
                                           s_max, window, sinks, _stream(stream)))
 
 
-def _token_stride(x, name, batch, s, d):
+def _token_stride(x, name, batch, s, heads, d):
     """Elements between the tokens of x [batch][s][heads][d], whose heads are dense."""
-    if x is None:
-        return 0
-    st = x.stride()
-    if x.dim() != 4 or tuple(x.shape[:2]) != (batch, s) or x.shape[3] != d:
-        raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must be [{batch}][{s}][heads][{d}]")
-    if st[3] != 1 or (x.shape[2] > 1 and st[2] != d) or (batch > 1 and s > 1 and st[0] != s * st[1]):
+    if x.shape != (batch, s, heads, d):
+        raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must be [{batch}][{s}][{heads}][{d}]")
+    s0, s1, s2, s3 = x.stride()
+    if s3 != 1 or (s2 != d and heads > 1) or (s > 1 and batch > 1 and s0 != s * s1):
         raise MLKVError(MLKV_ERR_INVALID_ARG,
                         f"{name}'s heads must be dense and its tokens one stride apart")
-    return st[1] if s > 1 else st[0]
+    return s1 if s > 1 else s0
+
+
+def _dense(x, n, what):
+    if x.numel() != n or not x.is_contiguous():
+        raise MLKVError(MLKV_ERR_INVALID_ARG, f"{what} must be dense and of {n} elements")
+    return x.data_ptr()
 
 
 def mlkv_qk_norm_rope(Q, K, V, q_gain, k_gain, cos, sin, positions, Q_out, K_out, V_out, eps=1e-6,
@@ -347,27 +351,25 @@ def mlkv_qk_norm_rope(Q, K, V, q_gain, k_gain, cos, sin, positions, Q_out, K_out
     rotary encoding) -> Q_out [b][s][h][d], K_out and V_out [b][g][s][d], all bf16."""
     b, s, h, d = Q.shape
     g = K.shape[2]
-    strides = [_token_stride(x, n, b, s, d) for x, n in ((Q, "Q"), (K, "K"), (V, "V"))]
-    if V is not None and V.shape[2] != g:
-        raise MLKVError(MLKV_ERR_INVALID_ARG, "K and V must have the same heads")
-    for x, n, heads in ((Q_out, "Q_out", h), (K_out, "K_out", g), (V_out, "V_out", g)):
-        if x is not None and (x.numel() != b * s * heads * d or not x.is_contiguous()):
-            raise MLKVError(MLKV_ERR_INVALID_ARG, f"{n} must be dense and hold every head")
-    for x, n in ((q_gain, "q_gain"), (k_gain, "k_gain")):
-        if x is not None and (x.numel() != d or not x.is_contiguous()):
-            raise MLKVError(MLKV_ERR_INVALID_ARG, f"{n} must be dense and hold {d} channels")
-    n_pos, half = (0, 0) if cos is None else cos.shape
-    if cos is not None and (sin is None or sin.shape != cos.shape or positions is None or
-                            not (cos.is_contiguous() and sin.is_contiguous() and
-                                 positions.is_contiguous()) or positions.numel() != b * s or
-                            cos.element_size() != 4 or sin.element_size() != 4 or
-                            positions.element_size() != 4):
-        raise MLKVError(MLKV_ERR_INVALID_ARG,
-                        "cos and sin must be dense fp32 of one shape, positions dense int32 [b][s]")
+    tokens = b * s
+    n_pos = half = 0
+    p_cos = p_sin = p_pos = None
+    if cos is not None:
+        n_pos, half = cos.shape
+        if sin is None or positions is None or not (
+                cos.element_size() == sin.element_size() == positions.element_size() == 4):
+            raise MLKVError(MLKV_ERR_INVALID_ARG, "cos, sin (fp32) and positions (int32) belong together")
+        p_cos, p_sin = _dense(cos, n_pos * half, "cos"), _dense(sin, n_pos * half, "sin")
+        p_pos = _dense(positions, tokens, "positions")
+    kv = tokens * g * d
     return _check(lib.mlkv_qk_norm_rope(
-        _ptr(Q), _ptr(K), _ptr(V), *strides, _ptr(q_gain), _ptr(k_gain), _ptr(cos), _ptr(sin), n_pos,
-        2 * half, int(interleaved), _ptr(positions), eps, b, s, h, g, d, _ptr(Q_out), _ptr(K_out),
-        _ptr(V_out), _stream(stream)))
+        Q.data_ptr(), K.data_ptr(), _ptr(V), _token_stride(Q, "Q", b, s, h, d),
+        _token_stride(K, "K", b, s, g, d), 0 if V is None else _token_stride(V, "V", b, s, g, d),
+        None if q_gain is None else _dense(q_gain, d, "q_gain"),
+        None if k_gain is None else _dense(k_gain, d, "k_gain"), p_cos, p_sin, n_pos, 2 * half,
+        int(interleaved), p_pos, eps, b, s, h, g, d, _dense(Q_out, tokens * h * d, "Q_out"),
+        _dense(K_out, kv, "K_out"), None if V_out is None else _dense(V_out, kv, "V_out"),
+        _stream(stream)))
 
 
 def mlkv_q4_create(n_layers, n_q_heads, head_dim, layer_owner, kv_heads_per_owner, batch, max_seq):
