@@ -5,11 +5,15 @@
 //   (a, b) -> (a cos - b sin, b cos + a sin)       on the first rot channels, (a, b) = channels i and
 //                                                  i + rot/2, or 2i and 2i + 1 (interleaved)
 //
-// In fp32, rounded once, to bf16.  Every channel is read once and written once, so HBM bounds it (per
-// channel 4 bytes against ~12 operations); a head is D / 8 lanes of 16 bytes each, whose square sums
-// and rotation partners are exchanged with shuffles.  A warp takes U x (256 / D) heads of one token: the
-// token's row of the table and the gains are loaded once for all of them and U loads are in flight per
-// lane.
+// In fp32, rounded once, to bf16.  Every channel is read once and written once; at 4 bytes a channel HBM
+// leaves ~12 instructions for the 8 channels of a 16-byte load, so the instructions are kept few: a lane
+// holds 16 channels of a head, two pieces of 8 that are each other's rotation partners, and D / 16 lanes
+// a head, so that only the sum of squares crosses lanes; gain and rotation are one pair of factors a
+// channel, made once per token:
+//   a' = r (a (g_a cos) - b (g_b sin)),  b' = r (b (g_b cos) + a (g_a sin)),  r = 1 / sqrt(...)
+// A block's warps take heads of one kind (queries, keys or values), whose addresses are then uniform: a
+// token each and 512 / D heads at a time, two such loads in flight, or, where a token has fewer heads of
+// the kind, those of several tokens.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -24,77 +28,122 @@ namespace mlkv {
 namespace {
 
 struct NormRopeParams {
-    const __nv_bfloat16 *Q, *K, *V;            // token rows of h, g, g heads, strides apart
-    long long q_stride, k_stride, v_stride;    // elements
-    const __nv_bfloat16 *q_gain, *k_gain;      // [D] or null
+    // by kind: queries, keys, values
+    const __nv_bfloat16 *in[3];                // token rows of heads, in_stride elements apart
+    long long in_stride[3];
+    const __nv_bfloat16 *gain[2];              // [D] or null
+    __nv_bfloat16 *out[3];
+    long long out_seq[3], out_token[3], out_head[3];   // elements: a sequence, token, head further
+    int heads[3];
+    int wide[3];                               // heads of a token that a warp has lanes for (a power of
+                                               // two; 512 / D: one token a warp)
+    int parts[3];                              // warps that share a token's heads
+    unsigned first_block[3];                   // of the kind's blocks, part by part
     const float *cos, *sin;                    // [n_pos][rot / 2]
     const int *positions;                      // [tokens]
-    __nv_bfloat16 *q_out;                      // [b][s][h][D]
-    __nv_bfloat16 *k_out, *v_out;              // [b][g][s][D]
     float eps;
-    int tokens, s, h, g, heads;                // heads: h + g, and g more with V
-    int rot, n_pos, interleaved, chunks;       // chunks: warps per token
+    int tokens, s, rot, n_pos;
+    int per_block;                             // heads of a block, a multiple of 512 / D
 };
 
 constexpr int kNormThreads = 128;
+constexpr int kNormLoads = 2;                  // in flight
 
-template <int D, int U>
-__global__ void __launch_bounds__(kNormThreads)
+// kInter: pairs are neighbouring channels.
+template <int D, bool kInter>
+__global__ void __launch_bounds__(kNormThreads, 6)
     norm_rope_kernel(const __grid_constant__ NormRopeParams p)
 {
-    constexpr int LPH = D / 8;        // lanes per head, 8 channels each
-    constexpr int HPI = 32 / LPH;     // heads per warp-wide load
+    constexpr int LPH = D / 16;       // lanes per head
+    constexpr int HPI = 32 / LPH;     // heads a warp holds at a time
+    constexpr int U = kNormLoads;
     grid_dependency_wait();
     grid_dependents_launch();
+    const int kind = blockIdx.x < p.first_block[1] ? 0 : blockIdx.x < p.first_block[2] ? 1 : 2;
     const int lane = threadIdx.x & 31;
-    const long long w = static_cast<long long>(blockIdx.x) * (kNormThreads / 32) + (threadIdx.x >> 5);
-    const long long token = w / p.chunks;
-    if (token >= p.tokens)
-        return;
-    const int c = static_cast<int>(w - token * p.chunks);
-    const int sub = lane % LPH;       // channels 8 sub .. 8 sub + 7
-    const int hd0 = c * U * HPI + lane / LPH;
-    uint4 x[U];
+    const int sel = lane / LPH, wide = p.wide[kind], parts = p.parts[kind];
+    const unsigned block = (blockIdx.x - p.first_block[kind]) / parts;
+    const int part = static_cast<int>(blockIdx.x - p.first_block[kind] - block * parts);
+    // this lane's token; past the last one there is nothing to do, but the warp's shuffles need it
+    const long long token_at =
+        (static_cast<long long>(block) * (kNormThreads / 32) + (threadIdx.x >> 5)) * (HPI / wide) +
+        sel / wide;
+    const bool live = token_at < p.tokens;
+    const int token = live ? static_cast<int>(token_at) : p.tokens - 1;
+    // This lane's pieces of 8 channels: rotation partners, or (past the rotated ones) neighbours.
+    const int c = lane % LPH;
+    const int hp = p.rot / 16;        // pieces in half the rotated channels
+    const bool rotates = c < hp;
+    const int pa = kInter ? 16 * c : rotates ? 8 * c : 8 * (2 * hp + 2 * (c - hp));
+    const int pb = kInter || !rotates ? pa + 8 : 8 * (c + hp);
+    // its heads: from head0 on, HPI apart, below head1; no lane of the warp has any from `stop` on
+    const int first = part * p.per_block, stop = min(p.heads[kind], first + p.per_block);
+    const int head0 = first + sel % wide, head1 = live ? stop : 0;
+    const int beta = token / p.s;
+    const __nv_bfloat16 *src =
+        p.in[kind] + token * p.in_stride[kind] + static_cast<long long>(head0) * D;
+    __nv_bfloat16 *dst = p.out[kind] + beta * p.out_seq[kind] +
+                         (token - beta * p.s) * p.out_token[kind] + head0 * p.out_head[kind];
+    const int d_ab = pb - pa;
+    src += pa;
+    dst += pa;
+    const long long out_step = HPI * p.out_head[kind];
+    auto read = [&](uint4 (&a)[U], uint4 (&b)[U], int head) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int hd = hd0 + u * HPI;
-        const __nv_bfloat16 *src = nullptr;
-        if (hd < p.h)
-            src = p.Q + token * p.q_stride + hd * D;
-        else if (hd < p.h + p.g)
-            src = p.K + token * p.k_stride + (hd - p.h) * D;
-        else if (hd < p.heads)
-            src = p.V + token * p.v_stride + (hd - p.h - p.g) * D;
-        x[u] = src != nullptr ? *reinterpret_cast<const uint4 *>(src + sub * 8)
-                              : make_uint4(0, 0, 0, 0);
-    }
-    // The token's rotation of this lane's channels: y[i] cos[i] + other[i] sin[i], sin signed.
-    const int hc = p.rot / 16;        // 8-channel pieces of half the rotated channels
-    const bool rotates = sub < 2 * hc;
-    const bool low = sub < hc;
-    float cs[8], sn[8];
+        for (int u = 0; u < U; ++u)
+            if (head + u * HPI < head1) {
+                a[u] = *reinterpret_cast<const uint4 *>(src + u * HPI * D);
+                b[u] = *reinterpret_cast<const uint4 *>(src + u * HPI * D + d_ab);
+            }
+        src += U * HPI * D;
+    };
+    uint4 xa[U], xb[U];
+    if (kind == 2) {   // values only move
+        for (int h0 = first, head = head0; h0 < stop; h0 += U * HPI, head += U * HPI) {
+            read(xa, xb, head);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        cs[i] = 1.f;
-        sn[i] = 0.f;
-    }
-    if (rotates) {
-        const int pos = p.positions[token];
-        if (pos >= 0 && pos < p.n_pos) {
-            if (p.interleaved) {
-                // pairs of neighbours: 4 table entries for 8 channels
-                const size_t at = static_cast<size_t>(pos) * (p.rot / 2) + sub * 4;
-                const float4 a = *reinterpret_cast<const float4 *>(p.cos + at);
-                const float4 b = *reinterpret_cast<const float4 *>(p.sin + at);
-                const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    cs[i] = av[i / 2];
-                    sn[i] = (i & 1) ? bv[i / 2] : -bv[i / 2];
+            for (int u = 0; u < U; ++u) {
+                if (head + u * HPI < head1) {
+                    *reinterpret_cast<uint4 *>(dst) = xa[u];
+                    *reinterpret_cast<uint4 *>(dst + d_ab) = xb[u];
                 }
-            } else {
-                const size_t at =
-                    static_cast<size_t>(pos) * (p.rot / 2) + (low ? sub : sub - hc) * 8;
+                dst += out_step;
+            }
+        }
+        return;
+    }
+    read(xa, xb, head0);
+    auto unpack = [](const uint4 &v, float (&f)[8]) {
+        const uint32_t r[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = bf16_lo(r[i]);
+            f[2 * i + 1] = bf16_hi(r[i]);
+        }
+    };
+    auto pack = [](const float (&f)[8]) {
+        return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
+                          pack_bf16x2(f[6], f[7]));
+    };
+    // The factors of the lane's 8 pairs (elements i of both pieces, or, interleaved, neighbours: pairs
+    // 0 .. 3 in piece a): gains times cos and sin, of the pairs' first and second elements.
+    float ac[8], as[8], bc[8], bs[8];
+    {
+        float cs[8], sn[8], ga[8], gb[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            cs[i] = ga[i] = gb[i] = 1.f;
+            sn[i] = 0.f;
+        }
+        const __nv_bfloat16 *gain = p.gain[kind];
+        if (gain != nullptr) {
+            unpack(*reinterpret_cast<const uint4 *>(gain + pa), ga);
+            unpack(*reinterpret_cast<const uint4 *>(gain + pb), gb);
+        }
+        if (kInter ? 16 * c < p.rot : rotates) {
+            const int pos = p.positions[token];
+            if (pos >= 0 && pos < p.n_pos) {
+                const size_t at = static_cast<size_t>(pos) * (p.rot / 2) + 8 * c;
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
                     const float4 a = *reinterpret_cast<const float4 *>(p.cos + at + 4 * q);
@@ -103,84 +152,80 @@ __global__ void __launch_bounds__(kNormThreads)
                     cs[4 * q + 1] = a.y;
                     cs[4 * q + 2] = a.z;
                     cs[4 * q + 3] = a.w;
-                    sn[4 * q] = low ? -b.x : b.x;
-                    sn[4 * q + 1] = low ? -b.y : b.y;
-                    sn[4 * q + 2] = low ? -b.z : b.z;
-                    sn[4 * q + 3] = low ? -b.w : b.w;
+                    sn[4 * q] = b.x;
+                    sn[4 * q + 1] = b.y;
+                    sn[4 * q + 2] = b.z;
+                    sn[4 * q + 3] = b.w;
                 }
-            }
-        } else {
-            // outside the table: the rotated channels say so
+            } else {
+                // outside the table: the rotated channels say so
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                cs[i] = __int_as_float(0x7fffffff);
+                for (int i = 0; i < 8; ++i)
+                    cs[i] = __int_as_float(0x7fffffff);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float g0 = kInter ? (i < 4 ? ga[2 * i & 7] : gb[2 * i & 7]) : ga[i];
+            const float g1 = kInter ? (i < 4 ? ga[(2 * i + 1) & 7] : gb[(2 * i + 1) & 7]) : gb[i];
+            ac[i] = g0 * cs[i];
+            as[i] = g0 * sn[i];
+            bc[i] = g1 * cs[i];
+            bs[i] = g1 * sn[i];
         }
     }
-    uint4 gq = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), gk = gq;
-    if (p.q_gain != nullptr)
-        gq = *reinterpret_cast<const uint4 *>(p.q_gain + sub * 8);
-    if (p.k_gain != nullptr)
-        gk = *reinterpret_cast<const uint4 *>(p.k_gain + sub * 8);
-    const int partner = (lane & ~(LPH - 1)) | (rotates ? (low ? sub + hc : sub - hc) : sub);
-    const long long beta = token / p.s;
-    const long long t = token - beta * p.s;
+    for (int h0 = first, head = head0;;) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int hd = hd0 + u * HPI;
-        const bool is_q = hd < p.h, is_v = hd >= p.h + p.g;
-        float y[8] = {bf16_lo(x[u].x), bf16_hi(x[u].x), bf16_lo(x[u].y), bf16_hi(x[u].y),
-                      bf16_lo(x[u].z), bf16_hi(x[u].z), bf16_lo(x[u].w), bf16_hi(x[u].w)};
-        float ss = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            ss = fmaf(y[i], y[i], ss);
-#pragma unroll
-        for (int m = 1; m < LPH; m <<= 1)
-            ss += __shfl_xor_sync(0xffffffffu, ss, m);
-        const float inv = rsqrtf(ss * (1.f / D) + p.eps);
-        const uint4 gw = is_q ? gq : gk;
-        const float gain[8] = {bf16_lo(gw.x), bf16_hi(gw.x), bf16_lo(gw.y), bf16_hi(gw.y),
-                               bf16_lo(gw.z), bf16_hi(gw.z), bf16_lo(gw.w), bf16_hi(gw.w)};
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            y[i] = y[i] * inv * gain[i];
-        float r[8];
-        if (p.interleaved) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                r[i] = fmaf(y[i ^ 1], sn[i], y[i] * cs[i]);
-        } else if (hc > 0) {
+        for (int u = 0; u < U; ++u) {
+            if (h0 + u * HPI >= stop)
+                break;
+            float a[8], b[8], oa[8], ob[8];
+            unpack(xa[u], a);
+            unpack(xb[u], b);
+            float s0 = 0.f, s1 = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float o = __shfl_sync(0xffffffffu, y[i], partner);
-                r[i] = fmaf(o, sn[i], y[i] * cs[i]);
+                s0 = fmaf(a[i], a[i], s0);
+                s1 = fmaf(b[i], b[i], s1);
             }
-        } else {
+            float ss = s0 + s1;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                r[i] = y[i];
-        }
-        uint4 v = make_uint4(pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]),
-                             pack_bf16x2(r[4], r[5]), pack_bf16x2(r[6], r[7]));
-        if (is_v)
-            v = x[u];
-        if (hd < p.heads) {
-            __nv_bfloat16 *dst;
-            if (is_q) {
-                dst = p.q_out + (token * p.h + hd) * D;
-            } else {
-                const int j = hd - p.h - (is_v ? p.g : 0);
-                dst = (is_v ? p.v_out : p.k_out) + ((beta * p.g + j) * p.s + t) * D;
+            for (int m = 1; m < LPH; m <<= 1)
+                ss += __shfl_xor_sync(0xffffffffu, ss, m);
+            const float r = rsqrtf(ss * (1.f / D) + p.eps);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                // pair i: x its first element, y its second
+                const float x = kInter ? (i < 4 ? a[2 * i & 7] : b[2 * i & 7]) : a[i];
+                const float y = kInter ? (i < 4 ? a[(2 * i + 1) & 7] : b[(2 * i + 1) & 7]) : b[i];
+                const float x1 = r * fmaf(x, ac[i], -y * bs[i]), y1 = r * fmaf(y, bc[i], x * as[i]);
+                if (kInter) {
+                    (i < 4 ? oa : ob)[2 * i & 7] = x1;
+                    (i < 4 ? oa : ob)[(2 * i + 1) & 7] = y1;
+                } else {
+                    oa[i] = x1;
+                    ob[i] = y1;
+                }
             }
-            *reinterpret_cast<uint4 *>(dst + sub * 8) = v;
+            if (head + u * HPI < head1) {
+                *reinterpret_cast<uint4 *>(dst) = pack(oa);
+                *reinterpret_cast<uint4 *>(dst + d_ab) = pack(ob);
+            }
+            dst += out_step;
         }
+        h0 += U * HPI;
+        head += U * HPI;
+        if (h0 >= stop)
+            break;
+        read(xa, xb, head);
     }
 }
 
-template <int D, int U>
-const void *norm_fn()
+template <int D>
+const void *norm_fn(bool interleaved)
 {
-    return reinterpret_cast<const void *>(&norm_rope_kernel<D, U>);
+    return interleaved ? reinterpret_cast<const void *>(&norm_rope_kernel<D, true>)
+                       : reinterpret_cast<const void *>(&norm_rope_kernel<D, false>);
 }
 
 }  // namespace
@@ -258,39 +303,48 @@ extern "C" int mlkv_qk_norm_rope(const void *Q, const void *K, const void *V, in
         }
     }
     NormRopeParams p;
-    p.Q = static_cast<const __nv_bfloat16 *>(Q);
-    p.K = static_cast<const __nv_bfloat16 *>(K);
-    p.V = static_cast<const __nv_bfloat16 *>(V);
-    p.q_stride = q_stride;
-    p.k_stride = k_stride;
-    p.v_stride = v_stride;
-    p.q_gain = static_cast<const __nv_bfloat16 *>(q_gain);
-    p.k_gain = static_cast<const __nv_bfloat16 *>(k_gain);
+    const void *in_ptr[3] = {Q, K, V};
+    void *out_ptr[3] = {Q_out, K_out, V_out};
+    const int64_t in_stride[3] = {q_stride, k_stride, v_stride};
+    const long long d = head_dim;
+    for (int k = 0; k < 3; ++k) {
+        p.in[k] = static_cast<const __nv_bfloat16 *>(in_ptr[k]);
+        p.in_stride[k] = in_stride[k];
+        p.out[k] = static_cast<__nv_bfloat16 *>(out_ptr[k]);
+        p.heads[k] = k == 0 ? n_q_heads : kv_heads;
+        p.out_seq[k] = static_cast<long long>(s) * p.heads[k] * d;
+        p.out_token[k] = k == 0 ? n_q_heads * d : d;
+        p.out_head[k] = k == 0 ? d : s * d;
+    }
+    p.gain[0] = static_cast<const __nv_bfloat16 *>(q_gain);
+    p.gain[1] = static_cast<const __nv_bfloat16 *>(k_gain);
     p.cos = cos_table;
     p.sin = sin_table;
     p.positions = positions;
-    p.q_out = static_cast<__nv_bfloat16 *>(Q_out);
-    p.k_out = static_cast<__nv_bfloat16 *>(K_out);
-    p.v_out = static_cast<__nv_bfloat16 *>(V_out);
     p.eps = eps;
     p.tokens = static_cast<int>(tokens);
     p.s = s;
-    p.h = n_q_heads;
-    p.g = kv_heads;
-    p.heads = static_cast<int>(heads);
     p.rot = rot_dim;
     p.n_pos = n_pos;
-    p.interleaved = interleaved != 0 ? 1 : 0;
-    // Few tokens: one load a lane, so that the heads spread over the GPU.  Many: four, for the bytes
-    // in flight and the table's reuse.
-    const int hpi = 256 / head_dim;
+    // Few tokens: a load a warp, so that the heads spread over the GPU.  Many: all of a kind's heads, for
+    // the factors' reuse.
+    const int hpi = 512 / head_dim;
     const long long loads = tokens * ((heads + hpi - 1) / hpi);
-    const int U = loads >= 152LL * 64 * 4 ? 4 : 1;
-    p.chunks = static_cast<int>((heads + static_cast<long long>(U) * hpi - 1) / (U * hpi));
-    const long long blocks = (tokens * p.chunks + kNormThreads / 32 - 1) / (kNormThreads / 32);
-    if (blocks > 0x7fffffffLL)
-        return fail(MLKV_ERR_UNSUPPORTED, "%lld tokens of %lld heads exceed what one call takes",
-                    tokens, heads);
+    p.per_block = loads >= 152LL * 64 ? 8 * kNormLoads * hpi : hpi;
+    long long blocks = 0;
+    for (int k = 0; k < 3; ++k) {
+        p.wide[k] = 1;
+        while (p.wide[k] < hpi && p.wide[k] < p.heads[k])
+            p.wide[k] *= 2;
+        p.parts[k] = (p.heads[k] + p.per_block - 1) / p.per_block;
+        p.first_block[k] = static_cast<unsigned>(blocks);
+        const long long a_block = kNormThreads / 32 * (hpi / p.wide[k]);
+        if (in_ptr[k] != nullptr)
+            blocks += (tokens + a_block - 1) / a_block * p.parts[k];
+        if (blocks > 0x7fffffffLL)
+            return fail(MLKV_ERR_UNSUPPORTED, "%lld tokens of %lld heads exceed what one call takes",
+                        tokens, heads);
+    }
     DeviceGuard guard(current_device());
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(blocks));
@@ -302,8 +356,7 @@ extern "C" int mlkv_qk_norm_rope(const void *Q, const void *K, const void *V, in
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     void *args[] = {&p};
-    const void *fn = head_dim == 64 ? (U == 4 ? norm_fn<64, 4>() : norm_fn<64, 1>())
-                                    : (U == 4 ? norm_fn<128, 4>() : norm_fn<128, 1>());
+    const void *fn = head_dim == 64 ? norm_fn<64>(interleaved != 0) : norm_fn<128>(interleaved != 0);
     const cudaError_t e = cudaLaunchKernelExC(&cfg, fn, args);
     return e == cudaSuccess ? MLKV_OK : fail_cuda(e, "qk_norm_rope launch");
 }
