@@ -66,14 +66,9 @@ struct Q4Layout {
     }
 };
 
-// A word's pair j, half o: mask, lowest bit of the magnitude, sign bit; the bits of half o of all pairs.
 constexpr uint32_t kQ4Mask = 0x87008700u;
 constexpr float kQ4Unit = 65536.f;   // what makes a magnitude whole
-__host__ __device__ constexpr int q4_mag(int j, int o)
-{
-    return 16 * o + (j == 0 ? 8 : j == 1 ? 12 : j == 2 ? 0 : 4);
-}
-__host__ __device__ constexpr int q4_sign(int j, int o) { return (q4_mag(j, o) + 7) & 31; }
+// The bits of half o of all pairs.
 __host__ __device__ constexpr uint32_t q4_bits(int o) { return o ? 0xfff70008u : 0x0008fff7u; }
 
 #ifdef __CUDACC__
@@ -82,6 +77,12 @@ __device__ __forceinline__ uint32_t q4_pair(uint32_t w, int j)
 {
     const uint32_t x = j == 0 ? w : j == 1 ? __funnelshift_r(w, w, 4) : j == 2 ? w * 256u : w * 16u;
     return x & kQ4Mask;
+}
+
+// The word of four pairs (bits of kQ4Mask only).
+__device__ __forceinline__ uint32_t q4_word(uint32_t p0, uint32_t p1, uint32_t p2, uint32_t p3)
+{
+    return p0 | __funnelshift_l(p1, p1, 4) | p2 >> 8 | p3 >> 4;
 }
 #endif
 
