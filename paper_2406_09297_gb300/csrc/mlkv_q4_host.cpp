@@ -293,7 +293,7 @@ int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *o
         return true;
     };
     // One wave of resident CTAs.  A warp a run where each gets at least 8 tiles (and no segment more
-    // records than one merge takes), else a CTA a run, with at least a tile for every warp.  The start and
+    // records than one merge takes), else a CTA a run.  The start and
     // end of a segment's part cost a warp ~2 us and more, a tile 1.75: three empty tiles a segment (64
     // uneven sequences of up to 8192 positions, 8 KV heads of 128: 58.8, 57.5, 56.6 us with 1, 2, 3).
     if (!lay_tiles(3))
@@ -303,7 +303,14 @@ int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *o
     const bool warp_runs = tiles >= 8 * slots * W && pieces <= mlkv::kCombineMaxPiecesHost;
     if (!warp_runs) {
         lay_tiles(0);
-        grid = static_cast<int>(std::max(1LL, std::min(slots, (tiles + W - 1) / W)));
+        // Few segments: k CTAs for each (of the mean length), the fewest whose warps take no more tiles
+        // in turn than those of the most CTAs there are; else all of those.
+        const long long S = static_cast<long long>(c->b) * c->g;
+        if (S <= slots) {
+            const long long nt = (tiles + S - 1) / S;
+            const long long turns = (nt + W * (slots / S) - 1) / (W * (slots / S));
+            grid = static_cast<int>(S * ((nt + W * turns - 1) / (W * turns)));
+        }
         pieces = mlkv::max_pieces_per_segment(m, T, grid);
     }
     p.deferred_merge = pieces > mlkv::kQ4InlineMergePieces ? 1 : 0;
