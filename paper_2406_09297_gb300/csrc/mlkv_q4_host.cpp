@@ -271,13 +271,17 @@ int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *o
     m.ml_layers = 0;
     // Every segment's tiles and `empty` more; the merges see lengths whose plain tiling gives them.
     long long tiles = 0;
+    int nt_min = 0x7fffffff, nt_max = 0;   // of a segment
     auto lay_tiles = [&](int empty) {
         tiles = 0;
         bool uniform = true;
         for (int beta = 0; beta < c->b; ++beta) {
             const int L = seq_lens[beta];
             uniform = uniform && L == seq_lens[0];
-            const int nt = mlkv::visible_tiles(L, window, sinks, T, mlkv::kQ4Block).nt + empty;
+            const int real = mlkv::visible_tiles(L, window, sinks, T, mlkv::kQ4Block).nt;
+            const int nt = real + empty;
+            nt_min = std::min(nt_min, real);
+            nt_max = std::max(nt_max, real);
             p.seq_len[beta] = L;
             m.seq_len[beta] = nt * T;
             p.tile_start[beta] = m.tile_start[beta] = static_cast<int>(tiles);
@@ -292,15 +296,20 @@ int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *o
         m.uniform_len = uniform ? m.seq_len[0] : 0;
         return true;
     };
-    // One wave of resident CTAs.  A warp a run where each gets at least 8 tiles (and no segment more
-    // records than one merge takes), else a CTA a run.  The start and
-    // end of a segment's part cost a warp ~2 us and more, a tile 1.75: three empty tiles a segment (64
-    // uneven sequences of up to 8192 positions, 8 KV heads of 128: 58.8, 57.5, 56.6 us with 1, 2, 3).
+    // One wave of resident CTAs.  A run of tiles is a warp's or a CTA's.  A warp's costs records and their
+    // merge, a CTA's that its warps wait for one another at a segment's ends (~3 us, against 2 of one
+    // warp).  So a warp a run where there are many tiles a warp, or segments of uneven lengths, which meet
+    // many ends in some runs (never a segment with more records than one merge takes); measured, us, a
+    // warp / a CTA a run: 64 uneven sequences of up to 8192 positions, 8 KV heads of 128, 56.6 / 84.9; 32
+    // of 4096 (13 tiles a warp) 35.8 / 31.9; 64 of 4096 (27) 57.9 / 59.2; 128 of 4096 (54) 102.5 / 108.4.
+    // Three empty tiles stand for the cost of a segment's ends to a warp (58.8, 57.5, 56.6 us for the
+    // uneven ones with 1, 2, 3).
     if (!lay_tiles(3))
         return fail(MLKV_ERR_UNSUPPORTED, "the tiles exceed the int32 tile index");
     int grid = static_cast<int>(slots);
     int pieces = mlkv::max_pieces_per_segment(m, T, grid * W);
-    const bool warp_runs = tiles >= 8 * slots * W && pieces <= mlkv::kCombineMaxPiecesHost;
+    const bool even = nt_max <= nt_min + nt_min / 4 + 1;
+    const bool warp_runs = tiles >= (even ? 24 : 8) * slots * W && pieces <= mlkv::kCombineMaxPiecesHost;
     if (!warp_runs) {
         lay_tiles(0);
         // Few segments: k CTAs for each (of the mean length), the fewest whose warps take no more tiles

@@ -177,12 +177,13 @@ def _uneven(n, most):
 
 
 @pytest.mark.parametrize("d,h,g,lens,window,sinks", [
-    (64, 12, 4, [5000] * 80, 0, 0),              # the smallest launches in which every warp has a run
+    (64, 12, 4, [5000] * 40 + [3000] * 60, 0, 0),   # every warp has a run, of few tiles
+    (128, 32, 8, [9000] * 32, 0, 0),             # equal lengths
     (64, 12, 1, _uneven(90, 60000), 0, 0),
     (128, 32, 8, _uneven(64, 8000), 0, 0),
     (128, 32, 2, _uneven(100, 16000), 0, 0),     # groups of 16
     (128, 8, 2, _uneven(300, 9000), 3000, 70),
-    (64, 16, 1, [131072] * 10, 0, 0),            # hundreds of runs a segment
+    (64, 16, 1, [131072] * 22, 0, 0),            # dozens of runs a segment
 ])
 def test_decode_warp_runs(d, h, g, lens, window, sinks):
     out = _decode(d, h, g, lens, window, sinks)
