@@ -41,7 +41,7 @@ namespace {
 template <int D, int NB, bool kWarpRuns>
 struct Q4Plan {
     using LY = Q4Layout<D>;
-    static constexpr int kWarps = q4_warps(8 * NB);
+    static constexpr int kWarps = q4_warps(D, 8 * NB);
     static constexpr int kThreads = kWarps * 32;
     static constexpr int kT = q4_tile_tokens(D);
     static constexpr int kSub = kT / kQ4Block;                  // blocks of a tile
@@ -870,7 +870,7 @@ cudaError_t prepare_q4_decode(int d, int group, int *ctas_per_sm)
                                              static_cast<int>(v.smem));
         int n = 0;
         if (e == cudaSuccess)
-            e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, v.fn, q4_warps(group) * 32,
+            e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, v.fn, q4_warps(d, group) * 32,
                                                               v.smem);
         if (e != cudaSuccess)
             return e;
@@ -885,7 +885,7 @@ cudaError_t launch_q4_decode(int d, int grid, bool warp_runs, const Q4DecodePara
     const Variant v = find_variant(d, p.G, warp_runs);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(grid));
-    cfg.blockDim = dim3(static_cast<unsigned>(q4_warps(p.G) * 32));
+    cfg.blockDim = dim3(static_cast<unsigned>(q4_warps(d, p.G) * 32));
     cfg.dynamicSmemBytes = v.smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];

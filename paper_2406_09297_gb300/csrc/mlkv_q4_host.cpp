@@ -137,7 +137,7 @@ int mlkv_q4_create(mlkv_q4cache_t *out, int n_layers, int n_q_heads, int head_di
     c->cache_bytes = rows * c->m * c->row_bytes;
     // a record for each segment and each run of a launch
     const size_t records =
-        rows + static_cast<size_t>(c->ctas_per_sm) * c->sm_count * mlkv::q4_warps(c->G);
+        rows + static_cast<size_t>(c->ctas_per_sm) * c->sm_count * mlkv::q4_warps(c->d, c->G);
     auto alloc = [&](void **ptr, size_t n) {
         if (e == cudaSuccess)
             e = cudaMalloc(ptr, n);
@@ -261,7 +261,7 @@ int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *o
     mlkv::clamp_window(c->max_seq, &window, &sinks);
     static thread_local mlkv::Q4DecodeParams p;
     static thread_local mlkv::DecodeParams m;   // what the merges see
-    const int T = mlkv::q4_tile_tokens(c->d), W = mlkv::q4_warps(c->G);
+    const int T = mlkv::q4_tile_tokens(c->d), W = mlkv::q4_warps(c->d, c->G);
     const long long slots = std::min<long long>(static_cast<long long>(c->ctas_per_sm) * c->sm_count,
                                                 mlkv::kCombineMaxPiecesHost);
     m.b = c->b;
