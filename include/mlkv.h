@@ -265,7 +265,9 @@ int mlkv_prefill_window(mlkv_cache_t c, int layer, const void *Q, const void *K,
  *
  *   Q          device bf16, batch * s tokens of n_q_heads heads of head_dim; token k at Q + k q_stride
  *   K, V       the same with kv_heads heads and their strides (the three may be parts of one fused
- *              projection); V and V_out may both be NULL, else values are copied unchanged
+ *              projection); values are copied unchanged.  V and V_out may both be NULL, and so may all
+ *              four of K, K_out, V and V_out: a layer that reads another's cache has queries alone
+ *              (kv_heads is then ignored)
  *   *_stride   elements between tokens, >= 0, a multiple of 8
  *   q_gain, k_gain   device bf16 [head_dim], or NULL: gain 1
  *   cos_table, sin_table   device fp32 [n_pos][rot_dim / 2]

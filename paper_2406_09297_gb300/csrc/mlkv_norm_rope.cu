@@ -240,11 +240,15 @@ extern "C" int mlkv_qk_norm_rope(const void *Q, const void *K, const void *V, in
                                  void *cuda_stream)
 {
     using namespace mlkv;
-    if (Q == nullptr || K == nullptr || Q_out == nullptr || K_out == nullptr)
-        return fail(MLKV_ERR_INVALID_ARG, "Q, K, Q_out and K_out must be non-NULL");
-    if ((V == nullptr) != (V_out == nullptr))
-        return fail(MLKV_ERR_INVALID_ARG, "V and V_out must both be given or both be NULL");
-    if (batch < 1 || s < 1 || n_q_heads < 1 || kv_heads < 1)
+    if (Q == nullptr || Q_out == nullptr)
+        return fail(MLKV_ERR_INVALID_ARG, "Q and Q_out must be non-NULL");
+    if ((K == nullptr) != (K_out == nullptr) || (V == nullptr) != (V_out == nullptr))
+        return fail(MLKV_ERR_INVALID_ARG, "K and K_out, V and V_out: both given or both NULL");
+    if (K == nullptr && V != nullptr)
+        return fail(MLKV_ERR_INVALID_ARG, "V without K");
+    if (K == nullptr)
+        kv_heads = 0;
+    if (batch < 1 || s < 1 || n_q_heads < 1 || kv_heads < (K != nullptr))
         return fail(MLKV_ERR_INVALID_ARG, "sizes must be positive (batch=%d s=%d h=%d g=%d)", batch,
                     s, n_q_heads, kv_heads);
     if (head_dim != 64 && head_dim != 128)
@@ -274,6 +278,10 @@ extern "C" int mlkv_qk_norm_rope(const void *Q, const void *K, const void *V, in
     if (tokens > 0x7fffffffLL || heads > (1 << 20))
         return fail(MLKV_ERR_UNSUPPORTED, "%lld tokens of %lld heads exceed what one call takes",
                     tokens, heads);
+    for (const int64_t st : {q_stride, k_stride, v_stride})   // addresses stay below 2^62
+        if (st > (1LL << 60) / tokens)
+            return fail(MLKV_ERR_UNSUPPORTED, "a token stride of %lld elements exceeds what one call takes",
+                        static_cast<long long>(st));
     // Outputs may not share memory with inputs or each other, but for one that is its own input, row
     // for row (each warp then reads a head before it writes it).
     const size_t dd = static_cast<size_t>(head_dim) * 2;
@@ -289,7 +297,7 @@ extern "C" int mlkv_qk_norm_rope(const void *Q, const void *K, const void *V, in
     const Span ins[3] = {in(Q, q_stride, n_q_heads), in(K, k_stride, kv_heads),
                          in(V, v_stride, kv_heads)};
     const Span outs[3] = {{Q_out, static_cast<size_t>(tokens) * n_q_heads * dd},
-                          {K_out, static_cast<size_t>(tokens) * kv_heads * dd},
+                          {K_out, K_out != nullptr ? static_cast<size_t>(tokens) * kv_heads * dd : 0},
                           {V_out, V_out != nullptr ? static_cast<size_t>(tokens) * kv_heads * dd : 0}};
     const bool same[3] = {Q_out == Q && q_stride == static_cast<int64_t>(n_q_heads) * head_dim,
                           K_out == K && s == 1 && k_stride == static_cast<int64_t>(kv_heads) * head_dim,

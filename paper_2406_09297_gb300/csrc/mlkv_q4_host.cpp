@@ -115,8 +115,13 @@ int mlkv_q4_create(mlkv_q4cache_t *out, int n_layers, int n_q_heads, int head_di
     c->G = n_q_heads / kv_heads_per_owner;
     c->b = batch;
     c->max_seq = max_seq;
-    c->owner.assign(layer_owner, layer_owner + n_layers);
-    c->slot.resize(n_layers);
+    try {
+        c->owner.assign(layer_owner, layer_owner + n_layers);
+        c->slot.resize(n_layers);
+    } catch (const std::bad_alloc &) {
+        delete c;
+        return fail(MLKV_ERR_OOM, "out of host memory");
+    }
     for (int n = 0; n < n_layers; ++n)   // an owner comes before its readers
         c->slot[n] = c->owner[n] == n ? c->m++ : c->slot[c->owner[n]];
     c->device = mlkv::current_device();

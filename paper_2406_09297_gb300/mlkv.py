@@ -347,10 +347,10 @@ def _dense(x, n, what):
 def mlkv_qk_norm_rope(Q, K, V, q_gain, k_gain, cos, sin, positions, Q_out, K_out, V_out, eps=1e-6,
                       interleaved=False, stream=None):
     """Q [b][s][h][d], K and V [b][s][g][d] (views of a fused projection will do; V and V_out may be
-    None), gains [d] or None, cos and sin fp32 [n_pos][rot / 2] and positions int32 [b][s] (None: no
+    None, K and K_out too where a layer has queries alone), gains [d] or None, cos and sin fp32 [n_pos][rot / 2] and positions int32 [b][s] (None: no
     rotary encoding) -> Q_out [b][s][h][d], K_out and V_out [b][g][s][d], all bf16."""
     b, s, h, d = Q.shape
-    g = K.shape[2]
+    g = 0 if K is None else K.shape[2]
     tokens = b * s
     n_pos = half = 0
     p_cos = p_sin = p_pos = None
@@ -363,13 +363,13 @@ def mlkv_qk_norm_rope(Q, K, V, q_gain, k_gain, cos, sin, positions, Q_out, K_out
         p_pos = _dense(positions, tokens, "positions")
     kv = tokens * g * d
     return _check(lib.mlkv_qk_norm_rope(
-        Q.data_ptr(), K.data_ptr(), _ptr(V), _token_stride(Q, "Q", b, s, h, d),
-        _token_stride(K, "K", b, s, g, d), 0 if V is None else _token_stride(V, "V", b, s, g, d),
+        Q.data_ptr(), _ptr(K), _ptr(V), _token_stride(Q, "Q", b, s, h, d),
+        0 if K is None else _token_stride(K, "K", b, s, g, d), 0 if V is None else _token_stride(V, "V", b, s, g, d),
         None if q_gain is None else _dense(q_gain, d, "q_gain"),
         None if k_gain is None else _dense(k_gain, d, "k_gain"), p_cos, p_sin, n_pos, 2 * half,
         int(interleaved), p_pos, eps, b, s, h, g, d, _dense(Q_out, tokens * h * d, "Q_out"),
-        _dense(K_out, kv, "K_out"), None if V_out is None else _dense(V_out, kv, "V_out"),
-        _stream(stream)))
+        None if K_out is None else _dense(K_out, kv, "K_out"),
+        None if V_out is None else _dense(V_out, kv, "V_out"), _stream(stream)))
 
 
 def mlkv_q4_create(n_layers, n_q_heads, head_dim, layer_owner, kv_heads_per_owner, batch, max_seq):

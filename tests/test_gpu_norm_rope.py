@@ -116,3 +116,16 @@ def test_position_outside_the_table():
         assert torch.isnan(out[:, 1:3, :, :16]).all()
         assert torch.isfinite(out[:, 1:3, :, 16:]).all()
         assert torch.isfinite(out[:, [0, 3]]).all()
+
+
+@pytest.mark.parametrize("s", [1, 700])
+def test_queries_alone(s):
+    """A layer that reads another's cache has no keys of its own."""
+    torch.manual_seed(11)
+    Q = torch.randn((3, s, 12, 64), device="cuda").bfloat16()
+    gain = torch.randn(64, device="cuda").bfloat16()
+    cos, sin = _tables(32)
+    pos = torch.randint(0, N_POS, (3, s), device="cuda", dtype=torch.int32)
+    out = torch.empty_like(Q)
+    mlkv.mlkv_qk_norm_rope(Q, None, None, gain, None, cos, sin, pos, out, None, None)
+    _check(out, *_want(Q, gain, cos, sin, pos, 1e-6, False))
