@@ -300,9 +300,10 @@ void set_last_error(const char *msg);
 int max_pieces_per_segment(const DecodeParams &p, int T, int grid);
 
 // Merges the partials of every split segment of the decode launch described by p (which must
-// have deferred_merge = 1), launched right after it on the same stream.
+// have deferred_merge = 1), launched right after it on the same stream.  wide: 1024 threads a CTA,
+// which hold four times the records of 256 at a time.
 cudaError_t launch_combine(const DecodeParams &p, int head_dim, cudaStream_t stream,
-                           bool pdl = true);
+                           bool pdl = true, bool wide = false);
 
 // Pieces per segment above which the decode launch defers its merges to combine_kernel, for records
 // of `group` rows of d floats.  A record of at most 512 floats is one pass of the consumer threads,

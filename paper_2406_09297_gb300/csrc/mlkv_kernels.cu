@@ -1164,15 +1164,14 @@ __global__ void __launch_bounds__(Plan<D, T, STAGES, NCW, kT>::kThreads,
 // weights w_c = 2^(lse_c - M) (M = max_c lse_c) and each thread sums w_c * o_c[e] for one column
 // e over a strided subset of the pieces, 16 loads in flight (the first 16 issued with the
 // log-sum-exps); the subsets are added through shared memory and scaled by 1 / sum_c w_c.
-constexpr int kCombineThreads = 256;
 constexpr int kCombineMaxPieces = 1024;
 
-template <int D>
-__global__ void __launch_bounds__(kCombineThreads)
+template <int D, int kThreads>
+__global__ void __launch_bounds__(kThreads)
     combine_kernel(const __grid_constant__ DecodeParams p)
 {
     __shared__ float s_w[kCombineMaxPieces];
-    __shared__ float s_red[kCombineThreads];
+    __shared__ float s_red[kThreads];
     // The next layer's decode may start at once: it reads neither the partials nor `out`, and it
     // writes partials only after its own dependency wait (after this grid).
     grid_dependents_launch();
@@ -1219,9 +1218,9 @@ __global__ void __launch_bounds__(kCombineThreads)
     const int j = seg - beta * p.g;
     const int tid = threadIdx.x;
     const int lane = tid & 31, wid = tid >> 5;
-    constexpr int kWarps = kCombineThreads / 32;
+    constexpr int kWarps = kThreads / 32;
     const float NEG_INF = -__int_as_float(0x7f800000);
-    constexpr int kGroups = kCombineThreads / D;   // pieces summed side by side per column
+    constexpr int kGroups = kThreads / D;   // pieces summed side by side per column
     const int e = tid % D;
     const int grp = tid / D;
     const float *src = p.part_o + rec0 * G * D + static_cast<size_t>(row) * D + e;
@@ -1234,7 +1233,7 @@ __global__ void __launch_bounds__(kCombineThreads)
         v[m] = k < np ? __ldcg(src + static_cast<size_t>(k) * G * D) : 0.f;
     }
     float mx = NEG_INF;
-    for (int k = tid; k < np; k += kCombineThreads) {
+    for (int k = tid; k < np; k += kThreads) {
         const float l = __ldcg(&p.part_lse[(rec0 + k) * G + row]);
         s_w[k] = l;
         mx = fmaxf(mx, l);
@@ -1251,7 +1250,7 @@ __global__ void __launch_bounds__(kCombineThreads)
     for (int w = 1; w < kWarps; ++w)
         mx = fmaxf(mx, s_red[w]);
     float tot = 0.f;
-    for (int k = tid; k < np; k += kCombineThreads) {
+    for (int k = tid; k < np; k += kThreads) {
         const float w = fast_exp2(s_w[k] - mx);
         s_w[k] = w;
         tot += w;
@@ -1455,12 +1454,12 @@ int max_pieces_per_segment(const DecodeParams &p, int T, int grid)
     return worst;
 }
 
-cudaError_t launch_combine(const DecodeParams &p, int head_dim, cudaStream_t stream, bool pdl)
+cudaError_t launch_combine(const DecodeParams &p, int head_dim, cudaStream_t stream, bool pdl, bool wide)
 {
     cudaLaunchConfig_t cfg = {};
     const int segs = p.b * p.g * (p.ml_layers > 0 ? p.ml_layers : 1);
     cfg.gridDim = dim3(static_cast<unsigned>(segs), static_cast<unsigned>(p.G));
-    cfg.blockDim = dim3(kCombineThreads);
+    cfg.blockDim = dim3(wide ? 1024 : 256);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1468,8 +1467,10 @@ cudaError_t launch_combine(const DecodeParams &p, int head_dim, cudaStream_t str
     cfg.attrs = attr;
     cfg.numAttrs = pdl ? 1 : 0;
     void *args[] = {const_cast<DecodeParams *>(&p)};
-    const void *fn = head_dim == 64 ? reinterpret_cast<const void *>(&combine_kernel<64>)
-                                    : reinterpret_cast<const void *>(&combine_kernel<128>);
+    const void *fn = head_dim == 64 ? wide ? reinterpret_cast<const void *>(&combine_kernel<64, 1024>)
+                                           : reinterpret_cast<const void *>(&combine_kernel<64, 256>)
+                     : wide         ? reinterpret_cast<const void *>(&combine_kernel<128, 1024>)
+                                    : reinterpret_cast<const void *>(&combine_kernel<128, 256>);
     return cudaLaunchKernelExC(&cfg, fn, args);
 }
 

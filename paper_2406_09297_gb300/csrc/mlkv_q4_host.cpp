@@ -354,7 +354,11 @@ int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *o
         m.part_lse = p.part_lse;
         m.tile_tokens = T;
         m.decode_grid = grid * (warp_runs ? W : 1);
-        if ((e = mlkv::launch_combine(m, c->d, stream)) != cudaSuccess)
+        // 256 threads a row take 4096 / d records a round trip to L2, 1024 four times as many but ~1 us
+        // more for themselves: wide from the third round trip on (256 / 1024 threads, us: 171 records of
+        // 12 heads of 64 12.7 / 11.1, 128 of 16 heads of 128 14.6 / 10.9; two: 38 of 128 14.5 / 15.7).
+        const bool wide = pieces > 2 * 4096 / c->d;
+        if ((e = mlkv::launch_combine(m, c->d, stream, true, wide)) != cudaSuccess)
             return fail_cuda(e, "combine launch");
     }
     return MLKV_OK;
