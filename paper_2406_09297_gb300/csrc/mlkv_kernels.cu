@@ -167,6 +167,8 @@ constexpr uint32_t kOnesBf16x2 = 0x3f803f80u;
 // Measured on GB300 (layer calls, 16-row form -> this one): 32 layers of 8 uneven sequences, 8 KV
 // heads of 128 with 4 heads each 413 -> 404 us; 12 layers of 128 uneven sequences, 4 KV heads of 64
 // with 3 heads each 602 -> 579 us.
+// kWin: a sliding window with sinks; a segment's tiles are those with visible positions (visible_tiles).
+// 32 uneven sequences of up to 16384, window 2048, 16 sinks, 8 KV heads of 128: 40.7 us, 5.7 TB/s.
 template <int D, int T, int STAGES, int NCW, bool kT, bool kWin = false>
 __global__ void __launch_bounds__(Plan<D, T, STAGES, NCW, kT>::kThreads,
                                   Plan<D, T, STAGES, NCW, kT>::kMinBlocks)

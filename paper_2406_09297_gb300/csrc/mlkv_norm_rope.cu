@@ -14,6 +14,11 @@
 // A block's warps take heads of one kind (queries, keys or values), whose addresses are then uniform: a
 // token each and 512 / D heads at a time, two such loads in flight, or, where a token has fewer heads of
 // the kind, those of several tokens.
+//
+// Measured on GB300: 16,004 tokens of 32 + 8 + 8 heads of 128 in 63.3 us, 6.2 TB/s of 6.8 (97.6 with the
+// partner channels fetched from other lanes and factors made a head); 16,016 of 12 + 4 + 4 heads of 64 in
+// 21.0 us, 3.9 TB/s: there a token's factors serve one or two loads, and their latency bounds it.  A
+// batch's single tokens are bound by the caller: 8.2 us of Python and launch.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>

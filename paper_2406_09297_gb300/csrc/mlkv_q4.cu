@@ -7,9 +7,13 @@
 // quotient's distance from n + 1/2 is a multiple of 1 / (2 S), S the scale's significand, shifted by
 // at most the quotient's own exponent).  x times the approximate reciprocal of s, raised by 2^-16 of
 // itself, is therefore on the right side of every half; the sum of its magnitude and 1.5 2^23 rounds it
-// and leaves the code's magnitude in the low bits: one multiply-add a channel.  Likewise max |x| times fp32(1/7) rounds to the
-// same bf16 as the exact quotient, which is at least 2^-12 of itself away from a bf16 midpoint unless
-// it is a bf16.
+// and leaves the code's magnitude in the low bits: one multiply-add a channel.  Likewise max |x| times
+// fp32(1/7) rounds to the same bf16 as the exact quotient, which is at least 2^-12 of itself away from a
+// bf16 midpoint unless it is a bf16.
+//
+// HBM-bound: 2 bytes a channel on one side, 0.5625 on the other.  Measured on GB300, K and V of 8 sequences
+// of 4096 positions, 8 KV heads of 128 (floor 25.3 us each way): store 32.4 us, 5.3 TB/s; read 28.8 us, 6.0
+// TB/s.  A batch's new tokens are bound by the call (4.0 us in Python).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>

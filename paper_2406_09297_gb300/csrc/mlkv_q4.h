@@ -133,7 +133,7 @@ cudaError_t prepare_q4_decode(int d, int group, int *ctas_per_sm);
 // 32 sequences of 16384, groups of 16 heads of 128, with 4 / 5 / 6 / 8 warps 46.9 / 55.1 / 49.7 / 81.5; 64 of
 // 16384, groups of 12 heads of 64, 27.8 / 30.8 / 27.0 / 28.4.
 constexpr int q4_warps(int d, int group) { return group <= 8 ? 8 : d == 64 ? 6 : 4; }
-// Records of a segment up to which the launch merges them itself.
+// Records of a segment up to which the launch merges them itself (more take a launch of their own, ~3 us).
 constexpr int kQ4InlineMergePieces = 16;
 // warp_runs: P = grid x warps runs of tiles, a warp each; else P = grid, a CTA each (see the kernel).
 cudaError_t launch_q4_decode(int d, int grid, bool warp_runs, const Q4DecodeParams &p,

@@ -12,6 +12,11 @@
 //   O = V^T P^T, 16 channels by 8 heads.  The group's scale goes into P: P' = fp16(fp16(p) s / f), f a
 //       power of two that bounds the scales the warp has met (raised with a rescaled O, like the
 //       running maximum), so that fp16's range holds whatever the values' magnitude.
+// Measured on GB300, one layer, 8 KV heads of 128 with 4 query heads each, us (TB/s of 6.8): 128 sequences
+// of 4096 positions 102.5 (5.9), 64 57.9 (5.2), 32 32.0 (4.7), 64 uneven ones of up to 8192 56.6 (4.9).
+// The stream itself runs at HBM's rate (44.5 us more for 44.4 us more of bytes); what is left is ~3 us of
+// start and, at the end, warps that finish up to 12 us apart and then merge for 3 to 5 us.  One sequence of
+// 131072, 12 heads of 64 over one KV head: 11.1, two launches' latencies.
 // (Tried before.  Codes as bf16 128 + c, the surplus cancelled in the accumulators, P in bf16: as fast,
 // outputs 0.0024 to 0.0029 from the 64-bit ones instead of 0.0017.  K in e4m3: mma.sync takes 8-bit
 // operands apart again, 385 instructions per 16 positions of 128 channels and 8 heads.)
