@@ -291,6 +291,20 @@ int mlkv_qk_norm_rope(const void *Q, const void *K, const void *V, int64_t q_str
                       int n_q_heads, int kv_heads, int head_dim, void *Q_out, void *K_out,
                       void *V_out, void *cuda_stream);
 
+/* The same call with its arguments in a struct (read during the call alone), for callers whose foreign
+ * calls cost by the argument.  Errors as above, and MLKV_ERR_INVALID_ARG for a NULL args. */
+typedef struct {
+    const void *Q, *K, *V;
+    int64_t q_stride, k_stride, v_stride;
+    const void *q_gain, *k_gain;
+    const float *cos_table, *sin_table;
+    const int *positions;
+    void *Q_out, *K_out, *V_out, *cuda_stream;
+    int32_t n_pos, rot_dim, interleaved, batch, s, n_q_heads, kv_heads, head_dim;
+    float eps;
+} mlkv_qk_norm_rope_args;
+int mlkv_qk_norm_rope_struct(const mlkv_qk_norm_rope_args *args);
+
 /*
  * The 4-bit cache: the m owner layers' keys and values (Sec. 3) in 4 bits a channel, for contexts or
  * batches whose bf16 cache is too large or too slow to read; 0.28 of its bytes.

@@ -456,11 +456,27 @@ static int decode_impl(mlkv_cache_t c, int layer, const void *K_new, const void 
     if (rc != MLKV_OK)
         return rc;
     // What a sliding window leaves of a length, in positions (the tiles' count follows below).
-    auto seen = [&](int L) { return window > 0 && L - window > sinks ? window + sinks : L; };
+    auto gap = [&](int L) { return window > 0 && L - window > sinks; };
+    auto seen = [&](int L) { return gap(L) ? window + sinks : L; };
     double mean_len = 0.0;
-    for (int beta = 0; beta < c->b; ++beta)
+    bool even = true;   // every sequence shows the same tiles
+    for (int beta = 0; beta < c->b; ++beta) {
         mean_len += seen(seq_lens[beta]);
+        even = even && seen(seq_lens[beta]) == seen(seq_lens[0]) &&
+               gap(seq_lens[beta]) == gap(seq_lens[0]);
+    }
     mean_len /= c->b;
+    // Windows of one visible length on d = 64, as many segments as CTAs of the 256-position tile fit: that
+    // tile, mostly a whole segment a CTA.  128 / 256 positions, us, 4 sinks: 64 segments of 12 heads,
+    // window 511 6.5 / 5.6, 1020 11.7 / 7.0, 4090 15.4 / 13.3; 128 of 3, 1020 8.9 / 6.7; not for
+    // uneven ones (64 of up to 6000, 511 8.1 / 9.0; 128, 1020 11.2 / 13.2), 256 segments (1020 10.5 / 13.3)
+    // or 32 of more tiles (2040 9.7 / 10.3).
+    const long long segments = static_cast<long long>(c->b) * c->g;
+    const int window_tile =
+        window > 0 && even && c->d == 64 && c->tile_tokens == 0 && segments <= c->sm_count &&
+                (segments >= 64 || (segments >= 32 && mean_len <= 5 * 256)) && mean_len > 128
+            ? 256
+            : 0;
     // Inside a decode step, a layer that is one long segment (d = 64) runs on the 128-position
     // tile (two CTAs per SM) over 64 CTAs, so the next layers' grids stream beside it (measured,
     // batch 1, 131072 positions, per-layer steps of 12 layers: MLKV-2 63 us against 86 for the
@@ -468,7 +484,7 @@ static int decode_impl(mlkv_cache_t c, int layer, const void *K_new, const void 
     // against 104 and 129).
     const bool single_long = in_step && c->tile_tokens == 0 && c->grid <= 0 && c->d == 64 &&
                              c->b * c->g == 1 && seq_lens[0] >= 16384;
-    mlkv_cache::Variant *var = pick_variant(c, mean_len, single_long ? 128 : 0);
+    mlkv_cache::Variant *var = pick_variant(c, mean_len, single_long ? 128 : window_tile);
     if (var != nullptr && window > 0 && var->v->win_fn == nullptr)   // the tcgen05 kernel has none
         for (auto &v : c->variants)
             if (v.v->win_fn != nullptr && v.v->tile_tokens == var->v->tile_tokens)
@@ -562,7 +578,7 @@ static int decode_impl(mlkv_cache_t c, int layer, const void *K_new, const void 
         grid = static_cast<int>(whole);
     } else {
         grid = static_cast<int>((tiles + per_wave - 1) / per_wave);
-        if (uniform) {
+        if (uniform || (window > 0 && even)) {
             const long long nt = tiles / S_all;
             const long long S = static_cast<long long>(c->b) * c->g;
             const long long per = tiles / grid;
@@ -572,7 +588,7 @@ static int decode_impl(mlkv_cache_t c, int layer, const void *K_new, const void 
                 best = nt;   // whole segments: grid S, each CTA exactly one segment
                 grid = static_cast<int>(S);
             }
-            if (c->cluster) {
+            if (c->cluster && uniform) {
                 // Inside a step whose next layer reads its tiles early (early_fetch), with two
                 // CTAs per SM, a grid that fits twice lets the next layer's CTAs all be resident,
                 // streaming their tiles, while this layer's finish; that hides the ramp of each

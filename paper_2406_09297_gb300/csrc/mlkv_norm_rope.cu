@@ -373,3 +373,13 @@ extern "C" int mlkv_qk_norm_rope(const void *Q, const void *K, const void *V, in
     const cudaError_t e = cudaLaunchKernelExC(&cfg, fn, args);
     return e == cudaSuccess ? MLKV_OK : fail_cuda(e, "qk_norm_rope launch");
 }
+
+extern "C" int mlkv_qk_norm_rope_struct(const mlkv_qk_norm_rope_args *a)
+{
+    if (a == nullptr)
+        return mlkv::fail(MLKV_ERR_INVALID_ARG, "args is NULL");
+    return mlkv_qk_norm_rope(a->Q, a->K, a->V, a->q_stride, a->k_stride, a->v_stride, a->q_gain,
+                             a->k_gain, a->cos_table, a->sin_table, a->n_pos, a->rot_dim,
+                             a->interleaved, a->positions, a->eps, a->batch, a->s, a->n_q_heads,
+                             a->kv_heads, a->head_dim, a->Q_out, a->K_out, a->V_out, a->cuda_stream);
+}

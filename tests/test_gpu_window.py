@@ -63,6 +63,17 @@ def test_decode_splits(d, h, g, lens, window, sinks):
     assert torch.equal(out, _decode(d, h, g, lens, window, sinks))
 
 
+@pytest.mark.parametrize("d,h,g,lens,window,sinks", [
+    (64, 12, 1, [600 + 7 * i for i in range(64)], 511, 4),     # the same tiles, other lengths
+    (64, 12, 4, [1300 + i for i in range(32)], 1020, 0),
+    (64, 3, 1, [512] + [900] * 63, 508, 4),                    # one just inside its window: fewer tiles
+    (64, 12, 1, [2500 + 3 * i for i in range(33)], 2040, 300),
+    (128, 32, 8, [1100 + i for i in range(16)], 1000, 16),
+])
+def test_decode_even_windows_of_uneven_lengths(d, h, g, lens, window, sinks):
+    _decode(d, h, g, lens, window, sinks)
+
+
 def test_decode_no_window_is_the_plain_call():
     """window 0, or one that no length outgrows, gives mlkv_decode_attention's bits."""
     torch.manual_seed(3)

@@ -1,6 +1,7 @@
 """What the entry points around the decode step refuse before they touch a GPU."""
 import ctypes
 import os
+import struct
 
 import numpy as np
 import pytest
@@ -91,6 +92,27 @@ def test_qk_norm_rope_rejects(change, code):
     a = dict(GOOD, **change)
     assert mlkv.lib.mlkv_qk_norm_rope(*[a[k] for k in ORDER], NULL) == code
     assert mlkv.mlkv_last_error()
+
+
+def test_qk_norm_rope_struct_rejects_the_same():
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are made up")
+    assert mlkv.lib.mlkv_qk_norm_rope_struct(NULL) == BAD
+    order = ["Q", "K", "V", "q_stride", "k_stride", "v_stride", "q_gain", "k_gain", "cos", "sin",
+             "positions", "Q_out", "K_out", "V_out", "stream", "n_pos", "rot", "interleaved", "batch", "s",
+             "h", "g", "d", "eps"]
+    # every field at a value that only its own check refuses
+    for change, code in ((dict(Q=0), BAD), (dict(Q_out=0), BAD), (dict(K=0), BAD), (dict(V_out=0), BAD),
+                         (dict(K_out=0), BAD), (dict(V=0), BAD), (dict(q_stride=-8), BAD),
+                         (dict(k_stride=4), BAD), (dict(v_stride=12), BAD), (dict(cos=0), BAD),
+                         (dict(sin=0), BAD), (dict(positions=0), BAD), (dict(q_gain=8), BAD),
+                         (dict(k_gain=8), BAD), (dict(n_pos=0), BAD), (dict(rot=24), UNSUPPORTED),
+                         (dict(batch=0), BAD), (dict(s=0), BAD), (dict(h=0), BAD), (dict(g=0), BAD),
+                         (dict(d=96), UNSUPPORTED), (dict(eps=-1.0), BAD)):
+        a = dict(dict(GOOD, stream=0), **change)
+        args = struct.pack("@3P3q9P8if", *[a[k] for k in order])
+        assert mlkv.lib.mlkv_qk_norm_rope_struct(args) == code, change
 
 
 def test_qk_norm_rope_binding_rejects_layouts():
