@@ -120,7 +120,9 @@ struct Q4DecodeParams {
     int b, h, g, G;
     int window, sinks;
     int num_tiles;
-    int empty_tiles;           // of the tiles: empty ones behind every segment's, its ends' cost
+    // of the tiles: empty ones behind every segment's.  Runs of warps: empty_tiles, for the ends' cost; of
+    // CTAs: as many as make its tiles a multiple of round_tiles, a run's (0: runs of warps)
+    int empty_tiles, round_tiles;
     int uniform_len;           // the common length, or 0
     int deferred_merge;        // 1: combine_kernel merges the records
     int seq_len[MLKV_MAX_BATCH];
@@ -133,7 +135,7 @@ cudaError_t prepare_q4_decode(int d, int group, int *ctas_per_sm);
 // 32 sequences of 16384, groups of 16 heads of 128, with 4 / 5 / 6 / 8 warps 46.9 / 55.1 / 49.7 / 81.5; 64 of
 // 16384, groups of 12 heads of 64, 27.8 / 30.8 / 27.0 / 28.4.
 constexpr int q4_warps(int d, int group) { return group <= 8 ? 8 : d == 64 ? 6 : 4; }
-// Records of a segment up to which the launch merges them itself (more take a launch of their own, ~3 us).
+// Records of warps' runs up to which the warp that finishes a segment merges them (else a launch of its own).
 constexpr int kQ4InlineMergePieces = 16;
 // warp_runs: P = grid x warps runs of tiles, a warp each; else P = grid, a CTA each (see the kernel).
 cudaError_t launch_q4_decode(int d, int grid, bool warp_runs, const Q4DecodeParams &p,

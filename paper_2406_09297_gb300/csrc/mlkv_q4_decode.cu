@@ -13,20 +13,20 @@
 //       power of two that bounds the scales the warp has met (raised with a rescaled O, like the
 //       running maximum), so that fp16's range holds whatever the values' magnitude.
 // Measured on GB300, one layer, 8 KV heads of 128 with 4 query heads each, us (TB/s of 6.8): 128 sequences
-// of 4096 positions 102.5 (5.9), 64 57.9 (5.2), 32 32.0 (4.7), 64 uneven ones of up to 8192 56.6 (4.9).
+// of 4096 positions 102.4 (5.9), 64 57.6 (5.2), 32 30.9 (4.9), 64 uneven ones of up to 8192 56.6 (4.9).
 // The stream itself runs at HBM's rate (44.5 us more for 44.4 us more of bytes); what is left is ~3 us of
 // start and, at the end, warps that finish up to 12 us apart and then merge for 3 to 5 us.  One sequence of
-// 131072, 12 heads of 64 over one KV head: 11.1, two launches' latencies.
+// 131072, 12 heads of 64 over one KV head: 10.7, two launches' latencies.
 // (Tried before.  Codes as bf16 128 + c, the surplus cancelled in the accumulators, P in bf16: as fast,
 // outputs 0.0024 to 0.0029 from the 64-bit ones instead of 0.0017.  K in e4m3: mma.sync takes 8-bit
 // operands apart again, 385 instructions per 16 positions of 128 channels and 8 heads.)
 //
-// Work split as in decode_kernel: the tiles of all (sequence, KV head) segments end to end, an equal run
-// of them for each persistent worker, the part of a segment in one run a piece.  Every warp has a ring of
-// its own (one bulk copy a tile: a block's codes and scales lie together).  With many tiles a worker is
-// a warp, which meets no other until it stores its pieces: no barrier, and a piece of a few tiles costs
-// its warp a round trip or two while the others stream.  With few, a CTA is, whose warps take its tiles
-// in turn and merge their sums at the ends of pieces: fewer records for long segments.
+// Work split.  The tiles of all (sequence, KV head) segments end to end, an equal run of them for each
+// worker, the part of a segment in one run a piece.  Every warp has a ring of its own (one bulk copy a tile: a
+// block's codes and scales lie together).  With many tiles a worker is a warp, which meets no other until
+// it stores its pieces: no barrier, and a piece of a few tiles costs its warp a round trip or two while
+// the others stream.  With few, it is a CTA, whose warps take its tiles in turn and merge their sums at its
+// end; segments are filled up with empty tiles so that a run holds tiles of one of them.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -93,7 +93,8 @@ __device__ __forceinline__ void load_segment(const Q4DecodeParams &p, Segment &s
 {
     s.L = p.uniform_len > 0 ? p.uniform_len : p.seq_len[s.beta];
     s.v = visible_tiles(s.L, p.window, p.sinks, T, kQ4Block);
-    s.nt = s.v.nt + p.empty_tiles;
+    s.nt = p.round_tiles > 0 ? (s.v.nt + p.round_tiles - 1) / p.round_tiles * p.round_tiles
+                             : s.v.nt + p.empty_tiles;
 }
 
 template <int T>
@@ -216,6 +217,8 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
 
     // Lane 0 sends the copies of the warp's tiles R ahead; f_run of them follow one another at f_src.
     Segment fs = segment_of_tile<T>(p, tile_lo < N ? tile_lo : N - 1);
+    // where the tiles to read end (a CTA's run lies in one segment, filled up with empty tiles)
+    const int tile_end = kWarpRuns ? tile_hi : min(tile_hi, fs.first + fs.v.nt);
     int f_tile = tile_first, f_it = 0, f_run = 0;
     const uint8_t *f_src = nullptr;
     auto send = [&](uint32_t bytes) {
@@ -234,7 +237,7 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
             --f_run;
             return;
         }
-        for (; f_tile < tile_hi; f_tile += kStep) {
+        for (; f_tile < tile_end; f_tile += kStep) {
             while (f_tile >= fs.first + fs.nt)
                 next_segment<T>(p, fs);
             const int tt = f_tile - fs.first;
@@ -247,7 +250,7 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
                     static_cast<long long>(pos0 / kQ4Block) * LY::kBytes;
             send(static_cast<uint32_t>(n) * LY::kBytes);
             // the whole tiles behind it, of the same part of the segment and this run
-            const int stop = min(tile_hi, fs.first + (tt < fs.v.ns ? fs.v.ns : fs.v.nt)) - 1;
+            const int stop = min(tile_end, fs.first + (tt < fs.v.ns ? fs.v.ns : fs.v.nt)) - 1;
             f_run = f_tile < stop ? (stop - f_tile + kStep - 1) / kStep : 0;
             f_src += kStep * PL::kTileBytes;
             return;
@@ -330,7 +333,7 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
     if (tile_lo >= tile_hi)
         return;
     // The first queries before the first tiles: behind the whole GPU's first tiles they took 4 us.
-    Segment cs = segment_of_tile<T>(p, tile_lo);
+    Segment cs = fs;
     if constexpr (kWarpRuns) {
         WarpQ q;
         load_warp_q(cs, q);
@@ -357,25 +360,13 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
     for (int piece = tile_lo; piece < tile_hi;) {
         const int seg_end = cs.first + cs.nt;
         const int piece_end = min(seg_end, tile_hi);
-        const bool last = piece_end == tile_hi;
+        const bool last = !kWarpRuns || piece_end == tile_hi;
         Segment ns = cs;
         if (!last)
             next_segment<T>(p, ns);
-        // (shared runs: the next piece's queries travel while this one is computed)
-        uint4 q_next[kQPer] = {};
-        if (!last) {
-            if constexpr (kWarpRuns) {
-                // the next piece's queries to L2
-                if (lane * 64 < p.G * D)
-                    asm volatile("prefetch.global.L2 [%0];" ::"l"(
-                        p.Q + (static_cast<size_t>(ns.beta) * p.h + static_cast<size_t>(ns.j) * p.G) * D +
-                        lane * 64));
-            } else {
-#pragma unroll
-                for (int i = 0; i < kQPer; ++i)
-                    q_next[i] = load_q(ns, tid + i * PL::kThreads);
-            }
-        }
+        if (kWarpRuns && !last && lane * 64 < p.G * D)   // the next piece's queries to L2
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(
+                p.Q + (static_cast<size_t>(ns.beta) * p.h + static_cast<size_t>(ns.j) * p.G) * D + lane * 64));
         // A thread's statistics are those of heads 2 tig and 2 tig + 1 (la: over its own positions);
         // O is in units of 2^-16 times the scales' bound.
         float o[NB][2 * NG][4];
@@ -396,9 +387,9 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
             mul[nb][1] = f.y;
         }
         uint32_t *vscale = reinterpret_cast<uint32_t *>(smem + PL::kVs) + warp * 64;
-        for (; tile < piece_end; tile += kStep, ++it) {
+        for (const int stop = kWarpRuns ? piece_end : tile_end; tile < stop; tile += kStep, ++it) {
             const int s = it % R;
-            if (tile - cs.first >= cs.v.nt) {
+            if (kWarpRuns && tile - cs.first >= cs.v.nt) {
                 --it;
                 continue;   // an empty tile
             }
@@ -808,11 +799,6 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
                 }
             }
         }
-        if (!last) {   // every warp has passed this piece's last use of the queries
-#pragma unroll
-            for (int i = 0; i < kQPer; ++i)
-                store_q(q_next[i], tid + i * PL::kThreads);
-        }
         if (!whole && !p.deferred_merge) {
             // The CTA that finishes a segment last merges its records.
             __syncthreads();
@@ -827,9 +813,7 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
                     p.counters[seg] = 0u;
             }
         }
-        __syncthreads();   // the next piece's queries are in place; sums and flags may be rewritten
-        piece = piece_end;
-        cs = ns;
+        break;
     }
     // No copy may still be in flight when the CTA exits (after an expired wait).
     if (lane == 0 && expired) {

@@ -89,6 +89,85 @@ int store(mlkv_q4cache *c, int layer, const void *K, const void *V, int len, con
     return e == cudaSuccess ? MLKV_OK : fail_cuda(e, "4-bit store launch");
 }
 
+constexpr int kEmpty = 3;   // runs of warps: empty tiles behind a segment
+
+// Runs of at least `run` tiles that a segment of nt and the empty ones meets, at most.
+long long warp_pieces(int nt, long long run) { return (nt + kEmpty - 2 + run) / run + 1; }
+
+// Estimated us of merging S segments' records of CTAs, up to `pieces` each: by the CTA that finishes a
+// segment, in round trips to L2 (8 records of four columns a thread), or by a launch of a CTA for every row.
+// Measured, us, the first / the second: one sequence of 8192, 8 KV heads of 128, 4 query heads each, 16
+// records 8.1 / 32 records 7.5; 4 sequences of 4000, 2 KV heads, 16 query heads each, 16 records 11.5 / 9.3,
+// 64 of them, 2 records 27.4 / 34.0.
+struct Q4Merge {
+    float us;
+    bool deferred;
+};
+Q4Merge merge_of(const mlkv_q4cache *c, long long S, long long pieces)
+{
+    if (pieces <= 1)
+        return {0.f, false};
+    const int at_once = 4 * 32 * mlkv::q4_warps(c->d, c->G);
+    const float here = 1.f + 0.9f * ((c->G * c->d + at_once - 1) / at_once) * ((pieces + 7) / 8);
+    const float apart = (c->G <= 8 || c->d == 64 ? 2.4f : 4.2f) + 0.0034f * S * c->G;
+    return {std::min(here, apart), apart < here};
+}
+
+// How a launch's tiles are dealt out (see mlkv_q4_decode_attention).
+struct Q4Deal {
+    int turns;       // of a CTA's warps per run; 0: a run per warp
+    float us;        // estimated
+};
+
+// S segments of at most nt_max tiles, `sum` of them in all (warp_tiles with the empty ones); same: of one
+// number of tiles.  The least of the estimated times, whose terms are fits to calls of 4 to 128 sequences of
+// 64 to 4000 positions, even and uneven.
+Q4Deal deal(const mlkv_q4cache *c, long long S, long long sum, long long warp_tiles, int nt_max, bool same)
+{
+    const int W = mlkv::q4_warps(c->d, c->G);
+    const bool small = c->G <= 8;   // one accumulator
+    // us: a launch's start and end; a tile per warp with one CTA and with two CTAs on the SM; records and merge
+    // of warps, uneven ends included
+    const float start = 3.f, one = small ? 1.05f : c->d == 64 ? 1.4f : 0.87f;
+    const float two = small ? 1.75f : c->d == 64 ? 1.95f : 1.3f;
+    const float warp_end = small ? 7.f : 10.f;
+    const float sms = static_cast<float>(c->sm_count);
+    const long long warps = static_cast<long long>(c->ctas_per_sm) * c->sm_count * W;
+    const int whole = (nt_max + W - 1) / W;
+    Q4Deal best = {whole, 1e30f};
+    for (int k = 1, turns = whole;; k += (k + 7) / 8) {   // CTAs of the longest segment
+        const int next = (whole + k - 1) / k;
+        if (k > 1 && next == turns)
+            continue;
+        turns = next;
+        const long long run = static_cast<long long>(turns) * W;
+        const bool split = turns < whole;
+        const long long pieces = (nt_max + run - 1) / run;
+        // (uneven segments: their last runs are half full on average)
+        const float ctas = same || !split ? static_cast<float>(S * pieces)
+                                          : static_cast<float>(sum) / run + 0.5f * S;
+        float t = start + merge_of(c, S, pieces).us;
+        const int n = static_cast<int>(std::ceil(ctas / sms));   // CTAs on the busiest SM, two at a time
+        if (same || n <= 2) {
+            t += (n / 2) * turns * two + (n % 2) * turns * one + start * ((n + 1) / 2 - 1);
+        } else {
+            const float all = static_cast<float>(sum) / W + 0.5f * ctas;   // turns of all CTAs
+            t += all * two / (2.f * sms) + 0.5f * turns * two + start * (ctas / (2.f * sms) - 1.f);
+        }
+        if (t < best.us)
+            best = {turns, t};
+        if (turns == 1)
+            break;
+    }
+    const long long per_warp = warp_tiles / warps;
+    const long long pieces = per_warp > 0 ? warp_pieces(nt_max, per_warp) : warps;
+    const float t = start + warp_end + static_cast<float>(warp_tiles) / warps * two +
+                    (pieces > mlkv::kQ4InlineMergePieces ? 1.5f : 0.f);
+    if (per_warp > 0 && pieces <= mlkv::kCombineMaxPiecesHost && t < best.us)
+        best = {0, t};
+    return best;
+}
+
 }  // namespace
 
 extern "C" {
@@ -265,69 +344,74 @@ int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *o
         return rc;
     mlkv::clamp_window(c->max_seq, &window, &sinks);
     static thread_local mlkv::Q4DecodeParams p;
-    static thread_local mlkv::DecodeParams m;   // what the merges see
+    static thread_local int real[MLKV_MAX_BATCH];   // a sequence's segments' tiles
     const int T = mlkv::q4_tile_tokens(c->d), W = mlkv::q4_warps(c->d, c->G);
-    const long long slots = std::min<long long>(static_cast<long long>(c->ctas_per_sm) * c->sm_count,
-                                                mlkv::kCombineMaxPiecesHost);
-    m.b = c->b;
-    m.h = c->h;
-    m.g = c->g;
-    m.G = c->G;
-    m.ml_layers = 0;
-    // Every segment's tiles and `empty` more; the merges see lengths whose plain tiling gives them.
-    long long tiles = 0;
-    int nt_min = 0x7fffffff, nt_max = 0;   // of a segment
-    auto lay_tiles = [&](int empty) {
-        tiles = 0;
-        bool uniform = true;
-        for (int beta = 0; beta < c->b; ++beta) {
-            const int L = seq_lens[beta];
-            uniform = uniform && L == seq_lens[0];
-            const int real = mlkv::visible_tiles(L, window, sinks, T, mlkv::kQ4Block).nt;
-            const int nt = real + empty;
-            nt_min = std::min(nt_min, real);
-            nt_max = std::max(nt_max, real);
-            p.seq_len[beta] = L;
-            m.seq_len[beta] = nt * T;
-            p.tile_start[beta] = m.tile_start[beta] = static_cast<int>(tiles);
-            tiles += static_cast<long long>(c->g) * nt;
-            if (tiles > 0x7fffffffLL)
-                return false;
-        }
-        p.tile_start[c->b] = m.tile_start[c->b] = static_cast<int>(tiles);
-        p.num_tiles = m.num_tiles = static_cast<int>(tiles);
-        p.empty_tiles = empty;
-        p.uniform_len = uniform ? seq_lens[0] : 0;
-        m.uniform_len = uniform ? m.seq_len[0] : 0;
-        return true;
-    };
-    // One wave of resident CTAs.  A run of tiles is a warp's or a CTA's.  A warp's costs records and their
-    // merge, a CTA's that its warps wait for one another at a segment's ends (~3 us, against 2 of one
-    // warp).  So a warp a run where there are many tiles a warp, or segments of uneven lengths, which meet
-    // many ends in some runs (never a segment with more records than one merge takes); measured, us, a
-    // warp / a CTA a run: 64 uneven sequences of up to 8192 positions, 8 KV heads of 128, 56.6 / 84.9; 32
-    // of 4096 (13 tiles a warp) 35.8 / 31.9; 64 of 4096 (27) 57.9 / 59.2; 128 of 4096 (54) 102.5 / 108.4.
-    // Three empty tiles stand for the cost of a segment's ends to a warp (58.8, 57.5, 56.6 us for the
-    // uneven ones with 1, 2, 3).
-    if (!lay_tiles(3))
-        return fail(MLKV_ERR_UNSUPPORTED, "the tiles exceed the int32 tile index");
-    int grid = static_cast<int>(slots);
-    int pieces = mlkv::max_pieces_per_segment(m, T, grid * W);
-    const bool even = nt_max <= nt_min + nt_min / 4 + 1;
-    const bool warp_runs = tiles >= (even ? 24 : 8) * slots * W && pieces <= mlkv::kCombineMaxPiecesHost;
-    if (!warp_runs) {
-        lay_tiles(0);
-        // Few segments: k CTAs for each (of the mean length), the fewest whose warps take no more tiles
-        // in turn than those of the most CTAs there are; else all of those.
-        const long long S = static_cast<long long>(c->b) * c->g;
-        if (S <= slots) {
-            const long long nt = (tiles + S - 1) / S;
-            const long long turns = (nt + W * (slots / S) - 1) / (W * (slots / S));
-            grid = static_cast<int>(S * ((nt + W * turns - 1) / (W * turns)));
-        }
-        pieces = mlkv::max_pieces_per_segment(m, T, grid);
+    const long long S = static_cast<long long>(c->b) * c->g;
+    const long long slots = static_cast<long long>(c->ctas_per_sm) * c->sm_count;   // resident CTAs
+    int nt_min = 0x7fffffff, nt_max = 0;
+    long long sum = 0;
+    bool uniform = true;
+    for (int beta = 0; beta < c->b; ++beta) {
+        const int L = seq_lens[beta];
+        const int nt = window > 0 ? mlkv::visible_tiles(L, window, sinks, T, mlkv::kQ4Block).nt
+                                  : static_cast<int>((static_cast<unsigned>(L) + T - 1) / T);
+        uniform = uniform && L == seq_lens[0];
+        real[beta] = nt;
+        p.seq_len[beta] = L;
+        nt_min = std::min(nt_min, nt);
+        nt_max = std::max(nt_max, nt);
+        sum += nt;
     }
-    p.deferred_merge = pieces > mlkv::kQ4InlineMergePieces ? 1 : 0;
+    p.uniform_len = uniform ? seq_lens[0] : 0;
+    // The tiles are dealt out in equal runs.  A run a warp: tiles end to end, with three empty ones behind a
+    // segment for the cost of its end (64 uneven sequences of up to 8192 positions, 8 KV heads of 128: 58.8,
+    // 57.5, 56.6 us with 1, 2, 3, 56.1 to 57.5 with 4 to 8); every end is a record and its merge.  A run a
+    // CTA: a segment's tiles filled up to whole runs, so that no run crosses a segment, of as many turns of
+    // the warps as the estimate says; a whole segment needs no merge.  (Equal runs that cross segments
+    // cost each CTA ~3 us an end: 16 uneven sequences of up to 1000, 8 KV heads of 128, 25.5 us, 7.9 now, 64
+    // of them 39.2 and 15.6.)  Measured, us, a warp / a CTA: 32 sequences of 4096 35.8 / 30.9, 64 of 1000 21.3 /
+    // 19.2, 20 of 4000 23.8 / 30.5, 64 uneven ones of up to 4000, 4 KV heads of 64, 16.1 / 14.9.
+    const long long warp_tiles = c->g * (sum + static_cast<long long>(kEmpty) * c->b);
+    int turns = deal(c, S, sum * c->g, warp_tiles, nt_max, nt_min == nt_max).turns;
+    const bool warp_runs = turns == 0;
+    int grid = static_cast<int>(slots);
+    long long tiles = warp_tiles;
+    long long pieces = 1;   // of a segment, at most
+    p.empty_tiles = p.round_tiles = 0;
+    if (warp_runs) {
+        p.empty_tiles = kEmpty;
+        pieces = warp_pieces(nt_max, warp_tiles / (slots * W));
+    } else {
+        // (as many runs as there are records for, and one merge takes; whole segments leave none)
+        for (;; turns *= 2) {
+            p.round_tiles = turns * W;
+            tiles = 0;
+            for (int beta = 0; beta < c->b; ++beta)
+                tiles += (real[beta] + p.round_tiles - 1) / p.round_tiles;
+            tiles *= c->g;
+            pieces = (nt_max + p.round_tiles - 1) / p.round_tiles;
+            if (pieces == 1 || (tiles <= slots * W && pieces <= mlkv::kCombineMaxPiecesHost))
+                break;
+        }
+        grid = static_cast<int>(tiles);
+        tiles *= p.round_tiles;
+    }
+    if (tiles > 0x7fffffffLL)
+        return fail(MLKV_ERR_UNSUPPORTED, "%lld tiles exceed the int32 tile index", tiles);
+    auto laid = [&](int beta) {   // tiles of one of beta's segments in the list
+        return warp_runs ? real[beta] + kEmpty
+                         : (real[beta] + p.round_tiles - 1) / p.round_tiles * p.round_tiles;
+    };
+    p.num_tiles = static_cast<int>(tiles);
+    if (!uniform) {
+        int at = 0;
+        for (int beta = 0; beta < c->b; ++beta) {
+            p.tile_start[beta] = at;
+            at += c->g * laid(beta);
+        }
+        p.tile_start[c->b] = at;
+    }
+    p.deferred_merge = warp_runs ? pieces > mlkv::kQ4InlineMergePieces : merge_of(c, S, pieces).deferred;
     p.Q = static_cast<const __nv_bfloat16 *>(Q);
     p.out = static_cast<__nv_bfloat16 *>(out);
     p.slot = slot_base(c, layer);
@@ -349,6 +433,20 @@ int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *o
     if (e != cudaSuccess)
         return fail_cuda(e, "4-bit decode launch");
     if (p.deferred_merge) {
+        // The merge sees lengths whose plain tiling gives the launch's tiles.
+        static thread_local mlkv::DecodeParams m;
+        m.b = c->b;
+        m.h = c->h;
+        m.g = c->g;
+        m.G = c->G;
+        m.ml_layers = 0;
+        m.num_tiles = p.num_tiles;
+        m.uniform_len = uniform ? laid(0) * T : 0;
+        if (!uniform)
+            for (int beta = 0; beta < c->b; ++beta) {
+                m.seq_len[beta] = laid(beta) * T;
+                m.tile_start[beta] = p.tile_start[beta];
+            }
         m.out = p.out;
         m.part_o = p.part_o;
         m.part_lse = p.part_lse;

@@ -158,6 +158,20 @@ def test_decode_window(d, h, g, window, sinks):
 
 
 @pytest.mark.parametrize("d,h,g,lens,window,sinks", [
+    (128, 32, 8, [1 + 61 * i % 997 for i in range(40)], 0, 0),     # more segments than CTAs at a time
+    (64, 12, 4, [1 + 37 * i % 300 for i in range(200)], 0, 0),
+    (64, 12, 1, [20000] + [5] * 63, 0, 0),                         # one long one among short ones
+    (128, 32, 2, [4000 - 9 * i for i in range(64)], 0, 0),         # two records a segment, 16 heads
+    (128, 32, 2, [4000, 1, 2500, 257], 0, 0),                      # many records, 16 heads
+    (64, 12, 1, [8192], 0, 0), (128, 4, 1, [8192, 33], 0, 0),
+    (128, 32, 8, [900 + i for i in range(20)], 700, 5),            # equal windows
+    (64, 12, 1, [385 * (1 + i % 7) for i in range(300)], 0, 0),    # runs just passed by a tile
+])
+def test_decode_deals(d, h, g, lens, window, sinks):
+    _decode(d, h, g, lens, window, sinks)
+
+
+@pytest.mark.parametrize("d,h,g,lens,window,sinks", [
     (64, 12, 1, [70001], 0, 0),                  # hundreds of pieces: the separate merge
     (128, 8, 1, [40000], 0, 0),
     (128, 32, 8, [3000, 1, 2999, 700], 0, 0),    # a few pieces a segment: merged in the launch
