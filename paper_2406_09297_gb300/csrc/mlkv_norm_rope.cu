@@ -11,14 +11,15 @@
 // a head, so that only the sum of squares crosses lanes; gain and rotation are one pair of factors a
 // channel, made once per token:
 //   a' = r (a (g_a cos) - b (g_b sin)),  b' = r (b (g_b cos) + a (g_a sin)),  r = 1 / sqrt(...)
-// A block's warps take heads of one kind (queries, keys or values), whose addresses are then uniform: a
-// token each and 512 / D heads at a time, two such loads in flight, or, where a token has fewer heads of
-// the kind, those of several tokens.
+// A block's warps take heads of one kind (queries, keys or values), whose addresses are then uniform: of one
+// token or several, up to 512 / D heads at a time, two (D = 64: three) such loads in flight.
 //
 // Measured on GB300: 16,004 tokens of 32 + 8 + 8 heads of 128 in 63.3 us, 6.2 TB/s of 6.8 (97.6 with the
-// partner channels fetched from other lanes and factors made a head); 16,016 of 12 + 4 + 4 heads of 64 in
-// 21.0 us, 3.9 TB/s: there a token's factors serve one or two loads, and their latency bounds it.  A
-// batch's single tokens are bound by the caller: 8.2 us of Python and launch.
+// partner channels fetched from other lanes and factors made a head); 32,000 of 12 + 4 + 4 heads of 64 in
+// 29.8 us, 5.6 TB/s.  Heads of 64 are bound by latency (a token's position, then its factors): several tokens
+// a warp, few enough heads of each at a time that they take three loads and divide evenly (39.3 us with
+// whole tokens a warp, the last load half empty), five blocks an SM for their registers (six with two
+// loads 30.4, four 32.7).  A batch's single tokens are bound by the caller: 6.2 us of Python and launch.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -40,7 +41,7 @@ struct NormRopeParams {
     __nv_bfloat16 *out[3];
     long long out_seq[3], out_token[3], out_head[3];   // elements: a sequence, token, head further
     int heads[3];
-    int wide[3];                               // heads of a token that a warp has lanes for (a power of
+    int wide[3];                               // heads of a token that a warp holds at a time (a power of
                                                // two; 512 / D: one token a warp)
     int parts[3];                              // warps that share a token's heads
     unsigned first_block[3];                   // of the kind's blocks, part by part
@@ -52,21 +53,24 @@ struct NormRopeParams {
 };
 
 constexpr int kNormThreads = 128;
-constexpr int kNormLoads = 2;                  // in flight
+// Loads of a lane in flight.
+__host__ __device__ constexpr int norm_loads(int d) { return d == 64 ? 3 : 2; }
 
 // kInter: pairs are neighbouring channels.
 template <int D, bool kInter>
-__global__ void __launch_bounds__(kNormThreads, 6)
+__global__ void __launch_bounds__(kNormThreads, D == 64 ? 5 : 6)
     norm_rope_kernel(const __grid_constant__ NormRopeParams p)
 {
     constexpr int LPH = D / 16;       // lanes per head
     constexpr int HPI = 32 / LPH;     // heads a warp holds at a time
-    constexpr int U = kNormLoads;
+    constexpr int U = norm_loads(D);
     grid_dependency_wait();
     grid_dependents_launch();
     const int kind = blockIdx.x < p.first_block[1] ? 0 : blockIdx.x < p.first_block[2] ? 1 : 2;
     const int lane = threadIdx.x & 31;
     const int sel = lane / LPH, wide = p.wide[kind], parts = p.parts[kind];
+    // heads from a lane's load to its next (of 128 channels, fewer than HPI heads are one load)
+    const int step = D == 64 ? wide : HPI;
     const unsigned block = (blockIdx.x - p.first_block[kind]) / parts;
     const int part = static_cast<int>(blockIdx.x - p.first_block[kind] - block * parts);
     // this lane's token; past the last one there is nothing to do, but the warp's shuffles need it
@@ -81,7 +85,7 @@ __global__ void __launch_bounds__(kNormThreads, 6)
     const bool rotates = c < hp;
     const int pa = kInter ? 16 * c : rotates ? 8 * c : 8 * (2 * hp + 2 * (c - hp));
     const int pb = kInter || !rotates ? pa + 8 : 8 * (c + hp);
-    // its heads: from head0 on, HPI apart, below head1; no lane of the warp has any from `stop` on
+    // its heads: from head0 on, `step` apart, below head1; no lane of the warp has any from `stop` on
     const int first = part * p.per_block, stop = min(p.heads[kind], first + p.per_block);
     const int head0 = first + sel % wide, head1 = live ? stop : 0;
     const int beta = token / p.s;
@@ -92,23 +96,23 @@ __global__ void __launch_bounds__(kNormThreads, 6)
     const int d_ab = pb - pa;
     src += pa;
     dst += pa;
-    const long long out_step = HPI * p.out_head[kind];
+    const long long out_step = step * p.out_head[kind];
     auto read = [&](uint4 (&a)[U], uint4 (&b)[U], int head) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (head + u * HPI < head1) {
-                a[u] = *reinterpret_cast<const uint4 *>(src + u * HPI * D);
-                b[u] = *reinterpret_cast<const uint4 *>(src + u * HPI * D + d_ab);
+            if (head + u * step < head1) {
+                a[u] = *reinterpret_cast<const uint4 *>(src + u * step * D);
+                b[u] = *reinterpret_cast<const uint4 *>(src + u * step * D + d_ab);
             }
-        src += U * HPI * D;
+        src += U * step * D;
     };
     uint4 xa[U], xb[U];
     if (kind == 2) {   // values only move
-        for (int h0 = first, head = head0; h0 < stop; h0 += U * HPI, head += U * HPI) {
+        for (int h0 = first, head = head0; h0 < stop; h0 += U * step, head += U * step) {
             read(xa, xb, head);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (head + u * HPI < head1) {
+                if (head + u * step < head1) {
                     *reinterpret_cast<uint4 *>(dst) = xa[u];
                     *reinterpret_cast<uint4 *>(dst + d_ab) = xb[u];
                 }
@@ -182,7 +186,7 @@ __global__ void __launch_bounds__(kNormThreads, 6)
     for (int h0 = first, head = head0;;) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (h0 + u * HPI >= stop)
+            if (h0 + u * step >= stop)
                 break;
             float a[8], b[8], oa[8], ob[8];
             unpack(xa[u], a);
@@ -212,14 +216,14 @@ __global__ void __launch_bounds__(kNormThreads, 6)
                     ob[i] = y1;
                 }
             }
-            if (head + u * HPI < head1) {
+            if (head + u * step < head1) {
                 *reinterpret_cast<uint4 *>(dst) = pack(oa);
                 *reinterpret_cast<uint4 *>(dst + d_ab) = pack(ob);
             }
             dst += out_step;
         }
-        h0 += U * HPI;
-        head += U * HPI;
+        h0 += U * step;
+        head += U * step;
         if (h0 >= stop)
             break;
         read(xa, xb, head);
@@ -343,11 +347,15 @@ extern "C" int mlkv_qk_norm_rope(const void *Q, const void *K, const void *V, in
     // the factors' reuse.
     const int hpi = 512 / head_dim;
     const long long loads = tokens * ((heads + hpi - 1) / hpi);
-    p.per_block = loads >= 152LL * 64 ? 8 * kNormLoads * hpi : hpi;
+    const bool many = loads >= 152LL * 64;
+    p.per_block = many ? 16 * hpi : hpi;
     long long blocks = 0;
     for (int k = 0; k < 3; ++k) {
         p.wide[k] = 1;
-        while (p.wide[k] < hpi && p.wide[k] < p.heads[k])
+        // many tokens, 64 channels a head: a divisor of the heads that makes three loads of them or more
+        while (p.wide[k] < hpi && p.wide[k] < p.heads[k] &&
+               !(many && head_dim == 64 &&
+                 (p.heads[k] % (2 * p.wide[k]) != 0 || p.heads[k] < 6 * p.wide[k])))
             p.wide[k] *= 2;
         p.parts[k] = (p.heads[k] + p.per_block - 1) / p.per_block;
         p.first_block[k] = static_cast<unsigned>(blocks);

@@ -85,6 +85,26 @@ def test_many_tokens_take_the_wide_form():
     _check(ko, want.transpose(1, 2), mag.transpose(1, 2))
 
 
+@pytest.mark.parametrize("h,g", [(12, 4), (16, 2), (3, 1), (32, 12)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_many_tokens_of_every_grouping(h, g, interleaved):
+    b, s, d = 3, 4001, 64
+    torch.manual_seed(h)
+    fused = torch.randn((b, s, h + 2 * g, d), device="cuda").bfloat16()
+    Q, K, V = fused[:, :, :h], fused[:, :, h:h + g], fused[:, :, h + g:]
+    gq, gk = torch.randn(d, device="cuda").bfloat16(), torch.randn(d, device="cuda").bfloat16()
+    cos, sin = _tables(16)
+    pos = torch.randint(0, N_POS, (b, s), device="cuda", dtype=torch.int32)
+    qo = torch.full((b, s, h, d), 7.0, device="cuda").bfloat16()
+    ko = torch.full((b, g, s, d), 7.0, device="cuda").bfloat16()
+    vo = torch.full((b, g, s, d), 7.0, device="cuda").bfloat16()
+    mlkv.mlkv_qk_norm_rope(Q, K, V, gq, gk, cos, sin, pos, qo, ko, vo, interleaved=interleaved)
+    _check(qo, *_want(Q, gq, cos, sin, pos, 1e-6, interleaved))
+    want, mag = _want(K, gk, cos, sin, pos, 1e-6, interleaved)
+    _check(ko, want.transpose(1, 2), mag.transpose(1, 2))
+    assert torch.equal(vo, V.transpose(1, 2))
+
+
 def test_in_place_and_other_stream():
     b, h, g, d = 9, 12, 4, 64
     torch.manual_seed(5)
