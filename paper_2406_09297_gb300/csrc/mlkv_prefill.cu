@@ -62,7 +62,7 @@
 // Sliding window with sinks (kWin): a unit's key tiles are the sinks' and those from the first one its
 // first query's window reaches on; the rest is never loaded.  Rows mask what lies before their own
 // window in the one or two tiles of its edge.  Measured: 8192 positions, window 1024, 4 sinks, 32 heads of
-// 128 123.5 us (0.54 of the tensor core's rate for what is visible; 112 without the sinks' tile); 32 prompts
+// 128 124.5 us (0.53 of the tensor core's rate for what is visible; 112 without the sinks' tile); 32 prompts
 // of 1 to 777, window 200, 12 heads of 64 33.0.  A unit's middle tiles take 1.22 us, as without a window;
 // its masked ones 0.5 more, its start, its output and the sinks' tile, of which 4 keys count, the rest.
 //
