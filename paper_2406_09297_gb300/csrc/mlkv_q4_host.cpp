@@ -1,8 +1,8 @@
 // Host side of the 4-bit KV cache: argument checks, allocation and the mlkv_q4_* calls of mlkv.h.
 //
 // The cache of an MLKV model's m owner layers (arXiv 2406.09297, Sec. 3) as one allocation of
-// [m][b][g] rows of blocks (mlkv_q4.h).  The decode kernel splits its work as the bf16 decode kernel
-// does and shares its merge of many records (combine_kernel).
+// [m][b][g] rows of blocks (mlkv_q4.h).  The decode kernel's tiles are dealt out here (deal); it shares
+// the bf16 decode kernel's merge of many records (combine_kernel).
 #include <cuda_runtime.h>
 
 #include <algorithm>

@@ -371,6 +371,8 @@ def mlkv_qk_norm_rope(Q, K, V, q_gain, k_gain, cos, sin, positions, Q_out, K_out
         if V_out is not None:
             dense = dense and V_out.is_contiguous() and V_out.numel() == nk
             p_vo = V_out.data_ptr()
+    elif not (V is None and K_out is None and V_out is None):
+        raise MLKVError(MLKV_ERR_INVALID_ARG, "without K there is neither V nor K_out nor V_out")
     if q_gain is not None:
         dense = dense and q_gain.is_contiguous() and q_gain.numel() == d
         p_gq = q_gain.data_ptr()

@@ -139,6 +139,9 @@ def test_qk_norm_rope_binding_rejects_layouts():
     call(positions=torch.zeros(5, dtype=torch.int32))
     call(sin=torch.zeros(8, 15))
     call(q_gain=torch.ones(32).bfloat16())
+    call(K=None)                                                  # K_out is left without its input
+    call(K=None, K_out=None, V=torch.zeros(2, 3, 2, 64).bfloat16())
+    call(K=None, K_out=None, V_out=torch.zeros(2, 2, 3, 64).bfloat16())
     call(Q_out=torch.zeros(2, 4, 3, 64).bfloat16().transpose(1, 2))
     call(K_out=torch.zeros(2, 2, 2, 64).bfloat16())
 
