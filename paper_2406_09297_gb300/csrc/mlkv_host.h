@@ -92,6 +92,16 @@ inline bool overlap(const void *a, size_t na, const void *b, size_t nb)
     return x < y + nb && y < x + na;
 }
 
+// Refuses a cache of `rows` times `row_bytes` bytes that no device holds: 64 bits would wrap, and the
+// allocation would be of what is left.
+inline int check_cache_bytes(long long rows, long long row_bytes)
+{
+    if (rows > (1LL << 62) / row_bytes)
+        return fail(MLKV_ERR_OOM, "a cache of %lld rows of %lld bytes exceeds any device's memory", rows,
+                    row_bytes);
+    return MLKV_OK;
+}
+
 // The checks of a cache's sizes and layer-to-owner map (mlkv_cache_create).
 int validate_map(int l, int h, int d, const int *owner, int g, int b, int max_seq);
 

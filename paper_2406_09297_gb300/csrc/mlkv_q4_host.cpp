@@ -177,8 +177,8 @@ int mlkv_q4_create(mlkv_q4cache_t *out, int n_layers, int n_q_heads, int head_di
 {
     if (out == nullptr)
         return fail(MLKV_ERR_INVALID_ARG, "out is NULL");
-    const int rc = mlkv::validate_map(n_layers, n_q_heads, head_dim, layer_owner, kv_heads_per_owner,
-                                      batch, max_seq);
+    int rc = mlkv::validate_map(n_layers, n_q_heads, head_dim, layer_owner, kv_heads_per_owner, batch,
+                                max_seq);
     if (rc != MLKV_OK)
         return rc;
     if (static_cast<long long>(batch) * kv_heads_per_owner > (1 << 24) || max_seq > (1 << 30))
@@ -203,6 +203,12 @@ int mlkv_q4_create(mlkv_q4cache_t *out, int n_layers, int n_q_heads, int head_di
     }
     for (int n = 0; n < n_layers; ++n)   // an owner comes before its readers
         c->slot[n] = c->owner[n] == n ? c->m++ : c->slot[c->owner[n]];
+    c->row_bytes = mlkv::q4_row_bytes(max_seq, c->d);
+    rc = mlkv::check_cache_bytes(static_cast<long long>(c->b) * c->g * c->m, c->row_bytes);
+    if (rc != MLKV_OK) {
+        delete c;
+        return rc;
+    }
     c->device = mlkv::current_device();
     DeviceGuard guard(c->device);
     cudaError_t e = cudaDeviceGetAttribute(&c->sm_count, cudaDevAttrMultiProcessorCount, c->device);
@@ -216,7 +222,6 @@ int mlkv_q4_create(mlkv_q4cache_t *out, int n_layers, int n_q_heads, int head_di
         return e != cudaSuccess ? fail_cuda(e, "preparing the 4-bit cache's kernels")
                                 : fail(MLKV_ERR_CUDA, "the 4-bit decode kernel cannot be resident");
     }
-    c->row_bytes = mlkv::q4_row_bytes(max_seq, c->d);
     const size_t rows = static_cast<size_t>(c->b) * c->g;
     c->cache_bytes = rows * c->m * c->row_bytes;
     // a record for each segment and each run of a launch
