@@ -278,6 +278,11 @@ int mlkv_cache_create(mlkv_cache_t *out, int n_layers, int n_q_heads, int head_d
         return fail(MLKV_ERR_UNSUPPORTED, "m*2*b*g = %lld rows exceed the TMA coordinate range",
                     rows);
     }
+    rc = mlkv::check_cache_bytes(rows, static_cast<long long>(max_seq) * c->d * 2);
+    if (rc != MLKV_OK) {
+        delete c;
+        return rc;
+    }
 
     c->device = current_device();
     DeviceGuard guard(c->device);

@@ -16,3 +16,15 @@ def test_q4_create_refuses_bytes_past_64_bits(g, d, max_seq, owners):
     with pytest.raises(mlkv.MLKVError) as e:
         mlkv.mlkv_q4_create(owners, g, d, list(range(owners)), g, 1024, max_seq)
     assert e.value.code == mlkv.MLKV_ERR_OOM
+
+
+@pytest.mark.parametrize("g,d,max_seq,owners", [
+    (16384, 128, 1 << 30, 32),          # 0 modulo 2^64
+    (16384, 64, (1 << 31) - 1, 63),
+    (8, 128, (1 << 31) - 1, 1100),
+])
+def test_cache_create_refuses_bytes_past_64_bits(g, d, max_seq, owners):
+    assert 2 * 1024 * g * owners * max_seq * d * 2 >= 1 << 63
+    with pytest.raises(mlkv.MLKVError) as e:
+        mlkv.mlkv_cache_create(owners, g, d, list(range(owners)), g, 1024, max_seq)
+    assert e.value.code == mlkv.MLKV_ERR_OOM
