@@ -338,6 +338,18 @@ def _token_stride(x, name, batch, s, heads, d):
     return s1 if s > 1 else s0
 
 
+_types = None
+
+
+def _norm_rope_types():
+    """The types of heads, gains and outputs, of the tables, of the positions."""
+    global _types
+    if _types is None:
+        import torch
+        _types = (torch.bfloat16, torch.float32, torch.int32)
+    return _types
+
+
 _NORM_ROPE_ARGS = struct.Struct("@3P3q9P8if").pack   # mlkv_qk_norm_rope_args
 
 
@@ -354,43 +366,45 @@ def mlkv_qk_norm_rope(Q, K, V, q_gain, k_gain, cos, sin, positions, Q_out, K_out
     g = n_pos = half = k_stride = v_stride = 0
     p_k = p_v = p_cos = p_sin = p_pos = p_gq = p_gk = p_ko = p_vo = 0
     nq = tokens * h * d
-    dense = Q_out.is_contiguous() and Q_out.numel() == nq
+    bf16, fp32, int32 = _types or _norm_rope_types()
+    good = (Q.dtype is bf16 and Q_out.dtype is bf16 and Q_out.is_contiguous() and
+            Q_out.numel() == nq)
     if K is not None:
         kb, ks, g, kd = K.shape
         nk = tokens * g * d
         k_stride = _token_stride(K, "K", b, s, g, d)
-        dense = dense and kb == b and ks == s and kd == d
+        good = good and K.dtype is bf16 and kb == b and ks == s and kd == d
         p_k = K.data_ptr()
         if K_out is not None:
-            dense = dense and K_out.is_contiguous() and K_out.numel() == nk
+            good = good and K_out.dtype is bf16 and K_out.is_contiguous() and K_out.numel() == nk
             p_ko = K_out.data_ptr()
         if V is not None:
-            dense = dense and V.shape == K.shape
+            good = good and V.dtype is bf16 and V.shape == K.shape
             v_stride = _token_stride(V, "V", b, s, g, d)
             p_v = V.data_ptr()
         if V_out is not None:
-            dense = dense and V_out.is_contiguous() and V_out.numel() == nk
+            good = good and V_out.dtype is bf16 and V_out.is_contiguous() and V_out.numel() == nk
             p_vo = V_out.data_ptr()
     elif not (V is None and K_out is None and V_out is None):
         raise MLKVError(MLKV_ERR_INVALID_ARG, "without K there is neither V nor K_out nor V_out")
     if q_gain is not None:
-        dense = dense and q_gain.is_contiguous() and q_gain.numel() == d
+        good = good and q_gain.dtype is bf16 and q_gain.is_contiguous() and q_gain.numel() == d
         p_gq = q_gain.data_ptr()
     if k_gain is not None:
-        dense = dense and k_gain.is_contiguous() and k_gain.numel() == d
+        good = good and k_gain.dtype is bf16 and k_gain.is_contiguous() and k_gain.numel() == d
         p_gk = k_gain.data_ptr()
     if cos is not None:
         n_pos, half = cos.shape
-        if sin is None or positions is None or not (
-                cos.element_size() == sin.element_size() == positions.element_size() == 4):
-            raise MLKVError(MLKV_ERR_INVALID_ARG, "cos, sin (fp32) and positions (int32) belong together")
-        dense = (dense and cos.is_contiguous() and sin.is_contiguous() and
-                 sin.numel() == n_pos * half and positions.is_contiguous() and
-                 positions.numel() == tokens)
+        if sin is None or positions is None:
+            raise MLKVError(MLKV_ERR_INVALID_ARG, "cos, sin and positions belong together")
+        good = (good and cos.dtype is fp32 and sin.dtype is fp32 and positions.dtype is int32 and
+                cos.is_contiguous() and sin.is_contiguous() and sin.numel() == n_pos * half and
+                positions.is_contiguous() and positions.numel() == tokens)
         p_cos, p_sin, p_pos = cos.data_ptr(), sin.data_ptr(), positions.data_ptr()
-    if not dense:
-        raise MLKVError(MLKV_ERR_INVALID_ARG, "outputs, gains, tables and positions must be dense, and "
-                        "every tensor of the sizes that Q, K and cos give")
+    if not good:
+        raise MLKVError(MLKV_ERR_INVALID_ARG, "cos and sin must be fp32, positions int32 and every other "
+                        "tensor bf16; outputs, gains, tables and positions dense; and every tensor of the "
+                        "sizes that Q, K and cos give")
     return _check(lib.mlkv_qk_norm_rope_struct(_NORM_ROPE_ARGS(
         Q.data_ptr(), p_k, p_v, _token_stride(Q, "Q", b, s, h, d), k_stride, v_stride, p_gq, p_gk,
         p_cos, p_sin, p_pos, Q_out.data_ptr(), p_ko, p_vo, _stream(stream) or 0, n_pos, 2 * half,
