@@ -279,7 +279,7 @@ int mlkv_prefill_window(mlkv_cache_t c, int layer, const void *Q, const void *K,
  *   Q_out      device bf16 [batch][s][n_q_heads][head_dim]
  *   K_out, V_out   device bf16 [batch][kv_heads][s][head_dim] (one token: [batch][kv_heads][head_dim])
  * Every tensor 16-byte aligned (positions 4).  An output may be its own input where every head keeps its
- * place (dense tokens; for K and V, s = 1), and otherwise overlaps no input and no other output.
+ * place (dense tokens, or one; for K and V, s = 1), and otherwise overlaps no input and no other output.
  * Arithmetic: fp32, each output rounded once.  Runs on the calling thread's current device.
  * Errors: MLKV_ERR_INVALID_ARG, MLKV_ERR_UNSUPPORTED (head_dim not 64 or 128, rot_dim not a multiple of
  * 16), MLKV_ERR_CUDA.

@@ -308,9 +308,10 @@ extern "C" int mlkv_qk_norm_rope(const void *Q, const void *K, const void *V, in
     const Span outs[3] = {{Q_out, static_cast<size_t>(tokens) * n_q_heads * dd},
                           {K_out, K_out != nullptr ? static_cast<size_t>(tokens) * kv_heads * dd : 0},
                           {V_out, V_out != nullptr ? static_cast<size_t>(tokens) * kv_heads * dd : 0}};
-    const bool same[3] = {Q_out == Q && q_stride == static_cast<int64_t>(n_q_heads) * head_dim,
-                          K_out == K && s == 1 && k_stride == static_cast<int64_t>(kv_heads) * head_dim,
-                          V_out == V && s == 1 && v_stride == static_cast<int64_t>(kv_heads) * head_dim};
+    auto dense = [&](int64_t st, int n) { return tokens == 1 || st == static_cast<int64_t>(n) * head_dim; };
+    const bool same[3] = {Q_out == Q && dense(q_stride, n_q_heads),
+                          K_out == K && s == 1 && dense(k_stride, kv_heads),
+                          V_out == V && s == 1 && dense(v_stride, kv_heads)};
     for (int o = 0; o < 3; ++o) {
         for (int i = 0; i < 3; ++i) {
             if (overlap(outs[o].p, outs[o].n, ins[i].p, ins[i].n) && !(o == i && same[o]))

@@ -62,3 +62,18 @@ def test_norm_rope_binding_refuses_other_types(monkeypatch, name, dtype):
     with pytest.raises(mlkv.MLKVError) as e:
         mlkv.mlkv_qk_norm_rope(**args, stream=0)
     assert e.value.code == mlkv.MLKV_ERR_INVALID_ARG and len(calls) == 1
+
+
+def test_norm_rope_takes_one_token_in_place():
+    """One token's heads keep their places whatever the stride to the next.  (Without a GPU the launch is
+    what fails.)"""
+    torch = pytest.importorskip("torch")
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are the host's")
+    h, g, d = 4, 2, 64
+    rows = torch.zeros((1, 1, h + 2 * g, d), dtype=torch.bfloat16)
+    Q, K, V = rows[:, :, :h], rows[:, :, h:h + g], rows[:, :, h + g:]
+    with pytest.raises(mlkv.MLKVError) as e:
+        mlkv.mlkv_qk_norm_rope(Q, K, V, None, None, None, None, None, Q, K.view(1, g, 1, d),
+                               V.view(1, g, 1, d), stream=0)
+    assert e.value.code == mlkv.MLKV_ERR_CUDA
