@@ -320,16 +320,17 @@ int mlkv_qk_norm_rope_struct(const mlkv_qk_norm_rope_args *args);
  *   mlkv_q4_bytes             bytes of the cache, 2.25 * b * g * m * head_dim / 2 a position, positions
  *                             rounded up to a multiple of 64
  *   mlkv_q4_append            as mlkv_append
- *   mlkv_q4_load_prefix       as mlkv_load_prefix (K and V in the device's memory, 16-byte aligned);
- *                             positions from len on keep what they hold
+ *   mlkv_q4_load_prefix       as mlkv_load_prefix, positions from len on keep what they hold; K and V
+ *                             16-byte aligned in the memory of the cache's device (managed memory will do),
+ *                             MLKV_ERR_INVALID_ARG elsewhere
  *   mlkv_q4_read              positions [start, start + len) of the layer's owner as bf16 K and V
  *                             [batch][g][len][d]: each value rounded to nearest even
  *   mlkv_q4_decode_attention  as mlkv_decode_attention over what the cache holds, with the window and
  *                             sinks of mlkv_decode_attention_window (window 0 = every position)
  *   mlkv_q4_prefill           as mlkv_prefill_window, over the prompt's own K and V (bf16, so that a
  *                             prompt's outputs do not depend on the cache's precision): every layer is
- *                             given its owner's K and V, and an owner layer stores them; out overlaps
- *                             none of Q, K and V
+ *                             given its owner's K and V (where mlkv_q4_load_prefix takes them), and an
+ *                             owner layer stores them; out overlaps none of Q, K and V
  *   mlkv_q4_sync_status       as mlkv_sync_status
  */
 typedef struct mlkv_q4cache *mlkv_q4cache_t;

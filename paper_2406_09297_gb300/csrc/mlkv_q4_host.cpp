@@ -66,6 +66,24 @@ int check_lens(const mlkv_q4cache *c, const int *seq_lens)
     return MLKV_OK;
 }
 
+// A prompt's keys and values, which kernels read where they lie: in memory of the cache's device.  (Another
+// GPU's may not be mapped here, the host's may not be readable by kernels.)
+int check_prompt_kv(const mlkv_q4cache *c, const void *K, const void *V)
+{
+    for (const void *x : {K, V}) {
+        if (x == nullptr || !aligned16(x))
+            return fail(MLKV_ERR_INVALID_ARG, "K and V must be non-NULL and 16-byte aligned");
+        cudaPointerAttributes at;
+        const cudaError_t e = cudaPointerGetAttributes(&at, x);
+        if (e != cudaSuccess)
+            cudaGetLastError();
+        if (e != cudaSuccess || !((at.type == cudaMemoryTypeDevice && at.device == c->device) ||
+                                  at.type == cudaMemoryTypeManaged))
+            return fail(MLKV_ERR_INVALID_ARG, "K and V must lie in the memory of the cache's device");
+    }
+    return MLKV_OK;
+}
+
 uint8_t *slot_base(const mlkv_q4cache *c, int layer)
 {
     return c->cache + c->cache_bytes / c->m * c->slot[layer];
@@ -290,7 +308,7 @@ int mlkv_q4_append(mlkv_q4cache_t c, int layer, const void *K, const void *V, co
 int mlkv_q4_load_prefix(mlkv_q4cache_t c, int layer, const void *K, const void *V, int len,
                         void *cuda_stream)
 {
-    const int rc = check_layer(c, layer);
+    int rc = check_layer(c, layer);
     if (rc != MLKV_OK)
         return rc;
     if (c->owner[layer] != layer)
@@ -299,9 +317,9 @@ int mlkv_q4_load_prefix(mlkv_q4cache_t c, int layer, const void *K, const void *
         return fail(MLKV_ERR_RANGE, "prefix length %d outside [0, %d]", len, c->max_seq);
     if (len == 0)
         return MLKV_OK;
-    if (K == nullptr || V == nullptr || !aligned16(K) || !aligned16(V))
-        return fail(MLKV_ERR_INVALID_ARG, "K and V must be non-NULL and 16-byte aligned");
     DeviceGuard guard(c->device);
+    if ((rc = check_prompt_kv(c, K, V)) != MLKV_OK)
+        return rc;
     return store(c, layer, K, V, len, nullptr, static_cast<cudaStream_t>(cuda_stream));
 }
 
@@ -477,14 +495,14 @@ int mlkv_q4_prefill(mlkv_q4cache_t c, int layer, const void *Q, const void *K, c
             MLKV_OK ||
         (rc = mlkv::check_window(window, sinks)) != MLKV_OK)
         return rc;
-    if (K == nullptr || V == nullptr || !aligned16(K) || !aligned16(V))
-        return fail(MLKV_ERR_INVALID_ARG, "K and V must be non-NULL and 16-byte aligned");
+    DeviceGuard guard(c->device);
+    if ((rc = check_prompt_kv(c, K, V)) != MLKV_OK)
+        return rc;
     const size_t qbytes = static_cast<size_t>(c->b) * s_max * c->h * c->d * 2;
     const size_t kvbytes = static_cast<size_t>(c->b) * c->g * s_max * c->d * 2;
     if (overlap(K, kvbytes, out, qbytes) || overlap(V, kvbytes, out, qbytes))
         return fail(MLKV_ERR_INVALID_ARG, "out overlaps K or V");
     mlkv::clamp_window(s_max, &window, &sinks);
-    DeviceGuard guard(c->device);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     mlkv::PrefillCall a = {};
     a.Q = Q;

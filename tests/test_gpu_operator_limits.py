@@ -20,3 +20,28 @@ def test_norm_rope_of_one_fused_row_in_place(h, g, d):
     assert torch.equal(V, want[:, :, h + g:])
     # half a unit of bf16, fp32 before it
     assert float(((rows[:, :, :h + g].double() - heads).abs() / heads.abs()).max()) <= 2.0 ** -8 * 1.01
+
+
+def test_q4_prompts_outside_the_device_are_refused():
+    """The kernels read a prompt's keys and values where they lie: the host's memory may not be readable to
+    them (mlkv_prefill copies such prompts, a 4-bit cache has no bf16 place to copy them to)."""
+    b, g, h, s, d = 2, 2, 4, 70, 64
+    cache = mlkv.MLKVQ4Cache(2, h, d, [0, 0], g, b, s)
+    K = torch.randn((b, g, s, d), device="cuda").bfloat16()
+    Q = torch.randn((b, s, h, d), device="cuda").bfloat16()
+    out = torch.zeros_like(Q)
+    for far in (K.cpu(), K.cpu().pin_memory()):
+        for k, v in ((far, K), (K, far)):
+            for layer in (0, 1):   # an owner and a reader
+                with pytest.raises(mlkv.MLKVError) as e:
+                    cache.prefill(layer, Q, k, v, out, [s, 5])
+                assert e.value.code == mlkv.MLKV_ERR_INVALID_ARG
+            with pytest.raises(mlkv.MLKVError) as e:
+                cache.load_prefix(0, k, v, s)
+            assert e.value.code == mlkv.MLKV_ERR_INVALID_ARG
+    cache.sync_status()
+    assert not out.any()
+    cache.prefill(0, Q, K, K, out, [s, 5])
+    cache.load_prefix(0, K, K, s)
+    cache.sync_status()
+    assert out[0].any(-1).all()
