@@ -326,7 +326,10 @@ int mlkv_qk_norm_rope_struct(const mlkv_qk_norm_rope_args *args);
  *   mlkv_q4_read              positions [start, start + len) of the layer's owner as bf16 K and V
  *                             [batch][g][len][d]: each value rounded to nearest even
  *   mlkv_q4_decode_attention  as mlkv_decode_attention over what the cache holds, with the window and
- *                             sinks of mlkv_decode_attention_window (window 0 = every position)
+ *                             sinks of mlkv_decode_attention_window (window 0 = every position).  A softmax
+ *                             weight times a scale is rounded once, to 11 bits (below 2^-16 of the largest of
+ *                             its head and its 32 channels to fewer, to nothing below 2^-27 of that); queries
+ *                             below 2^-29 of their head's largest lose bits; everything else is fp32
  *   mlkv_q4_prefill           as mlkv_prefill_window, over the prompt's own K and V (bf16, so that a
  *                             prompt's outputs do not depend on the cache's precision): every layer is
  *                             given its owner's K and V (where mlkv_q4_load_prefix takes them), and an

@@ -9,16 +9,20 @@
 //   S = K Q^T, 16 positions by 8 heads a group of 32 channels: exact codes, queries as fp16 scaled by a
 //       power of two per head to at most 2^15 (bf16's 8 bits fit; below 2^-29 of the head's largest
 //       magnitude bits are lost); fp32 sums, times the group's scale in fp32.
-//   O = V^T P^T, 16 channels by 8 heads.  The group's scale goes into P: P' = fp16(fp16(p) s / f), f a
-//       power of two that bounds the scales the warp has met (raised with a rescaled O, like the
-//       running maximum), so that fp16's range holds whatever the values' magnitude.
+//   O = V^T P^T, 16 channels by 8 heads.  The group's scale goes into P: P' = fp16(p s u), p s in fp32, u a
+//       power of two of the head and group that follows the largest product p s the warp has met (with a
+//       rescaled O, like the running maximum, and rarely: a bound on the scales tells when it may have to).  A
+//       scale thus counts with its weight, and a group by itself: each product is off by 2^-11 of itself, and
+//       below 2^-16 of the largest by up to 2^-27 of that.  (With fp16(p) times fp16(s / f), one f for all
+//       groups and positions, 6 to 10% faster, a large value of no weight or a sink of small value drove the
+//       others below fp16's range: errors of percents to 100%.)
 // Measured on GB300, one layer, 8 KV heads of 128 with 4 query heads each, us (TB/s of 6.8): 128 sequences
-// of 4096 positions 102.4 (5.9), 64 57.6 (5.2), 32 30.9 (4.9), 64 uneven ones of up to 8192 56.6 (4.9).
-// The stream itself runs at HBM's rate (44.5 us more for 44.4 us more of bytes); what is left is ~3 us of
-// start and, at the end, warps that finish up to 12 us apart and then merge for 3 to 5 us.  One sequence of
-// 131072, 12 heads of 64 over one KV head: 10.7, two launches' latencies.
-// (Tried before.  Codes as bf16 128 + c, the surplus cancelled in the accumulators, P in bf16: as fast,
-// outputs 0.0024 to 0.0029 from the 64-bit ones instead of 0.0017.  K in e4m3: mma.sync takes 8-bit
+// of 4096 positions 109.5 (5.5), 64 61.4 (4.9), 32 33.1 (4.6), 64 uneven ones of up to 8192 60.0 (4.7).
+// Twice the sequences cost 48.1 us more for 44.4 us more of bytes; beside that there are ~3 us of start and, at
+// the end, warps that finish up to 12 us apart and then merge for 3 to 5 us.  One sequence of 131072, 12 heads
+// of 64 over one KV head: 11.7, two launches' latencies.
+// (Tried before.  Codes as bf16 128 + c, the surplus cancelled in the accumulators, P in bf16: outputs 0.0024 to
+// 0.0029 from the 64-bit ones instead of 0.0017.  K in e4m3: mma.sync takes 8-bit
 // operands apart again, 385 instructions per 16 positions of 128 channels and 8 heads.)
 //
 // Work split.  The tiles of all (sequence, KV head) segments end to end, an equal run of them for each
@@ -62,8 +66,7 @@ struct Q4Plan {
     static constexpr int kQ = kRing + kWarps * kStages * kTileBytes;
     static constexpr int kQSet = 8 * NB * kQRow;
     static constexpr int kMul = kQ + kQSets * kQSet;
-    static constexpr int kVs = kMul + kQSets * 8 * NB * 4;      // [kWarps][64] V scales, fp16 pairs
-    static constexpr int kBars = kVs + kWarps * 256;
+    static constexpr int kBars = kMul + kQSets * 8 * NB * 4;
     static constexpr int kFlags = kBars + kWarps * kStages * 8;
     // Shared runs: a piece's sums of 8 heads from every warp, rows padded so that the fragments' 16-byte
     // stores fall in distinct banks, and m, l [8 NB heads][kWarps].
@@ -71,10 +74,8 @@ struct Q4Plan {
     static constexpr int kRaw = kFlags + 16;
     static constexpr int kStat = kRaw + (kWarpRuns ? 0 : kWarps * 8 * kRow * 4);
     static constexpr int kBytes = kStat + (kWarpRuns ? 0 : 2 * 8 * NB * kWarps * 4);
-    static_assert(kSub * 8 * LY::kGroups == 64, "two words of V scales a lane");
     static_assert(kMinBlocks * (kBytes + 1024) <= 228 * 1024, "shared memory of the resident CTAs");
-    static_assert(kTileBytes % 128 == 0 && kQ % 16 == 0 && kVs % 16 == 0 && kBars % 8 == 0 &&
-                      kRaw % 16 == 0, "");
+    static_assert(kTileBytes % 128 == 0 && kQ % 16 == 0 && kBars % 8 == 0 && kRaw % 16 == 0, "");
     __device__ static constexpr int q_at(int head, int group, int tig)
     {
         return kQ + head * kQRow + (((group * 4 + tig) ^ ((head & 1) * 4)) * 16);
@@ -170,16 +171,23 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
-__device__ __forceinline__ uint32_t hmul2_f16(uint32_t a, uint32_t b)
+// 1 / x, x a power of two in [2^-126, 2^126].
+__device__ __forceinline__ float reciprocal2(float x)
 {
-    const __half2 x = *reinterpret_cast<const __half2 *>(&a);
-    const __half2 y = *reinterpret_cast<const __half2 *>(&b);
-    const __half2 z = __hmul2(x, y);
-    return *reinterpret_cast<const uint32_t *>(&z);
+    return __uint_as_float((254u << 23) - __float_as_uint(x));
 }
 
-// Reference maxima move when a score exceeds them by more than this (log2 units): weights stay <= 2^8.
-constexpr float kQ4LazyMax = 8.f;
+// A head's reference lies this much (log2 units) above its largest score when it is set, and moves when a
+// score exceeds it: weights are at most 1.
+constexpr float kQ4LazyMax = 4.f;
+// A power of two of a head and group brings their largest product of weight and scale to
+// [2^kQ4ProductTop, 2^(kQ4ProductTop + 1)) when it is set, and moves when one reaches 2^15.  As weights are
+// at most 1, scales below 2^15 over the largest power of two need no look at the products.  (128 sequences of
+// 4096 that begin with a sink of 12 nats and values 0.02 of the others', us: 2^7 and 3 log2 units 148, 2^3 and
+// 5 125, these 110, as without the sink.)
+constexpr uint32_t kQ4ProductTop = 2;
+constexpr float kQ4ProductMost = 32768.f;
+constexpr uint32_t kQ4UpNone = 0x7e807e80u;   // bf16 pair of 2^126: nothing met yet, and the largest power
 
 template <int D, int NB, bool kWarpRuns>
 __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
@@ -368,25 +376,29 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
             asm volatile("prefetch.global.L2 [%0];" ::"l"(
                 p.Q + (static_cast<size_t>(ns.beta) * p.h + static_cast<size_t>(ns.j) * p.G) * D + lane * 64));
         // A thread's statistics are those of heads 2 tig and 2 tig + 1 (la: over its own positions);
-        // O is in units of 2^-16 times the scales' bound.
+        // O is in units of 2^-16 / up, up a power of two a head and group.
         float o[NB][2 * NG][4];
-        // A head's reference maximum is -nm, in log2 units; it moves when a product exceeds `top`
-        // (products times mul are log2 units).  Without one yet top is -inf and nm 0.
-        float la[NB][2], nm[NB][2], top[NB][2], mul[NB][2];
-        float bound = 0x1p-100f, inv_bound = 0x1p100f;
+        uint32_t up[NB][NG];   // bf16, of both heads
+        // A head's reference is -nm, in log2 units (products times mul are); it moves when a score exceeds
+        // it.  Without one yet every score does.
+        float la[NB][2], nm[NB][2], mul[NB][2];
+        // The scale (bf16, twice) up to which no product of group lane % NG passes its range.
+        uint32_t v_most = 0u;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
             for (int n = 0; n < 2 * NG; ++n)
                 o[nb][n][0] = o[nb][n][1] = o[nb][n][2] = o[nb][n][3] = 0.f;
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+                up[nb][g] = kQ4UpNone;
             la[nb][0] = la[nb][1] = 0.f;
-            nm[nb][0] = nm[nb][1] = 0.f;
-            top[nb][0] = top[nb][1] = NEG_INF;
+            nm[nb][0] = nm[nb][1] = 3e38f;
             const float2 f = *reinterpret_cast<const float2 *>(q_mul + 8 * nb + 2 * tig);
             mul[nb][0] = f.x;
             mul[nb][1] = f.y;
         }
-        uint32_t *vscale = reinterpret_cast<uint32_t *>(smem + PL::kVs) + warp * 64;
+        const uint32_t half_sel = (gid & 1) ? 0x3244u : 0x1044u;   // a position of a pair, as fp32
         for (const int stop = kWarpRuns ? piece_end : tile_end; tile < stop; tile += kStep, ++it) {
             const int s = it % R;
             if (kWarpRuns && tile - cs.first >= cs.v.nt) {
@@ -404,45 +416,31 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
             const int vis1 = end - pos0;
             const bool edge = vis0 > 0 || vis1 < T;
             {
-                // ---- the scales of V as fp16, over their bound: two pairs a lane ----
-                float2 vf[2];
-                float peak = 0.f;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int k = lane + 32 * i, blk = k / (8 * NG), at = k % (8 * NG);
-                    const uint32_t w = *reinterpret_cast<const uint32_t *>(st + blk * LY::kBytes +
-                                                                           LY::kVs + at * 4);
-                    vf[i] = make_float2(bf16_lo(w), bf16_hi(w));
-                    if (edge) {
-                        // positions outside [vis0, vis1) hold anything, NaN scales among it
-                        const int r = 16 * blk + 8 * (at / NG & 1) + 2 * (at / (2 * NG));
-                        if (r < vis0 || r >= vis1)
-                            vf[i].x = 0.f;
-                        if (r + 1 < vis0 || r + 1 >= vis1)
-                            vf[i].y = 0.f;
+                // The words of V's scales are pairs of positions; two words a lane (of one group), and as a
+                // position's the scales at gid (hi: gid + 8) of block b.
+                auto v_word = [&](int i) {
+                    const int k = lane + 32 * i;
+                    return st + k / (8 * NG) * LY::kBytes + LY::kVs + k % (8 * NG) * 4;
+                };
+                auto v_scales = [&](int b, int hi, float (&f)[NG]) {
+                    const uint8_t *at =
+                        st + b * LY::kBytes + LY::kVs + ((gid >> 1) * 2 + hi) * NG * 4;
+                    uint32_t w[NG];
+                    if constexpr (NG == 4) {
+                        const uint4 x = *reinterpret_cast<const uint4 *>(at);
+                        w[0] = x.x;
+                        w[1] = x.y;
+                        w[2] = x.z;
+                        w[3] = x.w;
+                    } else {
+                        const uint2 x = *reinterpret_cast<const uint2 *>(at);
+                        w[0] = x.x;
+                        w[1] = x.y;
                     }
-                    peak = fmaxf(peak, fmaxf(vf[i].x, vf[i].y));
-                }
-                if (__any_sync(0xffffffffu, peak > bound)) {
 #pragma unroll
-                    for (int m = 1; m < 32; m <<= 1)
-                        peak = fmaxf(peak, __shfl_xor_sync(0xffffffffu, peak, m));
-                    // the power of two above it (scales are below 2^126)
-                    const uint32_t eb = (__float_as_uint(peak) >> 23) + 1;
-                    const float down = bound * __uint_as_float((254u - eb) << 23);
-                    bound = __uint_as_float(eb << 23);
-                    inv_bound = __uint_as_float((254u - eb) << 23);
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                        for (int n = 0; n < 2 * NG; ++n)
-#pragma unroll
-                            for (int c = 0; c < 4; ++c)
-                                o[nb][n][c] *= down;
-                }
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    vscale[lane + 32 * i] = pack_f16x2(vf[i].x * inv_bound, vf[i].y * inv_bound);
+                    for (int g = 0; g < NG; ++g)
+                        f[g] = __uint_as_float(__byte_perm(w[g], 0u, half_sel));
+                };
                 // ---- S = K Q^T, 16 positions by 8 heads a block ----
                 float sc[NS][NB][4];
                 uint32_t kw[NS][2 * NG];       // [hi][group]
@@ -509,61 +507,165 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
                                     sc[b][nb][c] = NEG_INF;
                             }
                         }
+                    // Positions outside [vis0, vis1) hold anything, NaN scales among it: V's become zeros, in
+                    // place (the stage's next copy comes after the fence).
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int k = lane + 32 * i, at = k % (8 * NG);
+                        const int r = 16 * (k / (8 * NG)) + 8 * (at / NG & 1) + 2 * (at / (2 * NG));
+                        uint16_t *pair =
+                            reinterpret_cast<uint16_t *>(const_cast<uint8_t *>(v_word(i)));
+                        if (r < vis0 || r >= vis1)
+                            pair[0] = 0;
+                        if (r + 1 < vis0 || r + 1 >= vis1)
+                            pair[1] = 0;
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
                 }
-                // ---- online softmax (base 2), the reference maximum raised rarely ----
-                uint32_t pb[NS][NB][2];
+                // ---- online softmax (base 2), references and powers of two moved rarely ----
+                float mx[NB][2];
+                bool raise = false;
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    float mx[2] = {NEG_INF, NEG_INF};
+                    mx[nb][0] = mx[nb][1] = NEG_INF;
 #pragma unroll
                     for (int b = 0; b < NS; ++b) {
-                        mx[0] = fmaxf(mx[0], fmaxf(sc[b][nb][0], sc[b][nb][2]));
-                        mx[1] = fmaxf(mx[1], fmaxf(sc[b][nb][1], sc[b][nb][3]));
+                        mx[nb][0] = fmaxf(mx[nb][0], fmaxf(sc[b][nb][0], sc[b][nb][2]));
+                        mx[nb][1] = fmaxf(mx[nb][1], fmaxf(sc[b][nb][1], sc[b][nb][3]));
                     }
-                    const bool raise = mx[0] > top[nb][0] || mx[1] > top[nb][1];
-                    if (__any_sync(0xffffffffu, raise)) {
-                        float alpha[2];
+                    raise |= fmaf(mx[nb][0], mul[nb][0], nm[nb][0]) > 0.f ||
+                             fmaf(mx[nb][1], mul[nb][1], nm[nb][1]) > 0.f;
+                }
+                // whether a product of weight and scale may pass its range (bf16 numbers >= 0 are ordered like
+                // their bits, NaN last)
+                const bool may_pass =
+                    __vimax3_u16x2(*reinterpret_cast<const uint32_t *>(v_word(0)),
+                                   *reinterpret_cast<const uint32_t *>(v_word(1)), v_most) != v_most;
+                if (__any_sync(0xffffffffu, raise || may_pass)) {
+                    float alpha[NB][2], lift[NB][2];   // of the sums so far; of the powers of two
+                    uint32_t x[NB][NG];   // the largest products, two heads' leading 16 bits
+                    bool move = raise;
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 4));
-                            mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 8));
-                            mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 16));
-                            const float m_old = top[nb][i] == NEG_INF ? NEG_INF : -nm[nb][i];
-                            const float m_new = fmaxf(m_old, mx[i] * mul[nb][i]);
-                            alpha[i] = 1.f;
-                            if (m_new != NEG_INF) {
-                                alpha[i] = fast_exp2(m_old - m_new);
-                                nm[nb][i] = -m_new;
-                                top[nb][i] = (m_new + kQ4LazyMax) * fast_rcp(mul[nb][i]);
+                            float y = mx[nb][i];
+                            y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 4));
+                            y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 8));
+                            y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 16));
+                            alpha[nb][i] = lift[nb][i] = 1.f;
+                            if (fmaf(y, mul[nb][i], nm[nb][i]) > 0.f) {
+                                const float nm_new = fmaf(-y, mul[nb][i], -kQ4LazyMax);
+                                const float by = nm_new - nm[nb][i];
+                                alpha[nb][i] = fast_exp2(by);   // 0 where there was none
+                                // what has been summed keeps its size: floor(-by), 2^120 at most
+                                lift[nb][i] =
+                                    __int_as_float((127 + static_cast<int>(fminf(-by, 120.f))) << 23);
+                                nm[nb][i] = nm_new;
                             }
-                            la[nb][i] *= alpha[i];
+                            la[nb][i] *= alpha[nb][i];
                         }
+                        float y[NG][2];   // the largest products (NaN ones move nothing)
 #pragma unroll
-                        for (int n = 0; n < 2 * NG; ++n) {
-                            o[nb][n][0] *= alpha[0];
-                            o[nb][n][1] *= alpha[1];
-                            o[nb][n][2] *= alpha[0];
-                            o[nb][n][3] *= alpha[1];
+                        for (int g = 0; g < NG; ++g)
+                            y[g][0] = y[g][1] = 0.f;
+#pragma unroll
+                        for (int b = 0; b < NS; ++b)
+#pragma unroll
+                            for (int hi = 0; hi < 2; ++hi) {
+                                float f[NG];
+                                v_scales(b, hi, f);
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    const float w = fast_exp2(
+                                        fmaf(sc[b][nb][2 * hi + i], mul[nb][i], nm[nb][i]));
+#pragma unroll
+                                    for (int g = 0; g < NG; ++g)
+                                        y[g][i] = fmaxf(y[g][i], w * f[g]);
+                                }
+                            }
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) {
+                            x[nb][g] = __byte_perm(__float_as_uint(y[g][0]), __float_as_uint(y[g][1]), 0x7632);
+                            move |= y[g][0] * bf16_lo(up[nb][g]) >= kQ4ProductMost ||
+                                    y[g][1] * bf16_hi(up[nb][g]) >= kQ4ProductMost;
                         }
                     }
+                    if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
-                    for (int b = 0; b < NS; ++b) {
-                        const float p0 = fast_exp2(fmaf(sc[b][nb][0], mul[nb][0], nm[nb][0]));
-                        const float p1 = fast_exp2(fmaf(sc[b][nb][1], mul[nb][1], nm[nb][1]));
-                        const float p2 = fast_exp2(fmaf(sc[b][nb][2], mul[nb][0], nm[nb][0]));
-                        const float p3 = fast_exp2(fmaf(sc[b][nb][3], mul[nb][1], nm[nb][1]));
-                        la[nb][0] += p0 + p2;
-                        la[nb][1] += p1 + p3;
-                        pb[b][nb][0] = movmatrix_trans(pack_f16x2(p0, p1));
-                        pb[b][nb][1] = movmatrix_trans(pack_f16x2(p2, p3));
+                        for (int g = 0; g < NG; ++g) {
+                            float m = 0.f;   // the largest power of two of the lane's heads
+#pragma unroll
+                            for (int nb = 0; nb < NB; ++nb) {
+                                uint32_t z = x[nb][g];
+                                z = __vmaxu2(z, __shfl_xor_sync(0xffffffffu, z, 4));
+                                z = __vmaxu2(z, __shfl_xor_sync(0xffffffffu, z, 8));
+                                z = __vmaxu2(z, __shfl_xor_sync(0xffffffffu, z, 16));
+                                float to[2];
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    const float y = i == 0 ? bf16_lo(z) : bf16_hi(z);
+                                    const float u = i == 0 ? bf16_lo(up[nb][g]) : bf16_hi(up[nb][g]);
+                                    to[i] = fminf(u * lift[nb][i], 0x1p126f);
+                                    if (y * to[i] >= kQ4ProductMost)   // 2^(kQ4ProductTop - floor(log2 y))
+                                        to[i] = __uint_as_float(
+                                            (254u + kQ4ProductTop - (__float_as_uint(y) >> 23)) << 23);
+                                    const float f = alpha[nb][i] * (to[i] * reciprocal2(u));
+#pragma unroll
+                                    for (int n = 0; n < 2; ++n) {
+                                        o[nb][2 * g + n][i] *= f;
+                                        o[nb][2 * g + n][2 + i] *= f;
+                                    }
+                                    m = fmaxf(m, to[i]);
+                                }
+                                up[nb][g] = __byte_perm(__float_as_uint(to[0]), __float_as_uint(to[1]), 0x7632);
+                            }
+                            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                            if (lane % NG == g)   // a power of two
+                                v_most = (__float_as_uint(kQ4ProductMost * reciprocal2(m)) >> 16) * 0x10001u;
+                        }
                     }
                 }
-                __syncwarp();   // the scales of V are in place
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    const float2 mul2 = make_float2(mul[nb][0], mul[nb][1]);
+                    const float2 nm2 = make_float2(nm[nb][0], nm[nb][1]);
+                    float2 l2 = make_float2(la[nb][0], la[nb][1]);
+#pragma unroll
+                    for (int b = 0; b < NS; ++b)
+#pragma unroll
+                        for (int hi = 0; hi < 2; ++hi) {
+                            float *x = sc[b][nb] + 2 * hi;
+                            const float2 y = __ffma2_rn(make_float2(x[0], x[1]), mul2, nm2);
+                            x[0] = fast_exp2(y.x);
+                            x[1] = fast_exp2(y.y);
+                            l2 = __fadd2_rn(l2, make_float2(x[0], x[1]));
+                        }
+                    la[nb][0] = l2.x;
+                    la[nb][1] = l2.y;
+                }
                 // ---- O += V^T (s P)^T ----
 #pragma unroll
                 for (int b = 0; b < NS; ++b) {
                     const uint8_t *blk = st + b * LY::kBytes;
-                    uint32_t vw[2 * NG], vs[2 * NG];   // [th][group]
+                    // weights times scales, in fp32, rounded once, [hi][group]
+                    uint32_t pb[NB][2 * NG];
+                    float f[2][NG];
+                    v_scales(b, 0, f[0]);
+                    v_scales(b, 1, f[1]);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int k = 0; k < 2 * NG; ++k) {
+                            const int hi = k / NG, g = k % NG;
+                            const float2 w = make_float2(sc[b][nb][2 * hi], sc[b][nb][2 * hi + 1]);
+                            const float2 u = make_float2(bf16_lo(up[nb][g]), bf16_hi(up[nb][g]));
+                            const float2 x = __fmul2_rn(__fmul2_rn(w, make_float2(f[hi][g], f[hi][g])), u);
+                            pb[nb][k] = movmatrix_trans(pack_f16x2(x.x, x.y));
+                        }
+                    uint32_t vw[2 * NG];   // [th][group]
 #pragma unroll
                     for (int q = 0; q < 2 * NG / 4; ++q) {
                         const uint4 w =
@@ -572,12 +674,6 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
                         vw[4 * q + 1] = w.y;
                         vw[4 * q + 2] = w.z;
                         vw[4 * q + 3] = w.w;
-                        const uint4 f = *reinterpret_cast<const uint4 *>(
-                            vscale + b * 8 * NG + tig * 2 * NG + q * 4);
-                        vs[4 * q] = f.x;
-                        vs[4 * q + 1] = f.y;
-                        vs[4 * q + 2] = f.z;
-                        vs[4 * q + 3] = f.w;
                     }
 #pragma unroll
                     for (int g = 0; g < NG; ++g) {
@@ -587,10 +683,8 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
                                                q4_pair(w1, 2), q4_pair(w1, 3)};
 #pragma unroll
                         for (int nb = 0; nb < NB; ++nb) {
-                            const uint32_t b0 = hmul2_f16(pb[b][nb][0], vs[g]);
-                            const uint32_t b1 = hmul2_f16(pb[b][nb][1], vs[NG + g]);
-                            mma_f16(o[nb][2 * g], a[0], a[1], a[2], a[3], b0, b1);
-                            mma_f16(o[nb][2 * g + 1], a[4], a[5], a[6], a[7], b0, b1);
+                            mma_f16(o[nb][2 * g], a[0], a[1], a[2], a[3], pb[nb][g], pb[nb][NG + g]);
+                            mma_f16(o[nb][2 * g + 1], a[4], a[5], a[6], a[7], pb[nb][g], pb[nb][NG + g]);
                         }
                     }
                 }
@@ -607,8 +701,6 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
             p.out + (static_cast<size_t>(cs.beta) * p.h + static_cast<size_t>(cs.j) * G) * D;
         // the runs that hold the segment
         const int c0 = cta_of_tile(cs.first, N, P), c1 = cta_of_tile(seg_end - 1, N, P);
-        // out of the units of the codes and of the scales' bound (whose product may pass fp32's range)
-        auto whole_units = [&](float x) { return x * kQ4Unit * bound; };
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -617,6 +709,15 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
                 la[nb][i] += __shfl_xor_sync(0xffffffffu, la[nb][i], 8);
                 la[nb][i] += __shfl_xor_sync(0xffffffffu, la[nb][i], 16);
             }
+        // Four channels of head 2 tig + i and group g: the piece's sums, over its weights' (inv: 1 / la) before
+        // they leave the units of codes and scales, lest they pass fp32's range.
+        auto mean4 = [&](int nb, int g, int i, float inv) {
+            const float u = i == 0 ? bf16_lo(up[nb][g]) : bf16_hi(up[nb][g]);
+            const float down = reciprocal2(u);
+            inv *= kQ4Unit;
+            return make_float4(o[nb][2 * g][i] * inv * down, o[nb][2 * g][2 + i] * inv * down,
+                               o[nb][2 * g + 1][i] * inv * down, o[nb][2 * g + 1][2 + i] * inv * down);
+        };
         // Merges the segment's records, in their order, by the threads t of n: C times four columns of K
         // records a thread in flight (one round trip to L2 after another otherwise: 6 us at the end of
         // a launch).
@@ -699,10 +800,7 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
                         const size_t at = static_cast<size_t>(head) * D + gid * 4;
 #pragma unroll
                         for (int g = 0; g < NG; ++g) {
-                            const float4 v = make_float4(whole_units(o[nb][2 * g][i]) * inv,
-                                                         whole_units(o[nb][2 * g][2 + i]) * inv,
-                                                         whole_units(o[nb][2 * g + 1][i]) * inv,
-                                                         whole_units(o[nb][2 * g + 1][2 + i]) * inv);
+                            const float4 v = mean4(nb, g, i, inv);
                             if (whole)
                                 *reinterpret_cast<uint2 *>(ob + at + 32 * g) =
                                     make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
@@ -750,15 +848,13 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 float *dst = raw + (warp * 8 + 2 * tig + i) * PL::kRow + gid * 4;
+                // (a warp without a tile: zeros, with the weight 0)
+                const float inv = la[nb][i] == 0.f ? 0.f : fast_rcp(la[nb][i]);
 #pragma unroll
                 for (int g = 0; g < NG; ++g)
-                    *reinterpret_cast<float4 *>(dst + g * 32) =
-                        make_float4(whole_units(o[nb][2 * g][i]), whole_units(o[nb][2 * g][2 + i]),
-                                    whole_units(o[nb][2 * g + 1][i]),
-                                    whole_units(o[nb][2 * g + 1][2 + i]));
+                    *reinterpret_cast<float4 *>(dst + g * 32) = mean4(nb, g, i, inv);
                 if (gid == 0) {
-                    st_m[(8 * nb + 2 * tig + i) * NW + warp] =
-                        top[nb][i] == NEG_INF ? NEG_INF : -nm[nb][i];
+                    st_m[(8 * nb + 2 * tig + i) * NW + warp] = -nm[nb][i];
                     st_l[(8 * nb + 2 * tig + i) * NW + warp] = la[nb][i];
                 }
             }
@@ -770,12 +866,18 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
 #pragma unroll
                 for (int w = 0; w < NW; ++w)
                     ms = fmaxf(ms, st_m[(8 * nb + row) * NW + w]);
-                float ls = 0.f;
+                float ls = 0.f, weight[NW];
                 float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < NW; ++w) {
-                    const float f = fast_exp2(st_m[(8 * nb + row) * NW + w] - ms);
-                    ls = fmaf(st_l[(8 * nb + row) * NW + w], f, ls);
+                    weight[w] = st_l[(8 * nb + row) * NW + w] *
+                                fast_exp2(st_m[(8 * nb + row) * NW + w] - ms);
+                    ls += weight[w];
+                }
+                const float inv = fast_rcp(ls);
+#pragma unroll
+                for (int w = 0; w < NW; ++w) {
+                    const float f = weight[w] * inv;
                     const float4 x =
                         *reinterpret_cast<const float4 *>(raw + (w * 8 + row) * PL::kRow + e);
                     v.x = fmaf(f, x.x, v.x);
@@ -783,11 +885,6 @@ __global__ void __launch_bounds__(Q4Plan<D, NB, kWarpRuns>::kThreads,
                     v.z = fmaf(f, x.z, v.z);
                     v.w = fmaf(f, x.w, v.w);
                 }
-                const float inv = fast_rcp(ls);
-                v.x *= inv;
-                v.y *= inv;
-                v.z *= inv;
-                v.w *= inv;
                 const int at = 8 * nb * D + i;
                 if (whole) {
                     *reinterpret_cast<uint2 *>(ob + at) =
