@@ -37,7 +37,7 @@ extern "C" {
 #define MLKV_ERR_INVALID_ARG (-1) /* null handle/pointer, misaligned buffer, bad index */
 #define MLKV_ERR_MAP (-2)         /* invalid layer->owner map or head counts */
 #define MLKV_ERR_RANGE (-3)       /* a sequence length outside [1, max_seq] */
-#define MLKV_ERR_OOM (-4)         /* device allocation failed */
+#define MLKV_ERR_OOM (-4)         /* device allocation failed, or more bytes than any device has */
 #define MLKV_ERR_CUDA (-5)        /* a CUDA runtime / driver call failed */
 #define MLKV_ERR_UNSUPPORTED (-6) /* valid request outside what this build supports */
 #define MLKV_ERR_DEVICE (-7)      /* a kernel reported an error (bounded wait expired) */

@@ -460,7 +460,9 @@ static int decode_impl(mlkv_cache_t c, int layer, const void *K_new, const void 
     int rc = check_seq_lens(c, seq_lens);
     if (rc != MLKV_OK)
         return rc;
-    // What a sliding window leaves of a length, in positions (the tiles' count follows below).
+    // What a sliding window leaves of a length, in positions (the tiles' count follows below).  (No call has
+    // both a window and new tokens: the kernel puts a new token into a segment's last tile, and would take
+    // the sinks' last one for it.)
     auto gap = [&](int L) { return window > 0 && L - window > sinks; };
     auto seen = [&](int L) { return gap(L) ? window + sinks : L; };
     double mean_len = 0.0;

@@ -19,7 +19,7 @@
 // 29.8 us, 5.6 TB/s.  Heads of 64 are bound by latency (a token's position, then its factors): several tokens
 // a warp, few enough heads of each at a time that they take three loads and divide evenly (39.3 us with
 // whole tokens a warp, the last load half empty), five blocks an SM for their registers (six with two
-// loads 30.4, four 32.7).  A batch's single tokens are bound by the caller: 6.2 us of Python and launch.
+// loads 30.4, four 32.7).  A batch's single tokens are bound by the caller: 7.0 us of Python and launch.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>

@@ -132,8 +132,8 @@ struct Q4DecodeParams {
 constexpr int q4_tile_tokens(int d) { return d == 128 ? 32 : 64; }
 cudaError_t prepare_q4_decode(int d, int group, int *ctas_per_sm);
 // Warps of a CTA, two CTAs an SM: what the accumulators of 8 or 16 heads leave registers for.  Measured, us:
-// 32 sequences of 16384, groups of 16 heads of 128, with 4 / 5 / 6 / 8 warps 46.9 / 55.1 / 49.7 / 81.5; 64 of
-// 16384, groups of 12 heads of 64, 27.8 / 30.8 / 27.0 / 28.4.
+// 32 sequences of 16384, groups of 16 heads of 128, with 4 / 5 / 6 / 8 warps 51.4 / 83.4 / 79.7 / 107.4; 64 of
+// 16384, groups of 12 heads of 64, 27.9 / 32.7 / 28.5 / 39.5.
 constexpr int q4_warps(int d, int group) { return group <= 8 ? 8 : d == 64 ? 6 : 4; }
 // Records of warps' runs up to which the warp that finishes a segment merges them (else a launch of its own).
 constexpr int kQ4InlineMergePieces = 16;

@@ -115,8 +115,8 @@ long long warp_pieces(int nt, long long run) { return (nt + kEmpty - 2 + run) / 
 // Estimated us of merging S segments' records of CTAs, up to `pieces` each: by the CTA that finishes a
 // segment, in round trips to L2 (8 records of four columns a thread), or by a launch of a CTA for every row.
 // Measured, us, the first / the second: one sequence of 8192, 8 KV heads of 128, 4 query heads each, 16
-// records 8.1 / 32 records 7.5; 4 sequences of 4000, 2 KV heads, 16 query heads each, 16 records 11.5 / 9.3,
-// 64 of them, 2 records 27.4 / 34.0.
+// records 8.7 / 7.8, 32 records 9.6 / 8.0; 4 sequences of 4000, 2 KV heads, 16 query heads each, 16 records
+// 12.5 / 9.5, 64 of them, 2 records 30.0 / 36.9.
 struct Q4Merge {
     float us;
     bool deferred;
@@ -138,8 +138,11 @@ struct Q4Deal {
 };
 
 // S segments of at most nt_max tiles, `sum` of them in all (warp_tiles with the empty ones); same: of one
-// number of tiles.  The least of the estimated times, whose terms are fits to calls of 4 to 128 sequences of
-// 64 to 4000 positions, even and uneven.
+// number of tiles.  The least of the estimated times, whose terms are fits to 137 calls, even and uneven: 4 to
+// 512 sequences of 64 to 4000 positions, 2 of 30000 and 3 of 60000.  (Fitted to a kernel whose tiles took 8%
+// less; the split taken was measured again against every other since: at most 6% behind the best in 129 of
+// them, at most 14% in the rest.  Outside, the terms are extrapolated: one sequence of 131072, 12 heads of 64,
+// 11.4 us; 8 of 65536, 8 KV heads of 128, 107.6, of which the bytes take 88.8.)
 Q4Deal deal(const mlkv_q4cache *c, long long S, long long sum, long long warp_tiles, int nt_max, bool same)
 {
     const int W = mlkv::q4_warps(c->d, c->G);
@@ -387,13 +390,13 @@ int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *o
     }
     p.uniform_len = uniform ? seq_lens[0] : 0;
     // The tiles are dealt out in equal runs.  A run a warp: tiles end to end, with three empty ones behind a
-    // segment for the cost of its end (64 uneven sequences of up to 8192 positions, 8 KV heads of 128: 58.8,
-    // 57.5, 56.6 us with 1, 2, 3, 56.1 to 57.5 with 4 to 8); every end is a record and its merge.  A run a
+    // segment for the cost of its end (64 uneven sequences of up to 8192 positions, 8 KV heads of 128: 63.6,
+    // 61.1, 60.1 us with 1, 2, 3, 59.7 to 61.2 with 4 to 8); every end is a record and its merge.  A run a
     // CTA: a segment's tiles filled up to whole runs, so that no run crosses a segment, of as many turns of
     // the warps as the estimate says; a whole segment needs no merge.  (Equal runs that cross segments
-    // cost each CTA ~3 us an end: 16 uneven sequences of up to 1000, 8 KV heads of 128, 25.5 us, 7.9 now, 64
-    // of them 39.2 and 15.6.)  Measured, us, a warp / a CTA: 32 sequences of 4096 35.8 / 30.9, 64 of 1000 21.3 /
-    // 19.2, 20 of 4000 23.8 / 30.5, 64 uneven ones of up to 4000, 4 KV heads of 64, 16.1 / 14.9.
+    // cost each CTA ~3 us an end: 16 uneven sequences of up to 1000, 8 KV heads of 128, 25.5 us, 9.0 now, 64
+    // of them 39.2 and 18.5.)  Measured, us, a warp / a CTA: 32 sequences of 4096 37.9 / 33.2, 64 of 1000 24.1 /
+    // 22.4, 20 of 4000 27.4 / 30.0, 64 uneven ones of up to 4000, 4 KV heads of 64, 18.7 / 17.2.
     const long long warp_tiles = c->g * (sum + static_cast<long long>(kEmpty) * c->b);
     int turns = deal(c, S, sum * c->g, warp_tiles, nt_max, nt_min == nt_max).turns;
     const bool warp_runs = turns == 0;
@@ -477,7 +480,7 @@ int mlkv_q4_decode_attention(mlkv_q4cache_t c, int layer, const void *Q, void *o
         m.decode_grid = grid * (warp_runs ? W : 1);
         // 256 threads a row take 4096 / d records a round trip to L2, 1024 four times as many but ~1 us
         // more for themselves: wide from the third round trip on (256 / 1024 threads, us: 171 records of
-        // 12 heads of 64 12.7 / 11.1, 128 of 16 heads of 128 14.6 / 10.9; two: 38 of 128 14.5 / 15.7).
+        // 12 heads of 64 12.9 / 11.4, 128 of 16 heads of 128 13.3 / 9.9; two: 38 of 16 heads of 128 9.9 / 9.6).
         const bool wide = pieces > 2 * 4096 / c->d;
         if ((e = mlkv::launch_combine(m, c->d, stream, true, wide)) != cudaSuccess)
             return fail_cuda(e, "combine launch");

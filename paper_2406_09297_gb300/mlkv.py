@@ -359,8 +359,8 @@ def mlkv_qk_norm_rope(Q, K, V, q_gain, k_gain, cos, sin, positions, Q_out, K_out
     None, K and K_out too where a layer has queries alone), gains [d] or None, cos and sin fp32
     [n_pos][rot / 2] and positions int32 [b][s] (None: no rotary encoding) -> Q_out [b][s][h][d],
     K_out and V_out [b][g][s][d], all bf16."""
-    # (one condition over all tensors, and one block of arguments: of a step's call 6.1 us were here with
-    # a function call a tensor and 23 converted arguments)
+    # (one condition over all tensors, and one block of arguments: of a step's call 4.0 us are here, 6.1
+    # with a function call a tensor and 23 converted arguments, without types)
     b, s, h, d = Q.shape
     tokens = b * s
     g = n_pos = half = k_stride = v_stride = 0

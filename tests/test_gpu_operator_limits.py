@@ -45,3 +45,26 @@ def test_q4_prompts_outside_the_device_are_refused():
     cache.load_prefix(0, K, K, s)
     cache.sync_status()
     assert out[0].any(-1).all()
+
+
+def test_q4_prompts_in_a_graph():
+    """Where a prompt lies is asked while a graph records, too."""
+    b, g, h, s, d = 2, 2, 4, 70, 64
+    cache = mlkv.MLKVQ4Cache(1, h, d, [0], g, b, s)
+    K = torch.randn((b, g, s, d), device="cuda").bfloat16()
+    Q = torch.randn((b, s, h, d), device="cuda").bfloat16()
+    out = torch.zeros_like(Q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        cache.prefill(0, Q, K, K, out, [s, s])
+    torch.cuda.current_stream().wait_stream(side)
+    want = out.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.prefill(0, Q, K, K, out, [s, s])
+        cache.load_prefix(0, K, K, s)
+    out.zero_()
+    graph.replay()
+    cache.sync_status()
+    assert torch.equal(out, want)
