@@ -142,3 +142,21 @@ def test_logits_that_rise_as_values_fall(d, h, g, lens, window, sinks):
     K[:] = K * 0.2 + at[:, None] * logit(1.0)
     V *= torch.exp(-at)[:, None]
     _check(d, h, g, lens, Q, K, V, window, sinks)
+
+
+@pytest.mark.parametrize("d,h,g,lens,window,sinks", FORMS)
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_bad_value_stays_in_its_group(d, h, g, lens, window, sinks, bad):
+    """A visible value that is none spoils its 32 channels, of its KV head and sequence alone."""
+    Q, K, V, _, _ = _inputs(d, h, g, lens, 7)
+    K, V = K.bfloat16(), V.bfloat16()
+    i = len(lens) - 1
+    V[i, g - 1, lens[i] - 1, 33] = bad
+    cache = mlkv.MLKVQ4Cache(1, h, d, [0], g, len(lens), max(lens))
+    cache.load_prefix(0, K, V, max(lens))
+    out = torch.zeros_like(Q)
+    cache.decode_attention(0, Q, out, lens, window, sinks)
+    cache.sync_status()
+    want = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+    want[i, (g - 1) * (h // g):, 32:64] = True
+    assert torch.equal(torch.isnan(out), want) and torch.isfinite(out[~want]).all()
