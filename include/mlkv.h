@@ -45,6 +45,7 @@ extern "C" {
 #define MLKV_MAX_BATCH 1024       /* largest batch a cache may hold */
 #define MLKV_MAX_GROUP 16         /* largest query group h/g per KV head */
 #define MLKV_STATIC_SCRATCH_BYTES (8u << 20) /* scratch of mlkv_decode_attention_static */
+#define MLKV_BLOCK 64              /* positions of a block (mlkv_block_bounds) */
 
 typedef struct mlkv_cache *mlkv_cache_t;
 
@@ -253,6 +254,134 @@ int mlkv_decode_attention_window(mlkv_cache_t c, int layer, const void *Q, void 
 int mlkv_prefill_window(mlkv_cache_t c, int layer, const void *Q, const void *K, const void *V,
                         void *out, const int *prompt_lens, int s_max, int window, int sinks,
                         void *cuda_stream);
+
+/*
+ * mlkv_decode_attention_prefix - mlkv_decode_attention of sequences that share long beginnings, each of them held
+ * once: sequence beta attends to positions [0, prefix_lens[x]) of sequence x = prefix_of[beta] of the cache
+ * `prefix`, and then to its own positions [0, seq_lens[beta]) of c, under one softmax.  A prefix's keys and values
+ * are read once for all the sequences that share it.  (The paper's decode, Eqs. 2-3 with the maps of Eqs. 15 and
+ * 18, over the two caches' positions end to end.)
+ *
+ *   prefix       a cache of the same layers, heads and owner map on the same device, filled as any other
+ *                (mlkv_prefill, mlkv_load_prefix); c itself will do
+ *   prefix_of    host int32[batch]: a sequence of `prefix`, or -1: none
+ *   prefix_lens  host int32[prefix's batch], 0 <= prefix_lens[x] <= prefix's max_seq
+ * The other arguments as for mlkv_decode_attention: seq_lens counts a sequence's own positions, the new token
+ * included (keys are encoded by the caller: a sequence's own positions follow its prefix's).  Calls on c must be
+ * ordered with those on `prefix` that store what it reads.  Scratch of c is allocated when a call needs more than
+ * any before (not while cuda_stream is captured: MLKV_ERR_UNSUPPORTED); at most 255 KV heads.
+ * Errors: as mlkv_decode_attention; MLKV_ERR_MAP (the caches' layers or heads differ), MLKV_ERR_RANGE (prefixes,
+ * lengths), MLKV_ERR_OOM.
+ */
+int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix, const int *prefix_of,
+                                 const int *prefix_lens, const void *Q, void *out, const int *seq_lens,
+                                 void *cuda_stream);
+
+/*
+ * mlkv_prefill_prefix - mlkv_prefill of prompts that go on behind a shared beginning: prompt position t of
+ * sequence beta attends to all of its prefix's positions and to positions 0 .. t of its prompt.  An owner layer
+ * stores its prompt's K/V in c at positions [0, s_max); the prefix stays where it is, and mlkv_decode_attention_prefix
+ * goes on from there.
+ * prefix, prefix_of and prefix_lens as above, but prefix != c; the others and errors as for mlkv_prefill.
+ */
+int mlkv_prefill_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix, const int *prefix_of,
+                        const int *prefix_lens, const void *Q, const void *K, const void *V, void *out,
+                        const int *prompt_lens, int s_max, void *cuda_stream);
+
+/*
+ * mlkv_block_bounds - what the keys of each block of MLKV_BLOCK positions lie between, in 8 bits a channel: 1/64 of
+ * the keys' and values' bytes, from which mlkv_select_blocks tells which blocks a step needs.
+ *
+ * Block n holds positions [64 n, 64 n + 64) below seq_lens[beta].  With amax its keys' largest magnitude, its
+ * scale is 2^e for the least whole number e in [-60, 40] with amax <= 127 * 2^e, and channel i has the codes
+ * floor(min / scale) and ceil(max / scale).  A block with a NaN, an infinity or a magnitude above 127 * 2^40 has
+ * scale infinity and codes -127 and 127.
+ *
+ *   layer     an owner layer; for another layer the call returns MLKV_OK and queues nothing (its owner's bounds
+ *             are its own)
+ *   first     host int32[batch], 0 <= first[beta] <= seq_lens[beta], or NULL: 0.  Blocks that end at or before
+ *             position first[beta] are left as they are: after a step's mlkv_append, seq_lens[beta] - 1
+ *   bounds    device int8 [batch][g][n_blocks][2][d], n_blocks = ceil(max_seq / 64): least and largest codes;
+ *             16-byte aligned
+ *   scales    device fp32 [batch][g][n_blocks]
+ * The caller keeps both from step to step.  Blocks behind a sequence's last are left as they are.
+ * Errors: MLKV_ERR_INVALID_ARG, MLKV_ERR_RANGE (lengths, first), MLKV_ERR_UNSUPPORTED (more blocks than a launch
+ * has CTAs), MLKV_ERR_CUDA.
+ */
+int mlkv_block_bounds(mlkv_cache_t c, int layer, const int *first, const int *seq_lens, void *bounds,
+                      float *scales, void *cuda_stream);
+
+/*
+ * mlkv_select_blocks - the blocks of each (sequence, KV head) in which its queries' largest scores may lie.
+ *
+ * Each query head in 8 bits, q8 = q / 2^f to the nearest (halves to even), 2^f a scale as above but of the head; a
+ * block's score is the largest, over the group's heads, of 2^f scale sum_i max(q8_i lo_i, q8_i hi_i), exact in
+ * fp32.  Selected are the first n_first and the last n_last of a sequence's blocks, and of the others those of
+ * the largest scores (a scale of infinity before all), of equal ones the first; n_select in all, or all
+ * there are.  A head with a NaN, an infinity or a magnitude above 127 * 2^40 has no say.
+ *
+ *   bounds, scales   of the layer's owner (mlkv_block_bounds), current for every block below seq_lens but the
+ *                    n_last last
+ *   n_select         >= 1, n_first and n_last >= 0, n_first + n_last <= n_select
+ *   blocks           device int32 [batch][g][n_select]: block numbers in rising order, -1 behind them
+ * Errors: MLKV_ERR_INVALID_ARG, MLKV_ERR_RANGE (lengths), MLKV_ERR_UNSUPPORTED (a sequence of more than 327,680
+ * blocks), MLKV_ERR_CUDA.
+ */
+int mlkv_select_blocks(mlkv_cache_t c, int layer, const void *Q, const void *bounds, const float *scales,
+                       const int *seq_lens, int n_select, int n_first, int n_last, int *blocks,
+                       void *cuda_stream);
+
+/*
+ * mlkv_decode_attention_blocks - mlkv_decode_attention over listed blocks alone: the queries of KV head j of
+ * sequence beta attend to the positions below seq_lens[beta] of the blocks blocks[beta][j][0 .. n_blocks).
+ *
+ *   blocks    device int32 [batch][g][n_blocks], 4-byte aligned; a number that is no block of a visible position
+ *             (-1, say) is passed over, one that comes twice counts twice; without any, outputs are zeros
+ *   n_blocks  >= 1
+ * The other arguments and errors as for mlkv_decode_attention (its options do not apply), and
+ * MLKV_ERR_UNSUPPORTED for 2^31 listed blocks or more.
+ */
+int mlkv_decode_attention_blocks(mlkv_cache_t c, int layer, const void *Q, void *out, const int *seq_lens,
+                                 const int *blocks, int n_blocks, void *cuda_stream);
+
+/*
+ * mlkv_decode_attention_weights - mlkv_decode_attention that also adds up what each position of each KV head
+ * was given: weights_out[beta][j][u] = weights_in[beta][j][u] + the sum over the group's heads of their softmax
+ * weight of position u < seq_lens[beta] (Eq. 2's alpha).  The layers of an owner's block add to the owner's
+ * weights one after the other.
+ *
+ *   weights_in   device fp32 [batch][g][max_seq], or NULL: zeros
+ *   weights_out  device fp32 [batch][g][max_seq], written whole; weights_in itself, or apart from it
+ * The other arguments and errors as for mlkv_decode_attention (its options do not apply).  Scratch of
+ * batch * n_q_heads * (longest sequence) * 4 bytes, allocated as for mlkv_decode_attention_prefix.
+ */
+int mlkv_decode_attention_weights(mlkv_cache_t c, int layer, const void *Q, void *out, const int *seq_lens,
+                                  const float *weights_in, float *weights_out, void *cuda_stream);
+
+/*
+ * mlkv_evict - keeps, of each (sequence, KV head) of an owner layer, the `recent` newest positions and, of the
+ * others, those of the largest weights, keep[beta] in all (or all there are), of equal weights the earlier
+ * ones: their keys, values and weights move to positions 0, 1, ... in their order.  A NaN counts as the largest
+ * weight.  KV heads keep positions of their own; a sequence goes on at length min(keep[beta], seq_lens[beta]) in
+ * every owner layer that is evicted the same way.  (Keys are encoded before they are stored, so attention does not
+ * depend on where they lie; windows and `recent` go by the order, which is kept.)
+ *
+ *   to           the cache that receives the positions, of the same layers, heads, owner map, device and batch;
+ *                c itself: in place
+ *   layer        an owner layer; for another layer the call returns MLKV_OK and queues nothing
+ *   weights_in   device fp32 [batch][g][max_seq of c]
+ *   weights_out  device fp32 [batch][g][max_seq of `to`]: the kept positions' weights, zeros behind them; weights_in
+ *                itself (where the two rows are of one length), or apart from it
+ *   keep         host int32[batch], >= 1 and >= recent; min(keep, seq_lens) at most max_seq of `to`, and k_max
+ *   recent       >= 0
+ *   kept         device int32 [batch][g][k_max]: where each kept position lay, rising; what is behind a
+ *                sequence's last is left as it was
+ * Positions of `to` behind the kept ones are left as they were.  Scratch of c, allocated as for
+ * mlkv_decode_attention_prefix.  Errors: MLKV_ERR_INVALID_ARG, MLKV_ERR_MAP (another model or batch),
+ * MLKV_ERR_RANGE (lengths, keep), MLKV_ERR_UNSUPPORTED, MLKV_ERR_OOM, MLKV_ERR_CUDA.
+ */
+int mlkv_evict(mlkv_cache_t c, mlkv_cache_t to, int layer, const float *weights_in, float *weights_out,
+               const int *seq_lens, const int *keep, int recent, int *kept, int k_max, void *cuda_stream);
 
 /*
  * mlkv_qk_norm_rope - queries, keys and values as a projection leaves them, made ready for the calls of

@@ -21,7 +21,8 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 COMMON = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 SOURCES = ["mlkv_kernels.cu", "mlkv_decode_tc.cu", "mlkv_prefill.cu", "mlkv_merge.cu",
            "mlkv_stage.cu", "mlkv_host.cpp", "mlkv_noalloc.cu", "mlkv_measure.cu", "mlkv_norm_rope.cu",
-           "mlkv_q4.cu", "mlkv_q4_decode.cu", "mlkv_q4_host.cpp"]
+           "mlkv_q4.cu", "mlkv_q4_decode.cu", "mlkv_q4_host.cpp", "mlkv_pieces.cu", "mlkv_blocks.cu",
+           "mlkv_evict.cu", "mlkv_long_host.cpp"]
 
 
 def _sources():
@@ -31,7 +32,8 @@ def _sources():
 def _deps():
     deps = _sources() + [os.path.join(CSRC, "mlkv_internal.h"), os.path.join(CSRC, "mlkv_device.cuh"),
                          os.path.join(CSRC, "mlkv_tcgen05.cuh"), os.path.join(CSRC, "mlkv_host.h"),
-                         os.path.join(CSRC, "mlkv_q4.h"),
+                         os.path.join(CSRC, "mlkv_q4.h"), os.path.join(CSRC, "mlkv_cache.h"),
+                         os.path.join(CSRC, "mlkv_long.h"), os.path.join(CSRC, "mlkv_topk.cuh"),
                          os.path.join(INCLUDE, "mlkv.h"),
                          os.path.abspath(__file__)]
     return deps

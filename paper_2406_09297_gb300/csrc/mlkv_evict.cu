@@ -1,0 +1,249 @@
+// Eviction from a KV cache by accumulated attention weight, for GB300: of every (sequence, KV head) the
+// `recent` newest positions stay and, of the others, those of the largest weights, `keep` in all, of equal
+// weights the earlier ones; keys, values and weights of what stays move together, in order.
+//
+// Two launches.  keep_kernel selects: a cluster a segment, a radix select over the weights (cluster_topk), whose
+// result is the list of kept positions.  move_kernel moves: a unit is a run of rows of a segment, which a CTA
+// loads whole before it stores it.  In place, row m takes position kept[m] >= m, so a unit overwrites positions
+// that only units before it, and it itself, still have to read: it stores after those have set their flags.
+// Units are handed out by a counter in rising order within a segment, so that what a unit waits for has been
+// handed out before it and is running: no wait depends on a CTA that has not started.
+// Bound by the bytes of what stays, read and written once.
+#include "mlkv_device.cuh"
+#include "mlkv_long.h"
+#include "mlkv_topk.cuh"
+
+namespace mlkv {
+namespace {
+
+constexpr size_t kKeepSmem = 128 * 1024;   // keys of a CTA that fit in shared memory
+constexpr int kMaxCluster = 8;
+
+// Ordered as the weights, both zeros alike, NaN above infinity.
+__device__ __forceinline__ unsigned weight_key(float w)
+{
+    const uint32_t u = __float_as_uint(w + 0.f);
+    return w != w ? 0xfffffffeu : (u >> 31) ? ~u : u | 0x80000000u;
+}
+
+__global__ void __launch_bounds__(kTopkThreads) keep_kernel(const __grid_constant__ EvictParams p)
+{
+    namespace cg = cooperative_groups;
+    __shared__ TopkShared sh;
+    extern __shared__ unsigned s_key[];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int size = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
+    const int seg = static_cast<int>(blockIdx.x) / size, beta = seg / p.g;
+    const int tid = static_cast<int>(threadIdx.x);
+    const int L = p.seq_len[beta], keep = p.keep[beta];
+    const int per = (L + size - 1) / size;
+    const int first = min(L, rank * per), n = min(L, first + per) - first;
+    const float *w = p.weights_in + static_cast<size_t>(seg) * p.src_seq;
+    int *kept = p.kept + static_cast<size_t>(seg) * p.k_max;
+    grid_dependency_wait();
+    grid_dependents_launch();
+    // the flags of this segment's units; the first CTA also resets the counter of units
+    for (int i = rank * kTopkThreads + tid; i < p.units; i += size * kTopkThreads)
+        p.flags[static_cast<size_t>(seg) * p.units + i] = 0u;
+    if (blockIdx.x == 0 && tid == 0)
+        p.flags[static_cast<size_t>(p.b) * p.g * p.units] = 0u;
+    if (L <= keep) {   // everything stays
+        for (int i = rank * kTopkThreads + tid; i < L; i += size * kTopkThreads)
+            kept[i] = i;
+        return;
+    }
+    const bool cached = static_cast<size_t>(per) * 4 <= kKeepSmem;
+    const int newest = L - p.recent;   // from there on everything stays
+    auto key_at = [&](int i) { return first + i >= newest ? 0xffffffffu : weight_key(__ldcg(w + first + i)); };
+    if (cached) {
+        for (int i = tid; i < n; i += kTopkThreads)
+            s_key[i] = key_at(i);
+        __syncthreads();
+    }
+    cluster_topk(sh, n, static_cast<unsigned>(keep), [&](int i) { return cached ? s_key[i] : key_at(i); },
+                 [&](unsigned place, int i) { kept[place] = first + i; });
+}
+
+constexpr int kMoveThreads = 256;
+constexpr int kUnitVecs = 8;   // 16-byte vectors of a thread and unit
+
+// Rows of a unit: its keys and values are kMoveThreads * kUnitVecs vectors.
+template <int D>
+__host__ __device__ constexpr int unit_rows() { return kMoveThreads * kUnitVecs / (2 * D / 8); }
+
+__device__ __forceinline__ unsigned ld_acquire(const unsigned *p)
+{
+    unsigned v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ void st_release(unsigned *p, unsigned v)
+{
+    asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+}
+
+template <int D>
+__global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constant__ EvictParams p)
+{
+    constexpr int R = unit_rows<D>(), C = D / 8;
+    __shared__ int s_at[R];
+    __shared__ unsigned s_unit;
+    __shared__ int s_first, s_ok, s_move;
+    const int tid = static_cast<int>(threadIdx.x);
+    const int segments = p.b * p.g;
+    const unsigned total = static_cast<unsigned>(segments) * p.units;
+    unsigned *ticket = p.flags + static_cast<size_t>(segments) * p.units;
+    grid_dependency_wait();
+    grid_dependents_launch();
+    for (;;) {
+        __syncthreads();
+        if (tid == 0)
+            s_unit = atomicAdd(ticket, 1u);
+        __syncthreads();
+        const unsigned unit = s_unit;
+        if (unit >= total)
+            return;
+        // units of one segment in rising order, the segments side by side
+        const int r = static_cast<int>(unit / segments), seg = static_cast<int>(unit % segments);
+        const int beta = seg / p.g;
+        const int L = p.seq_len[beta];
+        const int n = min(L, p.keep[beta]);
+        unsigned *flags = p.flags + static_cast<size_t>(seg) * p.units;
+        const int last = (n + R - 1) / R;   // the segment's units of rows; behind them one for the tail
+        if (r > last)
+            continue;
+        const float *w_in = p.weights_in + static_cast<size_t>(seg) * p.src_seq;
+        float *w_out = p.weights_out + static_cast<size_t>(seg) * p.dst_seq;
+        const int m0 = r * R;
+        int rows = min(R, n - m0);
+        uint4 v[kUnitVecs];
+        float w = 0.f;
+        int wait_from = 0;   // the units from there on to this one read what this one writes
+        if (r < last) {
+            const int *kept = p.kept + static_cast<size_t>(seg) * p.k_max;
+            for (int i = tid; i < rows; i += kMoveThreads)
+                s_at[i] = __ldcg(kept + m0 + i);
+            // (positions rise: if the last row is in its place, so are all)
+            if (tid == 0)
+                s_move = !p.same || __ldcg(kept + m0 + rows - 1) != m0 + rows - 1;
+            if (p.in_place && tid == 0) {
+                // the first row whose position is m0 or later: of the first rows, positions below are theirs
+                int lo = 0, hi = m0;
+                while (lo < hi) {
+                    const int mid = (lo + hi) / 2;
+                    if (__ldcg(kept + mid) >= m0)
+                        hi = mid;
+                    else
+                        lo = mid + 1;
+                }
+                s_first = lo / R;
+            }
+            __syncthreads();
+            wait_from = p.in_place ? s_first : 0;
+            if (!s_move) {   // nothing is stored, nothing has to be waited for
+                rows = 0;
+                wait_from = r;
+            }
+#pragma unroll
+            for (int k = 0; k < kUnitVecs; ++k) {
+                const int i = k * kMoveThreads + tid;          // K's vectors, then V's
+                const int kv = i / (R * C), row = i % (R * C) / C, c = i % C;
+                if (row < rows)
+                    v[k] = __ldcs(reinterpret_cast<const uint4 *>(p.src) +
+                                  ((static_cast<size_t>(kv) * segments + seg) * p.src_seq + s_at[row]) * C + c);
+            }
+            if (tid < rows)
+                w = __ldcg(w_in + s_at[tid]);
+        }
+        if (p.in_place) {
+            // (the loads have to have happened, not only been issued, before the flag says so)
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                s_ok = 1;
+                if (r < last)
+                    st_release(flags + r, 1u);
+            }
+            __syncthreads();
+            for (int u = wait_from + tid; u < min(r, last); u += kMoveThreads) {
+                const uint64_t t0 = global_timer_ns();
+                while (ld_acquire(flags + u) == 0u) {
+                    if (global_timer_ns() - t0 > kWaitLimitNs) {
+                        s_ok = 0;
+                        atomicOr(p.err, kErrWaitFull);
+                        break;
+                    }
+                }
+            }
+            __syncthreads();
+            if (!s_ok)
+                continue;   // nothing is stored over what may not have been read
+        }
+        if (r < last) {
+#pragma unroll
+            for (int k = 0; k < kUnitVecs; ++k) {
+                const int i = k * kMoveThreads + tid;
+                const int kv = i / (R * C), row = i % (R * C) / C, c = i % C;
+                if (row < rows)
+                    __stcs(reinterpret_cast<uint4 *>(p.dst) +
+                               ((static_cast<size_t>(kv) * segments + seg) * p.dst_seq + m0 + row) * C + c,
+                           v[k]);
+            }
+            if (tid < rows)
+                w_out[m0 + tid] = w;
+        } else {
+            for (int u = n + tid; u < p.dst_seq; u += kMoveThreads)
+                w_out[u] = 0.f;
+        }
+    }
+}
+
+}  // namespace
+
+int evict_units(int head_dim, int k_max)
+{
+    const int R = head_dim == 64 ? unit_rows<64>() : unit_rows<128>();
+    return (k_max + R - 1) / R + 1;
+}
+
+cudaError_t prepare_evict()
+{
+    return cudaFuncSetAttribute(reinterpret_cast<const void *>(&keep_kernel),
+                                cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kKeepSmem));
+}
+
+cudaError_t launch_evict(int head_dim, const EvictParams &p, int max_len, int sm_count, cudaStream_t stream)
+{
+    int size = 1;
+    while (size < kMaxCluster && size * kTopkThreads * 4 < max_len && p.b * p.g * size < 2 * sm_count)
+        size *= 2;
+    while (size < kMaxCluster && static_cast<size_t>((max_len + size - 1) / size) * 4 > kKeepSmem)
+        size *= 2;
+    const size_t keys = static_cast<size_t>((max_len + size - 1) / size) * 4;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(p.b * p.g * size));
+    cfg.blockDim = dim3(kTopkThreads);
+    cfg.dynamicSmemBytes = keys <= kKeepSmem ? keys : kKeepSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(size);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    void *args[] = {const_cast<EvictParams *>(&p)};
+    cudaError_t e = cudaLaunchKernelExC(&cfg, reinterpret_cast<const void *>(&keep_kernel), args);
+    if (e != cudaSuccess)
+        return e;
+    const long long units = static_cast<long long>(p.b) * p.g * p.units;
+    cfg.gridDim = dim3(static_cast<unsigned>(units < 6LL * sm_count ? units : 6LL * sm_count));
+    cfg.blockDim = dim3(kMoveThreads);
+    cfg.dynamicSmemBytes = 0;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelExC(&cfg, head_dim == 64 ? reinterpret_cast<const void *>(&move_kernel<64>)
+                                                    : reinterpret_cast<const void *>(&move_kernel<128>), args);
+}
+
+}  // namespace mlkv

@@ -17,10 +17,12 @@
 #include <vector>
 
 #include "mlkv.h"
+#include "mlkv_cache.h"
 #include "mlkv_host.h"
 #include "mlkv_internal.h"
 
 using mlkv::aligned16;
+using mlkv::check_seq_lens;
 using mlkv::current_device;
 using mlkv::DeviceGuard;
 using mlkv::driver_entry;
@@ -33,107 +35,6 @@ using mlkv::validate_map;
 namespace {
 
 thread_local std::string g_last_error;
-
-}  // namespace
-
-struct mlkv_cache {
-    int l = 0, h = 0, d = 0, g = 0, G = 0, b = 0, max_seq = 0, m = 0;
-    std::vector<int> owner, slot;
-    int device = 0;
-    int sm_count = 0;
-    int l2_bytes = 0;
-    int window_max = 0;
-    size_t max_smem = 0;        // opt-in dynamic shared memory per block
-    void *cache = nullptr;      // [m][2][b][g][max_seq][d] bf16
-    size_t cache_bytes = 0;
-    float *part_o = nullptr;    // [pieces][G][d]
-    float *part_lse = nullptr;  // [pieces][G]
-    unsigned *counters = nullptr;
-    int *err = nullptr;
-    int max_ctas = 0;           // capacity of the partial buffers beyond b*g pieces
-    long long records = 0;      // partial records the scratch holds
-    // options
-    int tile_tokens = 0;
-    int grid = 0;
-    int l2_persist = 0;
-    size_t persist_bytes = 0;   // the context's persisting-L2 set-aside while l2_persist is on
-    size_t persist_prev = 0;    // the set-aside before l2_persist was switched on
-    int l2_prefetch = 0;        // multi-layer step: prefetch the step's slots into L2 when they fit
-    int step_kernel = 1;        // mlkv_decode_step: one multi-layer launch where it applies
-    int last_step_kernel = 0;   // 1 if the most recent step ran as one multi-layer launch
-    int last_seg_major = 0;     // 1 if that launch ranked its items segment-major
-    int cluster = 1;            // allow the DSMEM cluster merge
-    int pdl = 1;                // programmatic dependent launch
-    int early_fetch = 1;        // per-layer step: later layers read Q and tiles before the wait
-    int tc = 0;                 // 1: the tcgen05 kernel where a variant exists (slower here)
-    int prefill_ready = 0;      // the prefill kernels' shared-memory limits are set (1 all, 2 windowed)
-    int fused_ready = 0;        // the same for the fused-decode forms (bit 1 << form)
-    int fused_deep = 1;         // fused decode: the deep one-tile form where one unit per SM
-    // Context-chunk partials of the fused decode.  A buffer that was outgrown lives until the cache
-    // is destroyed: recorded graphs, the caller's captures among them, hold its address.
-    float *fused_part = nullptr;
-    size_t fused_part_floats = 0;
-    std::vector<float *> fused_outgrown;
-    int step_fused = 1;         // mlkv_decode_step: the cross-layer fused form where it pays (1),
-                                // wherever the map allows it (2), never (0)
-    int last_step_fused = 0;    // 1 if the most recent step ran in that form
-    int last_step_launches = 0;   // this library's launches in the most recent step
-    int last_fused_kc = 0;      // key tiles per unit (chunk) of the most recent fused decode
-    int fused_kc = 0;           // > 0: key tiles per unit of the fused decode, else planned
-    // mlkv_decode_step's recorded graph and the arguments it was recorded for
-    int step_graph = 2;         // 2: direct when one multi-layer launch, else record/replay
-    cudaStream_t record_stream = nullptr;   // private stream the step graph is recorded on
-    cudaGraphExec_t step_exec = nullptr;
-    struct StepKey {
-        const void *Q = nullptr, *K = nullptr, *V = nullptr;
-        void *out = nullptr;
-        std::vector<int> lens;
-        int tile = -1, grid = -1, cluster = -1, pdl = -1, l2 = -1, tc = -1, pf = -1, sk = -1;
-        int sg = -1;   // step_graph: a graph recorded under one mode is not replayed under another
-        int ef = -1, sf = -1, fd = -1, fk = -1;
-        bool operator==(const StepKey &o) const
-        {
-            return Q == o.Q && K == o.K && V == o.V && out == o.out && lens == o.lens &&
-                   tile == o.tile && grid == o.grid && cluster == o.cluster && pdl == o.pdl &&
-                   l2 == o.l2 && tc == o.tc && pf == o.pf && sk == o.sk && sg == o.sg &&
-                   ef == o.ef && sf == o.sf && fd == o.fd && fk == o.fk;
-        }
-    } step_key, pending_key;   // recorded arguments; arguments seen once, not yet recorded
-    int step_graph_replays = 0;
-    // mlkv_decode_step_host: device staging of the step's inputs and outputs, its own graph
-    void *stage = nullptr;     // Q [l][b][h][d], K, V [m][b][g][d], out [l][b][h][d]
-    cudaGraphExec_t host_exec = nullptr;
-    cudaStream_t side = nullptr;   // the copies that overlap the step's layers
-    cudaEvent_t ev[2] = {nullptr, nullptr};   // fork, the later layers' queries in
-    StepKey host_key, host_pending;
-    // the most recent decode launch (read-only options, for tests and tuning)
-    int last_grid = 0, last_tile = 0, last_cluster_k = 0, last_deferred = 0, last_tc = 0;
-    int last_l2_prefetch = 0;
-    // per-variant launch state
-    struct Variant {
-        const mlkv::DecodeVariant *v = nullptr;
-        CUtensorMap tmap;        // boxes of tile_tokens positions
-        CUtensorMap tmap_rows;   // boxes of 64 positions (a partly visible last tile)
-        int ctas_per_sm = 0;
-        int clusters[5] = {0, 0, 0, 0, 0};   // resident k-CTA clusters, k = 2, 4
-    };
-    std::vector<Variant> variants;
-    std::vector<int> tile_start_scratch;
-};
-
-namespace {
-
-int check_seq_lens(const mlkv_cache *c, const int *seq_lens)
-{
-    if (seq_lens == nullptr)
-        return fail(MLKV_ERR_INVALID_ARG, "seq_lens is NULL");
-    for (int beta = 0; beta < c->b; ++beta) {
-        if (seq_lens[beta] < 1 || seq_lens[beta] > c->max_seq)
-            return fail(MLKV_ERR_RANGE, "seq_lens[%d] = %d outside [1, %d]", beta, seq_lens[beta],
-                        c->max_seq);
-    }
-    return MLKV_OK;
-}
 
 mlkv_cache::Variant *pick_variant(mlkv_cache *c, double mean_len = -1.0, int force_T = 0)
 {
@@ -212,6 +113,53 @@ void assign_map(mlkv_cache *c, int l, int h, int d, const int *owner, int g, int
 }  // namespace
 
 void mlkv::set_last_error(const char *msg) { g_last_error = msg; }
+
+int mlkv::check_seq_lens(const mlkv_cache *c, const int *seq_lens)
+{
+    if (seq_lens == nullptr)
+        return fail(MLKV_ERR_INVALID_ARG, "seq_lens is NULL");
+    for (int beta = 0; beta < c->b; ++beta) {
+        if (seq_lens[beta] < 1 || seq_lens[beta] > c->max_seq)
+            return fail(MLKV_ERR_RANGE, "seq_lens[%d] = %d outside [1, %d]", beta, seq_lens[beta],
+                        c->max_seq);
+    }
+    return MLKV_OK;
+}
+
+int mlkv::check_layer(const mlkv_cache *c, int layer)
+{
+    if (c == nullptr)
+        return fail(MLKV_ERR_INVALID_ARG, "null cache handle");
+    if (layer < 0 || layer >= c->l)
+        return fail(MLKV_ERR_INVALID_ARG, "layer %d outside [0, %d)", layer, c->l);
+    return MLKV_OK;
+}
+
+int mlkv::grow_scratch(mlkv_cache *c, size_t floats, const char *what)
+{
+    if (floats <= c->fused_part_floats)
+        return MLKV_OK;
+    // At least twice the former size, so that all the outgrown buffers together are smaller than the
+    // one in use; as much as is needed where that does not fit.
+    float *part = nullptr;
+    size_t want = std::max(floats, 2 * c->fused_part_floats);
+    cudaError_t e = cudaMalloc(&part, want * sizeof(float));
+    if (e != cudaSuccess && want > floats) {
+        cudaGetLastError();
+        want = floats;
+        e = cudaMalloc(&part, want * sizeof(float));
+    }
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return fail(MLKV_ERR_OOM, "%s (%zu bytes): %s", what, floats * sizeof(float),
+                    cudaGetErrorString(e));
+    }
+    if (c->fused_part != nullptr)
+        c->fused_outgrown.push_back(c->fused_part);
+    c->fused_part = part;
+    c->fused_part_floats = want;
+    return MLKV_OK;
+}
 
 int mlkv::validate_map(int l, int h, int d, const int *owner, int g, int b, int max_seq)
 {
@@ -896,24 +844,9 @@ static int fused_issue(mlkv_cache_t c, const void *Q, void *out, int n_q_layers,
     if (cmax > 1) {
         const size_t rows = static_cast<size_t>(nblk) * c->b * c->g * cmax * L * c->G;
         const size_t floats = rows * (c->d + 1);
-        if (floats > c->fused_part_floats) {
-            // At least twice the former size, so that all the outgrown buffers together are smaller
-            // than the one in use; as much as is needed where that does not fit.
-            float *part = nullptr;
-            size_t want = std::max(floats, 2 * c->fused_part_floats);
-            if ((e = cudaMalloc(&part, want * sizeof(float))) != cudaSuccess && want > floats) {
-                cudaGetLastError();
-                want = floats;
-                e = cudaMalloc(&part, want * sizeof(float));
-            }
-            if (e != cudaSuccess)
-                return fail(MLKV_ERR_OOM, "fused-decode partials (%zu bytes): %s",
-                            floats * sizeof(float), cudaGetErrorString(e));
-            if (c->fused_part != nullptr)
-                c->fused_outgrown.push_back(c->fused_part);
-            c->fused_part = part;
-            c->fused_part_floats = want;
-        }
+        const int rc = mlkv::grow_scratch(c, floats, "fused-decode partials");
+        if (rc != MLKV_OK)
+            return rc;
         p.part = c->fused_part;
         p.part_lse = c->fused_part + rows * c->d;
     }
@@ -1870,7 +1803,13 @@ int mlkv::issue_prefill(const PrefillCall &a, cudaStream_t stream)
                             static_cast<int>(r));
         }
     }
-    static thread_local mlkv::PrefillParams p;
+    // A launch takes so many units; the two kernels' parameters differ in their tables alone.
+    const bool shared = a.tmap_prefix != nullptr;
+    static thread_local mlkv::PrefillParams plain;
+    static thread_local mlkv::SharedPrefillParams over;
+    mlkv::PrefillCommon &p = shared ? static_cast<mlkv::PrefillCommon &>(over) : plain;
+    uint32_t *const units = shared ? over.units : plain.units;
+    const int most = shared ? mlkv::kPrefixMaxUnits : mlkv::kPrefillMaxUnits;
     p.out = static_cast<__nv_bfloat16 *>(a.out);
     p.err = a.err;
     p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(a.d)));
@@ -1887,42 +1826,50 @@ int mlkv::issue_prefill(const PrefillCall &a, cudaStream_t stream)
     p.fused_L = p.fused_L1 = 0;
     const CUtensorMap *tmap_k = a.direct ? &tmap_in[0] : a.tmap_kv;
     const CUtensorMap *tmap_v = a.direct ? &tmap_in[1] : a.tmap_kv;
-    int max_len = 0;
-    for (int beta = 0; beta < a.b; ++beta) {
+    for (int beta = 0; beta < a.b; ++beta)
         p.prompt_len[beta] = a.prompt_lens[beta];
-        max_len = std::max(max_len, a.prompt_lens[beta]);
-    }
     // Work units, those that see the most keys first.  head_dim 64: one query block of one head
     // per CTA (two CTAs per SM).  head_dim 128: two heads of a group at the same block when the
     // group size is even, else the blocks 2p and 2p+1 of one head (the unit of block 2p+1).
     const bool one_tile = a.d == 64;
     p.head_pairs = (!one_tile && p.G % 2 == 0) ? 1 : 0;
     const int sels = p.head_pairs ? a.h / 2 : a.h;
-    const int max_blocks = (max_len + 127) / 128;
-    int n = 0;
-    for (int qb = max_blocks - 1; qb >= 0; --qb) {
+    auto pre_blocks = [&](int beta) { return shared ? (over.prefix_len[beta] + 127) / 128 : 0; };
+    int max_blocks = 0;   // key blocks that some unit sees
+    if (shared) {
+        over.tmap_p = *a.tmap_prefix;
+        over.prefix_b = a.prefix_b;
         for (int beta = 0; beta < a.b; ++beta) {
-            const int nb = (a.prompt_lens[beta] + 127) / 128;
-            if (qb >= nb || (!one_tile && !p.head_pairs && qb % 2 == 0 && qb != nb - 1))
+            over.prefix_of[beta] = static_cast<int16_t>(a.prefix_of[beta]);
+            over.prefix_len[beta] = a.prefix_len[beta];
+        }
+    }
+    for (int beta = 0; beta < a.b; ++beta)
+        max_blocks = std::max(max_blocks, pre_blocks(beta) + (a.prompt_lens[beta] + 127) / 128);
+    auto issue = [&](int n) {
+        p.n_units = n;
+        return shared ? mlkv::launch_shared(a.d, false, &tmap_q, tmap_k, tmap_v, over, stream)
+                      : mlkv::launch_prefill(a.d, &tmap_q, tmap_k, tmap_v, plain, stream);
+    };
+    int n = 0;
+    for (int seen = max_blocks - 1; seen >= 0; --seen) {
+        for (int beta = 0; beta < a.b; ++beta) {
+            const int nb = (a.prompt_lens[beta] + 127) / 128, qb = seen - pre_blocks(beta);
+            if (qb < 0 || qb >= nb || (!one_tile && !p.head_pairs && qb % 2 == 0 && qb != nb - 1))
                 continue;
             for (int sel = 0; sel < sels; ++sel) {
-                p.units[n] = static_cast<uint32_t>(beta) | (static_cast<uint32_t>(qb) << 10) |
-                             (static_cast<uint32_t>(sel) << 24);
-                if (++n == mlkv::kPrefillMaxUnits) {
-                    p.n_units = n;
-                    if ((e = mlkv::launch_prefill(a.d, &tmap_q, tmap_k, tmap_v, p, stream)) !=
-                        cudaSuccess)
+                units[n] = static_cast<uint32_t>(beta) | (static_cast<uint32_t>(qb) << 10) |
+                           (static_cast<uint32_t>(sel) << 24);
+                if (++n == most) {
+                    if ((e = issue(n)) != cudaSuccess)
                         return fail_cuda(e, "prefill launch");
                     n = 0;
                 }
             }
         }
     }
-    if (n > 0) {
-        p.n_units = n;
-        if ((e = mlkv::launch_prefill(a.d, &tmap_q, tmap_k, tmap_v, p, stream)) != cudaSuccess)
-            return fail_cuda(e, "prefill launch");
-    }
+    if (n > 0 && (e = issue(n)) != cudaSuccess)
+        return fail_cuda(e, "prefill launch");
     return MLKV_OK;
 }
 
@@ -1959,7 +1906,8 @@ extern "C" {
 
 static int prefill_impl(mlkv_cache_t c, int layer, const void *Q, const void *K, const void *V,
                         void *out, const int *prompt_lens, int s_max, int window, int sinks,
-                        void *cuda_stream)
+                        void *cuda_stream, mlkv_cache_t prefix = nullptr,
+                        const int *prefix_of = nullptr, const int *prefix_lens = nullptr)
 {
     if (c == nullptr)
         return fail(MLKV_ERR_INVALID_ARG, "null cache handle");
@@ -1993,9 +1941,19 @@ static int prefill_impl(mlkv_cache_t c, int layer, const void *Q, const void *K,
                 return rc;
         }
     }
-    const int ready = window > 0 ? 2 : 1;   // the two kernels' bits
+    // (prompts of which none has anything in front are the plain prefill's)
+    static thread_local int pre_len[MLKV_MAX_BATCH];
+    bool shared = false;
+    if (prefix != nullptr) {
+        for (int beta = 0; beta < c->b; ++beta) {
+            pre_len[beta] = prefix_of[beta] >= 0 ? prefix_lens[prefix_of[beta]] : 0;
+            shared = shared || pre_len[beta] > 0;
+        }
+    }
+    const int ready = shared ? 4 : window > 0 ? 2 : 1;   // the three kernels' bits
     if (!(c->prefill_ready & ready)) {
-        const cudaError_t e = mlkv::prepare_prefill(c->d, window > 0);
+        const cudaError_t e = shared ? mlkv::prepare_shared(c->d, false)
+                                     : mlkv::prepare_prefill(c->d, window > 0);
         if (e != cudaSuccess)
             return fail_cuda(e, "cudaFuncSetAttribute(prefill)");
         c->prefill_ready |= ready;
@@ -2022,6 +1980,16 @@ static int prefill_impl(mlkv_cache_t c, int layer, const void *Q, const void *K,
     a.direct = direct;
     a.window = window;
     a.sinks = sinks;
+    if (shared) {
+        for (auto &v : prefix->variants)
+            if (v.v->tile_tokens == 128)
+                a.tmap_prefix = &v.tmap;
+        if (a.tmap_prefix == nullptr)
+            return fail(MLKV_ERR_UNSUPPORTED, "no 128-position cache map for d=%d", c->d);
+        a.prefix_b = prefix->b;
+        a.prefix_of = prefix_of;
+        a.prefix_len = pre_len;
+    }
     if ((rc = mlkv::issue_prefill(a, stream)) != MLKV_OK)
         return rc;
     // Sec. 3: only an owner layer stores K/V -- the prompt's, at positions [0, s_max).
@@ -2039,6 +2007,19 @@ int mlkv_prefill_window(mlkv_cache_t c, int layer, const void *Q, const void *K,
                         void *cuda_stream)
 {
     return prefill_impl(c, layer, Q, K, V, out, prompt_lens, s_max, window, sinks, cuda_stream);
+}
+
+int mlkv_prefill_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix, const int *prefix_of,
+                        const int *prefix_lens, const void *Q, const void *K, const void *V, void *out,
+                        const int *prompt_lens, int s_max, void *cuda_stream)
+{
+    int rc = mlkv::check_layer(c, layer);
+    if (rc != MLKV_OK || (rc = mlkv::check_prefix(c, prefix, prefix_of, prefix_lens)) != MLKV_OK)
+        return rc;
+    if (prefix == c)
+        return fail(MLKV_ERR_INVALID_ARG, "a prompt's prefix must lie in another cache: its own keeps the prompt");
+    return prefill_impl(c, layer, Q, K, V, out, prompt_lens, s_max, 0, 0, cuda_stream, prefix, prefix_of,
+                        prefix_lens);
 }
 
 int mlkv_decode_block_fused(mlkv_cache_t c, int owner_layer, const void *Q, void *out,

@@ -117,6 +117,11 @@ struct PrefillCall {
     bool direct;
     const CUtensorMap *tmap_kv; // the cache in boxes of 128 positions; only without direct
     int window, sinks;          // window 0: every earlier position is visible
+    // a shared prefix in front of every prompt: its cache's map of 128-position boxes and sequences, each
+    // prompt's prefix (-1: none) and positions of it; NULL map: none
+    const CUtensorMap *tmap_prefix;
+    int prefix_b;
+    const int *prefix_of, *prefix_len;
 };
 int issue_prefill(const PrefillCall &a, cudaStream_t stream);
 // The checks of a prompt's sizes, lengths, queries and outputs shared by the prefill calls.

@@ -139,7 +139,7 @@ constexpr int kFusedMaxChunks = 256;
 constexpr int kFusedMaxBlocks = 64;
 constexpr int kPrefillMaxHeads = 256;    // sel has 8 bits
 constexpr int kPrefillMaxBlocks = 1 << 14;
-struct PrefillParams {
+struct PrefillCommon {
     __nv_bfloat16 *out;       // [b][s_max][h][D]
     int *err;                 // device error word
     float scale_log2;         // log2(e) / sqrt(D)
@@ -170,8 +170,34 @@ struct PrefillParams {
     // its device-mapped address): each unit loads its rows with plain loads, not the tensor map.
     const __nv_bfloat16 *q_host;
     int prompt_len[MLKV_MAX_BATCH];
+};
+struct PrefillParams : PrefillCommon {
     uint32_t units[kPrefillMaxUnits];
 };
+
+// The same kernel over a shared prefix (a cache of its own, read through tmap_p).
+// Prefill: a unit's key tiles are those of its sequence's prefix (prefix_of, -1: none; prefix_len positions),
+//   which every query sees, then the prompt's own.
+// Decode (fused): a unit is the queries of up to two tiles of the sequences that share prefix `beta`, over
+//   chunk `chunk` of its positions (prompt_len[beta] of them); block `blk` of the unit word counts those pairs
+//   of tiles.  Sequences are packed: those of prefix x are places group_at[x] .. + group_n[x] of Q
+//   [places][h][D].  fused_L is the places in all, fused_L1 the sequences of a tile.  Records (o, lse) go to
+//   part [place][g][fused_cmax][G][D] and part_lse [place][g][fused_cmax][G].
+constexpr int kPrefixMaxUnits = 4096;
+struct SharedPrefillParams : PrefillCommon {
+    CUtensorMap tmap_p;
+    int prefix_b;                              // sequences of the prefix cache
+    union {
+        struct {                               // decode, by prefix
+            uint16_t group_at[MLKV_MAX_BATCH], group_n[MLKV_MAX_BATCH];
+        };
+        int16_t prefix_of[MLKV_MAX_BATCH];     // prefill, by sequence
+    };
+    int prefix_len[MLKV_MAX_BATCH];            // prefill, by sequence
+    uint32_t units[kPrefixMaxUnits];
+};
+static_assert(sizeof(SharedPrefillParams) + 3 * sizeof(CUtensorMap) < 32764, "kernel parameters");
+
 
 // Dynamic shared memory of the prefill kernel; sets its limit (once per device); launches it with
 // programmatic dependent launch on `stream`.
@@ -187,6 +213,10 @@ cudaError_t prepare_fused(int head_dim, int form);
 cudaError_t launch_fused(int head_dim, int form, const CUtensorMap *tmap_q,
                          const CUtensorMap *tmap_kv, const PrefillParams &p, cudaStream_t stream);
 cudaError_t launch_fused_combine(int head_dim, const PrefillParams &p, cudaStream_t stream);
+// The prefill (fused: the decode) over a shared prefix.
+cudaError_t prepare_shared(int head_dim, bool fused);
+cudaError_t launch_shared(int head_dim, bool fused, const CUtensorMap *tmap_q, const CUtensorMap *tmap_k,
+                          const CUtensorMap *tmap_v, const SharedPrefillParams &p, cudaStream_t stream);
 
 // Copies through device-mapped page-locked host memory (mlkv_stage.cu): up to 4 segments, each a
 // multiple of 16 bytes with 16-byte-aligned ends.

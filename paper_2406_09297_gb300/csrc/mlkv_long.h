@@ -1,0 +1,131 @@
+// Internal interface of the operators for long caches: decode over pieces of a cache (a shared prefix's
+// suffixes, listed blocks, or all positions with their weights), blocks' bounds and their selection,
+// eviction.  Not part of the public ABI.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "mlkv_internal.h"
+
+namespace mlkv {
+
+// Positions of a block, of a tile of the piece kernel, and rows of the cache's 64-position tensor map.
+constexpr int kBlock = MLKV_BLOCK;
+
+// What a piece launch attends to.
+enum : int {
+    kPieceSuffix = 0,   // positions [0, seq_len), merged with a shared prefix's records
+    kPieceBlocks = 1,   // the blocks listed for every (sequence, KV head)
+    kPieceWeights = 2,  // positions [0, seq_len); every score is stored, the merge left to weights_kernel
+};
+
+// Decode attention of one layer in pieces: a segment (sequence, KV head) of nt tiles of 64 positions is cut
+// into pieces of `tiles` tiles, a CTA each.  Passed by value.
+struct PieceParams {
+    const __nv_bfloat16 *Q;   // [b][h][D]
+    __nv_bfloat16 *out;       // [b][h][D]
+    float *part_o;            // [pieces][G][D]  normalised outputs of pieces
+    float *part_lse;          // [pieces][G]     log2 of their sums, -inf for an empty piece
+    unsigned *counters;       // [b*g]           pieces finished per segment; zero between launches
+    int *err;
+    float scale_log2;         // log2(e) / sqrt(D)
+    int b, h, g, G, slot;
+    int tiles;                // of a piece
+    // kPieceSuffix: records of the shared prefix, [place][g][pre_chunks][G][D] and [place][g][pre_chunks][G]
+    // with place = pre_place[beta] (below); 0 chunks: none
+    const float *pre_o, *pre_lse;
+    int pre_chunks;
+    int early;                // the stream's previous kernel is this call's prefix kernel, which writes
+                              // neither Q nor the cache and has itself waited for all before it: Q and
+                              // the tiles are read before the dependency wait
+    // kPieceBlocks: block numbers [b][g][n_blocks]; others than those of visible positions are passed over
+    const int *blocks;
+    int n_blocks;
+    // kPieceWeights: scores times log2(e) / sqrt(D), [b][h][score_stride]
+    float *scores;
+    long long score_stride;
+    int seq_len[MLKV_MAX_BATCH];
+    int first[MLKV_MAX_BATCH + 1];        // first piece of sequence beta (KV head after KV head inside)
+    uint16_t pre_place[MLKV_MAX_BATCH];   // kPieceSuffix: place of the sequence in the prefix's records
+    uint16_t pre_n[MLKV_MAX_BATCH];       // and their number
+};
+// Most records (pieces and a prefix's) that a segment's merge holds the weights of.
+int piece_max_records(int head_dim, int group);
+int piece_warps(int head_dim);   // consumer warps: tiles of a piece that are worked on at a time
+cudaError_t prepare_pieces(int head_dim, int mode, int *ctas_per_sm);
+cudaError_t launch_pieces(int head_dim, int mode, const CUtensorMap *tmap, const PieceParams &p,
+                          cudaStream_t stream);
+
+// Largest group of segments' records that launch_weights' shared memory holds.
+constexpr int kWeightsMaxRecords = 700;   // (700 + 1) * 16 heads * 4 bytes < 48 KB
+
+// Packs the queries of places [0, n): place i is sequence seq[i].
+struct PackParams {
+    const __nv_bfloat16 *Q;
+    __nv_bfloat16 *packed;
+    int n, row_vecs;           // 16-byte vectors of a sequence's queries
+    uint16_t seq[MLKV_MAX_BATCH];
+};
+cudaError_t launch_pack(const PackParams &p, cudaStream_t stream);
+
+// The merge of a kPieceWeights launch's pieces, and what every position got: out, and
+// weights_out[beta][j][u] = weights_in[beta][j][u] + sum over the heads of the group.
+struct WeightsParams {
+    const float *weights_in;   // [b][g][max_seq] or nullptr: zeros
+    float *weights_out;        // [b][g][max_seq]
+    int max_seq;
+    int chunk;                 // positions of a CTA
+    int ctas;                  // of a segment: one for the merge, then those of its positions
+};
+cudaError_t launch_weights(int head_dim, const PieceParams &p, const WeightsParams &w, int max_len,
+                           cudaStream_t stream);
+
+struct BoundsParams {
+    const __nv_bfloat16 *K;    // [b][g][max_seq][D], the slot's keys
+    int8_t *bounds;            // [b][g][n_blocks][2][D]
+    float *scales;             // [b][g][n_blocks]
+    int b, g, max_seq, n_blocks;
+    unsigned ctas;             // of a segment: blocks of the sequence with most new ones
+    int seq_len[MLKV_MAX_BATCH];
+    int first[MLKV_MAX_BATCH]; // first position that is new
+};
+cudaError_t launch_bounds(int head_dim, const BoundsParams &p, cudaStream_t stream);
+
+struct SelectParams {
+    const __nv_bfloat16 *Q;    // [b][h][D]
+    const int8_t *bounds;
+    const float *scales;
+    int *blocks;               // [b][g][n_select]
+    int b, h, g, G, n_blocks, n_select, n_first, n_last;
+    int seq_len[MLKV_MAX_BATCH];
+};
+// Most blocks of a sequence that a selection handles.
+int select_max_blocks();
+cudaError_t prepare_select(int head_dim);
+cudaError_t launch_select(int head_dim, const SelectParams &p, int max_blocks, cudaStream_t stream);
+
+struct EvictParams {
+    const __nv_bfloat16 *src;  // the slots: [2][b][g][src_seq][D]
+    __nv_bfloat16 *dst;        // [2][b][g][dst_seq][D]
+    const float *weights_in;   // [b][g][src_seq]
+    float *weights_out;        // [b][g][dst_seq]
+    int *kept;                 // [b][g][k_max]
+    unsigned *flags;           // [b][g][units] units whose rows have been read, then the ticket
+    int *err;
+    int b, g, src_seq, dst_seq, k_max, recent;
+    int in_place;              // the slots or the weights are the same memory
+    int same;                  // both are: rows that stay where they are need no store
+    int units;                 // of a segment: ceil(k_max / rows of a unit), and one for the tail
+    int seq_len[MLKV_MAX_BATCH];
+    int keep[MLKV_MAX_BATCH];
+};
+// Units of a segment of k_max kept positions; flags that a launch needs for `segments` of them.
+int evict_units(int head_dim, int k_max);
+inline size_t evict_flags(long long segments, int units) { return static_cast<size_t>(segments) * units + 1; }
+cudaError_t prepare_evict();
+cudaError_t launch_evict(int head_dim, const EvictParams &p, int max_len, int sm_count, cudaStream_t stream);
+
+}  // namespace mlkv

@@ -1,0 +1,610 @@
+// Host side of the operators for long caches: decode over a shared prefix, blocks' bounds, their selection and
+// the decode over listed blocks, decode that adds up attention weights, eviction by them.  Argument checks,
+// the split of the work, launches.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "mlkv_cache.h"
+#include "mlkv_long.h"
+
+using mlkv::aligned16;
+using mlkv::check_layer;
+using mlkv::check_seq_lens;
+using mlkv::DeviceGuard;
+using mlkv::driver_entry;
+using mlkv::EncodeTiledFn;
+using mlkv::fail;
+using mlkv::fail_cuda;
+using mlkv::overlap;
+
+namespace {
+
+// Bits of mlkv_cache::long_ready.
+enum : unsigned { kReadyPieces = 1, kReadySelect = 8, kReadyEvict = 16, kReadyShared = 32 };   // pieces: 3 bits
+
+bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+size_t query_bytes(const mlkv_cache *c) { return static_cast<size_t>(c->b) * c->h * c->d * 2; }
+
+int check_queries(const mlkv_cache *c, const void *Q, const void *out)
+{
+    if (Q == nullptr || out == nullptr || !aligned16(Q) || !aligned16(out))
+        return fail(MLKV_ERR_INVALID_ARG, "Q and out must be non-NULL and 16-byte aligned");
+    if (overlap(Q, query_bytes(c), out, query_bytes(c)))
+        return fail(MLKV_ERR_INVALID_ARG, "out overlaps Q");
+    return MLKV_OK;
+}
+
+const CUtensorMap *rows64(const mlkv_cache *c) { return &c->variants.front().tmap_rows; }
+
+int prepare_pieces(mlkv_cache *c, int mode)
+{
+    const unsigned bit = kReadyPieces << mode;
+    if (c->long_ready & bit)
+        return MLKV_OK;
+    const cudaError_t e = mlkv::prepare_pieces(c->d, mode, &c->piece_ctas);
+    if (e != cudaSuccess)
+        return fail_cuda(e, "preparing the piece kernel");
+    if (c->piece_ctas < 1)
+        return fail(MLKV_ERR_CUDA, "the piece kernel cannot be resident");
+    c->long_ready |= bit;
+    return MLKV_OK;
+}
+
+// Cuts the segments, nt(beta) tiles each, into pieces: fills p.tiles and p.first.  Up to 32 tiles a resident CTA
+// one piece each; beyond that four, so that the last ones to end are short (a record is 1% of 16 tiles).  Never
+// more pieces than there are records, nor of a segment than `most`, nor less than a tile a consumer warp.
+template <typename Tiles>
+void cut(const mlkv_cache *c, mlkv::PieceParams &p, int most, const Tiles &nt)
+{
+    long long total = 0;
+    int longest = 0;
+    for (int beta = 0; beta < c->b; ++beta) {
+        total += nt(beta);
+        longest = std::max(longest, nt(beta));
+    }
+    total *= c->g;
+    const long long slots = static_cast<long long>(c->piece_ctas) * c->sm_count;
+    const long long want = std::min(c->records, total <= 32 * slots ? slots : 4 * slots);
+    int tiles = static_cast<int>(std::max<long long>(mlkv::piece_warps(c->d), (total + want - 1) / want));
+    tiles = std::max(tiles, (longest + most - 1) / most);
+    for (;; tiles += (tiles + 7) / 8) {
+        long long n = 0;
+        for (int beta = 0; beta < c->b; ++beta)
+            n += (nt(beta) + tiles - 1) / tiles;
+        if (n * c->g <= want || tiles >= longest)
+            break;
+    }
+    p.tiles = tiles;
+    long long at = 0;
+    for (int beta = 0; beta < c->b; ++beta) {
+        p.first[beta] = static_cast<int>(at);
+        at += static_cast<long long>(c->g) * ((nt(beta) + tiles - 1) / tiles);
+    }
+    p.first[c->b] = static_cast<int>(at);
+}
+
+void fill_pieces(const mlkv_cache *c, int layer, const void *Q, void *out, const int *seq_lens,
+                 mlkv::PieceParams &p)
+{
+    p.Q = static_cast<const __nv_bfloat16 *>(Q);
+    p.out = static_cast<__nv_bfloat16 *>(out);
+    p.part_o = c->part_o;
+    p.part_lse = c->part_lse;
+    p.counters = c->counters;
+    p.err = c->err;
+    p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(c->d)));
+    p.b = c->b;
+    p.h = c->h;
+    p.g = c->g;
+    p.G = c->G;
+    p.slot = c->slot[layer];
+    p.pre_o = p.pre_lse = nullptr;
+    p.pre_chunks = p.early = 0;
+    p.blocks = nullptr;
+    p.n_blocks = 0;
+    p.scores = nullptr;
+    p.score_stride = 0;
+    std::memcpy(p.seq_len, seq_lens, sizeof(int) * c->b);
+}
+
+// A stream under capture takes no allocation: scratch that would have to grow is refused there.
+int scratch(mlkv_cache *c, size_t floats, const char *what, cudaStream_t stream)
+{
+    if (floats <= c->fused_part_floats)
+        return MLKV_OK;
+    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(stream, &st) != cudaSuccess || st != cudaStreamCaptureStatusNone) {
+        cudaGetLastError();
+        return fail(MLKV_ERR_UNSUPPORTED, "%s: %zu bytes to allocate while the stream is captured; make this "
+                    "call once outside", what, floats * sizeof(float));
+    }
+    return mlkv::grow_scratch(c, floats, what);
+}
+
+// Key tiles of 128 positions of a unit of the decode over shared prefixes, for `pairs` unit columns (pairs of query
+// tiles times KV heads) over prefixes of n_kt tiles: the least estimated time of ceil(units / SMs) rounds of
+// kc tiles and a start and end worth 3.
+int plan_prefix_chunk(const int *n_kt, const int *pairs, int n, int sm_count)
+{
+    long long work = 0;
+    int longest = 1;
+    for (int x = 0; x < n; ++x) {
+        work += static_cast<long long>(n_kt[x]) * pairs[x];
+        if (pairs[x] > 0)
+            longest = std::max(longest, n_kt[x]);
+    }
+    int best = longest;
+    double best_t = 1e30;
+    const int least = std::max(1, (longest + mlkv::kFusedMaxChunks - 1) / mlkv::kFusedMaxChunks);
+    for (int kc = std::max<long long>(least, work / (4LL * sm_count)); kc <= longest; kc += (kc + 15) / 16) {
+        long long units = 0;
+        for (int x = 0; x < n; ++x)
+            units += static_cast<long long>((n_kt[x] + kc - 1) / kc) * pairs[x];
+        const double t = static_cast<double>((units + sm_count - 1) / sm_count) * (kc + 3);
+        if (t < best_t) {
+            best_t = t;
+            best = kc;
+        }
+    }
+    return best;
+}
+
+}  // namespace
+
+int mlkv::check_same_model(const mlkv_cache *c, const mlkv_cache *other, const char *what)
+{
+    if (other == nullptr)
+        return fail(MLKV_ERR_INVALID_ARG, "null %s handle", what);
+    if (other->l != c->l || other->h != c->h || other->d != c->d || other->g != c->g ||
+        other->owner != c->owner)
+        return fail(MLKV_ERR_MAP, "the %s has other layers or heads", what);
+    if (other->device != c->device)
+        return fail(MLKV_ERR_INVALID_ARG, "the %s lies on another device", what);
+    return MLKV_OK;
+}
+
+int mlkv::check_prefix(const mlkv_cache *c, const mlkv_cache *prefix, const int *prefix_of,
+                       const int *prefix_lens)
+{
+    const int rc = check_same_model(c, prefix, "prefix cache");
+    if (rc != MLKV_OK)
+        return rc;
+    if (prefix_of == nullptr || prefix_lens == nullptr)
+        return fail(MLKV_ERR_INVALID_ARG, "prefix_of and prefix_lens must be non-NULL");
+    for (int beta = 0; beta < c->b; ++beta)
+        if (prefix_of[beta] < -1 || prefix_of[beta] >= prefix->b)
+            return fail(MLKV_ERR_RANGE, "prefix_of[%d] = %d outside [-1, %d)", beta, prefix_of[beta], prefix->b);
+    for (int x = 0; x < prefix->b; ++x)
+        if (prefix_lens[x] < 0 || prefix_lens[x] > prefix->max_seq)
+            return fail(MLKV_ERR_RANGE, "prefix_lens[%d] = %d outside [0, %d]", x, prefix_lens[x],
+                        prefix->max_seq);
+    return MLKV_OK;
+}
+
+extern "C" {
+
+int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix, const int *prefix_of,
+                                 const int *prefix_lens, const void *Q, void *out, const int *seq_lens,
+                                 void *cuda_stream)
+{
+    int rc = check_layer(c, layer);
+    if (rc != MLKV_OK || (rc = mlkv::check_prefix(c, prefix, prefix_of, prefix_lens)) != MLKV_OK ||
+        (rc = check_queries(c, Q, out)) != MLKV_OK || (rc = check_seq_lens(c, seq_lens)) != MLKV_OK)
+        return rc;
+    if (c->g > 255)
+        return fail(MLKV_ERR_UNSUPPORTED, "the decode over a shared prefix handles at most 255 KV heads");
+    DeviceGuard guard(c->device);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if ((rc = prepare_pieces(c, mlkv::kPieceSuffix)) != MLKV_OK)
+        return rc;
+    static thread_local mlkv::PieceParams p;
+    static thread_local mlkv::SharedPrefillParams u;
+    static thread_local mlkv::PackParams pack;
+    fill_pieces(c, layer, Q, out, seq_lens, p);
+    // Places: the sequences of prefix 0, then those of prefix 1, ...  Where every prefix's sequences are
+    // neighbours already, a sequence's place is its own number and Q stays as it is.
+    const int L1 = 128 / c->G, np = prefix->b;
+    static thread_local int n_kt[MLKV_MAX_BATCH], pairs[MLKV_MAX_BATCH];
+    std::fill(u.group_n, u.group_n + np, static_cast<uint16_t>(0));
+    auto of = [&](int beta) { return prefix_of[beta] >= 0 && prefix_lens[prefix_of[beta]] > 0 ? prefix_of[beta] : -1; };
+    bool neighbours = true;
+    int places = 0;
+    for (int beta = 0; beta < c->b; ++beta) {
+        const int x = of(beta);
+        if (x < 0)
+            continue;
+        ++places;
+        if (u.group_n[x]++ == 0)
+            u.group_at[x] = static_cast<uint16_t>(beta);
+        else
+            neighbours = neighbours && of(beta - 1) == x;
+    }
+    if (neighbours) {
+        for (int beta = 0; beta < c->b; ++beta)
+            p.pre_place[beta] = static_cast<uint16_t>(beta);
+        places = c->b;
+    } else {
+        int at = 0;
+        for (int x = 0; x < np; ++x) {
+            u.group_at[x] = static_cast<uint16_t>(at);
+            at += u.group_n[x];
+            u.group_n[x] = 0;
+        }
+        for (int beta = 0; beta < c->b; ++beta)
+            if (of(beta) >= 0) {
+                const int place = u.group_at[of(beta)] + u.group_n[of(beta)]++;
+                p.pre_place[beta] = static_cast<uint16_t>(place);
+                pack.seq[place] = static_cast<uint16_t>(beta);
+            }
+    }
+    int most_kt = 0;
+    for (int x = 0; x < np; ++x) {
+        n_kt[x] = u.group_n[x] > 0 ? (prefix_lens[x] + 127) / 128 : 0;
+        pairs[x] = (u.group_n[x] + 2 * L1 - 1) / (2 * L1) * c->g;
+        most_kt = std::max(most_kt, n_kt[x]);
+    }
+    int cmax = 0;
+    if (most_kt > 0) {
+        if (!(c->long_ready & kReadyShared)) {
+            const cudaError_t e = mlkv::prepare_shared(c->d, true);
+            if (e != cudaSuccess)
+                return fail_cuda(e, "preparing the decode over a shared prefix");
+            c->long_ready |= kReadyShared;
+        }
+        const int kc = plan_prefix_chunk(n_kt, pairs, np, c->sm_count);
+        cmax = (most_kt + kc - 1) / kc;
+        const size_t rows = static_cast<size_t>(places) * c->g * cmax * c->G;
+        const size_t packed = neighbours ? 0 : static_cast<size_t>(places) * c->h * c->d / 2;   // in floats
+        if ((rc = scratch(c, rows * (c->d + 1) + packed + 4, "records of the shared prefix", stream)) != MLKV_OK)
+            return rc;
+        const void *q_in = Q;
+        if (!neighbours) {
+            pack.Q = static_cast<const __nv_bfloat16 *>(Q);
+            pack.packed = reinterpret_cast<__nv_bfloat16 *>(c->fused_part);
+            pack.n = places;
+            pack.row_vecs = c->h * c->d / 8;
+            const cudaError_t e = mlkv::launch_pack(pack, stream);
+            if (e != cudaSuccess)
+                return fail_cuda(e, "query pack launch");
+            q_in = c->fused_part;
+        }
+        u.part = c->fused_part + packed;
+        u.part_lse = u.part + rows * c->d;
+        p.pre_o = u.part;
+        p.pre_lse = u.part_lse;
+        p.pre_chunks = cmax;
+        p.early = 1;
+        // The packed queries [places][h][D] as (channel, head in group, group, 1, place): a box of 64 channels x
+        // G heads x min(L1, places) places is a tile's rows.
+        static EncodeTiledFn encode = driver_entry<EncodeTiledFn>("cuTensorMapEncodeTiled");
+        if (encode == nullptr)
+            return fail(MLKV_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable from the driver");
+        CUtensorMap tmap_q;
+        const cuuint64_t row = static_cast<cuuint64_t>(c->h) * c->d * 2;
+        const cuuint64_t dims[5] = {static_cast<cuuint64_t>(c->d), static_cast<cuuint64_t>(c->G),
+                                    static_cast<cuuint64_t>(c->g), 1u, static_cast<cuuint64_t>(places)};
+        const cuuint64_t strides[4] = {static_cast<cuuint64_t>(c->d) * 2,
+                                       static_cast<cuuint64_t>(c->G) * c->d * 2, row, row};
+        const cuuint32_t box[5] = {64u, static_cast<cuuint32_t>(c->G), 1u, 1u,
+                                   static_cast<cuuint32_t>(std::min(L1, places))};
+        const cuuint32_t estr[5] = {1u, 1u, 1u, 1u, 1u};
+        const CUresult r = encode(&tmap_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(q_in), dims,
+                                  strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        if (r != CUDA_SUCCESS)
+            return fail(MLKV_ERR_CUDA, "cuTensorMapEncodeTiled(packed Q) failed (CUresult %d)",
+                        static_cast<int>(r));
+        const CUtensorMap *tmap_kv = nullptr;
+        for (auto &v : prefix->variants)
+            if (v.v->tile_tokens == 128)
+                tmap_kv = &v.tmap;
+        if (tmap_kv == nullptr)
+            return fail(MLKV_ERR_UNSUPPORTED, "no 128-position cache map for d=%d", c->d);
+        u.tmap_p = *tmap_kv;
+        u.out = nullptr;
+        u.err = c->err;
+        u.scale_log2 = p.scale_log2;
+        u.b = c->b;
+        u.h = c->h;
+        u.g = c->g;
+        u.G = c->G;
+        u.s_max = prefix->max_seq;
+        u.slot = p.slot;
+        u.head_pairs = 0;
+        u.sm_count = c->sm_count;
+        u.window = u.sinks = 0;
+        u.kv_direct = 0;
+        u.fused_L = places;
+        u.fused_L1 = L1;
+        u.fused_nblk = 1;
+        u.fused_kc = kc;
+        u.fused_cmax = cmax;
+        u.fused_early = 0;
+        u.fused_combine_w = 1;
+        u.q_host = nullptr;
+        u.prefix_b = np;
+        std::memcpy(u.prompt_len, prefix_lens, sizeof(int) * np);
+        int n = 0;
+        auto issue = [&]() {
+            u.n_units = n;
+            n = 0;
+            return mlkv::launch_shared(c->d, true, &tmap_q, tmap_kv, tmap_kv, u, stream);
+        };
+        for (int x = 0; x < np; ++x) {
+            const int nblk = (u.group_n[x] + 2 * L1 - 1) / (2 * L1);
+            for (int j = 0; j < c->g && n_kt[x] > 0; ++j)
+                for (int ch = 0; ch * kc < n_kt[x]; ++ch)
+                    for (int blk = 0; blk < nblk; ++blk) {   // neighbours read the same tiles
+                        u.units[n] = static_cast<uint32_t>(x) | (static_cast<uint32_t>(ch) << 10) |
+                                     (static_cast<uint32_t>(blk) << 18) | (static_cast<uint32_t>(j) << 24);
+                        if (++n == mlkv::kPrefixMaxUnits) {
+                            const cudaError_t e = issue();
+                            if (e != cudaSuccess)
+                                return fail_cuda(e, "shared prefix launch");
+                        }
+                    }
+        }
+        if (n > 0) {
+            const cudaError_t e = issue();
+            if (e != cudaSuccess)
+                return fail_cuda(e, "shared prefix launch");
+        }
+        for (int beta = 0; beta < c->b; ++beta) {
+            const int x = of(beta);
+            p.pre_n[beta] = static_cast<uint16_t>(x < 0 ? 0 : (n_kt[x] + kc - 1) / kc);
+        }
+    } else {
+        std::fill(p.pre_n, p.pre_n + c->b, static_cast<uint16_t>(0));
+    }
+    cut(c, p, mlkv::piece_max_records(c->d, c->G) - cmax,
+        [&](int beta) { return static_cast<int>((static_cast<unsigned>(seq_lens[beta]) + 63) / 64); });
+    const cudaError_t e = mlkv::launch_pieces(c->d, mlkv::kPieceSuffix, rows64(c), p, stream);
+    return e == cudaSuccess ? MLKV_OK : fail_cuda(e, "suffix decode launch");
+}
+
+int mlkv_block_bounds(mlkv_cache_t c, int layer, const int *first, const int *seq_lens, void *bounds,
+                      float *scales, void *cuda_stream)
+{
+    int rc = check_layer(c, layer);
+    if (rc != MLKV_OK)
+        return rc;
+    if (c->owner[layer] != layer)
+        return MLKV_OK;   // its owner's bounds are these
+    if ((rc = check_seq_lens(c, seq_lens)) != MLKV_OK)
+        return rc;
+    if (bounds == nullptr || scales == nullptr || !aligned16(bounds) || !aligned4(scales))
+        return fail(MLKV_ERR_INVALID_ARG, "bounds must be 16-byte and scales 4-byte aligned, neither NULL");
+    static thread_local mlkv::BoundsParams p;
+    p.n_blocks = static_cast<int>((static_cast<unsigned>(c->max_seq) + 63) / 64);
+    const size_t blocks = static_cast<size_t>(c->b) * c->g * p.n_blocks;
+    if (overlap(bounds, blocks * 2 * c->d, scales, blocks * 4))
+        return fail(MLKV_ERR_INVALID_ARG, "bounds overlap scales");
+    long long most = 0;
+    for (int beta = 0; beta < c->b; ++beta) {
+        const int f = first != nullptr ? first[beta] : 0;
+        if (f < 0 || f > seq_lens[beta])
+            return fail(MLKV_ERR_RANGE, "first[%d] = %d outside [0, %d]", beta, f, seq_lens[beta]);
+        p.seq_len[beta] = seq_lens[beta];
+        p.first[beta] = f;
+        most = std::max(most, (static_cast<long long>(seq_lens[beta]) + 63) / 64 - f / 64);
+    }
+    if (most == 0)
+        return MLKV_OK;
+    if (most * c->b * c->g > 0x7fffffffLL)
+        return fail(MLKV_ERR_UNSUPPORTED, "%lld blocks exceed a launch", most * c->b * c->g);
+    const size_t slot = c->cache_bytes / c->m;
+    p.K = reinterpret_cast<const __nv_bfloat16 *>(static_cast<char *>(c->cache) + slot * c->slot[layer]);
+    p.bounds = static_cast<int8_t *>(bounds);
+    p.scales = scales;
+    p.b = c->b;
+    p.g = c->g;
+    p.max_seq = c->max_seq;
+    p.ctas = static_cast<unsigned>(most);
+    DeviceGuard guard(c->device);
+    const cudaError_t e = mlkv::launch_bounds(c->d, p, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? MLKV_OK : fail_cuda(e, "block bounds launch");
+}
+
+int mlkv_select_blocks(mlkv_cache_t c, int layer, const void *Q, const void *bounds, const float *scales,
+                       const int *seq_lens, int n_select, int n_first, int n_last, int *blocks,
+                       void *cuda_stream)
+{
+    int rc = check_layer(c, layer);
+    if (rc != MLKV_OK)
+        return rc;
+    if (Q == nullptr || !aligned16(Q) || bounds == nullptr || !aligned16(bounds) || scales == nullptr ||
+        !aligned4(scales) || blocks == nullptr || !aligned4(blocks))
+        return fail(MLKV_ERR_INVALID_ARG, "Q and bounds must be 16-byte, scales and blocks 4-byte aligned, none NULL");
+    if ((rc = check_seq_lens(c, seq_lens)) != MLKV_OK)
+        return rc;
+    if (n_select < 1 || n_first < 0 || n_last < 0 || n_first > n_select - n_last)
+        return fail(MLKV_ERR_INVALID_ARG, "%d blocks cannot hold the %d first and the %d last ones", n_select,
+                    n_first, n_last);
+    static thread_local mlkv::SelectParams p;
+    p.n_blocks = static_cast<int>((static_cast<unsigned>(c->max_seq) + 63) / 64);
+    const size_t n = static_cast<size_t>(c->b) * c->g, out_bytes = n * n_select * 4;
+    if (overlap(blocks, out_bytes, Q, query_bytes(c)) ||
+        overlap(blocks, out_bytes, bounds, n * p.n_blocks * 2 * c->d) ||
+        overlap(blocks, out_bytes, scales, n * p.n_blocks * 4))
+        return fail(MLKV_ERR_INVALID_ARG, "blocks overlap an input");
+    int most = 0;
+    for (int beta = 0; beta < c->b; ++beta) {
+        p.seq_len[beta] = seq_lens[beta];
+        most = std::max(most, static_cast<int>((static_cast<unsigned>(seq_lens[beta]) + 63) / 64));
+    }
+    if (most > mlkv::select_max_blocks())
+        return fail(MLKV_ERR_UNSUPPORTED, "%d blocks of a sequence: a selection handles %d", most,
+                    mlkv::select_max_blocks());
+    if (n > (1u << 24))
+        return fail(MLKV_ERR_UNSUPPORTED, "%zu KV heads exceed a launch", n);
+    p.Q = static_cast<const __nv_bfloat16 *>(Q);
+    p.bounds = static_cast<const int8_t *>(bounds);
+    p.scales = scales;
+    p.blocks = blocks;
+    p.b = c->b;
+    p.h = c->h;
+    p.g = c->g;
+    p.G = c->G;
+    p.n_select = n_select;
+    p.n_first = n_first;
+    p.n_last = n_last;
+    DeviceGuard guard(c->device);
+    cudaError_t e = cudaSuccess;
+    if (!(c->long_ready & kReadySelect) && (e = mlkv::prepare_select(c->d)) == cudaSuccess)
+        c->long_ready |= kReadySelect;
+    if (e == cudaSuccess)
+        e = mlkv::launch_select(c->d, p, most, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? MLKV_OK : fail_cuda(e, "block selection launch");
+}
+
+int mlkv_decode_attention_blocks(mlkv_cache_t c, int layer, const void *Q, void *out, const int *seq_lens,
+                                 const int *blocks, int n_blocks, void *cuda_stream)
+{
+    int rc = check_layer(c, layer);
+    if (rc != MLKV_OK || (rc = check_queries(c, Q, out)) != MLKV_OK ||
+        (rc = check_seq_lens(c, seq_lens)) != MLKV_OK)
+        return rc;
+    if (blocks == nullptr || !aligned4(blocks) || n_blocks < 1)
+        return fail(MLKV_ERR_INVALID_ARG, "blocks must be non-NULL and 4-byte aligned, at least one");
+    const size_t segments = static_cast<size_t>(c->b) * c->g;
+    if (overlap(blocks, segments * n_blocks * 4, out, query_bytes(c)))
+        return fail(MLKV_ERR_INVALID_ARG, "out overlaps blocks");
+    if (segments * static_cast<size_t>(n_blocks) > 0x7fffffffu)
+        return fail(MLKV_ERR_UNSUPPORTED, "%zu listed blocks exceed the int32 indices", segments * n_blocks);
+    DeviceGuard guard(c->device);
+    if ((rc = prepare_pieces(c, mlkv::kPieceBlocks)) != MLKV_OK)
+        return rc;
+    static thread_local mlkv::PieceParams p;
+    fill_pieces(c, layer, Q, out, seq_lens, p);
+    p.blocks = blocks;
+    p.n_blocks = n_blocks;
+    cut(c, p, mlkv::piece_max_records(c->d, c->G), [&](int) { return n_blocks; });
+    const cudaError_t e = mlkv::launch_pieces(c->d, mlkv::kPieceBlocks, rows64(c), p,
+                                              static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? MLKV_OK : fail_cuda(e, "block decode launch");
+}
+
+int mlkv_decode_attention_weights(mlkv_cache_t c, int layer, const void *Q, void *out, const int *seq_lens,
+                                  const float *weights_in, float *weights_out, void *cuda_stream)
+{
+    int rc = check_layer(c, layer);
+    if (rc != MLKV_OK || (rc = check_queries(c, Q, out)) != MLKV_OK ||
+        (rc = check_seq_lens(c, seq_lens)) != MLKV_OK)
+        return rc;
+    if (weights_out == nullptr || !aligned4(weights_out) || !aligned4(weights_in))
+        return fail(MLKV_ERR_INVALID_ARG, "weights must be 4-byte aligned, weights_out non-NULL");
+    const size_t bytes = static_cast<size_t>(c->b) * c->g * c->max_seq * 4;
+    if ((weights_in != nullptr && weights_in != weights_out && overlap(weights_in, bytes, weights_out, bytes)) ||
+        overlap(weights_out, bytes, out, query_bytes(c)) || overlap(weights_out, bytes, Q, query_bytes(c)) ||
+        (weights_in != nullptr && overlap(weights_in, bytes, out, query_bytes(c))))
+        return fail(MLKV_ERR_INVALID_ARG, "weights_out overlaps another tensor, or out weights_in");
+    DeviceGuard guard(c->device);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if ((rc = prepare_pieces(c, mlkv::kPieceWeights)) != MLKV_OK)
+        return rc;
+    static thread_local mlkv::PieceParams p;
+    fill_pieces(c, layer, Q, out, seq_lens, p);
+    int longest = 0;
+    for (int beta = 0; beta < c->b; ++beta)
+        longest = std::max(longest, seq_lens[beta]);
+    p.score_stride = (static_cast<long long>(longest) + 63) / 64 * 64;
+    if ((rc = scratch(c, static_cast<size_t>(c->b) * c->h * p.score_stride, "scores", stream)) != MLKV_OK)
+        return rc;
+    p.scores = c->fused_part;
+    cut(c, p, mlkv::kWeightsMaxRecords,
+        [&](int beta) { return static_cast<int>((static_cast<unsigned>(seq_lens[beta]) + 63) / 64); });
+    mlkv::WeightsParams w;
+    w.weights_in = weights_in;
+    w.weights_out = weights_out;
+    w.max_seq = c->max_seq;
+    // (in place, what lies behind the longest sequence stays as it is)
+    const long long upto = weights_in == weights_out ? longest : c->max_seq;
+    w.chunk = 1024;
+    const long long segments = static_cast<long long>(c->b) * c->g;
+    while (((upto + w.chunk - 1) / w.chunk + 1) * segments > 0x7fffffffLL)
+        w.chunk *= 2;
+    w.ctas = static_cast<int>((upto + w.chunk - 1) / w.chunk) + 1;
+    cudaError_t e = mlkv::launch_pieces(c->d, mlkv::kPieceWeights, rows64(c), p, stream);
+    if (e != cudaSuccess)
+        return fail_cuda(e, "decode launch");
+    e = mlkv::launch_weights(c->d, p, w, longest, stream);
+    return e == cudaSuccess ? MLKV_OK : fail_cuda(e, "weights launch");
+}
+
+int mlkv_evict(mlkv_cache_t c, mlkv_cache_t to, int layer, const float *weights_in, float *weights_out,
+               const int *seq_lens, const int *keep, int recent, int *kept, int k_max, void *cuda_stream)
+{
+    int rc = check_layer(c, layer);
+    if (rc != MLKV_OK || (rc = mlkv::check_same_model(c, to, "target cache")) != MLKV_OK)
+        return rc;
+    if (to->b != c->b)
+        return fail(MLKV_ERR_MAP, "the target cache holds %d sequences, the cache %d", to->b, c->b);
+    if (c->owner[layer] != layer)
+        return MLKV_OK;   // its owner's positions are these
+    if ((rc = check_seq_lens(c, seq_lens)) != MLKV_OK)
+        return rc;
+    if (weights_in == nullptr || weights_out == nullptr || kept == nullptr || !aligned4(weights_in) ||
+        !aligned4(weights_out) || !aligned4(kept) || keep == nullptr)
+        return fail(MLKV_ERR_INVALID_ARG, "weights and kept must be 4-byte aligned; none, nor keep, may be NULL");
+    if (recent < 0 || k_max < 1)
+        return fail(MLKV_ERR_INVALID_ARG, "recent %d must not be negative, k_max %d be positive", recent, k_max);
+    static thread_local mlkv::EvictParams p;
+    int longest = 0, rows = 0;
+    for (int beta = 0; beta < c->b; ++beta) {
+        if (keep[beta] < 1 || keep[beta] < recent)
+            return fail(MLKV_ERR_INVALID_ARG, "keep[%d] = %d must be positive and hold the %d newest positions",
+                        beta, keep[beta], recent);
+        const int n = std::min(keep[beta], seq_lens[beta]);
+        if (n > to->max_seq || n > k_max)
+            return fail(MLKV_ERR_RANGE, "%d positions of sequence %d exceed k_max %d or the target's %d", n, beta,
+                        k_max, to->max_seq);
+        p.seq_len[beta] = seq_lens[beta];
+        p.keep[beta] = keep[beta];
+        longest = std::max(longest, seq_lens[beta]);
+        rows = std::max(rows, n);
+    }
+    const size_t segments = static_cast<size_t>(c->b) * c->g;
+    const size_t in = segments * c->max_seq * 4, out = segments * to->max_seq * 4, list = segments * k_max * 4;
+    const bool same_w = weights_in == weights_out;
+    if (same_w ? c->max_seq != to->max_seq : overlap(weights_in, in, weights_out, out))
+        return fail(MLKV_ERR_INVALID_ARG, "weights_out overlaps weights_in, or is it with rows of another length");
+    if (overlap(kept, list, weights_in, in) || overlap(kept, list, weights_out, out))
+        return fail(MLKV_ERR_INVALID_ARG, "kept overlaps weights");
+    p.units = mlkv::evict_units(c->d, rows);
+    if (segments * p.units > 0x7fffffffu || segments > (1u << 24))
+        return fail(MLKV_ERR_UNSUPPORTED, "%zu KV heads of %d units exceed a launch", segments, p.units);
+    DeviceGuard guard(c->device);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if ((rc = scratch(c, mlkv::evict_flags(static_cast<long long>(segments), p.units), "flags", stream)) != MLKV_OK)
+        return rc;
+    cudaError_t e = cudaSuccess;
+    if (!(c->long_ready & kReadyEvict) && (e = mlkv::prepare_evict()) == cudaSuccess)
+        c->long_ready |= kReadyEvict;
+    const size_t from_slot = c->cache_bytes / c->m, to_slot = to->cache_bytes / to->m;
+    p.src = reinterpret_cast<const __nv_bfloat16 *>(static_cast<char *>(c->cache) + from_slot * c->slot[layer]);
+    p.dst = reinterpret_cast<__nv_bfloat16 *>(static_cast<char *>(to->cache) + to_slot * to->slot[layer]);
+    p.weights_in = weights_in;
+    p.weights_out = weights_out;
+    p.kept = kept;
+    p.flags = reinterpret_cast<unsigned *>(c->fused_part);
+    p.err = c->err;
+    p.b = c->b;
+    p.g = c->g;
+    p.src_seq = c->max_seq;
+    p.dst_seq = to->max_seq;
+    p.k_max = k_max;
+    p.recent = recent;
+    p.in_place = c == to || same_w ? 1 : 0;
+    p.same = c == to && same_w ? 1 : 0;
+    if (e == cudaSuccess)
+        e = mlkv::launch_evict(c->d, p, longest, c->sm_count, stream);
+    return e == cudaSuccess ? MLKV_OK : fail_cuda(e, "eviction launch");
+}
+
+}  // extern "C"

@@ -1,0 +1,612 @@
+// Decode attention over pieces of a cache for GB300: the common core of three calls.
+//
+//   suffix    a sequence's own positions, merged with the records of a prefix that other sequences share
+//   blocks    the blocks of 64 positions listed for every (sequence, KV head)
+//   weights   all positions, every score stored on the way (weights_kernel turns them into weights)
+//
+// For the G query heads of one KV head, s_u = q k_u log2(e) / sqrt(d), m = max s, o = sum 2^(s_u - m) v_u / l,
+// l = sum 2^(s_u - m), in one pass with a running m (Eqs. 2-3 of arXiv 2406.09297 with the maps of Eqs. 15
+// and 18).  A piece's result is the record (o, m + log2 l); records merge as
+//   o = sum_c 2^(lse_c - M) o_c / sum_c 2^(lse_c - M),   M = max_c lse_c.
+//
+// A CTA is one piece: a producer warp brings tiles of 64 keys and values through a ring by TMA, the
+// consumer warps take the tiles in turn, each a whole tile (S = Q K^T and O += P V by mma.sync m16n8k16, the
+// group's heads as rows), with sums of its own that meet in shared memory at the end.  The CTA that finishes a
+// segment last merges its records, in their order, so that the outputs do not depend on which CTA that is.
+// Bound by the bytes of keys and values: 4 d flops a byte-pair at most 16 rows deep leaves the tensor
+// cores idle; two CTAs an SM keep 192 KB in flight, three times what the latency of HBM needs.
+#include "mlkv_device.cuh"
+#include "mlkv_long.h"
+
+namespace mlkv {
+namespace {
+
+constexpr int T = kBlock;
+
+template <int D>
+struct PiecePlan {
+    static constexpr int kTile = T * D * 2;            // K or V of a tile
+    static constexpr int kStages = D == 64 ? 6 : 3;
+    // Consumer warps: one a stage.  (A stage's barrier tells two of its phases apart, so whoever waits for one has
+    // to have seen the one before.)
+    static constexpr int kWarps = kStages;
+    static constexpr int kThreads = (kWarps + 1) * 32;
+    static constexpr int kBars = kStages * 2 * kTile;  // full[], empty[]
+    static constexpr int kML = kBars + 2 * 8 * kStages;   // float [kWarps][2][16]
+    static constexpr int kFlag = kML + kWarps * 2 * 16 * 4;
+    static constexpr int kBytes = kFlag + 16;
+    static constexpr int kRow = D + 4;                 // floats of a row of a warp's sums
+    static_assert(kWarps * 16 * kRow * 4 <= kBars, "sums fit in the ring");
+    static_assert(2 * (kBytes + 1024) <= 228 * 1024, "two CTAs an SM");
+};
+
+// Room for merge weights, in the ring.
+template <int D>
+constexpr int max_records(int G)
+{
+    return PiecePlan<D>::kBars / (4 * G);
+}
+
+__device__ __forceinline__ float neg_inf() { return -__int_as_float(0x7f800000); }
+
+struct Piece {
+    int beta, j, seg, index, count, t0, t1, L;
+};
+
+template <int kMode>
+__device__ __forceinline__ Piece piece_of(const PieceParams &p)
+{
+    Piece x;
+    const int c = static_cast<int>(blockIdx.x);
+    int lo = 0, hi = p.b - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.first[mid] <= c)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    x.beta = lo;
+    x.L = p.seq_len[lo];
+    const int nt = kMode == kPieceBlocks ? p.n_blocks : (x.L + T - 1) / T;
+    x.count = (nt + p.tiles - 1) / p.tiles;
+    const int rel = c - p.first[lo];
+    x.j = rel / x.count;
+    x.index = rel - x.j * x.count;
+    x.seg = lo * p.g + x.j;
+    x.t0 = x.index * p.tiles;
+    x.t1 = min(nt, x.t0 + p.tiles);
+    return x;
+}
+
+// Merges the segment's records (its own pieces', from own0 on, then the prefix's n_pre) into out: the weights
+// first, then the sums in the records' order.  s_w: room for a row of G floats a record, and one more.
+template <int D>
+__device__ void merge_records(const PieceParams &p, const Piece &x, size_t own0, int n_pre, float *s_w,
+                              int tid, int n_threads)
+{
+    const int G = p.G, n_own = x.count, n = n_own + n_pre;
+    const size_t pre0 =
+        n_pre > 0 ? (static_cast<size_t>(p.pre_place[x.beta]) * p.g + x.j) * p.pre_chunks : 0;
+    for (int i = tid; i < n * G; i += n_threads)
+        s_w[i] = i < n_own * G ? __ldcg(p.part_lse + own0 * G + i)
+                               : __ldcg(p.pre_lse + pre0 * G + (i - n_own * G));
+    asm volatile("bar.sync 1, %0;" ::"r"(n_threads) : "memory");
+    if (tid < G) {
+        float mx = neg_inf();
+        for (int k = 0; k < n; ++k)
+            mx = fmaxf(mx, s_w[k * G + tid]);
+        float tot = 0.f;
+        for (int k = 0; k < n; ++k) {
+            // (a NaN of a record goes on into the sum; without anything visible every weight is 0)
+            const float lse = s_w[k * G + tid];
+            const float w = lse == neg_inf() ? 0.f : fast_exp2(lse - mx);
+            s_w[k * G + tid] = w;
+            tot += w;
+        }
+        s_w[n * G + tid] = tot == 0.f ? 0.f : 1.f / tot;
+    }
+    asm volatile("bar.sync 1, %0;" ::"r"(n_threads) : "memory");
+    __nv_bfloat16 *ob = p.out + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * G) * D;
+    for (int i = tid * 4; i < G * D; i += n_threads * 4) {
+        const int row = i / D;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        constexpr int U = 8;
+        for (int k0 = 0; k0 < n; k0 += U) {
+            float4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int k = k0 + u;
+                const float *rec = k < n_own ? p.part_o + (own0 + k) * G * D
+                                             : p.pre_o + (pre0 + (k - n_own)) * G * D;
+                v[u] = k < n ? __ldcg(reinterpret_cast<const float4 *>(rec + i))
+                             : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int k = k0 + u;
+                const float w = k < n ? s_w[k * G + row] : 0.f;
+                if (w != 0.f) {
+                    acc.x = fmaf(w, v[u].x, acc.x);
+                    acc.y = fmaf(w, v[u].y, acc.y);
+                    acc.z = fmaf(w, v[u].z, acc.z);
+                    acc.w = fmaf(w, v[u].w, acc.w);
+                }
+            }
+        }
+        const float inv = s_w[n * G + row];
+        uint2 w2;
+        w2.x = pack_bf16x2(acc.x * inv, acc.y * inv);
+        w2.y = pack_bf16x2(acc.z * inv, acc.w * inv);
+        *reinterpret_cast<uint2 *>(ob + i) = w2;
+    }
+}
+
+template <int D, int kMode>
+__global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
+    piece_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ PieceParams p)
+{
+    using PL = PiecePlan<D>;
+    constexpr int S = PL::kStages, kWarps = PL::kWarps;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t sbase = smem_addr(smem);
+    const uint32_t bar_full = sbase + PL::kBars, bar_empty = bar_full + 8 * S;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int *flag = reinterpret_cast<volatile int *>(smem + PL::kFlag);
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) {
+            mbar_init(bar_full + 8 * s, 1);
+            mbar_init(bar_empty + 8 * s, 1);
+        }
+        flag[0] = 0;   // a wait gave up
+        fence_barrier_init();
+    }
+    if (threadIdx.x == kWarps * 32)
+        prefetch_tensormap(&tmap);
+    __syncthreads();
+    const bool early = kMode == kPieceSuffix && p.early;
+    if (!early)
+        grid_dependency_wait();
+    grid_dependents_launch();
+    const Piece x = piece_of<kMode>(p);
+    const int *list = kMode == kPieceBlocks ? p.blocks + static_cast<size_t>(x.seg) * p.n_blocks : nullptr;
+    // Block of tile t, or -1: none (kPieceBlocks); 32 of a list at a time, a lane each.
+    int listed = -1, listed_at = -1;
+    auto block_of = [&](int t) {
+        if (kMode != kPieceBlocks)
+            return t;
+        const int at = t & ~31;
+        if (at != listed_at) {
+            listed = at + lane < x.t1 ? list[at + lane] : -1;
+            listed_at = at;
+        }
+        const int blk = __shfl_sync(0xffffffffu, listed, t & 31);
+        return blk >= 0 && blk < (x.L + T - 1) / T ? blk : -1;
+    };
+
+    if (warp == kWarps) {
+        // ------------------------------------ producer ------------------------------------------
+        const int zk = ((p.slot * 2 + 0) * p.b + x.beta) * p.g + x.j, zv = zk + p.b * p.g;
+        int idx = 0;
+        for (int t = x.t0; t < x.t1; ++t) {
+            const int blk = block_of(t);
+            if (blk < 0)
+                continue;
+            const int s = idx % S;
+            int ok = 1;
+            if (lane == 0) {
+                if (idx >= S && !mbar_wait(bar_empty + 8 * s, ((idx / S) & 1) ^ 1)) {
+                    flag[0] = 1;
+                    atomicOr(p.err, kErrWaitEmpty);
+                }
+                ok = !flag[0];
+                if (ok) {
+                    const uint32_t fb = bar_full + 8 * s, dst = sbase + s * 2 * PL::kTile;
+                    mbar_arrive_expect_tx(fb, 2 * PL::kTile);
+#pragma unroll
+                    for (int sub = 0; sub < D / 64; ++sub)
+                        tma_load_3d(dst + sub * T * 128, &tmap, fb, sub * 64, blk * T, zk);
+#pragma unroll
+                    for (int sub = 0; sub < D / 64; ++sub)
+                        tma_load_3d(dst + PL::kTile + sub * T * 128, &tmap, fb, sub * 64, blk * T, zv);
+                }
+            }
+            if (!__shfl_sync(0xffffffffu, ok, 0))
+                break;
+            ++idx;
+        }
+        // No copy may still be in flight when the CTA exits.
+        if (lane == 0)
+            for (int k = idx > S ? idx - S : 0; k < idx; ++k)
+                if (!mbar_wait(bar_full + 8 * (k % S), (k / S) & 1))
+                    atomicOr(p.err, kErrDrain);
+        return;
+    }
+
+    // -------------------------------------- consumers -------------------------------------------
+    const int r0 = lane >> 2;   // this lane's rows: heads r0 and r0 + 8
+    uint32_t qf[D / 16][4];
+    {
+        const __nv_bfloat16 *q = p.Q + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * p.G) * D;
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = r0 + (i & 1) * 8, ch = kk * 16 + (i >> 1) * 8 + (lane & 3) * 2;
+                qf[kk][i] = row < p.G ? *reinterpret_cast<const uint32_t *>(q + row * D + ch) : 0u;
+            }
+    }
+    float m[2] = {neg_inf(), neg_inf()}, l[2] = {0.f, 0.f};
+    float o[D / 8][4];
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            o[c][e] = 0.f;
+    int idx = 0;
+    bool ok = true;
+    for (int t = x.t0; t < x.t1; ++t) {
+        const int blk = block_of(t);
+        if (blk < 0)
+            continue;
+        const int mine = idx++;
+        const int s = mine % S;
+        if (s != warp)
+            continue;
+        if (!mbar_wait(bar_full + 8 * s, (mine / S) & 1))
+            ok = false;
+        if (__any_sync(0xffffffffu, !ok || flag[0])) {
+            if (lane == 0) {
+                flag[0] = 1;
+                atomicOr(p.err, kErrWaitFull);
+            }
+            ok = false;
+            break;
+        }
+        const uint32_t kb = sbase + s * 2 * PL::kTile, vb = kb + PL::kTile;
+        float sc[8][4];
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                sc[n][e] = 0.f;
+        const int mi = lane >> 3, mr = lane & 7;   // ldmatrix: matrix and row of this lane's address
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                uint32_t b0, b1, b2, b3;
+                ldsm_x4(kb + swz<T>(n * 16 + (mi >> 1) * 8 + mr, kk * 2 + (mi & 1)), b0, b1, b2, b3);
+                mma_bf16_16816(sc[2 * n], qf[kk], b0, b1);
+                mma_bf16_16816(sc[2 * n + 1], qf[kk], b2, b3);
+            }
+        const int lim = x.L - blk * T;   // visible positions of the tile, 64 or more: all
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                sc[n][e] *= p.scale_log2;
+        if (lim < T) {
+#pragma unroll
+            for (int n = 0; n < 8; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (n * 8 + (lane & 3) * 2 + (e & 1) >= lim)
+                        sc[n][e] = neg_inf();
+            // Values behind the sequence's end may be anything: their weight 0 takes zeros.
+            for (int i = lane; i < (T - lim) * (D / 8); i += 32)
+                *reinterpret_cast<uint4 *>(smem + (vb - sbase) + swz<T>(lim + i / (D / 8), i % (D / 8))) =
+                    make_uint4(0, 0, 0, 0);
+            fence_proxy_async_smem();
+            __syncwarp();
+        }
+        if (kMode == kPieceWeights) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int row = r0 + 8 * i;
+                if (row >= p.G)
+                    continue;
+                float *to = p.scores +
+                            (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * p.G + row) *
+                                p.score_stride + static_cast<size_t>(blk) * T;
+#pragma unroll
+                for (int n = 0; n < 8; ++n)   // (rows of scores are whole tiles)
+                    *reinterpret_cast<float2 *>(to + n * 8 + (lane & 3) * 2) =
+                        make_float2(sc[n][2 * i], sc[n][2 * i + 1]);
+            }
+        }
+        float mt[2] = {neg_inf(), neg_inf()};
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+            mt[0] = fmaxf(mt[0], fmaxf(sc[n][0], sc[n][1]));
+            mt[1] = fmaxf(mt[1], fmaxf(sc[n][2], sc[n][3]));
+        }
+        float alpha[2], mu[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            mt[i] = fmaxf(mt[i], __shfl_xor_sync(0xffffffffu, mt[i], 1));
+            mt[i] = fmaxf(mt[i], __shfl_xor_sync(0xffffffffu, mt[i], 2));
+            const float mn = fmaxf(m[i], mt[i]);
+            alpha[i] = m[i] == mn ? 1.f : fast_exp2(m[i] - mn);
+            m[i] = mn;
+            mu[i] = mn == neg_inf() ? 0.f : mn;
+            l[i] *= alpha[i];
+        }
+        if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) {
+                o[c][0] *= alpha[0];
+                o[c][1] *= alpha[0];
+                o[c][2] *= alpha[1];
+                o[c][3] *= alpha[1];
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                sc[n][e] = fast_exp2(sc[n][e] - mu[e >> 1]);
+                l[e >> 1] += sc[n][e];
+            }
+        // Weights rounded to bf16 for the product (half a step, 2^-9 of each); their sum is not.
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+            const uint32_t a[4] = {pack_bf16x2(sc[2 * kk][0], sc[2 * kk][1]),
+                                   pack_bf16x2(sc[2 * kk][2], sc[2 * kk][3]),
+                                   pack_bf16x2(sc[2 * kk + 1][0], sc[2 * kk + 1][1]),
+                                   pack_bf16x2(sc[2 * kk + 1][2], sc[2 * kk + 1][3])};
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) {
+                uint32_t b0, b1, b2, b3;
+                ldsm_x4_trans(vb + swz<T>(kk * 16 + (mi & 1) * 8 + mr, c * 2 + (mi >> 1)), b0, b1, b2, b3);
+                mma_bf16_16816(o[2 * c], a, b0, b1);
+                mma_bf16_16816(o[2 * c + 1], a, b2, b3);
+            }
+        }
+        __syncwarp();
+        if (lane == 0)
+            mbar_arrive(bar_empty + 8 * s);
+    }
+    // The warps' sums meet in the ring (every tile has been read: a consumer takes each).
+    const int tid = threadIdx.x;
+    float *s_ml = reinterpret_cast<float *>(smem + PL::kML);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+        if ((lane & 3) == 0) {
+            s_ml[warp * 32 + r0 + 8 * i] = m[i];
+            s_ml[warp * 32 + 16 + r0 + 8 * i] = l[i];
+        }
+    }
+    consumer_bar_sync<kWarps>();
+    if (tid == 0)
+        flag[2] = flag[0];   // (the producer may still give up: one answer for all)
+    float *s_o = reinterpret_cast<float *>(smem);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int row = r0 + 8 * i;
+        if (row < p.G) {
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c)
+                *reinterpret_cast<float2 *>(s_o + (warp * 16 + row) * PL::kRow + c * 8 + (lane & 3) * 2) =
+                    make_float2(o[c][2 * i], o[c][2 * i + 1]);
+        }
+    }
+    consumer_bar_sync<kWarps>();
+    if (flag[2])
+        return;
+    if (early)
+        grid_dependency_wait();
+    const int n_pre = kMode == kPieceSuffix ? p.pre_n[x.beta] : 0;
+    const bool whole = kMode != kPieceWeights && x.count == 1 && n_pre == 0;
+    const size_t rec = blockIdx.x;
+    __nv_bfloat16 *ob = p.out + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * p.G) * D;
+    for (int i = tid * 4; i < p.G * D; i += kWarps * 32 * 4) {
+        const int row = i / D, ch = i - row * D;
+        float mx = neg_inf();
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w)
+            mx = fmaxf(mx, s_ml[w * 32 + row]);
+        float tot = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float mw = s_ml[w * 32 + row], lw = s_ml[w * 32 + 16 + row];
+            // (without a maximum the sum is 0, which has no say, or NaN, which has)
+            const float f = mw == neg_inf() ? (lw == 0.f ? 0.f : 1.f) : fast_exp2(mw - mx);
+            if (f != 0.f) {
+                const float4 v = *reinterpret_cast<const float4 *>(s_o + (w * 16 + row) * PL::kRow + ch);
+                tot = fmaf(f, lw, tot);
+                acc.x = fmaf(f, v.x, acc.x);
+                acc.y = fmaf(f, v.y, acc.y);
+                acc.z = fmaf(f, v.z, acc.z);
+                acc.w = fmaf(f, v.w, acc.w);
+            }
+        }
+        const float inv = tot == 0.f ? 0.f : 1.f / tot;
+        acc.x *= inv;
+        acc.y *= inv;
+        acc.z *= inv;
+        acc.w *= inv;
+        if (whole) {
+            uint2 w2;
+            w2.x = pack_bf16x2(acc.x, acc.y);
+            w2.y = pack_bf16x2(acc.z, acc.w);
+            *reinterpret_cast<uint2 *>(ob + i) = w2;
+        } else {
+            *reinterpret_cast<float4 *>(p.part_o + rec * p.G * D + i) = acc;
+            if (ch == 0)
+                p.part_lse[rec * p.G + row] = tot == 0.f ? neg_inf() : mx + log2f(tot);
+        }
+    }
+    if (whole || kMode == kPieceWeights)
+        return;
+    if (x.count > 1) {
+        __threadfence();
+        consumer_bar_sync<kWarps>();
+        if (tid == 0)
+            flag[1] = static_cast<int>(atomic_add_acq_rel_gpu(&p.counters[x.seg], 1u));
+        consumer_bar_sync<kWarps>();
+        if (flag[1] != x.count - 1)
+            return;
+        if (tid == 0)
+            p.counters[x.seg] = 0u;
+        __threadfence();
+    } else {
+        __threadfence_block();
+        consumer_bar_sync<kWarps>();
+    }
+    merge_records<D>(p, x, rec - x.index, n_pre, reinterpret_cast<float *>(smem), tid, kWarps * 32);
+}
+
+// --------------------------------------------------------------------------------------------------
+// kPieceWeights: what each position got
+// --------------------------------------------------------------------------------------------------
+
+// A segment's CTA 0 merges its records into out, CTA 1 + k takes chunk k of its positions.  Bound by the scores' and weights' bytes, 4 G + 8 a position of a KV head (the scores from L2
+// where they fit).
+constexpr int kWeightThreads = 256;
+template <int D>
+__global__ void __launch_bounds__(kWeightThreads)
+    weights_kernel(const __grid_constant__ PieceParams p, const __grid_constant__ WeightsParams w)
+{
+    __shared__ float s_lse[16];
+    extern __shared__ float s_w[];
+    grid_dependency_wait();
+    grid_dependents_launch();
+    const int seg = static_cast<int>(blockIdx.x) / w.ctas, tid = static_cast<int>(threadIdx.x);
+    const int part = static_cast<int>(blockIdx.x) - seg * w.ctas;
+    Piece x;
+    x.beta = seg / p.g;
+    x.j = seg - x.beta * p.g;
+    x.L = p.seq_len[x.beta];
+    x.seg = seg;
+    x.count = (((x.L + T - 1) / T) + p.tiles - 1) / p.tiles;
+    const size_t rec0 = static_cast<size_t>(p.first[x.beta]) + static_cast<size_t>(x.j) * x.count;
+    const int G = p.G;
+    if (part == 0) {
+        merge_records<D>(p, x, rec0, 0, s_w, tid, kWeightThreads);
+        return;
+    }
+    const int u0 = (part - 1) * w.chunk, u1 = min(u0 + w.chunk, w.max_seq);
+    const size_t row = static_cast<size_t>(seg) * w.max_seq;
+    if (u0 < x.L) {
+        // log2 of every head's sum, from the records: a warp a head
+        for (int i = tid >> 5; i < G; i += kWeightThreads / 32) {
+            const int lane = tid & 31;
+            float mx = neg_inf();
+            for (int k = lane; k < x.count; k += 32)
+                mx = fmaxf(mx, __ldcg(p.part_lse + (rec0 + k) * G + i));
+            for (int s = 16; s > 0; s >>= 1)
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
+            float tot = 0.f;
+            for (int k = lane; k < x.count; k += 32) {
+                const float lse = __ldcg(p.part_lse + (rec0 + k) * G + i);
+                tot += lse == neg_inf() ? 0.f : exp2f(lse - mx);
+            }
+            for (int s = 16; s > 0; s >>= 1)
+                tot += __shfl_xor_sync(0xffffffffu, tot, s);
+            if (lane == 0)
+                s_lse[i] = mx + log2f(tot);
+        }
+        __syncthreads();
+    }
+    const float *sc = p.scores + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * G) * p.score_stride;
+    for (int u = u0 + tid; u < u1; u += kWeightThreads) {
+        float a = 0.f;
+        if (u < x.L)
+            for (int i = 0; i < G; ++i)
+                a += exp2f(__ldcg(sc + i * p.score_stride + u) - s_lse[i]);
+        const float before = w.weights_in != nullptr ? w.weights_in[row + u] : 0.f;
+        w.weights_out[row + u] = before + a;
+    }
+}
+
+// Queries of the sequences that share a prefix, side by side.
+__global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackParams p)
+{
+    grid_dependency_wait();
+    grid_dependents_launch();
+    const uint4 *from = reinterpret_cast<const uint4 *>(p.Q) + static_cast<size_t>(p.seq[blockIdx.x]) * p.row_vecs;
+    uint4 *to = reinterpret_cast<uint4 *>(p.packed) + static_cast<size_t>(blockIdx.x) * p.row_vecs;
+    for (int i = threadIdx.x; i < p.row_vecs; i += 256)
+        to[i] = from[i];
+}
+
+template <int D>
+const void *piece_fn(int mode)
+{
+    return mode == kPieceSuffix   ? reinterpret_cast<const void *>(&piece_kernel<D, kPieceSuffix>)
+           : mode == kPieceBlocks ? reinterpret_cast<const void *>(&piece_kernel<D, kPieceBlocks>)
+                                  : reinterpret_cast<const void *>(&piece_kernel<D, kPieceWeights>);
+}
+const void *piece_fn(int head_dim, int mode) { return head_dim == 64 ? piece_fn<64>(mode) : piece_fn<128>(mode); }
+
+int piece_threads(int head_dim) { return head_dim == 64 ? PiecePlan<64>::kThreads : PiecePlan<128>::kThreads; }
+size_t piece_smem(int head_dim) { return head_dim == 64 ? PiecePlan<64>::kBytes : PiecePlan<128>::kBytes; }
+
+cudaError_t launch_pdl(const void *fn, dim3 grid, int threads, size_t smem, cudaStream_t stream, void **args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelExC(&cfg, fn, args);
+}
+
+}  // namespace
+
+
+int piece_warps(int head_dim) { return head_dim == 64 ? PiecePlan<64>::kWarps : PiecePlan<128>::kWarps; }
+
+int piece_max_records(int head_dim, int G)
+{
+    return (head_dim == 64 ? max_records<64>(G) : max_records<128>(G)) - 1;
+}
+
+cudaError_t prepare_pieces(int head_dim, int mode, int *ctas_per_sm)
+{
+    const void *fn = piece_fn(head_dim, mode);
+    cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         static_cast<int>(piece_smem(head_dim)));
+    if (e == cudaSuccess)
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(ctas_per_sm, fn, piece_threads(head_dim),
+                                                          piece_smem(head_dim));
+    return e;
+}
+
+cudaError_t launch_pieces(int head_dim, int mode, const CUtensorMap *tmap, const PieceParams &p,
+                          cudaStream_t stream)
+{
+    void *args[] = {const_cast<CUtensorMap *>(tmap), const_cast<PieceParams *>(&p)};
+    return launch_pdl(piece_fn(head_dim, mode), dim3(static_cast<unsigned>(p.first[p.b])), piece_threads(head_dim),
+                      piece_smem(head_dim), stream, args);
+}
+
+cudaError_t launch_weights(int head_dim, const PieceParams &p, const WeightsParams &w, int max_len,
+                           cudaStream_t stream)
+{
+    // room for the merge weights of the longest segment's records
+    const int most = (((max_len + T - 1) / T) + p.tiles - 1) / p.tiles;
+    const size_t smem = sizeof(float) * (static_cast<size_t>(most) + 1) * p.G;
+    void *args[] = {const_cast<PieceParams *>(&p), const_cast<WeightsParams *>(&w)};
+    return launch_pdl(head_dim == 64 ? reinterpret_cast<const void *>(&weights_kernel<64>)
+                                     : reinterpret_cast<const void *>(&weights_kernel<128>),
+                      dim3(static_cast<unsigned>(w.ctas) * p.b * p.g), kWeightThreads, smem, stream, args);
+}
+
+cudaError_t launch_pack(const PackParams &p, cudaStream_t stream)
+{
+    void *args[] = {const_cast<PackParams *>(&p)};
+    return launch_pdl(reinterpret_cast<const void *>(&pack_kernel), dim3(static_cast<unsigned>(p.n)), 256, 0,
+                      stream, args);
+}
+
+}  // namespace mlkv

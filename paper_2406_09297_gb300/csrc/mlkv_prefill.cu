@@ -183,20 +183,32 @@ struct Unit {
     int n_a, n_b;         // key tiles of query tiles A (0: no tile A) and B, n_a <= n_b
     int qb_b;             // prefill: tile B's query block
     int head_a, head_b, j;
-    int ns, skip;         // sliding window: key tiles of the sinks, and blocks left out behind them
+    int ns, skip;         // sliding window: key tiles of the sinks, and blocks left out behind them;
+                          // shared prefix: its key tiles, and less as many (own blocks count from 0)
     int zk, zv;           // rows of the K and V tensor maps: (slot, sequence, KV head)
+    int zp, n_pre;        // shared prefix: its keys' row of its map, and its positions
+    int place, seqs;      // decode over a shared prefix: the unit's first place, sequences from there on
     bool has_end;         // the unit holds the sequence's last key tile
 };
 
-// Block of 128 positions that the unit's key tile t covers.
-template <bool kWin>
+// Block of 128 positions that the unit's key tile t covers (kSkip: a sliding window, or a prefix in front).
+template <bool kSkip>
 __device__ __forceinline__ int key_block(const Unit &x, int t)
 {
-    return x.kt0 + t + (kWin && t >= x.ns ? x.skip : 0);
+    return x.kt0 + t + (kSkip && t >= x.ns ? x.skip : 0);
 }
 
-template <bool kFused, int kTiles, bool kWin>
-__device__ __forceinline__ Unit unit_of(const PrefillParams &p, int i)
+template <bool kShared>
+struct PrefillArgs {
+    using Type = PrefillParams;
+};
+template <>
+struct PrefillArgs<true> {
+    using Type = SharedPrefillParams;
+};
+
+template <bool kFused, int kTiles, bool kWin, bool kShared>
+__device__ __forceinline__ Unit unit_of(const typename PrefillArgs<kShared>::Type &p, int i)
 {
     Unit x;
     const uint32_t u = p.units[i];
@@ -204,6 +216,7 @@ __device__ __forceinline__ Unit unit_of(const PrefillParams &p, int i)
     const int sel = static_cast<int>(u >> 24);
     x.S = p.prompt_len[x.beta];
     x.ns = x.skip = 0;
+    x.zp = x.n_pre = x.place = x.seqs = 0;
     if (kFused) {
         // every query row sees positions [0, S); the unit takes key tiles [kt0, kt0 + n_b)
         const int n_kt = (x.S + 127) / 128;
@@ -214,6 +227,13 @@ __device__ __forceinline__ Unit unit_of(const PrefillParams &p, int i)
         x.has_end = kt1 == n_kt;
         x.n_b = kt1 - x.kt0;
         x.n_a = kTiles == 2 && p.fused_L > p.fused_L1 ? x.n_b : 0;
+        if constexpr (kShared) {
+            const int s0 = x.blk * 2 * p.fused_L1;
+            x.place = p.group_at[x.beta] + s0;
+            x.seqs = p.group_n[x.beta] - s0;
+            x.n_a = x.seqs > p.fused_L1 ? x.n_b : 0;
+            x.blk = 0;
+        }
         x.qb_b = 0;
         x.head_a = x.head_b = x.j = sel;
     } else {
@@ -228,40 +248,54 @@ __device__ __forceinline__ Unit unit_of(const PrefillParams &p, int i)
             x.ns = (p.sinks + 127) / 128;
             x.skip = max(0, max(0, q_first - p.window + 1) / 128 - x.ns);
         }
+        if constexpr (kShared) {
+            x.n_pre = p.prefix_len[x.beta];
+            x.ns = (x.n_pre + 127) / 128;
+            x.skip = -x.ns;
+        }
         x.n_b = x.qb_b + 1 - x.skip;
         x.n_a = kTiles == 1 ? 0 : p.head_pairs ? x.n_b : ((x.qb_b & 1) ? x.qb_b - x.skip : 0);
         x.head_a = p.head_pairs ? 2 * sel : sel;
         x.head_b = p.head_pairs ? 2 * sel + 1 : sel;
         x.j = x.head_b / p.G;   // Eq. 15
     }
+    if constexpr (kShared && !kFused)
+        x.zp = ((p.slot * 2) * p.prefix_b + max(0, static_cast<int>(p.prefix_of[x.beta]))) * p.g + x.j;
     if (!kFused && p.kv_direct) {   // the prompt's own tensors, [b][g][s_max][D] each
         x.zk = x.zv = x.beta * p.g + x.j;
     } else {
-        x.zk = (((p.slot + x.blk) * 2 + 0) * p.b + x.beta) * p.g + x.j;
-        x.zv = x.zk + p.b * p.g;
+        int b = p.b;
+        if constexpr (kShared && kFused)
+            b = p.prefix_b;
+        x.zk = (((p.slot + x.blk) * 2 + 0) * b + x.beta) * p.g + x.j;
+        x.zv = x.zk + b * p.g;
     }
     return x;
 }
 
 // The CTA's k-th unit, or -1 past its last: a snake deal of the units (longest first) to the
 // persistent CTAs, which evens out their key tiles.
-__device__ __forceinline__ int unit_index(const PrefillParams &p, int k)
+__device__ __forceinline__ int unit_index(const PrefillCommon &p, int k)
 {
     const int P = static_cast<int>(gridDim.x), c = static_cast<int>(blockIdx.x);
     const int i = k * P + ((k & 1) ? P - 1 - c : c);
     return i < p.n_units ? i : -1;
 }
 
-template <int D, bool kFused, int kForm, bool kWin>
+template <int D, bool kFused, int kForm, bool kWin, bool kShared>
 __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                                   PrefillPlan<D, kForm>::kMinBlocks)
     prefill_kernel(const __grid_constant__ CUtensorMap tmap_q,
                    const __grid_constant__ CUtensorMap tmap_k,
                    const __grid_constant__ CUtensorMap tmap_v,
-                   const __grid_constant__ PrefillParams p)
+                   const __grid_constant__ typename PrefillArgs<kShared>::Type p)
 {
     using PL = PrefillPlan<D, kForm>;
+    static_assert(!kShared || !kWin, "no window over a shared prefix");
     constexpr bool kSplit = PL::kSBuf == 2;   // key tiles alternate between two warpgroups
+    // (the decode over a shared prefix writes records straight from its registers; a unit of it may leave tile A
+    // out, whose warps would arrive ahead of the unit)
+    constexpr bool kStageInQ = PL::kStageInQ && !(kFused && kShared);
     constexpr int NQ = PL::kQBufs;
     constexpr int R = PL::kRingTiles;
     // Query tile g's shared-memory slot and tensor-memory columns (the only tile of a one-tile CTA
@@ -295,7 +329,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
             // S and, where the outputs are staged in the query tiles, by the softmax warps
             mbar_init(bar_q + 8 * q,
                       kSplit && kFused && p.q_host != nullptr ? PL::kSoftWarps : 1);
-            mbar_init(bar_q_free + 8 * q, 1 + (PL::kStageInQ ? PL::kSoftWarps : 0));
+            mbar_init(bar_q_free + 8 * q, 1 + (kStageInQ ? PL::kSoftWarps : 0));
         }
         for (int s = 0; s < R; ++s) {
             mbar_init(bar_full + 8 * s, 1);
@@ -420,9 +454,21 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
             mbar_arrive_expect_tx(fb, PL::kTileBytes);
 #pragma unroll
             for (int sub = 0; sub < PL::kSub; ++sub)
-                tma_load_3d(sbase + PL::kRing + s * PL::kTileBytes + sub * 16384,
-                            (k & 1) ? &tmap_v : &tmap_k, fb, sub * 64, key_block<kWin>(x, k >> 1) * 128,
-                            (k & 1) ? x.zv : x.zk);
+                if constexpr (kShared && !kFused) {
+                    const bool pre = (k >> 1) < x.ns;   // the prefix's tiles come first
+                    tma_load_3d(sbase + PL::kRing + s * PL::kTileBytes + sub * 16384,
+                                pre       ? &p.tmap_p
+                                : (k & 1) ? &tmap_v
+                                          : &tmap_k,
+                                fb, sub * 64, key_block<true>(x, k >> 1) * 128,
+                                pre       ? x.zp + ((k & 1) ? p.prefix_b * p.g : 0)
+                                : (k & 1) ? x.zv
+                                          : x.zk);
+                } else {
+                    tma_load_3d(sbase + PL::kRing + s * PL::kTileBytes + sub * 16384,
+                                (k & 1) ? &tmap_v : &tmap_k, fb, sub * 64,
+                                key_block<kWin>(x, k >> 1) * 128, (k & 1) ? x.zv : x.zk);
+                }
             ++idx;
             return true;
         };
@@ -452,7 +498,10 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
 #pragma unroll
                 for (int sub = 0; sub < PL::kSub; ++sub) {
                     const uint32_t d = dst + slot_of(g) * PL::kTileBytes + sub * 16384;
-                    if (kFused)
+                    if (kFused && kShared)   // (channel, head in group, group, 1, place)
+                        tma_load_5d(d, &tmap_q, qbar, sub * 64, 0, x.j, 0,
+                                    x.place + (g ? 0 : p.fused_L1));
+                    else if (kFused)
                         tma_load_5d(d, &tmap_q, qbar, sub * 64, 0, x.j, x.beta,
                                     x.blk * p.fused_L + (g ? 0 : p.fused_L1));
                     else
@@ -468,7 +517,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                 const int i = unit_index(p, n);
                 if (i < 0)
                     break;
-                const Unit x = unit_of<kFused, PL::kTiles, kWin>(p, i);
+                const Unit x = unit_of<kFused, PL::kTiles, kWin, kShared>(p, i);
                 const int n_idx = 2 * x.n_b;
                 int k = 0;
                 if (n == 0 && early && !q_early) {
@@ -570,7 +619,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                 const int i = unit_index(p, n);
                 if (i < 0)
                     break;
-                const Unit x = unit_of<kFused, PL::kTiles, kWin>(p, i);
+                const Unit x = unit_of<kFused, PL::kTiles, kWin, kShared>(p, i);
                 const int qb = n % NQ;
                 const uint64_t dq = dq0 + static_cast<uint32_t>(qb * PL::kTiles) * kSlot;
                 if (PL::kPSep && do_s) {
@@ -700,7 +749,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
             // The CTA's only unit: nothing to compute before its queries, so every softmax warp
             // loads, one round trip over the link (by the last warp alone, two: 64 sequences of
             // 2,048 tokens end to end 34.5 us a step, now 32.9).
-            load_q_host(unit_of<kFused, PL::kTiles, kWin>(p, unit_index(p, 0)), 0, threadIdx.x,
+            load_q_host(unit_of<kFused, PL::kTiles, kWin, kShared>(p, unit_index(p, 0)), 0, threadIdx.x,
                         std::integral_constant<int, 32 * PL::kSoftWarps>{},
                         std::integral_constant<int, 4>{});
             fence_proxy_async_smem();
@@ -715,7 +764,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
             const int i = unit_index(p, n);
             if (i < 0 || (!kSplit && __any_sync(0xffffffffu, flags[0])))
                 break;
-            const Unit x = unit_of<kFused, PL::kTiles, kWin>(p, i);
+            const Unit x = unit_of<kFused, PL::kTiles, kWin, kShared>(p, i);
             const int qb = n % NQ;
             const int n_g = grp ? x.n_b : x.n_a;
             const int q0 = (x.kt0 + n_g - 1 + x.skip) * 128;   // first position of the unit's last tile
@@ -763,6 +812,34 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                         *reinterpret_cast<uint4 *>(vrow + (c >> 3) * 16384 + r * 128 +
                                                    (((c & 7) ^ (r & 7)) << 4)) = make_uint4(0, 0, 0, 0);
                     fence_proxy_async_smem();
+                }
+                if constexpr (kShared && !kFused) {
+                    // The prefix's last tile holds keys past its end: masked, their V rows zeroed by the
+                    // first tile to reach it.
+                    const int lim = x.n_pre - 128 * t;
+                    if (t == x.ns - 1 && lim < 128) {
+                        if ((grp == 0 || x.n_a == 0) && r >= lim) {
+                            const int idx = 2 * (kb + t) + 1;
+                            wait(bar_full + 8 * (idx % R), idx / R);
+                            uint8_t *vrow = smem + PL::kRing + (idx % R) * PL::kTileBytes;
+#pragma unroll
+                            for (int c = 0; c < 8 * PL::kSub; ++c)
+                                *reinterpret_cast<uint4 *>(vrow + (c >> 3) * 16384 + r * 128 +
+                                                           (((c & 7) ^ (r & 7)) << 4)) =
+                                    make_uint4(0, 0, 0, 0);
+                            fence_proxy_async_smem();
+                        }
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            mx[c] = NEG_INF;
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) {
+                                if (c * 32 + k >= lim)
+                                    sv[c][k] = NEG_INF;
+                                mx[c] = fmaxf(mx[c], sv[c][k]);
+                            }
+                        }
+                    }
                 }
                 if (kWin && (diag || behind)) {
                     // Keys [0, hi) of the tile that are sinks (below lo_s) or in the window (from
@@ -888,7 +965,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
             // during the loop.
             int i_out = i;
             asm volatile("" : "+r"(i_out));
-            const Unit y = unit_of<kFused, PL::kTiles, kWin>(p, i_out);
+            const Unit y = unit_of<kFused, PL::kTiles, kWin, kShared>(p, i_out);
             // The unit's last product, and with it the last reader of its last V.
             const int n_mine = kSplit ? (n_g - wg + 1) / 2 : n_g;   // this warpgroup's tiles
             if (n_mine > 0) {
@@ -948,10 +1025,33 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                 // (grp ? 0 : L1) + r / G of the block, head j*G + r % G; out [layers][b][h][D].
                 const int lay0 = y.blk * p.fused_L + (grp ? 0 : p.fused_L1);
                 const int n_rows =
-                    !kFused ? min(128, y.S - q0)
-                            : (grp ? (p.fused_L < p.fused_L1 ? p.fused_L : p.fused_L1)
-                                   : p.fused_L - p.fused_L1) * p.G;
-                if (kFused && p.fused_cmax > 1) {
+                    !kFused  ? min(128, y.S - q0)
+                    : kShared ? min(p.fused_L1, y.seqs - (grp ? 0 : p.fused_L1)) * p.G
+                              : (grp ? (p.fused_L < p.fused_L1 ? p.fused_L : p.fused_L1)
+                                     : p.fused_L - p.fused_L1) * p.G;
+                if (kFused && kShared) {
+                    // Row r: head r % G of the unit's sequence r / G (tile A: of those behind tile B's).
+                    const bool valid = r < n_rows && !stop;
+                    const int sq = r / p.G;
+                    const size_t row =
+                        ((static_cast<size_t>(y.place + (grp ? 0 : p.fused_L1) + sq) * p.g + y.j) *
+                             p.fused_cmax + y.chunk) * p.G + (r - sq * p.G);
+                    if (valid)
+                        p.part_lse[row] = m_run + log2f(l_run);
+                    float *prow = p.part + row * D;
+#pragma unroll
+                    for (int c = 0; c < PL::kSub * 2; ++c) {
+                        float ov[32];
+                        load_o(c, ov);
+                        if (valid) {
+#pragma unroll
+                            for (int k = 0; k < 32; k += 4)
+                                *reinterpret_cast<float4 *>(prow + c * 32 + k) =
+                                    make_float4(ov[k] * inv, ov[k + 1] * inv, ov[k + 2] * inv,
+                                                ov[k + 3] * inv);
+                        }
+                    }
+                } else if (kFused && p.fused_cmax > 1) {
                     // One chunk of the context: o = O / l and lse = m + log2(l) for the merge.
                     const bool valid = r < n_rows && !stop;
                     const size_t row0 = (((static_cast<size_t>(y.blk) * p.b + y.beta) * p.g + y.j) *
@@ -1030,7 +1130,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                 }
                 tmem_fence_before();
             }
-            if (PL::kStageInQ) {
+            if (kStageInQ) {
                 // The next queries may be written over the stage.  (Every warpgroup has a tile in
                 // every unit here: two query tiles at head_dim 64 are a fused block of more rows
                 // than one holds.)
@@ -1051,7 +1151,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                 const int i = unit_index(p, n);
                 if (i < 0)
                     break;
-                const Unit x = unit_of<kFused, PL::kTiles, kWin>(p, i);
+                const Unit x = unit_of<kFused, PL::kTiles, kWin, kShared>(p, i);
                 const int qb = n % NQ;
                 int ok = 1;
                 if (lane == 0 && n >= NQ && !flags[0] &&
@@ -1207,10 +1307,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 3) combine_fused_kernel(con
             pack_bf16x2(acc[e] * inv, acc[e + 1] * inv);
 }
 
-template <int D, bool kFused, int kForm, bool kWin = false>
+template <int D, bool kFused, int kForm, bool kWin = false, bool kShared = false>
 const void *prefill_fn()
 {
-    return reinterpret_cast<const void *>(&prefill_kernel<D, kFused, kForm, kWin>);
+    return reinterpret_cast<const void *>(&prefill_kernel<D, kFused, kForm, kWin, kShared>);
 }
 
 // The forms built: prefill at head_dim 64 with one query tile per CTA, at 128 with two; the fused
@@ -1254,8 +1354,7 @@ const void *kernel_fn(int head_dim, bool fused, int form, bool windowed)
     return head_dim == 64 ? prefill_fn<64, false, kOneTile>() : prefill_fn<128, false, kTwoTiles>();
 }
 
-cudaError_t launch(int head_dim, bool fused, int form, const CUtensorMap *tmap_q,
-                   const CUtensorMap *tmap_k, const CUtensorMap *tmap_v, const PrefillParams &p,
+cudaError_t launch(const void *fn, int head_dim, int form, const PrefillCommon &p, void **args,
                    cudaStream_t stream)
 {
     cudaLaunchConfig_t cfg = {};
@@ -1270,9 +1369,28 @@ cudaError_t launch(int head_dim, bool fused, int form, const CUtensorMap *tmap_q
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
+    return cudaLaunchKernelExC(&cfg, fn, args);
+}
+
+cudaError_t launch(int head_dim, bool fused, int form, const CUtensorMap *tmap_q,
+                   const CUtensorMap *tmap_k, const CUtensorMap *tmap_v, const PrefillParams &p,
+                   cudaStream_t stream)
+{
     void *args[] = {const_cast<CUtensorMap *>(tmap_q), const_cast<CUtensorMap *>(tmap_k),
                     const_cast<CUtensorMap *>(tmap_v), const_cast<PrefillParams *>(&p)};
-    return cudaLaunchKernelExC(&cfg, kernel_fn(head_dim, fused, form, !fused && p.window > 0), args);
+    return launch(kernel_fn(head_dim, fused, form, !fused && p.window > 0), head_dim, form, p, args, stream);
+}
+
+// The form of the kernel over a shared prefix.
+int shared_form(int head_dim, bool fused) { return head_dim == 64 && !fused ? kOneTile : kTwoTiles; }
+
+const void *shared_fn(int head_dim, bool fused)
+{
+    if (fused)
+        return head_dim == 64 ? prefill_fn<64, true, kTwoTiles, false, true>()
+                              : prefill_fn<128, true, kTwoTiles, false, true>();
+    return head_dim == 64 ? prefill_fn<64, false, kOneTile, false, true>()
+                          : prefill_fn<128, false, kTwoTiles, false, true>();
 }
 
 // The prefill form of a head_dim; a fused-decode form valid for the head_dim.
@@ -1286,10 +1404,9 @@ size_t prefill_smem_bytes(int head_dim) { return smem_of(head_dim, prefill_form(
 // The warpgroups' register split (setmaxnreg) adds up to the registers the block is launched with;
 // a kernel built with another per-thread count would wait forever in setmaxnreg.inc, so it is
 // refused here instead of launched.
-cudaError_t prepare(int head_dim, bool fused, int form, bool windowed)
+cudaError_t prepare(const void *fn, int head_dim, int form)
 {
     cudaFuncAttributes fa;
-    const void *fn = kernel_fn(head_dim, fused, form, windowed);
     cudaError_t e = cudaFuncGetAttributes(&fa, fn);
     if (e != cudaSuccess)
         return e;
@@ -1301,12 +1418,27 @@ cudaError_t prepare(int head_dim, bool fused, int form, bool windowed)
 
 cudaError_t prepare_prefill(int head_dim, bool windowed)
 {
-    return prepare(head_dim, false, prefill_form(head_dim), windowed);
+    return prepare(kernel_fn(head_dim, false, prefill_form(head_dim), windowed), head_dim,
+                   prefill_form(head_dim));
 }
 
 cudaError_t prepare_fused(int head_dim, int form)
 {
-    return prepare(head_dim, true, fused_form(head_dim, form), false);
+    return prepare(kernel_fn(head_dim, true, fused_form(head_dim, form), false), head_dim,
+                   fused_form(head_dim, form));
+}
+
+cudaError_t prepare_shared(int head_dim, bool fused)
+{
+    return prepare(shared_fn(head_dim, fused), head_dim, shared_form(head_dim, fused));
+}
+
+cudaError_t launch_shared(int head_dim, bool fused, const CUtensorMap *tmap_q, const CUtensorMap *tmap_k,
+                          const CUtensorMap *tmap_v, const SharedPrefillParams &p, cudaStream_t stream)
+{
+    void *args[] = {const_cast<CUtensorMap *>(tmap_q), const_cast<CUtensorMap *>(tmap_k),
+                    const_cast<CUtensorMap *>(tmap_v), const_cast<SharedPrefillParams *>(&p)};
+    return launch(shared_fn(head_dim, fused), head_dim, shared_form(head_dim, fused), p, args, stream);
 }
 
 cudaError_t launch_prefill(int head_dim, const CUtensorMap *tmap_q, const CUtensorMap *tmap_k,

@@ -24,6 +24,7 @@ MLKV_ERR_UNSUPPORTED = -6
 MLKV_ERR_DEVICE = -7
 MLKV_MAX_BATCH = 1024
 MLKV_MAX_GROUP = 16
+MLKV_BLOCK = 64
 
 EXPORTED = [
     "mlkv_cache_create", "mlkv_cache_destroy", "mlkv_append", "mlkv_decode_attention",
@@ -36,6 +37,8 @@ EXPORTED = [
     "mlkv_decode_attention_window", "mlkv_prefill_window", "mlkv_qk_norm_rope", "mlkv_qk_norm_rope_struct", "mlkv_q4_create",
     "mlkv_q4_destroy", "mlkv_q4_bytes", "mlkv_q4_append", "mlkv_q4_load_prefix", "mlkv_q4_read",
     "mlkv_q4_decode_attention", "mlkv_q4_prefill", "mlkv_q4_sync_status",
+    "mlkv_decode_attention_prefix", "mlkv_prefill_prefix", "mlkv_block_bounds", "mlkv_select_blocks",
+    "mlkv_decode_attention_blocks", "mlkv_decode_attention_weights", "mlkv_evict",
 ]
 
 
@@ -97,6 +100,13 @@ def _load():
     L.mlkv_q4_decode_attention.argtypes = [vp, ci, vp, vp, vp, ci, ci, vp]
     L.mlkv_q4_prefill.argtypes = [vp, ci, vp, vp, vp, vp, vp, ci, ci, ci, vp]
     L.mlkv_q4_sync_status.argtypes = [vp]
+    L.mlkv_decode_attention_prefix.argtypes = [vp, ci] + [vp] * 7
+    L.mlkv_prefill_prefix.argtypes = [vp, ci] + [vp] * 8 + [ci, vp]
+    L.mlkv_block_bounds.argtypes = [vp, ci] + [vp] * 5
+    L.mlkv_select_blocks.argtypes = [vp, ci] + [vp] * 4 + [ci] * 3 + [vp] * 2
+    L.mlkv_decode_attention_blocks.argtypes = [vp, ci] + [vp] * 4 + [ci, vp]
+    L.mlkv_decode_attention_weights.argtypes = [vp, ci] + [vp] * 6
+    L.mlkv_evict.argtypes = [vp, vp, ci] + [vp] * 4 + [ci, vp, ci, vp]
     return L
 
 
@@ -454,6 +464,78 @@ def mlkv_q4_sync_status(handle):
     return _check(lib.mlkv_q4_sync_status(handle))
 
 
+def mlkv_decode_attention_prefix(handle, layer, prefix, prefix_of, prefix_lens, Q, out, seq_lens,
+                                 stream=None):
+    """prefix: the handle of the cache of the shared beginnings; prefix_of [b] (-1: none), prefix_lens
+    [sequences of prefix] and seq_lens [b] on the host."""
+    a, p = _lens_ptr(seq_lens)
+    o, po = _lens_ptr(prefix_of)
+    n, pn = _lens_ptr(prefix_lens)
+    return _check(lib.mlkv_decode_attention_prefix(handle, layer, prefix, po, pn, _ptr(Q), _ptr(out), p,
+                                                   _stream(stream)))
+
+
+def mlkv_prefill_prefix(handle, layer, prefix, prefix_of, prefix_lens, Q, K, V, out, prompt_lens, s_max,
+                        stream=None):
+    a, p = _lens_ptr(prompt_lens)
+    o, po = _lens_ptr(prefix_of)
+    n, pn = _lens_ptr(prefix_lens)
+    return _check(lib.mlkv_prefill_prefix(handle, layer, prefix, po, pn, _ptr(Q), _ptr(K), _ptr(V), _ptr(out),
+                                          p, s_max, _stream(stream)))
+
+
+def _dense(name, t, dtype, numel=None):
+    """A dense tensor's address; its type, and its size where it is known, are checked."""
+    if str(t.dtype) != "torch." + dtype or not t.is_contiguous() or numel not in (None, t.numel()):
+        raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must be dense, {dtype}" +
+                        ("" if numel is None else f" and of {numel} elements"))
+    return t.data_ptr()
+
+
+def mlkv_block_bounds(handle, layer, first, seq_lens, bounds, scales, stream=None):
+    """first: host [b] or None (every block); bounds int8 [b][g][n_blocks][2][d], scales fp32
+    [b][g][n_blocks], n_blocks = ceil(max_seq / 64)."""
+    a, p = _lens_ptr(seq_lens)
+    f, pf = (None, None) if first is None else _lens_ptr(first)
+    return _check(lib.mlkv_block_bounds(handle, layer, pf, p, _dense("bounds", bounds, "int8"),
+                                        _dense("scales", scales, "float32"), _stream(stream)))
+
+
+def mlkv_select_blocks(handle, layer, Q, bounds, scales, seq_lens, n_select, n_first, n_last, blocks,
+                       stream=None):
+    """blocks int32 [b][g][n_select]: written, rising, -1 behind the last."""
+    a, p = _lens_ptr(seq_lens)
+    return _check(lib.mlkv_select_blocks(handle, layer, _ptr(Q), _dense("bounds", bounds, "int8"),
+                                         _dense("scales", scales, "float32"), p, n_select, n_first, n_last,
+                                         _dense("blocks", blocks, "int32"), _stream(stream)))
+
+
+def mlkv_decode_attention_blocks(handle, layer, Q, out, seq_lens, blocks, n_blocks, stream=None):
+    """blocks int32 [b][g][n_blocks]."""
+    a, p = _lens_ptr(seq_lens)
+    return _check(lib.mlkv_decode_attention_blocks(handle, layer, _ptr(Q), _ptr(out), p,
+                                                   _dense("blocks", blocks, "int32"), n_blocks,
+                                                   _stream(stream)))
+
+
+def mlkv_decode_attention_weights(handle, layer, Q, out, seq_lens, weights_in, weights_out, stream=None):
+    """weights fp32 [b][g][max_seq]; weights_in None: zeros."""
+    a, p = _lens_ptr(seq_lens)
+    w = None if weights_in is None else _dense("weights_in", weights_in, "float32", weights_out.numel())
+    return _check(lib.mlkv_decode_attention_weights(handle, layer, _ptr(Q), _ptr(out), p, w,
+                                                    _dense("weights_out", weights_out, "float32"),
+                                                    _stream(stream)))
+
+
+def mlkv_evict(handle, to, layer, weights_in, weights_out, seq_lens, keep, recent, kept, k_max, stream=None):
+    """to: the handle of the cache that receives what stays; keep host [b]; kept int32 [b][g][k_max]."""
+    a, p = _lens_ptr(seq_lens)
+    k, pk = _lens_ptr(keep)
+    return _check(lib.mlkv_evict(handle, to, layer, _dense("weights_in", weights_in, "float32"),
+                                 _dense("weights_out", weights_out, "float32"), p, pk, recent,
+                                 _dense("kept", kept, "int32"), k_max, _stream(stream)))
+
+
 class MLKVCache:
     """Owning wrapper around an mlkv_cache_t handle."""
 
@@ -505,6 +587,78 @@ class MLKVCache:
         """prefill with a sliding window and sinks."""
         return mlkv_prefill_window(self.handle, layer, Q, K, V, out, prompt_lens, int(Q.shape[1]),
                                    window, sinks, stream)
+
+    def _sized(self, name, t, *shape):
+        if t is not None and tuple(t.shape) != shape:
+            raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must be of shape {list(shape)}")
+
+    def _host(self, name, a, n):
+        a = as_seq_lens(a)
+        if a.shape != (n,):
+            raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must hold {n} numbers")
+        return a
+
+    def decode_attention_prefix(self, layer, prefix, prefix_of, prefix_lens, Q, out, seq_lens, stream=None):
+        """Decode attention behind beginnings that sequences share: those of `prefix`, another MLKVCache
+        (or this one), sequence prefix_of[i] (-1: none) for sequence i."""
+        return mlkv_decode_attention_prefix(
+            self.handle, layer, prefix.handle, self._host("prefix_of", prefix_of, self.b),
+            self._host("prefix_lens", prefix_lens, prefix.b), Q, out,
+            self._host("seq_lens", seq_lens, self.b), stream)
+
+    def prefill_prefix(self, layer, prefix, prefix_of, prefix_lens, Q, K, V, out, prompt_lens, stream=None):
+        """Causal prefill behind a shared beginning; Q / out [b][s_max][h][d], K / V [b][g][s_max][d]."""
+        return mlkv_prefill_prefix(
+            self.handle, layer, prefix.handle, self._host("prefix_of", prefix_of, self.b),
+            self._host("prefix_lens", prefix_lens, prefix.b), Q, K, V, out,
+            self._host("prompt_lens", prompt_lens, self.b), int(Q.shape[1]), stream)
+
+    def block_bounds(self, layer, seq_lens, bounds, scales, first=None, stream=None):
+        """Bounds int8 [b][g][n_blocks][2][d] and scales fp32 [b][g][n_blocks] of the keys of every block
+        of 64 positions, from the one of position first[i] on (None: all)."""
+        n = (self.max_seq + MLKV_BLOCK - 1) // MLKV_BLOCK
+        self._sized("bounds", bounds, self.b, self.g, n, 2, self.d)
+        self._sized("scales", scales, self.b, self.g, n)
+        return mlkv_block_bounds(self.handle, layer,
+                                 None if first is None else self._host("first", first, self.b),
+                                 self._host("seq_lens", seq_lens, self.b), bounds, scales, stream)
+
+    def select_blocks(self, layer, Q, bounds, scales, seq_lens, blocks, n_first=1, n_last=1, stream=None):
+        """Writes the blocks that Q [b][h][d] needs most into blocks, int32 [b][g][n]."""
+        n = (self.max_seq + MLKV_BLOCK - 1) // MLKV_BLOCK
+        self._sized("bounds", bounds, self.b, self.g, n, 2, self.d)
+        self._sized("scales", scales, self.b, self.g, n)
+        self._sized("blocks", blocks, self.b, self.g, blocks.shape[-1])
+        return mlkv_select_blocks(self.handle, layer, Q, bounds, scales,
+                                  self._host("seq_lens", seq_lens, self.b), blocks.shape[-1], n_first, n_last,
+                                  blocks, stream)
+
+    def decode_attention_blocks(self, layer, Q, out, seq_lens, blocks, stream=None):
+        """Decode attention over the listed blocks alone, int32 [b][g][n]."""
+        self._sized("blocks", blocks, self.b, self.g, blocks.shape[-1])
+        return mlkv_decode_attention_blocks(self.handle, layer, Q, out,
+                                            self._host("seq_lens", seq_lens, self.b), blocks,
+                                            blocks.shape[-1], stream)
+
+    def decode_attention_weights(self, layer, Q, out, seq_lens, weights_in, weights_out, stream=None):
+        """Decode attention; weights_out = weights_in (None: zeros; fp32 [b][g][max_seq]) + what every
+        position was given."""
+        self._sized("weights_in", weights_in, self.b, self.g, self.max_seq)
+        self._sized("weights_out", weights_out, self.b, self.g, self.max_seq)
+        return mlkv_decode_attention_weights(self.handle, layer, Q, out,
+                                             self._host("seq_lens", seq_lens, self.b), weights_in,
+                                             weights_out, stream)
+
+    def evict(self, layer, weights_in, weights_out, seq_lens, keep, recent, kept, to=None, stream=None):
+        """Keeps the `recent` newest and the heaviest other positions, keep[i] in all, in this cache or in
+        `to`; kept int32 [b][g][n] receives where they lay."""
+        to = self if to is None else to
+        self._sized("weights_in", weights_in, self.b, self.g, self.max_seq)
+        self._sized("weights_out", weights_out, to.b, to.g, to.max_seq)
+        self._sized("kept", kept, self.b, self.g, kept.shape[-1])
+        return mlkv_evict(self.handle, to.handle, layer, weights_in, weights_out,
+                          self._host("seq_lens", seq_lens, self.b), self._host("keep", keep, self.b), recent,
+                          kept, kept.shape[-1], stream)
 
     def decode_step_host(self, Q, K, V, out, seq_lens, stream=None):
         return mlkv_decode_step_host(self.handle, Q, K, V, out, seq_lens, stream)
