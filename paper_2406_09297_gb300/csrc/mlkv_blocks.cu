@@ -39,25 +39,24 @@ __device__ __forceinline__ float inverse_power(float s)   // of a power of two
 constexpr int kBoundsThreads = 128;
 
 // A CTA is one block of one KV head: 16 bytes a load, D / 8 lanes a row, every row of the block in flight at
-// once.  Bound by the keys' bytes.
+// once; minima and maxima two channels at a time, across a warp's rows by shuffles, across the warps in shared
+// memory.  Bound by the keys' bytes.
 template <int D>
 __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_constant__ BoundsParams p)
 {
     constexpr int C = D / 8;                     // 16-byte columns of a row
     constexpr int RG = kBoundsThreads / C;       // rows at a time
     constexpr int N = kBlock / RG;               // rows of a thread
-    __shared__ float s_lo[RG][D + 4], s_hi[RG][D + 4];
-    __shared__ float s_max[kBoundsThreads / 32];
-    __shared__ int s_bad;
-    const int tid = static_cast<int>(threadIdx.x);
+    constexpr int W = kBoundsThreads / 32;
+    __shared__ __align__(16) __nv_bfloat16 s_lo[W][D], s_hi[W][D];
+    __shared__ float s_max[W];
+    const int tid = static_cast<int>(threadIdx.x), warp = tid >> 5, lane = tid & 31;
     const int seg = static_cast<int>(blockIdx.x / p.ctas), beta = seg / p.g;
     const int L = p.seq_len[beta];
     const int blk = p.first[beta] / kBlock + static_cast<int>(blockIdx.x % p.ctas);
-    if (tid == 0)
-        s_bad = 0;
     grid_dependency_wait();
     grid_dependents_launch();
-    if (blk * kBlock >= L)
+    if (static_cast<long long>(blk) * kBlock >= L)
         return;
     const int n = min(kBlock, L - blk * kBlock);
     const int col = tid % C, r0 = tid / C;
@@ -67,73 +66,86 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_con
 #pragma unroll
     for (int i = 0; i < N; ++i)
         v[i] = k[static_cast<size_t>(min(r0 + i * RG, n - 1)) * C];   // (a row twice changes nothing)
-    float lo[8], hi[8];
-    bool bad = false;
+    __nv_bfloat162 lo[4], hi[4], amax = __habs2(reinterpret_cast<const __nv_bfloat162 *>(&v[0])[0]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        lo[e] = __int_as_float(0x7f800000);
-        hi[e] = -lo[e];
-    }
+    for (int e = 0; e < 4; ++e)
+        lo[e] = hi[e] = reinterpret_cast<const __nv_bfloat162 *>(&v[0])[e];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+        const __nv_bfloat162 *x = reinterpret_cast<const __nv_bfloat162 *>(&v[i]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float a = bf16_lo(w[e]), b = bf16_hi(w[e]);
-            bad = bad || !(fabsf(a) <= kLargest) || !(fabsf(b) <= kLargest);
-            lo[2 * e] = fminf(lo[2 * e], a);
-            hi[2 * e] = fmaxf(hi[2 * e], a);
-            lo[2 * e + 1] = fminf(lo[2 * e + 1], b);
-            hi[2 * e + 1] = fmaxf(hi[2 * e + 1], b);
+            lo[e] = __hmin2(lo[e], x[e]);
+            hi[e] = __hmax2(hi[e], x[e]);
+            amax = __hmax2_nan(amax, __habs2(x[e]));   // (a NaN stays)
         }
     }
-    __syncthreads();
-    if (bad)
-        s_bad = 1;
+    auto other = [](__nv_bfloat162 x, int s) {
+        const uint32_t u = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t *>(&x), s);
+        return *reinterpret_cast<const __nv_bfloat162 *>(&u);
+    };
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        s_lo[r0][col * 8 + e] = lo[e];
-        s_hi[r0][col * 8 + e] = hi[e];
-    }
-    __syncthreads();
-    float a = 0.f, b = 0.f, amax = 0.f;
-    if (tid < D) {
-        a = s_lo[0][tid];
-        b = s_hi[0][tid];
-        for (int r = 1; r < RG; ++r) {
-            a = fminf(a, s_lo[r][tid]);
-            b = fmaxf(b, s_hi[r][tid]);
+    for (int s = C; s < 32; s <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            lo[e] = __hmin2(lo[e], other(lo[e], s));
+            hi[e] = __hmax2(hi[e], other(hi[e], s));
         }
-        amax = fmaxf(fabsf(a), fabsf(b));
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1)
+        amax = __hmax2_nan(amax, other(amax, s));
+    if (lane < C) {
+        *reinterpret_cast<uint4 *>(&s_lo[warp][col * 8]) = *reinterpret_cast<const uint4 *>(lo);
+        *reinterpret_cast<uint4 *>(&s_hi[warp][col * 8]) = *reinterpret_cast<const uint4 *>(hi);
     }
-    for (int s = 16; s > 0; s >>= 1)
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, s));
-    if ((tid & 31) == 0)
-        s_max[tid >> 5] = amax;
+    if (lane == 0) {
+        const float a = __low2float(amax), b = __high2float(amax);
+        s_max[warp] = a != a || b != b ? __int_as_float(0x7f800000) : fmaxf(a, b);
+    }
     __syncthreads();
-    amax = 0.f;
-    for (int w = 0; w < kBoundsThreads / 32; ++w)
-        amax = fmaxf(amax, s_max[w]);
-    const bool unknown = s_bad != 0;
-    const float scale = unknown ? __int_as_float(0x7f800000) : scale_of(amax);
+    float most = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+        most = fmaxf(most, s_max[w]);
+    const bool unknown = !(most <= kLargest);
+    const float scale = unknown ? __int_as_float(0x7f800000) : scale_of(most);
     const size_t at = static_cast<size_t>(seg) * p.n_blocks + blk;
-    if (tid < D) {
+    // four channels a thread: their least, then their largest codes
+    if (tid < D / 2) {
+        const bool upper = tid >= D / 4;
+        const int c = (upper ? tid - D / 4 : tid) * 4;
         const float inv = unknown ? 0.f : inverse_power(scale);   // exact quotients
-        p.bounds[at * 2 * D + tid] = unknown ? -127 : static_cast<int8_t>(floorf(a * inv));
-        p.bounds[at * 2 * D + D + tid] = unknown ? 127 : static_cast<int8_t>(ceilf(b * inv));
+        uint32_t codes = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            __nv_bfloat16 x = upper ? s_hi[0][c + e] : s_lo[0][c + e];
+#pragma unroll
+            for (int w = 1; w < W; ++w)
+                x = upper ? __hmax(x, s_hi[w][c + e]) : __hmin(x, s_lo[w][c + e]);
+            const float y = __bfloat162float(x) * inv;
+            const int code = unknown ? (upper ? 127 : -127) : static_cast<int>(upper ? ceilf(y) : floorf(y));
+            codes |= (static_cast<uint32_t>(code) & 255u) << (8 * e);
+        }
+        *reinterpret_cast<uint32_t *>(p.bounds + at * 2 * D + (upper ? D : 0) + c) = codes;
     }
     if (tid == 0)
         p.scales[at] = scale;
 }
 
-// A cluster is one (sequence, KV head): each CTA scores a run of its blocks, a thread a block (dp4a of the
-// codes with the query's positive and negative parts), keeps the scores as ordered keys in shared memory, and
-// the cluster takes the largest (cluster_topk).  Bound by latency for few blocks, else by the bounds' bytes.
+constexpr int kSelectThreads = 512;
+constexpr int kLanes = 4;   // lanes of a block's score
+
+// A cluster is one (sequence, KV head): each CTA scores a run of its blocks, four lanes a block (dp4a of the
+// codes with the query's positive and negative parts; 64 bytes a load), keeps the scores as ordered keys in shared
+// memory, and the cluster takes the largest (cluster_topk).  Bound by latency for few blocks, else by the
+// products, 2 D / 4 dp4a a block and head.
 template <int D>
-__global__ void __launch_bounds__(kTopkThreads) select_kernel(const __grid_constant__ SelectParams p)
+__global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_constant__ SelectParams p)
 {
     namespace cg = cooperative_groups;
-    __shared__ TopkShared sh;
+    constexpr int NT = kSelectThreads, C = D / 16 / kLanes;   // 16-byte columns of a lane
+    __shared__ TopkShared<NT> sh;
+    __shared__ unsigned s_mm[2 * NT / 32];
     __shared__ __align__(16) uint32_t s_q[2][MLKV_MAX_GROUP][D / 4];   // positive, negative part
     __shared__ float s_f[MLKV_MAX_GROUP];                              // 2^f, 0: no say
     extern __shared__ unsigned s_key[];
@@ -143,18 +155,43 @@ __global__ void __launch_bounds__(kTopkThreads) select_kernel(const __grid_const
     const int beta = seg / p.g, j = seg - beta * p.g;
     const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = tid >> 5;
     const int count = (p.seq_len[beta] + kBlock - 1) / kBlock;
-    const int per = (count + size - 1) / size;
-    const int first = min(count, rank * per), n = min(count, first + per) - first;
     int *to = p.blocks + static_cast<size_t>(seg) * p.n_select;
     grid_dependency_wait();
     grid_dependents_launch();
     if (count <= p.n_select) {   // all of them
-        for (int i = rank * kTopkThreads + tid; i < p.n_select; i += size * kTopkThreads)
+        for (int i = rank * NT + tid; i < p.n_select; i += size * NT)
             to[i] = i < count ? i : -1;
         return;
     }
+    // the blocks at either end, which are selected in any case
+    if (rank == 0)
+        for (int i = tid; i < p.n_first + p.n_last; i += NT)
+            to[i < p.n_first ? i : p.n_select - p.n_last + i - p.n_first] =
+                i < p.n_first ? i : count - p.n_last + i - p.n_first;
+    const int want = p.n_select - p.n_first - p.n_last;
+    if (want == 0)
+        return;
+    const int inner = count - p.n_first - p.n_last, per = (inner + size - 1) / size;
+    const int first = p.n_first + min(inner, rank * per), n = min(inner, (rank + 1) * per) - min(inner, rank * per);
+    // a lane's columns of its first block, on the way while the queries are made ready
+    const int part = tid % kLanes;
+    const size_t base = static_cast<size_t>(seg) * p.n_blocks + first;
+    uint4 lo4[C], hi4[C];
+    float scale = 0.f;
+    auto fetch = [&](int i) {
+        if (i >= n)
+            return;
+        const uint4 *lo = reinterpret_cast<const uint4 *>(p.bounds + (base + i) * 2 * D), *hi = lo + D / 16;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            lo4[c] = lo[c * kLanes + part];
+            hi4[c] = hi[c * kLanes + part];
+        }
+        scale = p.scales[base + i];
+    };
+    fetch(tid / kLanes);
     const __nv_bfloat16 *q = p.Q + (static_cast<size_t>(beta) * p.h + static_cast<size_t>(j) * p.G) * D;
-    for (int i = warp; i < p.G; i += kTopkThreads / 32) {
+    for (int i = warp; i < p.G; i += NT / 32) {
         constexpr int E = D / 32;
         float x[E], amax = 0.f;
         bool bad = false;
@@ -179,53 +216,48 @@ __global__ void __launch_bounds__(kTopkThreads) select_kernel(const __grid_const
             s_f[i] = f;
     }
     __syncthreads();
-    for (int i = tid; i < n; i += kTopkThreads) {
-        const int blk = first + i;
-        unsigned key = 0xffffffffu;   // selected in any case
-        if (blk >= p.n_first && blk < count - p.n_last) {
-            const size_t at = static_cast<size_t>(seg) * p.n_blocks + blk;
-            const uint4 *lo = reinterpret_cast<const uint4 *>(p.bounds + at * 2 * D), *hi = lo + D / 16;
-            const float scale = p.scales[at];
-            float best = -__int_as_float(0x7f800000);
-            int sum[MLKV_MAX_GROUP];
+    unsigned least = 0xffffffffu, most = 0u;
+    const int per_round = NT / kLanes;
+    for (int i0 = 0; i0 < n; i0 += per_round) {   // (all lanes stay: they add up in groups)
+        const int i = i0 + tid / kLanes;
+        float best = -__int_as_float(0x7f800000);
+        for (int a = 0; a < p.G; ++a) {
+            int t = 0;
 #pragma unroll
-            for (int a = 0; a < MLKV_MAX_GROUP; ++a)
-                sum[a] = 0;
-#pragma unroll
-            for (int c = 0; c < D / 16; ++c) {
-                const uint4 l4 = lo[c], h4 = hi[c];
-#pragma unroll
-                for (int a = 0; a < MLKV_MAX_GROUP; ++a) {
-                    if (a >= p.G)
-                        break;
-                    const uint4 qp = *reinterpret_cast<const uint4 *>(&s_q[0][a][c * 4]);
-                    const uint4 qn = *reinterpret_cast<const uint4 *>(&s_q[1][a][c * 4]);
-                    int t = sum[a];
-                    t = __dp4a(static_cast<int>(qp.x), static_cast<int>(h4.x), t);
-                    t = __dp4a(static_cast<int>(qp.y), static_cast<int>(h4.y), t);
-                    t = __dp4a(static_cast<int>(qp.z), static_cast<int>(h4.z), t);
-                    t = __dp4a(static_cast<int>(qp.w), static_cast<int>(h4.w), t);
-                    t = __dp4a(static_cast<int>(qn.x), static_cast<int>(l4.x), t);
-                    t = __dp4a(static_cast<int>(qn.y), static_cast<int>(l4.y), t);
-                    t = __dp4a(static_cast<int>(qn.z), static_cast<int>(l4.z), t);
-                    t = __dp4a(static_cast<int>(qn.w), static_cast<int>(l4.w), t);
-                    sum[a] = t;
-                }
+            for (int c = 0; c < C; ++c) {
+                const uint4 qp = *reinterpret_cast<const uint4 *>(&s_q[0][a][(c * kLanes + part) * 4]);
+                const uint4 qn = *reinterpret_cast<const uint4 *>(&s_q[1][a][(c * kLanes + part) * 4]);
+                t = __dp4a(static_cast<int>(qp.x), static_cast<int>(hi4[c].x), t);
+                t = __dp4a(static_cast<int>(qp.y), static_cast<int>(hi4[c].y), t);
+                t = __dp4a(static_cast<int>(qp.z), static_cast<int>(hi4[c].z), t);
+                t = __dp4a(static_cast<int>(qp.w), static_cast<int>(hi4[c].w), t);
+                t = __dp4a(static_cast<int>(qn.x), static_cast<int>(lo4[c].x), t);
+                t = __dp4a(static_cast<int>(qn.y), static_cast<int>(lo4[c].y), t);
+                t = __dp4a(static_cast<int>(qn.z), static_cast<int>(lo4[c].z), t);
+                t = __dp4a(static_cast<int>(qn.w), static_cast<int>(lo4[c].w), t);
             }
-            const bool unknown = scale == __int_as_float(0x7f800000);
 #pragma unroll
-            for (int a = 0; a < MLKV_MAX_GROUP; ++a)
-                if (a < p.G && s_f[a] != 0.f)
-                    best = fmaxf(best, static_cast<float>(sum[a]) * (s_f[a] * scale));
-            // ordered: negative numbers below positive ones, both zeros alike
-            const uint32_t u = __float_as_uint(best + 0.f);
-            key = unknown ? 0xfffffffeu : (u >> 31) ? ~u : u | 0x80000000u;
+            for (int s = 1; s < kLanes; s <<= 1)
+                t += __shfl_xor_sync(0xffffffffu, t, s);
+            if (s_f[a] != 0.f)
+                best = fmaxf(best, static_cast<float>(t) * (s_f[a] * scale));
         }
-        s_key[i] = key;
+        if (i < n) {
+            // ordered: negative numbers below positive ones, both zeros alike; nothing known: before all
+            const uint32_t u = __float_as_uint(best + 0.f);
+            const unsigned key = scale == __int_as_float(0x7f800000) ? 0xffffffffu
+                                 : (u >> 31)                         ? ~u
+                                                                     : u | 0x80000000u;
+            least = min(least, key);
+            most = max(most, key);
+            if (part == 0)
+                s_key[i] = key;
+        }
+        fetch(i + per_round);
     }
-    __syncthreads();
-    cluster_topk(sh, n, static_cast<unsigned>(p.n_select), [&](int i) { return s_key[i]; },
-                 [&](unsigned place, int i) { to[place] = first + i; });
+    block_min_max<NT>(least, most, s_mm);
+    cluster_topk<NT>(sh, n, least, most, static_cast<unsigned>(want), [&](int i) { return s_key[i]; },
+                     [&](unsigned place, int i) { to[p.n_first + place] = first + i; });
 }
 
 constexpr int kMaxCluster = 8;
@@ -265,16 +297,15 @@ cudaError_t prepare_select(int head_dim)
 
 cudaError_t launch_select(int head_dim, const SelectParams &p, int max_blocks, cudaStream_t stream)
 {
-    // CTAs of a cluster: a block a thread where there are that few, fewer CTAs where the clusters alone fill
-    // the GPU.
+    // CTAs of a cluster: two rounds of scores each, fewer CTAs where the clusters alone fill the GPU.
     int size = 1;
-    while (size < kMaxCluster && size * kTopkThreads < max_blocks && p.b * p.g * size < 304)
+    while (size < kMaxCluster && size * 256 < max_blocks && p.b * p.g * size < 152)
         size *= 2;
     while (size < kMaxCluster && static_cast<size_t>((max_blocks + size - 1) / size) * 4 > kSelectSmem)
         size *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.b * p.g * size));
-    cfg.blockDim = dim3(kTopkThreads);
+    cfg.blockDim = dim3(kSelectThreads);
     cfg.dynamicSmemBytes = static_cast<size_t>((max_blocks + size - 1) / size) * 4;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];

@@ -2,7 +2,7 @@
 // `recent` newest positions stay and, of the others, those of the largest weights, `keep` in all, of equal
 // weights the earlier ones; keys, values and weights of what stays move together, in order.
 //
-// Two launches.  keep_kernel selects: a cluster a segment, a radix select over the weights (cluster_topk), whose
+// Two launches.  keep_kernel selects: a cluster a segment, over its weights as ordered keys (cluster_topk), whose
 // result is the list of kept positions.  move_kernel moves: a unit is a run of rows of a segment, which a CTA
 // loads whole before it stores it.  In place, row m takes position kept[m] >= m, so a unit overwrites positions
 // that only units before it, and it itself, still have to read: it stores after those have set their flags.
@@ -26,42 +26,59 @@ __device__ __forceinline__ unsigned weight_key(float w)
     return w != w ? 0xfffffffeu : (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-__global__ void __launch_bounds__(kTopkThreads) keep_kernel(const __grid_constant__ EvictParams p)
+constexpr int kKeepThreads = 1024;
+
+__global__ void __launch_bounds__(kKeepThreads) keep_kernel(const __grid_constant__ EvictParams p)
 {
     namespace cg = cooperative_groups;
-    __shared__ TopkShared sh;
+    constexpr int NT = kKeepThreads;
+    __shared__ TopkShared<NT> sh;
+    __shared__ unsigned s_mm[2 * NT / 32];
     extern __shared__ unsigned s_key[];
     cg::cluster_group cluster = cg::this_cluster();
     const int size = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
     const int seg = static_cast<int>(blockIdx.x) / size, beta = seg / p.g;
     const int tid = static_cast<int>(threadIdx.x);
     const int L = p.seq_len[beta], keep = p.keep[beta];
-    const int per = (L + size - 1) / size;
-    const int first = min(L, rank * per), n = min(L, first + per) - first;
     const float *w = p.weights_in + static_cast<size_t>(seg) * p.src_seq;
     int *kept = p.kept + static_cast<size_t>(seg) * p.k_max;
     grid_dependency_wait();
     grid_dependents_launch();
     // the flags of this segment's units; the first CTA also resets the counter of units
-    for (int i = rank * kTopkThreads + tid; i < p.units; i += size * kTopkThreads)
+    for (int i = rank * NT + tid; i < p.units; i += size * NT)
         p.flags[static_cast<size_t>(seg) * p.units + i] = 0u;
     if (blockIdx.x == 0 && tid == 0)
         p.flags[static_cast<size_t>(p.b) * p.g * p.units] = 0u;
-    if (L <= keep) {   // everything stays
-        for (int i = rank * kTopkThreads + tid; i < L; i += size * kTopkThreads)
-            kept[i] = i;
+    // Everything stays of a shorter sequence, else the newest positions, and the heaviest of the others.
+    const int others = L <= keep ? 0 : L - p.recent, want = L <= keep ? 0 : keep - p.recent;
+    for (int i = rank * NT + tid; i < min(L, keep) - want; i += size * NT)
+        kept[want + i] = others + i;
+    if (want == 0)
         return;
-    }
+    const int per = (others + size - 1) / size;
+    const int first = min(others, rank * per), n = min(others, first + per) - first;
     const bool cached = static_cast<size_t>(per) * 4 <= kKeepSmem;
-    const int newest = L - p.recent;   // from there on everything stays
-    auto key_at = [&](int i) { return first + i >= newest ? 0xffffffffu : weight_key(__ldcg(w + first + i)); };
-    if (cached) {
-        for (int i = tid; i < n; i += kTopkThreads)
-            s_key[i] = key_at(i);
-        __syncthreads();
+    unsigned least = 0xffffffffu, most = 0u;
+    constexpr int U = 8;   // loads in flight
+    for (int i0 = tid; i0 < n; i0 += U * NT) {
+        float x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            x[u] = i0 + u * NT < n ? __ldcg(w + first + i0 + u * NT) : 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i0 + u * NT < n) {
+                const unsigned k = weight_key(x[u]);
+                least = min(least, k);
+                most = max(most, k);
+                if (cached)
+                    s_key[i0 + u * NT] = k;
+            }
     }
-    cluster_topk(sh, n, static_cast<unsigned>(keep), [&](int i) { return cached ? s_key[i] : key_at(i); },
-                 [&](unsigned place, int i) { kept[place] = first + i; });
+    block_min_max<NT>(least, most, s_mm);   // (and the keys are in place)
+    cluster_topk<NT>(sh, n, least, most, static_cast<unsigned>(want),
+                     [&](int i) { return cached ? s_key[i] : weight_key(__ldcg(w + first + i)); },
+                     [&](unsigned place, int i) { kept[place] = first + i; });
 }
 
 constexpr int kMoveThreads = 256;
@@ -215,14 +232,14 @@ cudaError_t prepare_evict()
 cudaError_t launch_evict(int head_dim, const EvictParams &p, int max_len, int sm_count, cudaStream_t stream)
 {
     int size = 1;
-    while (size < kMaxCluster && size * kTopkThreads * 4 < max_len && p.b * p.g * size < 2 * sm_count)
+    while (size < kMaxCluster && size * kKeepThreads * 4 < max_len && p.b * p.g * size < sm_count)
         size *= 2;
     while (size < kMaxCluster && static_cast<size_t>((max_len + size - 1) / size) * 4 > kKeepSmem)
         size *= 2;
     const size_t keys = static_cast<size_t>((max_len + size - 1) / size) * 4;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.b * p.g * size));
-    cfg.blockDim = dim3(kTopkThreads);
+    cfg.blockDim = dim3(kKeepThreads);
     cfg.dynamicSmemBytes = keys <= kKeepSmem ? keys : kKeepSmem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];

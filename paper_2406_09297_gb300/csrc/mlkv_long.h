@@ -41,6 +41,8 @@ struct PieceParams {
     int early;                // the stream's previous kernel is this call's prefix kernel, which writes
                               // neither Q nor the cache and has itself waited for all before it: Q and
                               // the tiles are read before the dependency wait
+    int defer;                // every piece writes its record, launch_merge_pieces merges them: nothing but that
+                              // waits for the prefix kernel, beside which the pieces run
     // kPieceBlocks: block numbers [b][g][n_blocks]; others than those of visible positions are passed over
     const int *blocks;
     int n_blocks;
@@ -59,8 +61,11 @@ cudaError_t prepare_pieces(int head_dim, int mode, int *ctas_per_sm);
 cudaError_t launch_pieces(int head_dim, int mode, const CUtensorMap *tmap, const PieceParams &p,
                           cudaStream_t stream);
 
-// Largest group of segments' records that launch_weights' shared memory holds.
-constexpr int kWeightsMaxRecords = 700;   // (700 + 1) * 16 heads * 4 bytes < 48 KB
+// The merge of a deferred kPieceSuffix launch's segments, of `most` records at most.
+cudaError_t launch_merge_pieces(int head_dim, const PieceParams &p, int most, cudaStream_t stream);
+
+// Most records of a segment that launch_merge_pieces and launch_weights take.
+constexpr int kDeferMaxRecords = 700;   // (700 + 1) * 16 heads * 4 bytes < 48 KB
 
 // Packs the queries of places [0, n): place i is sequence seq[i].
 struct PackParams {

@@ -104,7 +104,7 @@ void fill_pieces(const mlkv_cache *c, int layer, const void *Q, void *out, const
     p.G = c->G;
     p.slot = c->slot[layer];
     p.pre_o = p.pre_lse = nullptr;
-    p.pre_chunks = p.early = 0;
+    p.pre_chunks = p.early = p.defer = 0;
     p.blocks = nullptr;
     p.n_blocks = 0;
     p.scores = nullptr;
@@ -126,11 +126,20 @@ int scratch(mlkv_cache *c, size_t floats, const char *what, cudaStream_t stream)
     return mlkv::grow_scratch(c, floats, what);
 }
 
-// Key tiles of 128 positions of a unit of the decode over shared prefixes, for `pairs` unit columns (pairs of query
-// tiles times KV heads) over prefixes of n_kt tiles: the least estimated time of ceil(units / SMs) rounds of
-// kc tiles and a start and end worth 3.
-int plan_prefix_chunk(const int *n_kt, const int *pairs, int n, int sm_count)
+// How the decode over shared prefixes is launched.
+struct PrefixPlan {
+    int kc;       // key tiles of 128 positions of a unit
+    int sms;      // CTAs of the prefix kernel, one an SM
+    bool beside;  // the suffixes run beside it on the other SMs, and are merged by a launch of their own
+};
+
+// For `pairs` unit columns (pairs of query tiles times KV heads) over prefixes of n_kt tiles, and suffixes of
+// `bytes`: the least estimated time.  Microseconds: a unit's key tile `tile`, its start and end three of them; the
+// suffixes at most `rate` bytes a us an SM and `all` in total.  (The prefix kernel is bound by the tensor cores where
+// many sequences share one, the suffixes by HBM: side by side, each has what the other leaves.)
+PrefixPlan plan_prefix(const int *n_kt, const int *pairs, int n, int sm_count, int d, double bytes)
 {
+    const double tile = d == 64 ? 0.65 : 1.25, rate = 65e3, all = 6.5e6, merge = 5.0;
     long long work = 0;
     int longest = 1;
     for (int x = 0; x < n; ++x) {
@@ -138,17 +147,26 @@ int plan_prefix_chunk(const int *n_kt, const int *pairs, int n, int sm_count)
         if (pairs[x] > 0)
             longest = std::max(longest, n_kt[x]);
     }
-    int best = longest;
-    double best_t = 1e30;
     const int least = std::max(1, (longest + mlkv::kFusedMaxChunks - 1) / mlkv::kFusedMaxChunks);
+    PrefixPlan best = {longest, sm_count, false};
+    double best_t = 1e30;
     for (int kc = std::max<long long>(least, work / (4LL * sm_count)); kc <= longest; kc += (kc + 15) / 16) {
         long long units = 0;
         for (int x = 0; x < n; ++x)
             units += static_cast<long long>((n_kt[x] + kc - 1) / kc) * pairs[x];
-        const double t = static_cast<double>((units + sm_count - 1) / sm_count) * (kc + 3);
-        if (t < best_t) {
-            best_t = t;
-            best = kc;
+        for (int eighths = 8; eighths >= 2; --eighths) {
+            const int sms = sm_count * eighths / 8;
+            double t = static_cast<double>((units + sms - 1) / sms) * (kc + 3) * tile;
+            if (eighths == 8) {
+                t += bytes / all;
+            } else {
+                const double beside = t * std::min(all, rate * (sm_count - sms));
+                t += std::max(0.0, bytes - beside) / all + merge;
+            }
+            if (t < best_t) {
+                best_t = t;
+                best = {kc, sms, eighths < 8};
+            }
         }
     }
     return best;
@@ -256,7 +274,12 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
                 return fail_cuda(e, "preparing the decode over a shared prefix");
             c->long_ready |= kReadyShared;
         }
-        const int kc = plan_prefix_chunk(n_kt, pairs, np, c->sm_count);
+        double bytes = 0;   // of the suffixes
+        for (int beta = 0; beta < c->b; ++beta)
+            bytes += 4.0 * c->g * c->d * seq_lens[beta];
+        const PrefixPlan plan = plan_prefix(n_kt, pairs, np, c->sm_count, c->d, bytes);
+        const int kc = plan.kc;
+        p.defer = plan.beside ? 1 : 0;
         cmax = (most_kt + kc - 1) / kc;
         const size_t rows = static_cast<size_t>(places) * c->g * cmax * c->G;
         const size_t packed = neighbours ? 0 : static_cast<size_t>(places) * c->h * c->d / 2;   // in floats
@@ -317,7 +340,7 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
         u.s_max = prefix->max_seq;
         u.slot = p.slot;
         u.head_pairs = 0;
-        u.sm_count = c->sm_count;
+        u.sm_count = plan.sms;
         u.window = u.sinks = 0;
         u.kv_direct = 0;
         u.fused_L = places;
@@ -362,10 +385,20 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
     } else {
         std::fill(p.pre_n, p.pre_n + c->b, static_cast<uint16_t>(0));
     }
-    cut(c, p, mlkv::piece_max_records(c->d, c->G) - cmax,
+    const int most = std::min(mlkv::piece_max_records(c->d, c->G), mlkv::kDeferMaxRecords);
+    cut(c, p, most - cmax,
         [&](int beta) { return static_cast<int>((static_cast<unsigned>(seq_lens[beta]) + 63) / 64); });
-    const cudaError_t e = mlkv::launch_pieces(c->d, mlkv::kPieceSuffix, rows64(c), p, stream);
-    return e == cudaSuccess ? MLKV_OK : fail_cuda(e, "suffix decode launch");
+    cudaError_t e = mlkv::launch_pieces(c->d, mlkv::kPieceSuffix, rows64(c), p, stream);
+    if (e != cudaSuccess)
+        return fail_cuda(e, "suffix decode launch");
+    if (p.defer) {
+        int records = 0;
+        for (int beta = 0; beta < c->b; ++beta)
+            records = std::max(records, (p.first[beta + 1] - p.first[beta]) / c->g + p.pre_n[beta]);
+        if ((e = mlkv::launch_merge_pieces(c->d, p, records, stream)) != cudaSuccess)
+            return fail_cuda(e, "merge launch");
+    }
+    return MLKV_OK;
 }
 
 int mlkv_block_bounds(mlkv_cache_t c, int layer, const int *first, const int *seq_lens, void *bounds,
@@ -517,7 +550,7 @@ int mlkv_decode_attention_weights(mlkv_cache_t c, int layer, const void *Q, void
     if ((rc = scratch(c, static_cast<size_t>(c->b) * c->h * p.score_stride, "scores", stream)) != MLKV_OK)
         return rc;
     p.scores = c->fused_part;
-    cut(c, p, mlkv::kWeightsMaxRecords,
+    cut(c, p, mlkv::kDeferMaxRecords,
         [&](int beta) { return static_cast<int>((static_cast<unsigned>(seq_lens[beta]) + 63) / 64); });
     mlkv::WeightsParams w;
     w.weights_in = weights_in;

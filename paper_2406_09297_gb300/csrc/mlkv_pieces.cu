@@ -396,10 +396,11 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     consumer_bar_sync<kWarps>();
     if (flag[2])
         return;
-    if (early)
-        grid_dependency_wait();
+    if (early && (!p.defer || blockIdx.x == gridDim.x - 1))
+        grid_dependency_wait();   // (deferred merge: one CTA, so that this grid ends behind the prefix's)
     const int n_pre = kMode == kPieceSuffix ? p.pre_n[x.beta] : 0;
-    const bool whole = kMode != kPieceWeights && x.count == 1 && n_pre == 0;
+    const bool defer = kMode == kPieceWeights || (kMode == kPieceSuffix && p.defer);
+    const bool whole = !defer && x.count == 1 && n_pre == 0;
     const size_t rec = blockIdx.x;
     __nv_bfloat16 *ob = p.out + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * p.G) * D;
     for (int i = tid * 4; i < p.G * D; i += kWarps * 32 * 4) {
@@ -440,7 +441,7 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
                 p.part_lse[rec * p.G + row] = tot == 0.f ? neg_inf() : mx + log2f(tot);
         }
     }
-    if (whole || kMode == kPieceWeights)
+    if (whole || defer)
         return;
     if (x.count > 1) {
         __threadfence();
@@ -460,6 +461,24 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     merge_records<D>(p, x, rec - x.index, n_pre, reinterpret_cast<float *>(smem), tid, kWarps * 32);
 }
 
+// The merge of a deferred suffix launch: a CTA a segment.  Bound by the records' bytes, in L2.
+constexpr int kMergeThreads = 128;
+template <int D>
+__global__ void __launch_bounds__(kMergeThreads) merge_kernel(const __grid_constant__ PieceParams p)
+{
+    extern __shared__ float s_w[];
+    Piece x;
+    x.seg = static_cast<int>(blockIdx.x);
+    x.beta = x.seg / p.g;
+    x.j = x.seg - x.beta * p.g;
+    x.L = p.seq_len[x.beta];
+    x.count = (((x.L + T - 1) / T) + p.tiles - 1) / p.tiles;
+    grid_dependency_wait();
+    grid_dependents_launch();
+    merge_records<D>(p, x, static_cast<size_t>(p.first[x.beta]) + static_cast<size_t>(x.j) * x.count,
+                     p.pre_n[x.beta], s_w, static_cast<int>(threadIdx.x), kMergeThreads);
+}
+
 // --------------------------------------------------------------------------------------------------
 // kPieceWeights: what each position got
 // --------------------------------------------------------------------------------------------------
@@ -468,7 +487,7 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
 // where they fit).
 constexpr int kWeightThreads = 256;
 template <int D>
-__global__ void __launch_bounds__(kWeightThreads)
+__global__ void __launch_bounds__(kWeightThreads, 6)
     weights_kernel(const __grid_constant__ PieceParams p, const __grid_constant__ WeightsParams w)
 {
     __shared__ float s_lse[16];
@@ -513,13 +532,36 @@ __global__ void __launch_bounds__(kWeightThreads)
         __syncthreads();
     }
     const float *sc = p.scores + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * G) * p.score_stride;
-    for (int u = u0 + tid; u < u1; u += kWeightThreads) {
-        float a = 0.f;
-        if (u < x.L)
-            for (int i = 0; i < G; ++i)
-                a += exp2f(__ldcg(sc + i * p.score_stride + u) - s_lse[i]);
-        const float before = w.weights_in != nullptr ? w.weights_in[row + u] : 0.f;
-        w.weights_out[row + u] = before + a;
+    constexpr int U = 4;   // positions of a thread at a time
+    for (int v = u0 + tid; v < u1; v += U * kWeightThreads) {
+        float a[U], before[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int u = v + k * kWeightThreads;
+            before[k] = w.weights_in != nullptr && u < u1 ? w.weights_in[row + u] : 0.f;
+            a[k] = 0.f;
+        }
+        if (v < x.L) {
+#pragma unroll 4
+            for (int i = 0; i < G; ++i) {
+                const float lse = s_lse[i];
+                float s[U];
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    const int u = v + k * kWeightThreads;
+                    s[k] = u < x.L ? __ldcg(sc + i * p.score_stride + u) : neg_inf();
+                }
+#pragma unroll
+                for (int k = 0; k < U; ++k)
+                    a[k] += exp2f(s[k] - lse);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int u = v + k * kWeightThreads;
+            if (u < u1)
+                w.weights_out[row + u] = before[k] + (u < x.L ? a[k] : 0.f);   // (a NaN ends with its sequence)
+        }
     }
 }
 
@@ -588,6 +630,15 @@ cudaError_t launch_pieces(int head_dim, int mode, const CUtensorMap *tmap, const
     void *args[] = {const_cast<CUtensorMap *>(tmap), const_cast<PieceParams *>(&p)};
     return launch_pdl(piece_fn(head_dim, mode), dim3(static_cast<unsigned>(p.first[p.b])), piece_threads(head_dim),
                       piece_smem(head_dim), stream, args);
+}
+
+cudaError_t launch_merge_pieces(int head_dim, const PieceParams &p, int most, cudaStream_t stream)
+{
+    const size_t smem = sizeof(float) * (static_cast<size_t>(most) + 1) * p.G;
+    void *args[] = {const_cast<PieceParams *>(&p)};
+    return launch_pdl(head_dim == 64 ? reinterpret_cast<const void *>(&merge_kernel<64>)
+                                     : reinterpret_cast<const void *>(&merge_kernel<128>),
+                      dim3(static_cast<unsigned>(p.b) * p.g), kMergeThreads, smem, stream, args);
 }
 
 cudaError_t launch_weights(int head_dim, const PieceParams &p, const WeightsParams &w, int max_len,

@@ -1,6 +1,12 @@
-// The n largest of a list of 32-bit keys that a thread-block cluster holds, in the order of the list: a radix
-// select of four digits of eight bits.  Of equal keys the first ones are taken, so that the selection does not
-// depend on how the list is split.  Used by the block selection and the eviction.  Internal.
+// The n largest of a list of 32-bit keys that a thread-block cluster holds, in the order of the list.  Of equal
+// keys the first ones are taken, so that the selection does not depend on how the list is split.  Used by
+// the block selection and the eviction.  Internal.
+//
+// The last key taken is found by histograms of 1024 equal intervals between the least and the largest key, then
+// of the interval that holds it, and so on until all of an interval's keys are taken or it is one key wide: two
+// rounds for weights or scores as they come, at most four.  (Digits of eight bits, from the top: the keys are floats
+// whose upper digit is an exponent that most share, and four rounds are always four: eviction from 16 sequences of
+// up to 16,384 positions, 8 KV heads, 26.4 us a selection.)
 #pragma once
 
 #include <cooperative_groups.h>
@@ -10,132 +16,148 @@
 namespace mlkv {
 namespace {
 
-constexpr int kTopkThreads = 512;
+constexpr int kTopkBins = 1024;
 
+template <int NT>
 struct TopkShared {
-    unsigned hist[2][256];   // of this CTA's keys, by digit; the digits take turns
-    unsigned sum[256];       // of the cluster's, from this digit up
-    unsigned digit, above;   // the digit of the last key taken; keys above it
-    unsigned gt, eq;         // this CTA's keys above the last one taken, and equal to it
-    unsigned warp_gt[kTopkThreads / 32], warp_eq[kTopkThreads / 32];
+    unsigned hist[2][kTopkBins];   // of this CTA's keys; the rounds take turns
+    unsigned warp[NT / 32];
+    unsigned lo, hi;               // least and largest key of this CTA
+    unsigned bin, above, inside;   // interval of the last key taken; keys above it, and in it
+    unsigned gt, eq;               // this CTA's keys above the last one taken, and equal to it
+    unsigned warp_gt[NT / 32], warp_eq[NT / 32];
 };
 
-// CTA `rank` of `size` holds keys key(0) .. key(n - 1), the list's first_index and following ones; the cluster
-// holds at least `want` >= 1 keys.  Calls put(place, i) for every one of its keys among the `want` largest, place
-// its rank in the list's order among those.  All threads of the cluster call it.
-template <typename Key, typename Put>
-__device__ void cluster_topk(TopkShared &sh, int n, unsigned want, const Key &key, const Put &put)
+// CTA `rank` of a cluster of `size` holds keys key(0) .. key(n - 1), whose least and largest are lo and hi in
+// all threads (0xffffffff and 0 of none); the cluster holds at least `want` >= 1 keys.  Calls put(place, i) for
+// every one of its keys among the `want` largest, place its rank in the list's order among those.  All NT >= 256
+// threads of all the cluster's CTAs call it, behind a barrier for the keys.
+template <int NT, typename Key, typename Put>
+__device__ void cluster_topk(TopkShared<NT> &sh, int n, unsigned lo, unsigned hi, unsigned want, const Key &key,
+                             const Put &put)
 {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     const unsigned size = cluster.num_blocks(), rank = cluster.block_rank();
     const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = tid >> 5;
-    constexpr int W = kTopkThreads / 32;
+    constexpr int W = NT / 32;
     auto sync = [&] {
         if (size > 1)
             cluster.sync();
         else
             __syncthreads();
     };
-    unsigned prefix = 0, left = want;   // the last taken key's upper digits; keys still to take below
-    for (int d = 3; d >= 0; --d) {
-        unsigned *hist = sh.hist[d & 1];
-        if (tid < 256)
-            hist[tid] = 0;
+    for (int b = tid; b < kTopkBins; b += NT)
+        sh.hist[0][b] = 0;
+    if (size > 1) {
+        if (tid == 0) {
+            sh.lo = lo;
+            sh.hi = hi;
+        }
+        cluster.sync();
+        for (unsigned c = 0; c < size; ++c) {
+            lo = min(lo, *cluster.map_shared_rank(&sh.lo, c));
+            hi = max(hi, *cluster.map_shared_rank(&sh.hi, c));
+        }
+    } else {
         __syncthreads();
-        const unsigned high = d == 3 ? 0u : ~0u << (8 * (d + 1));
-        for (int base = warp * 32; base < n; base += kTopkThreads) {
-            const unsigned k = base + lane < n ? key(base + lane) : 0u;
-            const unsigned b = (k >> (8 * d)) & 255u;
-            const bool in = base + lane < n && (k & high) == prefix;
-            // (many keys share a digit: one addition for the lanes that agree with the warp's first)
-            const unsigned live = __ballot_sync(0xffffffffu, in);
-            if (live == 0)
-                continue;
-            const int lead = __ffs(static_cast<int>(live)) - 1;
-            const unsigned b0 = __shfl_sync(0xffffffffu, b, lead);
-            const unsigned same = __ballot_sync(0xffffffffu, in && b == b0);
-            if (in && b != b0)
-                atomicAdd(&hist[b], 1u);
-            else if (lane == lead)
-                atomicAdd(&hist[b0], static_cast<unsigned>(__popc(same)));
+    }
+    unsigned left = want;   // keys still to take of [lo, hi]
+    bool all = false;       // every key of [lo, hi] is taken
+    for (int round = 0; !all && lo != hi; ++round) {
+        unsigned *hist = sh.hist[round & 1];
+        const int s = max(0, 22 - __clz(static_cast<int>(hi - lo)));   // (hi - lo) >> s below 1024
+        for (int i = tid; i < n; i += NT) {
+            const unsigned k = key(i);
+            if (k >= lo && k <= hi)
+                atomicAdd(&hist[(k - lo) >> s], 1u);
         }
         sync();
-        if (tid < 256) {
-            unsigned t = 0;
-            for (unsigned c = 0; c < size; ++c)
-                t += *cluster.map_shared_rank(&hist[tid], c);
-            sh.sum[tid] = t;
-        }
-        __syncthreads();
-        if (warp == 0) {
-            // from the top: lane i takes digits 255 - 8 i downwards
-            unsigned mine = 0;
-            for (int k = 0; k < 8; ++k)
-                mine += sh.sum[255 - 8 * lane - k];
-            unsigned up = mine;   // keys of this lane's digits and those above
-            for (int s = 1; s < 32; s <<= 1) {
-                const unsigned o = __shfl_up_sync(0xffffffffu, up, s);
-                if (lane >= s)
-                    up += o;
+        // the cluster's counts from the top: thread t takes the kPer intervals below kTopkBins - kPer t
+        constexpr int kPer = kTopkBins >= NT ? kTopkBins / NT : 1;
+        unsigned mine[kPer], total = 0;
+        const bool has = tid * kPer < kTopkBins;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            mine[k] = 0;
+            if (has) {
+                const int b = kTopkBins - 1 - tid * kPer - k;
+                for (unsigned c = 0; c < size; ++c)
+                    mine[k] += size > 1 ? *cluster.map_shared_rank(&hist[b], c) : hist[b];
             }
-            unsigned above = up - mine;
-            if (above < left && left <= up) {
-                for (int k = 0; k < 8; ++k) {
-                    const unsigned c = sh.sum[255 - 8 * lane - k];
-                    if (above + c >= left) {
-                        sh.digit = 255u - 8u * lane - k;
-                        sh.above = above;
-                        break;
-                    }
-                    above += c;
+            total += mine[k];
+        }
+        for (int b = tid; b < kTopkBins; b += NT)
+            sh.hist[(round + 1) & 1][b] = 0;   // (read last before the sync above)
+        unsigned up = total;
+        for (int d = 1; d < 32; d <<= 1) {
+            const unsigned o = __shfl_up_sync(0xffffffffu, up, d);
+            if (lane >= d)
+                up += o;
+        }
+        if (lane == 31)
+            sh.warp[warp] = up;
+        __syncthreads();
+        unsigned before = lane < W && lane < warp ? sh.warp[lane] : 0;
+        before = __reduce_add_sync(0xffffffffu, before);
+        unsigned above = before + up - total;
+        if (above < left && left <= before + up) {
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                if (above < left && left <= above + mine[k]) {
+                    sh.bin = static_cast<unsigned>(kTopkBins - 1 - tid * kPer - k);
+                    sh.above = above;
+                    sh.inside = mine[k];
                 }
+                above += mine[k];
             }
         }
         __syncthreads();
-        prefix |= sh.digit << (8 * d);
         left -= sh.above;
+        all = sh.inside == left;
+        lo += sh.bin << s;
+        hi = min(hi, lo + ((1u << s) - 1u));
     }
-    // Keys above `prefix` are taken, and the first `left` that equal it.  Each warp has a run of the CTA's keys.
+    // Keys above `top` are taken, and the first `left` that equal it (none where whole intervals are taken).  Each
+    // warp has a run of the CTA's keys.
+    const unsigned top = all ? lo - 1u : lo;   // (all of [0, hi]: every key, and above 0xffffffff is none)
+    const bool every = all && lo == 0u;
+    if (all)
+        left = 0;
     const int run = ((n + W - 1) / W + 31) & ~31;
     const int i0 = min(n, warp * run), i1 = min(n, i0 + run);
     unsigned gt = 0, eq = 0;
     for (int i = i0 + lane; i < i1; i += 32) {
         const unsigned k = key(i);
-        gt += k > prefix;
-        eq += k == prefix;
+        gt += every || k > top;
+        eq += !all && k == top;
     }
-    for (int s = 16; s > 0; s >>= 1) {
-        gt += __shfl_xor_sync(0xffffffffu, gt, s);
-        eq += __shfl_xor_sync(0xffffffffu, eq, s);
-    }
+    gt = __reduce_add_sync(0xffffffffu, gt);
+    eq = __reduce_add_sync(0xffffffffu, eq);
     if (lane == 0) {
         sh.warp_gt[warp] = gt;
         sh.warp_eq[warp] = eq;
     }
     __syncthreads();
-    if (tid == 0) {
-        unsigned a = 0, b = 0;
-        for (int w = 0; w < W; ++w) {
-            a += sh.warp_gt[w];
-            b += sh.warp_eq[w];
+    const unsigned a = lane < W ? sh.warp_gt[lane] : 0u, b = lane < W ? sh.warp_eq[lane] : 0u;
+    unsigned gt0 = __reduce_add_sync(0xffffffffu, lane < warp ? a : 0u);   // before this warp's run
+    unsigned eq0 = __reduce_add_sync(0xffffffffu, lane < warp ? b : 0u);
+    if (size > 1) {
+        const unsigned ga = __reduce_add_sync(0xffffffffu, a), ea = __reduce_add_sync(0xffffffffu, b);
+        if (tid == 0) {
+            sh.gt = ga;
+            sh.eq = ea;
         }
-        sh.gt = a;
-        sh.eq = b;
-    }
-    sync();
-    unsigned gt0 = 0, eq0 = 0;   // before this warp's run
-    for (unsigned c = 0; c < rank; ++c) {
-        gt0 += *cluster.map_shared_rank(&sh.gt, c);
-        eq0 += *cluster.map_shared_rank(&sh.eq, c);
-    }
-    for (int w = 0; w < warp; ++w) {
-        gt0 += sh.warp_gt[w];
-        eq0 += sh.warp_eq[w];
+        cluster.sync();
+        for (unsigned c = 0; c < rank; ++c) {
+            gt0 += *cluster.map_shared_rank(&sh.gt, c);
+            eq0 += *cluster.map_shared_rank(&sh.eq, c);
+        }
     }
     for (int i = i0; i < i1; i += 32) {
-        const unsigned k = i + lane < i1 ? key(i + lane) : 0u;
-        const bool is_gt = i + lane < i1 && k > prefix, is_eq = i + lane < i1 && k == prefix;
+        const bool in = i + lane < i1;
+        const unsigned k = in ? key(i + lane) : 0u;
+        const bool is_gt = in && (every || k > top), is_eq = in && !all && k == top;
         const unsigned bg = __ballot_sync(0xffffffffu, is_gt), be = __ballot_sync(0xffffffffu, is_eq);
         const unsigned below = (1u << lane) - 1u;
         const unsigned g = gt0 + __popc(bg & below), e = eq0 + __popc(be & below);
@@ -146,6 +168,22 @@ __device__ void cluster_topk(TopkShared &sh, int n, unsigned want, const Key &ke
     }
     if (size > 1)
         cluster.sync();   // no CTA leaves while its counts are read
+}
+
+// The least and the largest over the CTA's threads; s: room for 2 * NT / 32 numbers.
+template <int NT>
+__device__ __forceinline__ void block_min_max(unsigned &lo, unsigned &hi, unsigned *s)
+{
+    const int lane = static_cast<int>(threadIdx.x) & 31, warp = static_cast<int>(threadIdx.x) >> 5;
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    if (lane == 0) {
+        s[warp] = lo;
+        s[NT / 32 + warp] = hi;
+    }
+    __syncthreads();
+    lo = __reduce_min_sync(0xffffffffu, lane < NT / 32 ? s[lane] : 0xffffffffu);
+    hi = __reduce_max_sync(0xffffffffu, lane < NT / 32 ? s[NT / 32 + lane] : 0u);
 }
 
 }  // namespace
