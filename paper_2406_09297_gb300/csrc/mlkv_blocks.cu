@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_con
                      [&](unsigned place, int i) { to[p.n_first + place] = first + i; });
 }
 
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = kTopkCluster;
 constexpr size_t kSelectSmem = 160 * 1024;
 
 template <int D>

@@ -17,7 +17,7 @@ namespace mlkv {
 namespace {
 
 constexpr size_t kKeepSmem = 128 * 1024;   // keys of a CTA that fit in shared memory
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = kTopkCluster;
 
 // Ordered as the weights, both zeros alike, NaN above infinity.
 __device__ __forceinline__ unsigned weight_key(float w)
@@ -232,7 +232,7 @@ cudaError_t prepare_evict()
 cudaError_t launch_evict(int head_dim, const EvictParams &p, int max_len, int sm_count, cudaStream_t stream)
 {
     int size = 1;
-    while (size < kMaxCluster && size * kKeepThreads * 4 < max_len && p.b * p.g * size < sm_count)
+    while (size < kMaxCluster && size * kKeepThreads * 4 < max_len && 2 * p.b * p.g * size <= sm_count)
         size *= 2;
     while (size < kMaxCluster && static_cast<size_t>((max_len + size - 1) / size) * 4 > kKeepSmem)
         size *= 2;

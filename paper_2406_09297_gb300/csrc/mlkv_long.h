@@ -56,8 +56,8 @@ struct PieceParams {
 };
 // Most records (pieces and a prefix's) that a segment's merge holds the weights of.
 int piece_max_records(int head_dim, int group);
-int piece_warps(int head_dim);   // consumer warps: tiles of a piece that are worked on at a time
-cudaError_t prepare_pieces(int head_dim, int mode, int *ctas_per_sm);
+int piece_stages(int head_dim);   // tiles of a piece that are worked on at a time
+cudaError_t prepare_pieces(int head_dim, int group, int mode, int *ctas_per_sm);
 cudaError_t launch_pieces(int head_dim, int mode, const CUtensorMap *tmap, const PieceParams &p,
                           cudaStream_t stream);
 

@@ -46,7 +46,7 @@ int prepare_pieces(mlkv_cache *c, int mode)
     const unsigned bit = kReadyPieces << mode;
     if (c->long_ready & bit)
         return MLKV_OK;
-    const cudaError_t e = mlkv::prepare_pieces(c->d, mode, &c->piece_ctas);
+    const cudaError_t e = mlkv::prepare_pieces(c->d, c->G, mode, &c->piece_ctas);
     if (e != cudaSuccess)
         return fail_cuda(e, "preparing the piece kernel");
     if (c->piece_ctas < 1)
@@ -70,7 +70,7 @@ void cut(const mlkv_cache *c, mlkv::PieceParams &p, int most, const Tiles &nt)
     total *= c->g;
     const long long slots = static_cast<long long>(c->piece_ctas) * c->sm_count;
     const long long want = std::min(c->records, total <= 32 * slots ? slots : 4 * slots);
-    int tiles = static_cast<int>(std::max<long long>(mlkv::piece_warps(c->d), (total + want - 1) / want));
+    int tiles = static_cast<int>(std::max<long long>(mlkv::piece_stages(c->d), (total + want - 1) / want));
     tiles = std::max(tiles, (longest + most - 1) / most);
     for (;; tiles += (tiles + 7) / 8) {
         long long n = 0;

@@ -27,9 +27,11 @@ template <int D>
 struct PiecePlan {
     static constexpr int kTile = T * D * 2;            // K or V of a tile
     static constexpr int kStages = D == 64 ? 6 : 3;
-    // Consumer warps: one a stage.  (A stage's barrier tells two of its phases apart, so whoever waits for one has
-    // to have seen the one before.)
-    static constexpr int kWarps = kStages;
+    // Consumer warps: the same ones for a stage throughout.  (A stage's barrier tells two of its phases apart, so
+    // whoever waits for one has to have seen the one before.)
+    static constexpr int kPerStage = D == 64 ? 1 : 2;
+    static constexpr int kWarps = kStages * kPerStage;
+    static constexpr int kKeys = T / kPerStage;        // of a warp and tile
     static constexpr int kThreads = (kWarps + 1) * 32;
     static constexpr int kBars = kStages * 2 * kTile;  // full[], empty[]
     static constexpr int kML = kBars + 2 * 8 * kStages;   // float [kWarps][2][16]
@@ -142,7 +144,8 @@ __device__ void merge_records(const PieceParams &p, const Piece &x, size_t own0,
     }
 }
 
-template <int D, int kMode>
+// NH: groups of eight query heads, 1 or 2.
+template <int D, int kMode, int NH>
 __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     piece_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ PieceParams p)
 {
@@ -156,7 +159,7 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
             mbar_init(bar_full + 8 * s, 1);
-            mbar_init(bar_empty + 8 * s, 1);
+            mbar_init(bar_empty + 8 * s, PL::kPerStage);
         }
         flag[0] = 0;   // a wait gave up
         fence_barrier_init();
@@ -224,25 +227,40 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     }
 
     // -------------------------------------- consumers -------------------------------------------
-    const int r0 = lane >> 2;   // this lane's rows: heads r0 and r0 + 8
-    uint32_t qf[D / 16][4];
+    // Transposed: S^T = K Q^T has the warp's keys as rows and the heads as columns, O^T = V^T P the channels as rows, so
+    // that up to eight heads take half the products of heads as 16 rows.  A lane holds heads 2 q and 2 q + 1 of a group
+    // of eight (q = lane % 4), keys or channels lane / 4 and 8 more of 16.
+    constexpr int M = PL::kKeys / 16;
+    const int half = warp % PL::kPerStage * PL::kKeys;   // the warp's first key of a tile
+    uint32_t qf[D / 16][NH][2];   // columns n = lane / 4
     {
         const __nv_bfloat16 *q = p.Q + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * p.G) * D;
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = r0 + (i & 1) * 8, ch = kk * 16 + (i >> 1) * 8 + (lane & 3) * 2;
-                qf[kk][i] = row < p.G ? *reinterpret_cast<const uint32_t *>(q + row * D + ch) : 0u;
-            }
+            for (int nh = 0; nh < NH; ++nh)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int head = nh * 8 + (lane >> 2), ch = kk * 16 + i * 8 + (lane & 3) * 2;
+                    qf[kk][nh][i] = head < p.G ? *reinterpret_cast<const uint32_t *>(q + head * D + ch) : 0u;
+                }
     }
-    float m[2] = {neg_inf(), neg_inf()}, l[2] = {0.f, 0.f};
-    float o[D / 8][4];
+    float m[NH][2], l[NH][2];
+    float o[D / 16][NH][4];
 #pragma unroll
-    for (int c = 0; c < D / 8; ++c)
+    for (int nh = 0; nh < NH; ++nh) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            o[c][e] = 0.f;
+        for (int i = 0; i < 2; ++i) {
+            m[nh][i] = neg_inf();
+            l[nh][i] = 0.f;
+        }
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                o[c][nh][e] = 0.f;
+    }
+    const int mi = lane >> 3, mr = lane & 7;   // ldmatrix: matrix and row of this lane's address
     int idx = 0;
     bool ok = true;
     for (int t = x.t0; t < x.t1; ++t) {
@@ -251,7 +269,7 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
             continue;
         const int mine = idx++;
         const int s = mine % S;
-        if (s != warp)
+        if (s != warp / PL::kPerStage)
             continue;
         if (!mbar_wait(bar_full + 8 * s, (mine / S) & 1))
             ok = false;
@@ -264,105 +282,122 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
             break;
         }
         const uint32_t kb = sbase + s * 2 * PL::kTile, vb = kb + PL::kTile;
-        float sc[8][4];
+        float sc[M][NH][4];
 #pragma unroll
-        for (int n = 0; n < 8; ++n)
+        for (int n = 0; n < M; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                sc[n][e] = 0.f;
-        const int mi = lane >> 3, mr = lane & 7;   // ldmatrix: matrix and row of this lane's address
+            for (int nh = 0; nh < NH; ++nh)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    sc[n][nh][e] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                uint32_t b0, b1, b2, b3;
-                ldsm_x4(kb + swz<T>(n * 16 + (mi >> 1) * 8 + mr, kk * 2 + (mi & 1)), b0, b1, b2, b3);
-                mma_bf16_16816(sc[2 * n], qf[kk], b0, b1);
-                mma_bf16_16816(sc[2 * n + 1], qf[kk], b2, b3);
+            for (int n = 0; n < M; ++n) {
+                uint32_t a[4];
+                ldsm_x4(kb + swz<T>(half + n * 16 + (mi & 1) * 8 + mr, kk * 2 + (mi >> 1)), a[0], a[1], a[2], a[3]);
+#pragma unroll
+                for (int nh = 0; nh < NH; ++nh)
+                    mma_bf16_16816(sc[n][nh], a, qf[kk][nh][0], qf[kk][nh][1]);
             }
-        const int lim = x.L - blk * T;   // visible positions of the tile, 64 or more: all
+        const int lim = x.L - blk * T - half;   // visible of the warp's keys; kKeys or more: all
 #pragma unroll
-        for (int n = 0; n < 8; ++n)
+        for (int n = 0; n < M; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                sc[n][e] *= p.scale_log2;
-        if (lim < T) {
-#pragma unroll
-            for (int n = 0; n < 8; ++n)
+            for (int nh = 0; nh < NH; ++nh)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (n * 8 + (lane & 3) * 2 + (e & 1) >= lim)
-                        sc[n][e] = neg_inf();
+                    sc[n][nh][e] *= p.scale_log2;
+        if (lim < PL::kKeys) {
+#pragma unroll
+            for (int n = 0; n < M; ++n)
+#pragma unroll
+                for (int nh = 0; nh < NH; ++nh)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (n * 16 + (lane >> 2) + (e >> 1) * 8 >= lim)
+                            sc[n][nh][e] = neg_inf();
             // Values behind the sequence's end may be anything: their weight 0 takes zeros.
-            for (int i = lane; i < (T - lim) * (D / 8); i += 32)
-                *reinterpret_cast<uint4 *>(smem + (vb - sbase) + swz<T>(lim + i / (D / 8), i % (D / 8))) =
-                    make_uint4(0, 0, 0, 0);
+            const int from = max(lim, 0);
+            for (int i = lane; i < (PL::kKeys - from) * (D / 8); i += 32)
+                *reinterpret_cast<uint4 *>(smem + (vb - sbase) +
+                                           swz<T>(half + from + i / (D / 8), i % (D / 8))) = make_uint4(0, 0, 0, 0);
             fence_proxy_async_smem();
             __syncwarp();
         }
         if (kMode == kPieceWeights) {
 #pragma unroll
+            for (int nh = 0; nh < NH; ++nh)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int head = nh * 8 + (lane & 3) * 2 + i;
+                    if (head >= p.G)
+                        continue;
+                    float *to = p.scores +
+                                (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * p.G + head) *
+                                    p.score_stride + static_cast<size_t>(blk) * T + half + (lane >> 2);
+#pragma unroll
+                    for (int n = 0; n < M; ++n) {   // (rows of scores are whole tiles)
+                        to[n * 16] = sc[n][nh][i];
+                        to[n * 16 + 8] = sc[n][nh][2 + i];
+                    }
+                }
+        }
+        float alpha[NH][2], mu[NH][2];
+        bool raised = false;
+#pragma unroll
+        for (int nh = 0; nh < NH; ++nh)
+#pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int row = r0 + 8 * i;
-                if (row >= p.G)
-                    continue;
-                float *to = p.scores +
-                            (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * p.G + row) *
-                                p.score_stride + static_cast<size_t>(blk) * T;
+                float mt = neg_inf();
 #pragma unroll
-                for (int n = 0; n < 8; ++n)   // (rows of scores are whole tiles)
-                    *reinterpret_cast<float2 *>(to + n * 8 + (lane & 3) * 2) =
-                        make_float2(sc[n][2 * i], sc[n][2 * i + 1]);
+                for (int n = 0; n < M; ++n)
+                    mt = fmaxf(mt, fmaxf(sc[n][nh][i], sc[n][nh][2 + i]));
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1)
+                    mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, d));
+                const float mn = fmaxf(m[nh][i], mt);
+                alpha[nh][i] = m[nh][i] == mn ? 1.f : fast_exp2(m[nh][i] - mn);
+                raised = raised || alpha[nh][i] != 1.f;
+                m[nh][i] = mn;
+                mu[nh][i] = mn == neg_inf() ? 0.f : mn;
+                l[nh][i] *= alpha[nh][i];
             }
-        }
-        float mt[2] = {neg_inf(), neg_inf()};
+        if (__any_sync(0xffffffffu, raised)) {
 #pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            mt[0] = fmaxf(mt[0], fmaxf(sc[n][0], sc[n][1]));
-            mt[1] = fmaxf(mt[1], fmaxf(sc[n][2], sc[n][3]));
-        }
-        float alpha[2], mu[2];
+            for (int c = 0; c < D / 16; ++c)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            mt[i] = fmaxf(mt[i], __shfl_xor_sync(0xffffffffu, mt[i], 1));
-            mt[i] = fmaxf(mt[i], __shfl_xor_sync(0xffffffffu, mt[i], 2));
-            const float mn = fmaxf(m[i], mt[i]);
-            alpha[i] = m[i] == mn ? 1.f : fast_exp2(m[i] - mn);
-            m[i] = mn;
-            mu[i] = mn == neg_inf() ? 0.f : mn;
-            l[i] *= alpha[i];
-        }
-        if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
+                for (int nh = 0; nh < NH; ++nh)
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c) {
-                o[c][0] *= alpha[0];
-                o[c][1] *= alpha[0];
-                o[c][2] *= alpha[1];
-                o[c][3] *= alpha[1];
+                    for (int e = 0; e < 4; ++e)
+                        o[c][nh][e] *= alpha[nh][e & 1];
+        }
+        // Weights rounded to bf16 for the product (half a step, 2^-8 of each at most); their sum is not.
+        uint32_t pf[M][NH][2];
+#pragma unroll
+        for (int n = 0; n < M; ++n)
+#pragma unroll
+            for (int nh = 0; nh < NH; ++nh) {
+                float w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    w[e] = fast_exp2(sc[n][nh][e] - mu[nh][e & 1]);
+                    l[nh][e & 1] += w[e];
+                }
+                pf[n][nh][0] = movmatrix_trans(pack_bf16x2(w[0], w[1]));
+                pf[n][nh][1] = movmatrix_trans(pack_bf16x2(w[2], w[3]));
             }
-        }
 #pragma unroll
-        for (int n = 0; n < 8; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                sc[n][e] = fast_exp2(sc[n][e] - mu[e >> 1]);
-                l[e >> 1] += sc[n][e];
-            }
-        // Weights rounded to bf16 for the product (half a step, 2^-9 of each); their sum is not.
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            const uint32_t a[4] = {pack_bf16x2(sc[2 * kk][0], sc[2 * kk][1]),
-                                   pack_bf16x2(sc[2 * kk][2], sc[2 * kk][3]),
-                                   pack_bf16x2(sc[2 * kk + 1][0], sc[2 * kk + 1][1]),
-                                   pack_bf16x2(sc[2 * kk + 1][2], sc[2 * kk + 1][3])};
+        for (int n = 0; n < M; ++n)
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) {
-                uint32_t b0, b1, b2, b3;
-                ldsm_x4_trans(vb + swz<T>(kk * 16 + (mi & 1) * 8 + mr, c * 2 + (mi >> 1)), b0, b1, b2, b3);
-                mma_bf16_16816(o[2 * c], a, b0, b1);
-                mma_bf16_16816(o[2 * c + 1], a, b2, b3);
+                uint32_t a[4];
+                ldsm_x4_trans(vb + swz<T>(half + n * 16 + (mi >> 1) * 8 + mr, c * 2 + (mi & 1)), a[0], a[1], a[2],
+                              a[3]);
+#pragma unroll
+                for (int nh = 0; nh < NH; ++nh)
+                    mma_bf16_16816(o[c][nh], a, pf[n][nh][0], pf[n][nh][1]);
             }
-        }
         __syncwarp();
         if (lane == 0)
             mbar_arrive(bar_empty + 8 * s);
@@ -371,28 +406,35 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     const int tid = threadIdx.x;
     float *s_ml = reinterpret_cast<float *>(smem + PL::kML);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-        if ((lane & 3) == 0) {
-            s_ml[warp * 32 + r0 + 8 * i] = m[i];
-            s_ml[warp * 32 + 16 + r0 + 8 * i] = l[i];
+    for (int nh = 0; nh < NH; ++nh)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1)
+                l[nh][i] += __shfl_xor_sync(0xffffffffu, l[nh][i], d);
+            if (lane < 4) {
+                s_ml[warp * 32 + nh * 8 + lane * 2 + i] = m[nh][i];
+                s_ml[warp * 32 + 16 + nh * 8 + lane * 2 + i] = l[nh][i];
+            }
         }
-    }
     consumer_bar_sync<kWarps>();
     if (tid == 0)
         flag[2] = flag[0];   // (the producer may still give up: one answer for all)
     float *s_o = reinterpret_cast<float *>(smem);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int row = r0 + 8 * i;
-        if (row < p.G) {
+    for (int nh = 0; nh < NH; ++nh)
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c)
-                *reinterpret_cast<float2 *>(s_o + (warp * 16 + row) * PL::kRow + c * 8 + (lane & 3) * 2) =
-                    make_float2(o[c][2 * i], o[c][2 * i + 1]);
+        for (int i = 0; i < 2; ++i) {
+            const int head = nh * 8 + (lane & 3) * 2 + i;
+            if (head < p.G) {
+                float *to = s_o + (warp * 16 + head) * PL::kRow + (lane >> 2);
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) {
+                    to[c * 16] = o[c][nh][i];
+                    to[c * 16 + 8] = o[c][nh][2 + i];
+                }
+            }
         }
-    }
     consumer_bar_sync<kWarps>();
     if (flag[2])
         return;
@@ -576,14 +618,19 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackP
         to[i] = from[i];
 }
 
-template <int D>
+template <int D, int NH>
 const void *piece_fn(int mode)
 {
-    return mode == kPieceSuffix   ? reinterpret_cast<const void *>(&piece_kernel<D, kPieceSuffix>)
-           : mode == kPieceBlocks ? reinterpret_cast<const void *>(&piece_kernel<D, kPieceBlocks>)
-                                  : reinterpret_cast<const void *>(&piece_kernel<D, kPieceWeights>);
+    return mode == kPieceSuffix   ? reinterpret_cast<const void *>(&piece_kernel<D, kPieceSuffix, NH>)
+           : mode == kPieceBlocks ? reinterpret_cast<const void *>(&piece_kernel<D, kPieceBlocks, NH>)
+                                  : reinterpret_cast<const void *>(&piece_kernel<D, kPieceWeights, NH>);
 }
-const void *piece_fn(int head_dim, int mode) { return head_dim == 64 ? piece_fn<64>(mode) : piece_fn<128>(mode); }
+const void *piece_fn(int head_dim, int G, int mode)
+{
+    if (G <= 8)
+        return head_dim == 64 ? piece_fn<64, 1>(mode) : piece_fn<128, 1>(mode);
+    return head_dim == 64 ? piece_fn<64, 2>(mode) : piece_fn<128, 2>(mode);
+}
 
 int piece_threads(int head_dim) { return head_dim == 64 ? PiecePlan<64>::kThreads : PiecePlan<128>::kThreads; }
 size_t piece_smem(int head_dim) { return head_dim == 64 ? PiecePlan<64>::kBytes : PiecePlan<128>::kBytes; }
@@ -606,16 +653,16 @@ cudaError_t launch_pdl(const void *fn, dim3 grid, int threads, size_t smem, cuda
 }  // namespace
 
 
-int piece_warps(int head_dim) { return head_dim == 64 ? PiecePlan<64>::kWarps : PiecePlan<128>::kWarps; }
+int piece_stages(int head_dim) { return head_dim == 64 ? PiecePlan<64>::kStages : PiecePlan<128>::kStages; }
 
 int piece_max_records(int head_dim, int G)
 {
     return (head_dim == 64 ? max_records<64>(G) : max_records<128>(G)) - 1;
 }
 
-cudaError_t prepare_pieces(int head_dim, int mode, int *ctas_per_sm)
+cudaError_t prepare_pieces(int head_dim, int G, int mode, int *ctas_per_sm)
 {
-    const void *fn = piece_fn(head_dim, mode);
+    const void *fn = piece_fn(head_dim, G, mode);
     cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          static_cast<int>(piece_smem(head_dim)));
     if (e == cudaSuccess)
@@ -628,7 +675,7 @@ cudaError_t launch_pieces(int head_dim, int mode, const CUtensorMap *tmap, const
                           cudaStream_t stream)
 {
     void *args[] = {const_cast<CUtensorMap *>(tmap), const_cast<PieceParams *>(&p)};
-    return launch_pdl(piece_fn(head_dim, mode), dim3(static_cast<unsigned>(p.first[p.b])), piece_threads(head_dim),
+    return launch_pdl(piece_fn(head_dim, p.G, mode), dim3(static_cast<unsigned>(p.first[p.b])), piece_threads(head_dim),
                       piece_smem(head_dim), stream, args);
 }
 

@@ -17,6 +17,7 @@ namespace mlkv {
 namespace {
 
 constexpr int kTopkBins = 1024;
+constexpr unsigned kTopkCluster = 8;   // CTAs of a cluster, at most
 
 template <int NT>
 struct TopkShared {
@@ -55,10 +56,12 @@ __device__ void cluster_topk(TopkShared<NT> &sh, int n, unsigned lo, unsigned hi
             sh.hi = hi;
         }
         cluster.sync();
-        for (unsigned c = 0; c < size; ++c) {
-            lo = min(lo, *cluster.map_shared_rank(&sh.lo, c));
-            hi = max(hi, *cluster.map_shared_rank(&sh.hi, c));
-        }
+#pragma unroll
+        for (unsigned c = 0; c < kTopkCluster; ++c)
+            if (c < size) {
+                lo = min(lo, *cluster.map_shared_rank(&sh.lo, c));
+                hi = max(hi, *cluster.map_shared_rank(&sh.hi, c));
+            }
     } else {
         __syncthreads();
     }
@@ -82,8 +85,17 @@ __device__ void cluster_topk(TopkShared<NT> &sh, int n, unsigned lo, unsigned hi
             mine[k] = 0;
             if (has) {
                 const int b = kTopkBins - 1 - tid * kPer - k;
-                for (unsigned c = 0; c < size; ++c)
-                    mine[k] += size > 1 ? *cluster.map_shared_rank(&hist[b], c) : hist[b];
+                if (size == 1) {
+                    mine[k] = hist[b];
+                } else {
+                    unsigned v[kTopkCluster];   // (all on the way at once)
+#pragma unroll
+                    for (unsigned c = 0; c < kTopkCluster; ++c)
+                        v[c] = c < size ? *cluster.map_shared_rank(&hist[b], c) : 0u;
+#pragma unroll
+                    for (unsigned c = 0; c < kTopkCluster; ++c)
+                        mine[k] += v[c];
+                }
             }
             total += mine[k];
         }
@@ -149,10 +161,12 @@ __device__ void cluster_topk(TopkShared<NT> &sh, int n, unsigned lo, unsigned hi
             sh.eq = ea;
         }
         cluster.sync();
-        for (unsigned c = 0; c < rank; ++c) {
-            gt0 += *cluster.map_shared_rank(&sh.gt, c);
-            eq0 += *cluster.map_shared_rank(&sh.eq, c);
-        }
+#pragma unroll
+        for (unsigned c = 0; c < kTopkCluster; ++c)
+            if (c < rank) {
+                gt0 += *cluster.map_shared_rank(&sh.gt, c);
+                eq0 += *cluster.map_shared_rank(&sh.eq, c);
+            }
     }
     for (int i = i0; i < i1; i += 32) {
         const bool in = i + lane < i1;
