@@ -324,8 +324,8 @@ int mlkv_block_bounds(mlkv_cache_t c, int layer, const int *first, const int *se
  *                    n_last last
  *   n_select         >= 1, n_first and n_last >= 0, n_first + n_last <= n_select
  *   blocks           device int32 [batch][g][n_select]: block numbers in rising order, -1 behind them
- * Errors: MLKV_ERR_INVALID_ARG, MLKV_ERR_RANGE (lengths), MLKV_ERR_UNSUPPORTED (a sequence of more than 327,680
- * blocks), MLKV_ERR_CUDA.
+ * Errors: MLKV_ERR_INVALID_ARG, MLKV_ERR_RANGE (lengths), MLKV_ERR_UNSUPPORTED (a sequence of more than 32,768
+ * blocks, 2,097,152 positions), MLKV_ERR_CUDA.
  */
 int mlkv_select_blocks(mlkv_cache_t c, int layer, const void *Q, const void *bounds, const float *scales,
                        const int *seq_lens, int n_select, int n_first, int n_last, int *blocks,

@@ -136,8 +136,8 @@ constexpr int kSelectThreads = 512;
 constexpr int kLanes = 4;   // lanes of a block's score
 
 // A cluster is one (sequence, KV head): each CTA scores a run of its blocks, four lanes a block (dp4a of the
-// codes with the query's positive and negative parts; 64 bytes a load), keeps the scores as ordered keys in shared
-// memory, and the cluster takes the largest (cluster_topk).  Bound by latency for few blocks, else by the
+// codes with the query's positive and negative parts; 64 bytes a load), and puts the scores as ordered keys into
+// the first CTA's shared memory, which takes the largest (cluster_topk).  Bound by latency for few blocks, else by the
 // products, 2 D / 4 dp4a a block and head.
 template <int D>
 __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_constant__ SelectParams p)
@@ -171,6 +171,8 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_con
     const int want = p.n_select - p.n_first - p.n_last;
     if (want == 0)
         return;
+    if (size > 1)
+        cluster_arrive();   // (the first CTA's shared memory is there once all have started)
     const int inner = count - p.n_first - p.n_last, per = (inner + size - 1) / size;
     const int first = p.n_first + min(inner, rank * per), n = min(inner, (rank + 1) * per) - min(inner, rank * per);
     // a lane's columns of its first block, on the way while the queries are made ready
@@ -216,7 +218,9 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_con
             s_f[i] = f;
     }
     __syncthreads();
-    unsigned least = 0xffffffffu, most = 0u;
+    unsigned *keys = size > 1 ? cluster.map_shared_rank(s_key, 0) + (first - p.n_first) : s_key;
+    if (size > 1)
+        cluster_wait();
     const int per_round = NT / kLanes;
     for (int i0 = 0; i0 < n; i0 += per_round) {   // (all lanes stay: they add up in groups)
         const int i = i0 + tid / kLanes;
@@ -248,20 +252,30 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_con
             const unsigned key = scale == __int_as_float(0x7f800000) ? 0xffffffffu
                                  : (u >> 31)                         ? ~u
                                                                      : u | 0x80000000u;
-            least = min(least, key);
-            most = max(most, key);
             if (part == 0)
-                s_key[i] = key;
+                keys[i] = key;
         }
         fetch(i + per_round);
     }
+    if (size > 1) {
+        cluster.sync();
+        if (rank != 0)
+            return;
+    } else {
+        __syncthreads();
+    }
+    unsigned least = 0xffffffffu, most = 0u;
+    for (int i = tid; i < inner; i += NT) {
+        least = min(least, s_key[i]);
+        most = max(most, s_key[i]);
+    }
     block_min_max<NT>(least, most, s_mm);
-    cluster_topk<NT>(sh, n, least, most, static_cast<unsigned>(want), [&](int i) { return s_key[i]; },
-                     [&](unsigned place, int i) { to[p.n_first + place] = first + i; });
+    cluster_topk<NT>(sh, 1, 0, inner, least, most, static_cast<unsigned>(want), [&](int i) { return s_key[i]; },
+                     [&](unsigned place, int i) { to[p.n_first + place] = p.n_first + i; });
 }
 
 constexpr int kMaxCluster = kTopkCluster;
-constexpr size_t kSelectSmem = 160 * 1024;
+constexpr size_t kSelectSmem = 128 * 1024;   // keys of a (sequence, KV head)
 
 template <int D>
 const void *select_fn()
@@ -287,7 +301,7 @@ cudaError_t launch_bounds(int head_dim, const BoundsParams &p, cudaStream_t stre
                                                     : reinterpret_cast<const void *>(&bounds_kernel<128>), args);
 }
 
-int select_max_blocks() { return kMaxCluster * static_cast<int>(kSelectSmem / 4); }
+int select_max_blocks() { return static_cast<int>(kSelectSmem / 4); }
 
 cudaError_t prepare_select(int head_dim)
 {
@@ -301,12 +315,10 @@ cudaError_t launch_select(int head_dim, const SelectParams &p, int max_blocks, c
     int size = 1;
     while (size < kMaxCluster && size * 256 < max_blocks && p.b * p.g * size < 152)
         size *= 2;
-    while (size < kMaxCluster && static_cast<size_t>((max_blocks + size - 1) / size) * 4 > kSelectSmem)
-        size *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.b * p.g * size));
     cfg.blockDim = dim3(kSelectThreads);
-    cfg.dynamicSmemBytes = static_cast<size_t>((max_blocks + size - 1) / size) * 4;
+    cfg.dynamicSmemBytes = static_cast<size_t>(max_blocks) * 4;   // (of use to a cluster's first CTA alone)
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const __grid_constan
             }
     }
     block_min_max<NT>(least, most, s_mm);   // (and the keys are in place)
-    cluster_topk<NT>(sh, n, least, most, static_cast<unsigned>(want),
+    cluster_topk<NT>(sh, size, rank, n, least, most, static_cast<unsigned>(want),
                      [&](int i) { return cached ? s_key[i] : weight_key(__ldcg(w + first + i)); },
                      [&](unsigned place, int i) { kept[place] = first + i; });
 }

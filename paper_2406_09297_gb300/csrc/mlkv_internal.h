@@ -180,16 +180,18 @@ struct PrefillParams : PrefillCommon {
 //   which every query sees, then the prompt's own.
 // Decode (fused): a unit is the queries of up to two tiles of the sequences that share prefix `beta`, over
 //   chunk `chunk` of its positions (prompt_len[beta] of them); block `blk` of the unit word counts those pairs
-//   of tiles.  Sequences are packed: those of prefix x are places group_at[x] .. + group_n[x] of Q
-//   [places][h][D].  fused_L is the places in all, fused_L1 the sequences of a tile.  Records (o, lse) go to
-//   part [place][g][fused_cmax][G][D] and part_lse [place][g][fused_cmax][G].
-constexpr int kPrefixMaxUnits = 4096;
+//   of tiles.  The sequences of prefix x are places group_at[x] .. + group_n[x] of an order that has them side by
+//   side: seq[place] is the place's sequence (scattered), or the place itself.  fused_L is the sequences in all,
+//   fused_L1 those of a tile, whose queries come as one box of the tensor map, or (scattered) one box each.
+//   Records (o, lse) go to part [place][g][fused_cmax][G][D] and part_lse [place][g][fused_cmax][G].
+constexpr int kPrefixMaxUnits = 3584;
 struct SharedPrefillParams : PrefillCommon {
     CUtensorMap tmap_p;
     int prefix_b;                              // sequences of the prefix cache
     union {
         struct {                               // decode, by prefix
-            uint16_t group_at[MLKV_MAX_BATCH], group_n[MLKV_MAX_BATCH];
+            uint16_t group_at[MLKV_MAX_BATCH], group_n[MLKV_MAX_BATCH], seq[MLKV_MAX_BATCH];
+            int scattered;
         };
         int16_t prefix_of[MLKV_MAX_BATCH];     // prefill, by sequence
     };

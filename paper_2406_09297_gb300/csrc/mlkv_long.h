@@ -41,8 +41,8 @@ struct PieceParams {
     int early;                // the stream's previous kernel is this call's prefix kernel, which writes
                               // neither Q nor the cache and has itself waited for all before it: Q and
                               // the tiles are read before the dependency wait
-    int defer;                // every piece writes its record, launch_merge_pieces merges them: nothing but that
-                              // waits for the prefix kernel, beside which the pieces run
+    int defer;                // every piece writes its record, launch_merge_pieces merges them: many records, or
+                              // pieces that run beside a prefix kernel, for which then nothing but that waits
     // kPieceBlocks: block numbers [b][g][n_blocks]; others than those of visible positions are passed over
     const int *blocks;
     int n_blocks;
@@ -61,20 +61,12 @@ cudaError_t prepare_pieces(int head_dim, int group, int mode, int *ctas_per_sm);
 cudaError_t launch_pieces(int head_dim, int mode, const CUtensorMap *tmap, const PieceParams &p,
                           cudaStream_t stream);
 
-// The merge of a deferred kPieceSuffix launch's segments, of `most` records at most.
-cudaError_t launch_merge_pieces(int head_dim, const PieceParams &p, int most, cudaStream_t stream);
+// The merge of a deferred launch's segments, of `most` records at most.
+cudaError_t launch_merge_pieces(int head_dim, int mode, const PieceParams &p, int most, cudaStream_t stream);
 
-// Most records of a segment that launch_merge_pieces and launch_weights take.
-constexpr int kDeferMaxRecords = 700;   // (700 + 1) * 16 heads * 4 bytes < 48 KB
-
-// Packs the queries of places [0, n): place i is sequence seq[i].
-struct PackParams {
-    const __nv_bfloat16 *Q;
-    __nv_bfloat16 *packed;
-    int n, row_vecs;           // 16-byte vectors of a sequence's queries
-    uint16_t seq[MLKV_MAX_BATCH];
-};
-cudaError_t launch_pack(const PackParams &p, cudaStream_t stream);
+// Most records of a segment that launch_merge_pieces and launch_weights take (the weights of two heads' records in
+// 48 KB of shared memory).
+constexpr int kDeferMaxRecords = 4096;
 
 // The merge of a kPieceWeights launch's pieces, and what every position got: out, and
 // weights_out[beta][j][u] = weights_in[beta][j][u] + sum over the heads of the group.
@@ -83,9 +75,11 @@ struct WeightsParams {
     float *weights_out;        // [b][g][max_seq]
     int max_seq;
     int chunk;                 // positions of a CTA
-    int ctas;                  // of a segment: one for the merge, then those of its positions
+    int merge_ctas, wide;      // of a segment: CTAs that merge its records, many of them (plan_weights)
+    int ctas;                  // of a segment: those, then those of its positions
 };
-cudaError_t launch_weights(int head_dim, const PieceParams &p, const WeightsParams &w, int max_len,
+void plan_weights(int head_dim, int group, int most, WeightsParams *w);
+cudaError_t launch_weights(int head_dim, const PieceParams &p, const WeightsParams &w, int most,
                            cudaStream_t stream);
 
 struct BoundsParams {

@@ -55,37 +55,70 @@ int prepare_pieces(mlkv_cache *c, int mode)
     return MLKV_OK;
 }
 
-// Cuts the segments, nt(beta) tiles each, into pieces: fills p.tiles and p.first.  Up to 32 tiles a resident CTA
-// one piece each; beyond that four, so that the last ones to end are short (a record is 1% of 16 tiles).  Never
-// more pieces than there are records, nor of a segment than `most`, nor less than a tile a consumer warp.
+// Cuts the segments, nt(beta) tiles each, into pieces of at most p.tiles tiles: the least estimated time, in us.  A
+// launch takes 4.5, and what is longer of its bytes at the rate of HBM and its longest piece; pieces beyond one wave
+// of resident CTAs half a piece more where segments are split (whole ones end evenly enough).  Split segments
+// are merged by the CTA that ends last, a round trip to L2 for every 8 records, or by a launch of their own
+// (`may_defer`; weights: always).  Never more pieces than there are records, nor of a segment than `most`.
+// `pre`: records that every merge has besides.
+struct Cut {
+    bool defer;
+    int records;   // of a segment, at most
+};
 template <typename Tiles>
-void cut(const mlkv_cache *c, mlkv::PieceParams &p, int most, const Tiles &nt)
+Cut cut(const mlkv_cache *c, mlkv::PieceParams &p, bool may_defer, bool must_defer, int pre, const Tiles &nt)
 {
     long long total = 0;
-    int longest = 0;
+    int longest = 1;
     for (int beta = 0; beta < c->b; ++beta) {
         total += nt(beta);
         longest = std::max(longest, nt(beta));
     }
     total *= c->g;
     const long long slots = static_cast<long long>(c->piece_ctas) * c->sm_count;
-    const long long want = std::min(c->records, total <= 32 * slots ? slots : 4 * slots);
-    int tiles = static_cast<int>(std::max<long long>(mlkv::piece_stages(c->d), (total + want - 1) / want));
-    tiles = std::max(tiles, (longest + most - 1) / most);
-    for (;; tiles += (tiles + 7) / 8) {
+    const int stages = mlkv::piece_stages(c->d);
+    // us: a tile of a CTA alone on its SM; all tiles at the rate of HBM; a record's part of an inline merge
+    const double tile = c->d == 64 ? 0.33 : c->G <= 8 ? 0.45 : 0.72;
+    const double bytes = total * 256.0 * c->d / 6.7e6, record = 0.1 * c->G * c->d / 512;
+    const int inline_most = mlkv::piece_max_records(c->d, c->G) - pre;
+    Cut best = {must_defer, 1};
+    double best_t = 1e30;
+    int best_tiles = longest;
+    for (int want = 1, tiles = longest;; want += (want + 7) / 8) {   // pieces of the longest segment
+        const int next = (longest + want - 1) / want;
+        if (want > 1 && next == tiles)
+            continue;
+        tiles = next;
         long long n = 0;
         for (int beta = 0; beta < c->b; ++beta)
             n += (nt(beta) + tiles - 1) / tiles;
-        if (n * c->g <= want || tiles >= longest)
+        n *= c->g;
+        const int pieces = (longest + tiles - 1) / tiles, records = pieces + pre;
+        if (want > 1 && (n > c->records || records > mlkv::kDeferMaxRecords))
+            break;
+        const double rounds = (tiles + stages - 1) / stages;   // (a short piece's tiles come at once)
+        double t = 4.5 + std::max(bytes, 1.15 * std::max(tiles * tile, rounds * 1.2));
+        if (n > slots && pieces > 1)
+            t += 0.5 * tiles * tile + 2.0;
+        const double here = records <= 1 ? 0.0 : 2.5 + record * records, apart = 4.5;
+        const bool defer = must_defer || (may_defer && (here > apart || records > inline_most) && records > 1);
+        t += defer ? apart : here;
+        if (t < best_t && (defer || records <= inline_most || pieces == 1)) {
+            best_t = t;
+            best = {defer, records};
+            best_tiles = tiles;
+        }
+        if (tiles == 1)
             break;
     }
-    p.tiles = tiles;
+    p.tiles = best_tiles;
     long long at = 0;
     for (int beta = 0; beta < c->b; ++beta) {
         p.first[beta] = static_cast<int>(at);
-        at += static_cast<long long>(c->g) * ((nt(beta) + tiles - 1) / tiles);
+        at += static_cast<long long>(c->g) * ((nt(beta) + p.tiles - 1) / p.tiles);
     }
     p.first[c->b] = static_cast<int>(at);
+    return best;
 }
 
 void fill_pieces(const mlkv_cache *c, int layer, const void *Q, void *out, const int *seq_lens,
@@ -126,6 +159,18 @@ int scratch(mlkv_cache *c, size_t floats, const char *what, cudaStream_t stream)
     return mlkv::grow_scratch(c, floats, what);
 }
 
+// The piece launch, and the merge's where it is one of its own.
+int decode_pieces(const mlkv_cache *c, int mode, mlkv::PieceParams &p, const Cut &split, cudaStream_t stream)
+{
+    p.defer = split.defer ? 1 : 0;
+    cudaError_t e = mlkv::launch_pieces(c->d, mode, rows64(c), p, stream);
+    if (e != cudaSuccess)
+        return fail_cuda(e, "decode launch");
+    if (p.defer && (e = mlkv::launch_merge_pieces(c->d, mode, p, split.records, stream)) != cudaSuccess)
+        return fail_cuda(e, "merge launch");
+    return MLKV_OK;
+}
+
 // How the decode over shared prefixes is launched.
 struct PrefixPlan {
     int kc;       // key tiles of 128 positions of a unit
@@ -139,7 +184,7 @@ struct PrefixPlan {
 // many sequences share one, the suffixes by HBM: side by side, each has what the other leaves.)
 PrefixPlan plan_prefix(const int *n_kt, const int *pairs, int n, int sm_count, int d, double bytes)
 {
-    const double tile = d == 64 ? 0.65 : 1.25, rate = 65e3, all = 6.5e6, merge = 5.0;
+    const double tile = d == 64 ? 0.9 : 1.65, rate = 62e3, all = 6.5e6, merge = 5.0;
     long long work = 0;
     int longest = 1;
     for (int x = 0; x < n; ++x) {
@@ -154,10 +199,11 @@ PrefixPlan plan_prefix(const int *n_kt, const int *pairs, int n, int sm_count, i
         long long units = 0;
         for (int x = 0; x < n; ++x)
             units += static_cast<long long>((n_kt[x] + kc - 1) / kc) * pairs[x];
-        for (int eighths = 8; eighths >= 2; --eighths) {
-            const int sms = sm_count * eighths / 8;
+        for (int rounds = 1; rounds <= 8; ++rounds) {   // of the units, on as many SMs as it takes
+            const int need = static_cast<int>((units + rounds - 1) / rounds);
+            const int sms = std::min(sm_count, need);
             double t = static_cast<double>((units + sms - 1) / sms) * (kc + 3) * tile;
-            if (eighths == 8) {
+            if (need >= sm_count || sm_count - sms < 8) {
                 t += bytes / all;
             } else {
                 const double beside = t * std::min(all, rate * (sm_count - sms));
@@ -165,7 +211,13 @@ PrefixPlan plan_prefix(const int *n_kt, const int *pairs, int n, int sm_count, i
             }
             if (t < best_t) {
                 best_t = t;
-                best = {kc, sms, eighths < 8};
+                best = {kc, sms, need < sm_count && sm_count - sms >= 8};
+            }
+            // the same one after the other, without a merge of its own
+            const double one = static_cast<double>((units + sms - 1) / sms) * (kc + 3) * tile + bytes / all;
+            if (one < best_t) {
+                best_t = one;
+                best = {kc, sms, false};
             }
         }
     }
@@ -222,10 +274,9 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
         return rc;
     static thread_local mlkv::PieceParams p;
     static thread_local mlkv::SharedPrefillParams u;
-    static thread_local mlkv::PackParams pack;
     fill_pieces(c, layer, Q, out, seq_lens, p);
     // Places: the sequences of prefix 0, then those of prefix 1, ...  Where every prefix's sequences are
-    // neighbours already, a sequence's place is its own number and Q stays as it is.
+    // neighbours already, a sequence's place is its own number.
     const int L1 = 128 / c->G, np = prefix->b;
     static thread_local int n_kt[MLKV_MAX_BATCH], pairs[MLKV_MAX_BATCH];
     std::fill(u.group_n, u.group_n + np, static_cast<uint16_t>(0));
@@ -234,6 +285,7 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
     int places = 0;
     for (int beta = 0; beta < c->b; ++beta) {
         const int x = of(beta);
+        p.pre_place[beta] = static_cast<uint16_t>(beta);
         if (x < 0)
             continue;
         ++places;
@@ -242,9 +294,8 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
         else
             neighbours = neighbours && of(beta - 1) == x;
     }
+    u.scattered = neighbours ? 0 : 1;
     if (neighbours) {
-        for (int beta = 0; beta < c->b; ++beta)
-            p.pre_place[beta] = static_cast<uint16_t>(beta);
         places = c->b;
     } else {
         int at = 0;
@@ -257,7 +308,7 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
             if (of(beta) >= 0) {
                 const int place = u.group_at[of(beta)] + u.group_n[of(beta)]++;
                 p.pre_place[beta] = static_cast<uint16_t>(place);
-                pack.seq[place] = static_cast<uint16_t>(beta);
+                u.seq[place] = static_cast<uint16_t>(beta);
             }
     }
     int most_kt = 0;
@@ -282,46 +333,34 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
         p.defer = plan.beside ? 1 : 0;
         cmax = (most_kt + kc - 1) / kc;
         const size_t rows = static_cast<size_t>(places) * c->g * cmax * c->G;
-        const size_t packed = neighbours ? 0 : static_cast<size_t>(places) * c->h * c->d / 2;   // in floats
-        if ((rc = scratch(c, rows * (c->d + 1) + packed + 4, "records of the shared prefix", stream)) != MLKV_OK)
+        if ((rc = scratch(c, rows * (c->d + 1), "records of the shared prefix", stream)) != MLKV_OK)
             return rc;
-        const void *q_in = Q;
-        if (!neighbours) {
-            pack.Q = static_cast<const __nv_bfloat16 *>(Q);
-            pack.packed = reinterpret_cast<__nv_bfloat16 *>(c->fused_part);
-            pack.n = places;
-            pack.row_vecs = c->h * c->d / 8;
-            const cudaError_t e = mlkv::launch_pack(pack, stream);
-            if (e != cudaSuccess)
-                return fail_cuda(e, "query pack launch");
-            q_in = c->fused_part;
-        }
-        u.part = c->fused_part + packed;
+        u.part = c->fused_part;
         u.part_lse = u.part + rows * c->d;
         p.pre_o = u.part;
         p.pre_lse = u.part_lse;
         p.pre_chunks = cmax;
         p.early = 1;
-        // The packed queries [places][h][D] as (channel, head in group, group, 1, place): a box of 64 channels x
-        // G heads x min(L1, places) places is a tile's rows.
+        // The queries [b][h][D] as (channel, head in group, group, 1, sequence): a box of 64 channels x G heads x
+        // min(L1, b) neighbours is a tile's rows, one of 64 channels x G heads a scattered sequence's.
         static EncodeTiledFn encode = driver_entry<EncodeTiledFn>("cuTensorMapEncodeTiled");
         if (encode == nullptr)
             return fail(MLKV_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable from the driver");
         CUtensorMap tmap_q;
         const cuuint64_t row = static_cast<cuuint64_t>(c->h) * c->d * 2;
         const cuuint64_t dims[5] = {static_cast<cuuint64_t>(c->d), static_cast<cuuint64_t>(c->G),
-                                    static_cast<cuuint64_t>(c->g), 1u, static_cast<cuuint64_t>(places)};
+                                    static_cast<cuuint64_t>(c->g), 1u, static_cast<cuuint64_t>(c->b)};
         const cuuint64_t strides[4] = {static_cast<cuuint64_t>(c->d) * 2,
                                        static_cast<cuuint64_t>(c->G) * c->d * 2, row, row};
         const cuuint32_t box[5] = {64u, static_cast<cuuint32_t>(c->G), 1u, 1u,
-                                   static_cast<cuuint32_t>(std::min(L1, places))};
+                                   static_cast<cuuint32_t>(neighbours ? std::min(L1, c->b) : 1)};
         const cuuint32_t estr[5] = {1u, 1u, 1u, 1u, 1u};
-        const CUresult r = encode(&tmap_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(q_in), dims,
+        const CUresult r = encode(&tmap_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(Q), dims,
                                   strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
         if (r != CUDA_SUCCESS)
-            return fail(MLKV_ERR_CUDA, "cuTensorMapEncodeTiled(packed Q) failed (CUresult %d)",
+            return fail(MLKV_ERR_CUDA, "cuTensorMapEncodeTiled(Q) failed (CUresult %d)",
                         static_cast<int>(r));
         const CUtensorMap *tmap_kv = nullptr;
         for (auto &v : prefix->variants)
@@ -343,7 +382,7 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
         u.sm_count = plan.sms;
         u.window = u.sinks = 0;
         u.kv_direct = 0;
-        u.fused_L = places;
+        u.fused_L = c->b;
         u.fused_L1 = L1;
         u.fused_nblk = 1;
         u.fused_kc = kc;
@@ -385,20 +424,10 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
     } else {
         std::fill(p.pre_n, p.pre_n + c->b, static_cast<uint16_t>(0));
     }
-    const int most = std::min(mlkv::piece_max_records(c->d, c->G), mlkv::kDeferMaxRecords);
-    cut(c, p, most - cmax,
-        [&](int beta) { return static_cast<int>((static_cast<unsigned>(seq_lens[beta]) + 63) / 64); });
-    cudaError_t e = mlkv::launch_pieces(c->d, mlkv::kPieceSuffix, rows64(c), p, stream);
-    if (e != cudaSuccess)
-        return fail_cuda(e, "suffix decode launch");
-    if (p.defer) {
-        int records = 0;
-        for (int beta = 0; beta < c->b; ++beta)
-            records = std::max(records, (p.first[beta + 1] - p.first[beta]) / c->g + p.pre_n[beta]);
-        if ((e = mlkv::launch_merge_pieces(c->d, p, records, stream)) != cudaSuccess)
-            return fail_cuda(e, "merge launch");
-    }
-    return MLKV_OK;
+    const Cut split = cut(c, p, true, p.defer != 0, cmax, [&](int beta) {
+        return static_cast<int>((static_cast<unsigned>(seq_lens[beta]) + 63) / 64);
+    });
+    return decode_pieces(c, mlkv::kPieceSuffix, p, split, stream);
 }
 
 int mlkv_block_bounds(mlkv_cache_t c, int layer, const int *first, const int *seq_lens, void *bounds,
@@ -517,10 +546,8 @@ int mlkv_decode_attention_blocks(mlkv_cache_t c, int layer, const void *Q, void 
     fill_pieces(c, layer, Q, out, seq_lens, p);
     p.blocks = blocks;
     p.n_blocks = n_blocks;
-    cut(c, p, mlkv::piece_max_records(c->d, c->G), [&](int) { return n_blocks; });
-    const cudaError_t e = mlkv::launch_pieces(c->d, mlkv::kPieceBlocks, rows64(c), p,
-                                              static_cast<cudaStream_t>(cuda_stream));
-    return e == cudaSuccess ? MLKV_OK : fail_cuda(e, "block decode launch");
+    const Cut split = cut(c, p, true, false, 0, [&](int) { return n_blocks; });
+    return decode_pieces(c, mlkv::kPieceBlocks, p, split, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int mlkv_decode_attention_weights(mlkv_cache_t c, int layer, const void *Q, void *out, const int *seq_lens,
@@ -550,8 +577,9 @@ int mlkv_decode_attention_weights(mlkv_cache_t c, int layer, const void *Q, void
     if ((rc = scratch(c, static_cast<size_t>(c->b) * c->h * p.score_stride, "scores", stream)) != MLKV_OK)
         return rc;
     p.scores = c->fused_part;
-    cut(c, p, mlkv::kDeferMaxRecords,
-        [&](int beta) { return static_cast<int>((static_cast<unsigned>(seq_lens[beta]) + 63) / 64); });
+    const Cut split = cut(c, p, true, true, 0, [&](int beta) {
+        return static_cast<int>((static_cast<unsigned>(seq_lens[beta]) + 63) / 64);
+    });
     mlkv::WeightsParams w;
     w.weights_in = weights_in;
     w.weights_out = weights_out;
@@ -560,13 +588,14 @@ int mlkv_decode_attention_weights(mlkv_cache_t c, int layer, const void *Q, void
     const long long upto = weights_in == weights_out ? longest : c->max_seq;
     w.chunk = 1024;
     const long long segments = static_cast<long long>(c->b) * c->g;
-    while (((upto + w.chunk - 1) / w.chunk + 1) * segments > 0x7fffffffLL)
+    mlkv::plan_weights(c->d, c->G, split.records, &w);
+    while (((upto + w.chunk - 1) / w.chunk + w.merge_ctas) * segments > 0x7fffffffLL)
         w.chunk *= 2;
-    w.ctas = static_cast<int>((upto + w.chunk - 1) / w.chunk) + 1;
+    w.ctas = static_cast<int>((upto + w.chunk - 1) / w.chunk) + w.merge_ctas;
     cudaError_t e = mlkv::launch_pieces(c->d, mlkv::kPieceWeights, rows64(c), p, stream);
     if (e != cudaSuccess)
         return fail_cuda(e, "decode launch");
-    e = mlkv::launch_weights(c->d, p, w, longest, stream);
+    e = mlkv::launch_weights(c->d, p, w, split.records, stream);
     return e == cudaSuccess ? MLKV_OK : fail_cuda(e, "weights launch");
 }
 

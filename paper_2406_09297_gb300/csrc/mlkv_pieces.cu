@@ -156,7 +156,10 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     const uint32_t bar_full = sbase + PL::kBars, bar_empty = bar_full + 8 * S;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *flag = reinterpret_cast<volatile int *>(smem + PL::kFlag);
-    if (threadIdx.x == 0) {
+    // The producer sets the barriers up and goes on to its first tiles; the consumers wait for that, behind the
+    // loads of their queries.
+    if (threadIdx.x == kWarps * 32) {
+        prefetch_tensormap(&tmap);
         for (int s = 0; s < S; ++s) {
             mbar_init(bar_full + 8 * s, 1);
             mbar_init(bar_empty + 8 * s, PL::kPerStage);
@@ -164,9 +167,6 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
         flag[0] = 0;   // a wait gave up
         fence_barrier_init();
     }
-    if (threadIdx.x == kWarps * 32)
-        prefetch_tensormap(&tmap);
-    __syncthreads();
     const bool early = kMode == kPieceSuffix && p.early;
     if (!early)
         grid_dependency_wait();
@@ -188,6 +188,8 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     };
 
     if (warp == kWarps) {
+        __syncwarp();
+        asm volatile("bar.arrive 2, %0;" ::"n"(PL::kThreads) : "memory");
         // ------------------------------------ producer ------------------------------------------
         const int zk = ((p.slot * 2 + 0) * p.b + x.beta) * p.g + x.j, zv = zk + p.b * p.g;
         int idx = 0;
@@ -245,6 +247,7 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
                     qf[kk][nh][i] = head < p.G ? *reinterpret_cast<const uint32_t *>(q + head * D + ch) : 0u;
                 }
     }
+    asm volatile("bar.sync 2, %0;" ::"n"(PL::kThreads) : "memory");
     float m[NH][2], l[NH][2];
     float o[D / 16][NH][4];
 #pragma unroll
@@ -441,7 +444,7 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     if (early && (!p.defer || blockIdx.x == gridDim.x - 1))
         grid_dependency_wait();   // (deferred merge: one CTA, so that this grid ends behind the prefix's)
     const int n_pre = kMode == kPieceSuffix ? p.pre_n[x.beta] : 0;
-    const bool defer = kMode == kPieceWeights || (kMode == kPieceSuffix && p.defer);
+    const bool defer = kMode == kPieceWeights || p.defer;
     const bool whole = !defer && x.count == 1 && n_pre == 0;
     const size_t rec = blockIdx.x;
     __nv_bfloat16 *ob = p.out + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * p.G) * D;
@@ -503,29 +506,134 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     merge_records<D>(p, x, rec - x.index, n_pre, reinterpret_cast<float *>(smem), tid, kWarps * 32);
 }
 
-// The merge of a deferred suffix launch: a CTA a segment.  Bound by the records' bytes, in L2.
-constexpr int kMergeThreads = 128;
+// The merge of many records by CTAs of their own, 128 floats each: a head of 128 channels or two of 64.  The
+// warps take the records in turn, 128 floats a warp and record, eight at a time on the way, and add up in the
+// warps' order.  Bound by the records' bytes, in L2, and three round trips to it.  For few records a CTA a segment
+// (merge_records): 1024 segments of 6 records of 4 heads of 128 6.4 us, 25 with four of these CTAs each; one segment of 152
+// records of 12 heads of 64 3 us, 23 with one CTA.
+constexpr int kWideRecords = 16;
+constexpr int kMergeThreads = 256;
 template <int D>
-__global__ void __launch_bounds__(kMergeThreads) merge_kernel(const __grid_constant__ PieceParams p)
+struct MergeShared {
+    static constexpr int kRows = 128 / D;   // heads of a CTA; the last one may be past the group
+    float inv[kRows];
+    float4 sum[kMergeThreads / 32][32];
+};
+template <int D>
+__device__ void merge_rows(MergeShared<D> &sh, const PieceParams &p, const Piece &x, size_t own0, int n_pre, int part,
+                           float *s_w)
+{
+    constexpr int R = MergeShared<D>::kRows, W = kMergeThreads / 32, U = 8;
+    const int G = p.G, n = x.count + n_pre, tid = static_cast<int>(threadIdx.x), warp = tid >> 5, lane = tid & 31;
+    const size_t pre0 =
+        n_pre > 0 ? (static_cast<size_t>(p.pre_place[x.beta]) * p.g + x.j) * p.pre_chunks : 0;
+    auto lse_of = [&](int k, int head) {
+        return k < x.count ? __ldcg(p.part_lse + (own0 + k) * G + head)
+                           : __ldcg(p.pre_lse + (pre0 + (k - x.count)) * G + head);
+    };
+    for (int i = tid; i < n * R; i += kMergeThreads) {
+        const int head = part * R + i % R;
+        s_w[i] = head < G ? lse_of(i / R, head) : neg_inf();
+    }
+    __syncthreads();
+    if (warp < R) {
+        float mx = neg_inf(), tot = 0.f;
+        for (int k = lane; k < n; k += 32)
+            mx = fmaxf(mx, s_w[k * R + warp]);
+        for (int d = 16; d > 0; d >>= 1)
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+        for (int k = lane; k < n; k += 32) {
+            const float lse = s_w[k * R + warp];
+            const float w = lse == neg_inf() ? 0.f : fast_exp2(lse - mx);   // (a NaN goes on)
+            s_w[k * R + warp] = w;
+            tot += w;
+        }
+        for (int d = 16; d > 0; d >>= 1)
+            tot += __shfl_xor_sync(0xffffffffu, tot, d);
+        if (lane == 0)
+            sh.inv[warp] = tot == 0.f ? 0.f : 1.f / tot;
+    }
+    __syncthreads();
+    const int r = lane * 4 / D, head = part * R + r;
+    const bool live = head < G;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = warp; live && k0 < n; k0 += U * W) {
+        float4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = k0 + u * W;
+            const float *rec = k < x.count ? p.part_o + (own0 + k) * G * D : p.pre_o + (pre0 + (k - x.count)) * G * D;
+            v[u] = k < n ? __ldcg(reinterpret_cast<const float4 *>(rec + part * 128) + lane)
+                         : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = k0 + u * W;
+            const float w = k < n ? s_w[k * R + r] : 0.f;
+            if (w != 0.f) {
+                acc.x = fmaf(w, v[u].x, acc.x);
+                acc.y = fmaf(w, v[u].y, acc.y);
+                acc.z = fmaf(w, v[u].z, acc.z);
+                acc.w = fmaf(w, v[u].w, acc.w);
+            }
+        }
+    }
+    sh.sum[warp][lane] = acc;
+    __syncthreads();
+    if (warp == 0 && live) {
+#pragma unroll
+        for (int w = 1; w < W; ++w) {
+            const float4 v = sh.sum[w][lane];
+            acc.x += v.x;
+            acc.y += v.y;
+            acc.z += v.z;
+            acc.w += v.w;
+        }
+        const float inv = sh.inv[r];
+        uint2 w2;
+        w2.x = pack_bf16x2(acc.x * inv, acc.y * inv);
+        w2.y = pack_bf16x2(acc.z * inv, acc.w * inv);
+        *reinterpret_cast<uint2 *>(p.out + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * G) * D +
+                                   part * 128 + lane * 4) = w2;
+    }
+}
+
+template <int kMode>
+__device__ __forceinline__ Piece segment_of(const PieceParams &p, int seg)
+{
+    Piece x;
+    x.seg = seg;
+    x.beta = seg / p.g;
+    x.j = seg - x.beta * p.g;
+    x.L = p.seq_len[x.beta];
+    const int nt = kMode == kPieceBlocks ? p.n_blocks : (x.L + T - 1) / T;
+    x.count = (nt + p.tiles - 1) / p.tiles;
+    return x;
+}
+
+template <int D, int kMode, bool kWide>
+__global__ void __launch_bounds__(kWide ? kMergeThreads : 128) merge_kernel(const __grid_constant__ PieceParams p)
 {
     extern __shared__ float s_w[];
-    Piece x;
-    x.seg = static_cast<int>(blockIdx.x);
-    x.beta = x.seg / p.g;
-    x.j = x.seg - x.beta * p.g;
-    x.L = p.seq_len[x.beta];
-    x.count = (((x.L + T - 1) / T) + p.tiles - 1) / p.tiles;
+    const int parts = kWide ? (p.G * D + 127) / 128 : 1, seg = static_cast<int>(blockIdx.x) / parts;
+    const Piece x = segment_of<kMode>(p, seg);
+    const size_t own0 = static_cast<size_t>(p.first[x.beta]) + static_cast<size_t>(x.j) * x.count;
+    const int n_pre = kMode == kPieceSuffix ? p.pre_n[x.beta] : 0;
     grid_dependency_wait();
     grid_dependents_launch();
-    merge_records<D>(p, x, static_cast<size_t>(p.first[x.beta]) + static_cast<size_t>(x.j) * x.count,
-                     p.pre_n[x.beta], s_w, static_cast<int>(threadIdx.x), kMergeThreads);
+    if constexpr (kWide) {
+        __shared__ MergeShared<D> sh;
+        merge_rows<D>(sh, p, x, own0, n_pre, static_cast<int>(blockIdx.x) % parts, s_w);
+    } else {
+        merge_records<D>(p, x, own0, n_pre, s_w, static_cast<int>(threadIdx.x), 128);
+    }
 }
 
 // --------------------------------------------------------------------------------------------------
 // kPieceWeights: what each position got
 // --------------------------------------------------------------------------------------------------
 
-// A segment's CTA 0 merges its records into out, CTA 1 + k takes chunk k of its positions.  Bound by the scores' and weights' bytes, 4 G + 8 a position of a KV head (the scores from L2
+// A segment's first CTAs merge its records into out (merge_rows), the others take a chunk of its positions each.  Bound by the scores' and weights' bytes, 4 G + 8 a position of a KV head (the scores from L2
 // where they fit).
 constexpr int kWeightThreads = 256;
 template <int D>
@@ -536,21 +644,22 @@ __global__ void __launch_bounds__(kWeightThreads, 6)
     extern __shared__ float s_w[];
     grid_dependency_wait();
     grid_dependents_launch();
+    static_assert(kWeightThreads == kMergeThreads, "one size of CTA");
+    __shared__ MergeShared<D> sh;
     const int seg = static_cast<int>(blockIdx.x) / w.ctas, tid = static_cast<int>(threadIdx.x);
-    const int part = static_cast<int>(blockIdx.x) - seg * w.ctas;
-    Piece x;
-    x.beta = seg / p.g;
-    x.j = seg - x.beta * p.g;
-    x.L = p.seq_len[x.beta];
-    x.seg = seg;
-    x.count = (((x.L + T - 1) / T) + p.tiles - 1) / p.tiles;
+    const int parts = w.merge_ctas;
+    const int part = static_cast<int>(blockIdx.x) - seg * w.ctas - parts;   // chunk of positions
+    const Piece x = segment_of<kPieceWeights>(p, seg);
     const size_t rec0 = static_cast<size_t>(p.first[x.beta]) + static_cast<size_t>(x.j) * x.count;
     const int G = p.G;
-    if (part == 0) {
-        merge_records<D>(p, x, rec0, 0, s_w, tid, kWeightThreads);
+    if (part < 0) {
+        if (w.wide)
+            merge_rows<D>(sh, p, x, rec0, 0, part + parts, s_w);
+        else
+            merge_records<D>(p, x, rec0, 0, s_w, tid, kWeightThreads);
         return;
     }
-    const int u0 = (part - 1) * w.chunk, u1 = min(u0 + w.chunk, w.max_seq);
+    const int u0 = part * w.chunk, u1 = min(u0 + w.chunk, w.max_seq);
     const size_t row = static_cast<size_t>(seg) * w.max_seq;
     if (u0 < x.L) {
         // log2 of every head's sum, from the records: a warp a head
@@ -605,17 +714,6 @@ __global__ void __launch_bounds__(kWeightThreads, 6)
                 w.weights_out[row + u] = before[k] + (u < x.L ? a[k] : 0.f);   // (a NaN ends with its sequence)
         }
     }
-}
-
-// Queries of the sequences that share a prefix, side by side.
-__global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackParams p)
-{
-    grid_dependency_wait();
-    grid_dependents_launch();
-    const uint4 *from = reinterpret_cast<const uint4 *>(p.Q) + static_cast<size_t>(p.seq[blockIdx.x]) * p.row_vecs;
-    uint4 *to = reinterpret_cast<uint4 *>(p.packed) + static_cast<size_t>(blockIdx.x) * p.row_vecs;
-    for (int i = threadIdx.x; i < p.row_vecs; i += 256)
-        to[i] = from[i];
 }
 
 template <int D, int NH>
@@ -679,32 +777,47 @@ cudaError_t launch_pieces(int head_dim, int mode, const CUtensorMap *tmap, const
                       piece_smem(head_dim), stream, args);
 }
 
-cudaError_t launch_merge_pieces(int head_dim, const PieceParams &p, int most, cudaStream_t stream)
+// Room for the merge's weights.
+size_t merge_smem(int head_dim, int G, int most)
 {
-    const size_t smem = sizeof(float) * (static_cast<size_t>(most) + 1) * p.G;
-    void *args[] = {const_cast<PieceParams *>(&p)};
-    return launch_pdl(head_dim == 64 ? reinterpret_cast<const void *>(&merge_kernel<64>)
-                                     : reinterpret_cast<const void *>(&merge_kernel<128>),
-                      dim3(static_cast<unsigned>(p.b) * p.g), kMergeThreads, smem, stream, args);
+    return sizeof(float) * (most > kWideRecords ? static_cast<size_t>(most) * (128 / head_dim)
+                                                : (static_cast<size_t>(most) + 1) * G);
 }
 
-cudaError_t launch_weights(int head_dim, const PieceParams &p, const WeightsParams &w, int max_len,
+template <int D, int kMode>
+const void *merge_fn(bool wide)
+{
+    return wide ? reinterpret_cast<const void *>(&merge_kernel<D, kMode, true>)
+                : reinterpret_cast<const void *>(&merge_kernel<D, kMode, false>);
+}
+
+cudaError_t launch_merge_pieces(int head_dim, int mode, const PieceParams &p, int most, cudaStream_t stream)
+{
+    const bool wide = most > kWideRecords;
+    const void *fn = head_dim == 64 ? mode == kPieceBlocks ? merge_fn<64, kPieceBlocks>(wide)
+                                                           : merge_fn<64, kPieceSuffix>(wide)
+                     : mode == kPieceBlocks ? merge_fn<128, kPieceBlocks>(wide)
+                                            : merge_fn<128, kPieceSuffix>(wide);
+    void *args[] = {const_cast<PieceParams *>(&p)};
+    const unsigned ctas = wide ? static_cast<unsigned>((p.G * head_dim + 127) / 128) : 1u;
+    return launch_pdl(fn, dim3(ctas * static_cast<unsigned>(p.b) * p.g), wide ? kMergeThreads : 128,
+                      merge_smem(head_dim, p.G, most), stream, args);
+}
+
+void plan_weights(int head_dim, int G, int most, WeightsParams *w)
+{
+    w->wide = most > kWideRecords ? 1 : 0;
+    w->merge_ctas = w->wide ? (G * head_dim + 127) / 128 : 1;
+}
+
+cudaError_t launch_weights(int head_dim, const PieceParams &p, const WeightsParams &w, int most,
                            cudaStream_t stream)
 {
-    // room for the merge weights of the longest segment's records
-    const int most = (((max_len + T - 1) / T) + p.tiles - 1) / p.tiles;
-    const size_t smem = sizeof(float) * (static_cast<size_t>(most) + 1) * p.G;
+    const size_t smem = merge_smem(head_dim, p.G, most);
     void *args[] = {const_cast<PieceParams *>(&p), const_cast<WeightsParams *>(&w)};
     return launch_pdl(head_dim == 64 ? reinterpret_cast<const void *>(&weights_kernel<64>)
                                      : reinterpret_cast<const void *>(&weights_kernel<128>),
                       dim3(static_cast<unsigned>(w.ctas) * p.b * p.g), kWeightThreads, smem, stream, args);
-}
-
-cudaError_t launch_pack(const PackParams &p, cudaStream_t stream)
-{
-    void *args[] = {const_cast<PackParams *>(&p)};
-    return launch_pdl(reinterpret_cast<const void *>(&pack_kernel), dim3(static_cast<unsigned>(p.n)), 256, 0,
-                      stream, args);
 }
 
 }  // namespace mlkv

@@ -293,11 +293,9 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
     using PL = PrefillPlan<D, kForm>;
     static_assert(!kShared || !kWin, "no window over a shared prefix");
     constexpr bool kSplit = PL::kSBuf == 2;   // key tiles alternate between two warpgroups
-    // (the decode over a shared prefix writes records straight from its registers; a unit of it may leave tile A
-    // out, whose warps would arrive ahead of the unit)
-    constexpr bool kStageInQ = PL::kStageInQ && !(kFused && kShared);
     constexpr int NQ = PL::kQBufs;
     constexpr int R = PL::kRingTiles;
+    constexpr int kAhead = R + 4;   // decode over a shared prefix: ring tiles ahead that are prefetched
     // Query tile g's shared-memory slot and tensor-memory columns (the only tile of a one-tile CTA
     // is tile B, in slot 0).
     auto slot_of = [](int g) { return PL::kTiles == 1 ? 0 : g; };
@@ -329,7 +327,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
             // S and, where the outputs are staged in the query tiles, by the softmax warps
             mbar_init(bar_q + 8 * q,
                       kSplit && kFused && p.q_host != nullptr ? PL::kSoftWarps : 1);
-            mbar_init(bar_q_free + 8 * q, 1 + (kStageInQ ? PL::kSoftWarps : 0));
+            mbar_init(bar_q_free + 8 * q, 1 + (PL::kStageInQ ? PL::kSoftWarps : 0));
         }
         for (int s = 0; s < R; ++s) {
             mbar_init(bar_full + 8 * s, 1);
@@ -450,6 +448,16 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                 grid_dependency_wait();   // the tile that holds the new row
                 waited = true;
             }
+            if constexpr (kFused && kShared) {
+                // Tiles ahead of the ring go to L2: each of these CTAs streams alone on its SM, and four tiles of 128
+                // channels in flight do not cover HBM's latency.
+                const int ahead = k + kAhead;
+                if (ahead < 2 * x.n_b)
+#pragma unroll
+                    for (int sub = 0; sub < PL::kSub; ++sub)
+                        tma_prefetch_3d(&tmap_k, sub * 64, (x.kt0 + (ahead >> 1)) * 128,
+                                        (ahead & 1) ? x.zv : x.zk);
+            }
             const uint32_t fb = bar_full + 8 * s;
             mbar_arrive_expect_tx(fb, PL::kTileBytes);
 #pragma unroll
@@ -493,6 +501,23 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
             // from the block's first layer (tile B) and its layer L1 (tile A)
             const int box_rows =
                 kFused ? (p.fused_L < p.fused_L1 ? p.fused_L : p.fused_L1) * p.G : 128;
+            if constexpr (kFused && kShared) {
+                if (p.scattered) {
+                    // One box of G rows a sequence.  (The swizzle goes by the address: a box may start on any row
+                    // of its tile.)  Rows behind the last sequence hold anything: nobody reads what becomes of them.
+                    const int most = min(x.seqs, n_tiles * p.fused_L1);
+                    mbar_arrive_expect_tx(qbar, most * p.G * PL::kSub * 128);
+                    for (int i = 0; i < most; ++i) {
+                        const int g = i < p.fused_L1 ? 1 : 0, row = (i - (g ? 0 : p.fused_L1)) * p.G;
+#pragma unroll
+                        for (int sub = 0; sub < PL::kSub; ++sub)
+                            tma_load_5d(dst + slot_of(g) * PL::kTileBytes + sub * 16384 + row * 128, &tmap_q,
+                                        qbar, sub * 64, 0, x.j, 0, p.seq[x.place + i]);
+                    }
+                    ++uc;
+                    return true;
+                }
+            }
             mbar_arrive_expect_tx(qbar, n_tiles * PL::kSub * box_rows * 128);
             for (int g = 1; g >= 2 - n_tiles; --g)
 #pragma unroll
@@ -1038,17 +1063,31 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                              p.fused_cmax + y.chunk) * p.G + (r - sq * p.G);
                     if (valid)
                         p.part_lse[row] = m_run + log2f(l_run);
-                    float *prow = p.part + row * D;
+                    // 32 channels of the warp's 32 rows at a time through shared memory (16-byte chunks swizzled
+                    // by row): 8 lanes a row, whole lines.  (A row a thread, 16 bytes a store, took 4 us more a
+                    // unit of 256 rows of 128 channels.)
+                    const int rw0 = (warp & 3) * 32;
+                    uint8_t *stage = PL::kStageInQ ? q_slot + rw0 * 128 : smem + PL::kStage + warp * 4096;
+                    const int row_lo = static_cast<int>(row);   // (records number less than 2^31)
 #pragma unroll
                     for (int c = 0; c < PL::kSub * 2; ++c) {
                         float ov[32];
                         load_o(c, ov);
-                        if (valid) {
+                        __syncwarp();
 #pragma unroll
-                            for (int k = 0; k < 32; k += 4)
-                                *reinterpret_cast<float4 *>(prow + c * 32 + k) =
-                                    make_float4(ov[k] * inv, ov[k + 1] * inv, ov[k + 2] * inv,
-                                                ov[k + 3] * inv);
+                        for (int k = 0; k < 32; k += 4)
+                            *reinterpret_cast<float4 *>(stage + lane * 128 + (((k >> 2) ^ (lane & 7)) << 4)) =
+                                make_float4(ov[k] * inv, ov[k + 1] * inv, ov[k + 2] * inv, ov[k + 3] * inv);
+                        __syncwarp();
+#pragma unroll
+                        for (int it = 0; it < 8; ++it) {
+                            const int rl = it * 4 + (lane >> 3);
+                            const float4 line = *reinterpret_cast<const float4 *>(
+                                stage + rl * 128 + (((lane & 7) ^ (rl & 7)) << 4));
+                            const int to = __shfl_sync(0xffffffffu, row_lo, rl);
+                            if (rw0 + rl < n_rows && !stop)
+                                *reinterpret_cast<float4 *>(p.part + static_cast<size_t>(to) * D + c * 32 +
+                                                            (lane & 7) * 4) = line;
                         }
                     }
                 } else if (kFused && p.fused_cmax > 1) {
@@ -1130,10 +1169,13 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                 }
                 tmem_fence_before();
             }
-            if (kStageInQ) {
+            if (PL::kStageInQ) {
                 // The next queries may be written over the stage.  (Every warpgroup has a tile in
                 // every unit here: two query tiles at head_dim 64 are a fused block of more rows
-                // than one holds.)
+                // than one holds.  Over a shared prefix tile A may be left out: its warps wait for
+                // the unit's queries, so as not to arrive ahead of the units.)
+                if (kFused && kShared && n_g == 0)
+                    wait(bar_q + 8 * qb, n / NQ);
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0)

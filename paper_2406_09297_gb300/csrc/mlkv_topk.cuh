@@ -30,16 +30,15 @@ struct TopkShared {
 };
 
 // CTA `rank` of a cluster of `size` holds keys key(0) .. key(n - 1), whose least and largest are lo and hi in
-// all threads (0xffffffff and 0 of none); the cluster holds at least `want` >= 1 keys.  Calls put(place, i) for
+// all threads (0xffffffff and 0 of none); the cluster (size 1: this CTA alone, whatever its cluster) holds at least `want` >= 1 keys.  Calls put(place, i) for
 // every one of its keys among the `want` largest, place its rank in the list's order among those.  All NT >= 256
 // threads of all the cluster's CTAs call it, behind a barrier for the keys.
 template <int NT, typename Key, typename Put>
-__device__ void cluster_topk(TopkShared<NT> &sh, int n, unsigned lo, unsigned hi, unsigned want, const Key &key,
-                             const Put &put)
+__device__ void cluster_topk(TopkShared<NT> &sh, unsigned size, unsigned rank, int n, unsigned lo, unsigned hi,
+                             unsigned want, const Key &key, const Put &put)
 {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
-    const unsigned size = cluster.num_blocks(), rank = cluster.block_rank();
     const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = tid >> 5;
     constexpr int W = NT / 32;
     auto sync = [&] {

@@ -484,11 +484,17 @@ def mlkv_prefill_prefix(handle, layer, prefix, prefix_of, prefix_lens, Q, K, V, 
                                           p, s_max, _stream(stream)))
 
 
-def _dense(name, t, dtype, numel=None):
-    """A dense tensor's address; its type, and its size where it is known, are checked."""
-    if str(t.dtype) != "torch." + dtype or not t.is_contiguous() or numel not in (None, t.numel()):
-        raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must be dense, {dtype}" +
-                        ("" if numel is None else f" and of {numel} elements"))
+_dtypes = {}
+
+
+def _dense(name, t, dtype):
+    """A dense tensor's address; its type is checked."""
+    want = _dtypes.get(dtype)
+    if want is None:
+        import torch
+        want = _dtypes[dtype] = getattr(torch, dtype)
+    if t.dtype is not want or not t.is_contiguous():
+        raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must be dense and {dtype}")
     return t.data_ptr()
 
 
@@ -521,7 +527,7 @@ def mlkv_decode_attention_blocks(handle, layer, Q, out, seq_lens, blocks, n_bloc
 def mlkv_decode_attention_weights(handle, layer, Q, out, seq_lens, weights_in, weights_out, stream=None):
     """weights fp32 [b][g][max_seq]; weights_in None: zeros."""
     a, p = _lens_ptr(seq_lens)
-    w = None if weights_in is None else _dense("weights_in", weights_in, "float32", weights_out.numel())
+    w = None if weights_in is None else _dense("weights_in", weights_in, "float32")
     return _check(lib.mlkv_decode_attention_weights(handle, layer, _ptr(Q), _ptr(out), p, w,
                                                     _dense("weights_out", weights_out, "float32"),
                                                     _stream(stream)))
@@ -589,11 +595,12 @@ class MLKVCache:
                                    window, sinks, stream)
 
     def _sized(self, name, t, *shape):
-        if t is not None and tuple(t.shape) != shape:
+        if t is not None and t.shape != shape:
             raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must be of shape {list(shape)}")
 
     def _host(self, name, a, n):
-        a = as_seq_lens(a)
+        if not (isinstance(a, np.ndarray) and a.dtype == _INT32 and a.flags.c_contiguous):
+            a = as_seq_lens(a)
         if a.shape != (n,):
             raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must hold {n} numbers")
         return a
