@@ -19,6 +19,7 @@ constexpr int kBlock = MLKV_BLOCK;
 enum : int {
     kPieceSuffix = 0,   // positions [0, seq_len), merged with a shared prefix's records
     kPieceBlocks = 1,   // the blocks listed for every (sequence, KV head)
+    kPieceJoined = 3,   // a prefix's positions, read for every sequence apart, and then [0, seq_len)
     kPieceWeights = 2,  // positions [0, seq_len); every score is stored, the merge left to weights_kernel
 };
 
@@ -51,15 +52,32 @@ struct PieceParams {
     long long score_stride;
     int seq_len[MLKV_MAX_BATCH];
     int first[MLKV_MAX_BATCH + 1];        // first piece of sequence beta (KV head after KV head inside)
-    uint16_t pre_place[MLKV_MAX_BATCH];   // kPieceSuffix: place of the sequence in the prefix's records
-    uint16_t pre_n[MLKV_MAX_BATCH];       // and their number
+    uint16_t pre_place[MLKV_MAX_BATCH];   // kPieceSuffix: place of the sequence in the prefix's records;
+                                          // kPieceJoined: its prefix's number
+    union {
+        uint16_t pre_n[MLKV_MAX_BATCH];   // kPieceSuffix: those records' number
+        int pre_len[MLKV_MAX_BATCH];      // kPieceJoined: positions of its prefix, 0: none
+    };
+    int prefix_b;                         // kPieceJoined: sequences of the prefix cache
 };
+// Tiles of a segment.
+template <int kMode>
+__host__ __device__ inline int piece_tiles(const PieceParams &p, int beta)
+{
+    if (kMode == kPieceBlocks)
+        return p.n_blocks;
+    const int own = static_cast<int>((static_cast<unsigned>(p.seq_len[beta]) + kBlock - 1) / kBlock);
+    return kMode == kPieceJoined
+               ? static_cast<int>((static_cast<unsigned>(p.pre_len[beta]) + kBlock - 1) / kBlock) + own
+               : own;
+}
 // Most records (pieces and a prefix's) that a segment's merge holds the weights of.
 int piece_max_records(int head_dim, int group);
 int piece_stages(int head_dim);   // tiles of a piece that are worked on at a time
 cudaError_t prepare_pieces(int head_dim, int group, int mode, int *ctas_per_sm);
-cudaError_t launch_pieces(int head_dim, int mode, const CUtensorMap *tmap, const PieceParams &p,
-                          cudaStream_t stream);
+// tmap_prefix: the prefix cache's (kPieceJoined; else not read).
+cudaError_t launch_pieces(int head_dim, int mode, const CUtensorMap *tmap, const CUtensorMap *tmap_prefix,
+                          const PieceParams &p, cudaStream_t stream);
 
 // The merge of a deferred launch's segments, of `most` records at most.
 cudaError_t launch_merge_pieces(int head_dim, int mode, const PieceParams &p, int most, cudaStream_t stream);

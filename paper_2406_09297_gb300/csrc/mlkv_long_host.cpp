@@ -24,7 +24,7 @@ using mlkv::overlap;
 namespace {
 
 // Bits of mlkv_cache::long_ready.
-enum : unsigned { kReadyPieces = 1, kReadySelect = 8, kReadyEvict = 16, kReadyShared = 32 };   // pieces: 3 bits
+enum : unsigned { kReadyPieces = 1, kReadySelect = 16, kReadyEvict = 32, kReadyShared = 64 };   // pieces: 4 bits
 
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
@@ -55,46 +55,52 @@ int prepare_pieces(mlkv_cache *c, int mode)
     return MLKV_OK;
 }
 
-// Cuts the segments, nt(beta) tiles each, into pieces of at most p.tiles tiles: the least estimated time, in us.  A
+// How the segments, nt(beta) tiles each, are cut into pieces: the least estimated time, in us.  A
 // launch takes 4.5, and what is longer of its bytes at the rate of HBM and its longest piece; pieces beyond one wave
 // of resident CTAs half a piece more where segments are split (whole ones end evenly enough).  Split segments
 // are merged by the CTA that ends last, a round trip to L2 for every 8 records, or by a launch of their own
 // (`may_defer`; weights: always).  Never more pieces than there are records, nor of a segment than `most`.
-// `pre`: records that every merge has besides.
+// `pre`: records that every merge has besides.  hbm_tiles: tiles that come from HBM, the others from L2 (10 TB/s); -1: all.
 struct Cut {
     bool defer;
     int records;   // of a segment, at most
+    int tiles;     // of a piece
+    double us;     // estimated
 };
 template <typename Tiles>
-Cut cut(const mlkv_cache *c, mlkv::PieceParams &p, bool may_defer, bool must_defer, int pre, const Tiles &nt)
+Cut plan_cut(const mlkv_cache *c, bool may_defer, bool must_defer, int pre, double hbm_tiles, const Tiles &nt)
 {
     long long total = 0;
-    int longest = 1;
+    int longest = 1, shortest = 0x7fffffff;
     for (int beta = 0; beta < c->b; ++beta) {
-        total += nt(beta);
-        longest = std::max(longest, nt(beta));
+        const int n = nt(beta);
+        total += n;
+        longest = std::max(longest, n);
+        shortest = std::min(shortest, n);
     }
     total *= c->g;
     const long long slots = static_cast<long long>(c->piece_ctas) * c->sm_count;
     const int stages = mlkv::piece_stages(c->d);
     // us: a tile of a CTA alone on its SM; all tiles at the rate of HBM; a record's part of an inline merge
     const double tile = c->d == 64 ? 0.33 : c->G <= 8 ? 0.45 : 0.72;
-    const double bytes = total * 256.0 * c->d / 6.7e6, record = 0.1 * c->G * c->d / 512;
+    const double from_hbm = hbm_tiles < 0 ? total : hbm_tiles;
+    const double bytes = std::max(from_hbm / 6.7e6, total / 10e6) * 256.0 * c->d, record = 0.1 * c->G * c->d / 512;
     const int inline_most = mlkv::piece_max_records(c->d, c->G) - pre;
-    Cut best = {must_defer, 1};
-    double best_t = 1e30;
-    int best_tiles = longest;
+    Cut best = {must_defer, 1, longest, 1e30};
     for (int want = 1, tiles = longest;; want += (want + 7) / 8) {   // pieces of the longest segment
         const int next = (longest + want - 1) / want;
         if (want > 1 && next == tiles)
             continue;
         tiles = next;
         long long n = 0;
-        for (int beta = 0; beta < c->b; ++beta)
-            n += (nt(beta) + tiles - 1) / tiles;
+        if (shortest == longest)
+            n = static_cast<long long>(c->b) * ((longest + tiles - 1) / tiles);
+        else
+            for (int beta = 0; beta < c->b; ++beta)
+                n += (nt(beta) + tiles - 1) / tiles;
         n *= c->g;
         const int pieces = (longest + tiles - 1) / tiles, records = pieces + pre;
-        if (want > 1 && (n > c->records || records > mlkv::kDeferMaxRecords))
+        if (want > 1 && (n > std::min(c->records, 4 * slots) || records > mlkv::kDeferMaxRecords))
             break;
         const double rounds = (tiles + stages - 1) / stages;   // (a short piece's tiles come at once)
         double t = 4.5 + std::max(bytes, 1.15 * std::max(tiles * tile, rounds * 1.2));
@@ -103,22 +109,25 @@ Cut cut(const mlkv_cache *c, mlkv::PieceParams &p, bool may_defer, bool must_def
         const double here = records <= 1 ? 0.0 : 2.5 + record * records, apart = 4.5;
         const bool defer = must_defer || (may_defer && (here > apart || records > inline_most) && records > 1);
         t += defer ? apart : here;
-        if (t < best_t && (defer || records <= inline_most || pieces == 1)) {
-            best_t = t;
-            best = {defer, records};
-            best_tiles = tiles;
-        }
+        if (t < best.us && (defer || records <= inline_most || pieces == 1))
+            best = {defer, records, tiles, t};
         if (tiles == 1)
             break;
     }
-    p.tiles = best_tiles;
+    return best;
+}
+
+// Lays the pieces of a plan out: p.tiles and p.first.
+template <typename Tiles>
+void lay_pieces(const mlkv_cache *c, mlkv::PieceParams &p, const Cut &split, const Tiles &nt)
+{
+    p.tiles = split.tiles;
     long long at = 0;
     for (int beta = 0; beta < c->b; ++beta) {
         p.first[beta] = static_cast<int>(at);
         at += static_cast<long long>(c->g) * ((nt(beta) + p.tiles - 1) / p.tiles);
     }
     p.first[c->b] = static_cast<int>(at);
-    return best;
 }
 
 void fill_pieces(const mlkv_cache *c, int layer, const void *Q, void *out, const int *seq_lens,
@@ -160,10 +169,11 @@ int scratch(mlkv_cache *c, size_t floats, const char *what, cudaStream_t stream)
 }
 
 // The piece launch, and the merge's where it is one of its own.
-int decode_pieces(const mlkv_cache *c, int mode, mlkv::PieceParams &p, const Cut &split, cudaStream_t stream)
+int decode_pieces(const mlkv_cache *c, int mode, mlkv::PieceParams &p, const Cut &split,
+                  const CUtensorMap *tmap_prefix, cudaStream_t stream)
 {
     p.defer = split.defer ? 1 : 0;
-    cudaError_t e = mlkv::launch_pieces(c->d, mode, rows64(c), p, stream);
+    cudaError_t e = mlkv::launch_pieces(c->d, mode, rows64(c), tmap_prefix, p, stream);
     if (e != cudaSuccess)
         return fail_cuda(e, "decode launch");
     if (p.defer && (e = mlkv::launch_merge_pieces(c->d, mode, p, split.records, stream)) != cudaSuccess)
@@ -176,15 +186,19 @@ struct PrefixPlan {
     int kc;       // key tiles of 128 positions of a unit
     int sms;      // CTAs of the prefix kernel, one an SM
     bool beside;  // the suffixes run beside it on the other SMs, and are merged by a launch of their own
+    double us;    // estimated
 };
 
 // For `pairs` unit columns (pairs of query tiles times KV heads) over prefixes of n_kt tiles, and suffixes of
-// `bytes`: the least estimated time.  Microseconds: a unit's key tile `tile`, its start and end three of them; the
+// `bytes`: the least estimated time.  Microseconds: a unit's key tile `tile`, its start and end `edges` of them; the
 // suffixes at most `rate` bytes a us an SM and `all` in total.  (The prefix kernel is bound by the tensor cores where
-// many sequences share one, the suffixes by HBM: side by side, each has what the other leaves.)
+// many sequences share one, the suffixes by HBM: side by side, each has what the other leaves.  Not for
+// suffixes of less than 16 MB, which the merge's launch outweighs.)  Fitted to eight shapes, each in ten splits: the
+// one taken is at most 3% behind the best of them.  128 sequences of 1024, 8 KV heads of 128, over one prefix of
+// 32768: 115 us beside 80 SMs of 52 tiles a unit, 147 one after the other.
 PrefixPlan plan_prefix(const int *n_kt, const int *pairs, int n, int sm_count, int d, double bytes)
 {
-    const double tile = d == 64 ? 0.9 : 1.65, rate = 62e3, all = 6.5e6, merge = 5.0;
+    const double tile = d == 64 ? 0.95 : 1.5, edges = 7, rate = 75e3, all = 6.5e6, start = 13;
     long long work = 0;
     int longest = 1;
     for (int x = 0; x < n; ++x) {
@@ -193,32 +207,21 @@ PrefixPlan plan_prefix(const int *n_kt, const int *pairs, int n, int sm_count, i
             longest = std::max(longest, n_kt[x]);
     }
     const int least = std::max(1, (longest + mlkv::kFusedMaxChunks - 1) / mlkv::kFusedMaxChunks);
-    PrefixPlan best = {longest, sm_count, false};
-    double best_t = 1e30;
+    PrefixPlan best = {longest, sm_count, false, 1e30};
     for (int kc = std::max<long long>(least, work / (4LL * sm_count)); kc <= longest; kc += (kc + 15) / 16) {
         long long units = 0;
         for (int x = 0; x < n; ++x)
             units += static_cast<long long>((n_kt[x] + kc - 1) / kc) * pairs[x];
         for (int rounds = 1; rounds <= 8; ++rounds) {   // of the units, on as many SMs as it takes
-            const int need = static_cast<int>((units + rounds - 1) / rounds);
-            const int sms = std::min(sm_count, need);
-            double t = static_cast<double>((units + sms - 1) / sms) * (kc + 3) * tile;
-            if (need >= sm_count || sm_count - sms < 8) {
-                t += bytes / all;
-            } else {
-                const double beside = t * std::min(all, rate * (sm_count - sms));
-                t += std::max(0.0, bytes - beside) / all + merge;
-            }
-            if (t < best_t) {
-                best_t = t;
-                best = {kc, sms, need < sm_count && sm_count - sms >= 8};
-            }
-            // the same one after the other, without a merge of its own
-            const double one = static_cast<double>((units + sms - 1) / sms) * (kc + 3) * tile + bytes / all;
-            if (one < best_t) {
-                best_t = one;
-                best = {kc, sms, false};
-            }
+            const int sms = static_cast<int>(std::min<long long>(sm_count, (units + rounds - 1) / rounds));
+            const double t = static_cast<double>((units + sms - 1) / sms) * (kc + edges) * tile;
+            const double one = start + 2 + t + bytes / all;
+            if (one < best.us)
+                best = {kc, sms, false, one};
+            const double beside =
+                start + t + std::max(0.0, bytes - t * std::min(all, rate * (sm_count - sms))) / all;
+            if (sm_count - sms >= 8 && bytes >= 16e6 && beside < best.us)
+                best = {kc, sms, true, beside};
         }
     }
     return best;
@@ -274,18 +277,37 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
         return rc;
     static thread_local mlkv::PieceParams p;
     static thread_local mlkv::SharedPrefillParams u;
+    static thread_local bool read[MLKV_MAX_BATCH];
     fill_pieces(c, layer, Q, out, seq_lens, p);
+    // Each sequence's prefix and positions end to end, if that is no longer than the prefixes apart: few sequences a
+    // prefix.
+    double hbm = 0, bytes = 0;   // tiles of 64 positions that are read once; bytes of the suffixes
+    for (int x = 0; x < prefix->b; ++x)
+        read[x] = false;
+    for (int beta = 0; beta < c->b; ++beta) {
+        const int x = prefix_of[beta];
+        p.pre_len[beta] = x >= 0 ? prefix_lens[x] : 0;
+        p.pre_place[beta] = static_cast<uint16_t>(x >= 0 ? x : 0);
+        hbm += (seq_lens[beta] + 63) / 64;
+        bytes += 4.0 * c->g * c->d * seq_lens[beta];
+        if (x >= 0 && !read[x]) {
+            read[x] = true;
+            hbm += (prefix_lens[x] + 63) / 64;
+        }
+    }
+    const auto joined = [&](int beta) { return mlkv::piece_tiles<mlkv::kPieceJoined>(p, beta); };
+    const Cut end_to_end = plan_cut(c, true, false, 0, hbm * c->g, joined);
     // Places: the sequences of prefix 0, then those of prefix 1, ...  Where every prefix's sequences are
     // neighbours already, a sequence's place is its own number.
     const int L1 = 128 / c->G, np = prefix->b;
     static thread_local int n_kt[MLKV_MAX_BATCH], pairs[MLKV_MAX_BATCH];
+    static thread_local PrefixPlan plan;
     std::fill(u.group_n, u.group_n + np, static_cast<uint16_t>(0));
     auto of = [&](int beta) { return prefix_of[beta] >= 0 && prefix_lens[prefix_of[beta]] > 0 ? prefix_of[beta] : -1; };
     bool neighbours = true;
     int places = 0;
     for (int beta = 0; beta < c->b; ++beta) {
         const int x = of(beta);
-        p.pre_place[beta] = static_cast<uint16_t>(beta);
         if (x < 0)
             continue;
         ++places;
@@ -295,7 +317,24 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
             neighbours = neighbours && of(beta - 1) == x;
     }
     u.scattered = neighbours ? 0 : 1;
+    int most_kt = 0;
+    for (int x = 0; x < np; ++x) {
+        n_kt[x] = u.group_n[x] > 0 ? (prefix_lens[x] + 127) / 128 : 0;
+        pairs[x] = (u.group_n[x] + 2 * L1 - 1) / (2 * L1) * c->g;
+        most_kt = std::max(most_kt, n_kt[x]);
+    }
+    if (most_kt > 0)
+        plan = plan_prefix(n_kt, pairs, np, c->sm_count, c->d, bytes);
+    if (most_kt == 0 || end_to_end.us <= plan.us) {
+        if ((rc = prepare_pieces(c, mlkv::kPieceJoined)) != MLKV_OK)
+            return rc;
+        p.prefix_b = prefix->b;
+        lay_pieces(c, p, end_to_end, joined);
+        return decode_pieces(c, mlkv::kPieceJoined, p, end_to_end, rows64(prefix), stream);
+    }
     if (neighbours) {
+        for (int beta = 0; beta < c->b; ++beta)
+            p.pre_place[beta] = static_cast<uint16_t>(beta);
         places = c->b;
     } else {
         int at = 0;
@@ -311,123 +350,108 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
                 u.seq[place] = static_cast<uint16_t>(beta);
             }
     }
-    int most_kt = 0;
+    if (!(c->long_ready & kReadyShared)) {
+        const cudaError_t e = mlkv::prepare_shared(c->d, true);
+        if (e != cudaSuccess)
+            return fail_cuda(e, "preparing the decode over a shared prefix");
+        c->long_ready |= kReadyShared;
+    }
+    const int kc = plan.kc;
+    p.defer = plan.beside ? 1 : 0;
+    const int cmax = (most_kt + kc - 1) / kc;
+    const size_t rows = static_cast<size_t>(places) * c->g * cmax * c->G;
+    if ((rc = scratch(c, rows * (c->d + 1), "records of the shared prefix", stream)) != MLKV_OK)
+        return rc;
+    u.part = c->fused_part;
+    u.part_lse = u.part + rows * c->d;
+    p.pre_o = u.part;
+    p.pre_lse = u.part_lse;
+    p.pre_chunks = cmax;
+    p.early = 1;
+    // The queries [b][h][D] as (channel, head in group, group, 1, sequence): a box of 64 channels x G heads x
+    // min(L1, b) neighbours is a tile's rows, one of 64 channels x G heads a scattered sequence's.
+    static EncodeTiledFn encode = driver_entry<EncodeTiledFn>("cuTensorMapEncodeTiled");
+    if (encode == nullptr)
+        return fail(MLKV_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable from the driver");
+    CUtensorMap tmap_q;
+    const cuuint64_t row = static_cast<cuuint64_t>(c->h) * c->d * 2;
+    const cuuint64_t dims[5] = {static_cast<cuuint64_t>(c->d), static_cast<cuuint64_t>(c->G),
+                                static_cast<cuuint64_t>(c->g), 1u, static_cast<cuuint64_t>(c->b)};
+    const cuuint64_t strides[4] = {static_cast<cuuint64_t>(c->d) * 2,
+                                   static_cast<cuuint64_t>(c->G) * c->d * 2, row, row};
+    const cuuint32_t box[5] = {64u, static_cast<cuuint32_t>(c->G), 1u, 1u,
+                               static_cast<cuuint32_t>(neighbours ? std::min(L1, c->b) : 1)};
+    const cuuint32_t estr[5] = {1u, 1u, 1u, 1u, 1u};
+    const CUresult r = encode(&tmap_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(Q), dims,
+                              strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS)
+        return fail(MLKV_ERR_CUDA, "cuTensorMapEncodeTiled(Q) failed (CUresult %d)",
+                    static_cast<int>(r));
+    const CUtensorMap *tmap_kv = nullptr;
+    for (auto &v : prefix->variants)
+        if (v.v->tile_tokens == 128)
+            tmap_kv = &v.tmap;
+    if (tmap_kv == nullptr)
+        return fail(MLKV_ERR_UNSUPPORTED, "no 128-position cache map for d=%d", c->d);
+    u.tmap_p = *tmap_kv;
+    u.out = nullptr;
+    u.err = c->err;
+    u.scale_log2 = p.scale_log2;
+    u.b = c->b;
+    u.h = c->h;
+    u.g = c->g;
+    u.G = c->G;
+    u.s_max = prefix->max_seq;
+    u.slot = p.slot;
+    u.head_pairs = 0;
+    u.sm_count = plan.sms;
+    u.window = u.sinks = 0;
+    u.kv_direct = 0;
+    u.fused_L = c->b;
+    u.fused_L1 = L1;
+    u.fused_nblk = 1;
+    u.fused_kc = kc;
+    u.fused_cmax = cmax;
+    u.fused_early = 0;
+    u.fused_combine_w = 1;
+    u.q_host = nullptr;
+    u.prefix_b = np;
+    std::memcpy(u.prompt_len, prefix_lens, sizeof(int) * np);
+    int n = 0;
+    auto issue = [&]() {
+        u.n_units = n;
+        n = 0;
+        return mlkv::launch_shared(c->d, true, &tmap_q, tmap_kv, tmap_kv, u, stream);
+    };
     for (int x = 0; x < np; ++x) {
-        n_kt[x] = u.group_n[x] > 0 ? (prefix_lens[x] + 127) / 128 : 0;
-        pairs[x] = (u.group_n[x] + 2 * L1 - 1) / (2 * L1) * c->g;
-        most_kt = std::max(most_kt, n_kt[x]);
-    }
-    int cmax = 0;
-    if (most_kt > 0) {
-        if (!(c->long_ready & kReadyShared)) {
-            const cudaError_t e = mlkv::prepare_shared(c->d, true);
-            if (e != cudaSuccess)
-                return fail_cuda(e, "preparing the decode over a shared prefix");
-            c->long_ready |= kReadyShared;
-        }
-        double bytes = 0;   // of the suffixes
-        for (int beta = 0; beta < c->b; ++beta)
-            bytes += 4.0 * c->g * c->d * seq_lens[beta];
-        const PrefixPlan plan = plan_prefix(n_kt, pairs, np, c->sm_count, c->d, bytes);
-        const int kc = plan.kc;
-        p.defer = plan.beside ? 1 : 0;
-        cmax = (most_kt + kc - 1) / kc;
-        const size_t rows = static_cast<size_t>(places) * c->g * cmax * c->G;
-        if ((rc = scratch(c, rows * (c->d + 1), "records of the shared prefix", stream)) != MLKV_OK)
-            return rc;
-        u.part = c->fused_part;
-        u.part_lse = u.part + rows * c->d;
-        p.pre_o = u.part;
-        p.pre_lse = u.part_lse;
-        p.pre_chunks = cmax;
-        p.early = 1;
-        // The queries [b][h][D] as (channel, head in group, group, 1, sequence): a box of 64 channels x G heads x
-        // min(L1, b) neighbours is a tile's rows, one of 64 channels x G heads a scattered sequence's.
-        static EncodeTiledFn encode = driver_entry<EncodeTiledFn>("cuTensorMapEncodeTiled");
-        if (encode == nullptr)
-            return fail(MLKV_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable from the driver");
-        CUtensorMap tmap_q;
-        const cuuint64_t row = static_cast<cuuint64_t>(c->h) * c->d * 2;
-        const cuuint64_t dims[5] = {static_cast<cuuint64_t>(c->d), static_cast<cuuint64_t>(c->G),
-                                    static_cast<cuuint64_t>(c->g), 1u, static_cast<cuuint64_t>(c->b)};
-        const cuuint64_t strides[4] = {static_cast<cuuint64_t>(c->d) * 2,
-                                       static_cast<cuuint64_t>(c->G) * c->d * 2, row, row};
-        const cuuint32_t box[5] = {64u, static_cast<cuuint32_t>(c->G), 1u, 1u,
-                                   static_cast<cuuint32_t>(neighbours ? std::min(L1, c->b) : 1)};
-        const cuuint32_t estr[5] = {1u, 1u, 1u, 1u, 1u};
-        const CUresult r = encode(&tmap_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(Q), dims,
-                                  strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-        if (r != CUDA_SUCCESS)
-            return fail(MLKV_ERR_CUDA, "cuTensorMapEncodeTiled(Q) failed (CUresult %d)",
-                        static_cast<int>(r));
-        const CUtensorMap *tmap_kv = nullptr;
-        for (auto &v : prefix->variants)
-            if (v.v->tile_tokens == 128)
-                tmap_kv = &v.tmap;
-        if (tmap_kv == nullptr)
-            return fail(MLKV_ERR_UNSUPPORTED, "no 128-position cache map for d=%d", c->d);
-        u.tmap_p = *tmap_kv;
-        u.out = nullptr;
-        u.err = c->err;
-        u.scale_log2 = p.scale_log2;
-        u.b = c->b;
-        u.h = c->h;
-        u.g = c->g;
-        u.G = c->G;
-        u.s_max = prefix->max_seq;
-        u.slot = p.slot;
-        u.head_pairs = 0;
-        u.sm_count = plan.sms;
-        u.window = u.sinks = 0;
-        u.kv_direct = 0;
-        u.fused_L = c->b;
-        u.fused_L1 = L1;
-        u.fused_nblk = 1;
-        u.fused_kc = kc;
-        u.fused_cmax = cmax;
-        u.fused_early = 0;
-        u.fused_combine_w = 1;
-        u.q_host = nullptr;
-        u.prefix_b = np;
-        std::memcpy(u.prompt_len, prefix_lens, sizeof(int) * np);
-        int n = 0;
-        auto issue = [&]() {
-            u.n_units = n;
-            n = 0;
-            return mlkv::launch_shared(c->d, true, &tmap_q, tmap_kv, tmap_kv, u, stream);
-        };
-        for (int x = 0; x < np; ++x) {
-            const int nblk = (u.group_n[x] + 2 * L1 - 1) / (2 * L1);
-            for (int j = 0; j < c->g && n_kt[x] > 0; ++j)
-                for (int ch = 0; ch * kc < n_kt[x]; ++ch)
-                    for (int blk = 0; blk < nblk; ++blk) {   // neighbours read the same tiles
-                        u.units[n] = static_cast<uint32_t>(x) | (static_cast<uint32_t>(ch) << 10) |
-                                     (static_cast<uint32_t>(blk) << 18) | (static_cast<uint32_t>(j) << 24);
-                        if (++n == mlkv::kPrefixMaxUnits) {
-                            const cudaError_t e = issue();
-                            if (e != cudaSuccess)
-                                return fail_cuda(e, "shared prefix launch");
-                        }
+        const int nblk = (u.group_n[x] + 2 * L1 - 1) / (2 * L1);
+        for (int j = 0; j < c->g && n_kt[x] > 0; ++j)
+            for (int ch = 0; ch * kc < n_kt[x]; ++ch)
+                for (int blk = 0; blk < nblk; ++blk) {   // neighbours read the same tiles
+                    u.units[n] = static_cast<uint32_t>(x) | (static_cast<uint32_t>(ch) << 10) |
+                                 (static_cast<uint32_t>(blk) << 18) | (static_cast<uint32_t>(j) << 24);
+                    if (++n == mlkv::kPrefixMaxUnits) {
+                        const cudaError_t e = issue();
+                        if (e != cudaSuccess)
+                            return fail_cuda(e, "shared prefix launch");
                     }
-        }
-        if (n > 0) {
-            const cudaError_t e = issue();
-            if (e != cudaSuccess)
-                return fail_cuda(e, "shared prefix launch");
-        }
-        for (int beta = 0; beta < c->b; ++beta) {
-            const int x = of(beta);
-            p.pre_n[beta] = static_cast<uint16_t>(x < 0 ? 0 : (n_kt[x] + kc - 1) / kc);
-        }
-    } else {
-        std::fill(p.pre_n, p.pre_n + c->b, static_cast<uint16_t>(0));
+                }
     }
-    const Cut split = cut(c, p, true, p.defer != 0, cmax, [&](int beta) {
-        return static_cast<int>((static_cast<unsigned>(seq_lens[beta]) + 63) / 64);
-    });
-    return decode_pieces(c, mlkv::kPieceSuffix, p, split, stream);
+    if (n > 0) {
+        const cudaError_t e = issue();
+        if (e != cudaSuccess)
+            return fail_cuda(e, "shared prefix launch");
+    }
+    for (int beta = 0; beta < c->b; ++beta) {
+        const int x = of(beta);
+        p.pre_n[beta] = static_cast<uint16_t>(x < 0 ? 0 : (n_kt[x] + kc - 1) / kc);
+    }
+    const auto own = [&](int beta) { return mlkv::piece_tiles<mlkv::kPieceSuffix>(p, beta); };
+    const Cut split = plan_cut(c, true, plan.beside, cmax, -1, own);
+    lay_pieces(c, p, split, own);
+    return decode_pieces(c, mlkv::kPieceSuffix, p, split, rows64(c), stream);
 }
 
 int mlkv_block_bounds(mlkv_cache_t c, int layer, const int *first, const int *seq_lens, void *bounds,
@@ -546,8 +570,10 @@ int mlkv_decode_attention_blocks(mlkv_cache_t c, int layer, const void *Q, void 
     fill_pieces(c, layer, Q, out, seq_lens, p);
     p.blocks = blocks;
     p.n_blocks = n_blocks;
-    const Cut split = cut(c, p, true, false, 0, [&](int) { return n_blocks; });
-    return decode_pieces(c, mlkv::kPieceBlocks, p, split, static_cast<cudaStream_t>(cuda_stream));
+    const auto tiles = [&](int) { return n_blocks; };
+    const Cut split = plan_cut(c, true, false, 0, -1, tiles);
+    lay_pieces(c, p, split, tiles);
+    return decode_pieces(c, mlkv::kPieceBlocks, p, split, rows64(c), static_cast<cudaStream_t>(cuda_stream));
 }
 
 int mlkv_decode_attention_weights(mlkv_cache_t c, int layer, const void *Q, void *out, const int *seq_lens,
@@ -577,9 +603,9 @@ int mlkv_decode_attention_weights(mlkv_cache_t c, int layer, const void *Q, void
     if ((rc = scratch(c, static_cast<size_t>(c->b) * c->h * p.score_stride, "scores", stream)) != MLKV_OK)
         return rc;
     p.scores = c->fused_part;
-    const Cut split = cut(c, p, true, true, 0, [&](int beta) {
-        return static_cast<int>((static_cast<unsigned>(seq_lens[beta]) + 63) / 64);
-    });
+    const auto tiles = [&](int beta) { return mlkv::piece_tiles<mlkv::kPieceWeights>(p, beta); };
+    const Cut split = plan_cut(c, true, true, 0, -1, tiles);
+    lay_pieces(c, p, split, tiles);
     mlkv::WeightsParams w;
     w.weights_in = weights_in;
     w.weights_out = weights_out;
@@ -592,7 +618,7 @@ int mlkv_decode_attention_weights(mlkv_cache_t c, int layer, const void *Q, void
     while (((upto + w.chunk - 1) / w.chunk + w.merge_ctas) * segments > 0x7fffffffLL)
         w.chunk *= 2;
     w.ctas = static_cast<int>((upto + w.chunk - 1) / w.chunk) + w.merge_ctas;
-    cudaError_t e = mlkv::launch_pieces(c->d, mlkv::kPieceWeights, rows64(c), p, stream);
+    cudaError_t e = mlkv::launch_pieces(c->d, mlkv::kPieceWeights, rows64(c), rows64(c), p, stream);
     if (e != cudaSuccess)
         return fail_cuda(e, "decode launch");
     e = mlkv::launch_weights(c->d, p, w, split.records, stream);

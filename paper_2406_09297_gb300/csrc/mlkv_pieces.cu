@@ -1,6 +1,7 @@
 // Decode attention over pieces of a cache for GB300: the common core of three calls.
 //
 //   suffix    a sequence's own positions, merged with the records of a prefix that other sequences share
+//   joined    a prefix's positions and then the sequence's own, end to end
 //   blocks    the blocks of 64 positions listed for every (sequence, KV head)
 //   weights   all positions, every score stored on the way (weights_kernel turns them into weights)
 //
@@ -70,7 +71,7 @@ __device__ __forceinline__ Piece piece_of(const PieceParams &p)
     }
     x.beta = lo;
     x.L = p.seq_len[lo];
-    const int nt = kMode == kPieceBlocks ? p.n_blocks : (x.L + T - 1) / T;
+    const int nt = piece_tiles<kMode>(p, lo);
     x.count = (nt + p.tiles - 1) / p.tiles;
     const int rel = c - p.first[lo];
     x.j = rel / x.count;
@@ -147,7 +148,8 @@ __device__ void merge_records(const PieceParams &p, const Piece &x, size_t own0,
 // NH: groups of eight query heads, 1 or 2.
 template <int D, int kMode, int NH>
 __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
-    piece_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ PieceParams p)
+    piece_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap tmap_prefix,
+                 const __grid_constant__ PieceParams p)
 {
     using PL = PiecePlan<D>;
     constexpr int S = PL::kStages, kWarps = PL::kWarps;
@@ -173,11 +175,13 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     grid_dependents_launch();
     const Piece x = piece_of<kMode>(p);
     const int *list = kMode == kPieceBlocks ? p.blocks + static_cast<size_t>(x.seg) * p.n_blocks : nullptr;
+    // (kPieceJoined: the prefix's tiles come first, then the sequence's own)
+    const int pre_len = kMode == kPieceJoined ? p.pre_len[x.beta] : 0, n_joined = (pre_len + T - 1) / T;
     // Block of tile t, or -1: none (kPieceBlocks); 32 of a list at a time, a lane each.
     int listed = -1, listed_at = -1;
     auto block_of = [&](int t) {
         if (kMode != kPieceBlocks)
-            return t;
+            return kMode == kPieceJoined && t >= n_joined ? t - n_joined : t;
         const int at = t & ~31;
         if (at != listed_at) {
             listed = at + lane < x.t1 ? list[at + lane] : -1;
@@ -192,6 +196,9 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
         asm volatile("bar.arrive 2, %0;" ::"n"(PL::kThreads) : "memory");
         // ------------------------------------ producer ------------------------------------------
         const int zk = ((p.slot * 2 + 0) * p.b + x.beta) * p.g + x.j, zv = zk + p.b * p.g;
+        const int zk_pre = kMode == kPieceJoined
+                               ? (p.slot * 2 * p.prefix_b + static_cast<int>(p.pre_place[x.beta])) * p.g + x.j
+                               : 0;
         int idx = 0;
         for (int t = x.t0; t < x.t1; ++t) {
             const int blk = block_of(t);
@@ -208,12 +215,15 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
                 if (ok) {
                     const uint32_t fb = bar_full + 8 * s, dst = sbase + s * 2 * PL::kTile;
                     mbar_arrive_expect_tx(fb, 2 * PL::kTile);
+                    const bool pre = kMode == kPieceJoined && t < n_joined;
+                    const CUtensorMap *map = pre ? &tmap_prefix : &tmap;
 #pragma unroll
                     for (int sub = 0; sub < D / 64; ++sub)
-                        tma_load_3d(dst + sub * T * 128, &tmap, fb, sub * 64, blk * T, zk);
+                        tma_load_3d(dst + sub * T * 128, map, fb, sub * 64, blk * T, pre ? zk_pre : zk);
 #pragma unroll
                     for (int sub = 0; sub < D / 64; ++sub)
-                        tma_load_3d(dst + PL::kTile + sub * T * 128, &tmap, fb, sub * 64, blk * T, zv);
+                        tma_load_3d(dst + PL::kTile + sub * T * 128, map, fb, sub * 64, blk * T,
+                                    pre ? zk_pre + p.prefix_b * p.g : zv);
                 }
             }
             if (!__shfl_sync(0xffffffffu, ok, 0))
@@ -303,7 +313,8 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
                 for (int nh = 0; nh < NH; ++nh)
                     mma_bf16_16816(sc[n][nh], a, qf[kk][nh][0], qf[kk][nh][1]);
             }
-        const int lim = x.L - blk * T - half;   // visible of the warp's keys; kKeys or more: all
+        // visible of the warp's keys; kKeys or more: all
+        const int lim = (kMode == kPieceJoined && t < n_joined ? pre_len : x.L) - blk * T - half;
 #pragma unroll
         for (int n = 0; n < M; ++n)
 #pragma unroll
@@ -606,8 +617,7 @@ __device__ __forceinline__ Piece segment_of(const PieceParams &p, int seg)
     x.beta = seg / p.g;
     x.j = seg - x.beta * p.g;
     x.L = p.seq_len[x.beta];
-    const int nt = kMode == kPieceBlocks ? p.n_blocks : (x.L + T - 1) / T;
-    x.count = (nt + p.tiles - 1) / p.tiles;
+    x.count = (piece_tiles<kMode>(p, x.beta) + p.tiles - 1) / p.tiles;
     return x;
 }
 
@@ -721,6 +731,7 @@ const void *piece_fn(int mode)
 {
     return mode == kPieceSuffix   ? reinterpret_cast<const void *>(&piece_kernel<D, kPieceSuffix, NH>)
            : mode == kPieceBlocks ? reinterpret_cast<const void *>(&piece_kernel<D, kPieceBlocks, NH>)
+           : mode == kPieceJoined ? reinterpret_cast<const void *>(&piece_kernel<D, kPieceJoined, NH>)
                                   : reinterpret_cast<const void *>(&piece_kernel<D, kPieceWeights, NH>);
 }
 const void *piece_fn(int head_dim, int G, int mode)
@@ -769,10 +780,11 @@ cudaError_t prepare_pieces(int head_dim, int G, int mode, int *ctas_per_sm)
     return e;
 }
 
-cudaError_t launch_pieces(int head_dim, int mode, const CUtensorMap *tmap, const PieceParams &p,
-                          cudaStream_t stream)
+cudaError_t launch_pieces(int head_dim, int mode, const CUtensorMap *tmap, const CUtensorMap *tmap_prefix,
+                          const PieceParams &p, cudaStream_t stream)
 {
-    void *args[] = {const_cast<CUtensorMap *>(tmap), const_cast<PieceParams *>(&p)};
+    void *args[] = {const_cast<CUtensorMap *>(tmap), const_cast<CUtensorMap *>(tmap_prefix),
+                    const_cast<PieceParams *>(&p)};
     return launch_pdl(piece_fn(head_dim, p.G, mode), dim3(static_cast<unsigned>(p.first[p.b])), piece_threads(head_dim),
                       piece_smem(head_dim), stream, args);
 }
@@ -790,14 +802,18 @@ const void *merge_fn(bool wide)
     return wide ? reinterpret_cast<const void *>(&merge_kernel<D, kMode, true>)
                 : reinterpret_cast<const void *>(&merge_kernel<D, kMode, false>);
 }
+template <int D>
+const void *merge_fn(int mode, bool wide)
+{
+    return mode == kPieceBlocks   ? merge_fn<D, kPieceBlocks>(wide)
+           : mode == kPieceJoined ? merge_fn<D, kPieceJoined>(wide)
+                                  : merge_fn<D, kPieceSuffix>(wide);
+}
 
 cudaError_t launch_merge_pieces(int head_dim, int mode, const PieceParams &p, int most, cudaStream_t stream)
 {
     const bool wide = most > kWideRecords;
-    const void *fn = head_dim == 64 ? mode == kPieceBlocks ? merge_fn<64, kPieceBlocks>(wide)
-                                                           : merge_fn<64, kPieceSuffix>(wide)
-                     : mode == kPieceBlocks ? merge_fn<128, kPieceBlocks>(wide)
-                                            : merge_fn<128, kPieceSuffix>(wide);
+    const void *fn = head_dim == 64 ? merge_fn<64>(mode, wide) : merge_fn<128>(mode, wide);
     void *args[] = {const_cast<PieceParams *>(&p)};
     const unsigned ctas = wide ? static_cast<unsigned>((p.G * head_dim + 127) / 128) : 1u;
     return launch_pdl(fn, dim3(ctas * static_cast<unsigned>(p.b) * p.g), wide ? kMergeThreads : 128,
