@@ -108,4 +108,17 @@ int check_same_model(const mlkv_cache *c, const mlkv_cache *other, const char *w
 // The checks of a shared prefix's cache, of each sequence's prefix in it (-1: none) and of their lengths.
 int check_prefix(const mlkv_cache *c, const mlkv_cache *prefix, const int *prefix_of, const int *prefix_lens);
 
+// Query rows of a decode over shared prefixes: row i attends to prefix[i]'s positions (-1: none) and then to the
+// first len[i] of its sequence.  scattered: it is row q_row[i] of Q and out, of sequence seq[i]; else n is the
+// cache's batch and every row its sequence's.
+struct PrefixRows {
+    int n, scattered, q_rows;   // q_rows: rows of Q
+    uint16_t q_row[MLKV_MAX_BATCH], seq[MLKV_MAX_BATCH];
+    int len[MLKV_MAX_BATCH], prefix[MLKV_MAX_BATCH];
+};
+// Issues the decode, with everything checked; or, with fits, only tells whether it is estimated to take less than
+// most_us.
+int decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const int *prefix_lens, const PrefixRows &rows,
+                const void *Q, void *out, cudaStream_t stream, double most_us = 0, bool *fits = nullptr);
+
 }  // namespace mlkv

@@ -1904,6 +1904,65 @@ int mlkv::check_window(int window, int sinks)
 
 extern "C" {
 
+// A few short prompts behind prefixes: every token a query row of its own of the decode over shared prefixes,
+// whose rows fill the tiles that a prompt's positions would leave empty, where that is estimated to take less than
+// the prefill kernel: us 6, and 1.25 (head_dim 64, two CTAs an SM) or 1.65 a unit's key tile and two more.  66 prompts
+// of one token behind 8086 positions, 12 heads of 64: 227 us by the prefill kernel.
+static int prefill_as_rows(mlkv_cache_t c, int layer, mlkv_cache_t prefix, const int *prefix_of,
+                           const int *prefix_lens, const int *pre_len, const void *Q, const void *K,
+                           const void *V, void *out, const int *prompt_lens, int s_max, cudaStream_t stream,
+                           bool *issued)
+{
+    long long tokens = 0, units = 0, tiles = 0;
+    for (int beta = 0; beta < c->b; ++beta) {
+        const long long blocks = (prompt_lens[beta] + 127) / 128;
+        tokens += prompt_lens[beta];
+        units += blocks;
+        tiles += blocks * ((pre_len[beta] + 127) / 128) + blocks * (blocks + 1) / 2;
+    }
+    if (tokens > MLKV_MAX_BATCH || static_cast<long long>(c->b) * s_max > 65535 || c->g > 255)
+        return MLKV_OK;
+    const bool small = c->d == 64;
+    const double prefill_us = 6 + (small ? 1.25 : 1.65) * (tiles + 2 * units) * (small ? c->h : (c->h + 1) / 2) /
+                                      ((small ? 2.0 : 1.0) * c->sm_count);
+    // What the rows take at the least, by either of their forms: the exact plan walks over all of them.
+    static thread_local int of_prefix[MLKV_MAX_BATCH];
+    std::fill(of_prefix, of_prefix + prefix->b, 0);
+    double apart = 0, joined = 0;
+    for (int beta = 0; beta < c->b; ++beta) {
+        joined += prompt_lens[beta] * ((pre_len[beta] + 63) / 64 + 1.0);
+        if (prefix_of[beta] >= 0)
+            of_prefix[prefix_of[beta]] += prompt_lens[beta];
+    }
+    const int per_unit = 2 * (128 / c->G);
+    for (int x = 0; x < prefix->b; ++x)
+        apart += (of_prefix[x] + per_unit - 1) / per_unit * ((prefix_lens[x] + 127) / 128);
+    apart = 15 + (small ? 0.95 : 1.5) * (8 + apart * c->g / c->sm_count);
+    joined = 4.5 + joined * c->g * 256.0 * c->d / 10e6;
+    if (std::min(apart, joined) >= prefill_us - 2)
+        return MLKV_OK;
+    static thread_local mlkv::PrefixRows rows;
+    rows.n = 0;
+    rows.scattered = 1;
+    rows.q_rows = c->b * s_max;
+    for (int beta = 0; beta < c->b; ++beta)
+        for (int t = 0; t < prompt_lens[beta]; ++t) {
+            rows.q_row[rows.n] = static_cast<uint16_t>(beta * s_max + t);
+            rows.seq[rows.n] = static_cast<uint16_t>(beta);
+            rows.len[rows.n] = t + 1;
+            rows.prefix[rows.n++] = prefix_of[beta];
+        }
+    bool fits;
+    int rc = mlkv::decode_rows(c, layer, prefix, prefix_lens, rows, Q, out, stream, prefill_us - 2, &fits);
+    if (rc != MLKV_OK || !fits)
+        return rc;
+    if (c->owner[layer] == layer &&   // the rows read the slot
+        (rc = store_prefix(c, layer, K, V, s_max, stream, on_device(c, K) && on_device(c, V), false)) != MLKV_OK)
+        return rc;
+    *issued = true;
+    return mlkv::decode_rows(c, layer, prefix, prefix_lens, rows, Q, out, stream);
+}
+
 static int prefill_impl(mlkv_cache_t c, int layer, const void *Q, const void *K, const void *V,
                         void *out, const int *prompt_lens, int s_max, int window, int sinks,
                         void *cuda_stream, mlkv_cache_t prefix = nullptr,
@@ -1923,6 +1982,21 @@ static int prefill_impl(mlkv_cache_t c, int layer, const void *Q, const void *K,
         return fail(MLKV_ERR_INVALID_ARG, "K and V must be non-NULL and 16-byte aligned");
     DeviceGuard guard(c->device);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    // (prompts of which none has anything in front are the plain prefill's)
+    static thread_local int pre_len[MLKV_MAX_BATCH];
+    bool shared = false;
+    if (prefix != nullptr) {
+        for (int beta = 0; beta < c->b; ++beta) {
+            pre_len[beta] = prefix_of[beta] >= 0 ? prefix_lens[prefix_of[beta]] : 0;
+            shared = shared || pre_len[beta] > 0;
+        }
+    }
+    if (shared) {
+        bool issued = false;
+        if ((rc = prefill_as_rows(c, layer, prefix, prefix_of, prefix_lens, pre_len, Q, K, V, out, prompt_lens,
+                                  s_max, stream, &issued)) != MLKV_OK || issued)
+            return rc;
+    }
     // An owner layer reads the prompt's K/V in place and stores them afterwards, unless they lie in
     // memory kernels may not read, the outputs would overwrite them or the store's target is one of
     // the inputs: then it stores them first.
@@ -1939,15 +2013,6 @@ static int prefill_impl(mlkv_cache_t c, int layer, const void *Q, const void *K,
         if (!direct) {
             if ((rc = store_prefix(c, layer, K, V, s_max, stream, local, false)) != MLKV_OK)
                 return rc;
-        }
-    }
-    // (prompts of which none has anything in front are the plain prefill's)
-    static thread_local int pre_len[MLKV_MAX_BATCH];
-    bool shared = false;
-    if (prefix != nullptr) {
-        for (int beta = 0; beta < c->b; ++beta) {
-            pre_len[beta] = prefix_of[beta] >= 0 ? prefix_lens[prefix_of[beta]] : 0;
-            shared = shared || pre_len[beta] > 0;
         }
     }
     const int ready = shared ? 4 : window > 0 ? 2 : 1;   // the three kernels' bits

@@ -33,7 +33,10 @@ struct PieceParams {
     unsigned *counters;       // [b*g]           pieces finished per segment; zero between launches
     int *err;
     float scale_log2;         // log2(e) / sqrt(D)
-    int b, h, g, G, slot;
+    int b, h, g, G, slot;     // b: sequences of the cache
+    // The query rows: decode has one a sequence, in their order; a prompt's tokens are rows of their own
+    // (scattered: row i is row q_row[i] of Q and out, of sequence seq[i]).
+    int n, scattered;
     int tiles;                // of a piece
     // kPieceSuffix: records of the shared prefix, [place][g][pre_chunks][G][D] and [place][g][pre_chunks][G]
     // with place = pre_place[beta] (below); 0 chunks: none
@@ -50,9 +53,10 @@ struct PieceParams {
     // kPieceWeights: scores times log2(e) / sqrt(D), [b][h][score_stride]
     float *scores;
     long long score_stride;
-    int seq_len[MLKV_MAX_BATCH];
-    int first[MLKV_MAX_BATCH + 1];        // first piece of sequence beta (KV head after KV head inside)
-    uint16_t pre_place[MLKV_MAX_BATCH];   // kPieceSuffix: place of the sequence in the prefix's records;
+    int seq_len[MLKV_MAX_BATCH];          // (this and what follows by row) positions that the row sees
+    int first[MLKV_MAX_BATCH + 1];        // its first piece (KV head after KV head inside)
+    uint16_t q_row[MLKV_MAX_BATCH], seq[MLKV_MAX_BATCH];
+    uint16_t pre_place[MLKV_MAX_BATCH];   // kPieceSuffix: its place in the prefix's records;
                                           // kPieceJoined: its prefix's number
     union {
         uint16_t pre_n[MLKV_MAX_BATCH];   // kPieceSuffix: those records' number

@@ -59,20 +59,28 @@ int prepare_pieces(mlkv_cache *c, int mode)
 // launch takes 4.5, and what is longer of its bytes at the rate of HBM and its longest piece; pieces beyond one wave
 // of resident CTAs half a piece more where segments are split (whole ones end evenly enough).  Split segments
 // are merged by the CTA that ends last, a round trip to L2 for every 8 records, or by a launch of their own
-// (`may_defer`; weights: always).  Never more pieces than there are records, nor of a segment than `most`.
-// `pre`: records that every merge has besides.  hbm_tiles: tiles that come from HBM, the others from L2 (10 TB/s); -1: all.
+// of their own.  Never more pieces than there are records.  pre: records that every merge has besides; hbm_tiles:
+// tiles that come from HBM, the others from L2 (10 TB/s); -1: all.
 struct Cut {
     bool defer;
     int records;   // of a segment, at most
     int tiles;     // of a piece
     double us;     // estimated
 };
+struct CutRules {
+    int n;                   // query rows
+    long long most_pieces;   // records that there is room for
+    bool always_apart;       // a merge of its own in any case
+    bool never_here;         // no merge by the CTA that ends last
+    int pre;
+    double hbm_tiles;
+};
 template <typename Tiles>
-Cut plan_cut(const mlkv_cache *c, bool may_defer, bool must_defer, int pre, double hbm_tiles, const Tiles &nt)
+Cut plan_cut(const mlkv_cache *c, const CutRules &r, const Tiles &nt)
 {
     long long total = 0;
     int longest = 1, shortest = 0x7fffffff;
-    for (int beta = 0; beta < c->b; ++beta) {
+    for (int beta = 0; beta < r.n; ++beta) {
         const int n = nt(beta);
         total += n;
         longest = std::max(longest, n);
@@ -83,34 +91,37 @@ Cut plan_cut(const mlkv_cache *c, bool may_defer, bool must_defer, int pre, doub
     const int stages = mlkv::piece_stages(c->d);
     // us: a tile of a CTA alone on its SM; all tiles at the rate of HBM; a record's part of an inline merge
     const double tile = c->d == 64 ? 0.33 : c->G <= 8 ? 0.45 : 0.72;
-    const double from_hbm = hbm_tiles < 0 ? total : hbm_tiles;
+    const double from_hbm = r.hbm_tiles < 0 ? total : r.hbm_tiles;
     const double bytes = std::max(from_hbm / 6.7e6, total / 10e6) * 256.0 * c->d, record = 0.1 * c->G * c->d / 512;
-    const int inline_most = mlkv::piece_max_records(c->d, c->G) - pre;
-    Cut best = {must_defer, 1, longest, 1e30};
-    for (int want = 1, tiles = longest;; want += (want + 7) / 8) {   // pieces of the longest segment
+    const int inline_most = mlkv::piece_max_records(c->d, c->G) - r.pre;
+    Cut best = {r.always_apart, 1, longest, 1e30};
+    for (int want = 1, tiles = longest;; want += (want + 3) / 4) {   // pieces of the longest segment
         const int next = (longest + want - 1) / want;
         if (want > 1 && next == tiles)
             continue;
         tiles = next;
         long long n = 0;
         if (shortest == longest)
-            n = static_cast<long long>(c->b) * ((longest + tiles - 1) / tiles);
+            n = static_cast<long long>(r.n) * ((longest + tiles - 1) / tiles);
         else
-            for (int beta = 0; beta < c->b; ++beta)
+            for (int beta = 0; beta < r.n; ++beta)
                 n += (nt(beta) + tiles - 1) / tiles;
         n *= c->g;
-        const int pieces = (longest + tiles - 1) / tiles, records = pieces + pre;
-        if (want > 1 && (n > std::min(c->records, 4 * slots) || records > mlkv::kDeferMaxRecords))
+        const int pieces = (longest + tiles - 1) / tiles, records = pieces + r.pre;
+        if (want > 1 && (n > std::min(r.most_pieces, 4 * slots) || records > mlkv::kDeferMaxRecords))
             break;
         const double rounds = (tiles + stages - 1) / stages;   // (a short piece's tiles come at once)
         double t = 4.5 + std::max(bytes, 1.15 * std::max(tiles * tile, rounds * 1.2));
         if (n > slots && pieces > 1)
             t += 0.5 * tiles * tile + 2.0;
         const double here = records <= 1 ? 0.0 : 2.5 + record * records, apart = 4.5;
-        const bool defer = must_defer || (may_defer && (here > apart || records > inline_most) && records > 1);
+        const bool defer = r.always_apart ||
+                           (records > 1 && (r.never_here || here > apart || records > inline_most));
         t += defer ? apart : here;
-        if (t < best.us && (defer || records <= inline_most || pieces == 1))
+        if (t < best.us)
             best = {defer, records, tiles, t};
+        if (best.us <= 4.5 + bytes + 2.5)   // no split takes less
+            break;
         if (tiles == 1)
             break;
     }
@@ -123,11 +134,11 @@ void lay_pieces(const mlkv_cache *c, mlkv::PieceParams &p, const Cut &split, con
 {
     p.tiles = split.tiles;
     long long at = 0;
-    for (int beta = 0; beta < c->b; ++beta) {
+    for (int beta = 0; beta < p.n; ++beta) {
         p.first[beta] = static_cast<int>(at);
         at += static_cast<long long>(c->g) * ((nt(beta) + p.tiles - 1) / p.tiles);
     }
-    p.first[c->b] = static_cast<int>(at);
+    p.first[p.n] = static_cast<int>(at);
 }
 
 void fill_pieces(const mlkv_cache *c, int layer, const void *Q, void *out, const int *seq_lens,
@@ -140,7 +151,8 @@ void fill_pieces(const mlkv_cache *c, int layer, const void *Q, void *out, const
     p.counters = c->counters;
     p.err = c->err;
     p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(c->d)));
-    p.b = c->b;
+    p.b = p.n = c->b;
+    p.scattered = 0;
     p.h = c->h;
     p.g = c->g;
     p.G = c->G;
@@ -178,6 +190,19 @@ int decode_pieces(const mlkv_cache *c, int mode, mlkv::PieceParams &p, const Cut
         return fail_cuda(e, "decode launch");
     if (p.defer && (e = mlkv::launch_merge_pieces(c->d, mode, p, split.records, stream)) != cudaSuccess)
         return fail_cuda(e, "merge launch");
+    return MLKV_OK;
+}
+
+// Scattered rows' records, behind `before` floats of the scratch (rounded up to 16 bytes).
+int own_records(mlkv_cache *c, mlkv::PieceParams &p, size_t before, cudaStream_t stream)
+{
+    before = (before + 3) / 4 * 4;
+    const size_t rows = static_cast<size_t>(p.first[p.n]) * c->G;
+    const int rc = scratch(c, before + rows * (c->d + 1), "records of a prompt's tokens", stream);
+    if (rc != MLKV_OK)
+        return rc;
+    p.part_o = c->fused_part + before;
+    p.part_lse = p.part_o + rows * c->d;
     return MLKV_OK;
 }
 
@@ -259,54 +284,56 @@ int mlkv::check_prefix(const mlkv_cache *c, const mlkv_cache *prefix, const int 
     return MLKV_OK;
 }
 
-extern "C" {
-
-int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix, const int *prefix_of,
-                                 const int *prefix_lens, const void *Q, void *out, const int *seq_lens,
-                                 void *cuda_stream)
+int mlkv::decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const int *prefix_lens,
+                      const PrefixRows &rows, const void *Q, void *out, cudaStream_t stream, double most_us,
+                      bool *fits)
 {
-    int rc = check_layer(c, layer);
-    if (rc != MLKV_OK || (rc = mlkv::check_prefix(c, prefix, prefix_of, prefix_lens)) != MLKV_OK ||
-        (rc = check_queries(c, Q, out)) != MLKV_OK || (rc = check_seq_lens(c, seq_lens)) != MLKV_OK)
-        return rc;
-    if (c->g > 255)
-        return fail(MLKV_ERR_UNSUPPORTED, "the decode over a shared prefix handles at most 255 KV heads");
-    DeviceGuard guard(c->device);
-    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if ((rc = prepare_pieces(c, mlkv::kPieceSuffix)) != MLKV_OK)
+    int rc = ::prepare_pieces(c, mlkv::kPieceSuffix);
+    if (rc != MLKV_OK)
         return rc;
     static thread_local mlkv::PieceParams p;
     static thread_local mlkv::SharedPrefillParams u;
     static thread_local bool read[MLKV_MAX_BATCH];
-    fill_pieces(c, layer, Q, out, seq_lens, p);
+    fill_pieces(c, layer, Q, out, rows.len, p);   // (scattered rows are no fewer than sequences)
+    p.n = rows.n;
+    p.scattered = rows.scattered;
+    if (rows.scattered) {
+        std::memcpy(p.seq_len, rows.len, sizeof(int) * rows.n);
+        std::memcpy(p.q_row, rows.q_row, sizeof(uint16_t) * rows.n);
+        std::memcpy(p.seq, rows.seq, sizeof(uint16_t) * rows.n);
+    }
     // Each sequence's prefix and positions end to end, if that is no longer than the prefixes apart: few sequences a
     // prefix.
     double hbm = 0, bytes = 0;   // tiles of 64 positions that are read once; bytes of the suffixes
     for (int x = 0; x < prefix->b; ++x)
         read[x] = false;
-    for (int beta = 0; beta < c->b; ++beta) {
-        const int x = prefix_of[beta];
+    for (int beta = 0; beta < rows.n; ++beta) {
+        const int x = rows.prefix[beta];
         p.pre_len[beta] = x >= 0 ? prefix_lens[x] : 0;
         p.pre_place[beta] = static_cast<uint16_t>(x >= 0 ? x : 0);
-        hbm += (seq_lens[beta] + 63) / 64;
-        bytes += 4.0 * c->g * c->d * seq_lens[beta];
+        hbm += (rows.len[beta] + 63) / 64;
+        bytes += 4.0 * c->g * c->d * rows.len[beta];
         if (x >= 0 && !read[x]) {
             read[x] = true;
             hbm += (prefix_lens[x] + 63) / 64;
         }
     }
     const auto joined = [&](int beta) { return mlkv::piece_tiles<mlkv::kPieceJoined>(p, beta); };
-    const Cut end_to_end = plan_cut(c, true, false, 0, hbm * c->g, joined);
+    // (scattered rows have no counters, and their records in the scratch)
+    const long long room = rows.scattered ? 0x7fffffff : c->records;
+    const Cut end_to_end = plan_cut(c, {rows.n, room, false, rows.scattered != 0, 0, hbm * c->g}, joined);
     // Places: the sequences of prefix 0, then those of prefix 1, ...  Where every prefix's sequences are
     // neighbours already, a sequence's place is its own number.
     const int L1 = 128 / c->G, np = prefix->b;
     static thread_local int n_kt[MLKV_MAX_BATCH], pairs[MLKV_MAX_BATCH];
     static thread_local PrefixPlan plan;
     std::fill(u.group_n, u.group_n + np, static_cast<uint16_t>(0));
-    auto of = [&](int beta) { return prefix_of[beta] >= 0 && prefix_lens[prefix_of[beta]] > 0 ? prefix_of[beta] : -1; };
-    bool neighbours = true;
+    auto of = [&](int beta) {
+        return rows.prefix[beta] >= 0 && prefix_lens[rows.prefix[beta]] > 0 ? rows.prefix[beta] : -1;
+    };
+    bool neighbours = rows.scattered == 0;
     int places = 0;
-    for (int beta = 0; beta < c->b; ++beta) {
+    for (int beta = 0; beta < rows.n; ++beta) {
         const int x = of(beta);
         if (x < 0)
             continue;
@@ -325,17 +352,24 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
     }
     if (most_kt > 0)
         plan = plan_prefix(n_kt, pairs, np, c->sm_count, c->d, bytes);
-    if (most_kt == 0 || end_to_end.us <= plan.us) {
-        if ((rc = prepare_pieces(c, mlkv::kPieceJoined)) != MLKV_OK)
+    const bool apart = most_kt > 0 && plan.us < end_to_end.us;
+    if (fits != nullptr) {
+        *fits = (apart ? plan.us : end_to_end.us) < most_us;
+        return MLKV_OK;
+    }
+    if (!apart) {
+        if ((rc = ::prepare_pieces(c, mlkv::kPieceJoined)) != MLKV_OK)
             return rc;
         p.prefix_b = prefix->b;
         lay_pieces(c, p, end_to_end, joined);
+        if (rows.scattered && (rc = own_records(c, p, 0, stream)) != MLKV_OK)
+            return rc;
         return decode_pieces(c, mlkv::kPieceJoined, p, end_to_end, rows64(prefix), stream);
     }
     if (neighbours) {
-        for (int beta = 0; beta < c->b; ++beta)
+        for (int beta = 0; beta < rows.n; ++beta)
             p.pre_place[beta] = static_cast<uint16_t>(beta);
-        places = c->b;
+        places = rows.n;
     } else {
         int at = 0;
         for (int x = 0; x < np; ++x) {
@@ -343,11 +377,11 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
             at += u.group_n[x];
             u.group_n[x] = 0;
         }
-        for (int beta = 0; beta < c->b; ++beta)
+        for (int beta = 0; beta < rows.n; ++beta)
             if (of(beta) >= 0) {
                 const int place = u.group_at[of(beta)] + u.group_n[of(beta)]++;
                 p.pre_place[beta] = static_cast<uint16_t>(place);
-                u.seq[place] = static_cast<uint16_t>(beta);
+                u.seq[place] = rows.scattered ? rows.q_row[beta] : static_cast<uint16_t>(beta);
             }
     }
     if (!(c->long_ready & kReadyShared)) {
@@ -357,13 +391,20 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
         c->long_ready |= kReadyShared;
     }
     const int kc = plan.kc;
-    p.defer = plan.beside ? 1 : 0;
     const int cmax = (most_kt + kc - 1) / kc;
-    const size_t rows = static_cast<size_t>(places) * c->g * cmax * c->G;
-    if ((rc = scratch(c, rows * (c->d + 1), "records of the shared prefix", stream)) != MLKV_OK)
+    const size_t records = static_cast<size_t>(places) * c->g * cmax * c->G;
+    for (int beta = 0; beta < rows.n; ++beta) {
+        const int x = of(beta);
+        p.pre_n[beta] = static_cast<uint16_t>(x < 0 ? 0 : (n_kt[x] + kc - 1) / kc);
+    }
+    const auto own = [&](int beta) { return mlkv::piece_tiles<mlkv::kPieceSuffix>(p, beta); };
+    const Cut split = plan_cut(c, {rows.n, room, plan.beside, rows.scattered != 0, cmax, -1}, own);
+    lay_pieces(c, p, split, own);
+    if ((rc = rows.scattered ? own_records(c, p, records * (c->d + 1), stream)
+                             : scratch(c, records * (c->d + 1), "records of the shared prefix", stream)) != MLKV_OK)
         return rc;
     u.part = c->fused_part;
-    u.part_lse = u.part + rows * c->d;
+    u.part_lse = u.part + records * c->d;
     p.pre_o = u.part;
     p.pre_lse = u.part_lse;
     p.pre_chunks = cmax;
@@ -376,11 +417,11 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
     CUtensorMap tmap_q;
     const cuuint64_t row = static_cast<cuuint64_t>(c->h) * c->d * 2;
     const cuuint64_t dims[5] = {static_cast<cuuint64_t>(c->d), static_cast<cuuint64_t>(c->G),
-                                static_cast<cuuint64_t>(c->g), 1u, static_cast<cuuint64_t>(c->b)};
+                                static_cast<cuuint64_t>(c->g), 1u, static_cast<cuuint64_t>(rows.q_rows)};
     const cuuint64_t strides[4] = {static_cast<cuuint64_t>(c->d) * 2,
                                    static_cast<cuuint64_t>(c->G) * c->d * 2, row, row};
     const cuuint32_t box[5] = {64u, static_cast<cuuint32_t>(c->G), 1u, 1u,
-                               static_cast<cuuint32_t>(neighbours ? std::min(L1, c->b) : 1)};
+                               static_cast<cuuint32_t>(neighbours ? std::min(L1, rows.n) : 1)};
     const cuuint32_t estr[5] = {1u, 1u, 1u, 1u, 1u};
     const CUresult r = encode(&tmap_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(Q), dims,
                               strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -409,7 +450,7 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
     u.sm_count = plan.sms;
     u.window = u.sinks = 0;
     u.kv_direct = 0;
-    u.fused_L = c->b;
+    u.fused_L = rows.n;
     u.fused_L1 = L1;
     u.fused_nblk = 1;
     u.fused_kc = kc;
@@ -444,14 +485,29 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
         if (e != cudaSuccess)
             return fail_cuda(e, "shared prefix launch");
     }
-    for (int beta = 0; beta < c->b; ++beta) {
-        const int x = of(beta);
-        p.pre_n[beta] = static_cast<uint16_t>(x < 0 ? 0 : (n_kt[x] + kc - 1) / kc);
-    }
-    const auto own = [&](int beta) { return mlkv::piece_tiles<mlkv::kPieceSuffix>(p, beta); };
-    const Cut split = plan_cut(c, true, plan.beside, cmax, -1, own);
-    lay_pieces(c, p, split, own);
     return decode_pieces(c, mlkv::kPieceSuffix, p, split, rows64(c), stream);
+}
+
+extern "C" {
+
+int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix, const int *prefix_of,
+                                 const int *prefix_lens, const void *Q, void *out, const int *seq_lens,
+                                 void *cuda_stream)
+{
+    int rc = check_layer(c, layer);
+    if (rc != MLKV_OK || (rc = mlkv::check_prefix(c, prefix, prefix_of, prefix_lens)) != MLKV_OK ||
+        (rc = check_queries(c, Q, out)) != MLKV_OK || (rc = check_seq_lens(c, seq_lens)) != MLKV_OK)
+        return rc;
+    if (c->g > 255)
+        return fail(MLKV_ERR_UNSUPPORTED, "the decode over a shared prefix handles at most 255 KV heads");
+    static thread_local mlkv::PrefixRows rows;
+    rows.n = rows.q_rows = c->b;
+    rows.scattered = 0;
+    std::memcpy(rows.len, seq_lens, sizeof(int) * c->b);
+    std::memcpy(rows.prefix, prefix_of, sizeof(int) * c->b);
+    DeviceGuard guard(c->device);
+    return mlkv::decode_rows(c, layer, prefix, prefix_lens, rows, Q, out,
+                             static_cast<cudaStream_t>(cuda_stream));
 }
 
 int mlkv_block_bounds(mlkv_cache_t c, int layer, const int *first, const int *seq_lens, void *bounds,
@@ -571,7 +627,7 @@ int mlkv_decode_attention_blocks(mlkv_cache_t c, int layer, const void *Q, void 
     p.blocks = blocks;
     p.n_blocks = n_blocks;
     const auto tiles = [&](int) { return n_blocks; };
-    const Cut split = plan_cut(c, true, false, 0, -1, tiles);
+    const Cut split = plan_cut(c, {c->b, c->records, false, false, 0, -1}, tiles);
     lay_pieces(c, p, split, tiles);
     return decode_pieces(c, mlkv::kPieceBlocks, p, split, rows64(c), static_cast<cudaStream_t>(cuda_stream));
 }
@@ -604,7 +660,7 @@ int mlkv_decode_attention_weights(mlkv_cache_t c, int layer, const void *Q, void
         return rc;
     p.scores = c->fused_part;
     const auto tiles = [&](int beta) { return mlkv::piece_tiles<mlkv::kPieceWeights>(p, beta); };
-    const Cut split = plan_cut(c, true, true, 0, -1, tiles);
+    const Cut split = plan_cut(c, {c->b, c->records, true, false, 0, -1}, tiles);
     lay_pieces(c, p, split, tiles);
     mlkv::WeightsParams w;
     w.weights_in = weights_in;

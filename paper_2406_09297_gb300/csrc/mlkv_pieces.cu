@@ -53,15 +53,19 @@ constexpr int max_records(int G)
 __device__ __forceinline__ float neg_inf() { return -__int_as_float(0x7f800000); }
 
 struct Piece {
-    int beta, j, seg, index, count, t0, t1, L;
+    int beta, j, seg, index, count, t0, t1, L;   // beta: the query row
 };
+
+// Row of Q and out, and sequence, of a query row.
+__device__ __forceinline__ int q_row(const PieceParams &p, int i) { return p.scattered ? p.q_row[i] : i; }
+__device__ __forceinline__ int row_seq(const PieceParams &p, int i) { return p.scattered ? p.seq[i] : i; }
 
 template <int kMode>
 __device__ __forceinline__ Piece piece_of(const PieceParams &p)
 {
     Piece x;
     const int c = static_cast<int>(blockIdx.x);
-    int lo = 0, hi = p.b - 1;
+    int lo = 0, hi = p.n - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (p.first[mid] <= c)
@@ -110,7 +114,7 @@ __device__ void merge_records(const PieceParams &p, const Piece &x, size_t own0,
         s_w[n * G + tid] = tot == 0.f ? 0.f : 1.f / tot;
     }
     asm volatile("bar.sync 1, %0;" ::"r"(n_threads) : "memory");
-    __nv_bfloat16 *ob = p.out + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * G) * D;
+    __nv_bfloat16 *ob = p.out + (static_cast<size_t>(q_row(p, x.beta)) * p.h + static_cast<size_t>(x.j) * G) * D;
     for (int i = tid * 4; i < G * D; i += n_threads * 4) {
         const int row = i / D;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -195,7 +199,7 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
         __syncwarp();
         asm volatile("bar.arrive 2, %0;" ::"n"(PL::kThreads) : "memory");
         // ------------------------------------ producer ------------------------------------------
-        const int zk = ((p.slot * 2 + 0) * p.b + x.beta) * p.g + x.j, zv = zk + p.b * p.g;
+        const int zk = ((p.slot * 2 + 0) * p.b + row_seq(p, x.beta)) * p.g + x.j, zv = zk + p.b * p.g;
         const int zk_pre = kMode == kPieceJoined
                                ? (p.slot * 2 * p.prefix_b + static_cast<int>(p.pre_place[x.beta])) * p.g + x.j
                                : 0;
@@ -246,7 +250,7 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     const int half = warp % PL::kPerStage * PL::kKeys;   // the warp's first key of a tile
     uint32_t qf[D / 16][NH][2];   // columns n = lane / 4
     {
-        const __nv_bfloat16 *q = p.Q + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * p.G) * D;
+        const __nv_bfloat16 *q = p.Q + (static_cast<size_t>(q_row(p, x.beta)) * p.h + static_cast<size_t>(x.j) * p.G) * D;
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
@@ -458,7 +462,7 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     const bool defer = kMode == kPieceWeights || p.defer;
     const bool whole = !defer && x.count == 1 && n_pre == 0;
     const size_t rec = blockIdx.x;
-    __nv_bfloat16 *ob = p.out + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * p.G) * D;
+    __nv_bfloat16 *ob = p.out + (static_cast<size_t>(q_row(p, x.beta)) * p.h + static_cast<size_t>(x.j) * p.G) * D;
     for (int i = tid * 4; i < p.G * D; i += kWarps * 32 * 4) {
         const int row = i / D, ch = i - row * D;
         float mx = neg_inf();
@@ -604,7 +608,7 @@ __device__ void merge_rows(MergeShared<D> &sh, const PieceParams &p, const Piece
         uint2 w2;
         w2.x = pack_bf16x2(acc.x * inv, acc.y * inv);
         w2.y = pack_bf16x2(acc.z * inv, acc.w * inv);
-        *reinterpret_cast<uint2 *>(p.out + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * G) * D +
+        *reinterpret_cast<uint2 *>(p.out + (static_cast<size_t>(q_row(p, x.beta)) * p.h + static_cast<size_t>(x.j) * G) * D +
                                    part * 128 + lane * 4) = w2;
     }
 }
@@ -785,7 +789,7 @@ cudaError_t launch_pieces(int head_dim, int mode, const CUtensorMap *tmap, const
 {
     void *args[] = {const_cast<CUtensorMap *>(tmap), const_cast<CUtensorMap *>(tmap_prefix),
                     const_cast<PieceParams *>(&p)};
-    return launch_pdl(piece_fn(head_dim, p.G, mode), dim3(static_cast<unsigned>(p.first[p.b])), piece_threads(head_dim),
+    return launch_pdl(piece_fn(head_dim, p.G, mode), dim3(static_cast<unsigned>(p.first[p.n])), piece_threads(head_dim),
                       piece_smem(head_dim), stream, args);
 }
 
@@ -816,7 +820,7 @@ cudaError_t launch_merge_pieces(int head_dim, int mode, const PieceParams &p, in
     const void *fn = head_dim == 64 ? merge_fn<64>(mode, wide) : merge_fn<128>(mode, wide);
     void *args[] = {const_cast<PieceParams *>(&p)};
     const unsigned ctas = wide ? static_cast<unsigned>((p.G * head_dim + 127) / 128) : 1u;
-    return launch_pdl(fn, dim3(ctas * static_cast<unsigned>(p.b) * p.g), wide ? kMergeThreads : 128,
+    return launch_pdl(fn, dim3(ctas * static_cast<unsigned>(p.n) * p.g), wide ? kMergeThreads : 128,
                       merge_smem(head_dim, p.G, most), stream, args);
 }
 

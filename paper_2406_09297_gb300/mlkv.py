@@ -487,13 +487,14 @@ def mlkv_prefill_prefix(handle, layer, prefix, prefix_of, prefix_lens, Q, K, V, 
 _dtypes = {}
 
 
+def _dtype(name):
+    import torch
+    return _dtypes.setdefault(name, getattr(torch, name))
+
+
 def _dense(name, t, dtype):
     """A dense tensor's address; its type is checked."""
-    want = _dtypes.get(dtype)
-    if want is None:
-        import torch
-        want = _dtypes[dtype] = getattr(torch, dtype)
-    if t.dtype is not want or not t.is_contiguous():
+    if t.dtype is not (_dtypes.get(dtype) or _dtype(dtype)) or not t.is_contiguous():
         raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must be dense and {dtype}")
     return t.data_ptr()
 
@@ -594,78 +595,93 @@ class MLKVCache:
         return mlkv_prefill_window(self.handle, layer, Q, K, V, out, prompt_lens, int(Q.shape[1]),
                                    window, sinks, stream)
 
-    def _sized(self, name, t, *shape):
-        if t is not None and t.shape != shape:
-            raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must be of shape {list(shape)}")
+    # (A step's call: one condition over a tensor's type, shape and density, one over an array's, and the library
+    # called from here: of a call with two tensors and one array 1.5 us are Python's, 2.2 through the functions
+    # of the same names.)
 
-    def _host(self, name, a, n):
-        if not (isinstance(a, np.ndarray) and a.dtype == _INT32 and a.flags.c_contiguous):
+    def _tensor(self, name, t, dtype, shape):
+        want = _dtypes.get(dtype) or _dtype(dtype)
+        if t.dtype is not want or t.shape != shape or not t.is_contiguous():
+            raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must be dense, {dtype} and of shape {list(shape)}")
+        return t.data_ptr()
+
+    def _numbers(self, name, a, n):
+        """n int32 numbers on the host (keep them while their address is in use) and their address."""
+        if not (type(a) is np.ndarray and a.dtype is _INT32 and a.flags.c_contiguous):
             a = as_seq_lens(a)
         if a.shape != (n,):
             raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must hold {n} numbers")
-        return a
+        return _lens_ptr(a)
+
+    def _blocks(self):
+        return (self.b, self.g, (self.max_seq + MLKV_BLOCK - 1) // MLKV_BLOCK)
 
     def decode_attention_prefix(self, layer, prefix, prefix_of, prefix_lens, Q, out, seq_lens, stream=None):
         """Decode attention behind beginnings that sequences share: those of `prefix`, another MLKVCache
         (or this one), sequence prefix_of[i] (-1: none) for sequence i."""
-        return mlkv_decode_attention_prefix(
-            self.handle, layer, prefix.handle, self._host("prefix_of", prefix_of, self.b),
-            self._host("prefix_lens", prefix_lens, prefix.b), Q, out,
-            self._host("seq_lens", seq_lens, self.b), stream)
+        o, po = self._numbers("prefix_of", prefix_of, self.b)
+        n, pn = self._numbers("prefix_lens", prefix_lens, prefix.b)
+        a, p = self._numbers("seq_lens", seq_lens, self.b)
+        return _check(lib.mlkv_decode_attention_prefix(self.handle, layer, prefix.handle, po, pn, _ptr(Q),
+                                                       _ptr(out), p, _stream(stream)))
 
     def prefill_prefix(self, layer, prefix, prefix_of, prefix_lens, Q, K, V, out, prompt_lens, stream=None):
         """Causal prefill behind a shared beginning; Q / out [b][s_max][h][d], K / V [b][g][s_max][d]."""
-        return mlkv_prefill_prefix(
-            self.handle, layer, prefix.handle, self._host("prefix_of", prefix_of, self.b),
-            self._host("prefix_lens", prefix_lens, prefix.b), Q, K, V, out,
-            self._host("prompt_lens", prompt_lens, self.b), int(Q.shape[1]), stream)
+        o, po = self._numbers("prefix_of", prefix_of, self.b)
+        n, pn = self._numbers("prefix_lens", prefix_lens, prefix.b)
+        a, p = self._numbers("prompt_lens", prompt_lens, self.b)
+        return _check(lib.mlkv_prefill_prefix(self.handle, layer, prefix.handle, po, pn, _ptr(Q), _ptr(K),
+                                              _ptr(V), _ptr(out), p, int(Q.shape[1]), _stream(stream)))
 
     def block_bounds(self, layer, seq_lens, bounds, scales, first=None, stream=None):
         """Bounds int8 [b][g][n_blocks][2][d] and scales fp32 [b][g][n_blocks] of the keys of every block
         of 64 positions, from the one of position first[i] on (None: all)."""
-        n = (self.max_seq + MLKV_BLOCK - 1) // MLKV_BLOCK
-        self._sized("bounds", bounds, self.b, self.g, n, 2, self.d)
-        self._sized("scales", scales, self.b, self.g, n)
-        return mlkv_block_bounds(self.handle, layer,
-                                 None if first is None else self._host("first", first, self.b),
-                                 self._host("seq_lens", seq_lens, self.b), bounds, scales, stream)
+        f, pf = (None, None) if first is None else self._numbers("first", first, self.b)
+        a, p = self._numbers("seq_lens", seq_lens, self.b)
+        n = self._blocks()
+        return _check(lib.mlkv_block_bounds(
+            self.handle, layer, pf, p, self._tensor("bounds", bounds, "int8", n + (2, self.d)),
+            self._tensor("scales", scales, "float32", n), _stream(stream)))
 
     def select_blocks(self, layer, Q, bounds, scales, seq_lens, blocks, n_first=1, n_last=1, stream=None):
         """Writes the blocks that Q [b][h][d] needs most into blocks, int32 [b][g][n]."""
-        n = (self.max_seq + MLKV_BLOCK - 1) // MLKV_BLOCK
-        self._sized("bounds", bounds, self.b, self.g, n, 2, self.d)
-        self._sized("scales", scales, self.b, self.g, n)
-        self._sized("blocks", blocks, self.b, self.g, blocks.shape[-1])
-        return mlkv_select_blocks(self.handle, layer, Q, bounds, scales,
-                                  self._host("seq_lens", seq_lens, self.b), blocks.shape[-1], n_first, n_last,
-                                  blocks, stream)
+        a, p = self._numbers("seq_lens", seq_lens, self.b)
+        n, n_select = self._blocks(), blocks.shape[-1]
+        return _check(lib.mlkv_select_blocks(
+            self.handle, layer, _ptr(Q), self._tensor("bounds", bounds, "int8", n + (2, self.d)),
+            self._tensor("scales", scales, "float32", n), p, n_select, n_first, n_last,
+            self._tensor("blocks", blocks, "int32", (self.b, self.g, n_select)), _stream(stream)))
 
     def decode_attention_blocks(self, layer, Q, out, seq_lens, blocks, stream=None):
         """Decode attention over the listed blocks alone, int32 [b][g][n]."""
-        self._sized("blocks", blocks, self.b, self.g, blocks.shape[-1])
-        return mlkv_decode_attention_blocks(self.handle, layer, Q, out,
-                                            self._host("seq_lens", seq_lens, self.b), blocks,
-                                            blocks.shape[-1], stream)
+        a, p = self._numbers("seq_lens", seq_lens, self.b)
+        n = blocks.shape[-1]
+        return _check(lib.mlkv_decode_attention_blocks(
+            self.handle, layer, _ptr(Q), _ptr(out), p,
+            self._tensor("blocks", blocks, "int32", (self.b, self.g, n)), n, _stream(stream)))
 
     def decode_attention_weights(self, layer, Q, out, seq_lens, weights_in, weights_out, stream=None):
         """Decode attention; weights_out = weights_in (None: zeros; fp32 [b][g][max_seq]) + what every
         position was given."""
-        self._sized("weights_in", weights_in, self.b, self.g, self.max_seq)
-        self._sized("weights_out", weights_out, self.b, self.g, self.max_seq)
-        return mlkv_decode_attention_weights(self.handle, layer, Q, out,
-                                             self._host("seq_lens", seq_lens, self.b), weights_in,
-                                             weights_out, stream)
+        a, p = self._numbers("seq_lens", seq_lens, self.b)
+        n = (self.b, self.g, self.max_seq)
+        w = None if weights_in is None else self._tensor("weights_in", weights_in, "float32", n)
+        return _check(lib.mlkv_decode_attention_weights(
+            self.handle, layer, _ptr(Q), _ptr(out), p, w,
+            self._tensor("weights_out", weights_out, "float32", n), _stream(stream)))
 
     def evict(self, layer, weights_in, weights_out, seq_lens, keep, recent, kept, to=None, stream=None):
         """Keeps the `recent` newest and the heaviest other positions, keep[i] in all, in this cache or in
         `to`; kept int32 [b][g][n] receives where they lay."""
         to = self if to is None else to
-        self._sized("weights_in", weights_in, self.b, self.g, self.max_seq)
-        self._sized("weights_out", weights_out, to.b, to.g, to.max_seq)
-        self._sized("kept", kept, self.b, self.g, kept.shape[-1])
-        return mlkv_evict(self.handle, to.handle, layer, weights_in, weights_out,
-                          self._host("seq_lens", seq_lens, self.b), self._host("keep", keep, self.b), recent,
-                          kept, kept.shape[-1], stream)
+        a, p = self._numbers("seq_lens", seq_lens, self.b)
+        k, pk = self._numbers("keep", keep, self.b)
+        n = kept.shape[-1]
+        return _check(lib.mlkv_evict(
+            self.handle, to.handle, layer,
+            self._tensor("weights_in", weights_in, "float32", (self.b, self.g, self.max_seq)),
+            self._tensor("weights_out", weights_out, "float32", (to.b, to.g, to.max_seq)), p, pk, recent,
+            self._tensor("kept", kept, "int32", (self.b, self.g, n)), n, _stream(stream)))
 
     def decode_step_host(self, Q, K, V, out, seq_lens, stream=None):
         return mlkv_decode_step_host(self.handle, Q, K, V, out, seq_lens, stream)

@@ -191,6 +191,40 @@ def test_prefill(d, h, g, lens, prefix_of, prefix_lens, owner):
         assert_attention(one[i], want[:, 0], spread[:, 0], ROUNDINGS)
 
 
+@pytest.mark.parametrize("d,h,g", [(64, 12, 4), (64, 12, 1), (128, 32, 8), (128, 6, 2), (128, 16, 1)])
+@pytest.mark.parametrize("b,s,p", [(66, 1, 2000), (40, 13, 700), (3, 300, 40), (9, 100, 5000), (1000, 1, 129)])
+def test_prefill_short_prompts(d, h, g, b, s, p):
+    """Prompts whose positions leave most of a tile empty; neighbours and others, uneven."""
+    torch.manual_seed(b)
+    rng = np.random.default_rng(b + s)
+    lens = [int(x) for x in rng.integers(max(1, s // 2), s + 1, b)]
+    lens[-1] = s
+    prefix_of = [int(x) for x in rng.integers(-1, 2, b)]
+    prefix_lens = [p, max(1, p - 70)]
+    cap = s + 2
+    cache, prefix = mlkv.MLKVCache(2, h, d, [0, 0], g, b, cap), mlkv.MLKVCache(2, h, d, [0, 0], g, 2, p)
+    K, V, Q = _randn(b, g, s, d), _randn(b, g, s, d), _randn(b, s, h, d)
+    for i, n in enumerate(lens):
+        K[i, :, n:], V[i, :, n:] = math.nan, math.inf
+    PK, PV = _randn(2, g, p, d), _randn(2, g, p, d)
+    prefix.load_prefix(0, PK, PV, p)
+    out = torch.full_like(Q, 9.0)
+    cache.prefill_prefix(0, prefix, prefix_of, prefix_lens, Q, K, V, out, lens)
+    again = torch.full_like(Q, 9.0)
+    cache.prefill_prefix(1, prefix, prefix_of, prefix_lens, Q, None, None, again, lens)
+    cache.sync_status()
+    for i in sorted(set([0, b - 1] + [int(x) for x in rng.integers(0, b, 10)])):
+        m, x = lens[i], prefix_of[i]
+        n = prefix_lens[x] if x >= 0 else 0
+        k, v = _joined(i, m, x, n, K, V, PK, PV)
+        t, u = torch.arange(m, device="cuda")[:, None], torch.arange(n + m, device="cuda")[None]
+        want, spread = attend(Q[i, :m].transpose(0, 1).double(), k, v, u <= n + t)
+        assert_attention(out[i, :m].transpose(0, 1), want, spread, ROUNDINGS)
+        assert_attention(again[i, :m].transpose(0, 1), want, spread, ROUNDINGS)
+    for i, m in enumerate(lens):
+        assert (out[i, m:] == 9.0).all() and (again[i, m:] == 9.0).all()
+
+
 def test_prefill_without_anything_in_front_is_the_plain_one():
     torch.manual_seed(0)
     d, h, g, lens = 128, 8, 2, [100, 333]
