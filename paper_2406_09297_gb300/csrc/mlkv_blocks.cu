@@ -36,100 +36,127 @@ __device__ __forceinline__ float inverse_power(float s)   // of a power of two
     return __uint_as_float((254u << 23) - __float_as_uint(s));
 }
 
-constexpr int kBoundsThreads = 128;
+constexpr int kBoundsThreads = 256;
+constexpr int kBoundsBlocks = 4;   // of a CTA
 
-// A CTA is one block of one KV head: 16 bytes a load, D / 8 lanes a row, every row of the block in flight at
-// once; minima and maxima two channels at a time, across a warp's rows by shuffles, across the warps in shared
-// memory.  Bound by the keys' bytes.
+// A CTA is four blocks of one KV head, 128 threads a block, two after one another, all rows on the way at once; 16 bytes
+// a load, D / 8 lanes a row; minima and maxima two channels at a time, across a warp's rows by shuffles, across the
+// warps in shared memory.  Bound by the keys' bytes.  (A CTA a block: 130 MB of keys 24.7 us, starting CTAs is
+// what took that.)
 template <int D>
-__global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_constant__ BoundsParams p)
+__global__ void __launch_bounds__(kBoundsThreads, 3) bounds_kernel(const __grid_constant__ BoundsParams p)
 {
     constexpr int C = D / 8;                     // 16-byte columns of a row
-    constexpr int RG = kBoundsThreads / C;       // rows at a time
+    constexpr int RG = 128 / C;                  // rows at a time
     constexpr int N = kBlock / RG;               // rows of a thread
-    constexpr int W = kBoundsThreads / 32;
-    __shared__ __align__(16) __nv_bfloat16 s_lo[W][D], s_hi[W][D];
-    __shared__ float s_max[W];
-    const int tid = static_cast<int>(threadIdx.x), warp = tid >> 5, lane = tid & 31;
-    const int seg = static_cast<int>(blockIdx.x / p.ctas), beta = seg / p.g;
-    const int L = p.seq_len[beta];
-    const int blk = p.first[beta] / kBlock + static_cast<int>(blockIdx.x % p.ctas);
+    constexpr int W = 4;                         // warps of a block
+    __shared__ __align__(16) __nv_bfloat16 s_lo[2][W][D], s_hi[2][W][D];
+    __shared__ float s_max[2][W];
+    const int half = static_cast<int>(threadIdx.x) >> 7, tid = static_cast<int>(threadIdx.x) & 127;
+    const int warp = tid >> 5, lane = tid & 31;
+    // the sequence whose CTAs these are
+    int beta = 0, above = p.b - 1;
+    while (beta < above) {
+        const int mid = (beta + above + 1) >> 1;
+        if (p.start[mid] <= static_cast<int>(blockIdx.x))
+            beta = mid;
+        else
+            above = mid - 1;
+    }
+    const int L = p.seq_len[beta], blk0 = p.first[beta] / kBlock, n_blk = (L + kBlock - 1) / kBlock - blk0;
+    const int ctas = (n_blk + kBoundsBlocks - 1) / kBoundsBlocks;   // of a KV head
+    const int rel = static_cast<int>(blockIdx.x) - p.start[beta];
+    const int j = rel / ctas, at0 = blk0 + (rel - j * ctas) * kBoundsBlocks + half;
+    const int seg = beta * p.g + j;
+    const int col = tid % C, r0 = tid / C;
     grid_dependency_wait();
     grid_dependents_launch();
-    if (static_cast<long long>(blk) * kBlock >= L)
-        return;
-    const int n = min(kBlock, L - blk * kBlock);
-    const int col = tid % C, r0 = tid / C;
-    const uint4 *k = reinterpret_cast<const uint4 *>(
-                         p.K + (static_cast<size_t>(seg) * p.max_seq + static_cast<size_t>(blk) * kBlock) * D) + col;
-    uint4 v[N];
+    uint4 v[2][N];
+    int n[2];
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-        v[i] = k[static_cast<size_t>(min(r0 + i * RG, n - 1)) * C];   // (a row twice changes nothing)
-    __nv_bfloat162 lo[4], hi[4], amax = __habs2(reinterpret_cast<const __nv_bfloat162 *>(&v[0])[0]);
+    for (int q = 0; q < 2; ++q) {
+        const int blk = at0 + 2 * q;
+        n[q] = min(kBlock, L - blk * kBlock);   // visible positions, none or less: no such block
+        const uint4 *k = reinterpret_cast<const uint4 *>(
+                             p.K + (static_cast<size_t>(seg) * p.max_seq + static_cast<size_t>(blk) * kBlock) * D) + col;
+        if (n[q] > 0)
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        lo[e] = hi[e] = reinterpret_cast<const __nv_bfloat162 *>(&v[0])[e];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const __nv_bfloat162 *x = reinterpret_cast<const __nv_bfloat162 *>(&v[i]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            lo[e] = __hmin2(lo[e], x[e]);
-            hi[e] = __hmax2(hi[e], x[e]);
-            amax = __hmax2_nan(amax, __habs2(x[e]));   // (a NaN stays)
-        }
+            for (int i = 0; i < N; ++i)
+                v[q][i] = k[static_cast<size_t>(min(r0 + i * RG, n[q] - 1)) * C];   // (a row twice changes nothing)
     }
     auto other = [](__nv_bfloat162 x, int s) {
         const uint32_t u = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t *>(&x), s);
         return *reinterpret_cast<const __nv_bfloat162 *>(&u);
     };
 #pragma unroll
-    for (int s = C; s < 32; s <<= 1)
+    for (int q = 0; q < 2; ++q) {
+        if (q > 0)
+            __syncthreads();   // the first block's reduction is read
+        if (n[q] > 0) {
+            __nv_bfloat162 lo[4], hi[4], amax = __habs2(reinterpret_cast<const __nv_bfloat162 *>(&v[q][0])[0]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            lo[e] = __hmin2(lo[e], other(lo[e], s));
-            hi[e] = __hmax2(hi[e], other(hi[e], s));
+            for (int e = 0; e < 4; ++e)
+                lo[e] = hi[e] = reinterpret_cast<const __nv_bfloat162 *>(&v[q][0])[e];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const __nv_bfloat162 *x = reinterpret_cast<const __nv_bfloat162 *>(&v[q][i]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    lo[e] = __hmin2(lo[e], x[e]);
+                    hi[e] = __hmax2(hi[e], x[e]);
+                    amax = __hmax2_nan(amax, __habs2(x[e]));   // (a NaN stays)
+                }
+            }
+#pragma unroll
+            for (int s = C; s < 32; s <<= 1)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    lo[e] = __hmin2(lo[e], other(lo[e], s));
+                    hi[e] = __hmax2(hi[e], other(hi[e], s));
+                }
+#pragma unroll
+            for (int s = 1; s < 32; s <<= 1)
+                amax = __hmax2_nan(amax, other(amax, s));
+            if (lane < C) {
+                *reinterpret_cast<uint4 *>(&s_lo[half][warp][col * 8]) = *reinterpret_cast<const uint4 *>(lo);
+                *reinterpret_cast<uint4 *>(&s_hi[half][warp][col * 8]) = *reinterpret_cast<const uint4 *>(hi);
+            }
+            if (lane == 0) {
+                const float a = __low2float(amax), b = __high2float(amax);
+                s_max[half][warp] = a != a || b != b ? __int_as_float(0x7f800000) : fmaxf(a, b);
+            }
         }
+        __syncthreads();
+        if (n[q] <= 0)
+            continue;
+        float most = 0.f;
 #pragma unroll
-    for (int s = 1; s < 32; s <<= 1)
-        amax = __hmax2_nan(amax, other(amax, s));
-    if (lane < C) {
-        *reinterpret_cast<uint4 *>(&s_lo[warp][col * 8]) = *reinterpret_cast<const uint4 *>(lo);
-        *reinterpret_cast<uint4 *>(&s_hi[warp][col * 8]) = *reinterpret_cast<const uint4 *>(hi);
-    }
-    if (lane == 0) {
-        const float a = __low2float(amax), b = __high2float(amax);
-        s_max[warp] = a != a || b != b ? __int_as_float(0x7f800000) : fmaxf(a, b);
-    }
-    __syncthreads();
-    float most = 0.f;
+        for (int w = 0; w < W; ++w)
+            most = fmaxf(most, s_max[half][w]);
+        const bool unknown = !(most <= kLargest);
+        const float scale = unknown ? __int_as_float(0x7f800000) : scale_of(most);
+        const size_t at = static_cast<size_t>(seg) * p.n_blocks + at0 + 2 * q;
+        // four channels a thread: their least, then their largest codes
+        if (tid < D / 2) {
+            const bool upper = tid >= D / 4;
+            const int c = (upper ? tid - D / 4 : tid) * 4;
+            const float inv = unknown ? 0.f : inverse_power(scale);   // exact quotients
+            uint32_t codes = 0;
 #pragma unroll
-    for (int w = 0; w < W; ++w)
-        most = fmaxf(most, s_max[w]);
-    const bool unknown = !(most <= kLargest);
-    const float scale = unknown ? __int_as_float(0x7f800000) : scale_of(most);
-    const size_t at = static_cast<size_t>(seg) * p.n_blocks + blk;
-    // four channels a thread: their least, then their largest codes
-    if (tid < D / 2) {
-        const bool upper = tid >= D / 4;
-        const int c = (upper ? tid - D / 4 : tid) * 4;
-        const float inv = unknown ? 0.f : inverse_power(scale);   // exact quotients
-        uint32_t codes = 0;
+            for (int e = 0; e < 4; ++e) {
+                __nv_bfloat16 x = upper ? s_hi[half][0][c + e] : s_lo[half][0][c + e];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            __nv_bfloat16 x = upper ? s_hi[0][c + e] : s_lo[0][c + e];
-#pragma unroll
-            for (int w = 1; w < W; ++w)
-                x = upper ? __hmax(x, s_hi[w][c + e]) : __hmin(x, s_lo[w][c + e]);
-            const float y = __bfloat162float(x) * inv;
-            const int code = unknown ? (upper ? 127 : -127) : static_cast<int>(upper ? ceilf(y) : floorf(y));
-            codes |= (static_cast<uint32_t>(code) & 255u) << (8 * e);
+                for (int w = 1; w < W; ++w)
+                    x = upper ? __hmax(x, s_hi[half][w][c + e]) : __hmin(x, s_lo[half][w][c + e]);
+                const float y = __bfloat162float(x) * inv;
+                const int code = unknown ? (upper ? 127 : -127) : static_cast<int>(upper ? ceilf(y) : floorf(y));
+                codes |= (static_cast<uint32_t>(code) & 255u) << (8 * e);
+            }
+            *reinterpret_cast<uint32_t *>(p.bounds + at * 2 * D + (upper ? D : 0) + c) = codes;
         }
-        *reinterpret_cast<uint32_t *>(p.bounds + at * 2 * D + (upper ? D : 0) + c) = codes;
+        if (tid == 0)
+            p.scales[at] = scale;
     }
-    if (tid == 0)
-        p.scales[at] = scale;
 }
 
 constexpr int kSelectThreads = 512;
@@ -285,10 +312,12 @@ const void *select_fn()
 
 }  // namespace
 
+int bounds_ctas(int n_blocks) { return (n_blocks + kBoundsBlocks - 1) / kBoundsBlocks; }
+
 cudaError_t launch_bounds(int head_dim, const BoundsParams &p, cudaStream_t stream)
 {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(p.ctas * static_cast<unsigned>(p.b * p.g));
+    cfg.gridDim = dim3(static_cast<unsigned>(p.start[p.b]));
     cfg.blockDim = dim3(kBoundsThreads);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];

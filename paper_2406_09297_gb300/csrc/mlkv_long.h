@@ -109,10 +109,11 @@ struct BoundsParams {
     int8_t *bounds;            // [b][g][n_blocks][2][D]
     float *scales;             // [b][g][n_blocks]
     int b, g, max_seq, n_blocks;
-    unsigned ctas;             // of a segment: blocks of the sequence with most new ones
     int seq_len[MLKV_MAX_BATCH];
     int first[MLKV_MAX_BATCH]; // first position that is new
+    int start[MLKV_MAX_BATCH + 1];   // first CTA of a sequence, bounds_ctas a KV head
 };
+int bounds_ctas(int n_blocks);   // of a KV head with n_blocks new blocks
 cudaError_t launch_bounds(int head_dim, const BoundsParams &p, cudaStream_t stream);
 
 struct SelectParams {

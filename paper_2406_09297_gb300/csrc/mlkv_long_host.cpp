@@ -527,19 +527,21 @@ int mlkv_block_bounds(mlkv_cache_t c, int layer, const int *first, const int *se
     const size_t blocks = static_cast<size_t>(c->b) * c->g * p.n_blocks;
     if (overlap(bounds, blocks * 2 * c->d, scales, blocks * 4))
         return fail(MLKV_ERR_INVALID_ARG, "bounds overlap scales");
-    long long most = 0;
+    long long ctas = 0;
     for (int beta = 0; beta < c->b; ++beta) {
         const int f = first != nullptr ? first[beta] : 0;
         if (f < 0 || f > seq_lens[beta])
             return fail(MLKV_ERR_RANGE, "first[%d] = %d outside [0, %d]", beta, f, seq_lens[beta]);
         p.seq_len[beta] = seq_lens[beta];
         p.first[beta] = f;
-        most = std::max(most, (static_cast<long long>(seq_lens[beta]) + 63) / 64 - f / 64);
+        p.start[beta] = static_cast<int>(std::min(ctas, 0x7fffffffLL));
+        ctas += static_cast<long long>(c->g) * mlkv::bounds_ctas((seq_lens[beta] + 63) / 64 - f / 64);
     }
-    if (most == 0)
+    if (ctas == 0)
         return MLKV_OK;
-    if (most * c->b * c->g > 0x7fffffffLL)
-        return fail(MLKV_ERR_UNSUPPORTED, "%lld blocks exceed a launch", most * c->b * c->g);
+    if (ctas > 0x7fffffffLL)
+        return fail(MLKV_ERR_UNSUPPORTED, "%lld CTAs exceed a launch", ctas);
+    p.start[c->b] = static_cast<int>(ctas);
     const size_t slot = c->cache_bytes / c->m;
     p.K = reinterpret_cast<const __nv_bfloat16 *>(static_cast<char *>(c->cache) + slot * c->slot[layer]);
     p.bounds = static_cast<int8_t *>(bounds);
@@ -547,7 +549,6 @@ int mlkv_block_bounds(mlkv_cache_t c, int layer, const int *first, const int *se
     p.b = c->b;
     p.g = c->g;
     p.max_seq = c->max_seq;
-    p.ctas = static_cast<unsigned>(most);
     DeviceGuard guard(c->device);
     const cudaError_t e = mlkv::launch_bounds(c->d, p, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? MLKV_OK : fail_cuda(e, "block bounds launch");

@@ -651,7 +651,7 @@ __global__ void __launch_bounds__(kWide ? kMergeThreads : 128) merge_kernel(cons
 // where they fit).
 constexpr int kWeightThreads = 256;
 template <int D>
-__global__ void __launch_bounds__(kWeightThreads, 6)
+__global__ void __launch_bounds__(kWeightThreads, 4)
     weights_kernel(const __grid_constant__ PieceParams p, const __grid_constant__ WeightsParams w)
 {
     __shared__ float s_lse[16];
@@ -675,6 +675,27 @@ __global__ void __launch_bounds__(kWeightThreads, 6)
     }
     const int u0 = part * w.chunk, u1 = min(u0 + w.chunk, w.max_seq);
     const size_t row = static_cast<size_t>(seg) * w.max_seq;
+    const float *sc = p.scores + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * G) * p.score_stride;
+    constexpr int U = 4, B = 4;   // positions of a thread, and heads, at a time
+    float s[B][U], before[U];
+    auto fetch = [&](int v, int i0) {
+#pragma unroll
+        for (int i = 0; i < B; ++i)
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int u = v + k * kWeightThreads;
+                s[i][k] = i0 + i < G && u < min(x.L, u1) ? __ldcg(sc + (i0 + i) * p.score_stride + u) : neg_inf();
+            }
+    };
+    auto fetch_before = [&](int v) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int u = v + k * kWeightThreads;
+            before[k] = w.weights_in != nullptr && u < u1 ? w.weights_in[row + u] : 0.f;
+        }
+    };
+    fetch(u0 + tid, 0);   // (on the way while the sums are added up)
+    fetch_before(u0 + tid);
     if (u0 < x.L) {
         // log2 of every head's sum, from the records: a warp a head
         for (int i = tid >> 5; i < G; i += kWeightThreads / 32) {
@@ -682,43 +703,40 @@ __global__ void __launch_bounds__(kWeightThreads, 6)
             float mx = neg_inf();
             for (int k = lane; k < x.count; k += 32)
                 mx = fmaxf(mx, __ldcg(p.part_lse + (rec0 + k) * G + i));
-            for (int s = 16; s > 0; s >>= 1)
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
+            for (int d = 16; d > 0; d >>= 1)
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
             float tot = 0.f;
             for (int k = lane; k < x.count; k += 32) {
                 const float lse = __ldcg(p.part_lse + (rec0 + k) * G + i);
                 tot += lse == neg_inf() ? 0.f : exp2f(lse - mx);
             }
-            for (int s = 16; s > 0; s >>= 1)
-                tot += __shfl_xor_sync(0xffffffffu, tot, s);
+            for (int d = 16; d > 0; d >>= 1)
+                tot += __shfl_xor_sync(0xffffffffu, tot, d);
             if (lane == 0)
                 s_lse[i] = mx + log2f(tot);
         }
         __syncthreads();
     }
-    const float *sc = p.scores + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * G) * p.score_stride;
-    constexpr int U = 4;   // positions of a thread at a time
     for (int v = u0 + tid; v < u1; v += U * kWeightThreads) {
-        float a[U], before[U];
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-            const int u = v + k * kWeightThreads;
-            before[k] = w.weights_in != nullptr && u < u1 ? w.weights_in[row + u] : 0.f;
-            a[k] = 0.f;
+        if (v != u0 + tid) {
+            fetch(v, 0);
+            fetch_before(v);
         }
-        if (v < x.L) {
-#pragma unroll 4
-            for (int i = 0; i < G; ++i) {
-                const float lse = s_lse[i];
-                float s[U];
+        float a[U];
 #pragma unroll
-                for (int k = 0; k < U; ++k) {
-                    const int u = v + k * kWeightThreads;
-                    s[k] = u < x.L ? __ldcg(sc + i * p.score_stride + u) : neg_inf();
-                }
+        for (int k = 0; k < U; ++k)
+            a[k] = 0.f;
+        for (int i0 = 0; v < x.L && i0 < G; i0 += B) {
+            if (i0 > 0)
+                fetch(v, i0);
+#pragma unroll
+            for (int i = 0; i < B; ++i) {
+                if (i0 + i >= G)
+                    break;
+                const float lse = s_lse[i0 + i];
 #pragma unroll
                 for (int k = 0; k < U; ++k)
-                    a[k] += exp2f(s[k] - lse);
+                    a[k] += exp2f(s[i][k] - lse);
             }
         }
 #pragma unroll
