@@ -19,9 +19,12 @@ constexpr int kBlock = MLKV_BLOCK;
 enum : int {
     kPieceSuffix = 0,   // positions [0, seq_len), merged with a shared prefix's records
     kPieceBlocks = 1,   // the blocks listed for every (sequence, KV head)
+    kPieceGroups = 4,   // kPieceSuffix with units in front, each a chunk of a prefix's positions for a few sequences
     kPieceJoined = 3,   // a prefix's positions, read for every sequence apart, and then [0, seq_len)
     kPieceWeights = 2,  // positions [0, seq_len); every score is stored, the merge left to weights_kernel
 };
+
+constexpr int kPieceMaxUnits = 1024;
 
 // Decode attention of one layer in pieces: a segment (sequence, KV head) of nt tiles of 64 positions is cut
 // into pieces of `tiles` tiles, a CTA each.  Passed by value.
@@ -55,15 +58,29 @@ struct PieceParams {
     long long score_stride;
     int seq_len[MLKV_MAX_BATCH];          // (this and what follows by row) positions that the row sees
     int first[MLKV_MAX_BATCH + 1];        // its first piece (KV head after KV head inside)
-    uint16_t q_row[MLKV_MAX_BATCH], seq[MLKV_MAX_BATCH];
+    union {
+        struct {
+            uint16_t q_row[MLKV_MAX_BATCH], seq[MLKV_MAX_BATCH];   // scattered
+        };
+        int prefix_len[MLKV_MAX_BATCH];   // kPieceGroups: of the prefix cache's sequences
+    };
     uint16_t pre_place[MLKV_MAX_BATCH];   // kPieceSuffix: its place in the prefix's records;
                                           // kPieceJoined: its prefix's number
     union {
-        uint16_t pre_n[MLKV_MAX_BATCH];   // kPieceSuffix: those records' number
+        struct {
+            uint16_t pre_n[MLKV_MAX_BATCH];         // kPieceSuffix: those records' number
+            uint16_t place_row[MLKV_MAX_BATCH];     // kPieceGroups: the row at a place
+        };
         int pre_len[MLKV_MAX_BATCH];      // kPieceJoined: positions of its prefix, 0: none
     };
-    int prefix_b;                         // kPieceJoined: sequences of the prefix cache
+    int prefix_b;                         // kPieceJoined, kPieceGroups: sequences of the prefix cache
+    // kPieceGroups: units, the launch's first CTAs: unit_tiles tiles from unit_tiles * chunk on of a prefix, for the
+    // heads of KV head j of up to 16 / G rows from a place on.
+    int n_units, unit_tiles;
+    uint32_t units[kPieceMaxUnits];       // prefix | chunk << 10 | j << 18 | (rows - 1) << 26
+    uint16_t unit_place[kPieceMaxUnits];
 };
+static_assert(sizeof(PieceParams) + 2 * sizeof(CUtensorMap) < 32764, "kernel parameters");
 // Tiles of a segment.
 template <int kMode>
 __host__ __device__ inline int piece_tiles(const PieceParams &p, int beta)

@@ -24,7 +24,7 @@ using mlkv::overlap;
 namespace {
 
 // Bits of mlkv_cache::long_ready.
-enum : unsigned { kReadyPieces = 1, kReadySelect = 16, kReadyEvict = 32, kReadyShared = 64 };   // pieces: 4 bits
+enum : unsigned { kReadyPieces = 1, kReadySelect = 32, kReadyEvict = 64, kReadyShared = 128 };   // pieces: 5 bits
 
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
@@ -60,7 +60,7 @@ int prepare_pieces(mlkv_cache *c, int mode)
 // of resident CTAs half a piece more where segments are split (whole ones end evenly enough).  Split segments
 // are merged by the CTA that ends last, a round trip to L2 for every 8 records, or by a launch of their own
 // of their own.  Never more pieces than there are records.  pre: records that every merge has besides; hbm_tiles:
-// tiles that come from HBM, the others from L2 (10 TB/s); -1: all.
+// tiles that come from HBM, the others from L2 (14 TB/s, groups above 8 heads 10); -1: all.
 struct Cut {
     bool defer;
     int records;   // of a segment, at most
@@ -92,7 +92,7 @@ Cut plan_cut(const mlkv_cache *c, const CutRules &r, const Tiles &nt)
     // us: a tile of a CTA alone on its SM; all tiles at the rate of HBM; a record's part of an inline merge
     const double tile = c->d == 64 ? 0.33 : c->G <= 8 ? 0.45 : 0.72;
     const double from_hbm = r.hbm_tiles < 0 ? total : r.hbm_tiles;
-    const double bytes = std::max(from_hbm / 6.7e6, total / 10e6) * 256.0 * c->d, record = 0.1 * c->G * c->d / 512;
+    const double bytes = std::max(from_hbm / 6.7e6, total / (c->G <= 8 ? 14e6 : 10e6)) * 256.0 * c->d, record = 0.1 * c->G * c->d / 512;
     const int inline_most = mlkv::piece_max_records(c->d, c->G) - r.pre;
     Cut best = {r.always_apart, 1, longest, 1e30};
     for (int want = 1, tiles = longest;; want += (want + 3) / 4) {   // pieces of the longest segment
@@ -223,7 +223,7 @@ struct PrefixPlan {
 // 32768: 115 us beside 80 SMs of 52 tiles a unit, 147 one after the other.
 PrefixPlan plan_prefix(const int *n_kt, const int *pairs, int n, int sm_count, int d, double bytes)
 {
-    const double tile = d == 64 ? 0.95 : 1.5, edges = 7, rate = 75e3, all = 6.5e6, start = 13;
+    const double tile = d == 64 ? 0.95 : 1.5, edges = 7, rate = 75e3, all = 6.5e6;
     long long work = 0;
     int longest = 1;
     for (int x = 0; x < n; ++x) {
@@ -240,11 +240,11 @@ PrefixPlan plan_prefix(const int *n_kt, const int *pairs, int n, int sm_count, i
         for (int rounds = 1; rounds <= 8; ++rounds) {   // of the units, on as many SMs as it takes
             const int sms = static_cast<int>(std::min<long long>(sm_count, (units + rounds - 1) / rounds));
             const double t = static_cast<double>((units + sms - 1) / sms) * (kc + edges) * tile;
-            const double one = start + 2 + t + bytes / all;
+            const double one = (bytes < 16e6 ? 7 : 15) + t + bytes / all;
             if (one < best.us)
                 best = {kc, sms, false, one};
             const double beside =
-                start + t + std::max(0.0, bytes - t * std::min(all, rate * (sm_count - sms))) / all;
+                13 + t + std::max(0.0, bytes - t * std::min(all, rate * (sm_count - sms))) / all;
             if (sm_count - sms >= 8 && bytes >= 16e6 && beside < best.us)
                 best = {kc, sms, true, beside};
         }
@@ -352,12 +352,48 @@ int mlkv::decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const 
     }
     if (most_kt > 0)
         plan = plan_prefix(n_kt, pairs, np, c->sm_count, c->d, bytes);
-    const bool apart = most_kt > 0 && plan.us < end_to_end.us;
+    // The prefixes for as many sequences at a time as have 16 heads together, beside the suffixes in their launch: read
+    // from L2 again for every group of them, and merged by a launch.  us: 9, and what is longest of the bytes from HBM,
+    // those through the SMs (8.5 TB/s) and a unit; half the longest suffix more where those are uneven.  Measured, us, end
+    // to end / by groups / by the prefix kernel: 4 sequences behind 16000 positions, 8 KV heads of 128, 31 / 22 / 27,
+    // 8 of them 46 / 27 / 32, 16 of them 65 / 39 / 34; 16 behind 4000, 12 KV heads of 64, 25 / 11 / 15.
+    const int S1 = 16 / c->G;
+    double grouped_us = 1e30;
+    int unit_tiles = 8;
+    if (most_kt > 0 && !rows.scattered) {
+        double from_l2 = 0, in_units = 0;
+        int longest = 1, shortest = 0x7fffffff;
+        for (int beta = 0; beta < rows.n; ++beta) {
+            const int nt = (rows.len[beta] + 63) / 64;
+            from_l2 += nt;
+            longest = std::max(longest, nt);
+            shortest = std::min(shortest, nt);
+        }
+        for (int x = 0; x < np; ++x)
+            if (u.group_n[x] > 0)
+                in_units += static_cast<double>((prefix_lens[x] + 63) / 64) * ((u.group_n[x] + S1 - 1) / S1);
+        from_l2 += in_units;
+        // as many units as CTAs are resident, at most; no more than 255 chunks of a prefix
+        unit_tiles = std::max({unit_tiles, static_cast<int>(in_units * c->g / (1.75 * c->sm_count)) + 1,
+                               (2 * most_kt + 254) / 255});
+        long long units = 0;
+        for (int x = 0; x < np; ++x)
+            if (u.group_n[x] > 0)
+                units += static_cast<long long>(((prefix_lens[x] + 63) / 64 + unit_tiles - 1) / unit_tiles) *
+                         ((u.group_n[x] + S1 - 1) / S1) * c->g;
+        const double tile_bytes = 256.0 * c->d * c->g, tile = c->d == 64 ? 0.34 : 0.72;
+        if (units <= mlkv::kPieceMaxUnits)
+            grouped_us = 9 + std::max({hbm / 6.3e6 * tile_bytes, from_l2 / 8.5e6 * tile_bytes,
+                                       1.15 * unit_tiles * tile}) +
+                         (longest > shortest + unit_tiles ? 0.5 * longest * tile : 0.0);
+    }
+    const double apart_us = most_kt > 0 ? plan.us : 1e30;
+    const bool grouped = grouped_us < std::min(apart_us, end_to_end.us);
     if (fits != nullptr) {
-        *fits = (apart ? plan.us : end_to_end.us) < most_us;
+        *fits = std::min(apart_us, end_to_end.us) < most_us;   // (scattered: no groups)
         return MLKV_OK;
     }
-    if (!apart) {
+    if (!grouped && end_to_end.us <= apart_us) {
         if ((rc = ::prepare_pieces(c, mlkv::kPieceJoined)) != MLKV_OK)
             return rc;
         p.prefix_b = prefix->b;
@@ -384,21 +420,28 @@ int mlkv::decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const 
                 u.seq[place] = rows.scattered ? rows.q_row[beta] : static_cast<uint16_t>(beta);
             }
     }
-    if (!(c->long_ready & kReadyShared)) {
+    if (!grouped && !(c->long_ready & kReadyShared)) {
         const cudaError_t e = mlkv::prepare_shared(c->d, true);
         if (e != cudaSuccess)
             return fail_cuda(e, "preparing the decode over a shared prefix");
         c->long_ready |= kReadyShared;
     }
-    const int kc = plan.kc;
-    const int cmax = (most_kt + kc - 1) / kc;
+    // chunks of a prefix, in key tiles of 128 positions, or of 64 by groups
+    const int kc = grouped ? unit_tiles : plan.kc;
+    const auto chunks = [&](int x) {
+        return ((grouped ? (prefix_lens[x] + 63) / 64 : (prefix_lens[x] + 127) / 128) + kc - 1) / kc;
+    };
+    int cmax = 0;
+    for (int x = 0; x < np; ++x)
+        if (n_kt[x] > 0)
+            cmax = std::max(cmax, chunks(x));
     const size_t records = static_cast<size_t>(places) * c->g * cmax * c->G;
     for (int beta = 0; beta < rows.n; ++beta) {
         const int x = of(beta);
-        p.pre_n[beta] = static_cast<uint16_t>(x < 0 ? 0 : (n_kt[x] + kc - 1) / kc);
+        p.pre_n[beta] = static_cast<uint16_t>(x < 0 ? 0 : chunks(x));
     }
     const auto own = [&](int beta) { return mlkv::piece_tiles<mlkv::kPieceSuffix>(p, beta); };
-    const Cut split = plan_cut(c, {rows.n, room, plan.beside, rows.scattered != 0, cmax, -1}, own);
+    const Cut split = plan_cut(c, {rows.n, room, grouped || plan.beside, rows.scattered != 0, cmax, -1}, own);
     lay_pieces(c, p, split, own);
     if ((rc = rows.scattered ? own_records(c, p, records * (c->d + 1), stream)
                              : scratch(c, records * (c->d + 1), "records of the shared prefix", stream)) != MLKV_OK)
@@ -408,6 +451,27 @@ int mlkv::decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const 
     p.pre_o = u.part;
     p.pre_lse = u.part_lse;
     p.pre_chunks = cmax;
+    if (grouped) {
+        if ((rc = ::prepare_pieces(c, mlkv::kPieceGroups)) != MLKV_OK)
+            return rc;
+        std::memcpy(p.prefix_len, prefix_lens, sizeof(int) * np);
+        for (int beta = 0; beta < rows.n; ++beta)
+            if (of(beta) >= 0)
+                p.place_row[p.pre_place[beta]] = static_cast<uint16_t>(beta);
+        p.prefix_b = np;
+        p.unit_tiles = kc;
+        p.n_units = 0;
+        for (int x = 0; x < np; ++x)
+            for (int j = 0; j < c->g && n_kt[x] > 0; ++j)
+                for (int ch = 0; ch < chunks(x); ++ch)
+                    for (int s = 0; s < u.group_n[x]; s += S1) {   // neighbours read the same tiles
+                        p.units[p.n_units] = static_cast<uint32_t>(x) | (static_cast<uint32_t>(ch) << 10) |
+                                             (static_cast<uint32_t>(j) << 18) |
+                                             (static_cast<uint32_t>(std::min(S1, u.group_n[x] - s) - 1) << 26);
+                        p.unit_place[p.n_units++] = static_cast<uint16_t>(u.group_at[x] + s);
+                    }
+        return decode_pieces(c, mlkv::kPieceGroups, p, split, rows64(prefix), stream);
+    }
     p.early = 1;
     // The queries [b][h][D] as (channel, head in group, group, 1, sequence): a box of 64 channels x G heads x
     // min(L1, b) neighbours is a tile's rows, one of 64 channels x G heads a scattered sequence's.

@@ -2,6 +2,7 @@
 //
 //   suffix    a sequence's own positions, merged with the records of a prefix that other sequences share
 //   joined    a prefix's positions and then the sequence's own, end to end
+//   groups    suffixes, and beside them the prefix's positions for as many sequences as have 16 heads together
 //   blocks    the blocks of 64 positions listed for every (sequence, KV head)
 //   weights   all positions, every score stored on the way (weights_kernel turns them into weights)
 //
@@ -54,17 +55,49 @@ __device__ __forceinline__ float neg_inf() { return -__int_as_float(0x7f800000);
 
 struct Piece {
     int beta, j, seg, index, count, t0, t1, L;   // beta: the query row
+    int rows;      // heads of the piece's tile
+    int out_row;   // of out
+    int unit, place, prefix, chunk;              // kPieceGroups: a unit (else 0), its place, prefix and chunk
 };
 
 // Row of Q and out, and sequence, of a query row.
-__device__ __forceinline__ int q_row(const PieceParams &p, int i) { return p.scattered ? p.q_row[i] : i; }
-__device__ __forceinline__ int row_seq(const PieceParams &p, int i) { return p.scattered ? p.seq[i] : i; }
+// (only what runs over prefixes has scattered rows, kPieceGroups none)
+template <int kMode>
+__device__ __forceinline__ int q_row_of(const PieceParams &p, int i)
+{
+    return (kMode == kPieceSuffix || kMode == kPieceJoined) && p.scattered ? p.q_row[i] : i;
+}
+template <int kMode>
+__device__ __forceinline__ int row_seq(const PieceParams &p, int i)
+{
+    return (kMode == kPieceSuffix || kMode == kPieceJoined) && p.scattered ? p.seq[i] : i;
+}
 
 template <int kMode>
 __device__ __forceinline__ Piece piece_of(const PieceParams &p)
 {
     Piece x;
-    const int c = static_cast<int>(blockIdx.x);
+    x.unit = x.place = x.prefix = x.chunk = 0;
+    x.rows = p.G;
+    int c = static_cast<int>(blockIdx.x);
+    if (kMode == kPieceGroups) {
+        if (c < p.n_units) {
+            const uint32_t u = p.units[c];
+            x.unit = 1;
+            x.prefix = static_cast<int>(u & 0x3ffu);
+            x.chunk = static_cast<int>((u >> 10) & 0xffu);
+            x.j = static_cast<int>((u >> 18) & 0xffu);
+            x.rows = (static_cast<int>(u >> 26) + 1) * p.G;
+            x.place = p.unit_place[c];
+            x.beta = x.seg = x.index = x.out_row = 0;
+            x.count = 1;
+            x.L = p.prefix_len[x.prefix];
+            x.t0 = x.chunk * p.unit_tiles;
+            x.t1 = min((x.L + T - 1) / T, x.t0 + p.unit_tiles);
+            return x;
+        }
+        c -= p.n_units;
+    }
     int lo = 0, hi = p.n - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -81,6 +114,7 @@ __device__ __forceinline__ Piece piece_of(const PieceParams &p)
     x.j = rel / x.count;
     x.index = rel - x.j * x.count;
     x.seg = lo * p.g + x.j;
+    x.out_row = q_row_of<kMode>(p, lo);
     x.t0 = x.index * p.tiles;
     x.t1 = min(nt, x.t0 + p.tiles);
     return x;
@@ -114,7 +148,7 @@ __device__ void merge_records(const PieceParams &p, const Piece &x, size_t own0,
         s_w[n * G + tid] = tot == 0.f ? 0.f : 1.f / tot;
     }
     asm volatile("bar.sync 1, %0;" ::"r"(n_threads) : "memory");
-    __nv_bfloat16 *ob = p.out + (static_cast<size_t>(q_row(p, x.beta)) * p.h + static_cast<size_t>(x.j) * G) * D;
+    __nv_bfloat16 *ob = p.out + (static_cast<size_t>(x.out_row) * p.h + static_cast<size_t>(x.j) * G) * D;
     for (int i = tid * 4; i < G * D; i += n_threads * 4) {
         const int row = i / D;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -174,6 +208,7 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
         fence_barrier_init();
     }
     const bool early = kMode == kPieceSuffix && p.early;
+    const bool group = kMode == kPieceGroups;
     if (!early)
         grid_dependency_wait();
     grid_dependents_launch();
@@ -199,9 +234,10 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
         __syncwarp();
         asm volatile("bar.arrive 2, %0;" ::"n"(PL::kThreads) : "memory");
         // ------------------------------------ producer ------------------------------------------
-        const int zk = ((p.slot * 2 + 0) * p.b + row_seq(p, x.beta)) * p.g + x.j, zv = zk + p.b * p.g;
-        const int zk_pre = kMode == kPieceJoined
-                               ? (p.slot * 2 * p.prefix_b + static_cast<int>(p.pre_place[x.beta])) * p.g + x.j
+        const int zk = ((p.slot * 2 + 0) * p.b + row_seq<kMode>(p, x.beta)) * p.g + x.j, zv = zk + p.b * p.g;
+        const int zk_pre = kMode == kPieceJoined || group
+                               ? (p.slot * 2 * p.prefix_b +
+                                  (group ? x.prefix : static_cast<int>(p.pre_place[x.beta]))) * p.g + x.j
                                : 0;
         int idx = 0;
         for (int t = x.t0; t < x.t1; ++t) {
@@ -219,7 +255,7 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
                 if (ok) {
                     const uint32_t fb = bar_full + 8 * s, dst = sbase + s * 2 * PL::kTile;
                     mbar_arrive_expect_tx(fb, 2 * PL::kTile);
-                    const bool pre = kMode == kPieceJoined && t < n_joined;
+                    const bool pre = (kMode == kPieceJoined && t < n_joined) || (group && x.unit);
                     const CUtensorMap *map = pre ? &tmap_prefix : &tmap;
 #pragma unroll
                     for (int sub = 0; sub < D / 64; ++sub)
@@ -250,16 +286,23 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     const int half = warp % PL::kPerStage * PL::kKeys;   // the warp's first key of a tile
     uint32_t qf[D / 16][NH][2];   // columns n = lane / 4
     {
-        const __nv_bfloat16 *q = p.Q + (static_cast<size_t>(q_row(p, x.beta)) * p.h + static_cast<size_t>(x.j) * p.G) * D;
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk)
+        for (int nh = 0; nh < NH; ++nh) {
+            const int head = nh * 8 + (lane >> 2);   // of the tile's rows
+            int row = q_row_of<kMode>(p, x.beta), at = head;
+            if (group && x.unit && head < x.rows) {
+                row = p.place_row[x.place + head / p.G];
+                at = head % p.G;
+            }
+            const __nv_bfloat16 *q =
+                p.Q + (static_cast<size_t>(row) * p.h + static_cast<size_t>(x.j) * p.G + at) * D + (lane & 3) * 2;
 #pragma unroll
-            for (int nh = 0; nh < NH; ++nh)
+            for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int head = nh * 8 + (lane >> 2), ch = kk * 16 + i * 8 + (lane & 3) * 2;
-                    qf[kk][nh][i] = head < p.G ? *reinterpret_cast<const uint32_t *>(q + head * D + ch) : 0u;
-                }
+                for (int i = 0; i < 2; ++i)
+                    qf[kk][nh][i] =
+                        head < x.rows ? *reinterpret_cast<const uint32_t *>(q + kk * 16 + i * 8) : 0u;
+        }
     }
     asm volatile("bar.sync 2, %0;" ::"n"(PL::kThreads) : "memory");
     float m[NH][2], l[NH][2];
@@ -444,7 +487,7 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int head = nh * 8 + (lane & 3) * 2 + i;
-            if (head < p.G) {
+            if (head < x.rows) {
                 float *to = s_o + (warp * 16 + head) * PL::kRow + (lane >> 2);
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) {
@@ -458,12 +501,12 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
         return;
     if (early && (!p.defer || blockIdx.x == gridDim.x - 1))
         grid_dependency_wait();   // (deferred merge: one CTA, so that this grid ends behind the prefix's)
-    const int n_pre = kMode == kPieceSuffix ? p.pre_n[x.beta] : 0;
-    const bool defer = kMode == kPieceWeights || p.defer;
+    const int n_pre = kMode == kPieceSuffix || kMode == kPieceGroups ? p.pre_n[x.beta] : 0;
+    const bool defer = kMode == kPieceWeights || group || p.defer;
     const bool whole = !defer && x.count == 1 && n_pre == 0;
-    const size_t rec = blockIdx.x;
-    __nv_bfloat16 *ob = p.out + (static_cast<size_t>(q_row(p, x.beta)) * p.h + static_cast<size_t>(x.j) * p.G) * D;
-    for (int i = tid * 4; i < p.G * D; i += kWarps * 32 * 4) {
+    const size_t rec = group ? blockIdx.x - static_cast<unsigned>(p.n_units) : blockIdx.x;
+    __nv_bfloat16 *ob = p.out + (static_cast<size_t>(q_row_of<kMode>(p, x.beta)) * p.h + static_cast<size_t>(x.j) * p.G) * D;
+    for (int i = tid * 4; i < x.rows * D; i += kWarps * 32 * 4) {
         const int row = i / D, ch = i - row * D;
         float mx = neg_inf();
 #pragma unroll
@@ -496,9 +539,17 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
             w2.y = pack_bf16x2(acc.z, acc.w);
             *reinterpret_cast<uint2 *>(ob + i) = w2;
         } else {
-            *reinterpret_cast<float4 *>(p.part_o + rec * p.G * D + i) = acc;
+            float *to_o = p.part_o, *to_lse = p.part_lse;
+            size_t to = rec * p.G + row;
+            if (group && x.unit) {   // the records of the rows' places
+                const int s = row / p.G;
+                to_o = const_cast<float *>(p.pre_o);
+                to_lse = const_cast<float *>(p.pre_lse);
+                to = ((static_cast<size_t>(x.place + s) * p.g + x.j) * p.pre_chunks + x.chunk) * p.G + row - s * p.G;
+            }
+            *reinterpret_cast<float4 *>(to_o + to * D + ch) = acc;
             if (ch == 0)
-                p.part_lse[rec * p.G + row] = tot == 0.f ? neg_inf() : mx + log2f(tot);
+                to_lse[to] = tot == 0.f ? neg_inf() : mx + log2f(tot);
         }
     }
     if (whole || defer)
@@ -608,7 +659,7 @@ __device__ void merge_rows(MergeShared<D> &sh, const PieceParams &p, const Piece
         uint2 w2;
         w2.x = pack_bf16x2(acc.x * inv, acc.y * inv);
         w2.y = pack_bf16x2(acc.z * inv, acc.w * inv);
-        *reinterpret_cast<uint2 *>(p.out + (static_cast<size_t>(q_row(p, x.beta)) * p.h + static_cast<size_t>(x.j) * G) * D +
+        *reinterpret_cast<uint2 *>(p.out + (static_cast<size_t>(x.out_row) * p.h + static_cast<size_t>(x.j) * G) * D +
                                    part * 128 + lane * 4) = w2;
     }
 }
@@ -622,6 +673,7 @@ __device__ __forceinline__ Piece segment_of(const PieceParams &p, int seg)
     x.j = seg - x.beta * p.g;
     x.L = p.seq_len[x.beta];
     x.count = (piece_tiles<kMode>(p, x.beta) + p.tiles - 1) / p.tiles;
+    x.out_row = q_row_of<kMode>(p, x.beta);
     return x;
 }
 
@@ -632,7 +684,7 @@ __global__ void __launch_bounds__(kWide ? kMergeThreads : 128) merge_kernel(cons
     const int parts = kWide ? (p.G * D + 127) / 128 : 1, seg = static_cast<int>(blockIdx.x) / parts;
     const Piece x = segment_of<kMode>(p, seg);
     const size_t own0 = static_cast<size_t>(p.first[x.beta]) + static_cast<size_t>(x.j) * x.count;
-    const int n_pre = kMode == kPieceSuffix ? p.pre_n[x.beta] : 0;
+    const int n_pre = kMode == kPieceSuffix || kMode == kPieceGroups ? p.pre_n[x.beta] : 0;
     grid_dependency_wait();
     grid_dependents_launch();
     if constexpr (kWide) {
@@ -754,6 +806,7 @@ const void *piece_fn(int mode)
     return mode == kPieceSuffix   ? reinterpret_cast<const void *>(&piece_kernel<D, kPieceSuffix, NH>)
            : mode == kPieceBlocks ? reinterpret_cast<const void *>(&piece_kernel<D, kPieceBlocks, NH>)
            : mode == kPieceJoined ? reinterpret_cast<const void *>(&piece_kernel<D, kPieceJoined, NH>)
+           : mode == kPieceGroups ? reinterpret_cast<const void *>(&piece_kernel<D, kPieceGroups, 2>)
                                   : reinterpret_cast<const void *>(&piece_kernel<D, kPieceWeights, NH>);
 }
 const void *piece_fn(int head_dim, int G, int mode)
@@ -807,7 +860,7 @@ cudaError_t launch_pieces(int head_dim, int mode, const CUtensorMap *tmap, const
 {
     void *args[] = {const_cast<CUtensorMap *>(tmap), const_cast<CUtensorMap *>(tmap_prefix),
                     const_cast<PieceParams *>(&p)};
-    return launch_pdl(piece_fn(head_dim, p.G, mode), dim3(static_cast<unsigned>(p.first[p.n])), piece_threads(head_dim),
+    return launch_pdl(piece_fn(head_dim, p.G, mode), dim3(static_cast<unsigned>(p.first[p.n] + (mode == kPieceGroups ? p.n_units : 0))), piece_threads(head_dim),
                       piece_smem(head_dim), stream, args);
 }
 
@@ -829,6 +882,7 @@ const void *merge_fn(int mode, bool wide)
 {
     return mode == kPieceBlocks   ? merge_fn<D, kPieceBlocks>(wide)
            : mode == kPieceJoined ? merge_fn<D, kPieceJoined>(wide)
+           : mode == kPieceGroups ? merge_fn<D, kPieceGroups>(wide)
                                   : merge_fn<D, kPieceSuffix>(wide);
 }
 

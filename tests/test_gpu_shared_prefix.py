@@ -85,6 +85,10 @@ def test_decode_small(d, h, g):
     (128, 16, 1, 33, 100, 2),       # eight sequences a tile
     (64, 12, 12, 300, 3, 2),        # one head a row: 128 sequences a tile
     (128, 14, 2, 50, 64, 1),        # 18 sequences of 7 heads: 126 rows of a tile
+    (128, 32, 8, 24, 1500, 4),      # four to seven sequences a prefix
+    (64, 12, 4, 21, 2500, 3),       # groups of five sequences of 3 heads, and what is left
+    (64, 14, 2, 12, 2500, 2),       # of two of 7
+    (128, 16, 1, 6, 3000, 2),       # of one of 16
 ])
 @pytest.mark.parametrize("p", [1, 127, 128, 1000, 5000])
 def test_decode_many_sequences(d, h, g, b, lens, n, p):
