@@ -356,7 +356,7 @@ cudaError_t launch_select(int head_dim, const SelectParams &p, int max_blocks, c
     attr[1].val.clusterDim.x = static_cast<unsigned>(size);
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 2;
+    cfg.numAttrs = size > 1 ? 2 : 1;   // (a cluster's launch costs the host a microsecond more)
     void *args[] = {const_cast<SelectParams *>(&p)};
     return cudaLaunchKernelExC(&cfg, head_dim == 64 ? select_fn<64>() : select_fn<128>(), args);
 }

@@ -249,7 +249,7 @@ cudaError_t launch_evict(int head_dim, const EvictParams &p, int max_len, int sm
     attr[1].val.clusterDim.x = static_cast<unsigned>(size);
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 2;
+    cfg.numAttrs = size > 1 ? 2 : 1;   // (a cluster's launch costs the host a microsecond more)
     void *args[] = {const_cast<EvictParams *>(&p)};
     cudaError_t e = cudaLaunchKernelExC(&cfg, reinterpret_cast<const void *>(&keep_kernel), args);
     if (e != cudaSuccess)
