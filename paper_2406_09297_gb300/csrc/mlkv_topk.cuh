@@ -30,9 +30,9 @@ struct TopkShared {
 };
 
 // CTA `rank` of a cluster of `size` holds keys key(0) .. key(n - 1), whose least and largest are lo and hi in
-// all threads (0xffffffff and 0 of none); the cluster (size 1: this CTA alone, whatever its cluster) holds at least `want` >= 1 keys.  Calls put(place, i) for
-// every one of its keys among the `want` largest, place its rank in the list's order among those.  All NT >= 256
-// threads of all the cluster's CTAs call it, behind a barrier for the keys.
+// all threads (0xffffffff and 0 of none); the cluster (size 1: this CTA alone, whatever its cluster) holds at least
+// `want` >= 1 keys.  Calls put(place, i) for every one of its keys among the `want` largest, place its rank in the
+// list's order among those.  All NT >= 256 threads of all the cluster's CTAs call it, behind a barrier for the keys.
 template <int NT, typename Key, typename Put>
 __device__ void cluster_topk(TopkShared<NT> &sh, unsigned size, unsigned rank, int n, unsigned lo, unsigned hi,
                              unsigned want, const Key &key, const Put &put)
@@ -69,11 +69,17 @@ __device__ void cluster_topk(TopkShared<NT> &sh, unsigned size, unsigned rank, i
     for (int round = 0; !all && lo != hi; ++round) {
         unsigned *hist = sh.hist[round & 1];
         const int s = max(0, 22 - __clz(static_cast<int>(hi - lo)));   // (hi - lo) >> s below 1024
+        // (keys that equal lo are counted apart: where many weights are the same, they are mostly the least)
+        unsigned at_lo = 0;
         for (int i = tid; i < n; i += NT) {
             const unsigned k = key(i);
-            if (k >= lo && k <= hi)
+            at_lo += k == lo;
+            if (k > lo && k <= hi)
                 atomicAdd(&hist[(k - lo) >> s], 1u);
         }
+        at_lo = __reduce_add_sync(0xffffffffu, at_lo);
+        if (lane == 0 && at_lo > 0)
+            atomicAdd(&hist[0], at_lo);
         sync();
         // the cluster's counts from the top: thread t takes the kPer intervals below kTopkBins - kPer t
         constexpr int kPer = kTopkBins >= NT ? kTopkBins / NT : 1;
