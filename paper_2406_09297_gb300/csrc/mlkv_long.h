@@ -56,8 +56,10 @@ struct PieceParams {
     // kPieceWeights: scores times log2(e) / sqrt(D), [b][h][score_stride]
     float *scores;
     long long score_stride;
+    int ordered;                          // rows are laid out as order lists them, the longest first; 0: as they are
+    uint16_t order[MLKV_MAX_BATCH];
+    int first[MLKV_MAX_BATCH + 1];        // first piece of the i-th row in that order (KV head after KV head inside)
     int seq_len[MLKV_MAX_BATCH];          // (this and what follows by row) positions that the row sees
-    int first[MLKV_MAX_BATCH + 1];        // its first piece (KV head after KV head inside)
     union {
         struct {
             uint16_t q_row[MLKV_MAX_BATCH], seq[MLKV_MAX_BATCH];   // scattered

@@ -73,6 +73,9 @@ __device__ __forceinline__ int row_seq(const PieceParams &p, int i)
     return (kMode == kPieceSuffix || kMode == kPieceJoined) && p.scattered ? p.seq[i] : i;
 }
 
+// The i-th row as the pieces are laid out.
+__device__ __forceinline__ int row_at(const PieceParams &p, int i) { return p.ordered ? p.order[i] : i; }
+
 template <int kMode>
 __device__ __forceinline__ Piece piece_of(const PieceParams &p)
 {
@@ -106,15 +109,15 @@ __device__ __forceinline__ Piece piece_of(const PieceParams &p)
         else
             hi = mid - 1;
     }
-    x.beta = lo;
-    x.L = p.seq_len[lo];
-    const int nt = piece_tiles<kMode>(p, lo);
+    x.beta = row_at(p, lo);
+    x.L = p.seq_len[x.beta];
+    const int nt = piece_tiles<kMode>(p, x.beta);
     x.count = (nt + p.tiles - 1) / p.tiles;
     const int rel = c - p.first[lo];
     x.j = rel / x.count;
     x.index = rel - x.j * x.count;
-    x.seg = lo * p.g + x.j;
-    x.out_row = q_row_of<kMode>(p, lo);
+    x.seg = x.beta * p.g + x.j;
+    x.out_row = q_row_of<kMode>(p, x.beta);
     x.t0 = x.index * p.tiles;
     x.t1 = min(nt, x.t0 + p.tiles);
     return x;
@@ -664,16 +667,19 @@ __device__ void merge_rows(MergeShared<D> &sh, const PieceParams &p, const Piece
     }
 }
 
+// The segment of KV head k % g of the (k / g)-th row as they are laid out, whose records begin at *own0.
 template <int kMode>
-__device__ __forceinline__ Piece segment_of(const PieceParams &p, int seg)
+__device__ __forceinline__ Piece segment_of(const PieceParams &p, int k, size_t *own0)
 {
     Piece x;
-    x.seg = seg;
-    x.beta = seg / p.g;
-    x.j = seg - x.beta * p.g;
+    const int i = k / p.g;
+    x.beta = row_at(p, i);
+    x.j = k - i * p.g;
+    x.seg = x.beta * p.g + x.j;
     x.L = p.seq_len[x.beta];
     x.count = (piece_tiles<kMode>(p, x.beta) + p.tiles - 1) / p.tiles;
     x.out_row = q_row_of<kMode>(p, x.beta);
+    *own0 = static_cast<size_t>(p.first[i]) + static_cast<size_t>(x.j) * x.count;
     return x;
 }
 
@@ -682,8 +688,8 @@ __global__ void __launch_bounds__(kWide ? kMergeThreads : 128) merge_kernel(cons
 {
     extern __shared__ float s_w[];
     const int parts = kWide ? (p.G * D + 127) / 128 : 1, seg = static_cast<int>(blockIdx.x) / parts;
-    const Piece x = segment_of<kMode>(p, seg);
-    const size_t own0 = static_cast<size_t>(p.first[x.beta]) + static_cast<size_t>(x.j) * x.count;
+    size_t own0;
+    const Piece x = segment_of<kMode>(p, seg, &own0);
     const int n_pre = kMode == kPieceSuffix || kMode == kPieceGroups ? p.pre_n[x.beta] : 0;
     grid_dependency_wait();
     grid_dependents_launch();
@@ -715,8 +721,8 @@ __global__ void __launch_bounds__(kWeightThreads, 4)
     const int seg = static_cast<int>(blockIdx.x) / w.ctas, tid = static_cast<int>(threadIdx.x);
     const int parts = w.merge_ctas;
     const int part = static_cast<int>(blockIdx.x) - seg * w.ctas - parts;   // chunk of positions
-    const Piece x = segment_of<kPieceWeights>(p, seg);
-    const size_t rec0 = static_cast<size_t>(p.first[x.beta]) + static_cast<size_t>(x.j) * x.count;
+    size_t rec0;
+    const Piece x = segment_of<kPieceWeights>(p, seg, &rec0);
     const int G = p.G;
     if (part < 0) {
         if (w.wide)
@@ -726,7 +732,7 @@ __global__ void __launch_bounds__(kWeightThreads, 4)
         return;
     }
     const int u0 = part * w.chunk, u1 = min(u0 + w.chunk, w.max_seq);
-    const size_t row = static_cast<size_t>(seg) * w.max_seq;
+    const size_t row = static_cast<size_t>(x.seg) * w.max_seq;
     const float *sc = p.scores + (static_cast<size_t>(x.beta) * p.h + static_cast<size_t>(x.j) * G) * p.score_stride;
     constexpr int U = 4, B = 4;   // positions of a thread, and heads, at a time
     float s[B][U], before[U];
