@@ -282,7 +282,8 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
  * sequence beta attends to all of its prefix's positions and to positions 0 .. t of its prompt.  An owner layer
  * stores its prompt's K/V in c at positions [0, s_max); the prefix stays where it is, and mlkv_decode_attention_prefix
  * goes on from there.
- * prefix, prefix_of and prefix_lens as above, but prefix != c; the others and errors as for mlkv_prefill.
+ * prefix, prefix_of and prefix_lens as above, but prefix != c; the others and errors as for mlkv_prefill.  Short
+ * prompts are taken as rows of a decode, with scratch of c as above; where that cannot be had, without.
  */
 int mlkv_prefill_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix, const int *prefix_of,
                         const int *prefix_lens, const void *Q, const void *K, const void *V, void *out,

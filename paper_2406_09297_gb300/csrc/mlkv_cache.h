@@ -116,9 +116,17 @@ struct PrefixRows {
     uint16_t q_row[MLKV_MAX_BATCH], seq[MLKV_MAX_BATCH];
     int len[MLKV_MAX_BATCH], prefix[MLKV_MAX_BATCH];
 };
-// Issues the decode, with everything checked; or, with fits, only tells whether it is estimated to take less than
-// most_us.
+// What a decode of a prompt's rows has to do besides.
+struct PromptStep {
+    double most_us;      // the decode is issued if it is estimated to take less,
+    bool issued;         // which is told here, as is scratch that cannot be had: the prompt can do without
+    int (*store)(const PromptStep &step, cudaStream_t stream);   // in front of the launches, behind every check
+    mlkv_cache *c;       // the store's: K, V of s_max positions into the layer's slot, if they are to be stored
+    int layer, s_max;
+    const void *K, *V;
+};
+// Issues the decode, with everything checked and nothing queued on an error of a check.
 int decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const int *prefix_lens, const PrefixRows &rows,
-                const void *Q, void *out, cudaStream_t stream, double most_us = 0, bool *fits = nullptr);
+                const void *Q, void *out, cudaStream_t stream, PromptStep *step = nullptr);
 
 }  // namespace mlkv

@@ -1952,15 +1952,15 @@ static int prefill_as_rows(mlkv_cache_t c, int layer, mlkv_cache_t prefix, const
             rows.len[rows.n] = t + 1;
             rows.prefix[rows.n++] = prefix_of[beta];
         }
-    bool fits;
-    int rc = mlkv::decode_rows(c, layer, prefix, prefix_lens, rows, Q, out, stream, prefill_us - 2, &fits);
-    if (rc != MLKV_OK || !fits)
-        return rc;
-    if (c->owner[layer] == layer &&   // the rows read the slot
-        (rc = store_prefix(c, layer, K, V, s_max, stream, on_device(c, K) && on_device(c, V), false)) != MLKV_OK)
-        return rc;
-    *issued = true;
-    return mlkv::decode_rows(c, layer, prefix, prefix_lens, rows, Q, out, stream);
+    mlkv::PromptStep step = {prefill_us - 2, false, nullptr, c, layer, s_max, K, V};
+    if (c->owner[layer] == layer)   // the rows read the slot
+        step.store = [](const mlkv::PromptStep &st, cudaStream_t on) {
+            return store_prefix(st.c, st.layer, st.K, st.V, st.s_max, on,
+                                on_device(st.c, st.K) && on_device(st.c, st.V), false);
+        };
+    const int rc = mlkv::decode_rows(c, layer, prefix, prefix_lens, rows, Q, out, stream, &step);
+    *issued = step.issued;
+    return rc;
 }
 
 static int prefill_impl(mlkv_cache_t c, int layer, const void *Q, const void *K, const void *V,

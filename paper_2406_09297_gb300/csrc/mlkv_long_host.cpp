@@ -58,8 +58,7 @@ int prepare_pieces(mlkv_cache *c, int mode)
 // How the segments, nt(beta) tiles each, are cut into pieces: the least estimated time, in us.  A
 // launch takes 4.5, and what is longer of its bytes at the rate of HBM and its longest piece; pieces beyond one wave
 // of resident CTAs half a piece more where segments are split (whole ones end evenly enough).  Split segments
-// are merged by the CTA that ends last, a round trip to L2 for every 8 records, or by a launch of their own
-// of their own.  Never more pieces than there are records.  pre: records that every merge has besides; hbm_tiles:
+// are merged by the CTA that ends last, a round trip to L2 for every 8 records, or by a launch of their own.  Never more pieces than there are records.  pre: records that every merge has besides; hbm_tiles:
 // tiles that come from HBM, the others from L2 (14 TB/s, groups above 8 heads 10); -1: all.
 struct Cut {
     bool defer;
@@ -302,8 +301,7 @@ int mlkv::check_prefix(const mlkv_cache *c, const mlkv_cache *prefix, const int 
 }
 
 int mlkv::decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const int *prefix_lens,
-                      const PrefixRows &rows, const void *Q, void *out, cudaStream_t stream, double most_us,
-                      bool *fits)
+                      const PrefixRows &rows, const void *Q, void *out, cudaStream_t stream, PromptStep *step)
 {
     int rc = ::prepare_pieces(c, mlkv::kPieceSuffix);
     if (rc != MLKV_OK)
@@ -406,16 +404,26 @@ int mlkv::decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const 
     }
     const double apart_us = most_kt > 0 ? plan.us : 1e30;
     const bool grouped = grouped_us < std::min(apart_us, end_to_end.us);
-    if (fits != nullptr) {
-        *fits = std::min(apart_us, end_to_end.us) < most_us;   // (scattered: no groups)
+    if (step != nullptr && std::min(apart_us, end_to_end.us) >= step->most_us)   // (scattered: no groups)
         return MLKV_OK;
-    }
+    // Scratch that cannot be had: a prompt goes on without its rows.
+    const auto no_scratch = [&](int err) {
+        return step != nullptr && (err == MLKV_ERR_UNSUPPORTED || err == MLKV_ERR_OOM) ? MLKV_OK : err;
+    };
+    const auto begin = [&]() {
+        if (step == nullptr)
+            return MLKV_OK;
+        step->issued = true;
+        return step->store != nullptr ? step->store(*step, stream) : MLKV_OK;
+    };
     if (!grouped && end_to_end.us <= apart_us) {
         if ((rc = ::prepare_pieces(c, mlkv::kPieceJoined)) != MLKV_OK)
             return rc;
         p.prefix_b = prefix->b;
         lay_pieces(c, p, end_to_end, joined);
         if (rows.scattered && (rc = own_records(c, p, 0, stream)) != MLKV_OK)
+            return no_scratch(rc);
+        if ((rc = begin()) != MLKV_OK)
             return rc;
         return decode_pieces(c, mlkv::kPieceJoined, p, end_to_end, rows64(prefix), stream);
     }
@@ -462,7 +470,7 @@ int mlkv::decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const 
     lay_pieces(c, p, split, own);
     if ((rc = rows.scattered ? own_records(c, p, records * (c->d + 1), stream)
                              : scratch(c, records * (c->d + 1), "records of the shared prefix", stream)) != MLKV_OK)
-        return rc;
+        return no_scratch(rc);
     u.part = c->fused_part;
     u.part_lse = u.part + records * c->d;
     p.pre_o = u.part;
@@ -541,6 +549,8 @@ int mlkv::decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const 
     u.q_host = nullptr;
     u.prefix_b = np;
     std::memcpy(u.prompt_len, prefix_lens, sizeof(int) * np);
+    if ((rc = begin()) != MLKV_OK)
+        return rc;
     int n = 0;
     auto issue = [&]() {
         u.n_units = n;

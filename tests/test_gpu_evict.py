@@ -125,8 +125,6 @@ class _Memory:
 def test_evict(d, g, where):
     lens, cap = [1, 5, 64, 500, 1000, 1000, 777], 1000
     b = len(lens)
-    if where == "rows":   # rows in place, weights apart
-        test = "same"
     for keep, recent in ([3, 5, 64, 100, 1000, 999, 300], 2), ([1] * b, 0), ([700] * b, 700), ([130] * b, 5):
         torch.manual_seed(keep[0])
         w = torch.randn(b, g, cap, device="cuda").exp()

@@ -198,6 +198,39 @@ def test_scratch_does_not_grow_under_capture():
     assert torch.allclose(w.sum(-1), torch.full((b, g), h / g, device="cuda"), rtol=1e-4)
 
 
+def test_prompts_do_without_scratch_under_capture():
+    """Short prompts are rows of a decode, whose records lie in scratch; a first call of a captured stream takes none
+    and is the prefill's kernel, with its store."""
+    torch.manual_seed(0)
+    d, h, g, b, p = 64, 12, 1, 66, 2000
+    Q, out = _randn(b, 1, h, d), _randn(b, 1, h, d)
+    K, V, PK, PV = _randn(b, g, 1, d), _randn(b, g, 1, d), _randn(1, g, p, d), _randn(1, g, p, d)
+    step, own = _randn(b, h, d), _randn(b, h, d)
+    prefix = mlkv.MLKVCache(1, h, d, [0], g, 1, p)
+    prefix.load_prefix(0, PK, PV, p)
+    torch.cuda.synchronize()
+    got = []
+    for captured in (False, True):
+        cache = mlkv.MLKVCache(1, h, d, [0], g, b, 4)
+        call = lambda: cache.prefill_prefix(0, prefix, [0] * b, [p], Q, K, V, out, [1] * b)
+        if captured:
+            graph = torch.cuda.CUDAGraph()
+            torch.cuda.synchronize()
+            with torch.cuda.graph(graph):
+                call()
+            out.zero_()
+            graph.replay()
+        else:
+            call()
+        for i in (0, 31, 65):
+            _check(out[i, 0], Q[i, 0], torch.cat([PK[0, 0], K[i, 0]]), torch.cat([PV[0, 0], V[i, 0]]))
+        cache.decode_attention(0, step, own, [1] * b)   # what was stored
+        cache.sync_status()
+        got.append(own.clone())
+        assert torch.equal(own, V[:, 0].expand_as(own))
+    assert torch.equal(*got)
+
+
 def test_scratch_that_is_outgrown_lives_on():
     """A graph recorded over a smaller scratch replays after a larger call has replaced it."""
     torch.manual_seed(0)
