@@ -340,7 +340,7 @@ int mlkv_select_blocks(mlkv_cache_t c, int layer, const void *Q, const void *bou
  *             (-1, say) is passed over, one that comes twice counts twice; without any, outputs are zeros
  *   n_blocks  >= 1
  * The other arguments and errors as for mlkv_decode_attention (its options do not apply), and
- * MLKV_ERR_UNSUPPORTED for 2^31 listed blocks or more.
+ * MLKV_ERR_UNSUPPORTED for 2^30 listed blocks or more.
  */
 int mlkv_decode_attention_blocks(mlkv_cache_t c, int layer, const void *Q, void *out, const int *seq_lens,
                                  const int *blocks, int n_blocks, void *cuda_stream);
@@ -348,7 +348,7 @@ int mlkv_decode_attention_blocks(mlkv_cache_t c, int layer, const void *Q, void 
 /*
  * mlkv_decode_attention_weights - mlkv_decode_attention that also adds up what each position of each KV head
  * was given: weights_out[beta][j][u] = weights_in[beta][j][u] + the sum over the group's heads of their softmax
- * weight of position u < seq_lens[beta] (Eq. 2's alpha).  The layers of an owner's block add to the owner's
+ * weight of position u < seq_lens[beta] (Eq. 2's alpha; scores that are all -infinity give none).  The layers of an owner's block add to the owner's
  * weights one after the other.
  *
  *   weights_in   device fp32 [batch][g][max_seq], or NULL: zeros

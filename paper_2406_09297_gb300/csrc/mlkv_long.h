@@ -19,9 +19,9 @@ constexpr int kBlock = MLKV_BLOCK;
 enum : int {
     kPieceSuffix = 0,   // positions [0, seq_len), merged with a shared prefix's records
     kPieceBlocks = 1,   // the blocks listed for every (sequence, KV head)
-    kPieceGroups = 4,   // kPieceSuffix with units in front, each a chunk of a prefix's positions for a few sequences
-    kPieceJoined = 3,   // a prefix's positions, read for every sequence apart, and then [0, seq_len)
     kPieceWeights = 2,  // positions [0, seq_len); every score is stored, the merge left to weights_kernel
+    kPieceJoined = 3,   // a prefix's positions, read for every sequence apart, and then [0, seq_len)
+    kPieceGroups = 4,   // kPieceSuffix with units in front, each a chunk of a prefix's positions for a few sequences
 };
 
 constexpr int kPieceMaxUnits = 1024;
@@ -83,6 +83,7 @@ struct PieceParams {
     uint16_t unit_place[kPieceMaxUnits];
 };
 static_assert(sizeof(PieceParams) + 2 * sizeof(CUtensorMap) < 32764, "kernel parameters");
+
 // Tiles of a segment.
 template <int kMode>
 __host__ __device__ inline int piece_tiles(const PieceParams &p, int beta)

@@ -709,7 +709,7 @@ int mlkv_decode_attention_blocks(mlkv_cache_t c, int layer, const void *Q, void 
     const size_t segments = static_cast<size_t>(c->b) * c->g;
     if (overlap(blocks, segments * n_blocks * 4, out, query_bytes(c)))
         return fail(MLKV_ERR_INVALID_ARG, "out overlaps blocks");
-    if (segments * static_cast<size_t>(n_blocks) > 0x7fffffffu)
+    if (segments * static_cast<size_t>(n_blocks) >= 1u << 30)   // (sums of two stay within int32)
         return fail(MLKV_ERR_UNSUPPORTED, "%zu listed blocks exceed the int32 indices", segments * n_blocks);
     DeviceGuard guard(c->device);
     if ((rc = prepare_pieces(c, mlkv::kPieceBlocks)) != MLKV_OK)

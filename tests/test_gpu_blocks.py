@@ -316,3 +316,7 @@ def test_rejections():
             (dict(layer=2), BAD), (dict(Q=None), BAD), (dict(out=None), BAD), (dict(out=Q), BAD),
             (dict(blocks=blocks[:, :, :0]), BAD), (dict(blocks=blocks.float()), BAD),
             (dict(blocks=blocks[:, :1]), BAD), (dict(seq_lens=[201]), RANGE))
+    many = torch.empty((1, g, 2 ** 29), dtype=torch.int32, device="cuda")
+    with pytest.raises(mlkv.MLKVError) as e:
+        cache.decode_attention_blocks(1, Q, out, [cap], many)
+    assert e.value.code == mlkv.MLKV_ERR_UNSUPPORTED

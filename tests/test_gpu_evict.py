@@ -70,6 +70,22 @@ def test_weights_long(d, h, g, lens):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_weights_of_scores_that_are_all_minus_infinity(d):
+    """KV head 0 has no finite score: zeros, and no weight."""
+    n, cap = 70, 200
+    cache = mlkv.MLKVCache(1, 4, d, [0], 2, 1, cap)
+    K, V, Q = torch.zeros(1, 2, cap, d).bfloat16().cuda(), _randn(1, 2, cap, d), torch.zeros(1, 4, d).bfloat16().cuda()
+    K[0, 0, :, 0] = -math.inf
+    Q[0, :, 0] = 1
+    cache.load_prefix(0, K, V, cap)
+    out, w = torch.full_like(Q, 9.0), torch.full((1, 2, cap), 7.0, device="cuda")
+    cache.decode_attention_weights(0, Q, out, [n], None, w)
+    cache.sync_status()
+    assert (out[0, :2] == 0).all() and (w[0, 0] == 0).all()
+    assert torch.allclose(w[0, 1, :n], torch.full((n,), 2 / n, device="cuda"), rtol=1e-5) and (w[0, 1, n:] == 0).all()
+
+
 def _evict(d, h, g, lens, cap, keep, recent, w, where="same", cap_to=None, seed=0, owners=(0, 0)):
     torch.manual_seed(seed)
     b = len(lens)

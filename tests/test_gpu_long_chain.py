@@ -306,3 +306,70 @@ def test_what_ran_before_shares_the_scratch():
         cache.decode_attention_weights(0, Q[0], o, lens, None, w)
     cache.sync_status()
     assert torch.equal(out, want) and torch.equal(w, want_w)
+
+
+def test_offsets_beyond_32_bits():
+    """Two caches of 2.4e9 elements a side; what is asked for lies in the last sequence."""
+    torch.manual_seed(0)
+    d, h, g, b, cap = 128, 16, 8, 9, 262144
+    G, i, n = h // g, b - 1, cap - 44
+    lens = [70] * i + [n]
+    K = torch.empty(b, g, cap, d, dtype=torch.bfloat16, device="cuda").normal_()
+    V = torch.empty_like(K).normal_()
+    cache, other = (mlkv.MLKVCache(1, h, d, [0], g, b, cap) for _ in range(2))
+    cache.load_prefix(0, K, V, cap)
+    Q, out = _randn(b, h, d), _randn(b, h, d)
+
+    def check(to, k, v, j):
+        _check(to[j * G:(j + 1) * G], Q[i, j * G:(j + 1) * G], k, v)
+
+    # behind its positions as a prefix
+    small = mlkv.MLKVCache(1, h, d, [0], g, 2, 64)
+    own = _randn(2, g, 64, d)
+    small.load_prefix(0, own, own, 64)
+    two = _randn(2, h, d)
+    small.decode_attention_prefix(0, cache, [i, -1], lens, Q[i - 1:].contiguous(), two, [5, 64])
+    for j in (0, 7):
+        q = Q[i - 1, j * G:(j + 1) * G]
+        _check(two[0, j * G:(j + 1) * G], q, torch.cat([K[i, j, :n], own[0, j, :5]]), torch.cat([V[i, j, :n], own[0, j, :5]]))
+    # blocks
+    blk = (cap + 63) // 64
+    bounds = torch.zeros(b, g, blk, 2, d, dtype=torch.int8, device="cuda")
+    scales = torch.zeros(b, g, blk, device="cuda")
+    blocks = torch.zeros(b, g, 50, dtype=torch.int32, device="cuda")
+    cache.block_bounds(0, lens, bounds, scales)
+    cache.select_blocks(0, Q, bounds, scales, lens, blocks, 1, 2)
+    cache.decode_attention_blocks(0, Q, out, lens, blocks)
+    last = (n + 63) // 64 - 1
+    for j in (0, 7):
+        for u in (0, 1000, last):
+            k = K[i, j, 64 * u:min(n, 64 * u + 64)].float()
+            assert scales[i, j, u] == 2.0 ** math.ceil(math.log2(float(k.abs().max()) / 127))
+            assert torch.equal(bounds[i, j, u, 0].float(), (k.amin(0) / scales[i, j, u]).floor())
+            assert torch.equal(bounds[i, j, u, 1].float(), (k.amax(0) / scales[i, j, u]).ceil())
+        took = blocks[i, j].tolist()
+        assert took == sorted(set(took)) and took[0] == 0 and took[-2:] == [last - 1, last]
+        pos = [u for x in took for u in range(64 * x, min(n, 64 * x + 64))]
+        check(out[i], K[i, j, pos], V[i, j, pos], j)
+    # weights, and eviction to another cache and in place
+    w, after = torch.zeros(b, g, cap, device="cuda"), torch.zeros(b, g, cap, device="cuda")
+    cache.decode_attention_weights(0, Q, out, lens, None, w)
+    kept = torch.zeros(b, g, 200000, dtype=torch.int32, device="cuda")
+    keep = [100] * i + [200000]   # (all there are of the short ones)
+    cache.evict(0, w, after, lens, keep, 100, kept, other)
+    for j in (0, 7):
+        check(out[i], K[i, j, :n], V[i, j, :n], j)
+        assert abs(float(w[i, j, :n].double().sum()) - G) < 1e-3
+        order = torch.sort(w[i, j, :n - 100], descending=True, stable=True).indices[:200000 - 100]
+        want = torch.cat([order.sort().values, torch.arange(n - 100, n, device="cuda")])
+        assert torch.equal(kept[i, j].long(), want)
+        assert torch.equal(after[i, j, :200000], w[i, j, want]) and not after[i, j, 200000:].any()
+    again = kept.clone().zero_()
+    cache.evict(0, w, w, lens, keep, 100, again)
+    assert torch.equal(again, kept) and torch.equal(w, after)
+    for c in (other, cache):
+        c.decode_attention(0, Q, out, [70] * i + [200000])
+        for j in (0, 7):
+            at = kept[i, j].long()
+            check(out[i], K[i, j, at], V[i, j, at], j)
+        c.sync_status()
