@@ -36,24 +36,22 @@ __device__ __forceinline__ float inverse_power(float s)   // of a power of two
     return __uint_as_float((254u << 23) - __float_as_uint(s));
 }
 
-constexpr int kBoundsThreads = 256;
-constexpr int kBoundsBlocks = 4;   // of a CTA
+constexpr int kBoundsThreads = 128;
+constexpr int kBoundsCtas = 5;     // an SM
 
-// A CTA is four blocks of one KV head, 128 threads a block, two after one another, all rows on the way at once; 16 bytes
-// a load, D / 8 lanes a row; minima and maxima two channels at a time, across a warp's rows by shuffles, across the
-// warps in shared memory.  Bound by the keys' bytes: 8 uneven sequences of up to 16,000 positions, 8 KV heads of 128, 128 MB,
-// 23 to 25 us, 5.4 TB/s, CTAs of 4096 rows' loads that start and end one after the other.  (A CTA a block: 27 us.)
+// A warp has a block at a time, half a block of 128 channels on the way at once: 16 bytes a load, D / 8 lanes a row.
+// Minima and maxima two channels at a time, NaNs kept, so that the largest magnitude is found among them at the end;
+// across rows by shuffles, without shared memory or barriers.  Bound by the keys' bytes: 8 uneven
+// sequences of up to 16,000 positions, 8 KV heads of 128, 218 MB, 34.3 us, 6.35 TB/s; 16 of 131,072, one KV head of 64,
+// 268 MB, 40.7 us.  (Four warps a block, two blocks after one another, sums through shared memory: 34.9 and 48.7 us.)
 template <int D>
-__global__ void __launch_bounds__(kBoundsThreads, 3) bounds_kernel(const __grid_constant__ BoundsParams p)
+__global__ void __launch_bounds__(kBoundsThreads, kBoundsCtas) bounds_kernel(const __grid_constant__ BoundsParams p)
 {
     constexpr int C = D / 8;                     // 16-byte columns of a row
-    constexpr int RG = 128 / C;                  // rows at a time
-    constexpr int N = kBlock / RG;               // rows of a thread
-    constexpr int W = 4;                         // warps of a block
-    __shared__ __align__(16) __nv_bfloat16 s_lo[2][W][D], s_hi[2][W][D];
-    __shared__ float s_max[2][W];
-    const int half = static_cast<int>(threadIdx.x) >> 7, tid = static_cast<int>(threadIdx.x) & 127;
-    const int warp = tid >> 5, lane = tid & 31;
+    constexpr int R = 32 / C;                    // rows of a warp's load
+    constexpr int N = 16;                        // loads on the way
+    constexpr int W = kBoundsThreads / 32;
+    const int warp = static_cast<int>(threadIdx.x) >> 5, lane = static_cast<int>(threadIdx.x) & 31;
     // the sequence whose CTAs these are
     int beta = 0, above = p.b - 1;
     while (beta < above) {
@@ -63,98 +61,70 @@ __global__ void __launch_bounds__(kBoundsThreads, 3) bounds_kernel(const __grid_
         else
             above = mid - 1;
     }
-    const int L = p.seq_len[beta], blk0 = p.first[beta] / kBlock, n_blk = (L + kBlock - 1) / kBlock - blk0;
-    const int ctas = (n_blk + kBoundsBlocks - 1) / kBoundsBlocks;   // of a KV head
+    const int L = p.seq_len[beta], blk0 = p.first[beta] / kBlock, n_blk = (L + kBlock - 1) / kBlock;
+    const int ctas = (n_blk - blk0 + p.per_cta - 1) / p.per_cta;   // of a KV head
     const int rel = static_cast<int>(blockIdx.x) - p.start[beta];
-    const int j = rel / ctas, at0 = blk0 + (rel - j * ctas) * kBoundsBlocks + half;
-    const int seg = beta * p.g + j;
-    const int col = tid % C, r0 = tid / C;
+    const int j = rel / ctas, at0 = blk0 + (rel - j * ctas) * p.per_cta;
+    const size_t seg = static_cast<size_t>(beta) * p.g + j;
+    const int col = lane % C, r0 = lane / C;
     grid_dependency_wait();
     grid_dependents_launch();
-    uint4 v[2][N];
-    int n[2];
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-        const int blk = at0 + 2 * q;
-        n[q] = min(kBlock, L - blk * kBlock);   // visible positions, none or less: no such block
+    for (int blk = at0 + warp; blk < min(n_blk, at0 + p.per_cta); blk += W) {
+        const int n = min(kBlock, L - blk * kBlock);   // visible positions
         const uint4 *k = reinterpret_cast<const uint4 *>(
-                             p.K + (static_cast<size_t>(seg) * p.max_seq + static_cast<size_t>(blk) * kBlock) * D) + col;
-        if (n[q] > 0)
+                             p.K + (seg * p.max_seq + static_cast<size_t>(blk) * kBlock) * D) + col;
+        __nv_bfloat162 lo[4], hi[4];
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                v[q][i] = k[static_cast<size_t>(min(r0 + i * RG, n[q] - 1)) * C];   // (a row twice changes nothing)
-    }
-    auto other = [](__nv_bfloat162 x, int s) {
-        const uint32_t u = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t *>(&x), s);
-        return *reinterpret_cast<const __nv_bfloat162 *>(&u);
-    };
+        for (int half = 0; half < kBlock / (N * R); ++half) {
+            uint4 v[N];
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-        if (q > 0)
-            __syncthreads();   // the first block's reduction is read
-        if (n[q] > 0) {
-            __nv_bfloat162 lo[4], hi[4], amax = __habs2(reinterpret_cast<const __nv_bfloat162 *>(&v[q][0])[0]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                lo[e] = hi[e] = reinterpret_cast<const __nv_bfloat162 *>(&v[q][0])[e];
+            for (int i = 0; i < N; ++i)   // (a row twice changes nothing)
+                v[i] = k[static_cast<size_t>(min(r0 + (half * N + i) * R, n - 1)) * C];
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const __nv_bfloat162 *x = reinterpret_cast<const __nv_bfloat162 *>(&v[q][i]);
+                const __nv_bfloat162 *x = reinterpret_cast<const __nv_bfloat162 *>(&v[i]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    lo[e] = __hmin2(lo[e], x[e]);
-                    hi[e] = __hmax2(hi[e], x[e]);
-                    amax = __hmax2_nan(amax, __habs2(x[e]));   // (a NaN stays)
+                    lo[e] = half + i == 0 ? x[e] : __hmin2_nan(lo[e], x[e]);
+                    hi[e] = half + i == 0 ? x[e] : __hmax2_nan(hi[e], x[e]);
                 }
-            }
-#pragma unroll
-            for (int s = C; s < 32; s <<= 1)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    lo[e] = __hmin2(lo[e], other(lo[e], s));
-                    hi[e] = __hmax2(hi[e], other(hi[e], s));
-                }
-#pragma unroll
-            for (int s = 1; s < 32; s <<= 1)
-                amax = __hmax2_nan(amax, other(amax, s));
-            if (lane < C) {
-                *reinterpret_cast<uint4 *>(&s_lo[half][warp][col * 8]) = *reinterpret_cast<const uint4 *>(lo);
-                *reinterpret_cast<uint4 *>(&s_hi[half][warp][col * 8]) = *reinterpret_cast<const uint4 *>(hi);
-            }
-            if (lane == 0) {
-                const float a = __low2float(amax), b = __high2float(amax);
-                s_max[half][warp] = a != a || b != b ? __int_as_float(0x7f800000) : fmaxf(a, b);
             }
         }
-        __syncthreads();
-        if (n[q] <= 0)
-            continue;
-        float most = 0.f;
+        auto other = [](__nv_bfloat162 x, int s) {
+            const uint32_t u = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t *>(&x), s);
+            return *reinterpret_cast<const __nv_bfloat162 *>(&u);
+        };
 #pragma unroll
-        for (int w = 0; w < W; ++w)
-            most = fmaxf(most, s_max[half][w]);
-        const bool unknown = !(most <= kLargest);
-        const float scale = unknown ? __int_as_float(0x7f800000) : scale_of(most);
-        const size_t at = static_cast<size_t>(seg) * p.n_blocks + at0 + 2 * q;
-        // four channels a thread: their least, then their largest codes
-        if (tid < D / 2) {
-            const bool upper = tid >= D / 4;
-            const int c = (upper ? tid - D / 4 : tid) * 4;
-            const float inv = unknown ? 0.f : inverse_power(scale);   // exact quotients
-            uint32_t codes = 0;
+        for (int s = C; s < 32; s <<= 1)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                __nv_bfloat16 x = upper ? s_hi[half][0][c + e] : s_lo[half][0][c + e];
-#pragma unroll
-                for (int w = 1; w < W; ++w)
-                    x = upper ? __hmax(x, s_hi[half][w][c + e]) : __hmin(x, s_lo[half][w][c + e]);
-                const float y = __bfloat162float(x) * inv;
-                const int code = unknown ? (upper ? 127 : -127) : static_cast<int>(upper ? ceilf(y) : floorf(y));
-                codes |= (static_cast<uint32_t>(code) & 255u) << (8 * e);
+                lo[e] = __hmin2_nan(lo[e], other(lo[e], s));
+                hi[e] = __hmax2_nan(hi[e], other(hi[e], s));
             }
-            *reinterpret_cast<uint32_t *>(p.bounds + at * 2 * D + (upper ? D : 0) + c) = codes;
+        __nv_bfloat162 amax = __habs2(lo[0]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            amax = __hmax2_nan(amax, __hmax2_nan(__habs2(lo[e]), __habs2(hi[e])));
+        // (as whole numbers, the bits of magnitudes are in their order, NaN last)
+        const uint32_t bits = *reinterpret_cast<const uint32_t *>(&amax);
+        const float most = __uint_as_float(__reduce_max_sync(0xffffffffu, max(bits << 16, bits & 0xffff0000u)));
+        const bool unknown = !(most <= kLargest);
+        const float scale = unknown ? __int_as_float(0x7f800000) : scale_of(most);
+        const size_t at = seg * p.n_blocks + blk;
+        // eight channels a lane: the first row's lanes their least codes, the second row's their largest, as -floor(-y)
+        if (r0 < 2) {
+            const float inv = (unknown ? 0.f : inverse_power(scale)) * (r0 == 1 ? -1.f : 1.f);   // exact quotients
+            uint32_t codes[2] = {0u, 0u};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float2 y = __bfloat1622float2(r0 == 1 ? hi[e] : lo[e]);
+                const int a = unknown ? -127 : __float2int_rd(y.x * inv), b = unknown ? -127 : __float2int_rd(y.y * inv);
+                codes[e / 2] |= ((static_cast<uint32_t>(r0 == 1 ? -a : a) & 255u) |
+                                 ((static_cast<uint32_t>(r0 == 1 ? -b : b) & 255u) << 8)) << (16 * (e % 2));
+            }
+            *reinterpret_cast<uint2 *>(p.bounds + at * 2 * D + r0 * D + col * 8) = make_uint2(codes[0], codes[1]);
         }
-        if (tid == 0)
+        if (lane == 0)
             p.scales[at] = scale;
     }
 }
@@ -313,7 +283,13 @@ const void *select_fn()
 
 }  // namespace
 
-int bounds_ctas(int n_blocks) { return (n_blocks + kBoundsBlocks - 1) / kBoundsBlocks; }
+// Blocks of a CTA: one a warp if the GPU holds them all at once, else two, which spares CTAs' starts (480 blocks of 64
+// channels 2.9 us, 3.3 with two a warp).
+int bounds_per_cta(long long blocks, int sm_count)
+{
+    constexpr int W = kBoundsThreads / 32;
+    return blocks <= static_cast<long long>(W) * kBoundsCtas * sm_count ? W : 2 * W;
+}
 
 cudaError_t launch_bounds(int head_dim, const BoundsParams &p, cudaStream_t stream)
 {

@@ -131,9 +131,10 @@ struct BoundsParams {
     int b, g, max_seq, n_blocks;
     int seq_len[MLKV_MAX_BATCH];
     int first[MLKV_MAX_BATCH]; // first position that is new
-    int start[MLKV_MAX_BATCH + 1];   // first CTA of a sequence, bounds_ctas a KV head
+    int per_cta;                     // blocks of a CTA
+    int start[MLKV_MAX_BATCH + 1];   // first CTA of a sequence
 };
-int bounds_ctas(int n_blocks);   // of a KV head with n_blocks new blocks
+int bounds_per_cta(long long blocks, int sm_count);
 cudaError_t launch_bounds(int head_dim, const BoundsParams &p, cudaStream_t stream);
 
 struct SelectParams {

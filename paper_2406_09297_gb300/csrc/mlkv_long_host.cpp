@@ -618,15 +618,20 @@ int mlkv_block_bounds(mlkv_cache_t c, int layer, const int *first, const int *se
     const size_t blocks = static_cast<size_t>(c->b) * c->g * p.n_blocks;
     if (overlap(bounds, blocks * 2 * c->d, scales, blocks * 4))
         return fail(MLKV_ERR_INVALID_ARG, "bounds overlap scales");
-    long long ctas = 0;
+    long long ctas = 0, total = 0;
     for (int beta = 0; beta < c->b; ++beta) {
         const int f = first != nullptr ? first[beta] : 0;
         if (f < 0 || f > seq_lens[beta])
             return fail(MLKV_ERR_RANGE, "first[%d] = %d outside [0, %d]", beta, f, seq_lens[beta]);
         p.seq_len[beta] = seq_lens[beta];
         p.first[beta] = f;
+        total += static_cast<long long>(c->g) * ((seq_lens[beta] + 63) / 64 - f / 64);
+    }
+    p.per_cta = mlkv::bounds_per_cta(total, c->sm_count);
+    for (int beta = 0; beta < c->b; ++beta) {
         p.start[beta] = static_cast<int>(std::min(ctas, 0x7fffffffLL));
-        ctas += static_cast<long long>(c->g) * mlkv::bounds_ctas((seq_lens[beta] + 63) / 64 - f / 64);
+        ctas += static_cast<long long>(c->g) *
+                (((seq_lens[beta] + 63) / 64 - p.first[beta] / 64 + p.per_cta - 1) / p.per_cta);
     }
     if (ctas == 0)
         return MLKV_OK;
