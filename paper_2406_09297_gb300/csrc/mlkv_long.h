@@ -8,6 +8,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "mlkv_internal.h"
 
 namespace mlkv {
@@ -27,8 +29,9 @@ enum : int {
 constexpr int kPieceMaxUnits = 1024;
 
 // Decode attention of one layer in pieces: a segment (sequence, KV head) of nt tiles of 64 positions is cut
-// into pieces of `tiles` tiles, a CTA each.  Passed by value.
-struct PieceParams {
+// into pieces of `tiles` tiles, a CTA each.  Passed by value, each mode its part (PieceArgs): 16 KB more of them cost
+// the host 0.2 us a launch.
+struct PieceBase {
     const __nv_bfloat16 *Q;   // [b][h][D]
     __nv_bfloat16 *out;       // [b][h][D]
     float *part_o;            // [pieces][G][D]  normalised outputs of pieces
@@ -59,7 +62,11 @@ struct PieceParams {
     int ordered;                          // rows are laid out as order lists them, the longest first; 0: as they are
     uint16_t order[MLKV_MAX_BATCH];
     int first[MLKV_MAX_BATCH + 1];        // first piece of the i-th row in that order (KV head after KV head inside)
-    int seq_len[MLKV_MAX_BATCH];          // (this and what follows by row) positions that the row sees
+    int seq_len[MLKV_MAX_BATCH];          // positions that a row sees
+};
+// What runs over prefixes; arrays by row.
+struct PiecePrefix : PieceBase {
+    int prefix_b;                         // kPieceJoined, kPieceGroups: sequences of the prefix cache
     union {
         struct {
             uint16_t q_row[MLKV_MAX_BATCH], seq[MLKV_MAX_BATCH];   // scattered
@@ -75,7 +82,9 @@ struct PieceParams {
         };
         int pre_len[MLKV_MAX_BATCH];      // kPieceJoined: positions of its prefix, 0: none
     };
-    int prefix_b;                         // kPieceJoined, kPieceGroups: sequences of the prefix cache
+};
+// And what has units.
+struct PieceParams : PiecePrefix {
     // kPieceGroups: units, the launch's first CTAs: unit_tiles tiles from unit_tiles * chunk on of a prefix, for the
     // heads of KV head j of up to 16 / G rows from a place on.
     int n_units, unit_tiles;
@@ -83,17 +92,21 @@ struct PieceParams {
     uint16_t unit_place[kPieceMaxUnits];
 };
 static_assert(sizeof(PieceParams) + 2 * sizeof(CUtensorMap) < 32764, "kernel parameters");
+template <int kMode>
+using PieceArgs = std::conditional_t<kMode == kPieceGroups, PieceParams,
+                                     std::conditional_t<kMode == kPieceSuffix || kMode == kPieceJoined, PiecePrefix,
+                                                        PieceBase>>;
 
 // Tiles of a segment.
 template <int kMode>
-__host__ __device__ inline int piece_tiles(const PieceParams &p, int beta)
+__host__ __device__ inline int piece_tiles(const PieceArgs<kMode> &p, int beta)
 {
-    if (kMode == kPieceBlocks)
+    if constexpr (kMode == kPieceBlocks)
         return p.n_blocks;
     const int own = static_cast<int>((static_cast<unsigned>(p.seq_len[beta]) + kBlock - 1) / kBlock);
-    return kMode == kPieceJoined
-               ? static_cast<int>((static_cast<unsigned>(p.pre_len[beta]) + kBlock - 1) / kBlock) + own
-               : own;
+    if constexpr (kMode == kPieceJoined)
+        return static_cast<int>((static_cast<unsigned>(p.pre_len[beta]) + kBlock - 1) / kBlock) + own;
+    return own;
 }
 // Most records (pieces and a prefix's) that a segment's merge holds the weights of.
 int piece_max_records(int head_dim, int group);

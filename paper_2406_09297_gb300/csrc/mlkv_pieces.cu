@@ -65,27 +65,47 @@ struct Piece {
 // Row of Q and out, and sequence, of a query row.
 // (only what runs over prefixes has scattered rows, kPieceGroups none)
 template <int kMode>
-__device__ __forceinline__ int q_row_of(const PieceParams &p, int i)
+__device__ __forceinline__ int q_row_of(const PieceArgs<kMode> &p, int i)
 {
-    return (kMode == kPieceSuffix || kMode == kPieceJoined) && p.scattered ? p.q_row[i] : i;
+    if constexpr (kMode == kPieceSuffix || kMode == kPieceJoined)
+        return p.scattered ? p.q_row[i] : i;
+    return i;
 }
 template <int kMode>
-__device__ __forceinline__ int row_seq(const PieceParams &p, int i)
+__device__ __forceinline__ int row_seq(const PieceArgs<kMode> &p, int i)
 {
-    return (kMode == kPieceSuffix || kMode == kPieceJoined) && p.scattered ? p.seq[i] : i;
+    if constexpr (kMode == kPieceSuffix || kMode == kPieceJoined)
+        return p.scattered ? p.seq[i] : i;
+    return i;
 }
 
 // The i-th row as the pieces are laid out.
-__device__ __forceinline__ int row_at(const PieceParams &p, int i) { return p.ordered ? p.order[i] : i; }
+__device__ __forceinline__ int row_at(const PieceBase &p, int i) { return p.ordered ? p.order[i] : i; }
+
+// The records of the prefix that the row merges, and their first one for KV head j.
+template <int kMode>
+__device__ __forceinline__ int prefix_records(const PieceArgs<kMode> &p, int i)
+{
+    if constexpr (kMode == kPieceSuffix || kMode == kPieceGroups)
+        return p.pre_n[i];
+    return 0;
+}
+template <int kMode>
+__device__ __forceinline__ size_t prefix_record(const PieceArgs<kMode> &p, int i, int j)
+{
+    if constexpr (kMode == kPieceSuffix || kMode == kPieceGroups)
+        return p.pre_n[i] > 0 ? (static_cast<size_t>(p.pre_place[i]) * p.g + j) * p.pre_chunks : 0;
+    return 0;
+}
 
 template <int kMode>
-__device__ __forceinline__ Piece piece_of(const PieceParams &p)
+__device__ __forceinline__ Piece piece_of(const PieceArgs<kMode> &p)
 {
     Piece x;
     x.unit = x.place = x.prefix = x.chunk = 0;
     x.rows = p.G;
     int c = static_cast<int>(blockIdx.x);
-    if (kMode == kPieceGroups) {
+    if constexpr (kMode == kPieceGroups) {
         if (c < p.n_units) {
             const uint32_t u = p.units[c];
             x.unit = 1;
@@ -125,15 +145,13 @@ __device__ __forceinline__ Piece piece_of(const PieceParams &p)
     return x;
 }
 
-// Merges the segment's records (its own pieces', from own0 on, then the prefix's n_pre) into out: the weights
+// Merges the segment's records (its own pieces', from own0 on, then the prefix's n_pre from pre0 on) into out: the weights
 // first, then the sums in the records' order.  s_w: room for a row of G floats a record, and one more.
 template <int D>
-__device__ void merge_records(const PieceParams &p, const Piece &x, size_t own0, int n_pre, float *s_w,
+__device__ void merge_records(const PieceBase &p, const Piece &x, size_t own0, int n_pre, size_t pre0, float *s_w,
                               int tid, int n_threads)
 {
     const int G = p.G, n_own = x.count, n = n_own + n_pre;
-    const size_t pre0 =
-        n_pre > 0 ? (static_cast<size_t>(p.pre_place[x.beta]) * p.g + x.j) * p.pre_chunks : 0;
     for (int i = tid; i < n * G; i += n_threads)
         s_w[i] = i < n_own * G ? __ldcg(p.part_lse + own0 * G + i)
                                : __ldcg(p.pre_lse + pre0 * G + (i - n_own * G));
@@ -192,7 +210,7 @@ __device__ void merge_records(const PieceParams &p, const Piece &x, size_t own0,
 template <int D, int kMode, int NH>
 __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     piece_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap tmap_prefix,
-                 const __grid_constant__ PieceParams p)
+                 const __grid_constant__ PieceArgs<kMode> p)
 {
     using PL = PiecePlan<D>;
     constexpr int S = PL::kStages, kWarps = PL::kWarps;
@@ -220,7 +238,10 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     const Piece x = piece_of<kMode>(p);
     const int *list = kMode == kPieceBlocks ? p.blocks + static_cast<size_t>(x.seg) * p.n_blocks : nullptr;
     // (kPieceJoined: the prefix's tiles come first, then the sequence's own)
-    const int pre_len = kMode == kPieceJoined ? p.pre_len[x.beta] : 0, n_joined = (pre_len + T - 1) / T;
+    int pre_len = 0;
+    if constexpr (kMode == kPieceJoined)
+        pre_len = p.pre_len[x.beta];
+    const int n_joined = (pre_len + T - 1) / T;
     // Block of tile t, or -1: none (kPieceBlocks); 32 of a list at a time, a lane each.
     int listed = -1, listed_at = -1;
     auto block_of = [&](int t) {
@@ -240,10 +261,12 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
         asm volatile("bar.arrive 2, %0;" ::"n"(PL::kThreads) : "memory");
         // ------------------------------------ producer ------------------------------------------
         const int zk = ((p.slot * 2 + 0) * p.b + row_seq<kMode>(p, x.beta)) * p.g + x.j, zv = zk + p.b * p.g;
-        const int zk_pre = kMode == kPieceJoined || group
-                               ? (p.slot * 2 * p.prefix_b +
-                                  (group ? x.prefix : static_cast<int>(p.pre_place[x.beta]))) * p.g + x.j
-                               : 0;
+        int zk_pre = 0, zv_pre = 0;
+        if constexpr (kMode == kPieceJoined || kMode == kPieceGroups) {
+            zk_pre = (p.slot * 2 * p.prefix_b +
+                      (group ? x.prefix : static_cast<int>(p.pre_place[x.beta]))) * p.g + x.j;
+            zv_pre = zk_pre + p.prefix_b * p.g;
+        }
         int idx = 0;
         for (int t = x.t0; t < x.t1; ++t) {
             const int blk = block_of(t);
@@ -268,7 +291,7 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
 #pragma unroll
                     for (int sub = 0; sub < D / 64; ++sub)
                         tma_load_3d(dst + PL::kTile + sub * T * 128, map, fb, sub * 64, blk * T,
-                                    pre ? zk_pre + p.prefix_b * p.g : zv);
+                                    pre ? zv_pre : zv);
                 }
             }
             if (!__shfl_sync(0xffffffffu, ok, 0))
@@ -295,10 +318,11 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
         for (int nh = 0; nh < NH; ++nh) {
             const int head = nh * 8 + (lane >> 2);   // of the tile's rows
             int row = q_row_of<kMode>(p, x.beta), at = head;
-            if (group && x.unit && head < x.rows) {
-                row = p.place_row[x.place + head / p.G];
-                at = head % p.G;
-            }
+            if constexpr (kMode == kPieceGroups)
+                if (x.unit && head < x.rows) {
+                    row = p.place_row[x.place + head / p.G];
+                    at = head % p.G;
+                }
             const __nv_bfloat16 *q =
                 p.Q + (static_cast<size_t>(row) * p.h + static_cast<size_t>(x.j) * p.G + at) * D + (lane & 3) * 2;
 #pragma unroll
@@ -506,10 +530,12 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
         return;
     if (early && (!p.defer || blockIdx.x == gridDim.x - 1))
         grid_dependency_wait();   // (deferred merge: one CTA, so that this grid ends behind the prefix's)
-    const int n_pre = kMode == kPieceSuffix || kMode == kPieceGroups ? p.pre_n[x.beta] : 0;
+    const int n_pre = prefix_records<kMode>(p, x.beta);
     const bool defer = kMode == kPieceWeights || group || p.defer;
     const bool whole = !defer && x.count == 1 && n_pre == 0;
-    const size_t rec = group ? blockIdx.x - static_cast<unsigned>(p.n_units) : blockIdx.x;
+    size_t rec = blockIdx.x;
+    if constexpr (kMode == kPieceGroups)
+        rec -= static_cast<unsigned>(p.n_units);   // (of a unit not used)
     __nv_bfloat16 *ob = p.out + (static_cast<size_t>(q_row_of<kMode>(p, x.beta)) * p.h + static_cast<size_t>(x.j) * p.G) * D;
     for (int i = tid * 4; i < x.rows * D; i += kWarps * 32 * 4) {
         const int row = i / D, ch = i - row * D;
@@ -574,7 +600,8 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
         __threadfence_block();
         consumer_bar_sync<kWarps>();
     }
-    merge_records<D>(p, x, rec - x.index, n_pre, reinterpret_cast<float *>(smem), tid, kWarps * 32);
+    merge_records<D>(p, x, rec - x.index, n_pre, prefix_record<kMode>(p, x.beta, x.j), reinterpret_cast<float *>(smem),
+                     tid, kWarps * 32);
 }
 
 // The merge of many records by CTAs of their own, 128 floats each: a head of 128 channels or two of 64.  The
@@ -591,13 +618,11 @@ struct MergeShared {
     float4 sum[kMergeThreads / 32][32];
 };
 template <int D>
-__device__ void merge_rows(MergeShared<D> &sh, const PieceParams &p, const Piece &x, size_t own0, int n_pre, int part,
-                           float *s_w)
+__device__ void merge_rows(MergeShared<D> &sh, const PieceBase &p, const Piece &x, size_t own0, int n_pre, size_t pre0,
+                           int part, float *s_w)
 {
     constexpr int R = MergeShared<D>::kRows, W = kMergeThreads / 32, U = 8;
     const int G = p.G, n = x.count + n_pre, tid = static_cast<int>(threadIdx.x), warp = tid >> 5, lane = tid & 31;
-    const size_t pre0 =
-        n_pre > 0 ? (static_cast<size_t>(p.pre_place[x.beta]) * p.g + x.j) * p.pre_chunks : 0;
     auto lse_of = [&](int k, int head) {
         return k < x.count ? __ldcg(p.part_lse + (own0 + k) * G + head)
                            : __ldcg(p.pre_lse + (pre0 + (k - x.count)) * G + head);
@@ -671,7 +696,7 @@ __device__ void merge_rows(MergeShared<D> &sh, const PieceParams &p, const Piece
 
 // The segment of KV head k % g of the (k / g)-th row as they are laid out, whose records begin at *own0.
 template <int kMode>
-__device__ __forceinline__ Piece segment_of(const PieceParams &p, int k, size_t *own0)
+__device__ __forceinline__ Piece segment_of(const PieceArgs<kMode> &p, int k, size_t *own0)
 {
     Piece x;
     const int i = k / p.g;
@@ -686,20 +711,21 @@ __device__ __forceinline__ Piece segment_of(const PieceParams &p, int k, size_t 
 }
 
 template <int D, int kMode, bool kWide>
-__global__ void __launch_bounds__(kWide ? kMergeThreads : 128) merge_kernel(const __grid_constant__ PieceParams p)
+__global__ void __launch_bounds__(kWide ? kMergeThreads : 128) merge_kernel(const __grid_constant__ PieceArgs<kMode> p)
 {
     extern __shared__ float s_w[];
     const int parts = kWide ? (p.G * D + 127) / 128 : 1, seg = static_cast<int>(blockIdx.x) / parts;
     size_t own0;
     const Piece x = segment_of<kMode>(p, seg, &own0);
-    const int n_pre = kMode == kPieceSuffix || kMode == kPieceGroups ? p.pre_n[x.beta] : 0;
+    const int n_pre = prefix_records<kMode>(p, x.beta);
+    const size_t pre0 = prefix_record<kMode>(p, x.beta, x.j);
     grid_dependency_wait();
     grid_dependents_launch();
     if constexpr (kWide) {
         __shared__ MergeShared<D> sh;
-        merge_rows<D>(sh, p, x, own0, n_pre, static_cast<int>(blockIdx.x) % parts, s_w);
+        merge_rows<D>(sh, p, x, own0, n_pre, pre0, static_cast<int>(blockIdx.x) % parts, s_w);
     } else {
-        merge_records<D>(p, x, own0, n_pre, s_w, static_cast<int>(threadIdx.x), 128);
+        merge_records<D>(p, x, own0, n_pre, pre0, s_w, static_cast<int>(threadIdx.x), 128);
     }
 }
 
@@ -713,7 +739,7 @@ __global__ void __launch_bounds__(kWide ? kMergeThreads : 128) merge_kernel(cons
 constexpr int kWeightThreads = 256;
 template <int D>
 __global__ void __launch_bounds__(kWeightThreads, 4)
-    weights_kernel(const __grid_constant__ PieceParams p, const __grid_constant__ WeightsParams w)
+    weights_kernel(const __grid_constant__ PieceBase p, const __grid_constant__ WeightsParams w)
 {
     __shared__ float s_lse[16];
     extern __shared__ float s_w[];
@@ -729,9 +755,9 @@ __global__ void __launch_bounds__(kWeightThreads, 4)
     const int G = p.G;
     if (part < 0) {
         if (w.wide)
-            merge_rows<D>(sh, p, x, rec0, 0, part + parts, s_w);
+            merge_rows<D>(sh, p, x, rec0, 0, 0, part + parts, s_w);
         else
-            merge_records<D>(p, x, rec0, 0, s_w, tid, kWeightThreads);
+            merge_records<D>(p, x, rec0, 0, 0, s_w, tid, kWeightThreads);
         return;
     }
     const int u0 = part * w.chunk, u1 = min(u0 + w.chunk, w.max_seq);
@@ -828,6 +854,16 @@ const void *piece_fn(int head_dim, int G, int mode)
 int piece_threads(int head_dim) { return head_dim == 64 ? PiecePlan<64>::kThreads : PiecePlan<128>::kThreads; }
 size_t piece_smem(int head_dim) { return head_dim == 64 ? PiecePlan<64>::kBytes : PiecePlan<128>::kBytes; }
 
+// The mode's part of the parameters (PieceArgs).
+void *args_of(int mode, const PieceParams &p)
+{
+    if (mode == kPieceGroups)
+        return const_cast<PieceParams *>(&p);
+    if (mode == kPieceSuffix || mode == kPieceJoined)
+        return const_cast<PiecePrefix *>(static_cast<const PiecePrefix *>(&p));
+    return const_cast<PieceBase *>(static_cast<const PieceBase *>(&p));
+}
+
 cudaError_t launch_pdl(const void *fn, dim3 grid, int threads, size_t smem, cudaStream_t stream, void **args)
 {
     cudaLaunchConfig_t cfg = {};
@@ -867,7 +903,7 @@ cudaError_t launch_pieces(int head_dim, int mode, const CUtensorMap *tmap, const
                           const PieceParams &p, cudaStream_t stream)
 {
     void *args[] = {const_cast<CUtensorMap *>(tmap), const_cast<CUtensorMap *>(tmap_prefix),
-                    const_cast<PieceParams *>(&p)};
+                    args_of(mode, p)};
     const int ctas = p.first[p.n] + (mode == kPieceGroups ? p.n_units : 0);
     return launch_pdl(piece_fn(head_dim, p.G, mode), dim3(static_cast<unsigned>(ctas)), piece_threads(head_dim),
                       piece_smem(head_dim), stream, args);
@@ -899,7 +935,7 @@ cudaError_t launch_merge_pieces(int head_dim, int mode, const PieceParams &p, in
 {
     const bool wide = most > kWideRecords;
     const void *fn = head_dim == 64 ? merge_fn<64>(mode, wide) : merge_fn<128>(mode, wide);
-    void *args[] = {const_cast<PieceParams *>(&p)};
+    void *args[] = {args_of(mode, p)};
     const unsigned ctas = wide ? static_cast<unsigned>((p.G * head_dim + 127) / 128) : 1u;
     return launch_pdl(fn, dim3(ctas * static_cast<unsigned>(p.n) * p.g), wide ? kMergeThreads : 128,
                       merge_smem(head_dim, p.G, most), stream, args);
@@ -915,7 +951,7 @@ cudaError_t launch_weights(int head_dim, const PieceParams &p, const WeightsPara
                            cudaStream_t stream)
 {
     const size_t smem = merge_smem(head_dim, p.G, most);
-    void *args[] = {const_cast<PieceParams *>(&p), const_cast<WeightsParams *>(&w)};
+    void *args[] = {args_of(kPieceWeights, p), const_cast<WeightsParams *>(&w)};
     return launch_pdl(head_dim == 64 ? reinterpret_cast<const void *>(&weights_kernel<64>)
                                      : reinterpret_cast<const void *>(&weights_kernel<128>),
                       dim3(static_cast<unsigned>(w.ctas) * p.b * p.g), kWeightThreads, smem, stream, args);

@@ -152,6 +152,7 @@ def as_seq_lens(seq_lens):
 
 _INT32 = np.dtype(np.int32)
 _byte_at = ctypes.c_char.from_buffer
+_address = ctypes.addressof
 
 
 def _lens_ptr(seq_lens):
@@ -611,7 +612,10 @@ class MLKVCache:
             a = as_seq_lens(a)
         if a.shape != (n,):
             raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must hold {n} numbers")
-        return _lens_ptr(a)
+        try:
+            return a, _address(_byte_at(a))
+        except (TypeError, ValueError):   # read-only or empty
+            return a, a.ctypes.data
 
     def _blocks(self):
         return (self.b, self.g, (self.max_seq + MLKV_BLOCK - 1) // MLKV_BLOCK)
