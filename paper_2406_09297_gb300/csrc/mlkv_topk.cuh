@@ -66,7 +66,7 @@ __device__ void cluster_topk(TopkShared<NT> &sh, unsigned size, unsigned rank, i
     }
     unsigned left = want;   // keys still to take of [lo, hi]
     bool all = false;       // every key of [lo, hi] is taken
-    for (int round = 0; !all && lo != hi; ++round) {
+    for (int round = 0; round < 4 && !all && lo != hi; ++round) {   // (widths 2^32, 2^22, 2^12, 4)
         unsigned *hist = sh.hist[round & 1];
         const int s = max(0, 22 - __clz(static_cast<int>(hi - lo)));   // (hi - lo) >> s below 1024
         // (keys that equal lo are counted apart: where many weights are the same, they are mostly the least)
@@ -133,7 +133,7 @@ __device__ void cluster_topk(TopkShared<NT> &sh, unsigned size, unsigned rank, i
         left -= sh.above;
         all = sh.inside == left;
         lo += sh.bin << s;
-        hi = min(hi, lo + ((1u << s) - 1u));
+        hi = lo + min(hi - lo, (1u << s) - 1u);   // (the interval's end may lie past 2^32)
     }
     // Keys above `top` are taken, and the first `left` that equal it (none where whole intervals are taken).  Each
     // warp has a run of the CTA's keys.

@@ -218,6 +218,18 @@ def test_select_extremes():
     _select(d, h, g, [cap] * 3, cap, 1, 0, 0, K, Q)
 
 
+@pytest.mark.parametrize("n_select", [1, 5, 20])
+@pytest.mark.parametrize("sigma", [1.0, -1.0])
+def test_select_more_unknown_than_stay(n_select, sigma):
+    """More blocks of which nothing is known than are selected."""
+    torch.manual_seed(n_select)
+    K, Q = _randn(2, 2, 6400, 64), _randn(2, 4, 64)
+    K[:, :, ::160, 3] = math.nan
+    K[..., 5] = 30.0
+    Q[..., 5] = 30.0 * sigma   # all other scores of one sign
+    _select(64, 4, 2, [6400, 6000], 6400, n_select, 0, 0, K, Q)
+
+
 def _listed(cache, d, h, g, lens, K, V, Q, blocks):
     out = torch.full_like(Q, 9.0)
     cache.decode_attention_blocks(1, Q, out, lens, blocks)

@@ -190,6 +190,17 @@ def test_evict_orders(kind, where):
     _evict(d, 2 * g, g, [n, n - 999], cap, [1024, 1000], 10, w, where)
 
 
+@pytest.mark.parametrize("largest", [math.nan, math.inf, 3.4028234663852886e38])
+@pytest.mark.parametrize("n", [609, 20000])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_evict_more_largest_than_stay(largest, n, sign):
+    """More positions of the largest weight, at the end of the keys' range, than are kept."""
+    torch.manual_seed(n)
+    w = torch.rand(2, 2, n, device="cuda") * sign
+    w[torch.rand_like(w) < 0.1] = largest
+    _evict(64, 4, 2, [n, n - 7], n, [2, 30], 1, w, "apart")
+
+
 @pytest.mark.parametrize("d,g,b,n,keep", [(64, 1, 1, 131072, 40000), (128, 8, 2, 20000, 5000),
                                           (128, 8, 16, 3000, 2999), (64, 1, 1, 300000, 1000)])
 @pytest.mark.parametrize("where", ["same", "apart"])
