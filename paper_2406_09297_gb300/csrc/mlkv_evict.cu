@@ -2,9 +2,9 @@
 // `recent` newest positions stay and, of the others, those of the largest weights, `keep` in all, of equal
 // weights the earlier ones; keys, values and weights of what stays move together, in order.
 //
-// Two launches.  keep_kernel selects: a cluster a segment, over its weights as ordered keys (cluster_topk), whose
-// result is the list of kept positions.  move_kernel moves: a unit is a run of rows of a segment, which a CTA
-// loads whole before it stores it.  In place, row m takes position kept[m] >= m, so a unit overwrites positions
+// keep_kernel selects: a cluster a segment, over its weights as ordered keys (cluster_topk), whose result is the list of
+// kept positions; what stays of short segments it moves as well, in rounds.  Else move_kernel moves: a unit is a run of
+// rows of a segment, which a CTA loads whole before it stores it.  In place, row m takes position kept[m] >= m, so a unit overwrites positions
 // that only units before it, and it itself, still have to read: it stores after those have set their flags.
 // Units are handed out by a counter in rising order within a segment, so that what a unit waits for has been
 // handed out before it and is running: no wait depends on a CTA that has not started.
@@ -27,12 +27,15 @@ __device__ __forceinline__ unsigned weight_key(float w)
     return w != w ? 0xfffffffeu : (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-constexpr int kKeepThreads = 1024;
+constexpr int kKeepThreads = 1024, kKeepFew = 256;   // of a CTA; of one among many
 
-__global__ void __launch_bounds__(kKeepThreads) keep_kernel(const __grid_constant__ EvictParams p)
+constexpr int kKeepVecs = 4;   // 16-byte vectors of a thread and round, where it moves as well
+
+// D: 0, or the head_dim of rows that it moves as well.
+template <int D, int NT>
+__global__ void __launch_bounds__(NT, kKeepThreads / NT) keep_kernel(const __grid_constant__ EvictParams p)
 {
     namespace cg = cooperative_groups;
-    constexpr int NT = kKeepThreads;
     __shared__ TopkShared<NT> sh;
     __shared__ unsigned s_mm[2 * NT / 32];
     extern __shared__ unsigned s_key[];
@@ -45,41 +48,87 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const __grid_constan
     int *kept = p.kept + static_cast<size_t>(seg) * p.k_max;
     grid_dependency_wait();
     grid_dependents_launch();
-    // the flags of this segment's units; the first CTA also resets the counter of units
-    for (int i = rank * NT + tid; i < p.units; i += size * NT)
-        p.flags[static_cast<size_t>(seg) * p.units + i] = 0u;
-    if (blockIdx.x == 0 && tid == 0)
-        p.flags[static_cast<size_t>(p.b) * p.g * p.units] = 0u;
+    if constexpr (D == 0) {
+        // the flags of this segment's units; the first CTA also resets the counter of units
+        for (int i = rank * NT + tid; i < p.units; i += size * NT)
+            p.flags[static_cast<size_t>(seg) * p.units + i] = 0u;
+        if (blockIdx.x == 0 && tid == 0)
+            p.flags[static_cast<size_t>(p.b) * p.g * p.units] = 0u;
+    }
     // Everything stays of a shorter sequence, else the newest positions, and the heaviest of the others.
     const int others = L <= keep ? 0 : L - p.recent, want = L <= keep ? 0 : keep - p.recent;
     for (int i = rank * NT + tid; i < min(L, keep) - want; i += size * NT)
         kept[want + i] = others + i;
-    if (want == 0)
-        return;
-    const int per = (others + size - 1) / size;
-    const int first = min(others, rank * per), n = min(others, first + per) - first;
-    const bool cached = static_cast<size_t>(per) * 4 <= kKeepSmem;
-    unsigned least = 0xffffffffu, most = 0u;
-    constexpr int U = 8;   // loads in flight
-    for (int i0 = tid; i0 < n; i0 += U * NT) {
-        float x[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            x[u] = i0 + u * NT < n ? __ldcg(w + first + i0 + u * NT) : 0.f;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (i0 + u * NT < n) {
-                const unsigned k = weight_key(x[u]);
-                least = min(least, k);
-                most = max(most, k);
-                if (cached)
-                    s_key[i0 + u * NT] = k;
-            }
+    if (want > 0) {
+        const int per = (others + size - 1) / size;
+        const int first = min(others, rank * per), n = min(others, first + per) - first;
+        const bool cached = static_cast<size_t>(per) * 4 <= kKeepSmem;
+        unsigned least = 0xffffffffu, most = 0u;
+        constexpr int U = 8;   // loads in flight
+        for (int i0 = tid; i0 < n; i0 += U * NT) {
+            float x[U];
+    #pragma unroll
+            for (int u = 0; u < U; ++u)
+                x[u] = i0 + u * NT < n ? __ldcg(w + first + i0 + u * NT) : 0.f;
+    #pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i0 + u * NT < n) {
+                    const unsigned k = weight_key(x[u]);
+                    least = min(least, k);
+                    most = max(most, k);
+                    if (cached)
+                        s_key[i0 + u * NT] = k;
+                }
+        }
+        block_min_max<NT>(least, most, s_mm);   // (and the keys are in place)
+        cluster_topk<NT>(sh, size, rank, n, least, most, static_cast<unsigned>(want),
+                         [&](int i) { return cached ? s_key[i] : weight_key(__ldcg(w + first + i)); },
+                         [&](unsigned place, int i) { kept[place] = first + i; });
     }
-    block_min_max<NT>(least, most, s_mm);   // (and the keys are in place)
-    cluster_topk<NT>(sh, size, rank, n, least, most, static_cast<unsigned>(want),
-                     [&](int i) { return cached ? s_key[i] : weight_key(__ldcg(w + first + i)); },
-                     [&](unsigned place, int i) { kept[place] = first + i; });
+    if constexpr (D > 0) {
+        // Rows in rounds, a run of them a CTA.  In place, row m takes position kept[m] >= m: a round stores over
+        // positions that none of the later ones reads, once all of its own have been read.
+        constexpr int C = D / 8, R = NT * kKeepVecs / (2 * C);
+        auto sync = [&] {
+            if (size > 1)
+                cluster.sync();
+            else
+                __syncthreads();
+        };
+        const int rows = min(L, keep), segments = p.b * p.g;
+        float *w_out = p.weights_out + static_cast<size_t>(seg) * p.dst_seq;
+        sync();   // the list is there
+        for (int m0 = 0; m0 < rows; m0 += size * R) {
+            const int at = m0 + rank * R, n_here = min(R, rows - at);   // (none or less at the end)
+            uint4 v[kKeepVecs];
+            float x = 0.f;
+#pragma unroll
+            for (int k = 0; k < kKeepVecs; ++k) {
+                const int i = k * NT + tid, kv = i / (R * C), row = i % (R * C) / C, c = i % C;   // K's vectors, then V's
+                if (row < n_here)
+                    v[k] = __ldcs(
+                        reinterpret_cast<const uint4 *>(p.src) +
+                        ((static_cast<size_t>(kv) * segments + seg) * p.src_seq + __ldcg(kept + at + row)) * C + c);
+            }
+            if (tid < n_here)
+                x = __ldcg(w + __ldcg(kept + at + tid));
+            if (p.in_place) {
+                __threadfence();   // (the loads have happened, not only been issued)
+                sync();
+            }
+#pragma unroll
+            for (int k = 0; k < kKeepVecs; ++k) {
+                const int i = k * NT + tid, kv = i / (R * C), row = i % (R * C) / C, c = i % C;
+                if (row < n_here)
+                    __stcs(reinterpret_cast<uint4 *>(p.dst) +
+                               ((static_cast<size_t>(kv) * segments + seg) * p.dst_seq + at + row) * C + c, v[k]);
+            }
+            if (tid < n_here)
+                w_out[at + tid] = x;
+        }
+        for (int u = rows + rank * NT + tid; u < p.dst_seq; u += size * NT)
+            w_out[u] = 0.f;
+    }
 }
 
 constexpr int kMoveThreads = 256;
@@ -216,6 +265,14 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constan
     }
 }
 
+template <int NT>
+const void *keep_fn(int head_dim)
+{
+    return head_dim == 0    ? reinterpret_cast<const void *>(&keep_kernel<0, NT>)
+           : head_dim == 64 ? reinterpret_cast<const void *>(&keep_kernel<64, NT>)
+                            : reinterpret_cast<const void *>(&keep_kernel<128, NT>);
+}
+
 }  // namespace
 
 int evict_units(int head_dim, int k_max)
@@ -226,8 +283,12 @@ int evict_units(int head_dim, int k_max)
 
 cudaError_t prepare_evict()
 {
-    return cudaFuncSetAttribute(reinterpret_cast<const void *>(&keep_kernel),
-                                cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kKeepSmem));
+    cudaError_t e = cudaSuccess;
+    for (const void *fn : {keep_fn<kKeepThreads>(0), keep_fn<kKeepThreads>(64), keep_fn<kKeepThreads>(128),
+                           keep_fn<kKeepFew>(0), keep_fn<kKeepFew>(64), keep_fn<kKeepFew>(128)})
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kKeepSmem));
+    return e;
 }
 
 cudaError_t launch_evict(int head_dim, const EvictParams &p, int max_len, int sm_count, cudaStream_t stream)
@@ -240,7 +301,11 @@ cudaError_t launch_evict(int head_dim, const EvictParams &p, int max_len, int sm
     const size_t keys = static_cast<size_t>((max_len + size - 1) / size) * 4;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.b * p.g * size));
-    cfg.blockDim = dim3(kKeepThreads);
+    // Small CTAs where there are more segments than SMs, which then hold four of them (480 of 1000 positions, 250 kept,
+    // of 64 channels 15.8 us, 26.1 with large ones; 144 of them 9.4, 6.7 with large ones).
+    const bool few = static_cast<long long>(p.b) * p.g > sm_count && max_len <= 8192;
+    const int nt = few ? kKeepFew : kKeepThreads;
+    cfg.blockDim = dim3(static_cast<unsigned>(nt));
     cfg.dynamicSmemBytes = keys <= kKeepSmem ? keys : kKeepSmem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -252,8 +317,16 @@ cudaError_t launch_evict(int head_dim, const EvictParams &p, int max_len, int sm
     cfg.attrs = attr;
     cfg.numAttrs = size > 1 ? 2 : 1;   // (a cluster's launch costs the host a microsecond more)
     void *args[] = {const_cast<EvictParams *>(&p)};
-    cudaError_t e = cudaLaunchKernelExC(&cfg, reinterpret_cast<const void *>(&keep_kernel), args);
-    if (e != cudaSuccess)
+    // One launch where few rounds move what stays of a segment.  A round is a trip to memory and back, the second launch
+    // takes 2 to 4 us here and two of the host's.  us, one / two launches: 144 segments of 1000 positions, 250 kept,
+    // 6.8 / 9.5, 16 of 2000, 500 kept (two rounds) 8.7 / 8.1, four of 2000, 1900 kept (eight) 16.6 / 8.2; where nearly every SM has
+    // a segment, 128 of 2000, 500 kept (four) 14.8 / 16.7, of 4000, 1000 kept (eight) 26.0 / 26.5, in place 28.1 / 27.4.
+    const int per_round = size * (nt * kKeepVecs / (head_dim / 4)), rounds = (p.rows + per_round - 1) / per_round;
+    const long long ctas = static_cast<long long>(p.b) * p.g * size;
+    const bool whole = rounds <= (few || (2 * ctas > sm_count && ctas <= sm_count) ? 4 : ctas <= sm_count ? 2 : 0);
+    cudaError_t e = cudaLaunchKernelExC(
+        &cfg, few ? keep_fn<kKeepFew>(whole ? head_dim : 0) : keep_fn<kKeepThreads>(whole ? head_dim : 0), args);
+    if (e != cudaSuccess || whole)
         return e;
     const long long units = static_cast<long long>(p.b) * p.g * p.units;
     cfg.gridDim = dim3(static_cast<unsigned>(units < 6LL * sm_count ? units : 6LL * sm_count));

@@ -174,7 +174,8 @@ struct EvictParams {
     int b, g, src_seq, dst_seq, k_max, recent;
     int in_place;              // the slots or the weights are the same memory
     int same;                  // both are: rows that stay where they are need no store
-    int units;                 // of a segment: ceil(k_max / rows of a unit), and one for the tail
+    int units;                 // of a segment: ceil(rows / rows of a unit), and one for the tail
+    int rows;                  // that stay of a segment, at most
     int seq_len[MLKV_MAX_BATCH];
     int keep[MLKV_MAX_BATCH];
 };

@@ -91,7 +91,8 @@ Cut plan_cut(const mlkv_cache *c, const CutRules &r, const Tiles &nt)
     // us: a tile of a CTA alone on its SM; all tiles at the rate of HBM; a record's part of an inline merge
     const double tile = c->d == 64 ? 0.33 : c->G <= 8 ? 0.45 : 0.72;
     const double from_hbm = r.hbm_tiles < 0 ? total : r.hbm_tiles;
-    const double bytes = std::max(from_hbm / 6.7e6, total / (c->G <= 8 ? 14e6 : 10e6)) * 256.0 * c->d, record = 0.1 * c->G * c->d / 512;
+    const double bytes = std::max(from_hbm / 6.7e6, total / (c->G <= 8 ? 14e6 : 10e6)) * 256.0 * c->d;
+    const double record = 0.1 * c->G * c->d / 512;
     const int inline_most = mlkv::piece_max_records(c->d, c->G) - r.pre;
     Cut best = {r.always_apart, 1, longest, 1e30};
     for (int want = 1, tiles = longest;; want += (want + 3) / 4) {   // pieces of the longest segment
@@ -820,6 +821,7 @@ int mlkv_evict(mlkv_cache_t c, mlkv_cache_t to, int layer, const float *weights_
     if (overlap(kept, list, weights_in, in) || overlap(kept, list, weights_out, out))
         return fail(MLKV_ERR_INVALID_ARG, "kept overlaps weights");
     p.units = mlkv::evict_units(c->d, rows);
+    p.rows = rows;
     if (segments * p.units > 0x7fffffffu || segments > (1u << 24))
         return fail(MLKV_ERR_UNSUPPORTED, "%zu KV heads of %d units exceed a launch", segments, p.units);
     DeviceGuard guard(c->device);

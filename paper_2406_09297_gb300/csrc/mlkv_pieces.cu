@@ -536,7 +536,8 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
     size_t rec = blockIdx.x;
     if constexpr (kMode == kPieceGroups)
         rec -= static_cast<unsigned>(p.n_units);   // (of a unit not used)
-    __nv_bfloat16 *ob = p.out + (static_cast<size_t>(q_row_of<kMode>(p, x.beta)) * p.h + static_cast<size_t>(x.j) * p.G) * D;
+    __nv_bfloat16 *ob =
+        p.out + (static_cast<size_t>(q_row_of<kMode>(p, x.beta)) * p.h + static_cast<size_t>(x.j) * p.G) * D;
     for (int i = tid * 4; i < x.rows * D; i += kWarps * 32 * 4) {
         const int row = i / D, ch = i - row * D;
         float mx = neg_inf();

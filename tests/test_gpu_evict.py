@@ -190,6 +190,18 @@ def test_evict_orders(kind, where):
     _evict(d, 2 * g, g, [n, n - 999], cap, [1024, 1000], 10, w, where)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("b,g,n,keep", [(1, 1, 700, 600), (2, 2, 1000, 130), (5, 1, 9000, 300), (40, 3, 600, 400),
+                                        (50, 4, 500, 30), (50, 4, 500, 260), (50, 4, 9000, 60), (170, 1, 300, 299)])
+@pytest.mark.parametrize("where", ["same", "apart", "weights"])
+def test_evict_forms(d, b, g, n, keep, where):
+    """Moved by the selecting CTA in one round or several, by one of many, by a cluster, or by units."""
+    lens = [n - 3 * i for i in range(b)] if 3 * b < n else [n - i for i in range(b)]
+    torch.manual_seed(b)
+    w = torch.rand(b, g, n, device="cuda")
+    _evict(d, g, g, lens, n, [max(1, keep - i % 50) for i in range(b)], 1, w, where)
+
+
 @pytest.mark.parametrize("largest", [math.nan, math.inf, 3.4028234663852886e38])
 @pytest.mark.parametrize("n", [609, 20000])
 @pytest.mark.parametrize("sign", [1, -1])
