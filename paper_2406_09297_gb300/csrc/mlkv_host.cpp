@@ -1905,26 +1905,36 @@ int mlkv::check_window(int window, int sinks)
 extern "C" {
 
 // A few short prompts behind prefixes: every token a query row of its own of the decode over shared prefixes,
-// whose rows fill the tiles that a prompt's positions would leave empty, where that is estimated to take less than
-// the prefill kernel: us 6, and 1.25 (head_dim 64, two CTAs an SM) or 1.65 a unit's key tile and two more.  66 prompts
-// of one token behind 8086 positions, 12 heads of 64: 227 us by the prefill kernel.
+// whose rows fill the tiles that a prompt's positions would leave empty and whose prefixes are split over the SMs, where
+// that is estimated to take less than the prefill kernel.  us, prefill kernel / rows: 2 uneven prompts of up to 12 behind
+// 3582 positions, 32 heads over 4 KV heads of 128, 43.5 / 10.0; 5 of up to 118 behind 5669, 12 heads of 64, 44.1 / 28.2;
+// 26 of 6 behind 1487, the same heads, 34.2 / 18.4.
 static int prefill_as_rows(mlkv_cache_t c, int layer, mlkv_cache_t prefix, const int *prefix_of,
                            const int *prefix_lens, const int *pre_len, const void *Q, const void *K,
                            const void *V, void *out, const int *prompt_lens, int s_max, cudaStream_t stream,
                            bool *issued)
 {
-    long long tokens = 0, units = 0, tiles = 0;
+    long long tokens = 0, units = 0, tiles = 0, most = 0;
     for (int beta = 0; beta < c->b; ++beta) {
-        const long long blocks = (prompt_lens[beta] + 127) / 128;
+        const long long blocks = (prompt_lens[beta] + 127) / 128, pre = (pre_len[beta] + 127) / 128;
         tokens += prompt_lens[beta];
         units += blocks;
-        tiles += blocks * ((pre_len[beta] + 127) / 128) + blocks * (blocks + 1) / 2;
+        tiles += blocks * pre + blocks * (blocks + 1) / 2;
+        most = std::max(most, pre + blocks);
     }
+    // (more rows, a launch's after another's: 104 prompts of 12, 32 heads over 4 KV heads of 128, 101 us for 79)
     if (tokens > MLKV_MAX_BATCH || static_cast<long long>(c->b) * s_max > 65535 || c->g > 255)
         return MLKV_OK;
+    // The prefill's kernel: units of a block of 128 queries of one head (64 channels, two at a time an SM) or two, their
+    // tiles and two more for start and end, in waves; a tile takes longer where the SM has two units or all SMs are busy.
     const bool small = c->d == 64;
-    const double prefill_us = 6 + (small ? 1.25 : 1.65) * (tiles + 2 * units) * (small ? c->h : (c->h + 1) / 2) /
-                                      ((small ? 2.0 : 1.0) * c->sm_count);
+    const double mean = 2.0 + static_cast<double>(tiles) / units;
+    units *= small ? c->h : (c->h + 1) / 2;
+    const long long slots = (small ? 2LL : 1LL) * c->sm_count, rest = units % slots;
+    const double busy = small ? 1.25 : 1.65, idle = small ? 0.85 : 1.25;
+    const double prefill_us =
+        6 + std::max((most + 2) * idle, mean * (static_cast<double>(units / slots) * busy +
+                                                (rest == 0 ? 0.0 : rest > slots / 2 ? busy : idle)));
     // What the rows take at the least, by either of their forms: the exact plan walks over all of them.
     static thread_local int of_prefix[MLKV_MAX_BATCH];
     std::fill(of_prefix, of_prefix + prefix->b, 0);
