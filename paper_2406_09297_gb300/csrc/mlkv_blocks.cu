@@ -134,8 +134,8 @@ constexpr int kLanes = 4;   // lanes of a block's score
 
 // A cluster is one (sequence, KV head): each CTA scores a run of its blocks, four lanes a block (dp4a of the
 // codes with the query's positive and negative parts; 64 bytes a load), and puts the scores as ordered keys into
-// the first CTA's shared memory, which takes the largest (cluster_topk).  Bound by latency for few blocks (2048 blocks of one
-// KV head, 12 heads of 64, 11 us), else by the products, 2 D / 4 dp4a a block and head (32 uneven sequences of up to 512
+// the first CTA's shared memory, which takes the largest (cluster_topk).  Bound by latency for few blocks (2048 blocks of
+// one KV head, 12 heads of 64, 11 us), else by the products, 2 D / 4 dp4a a block and head (32 uneven sequences of up to 512
 // blocks, 8 KV heads, 4 heads of 128 each, 12.5 us).
 template <int D>
 __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_constant__ SelectParams p)

@@ -58,8 +58,9 @@ int prepare_pieces(mlkv_cache *c, int mode)
 // How the segments, nt(beta) tiles each, are cut into pieces: the least estimated time, in us.  A
 // launch takes 4.5, and what is longer of its bytes at the rate of HBM and its longest piece; pieces beyond one wave
 // of resident CTAs half a piece more where segments are split (whole ones end evenly enough).  Split segments
-// are merged by the CTA that ends last, a round trip to L2 for every 8 records, or by a launch of their own.  Never more pieces than there are records.  pre: records that every merge has besides; hbm_tiles:
-// tiles that come from HBM, the others from L2 (14 TB/s, groups above 8 heads 10); -1: all.
+// are merged by the CTA that ends last, a round trip to L2 for every 8 records, or by a launch of their own.  Never more
+// pieces than there are records.  pre: records that every merge has besides; hbm_tiles: tiles that come from HBM, the
+// others from L2 (14 TB/s, groups above 8 heads 10); -1: all.
 struct Cut {
     bool defer;
     int records;   // of a segment, at most

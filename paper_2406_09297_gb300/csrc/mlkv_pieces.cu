@@ -145,8 +145,8 @@ __device__ __forceinline__ Piece piece_of(const PieceArgs<kMode> &p)
     return x;
 }
 
-// Merges the segment's records (its own pieces', from own0 on, then the prefix's n_pre from pre0 on) into out: the weights
-// first, then the sums in the records' order.  s_w: room for a row of G floats a record, and one more.
+// Merges the segment's records (its own pieces', from own0 on, then the prefix's n_pre from pre0 on) into out: the
+// weights first, then the sums in the records' order.  s_w: room for a row of G floats a record, and one more.
 template <int D>
 __device__ void merge_records(const PieceBase &p, const Piece &x, size_t own0, int n_pre, size_t pre0, float *s_w,
                               int tid, int n_threads)
@@ -608,8 +608,8 @@ __global__ void __launch_bounds__(PiecePlan<D>::kThreads, 2)
 // The merge of many records by CTAs of their own, 128 floats each: a head of 128 channels or two of 64.  The
 // warps take the records in turn, 128 floats a warp and record, eight at a time on the way, and add up in the
 // warps' order.  Bound by the records' bytes, in L2, and three round trips to it.  For few records a CTA a segment
-// (merge_records): 1024 segments of 6 records of 4 heads of 128 6.4 us, 25 with four of these CTAs each; one segment of 152
-// records of 12 heads of 64 3 us, 23 with one CTA.
+// (merge_records): 1024 segments of 6 records of 4 heads of 128 6.4 us, 25 with four of these CTAs each; one segment
+// of 152 records of 12 heads of 64 3 us, 23 with one CTA.
 constexpr int kWideRecords = 16;
 constexpr int kMergeThreads = 256;
 template <int D>
