@@ -267,7 +267,8 @@ int mlkv_prefill_window(mlkv_cache_t c, int layer, const void *Q, const void *K,
  *   prefix_of    host int32[batch]: a sequence of `prefix`, or -1: none
  *   prefix_lens  host int32[prefix's batch], 0 <= prefix_lens[x] <= prefix's max_seq
  * The other arguments as for mlkv_decode_attention: seq_lens counts a sequence's own positions, the new token
- * included (keys are encoded by the caller: a sequence's own positions follow its prefix's).  Calls on c must be
+ * included (keys are encoded by the caller: a sequence's own positions follow its prefix's).  A head whose scores are
+ * all -infinity gets zeros.  Calls on c must be
  * ordered with those on `prefix` that store what it reads.  Scratch of c is allocated when a call needs more than
  * any before (not while cuda_stream is captured: MLKV_ERR_UNSUPPORTED); at most 255 KV heads.
  * Errors: as mlkv_decode_attention; MLKV_ERR_MAP (the caches' layers or heads differ), MLKV_ERR_RANGE (prefixes,
@@ -281,7 +282,7 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
  * mlkv_prefill_prefix - mlkv_prefill of prompts that go on behind a shared beginning: prompt position t of
  * sequence beta attends to all of its prefix's positions and to positions 0 .. t of its prompt.  An owner layer
  * stores its prompt's K/V in c at positions [0, s_max); the prefix stays where it is, and mlkv_decode_attention_prefix
- * goes on from there.
+ * goes on from there.  (Scores that are all -infinity: zeros.)
  * prefix, prefix_of and prefix_lens as above, but prefix != c; the others and errors as for mlkv_prefill.  Short
  * prompts are taken as rows of a decode, with scratch of c as above; where that cannot be had, without.
  */

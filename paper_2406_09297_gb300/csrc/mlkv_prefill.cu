@@ -909,9 +909,8 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                 const bool raise = (m_run == NEG_INF) || (m_tile > m_run + 8.f);
                 if (__any_sync(0xffffffffu, raise)) {
                     const float m_new = raise ? fmaxf(m_run, m_tile) : m_run;
-                    // 0 while nothing is summed; a row without a visible key yet keeps its zeros
-                    const float alpha =
-                        kWin && m_new == NEG_INF ? 1.f : fast_exp2(m_run - m_new);
+                    // 0 while nothing is summed; a row without a score above -infinity yet keeps its zeros
+                    const float alpha = m_new == NEG_INF ? 1.f : fast_exp2(m_run - m_new);
                     if (t > wg) {
                         // Rescale this row of O once the previous tile's product has landed.
                         if (PL::kPSep)
@@ -933,7 +932,7 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                 }
                 // p = 2^(s log2(e)/sqrt(d) - m) as bf16 pairs, and the row's sum in fp32.
                 const float2 sc2 = make_float2(scale, scale);
-                const float m_use = m_run == NEG_INF ? 0.f : m_run;   // all masked so far: p = 0
+                const float m_use = m_run == NEG_INF ? 0.f : m_run;   // all -infinity so far: p = 0
                 const float2 nm2 = make_float2(-m_use, -m_use);
                 float2 acc[4];
 #pragma unroll
@@ -1044,7 +1043,10 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
             constexpr int kParts = kSplit ? 1 : 2;
             if (n_g > 0) {
                 tmem_fence_after();
-                const float inv = fast_rcp(l_run);
+                // A record without a score above -infinity is zeros (and lse -infinity), which a merge gives the
+                // weight 0; so is such a row behind a prefix, as in the decodes over pieces.
+                const bool empty = (kShared || (kFused && p.fused_cmax > 1)) && l_run == 0.f;
+                const float inv = empty ? 0.f : fast_rcp(l_run);
                 const int stop = flags[0];
                 // Row r of the tile.  Prefill: position q0 + r of the head.  Fused: layer
                 // (grp ? 0 : L1) + r / G of the block, head j*G + r % G; out [layers][b][h][D].
