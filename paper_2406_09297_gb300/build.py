@@ -34,6 +34,7 @@ def _deps():
                          os.path.join(CSRC, "mlkv_tcgen05.cuh"), os.path.join(CSRC, "mlkv_host.h"),
                          os.path.join(CSRC, "mlkv_q4.h"), os.path.join(CSRC, "mlkv_cache.h"),
                          os.path.join(CSRC, "mlkv_long.h"), os.path.join(CSRC, "mlkv_topk.cuh"),
+                         os.path.join(CSRC, "mlkv_plan.h"),
                          os.path.join(INCLUDE, "mlkv.h"),
                          os.path.abspath(__file__)]
     return deps

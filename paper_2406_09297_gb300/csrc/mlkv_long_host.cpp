@@ -10,6 +10,7 @@
 
 #include "mlkv_cache.h"
 #include "mlkv_long.h"
+#include "mlkv_plan.h"
 
 using mlkv::aligned16;
 using mlkv::check_layer;
@@ -224,52 +225,6 @@ int own_records(mlkv_cache *c, mlkv::PieceParams &p, size_t before, cudaStream_t
     return MLKV_OK;
 }
 
-// How the decode over shared prefixes is launched.
-struct PrefixPlan {
-    int kc;       // key tiles of 128 positions of a unit
-    int sms;      // CTAs of the prefix kernel, one an SM
-    bool beside;  // the suffixes run beside it on the other SMs, and are merged by a launch of their own
-    double us;    // estimated
-};
-
-// For `pairs` unit columns (pairs of query tiles times KV heads) over prefixes of n_kt tiles, and suffixes of
-// `bytes`: the least estimated time.  Microseconds: a unit's key tile `tile`, its start and end `edges` of them; the
-// suffixes at most `rate` bytes a us an SM and `all` in total.  (The prefix kernel is bound by the tensor cores where
-// many sequences share one, the suffixes by HBM: side by side, each has what the other leaves.  Not for
-// suffixes of less than 16 MB, which the merge's launch outweighs.)  Fitted to eight shapes, each in ten splits: the
-// one taken is at most 3% behind the best of them.  128 sequences of 1024, 8 KV heads of 128, over one prefix of
-// 32768: 115 us beside 80 SMs of 52 tiles a unit, 147 one after the other.
-PrefixPlan plan_prefix(const int *n_kt, const int *pairs, int n, int sm_count, int d, double bytes)
-{
-    const double tile = d == 64 ? 0.95 : 1.5, edges = 7, rate = 75e3, all = 6.5e6;
-    long long work = 0;
-    int longest = 1;
-    for (int x = 0; x < n; ++x) {
-        work += static_cast<long long>(n_kt[x]) * pairs[x];
-        if (pairs[x] > 0)
-            longest = std::max(longest, n_kt[x]);
-    }
-    const int least = std::max(1, (longest + mlkv::kFusedMaxChunks - 1) / mlkv::kFusedMaxChunks);
-    PrefixPlan best = {longest, sm_count, false, 1e30};
-    for (int kc = std::max<long long>(least, work / (4LL * sm_count)); kc <= longest; kc += (kc + 15) / 16) {
-        long long units = 0;
-        for (int x = 0; x < n; ++x)
-            units += static_cast<long long>((n_kt[x] + kc - 1) / kc) * pairs[x];
-        for (int rounds = 1; rounds <= 8; ++rounds) {   // of the units, on as many SMs as it takes
-            const int sms = static_cast<int>(std::min<long long>(sm_count, (units + rounds - 1) / rounds));
-            const double t = static_cast<double>((units + sms - 1) / sms) * (kc + edges) * tile;
-            const double one = (bytes < 16e6 ? 7 : 15) + t + bytes / all;
-            if (one < best.us)
-                best = {kc, sms, false, one};
-            const double beside =
-                13 + t + std::max(0.0, bytes - t * std::min(all, rate * (sm_count - sms))) / all;
-            if (sm_count - sms >= 8 && bytes >= 16e6 && beside < best.us)
-                best = {kc, sms, true, beside};
-        }
-    }
-    return best;
-}
-
 }  // namespace
 
 int mlkv::check_same_model(const mlkv_cache *c, const mlkv_cache *other, const char *what)
@@ -343,7 +298,7 @@ int mlkv::decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const 
     // neighbours already, a sequence's place is its own number.
     const int L1 = 128 / c->G, np = prefix->b;
     static thread_local int n_kt[MLKV_MAX_BATCH], pairs[MLKV_MAX_BATCH];
-    static thread_local PrefixPlan plan;
+    static thread_local mlkv::PrefixPlan plan;
     std::fill(u.group_n, u.group_n + np, static_cast<uint16_t>(0));
     auto of = [&](int beta) {
         return rows.prefix[beta] >= 0 && prefix_lens[rows.prefix[beta]] > 0 ? rows.prefix[beta] : -1;
@@ -368,7 +323,7 @@ int mlkv::decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const 
         most_kt = std::max(most_kt, n_kt[x]);
     }
     if (most_kt > 0)
-        plan = plan_prefix(n_kt, pairs, np, c->sm_count, c->d, bytes);
+        plan = mlkv::plan_prefix(n_kt, pairs, np, c->sm_count, c->d, bytes, mlkv::kFusedMaxChunks);
     // The prefixes for as many sequences at a time as have 16 heads together, beside the suffixes in their launch: read
     // from L2 again for every group of them, and merged by a launch.  us: 9, and what is longest of the bytes from HBM,
     // those through the SMs (8.5 TB/s) and a unit; half the longest suffix more where those are uneven.  Measured, us, end
