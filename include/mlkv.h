@@ -588,7 +588,10 @@ int mlkv_kv_ptr(mlkv_cache_t c, int slot, void **k_base, void **v_base, int64_t 
  * "last_fused_kc" the 128-position key tiles per unit), "last_step_launches" (this library's
  * launches of that step when it ran in either form, else 0), "last_seg_major" (1 if the
  * multi-layer launch ranked its items segment-major) and "last_l2_prefetch" (1 if it prefetched
- * the slots into L2).
+ * the slots into L2); for the most recent mlkv_decode_attention_prefix, or mlkv_prefill_prefix with a prefix in front of
+ * some prompt, "last_prefix_form" (1 each sequence's positions end to end, 2 a prefix for 16 heads at a time, 3 the
+ * prefix kernel and then the suffixes, 4 both side by side, 5 the prefill kernel; short prompts as rows: their decode's)
+ * and "last_prefix_launches" (this library's launches in it, a prompt's store apart).
  * Unknown keys or values return MLKV_ERR_INVALID_ARG.
  */
 int mlkv_set_option(mlkv_cache_t c, const char *key, int64_t value);

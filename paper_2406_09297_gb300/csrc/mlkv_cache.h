@@ -82,6 +82,8 @@ struct mlkv_cache {
     // the most recent decode launch (read-only options, for tests and tuning)
     int last_grid = 0, last_tile = 0, last_cluster_k = 0, last_deferred = 0, last_tc = 0;
     int last_l2_prefetch = 0;
+    // the most recent call behind shared prefixes: the form it took, and this library's launches (a store's apart)
+    int last_prefix_form = 0, last_prefix_launches = 0;
     unsigned long_ready = 0;   // kernels of mlkv_long_host.cpp whose limits are set (a bit each)
     int piece_ctas = 0;        // resident CTAs of the piece kernel per SM
     // per-variant launch state
@@ -107,6 +109,16 @@ int check_seq_lens(const mlkv_cache *c, const int *seq_lens);
 int check_same_model(const mlkv_cache *c, const mlkv_cache *other, const char *what);
 // The checks of a shared prefix's cache, of each sequence's prefix in it (-1: none) and of their lengths.
 int check_prefix(const mlkv_cache *c, const mlkv_cache *prefix, const int *prefix_of, const int *prefix_lens);
+
+// Forms of the calls behind shared prefixes (option "last_prefix_form").
+enum : int {
+    kFormNone = 0,
+    kFormJoined = 1,    // each sequence's prefix and positions end to end
+    kFormGroups = 2,    // a prefix for 16 heads at a time, in the suffixes' launch
+    kFormKernel = 3,    // the prefix kernel, then the suffixes
+    kFormBeside = 4,    // the prefix kernel and the suffixes side by side
+    kFormPrompt = 5,    // prompts: the prefill's kernel (else their rows' form)
+};
 
 // Query rows of a decode over shared prefixes: row i attends to prefix[i]'s positions (-1: none) and then to the
 // first len[i] of its sequence.  scattered: it is row q_row[i] of Q and out, of sequence seq[i]; else n is the

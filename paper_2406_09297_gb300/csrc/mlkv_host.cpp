@@ -1848,6 +1848,8 @@ int mlkv::issue_prefill(const PrefillCall &a, cudaStream_t stream)
         max_blocks = std::max(max_blocks, pre_blocks(beta) + (a.prompt_lens[beta] + 127) / 128);
     auto issue = [&](int n) {
         p.n_units = n;
+        if (a.launches != nullptr)
+            ++*a.launches;
         return shared ? mlkv::launch_shared(a.d, false, &tmap_q, tmap_k, tmap_v, over, stream)
                       : mlkv::launch_prefill(a.d, &tmap_q, tmap_k, tmap_v, plain, stream);
     };
@@ -2064,6 +2066,9 @@ static int prefill_impl(mlkv_cache_t c, int layer, const void *Q, const void *K,
         a.prefix_b = prefix->b;
         a.prefix_of = prefix_of;
         a.prefix_len = pre_len;
+        a.launches = &c->last_prefix_launches;
+        c->last_prefix_form = mlkv::kFormPrompt;
+        c->last_prefix_launches = 0;
     }
     if ((rc = mlkv::issue_prefill(a, stream)) != MLKV_OK)
         return rc;
@@ -2418,6 +2423,14 @@ int mlkv_get_option(mlkv_cache_t c, const char *key, int64_t *value)
     }
     if (std::strcmp(key, "last_l2_prefetch") == 0) {
         *value = c->last_l2_prefetch;
+        return MLKV_OK;
+    }
+    if (std::strcmp(key, "last_prefix_form") == 0) {
+        *value = c->last_prefix_form;
+        return MLKV_OK;
+    }
+    if (std::strcmp(key, "last_prefix_launches") == 0) {
+        *value = c->last_prefix_launches;
         return MLKV_OK;
     }
     if (std::strcmp(key, "cluster") == 0) {

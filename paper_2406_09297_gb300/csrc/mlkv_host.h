@@ -122,6 +122,7 @@ struct PrefillCall {
     const CUtensorMap *tmap_prefix;
     int prefix_b;
     const int *prefix_of, *prefix_len;
+    int *launches;              // counts them; NULL: nobody does
 };
 int issue_prefill(const PrefillCall &a, cudaStream_t stream);
 // The checks of a prompt's sizes, lengths, queries and outputs shared by the prefill calls.

@@ -382,6 +382,8 @@ int mlkv::decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const 
             return no_scratch(rc);
         if ((rc = begin()) != MLKV_OK)
             return rc;
+        c->last_prefix_form = mlkv::kFormJoined;
+        c->last_prefix_launches = end_to_end.defer ? 2 : 1;
         return decode_pieces(c, mlkv::kPieceJoined, p, end_to_end, rows64(prefix), stream);
     }
     if (neighbours) {
@@ -452,6 +454,8 @@ int mlkv::decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const 
                                              (static_cast<uint32_t>(std::min(S1, u.group_n[x] - s) - 1) << 26);
                         p.unit_place[p.n_units++] = static_cast<uint16_t>(u.group_at[x] + s);
                     }
+        c->last_prefix_form = mlkv::kFormGroups;
+        c->last_prefix_launches = 2;
         return decode_pieces(c, mlkv::kPieceGroups, p, split, rows64(prefix), stream);
     }
     p.early = 1;
@@ -508,10 +512,13 @@ int mlkv::decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const 
     std::memcpy(u.prompt_len, prefix_lens, sizeof(int) * np);
     if ((rc = begin()) != MLKV_OK)
         return rc;
+    c->last_prefix_form = plan.beside ? mlkv::kFormBeside : mlkv::kFormKernel;
+    c->last_prefix_launches = split.defer ? 2 : 1;
     int n = 0;
     auto issue = [&]() {
         u.n_units = n;
         n = 0;
+        ++c->last_prefix_launches;
         return mlkv::launch_shared(c->d, true, &tmap_q, tmap_kv, tmap_kv, u, stream);
     };
     for (int x = 0; x < np; ++x) {
