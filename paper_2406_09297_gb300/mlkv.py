@@ -465,26 +465,6 @@ def mlkv_q4_sync_status(handle):
     return _check(lib.mlkv_q4_sync_status(handle))
 
 
-def mlkv_decode_attention_prefix(handle, layer, prefix, prefix_of, prefix_lens, Q, out, seq_lens,
-                                 stream=None):
-    """prefix: the handle of the cache of the shared beginnings; prefix_of [b] (-1: none), prefix_lens
-    [sequences of prefix] and seq_lens [b] on the host."""
-    a, p = _lens_ptr(seq_lens)
-    o, po = _lens_ptr(prefix_of)
-    n, pn = _lens_ptr(prefix_lens)
-    return _check(lib.mlkv_decode_attention_prefix(handle, layer, prefix, po, pn, _ptr(Q), _ptr(out), p,
-                                                   _stream(stream)))
-
-
-def mlkv_prefill_prefix(handle, layer, prefix, prefix_of, prefix_lens, Q, K, V, out, prompt_lens, s_max,
-                        stream=None):
-    a, p = _lens_ptr(prompt_lens)
-    o, po = _lens_ptr(prefix_of)
-    n, pn = _lens_ptr(prefix_lens)
-    return _check(lib.mlkv_prefill_prefix(handle, layer, prefix, po, pn, _ptr(Q), _ptr(K), _ptr(V), _ptr(out),
-                                          p, s_max, _stream(stream)))
-
-
 _dtypes = {}
 
 
@@ -500,6 +480,33 @@ def _dense(name, t, dtype):
     return t.data_ptr()
 
 
+def _rows(name, t):
+    """The same of queries, keys, values and outputs, which may be absent."""
+    return None if t is None else _dense(name, t, "bfloat16")
+
+
+# (The functions on handles take the sizes of tensors as they are given; the methods of MLKVCache check them.)
+
+def mlkv_decode_attention_prefix(handle, layer, prefix, prefix_of, prefix_lens, Q, out, seq_lens,
+                                 stream=None):
+    """prefix: the handle of the cache of the shared beginnings; prefix_of [b] (-1: none), prefix_lens
+    [sequences of prefix] and seq_lens [b] on the host."""
+    a, p = _lens_ptr(seq_lens)
+    o, po = _lens_ptr(prefix_of)
+    n, pn = _lens_ptr(prefix_lens)
+    return _check(lib.mlkv_decode_attention_prefix(handle, layer, prefix, po, pn, _rows("Q", Q),
+                                                   _rows("out", out), p, _stream(stream)))
+
+
+def mlkv_prefill_prefix(handle, layer, prefix, prefix_of, prefix_lens, Q, K, V, out, prompt_lens, s_max,
+                        stream=None):
+    a, p = _lens_ptr(prompt_lens)
+    o, po = _lens_ptr(prefix_of)
+    n, pn = _lens_ptr(prefix_lens)
+    return _check(lib.mlkv_prefill_prefix(handle, layer, prefix, po, pn, _rows("Q", Q), _rows("K", K),
+                                          _rows("V", V), _rows("out", out), p, s_max, _stream(stream)))
+
+
 def mlkv_block_bounds(handle, layer, first, seq_lens, bounds, scales, stream=None):
     """first: host [b] or None (every block); bounds int8 [b][g][n_blocks][2][d], scales fp32
     [b][g][n_blocks], n_blocks = ceil(max_seq / 64)."""
@@ -513,7 +520,7 @@ def mlkv_select_blocks(handle, layer, Q, bounds, scales, seq_lens, n_select, n_f
                        stream=None):
     """blocks int32 [b][g][n_select]: written, rising, -1 behind the last."""
     a, p = _lens_ptr(seq_lens)
-    return _check(lib.mlkv_select_blocks(handle, layer, _ptr(Q), _dense("bounds", bounds, "int8"),
+    return _check(lib.mlkv_select_blocks(handle, layer, _rows("Q", Q), _dense("bounds", bounds, "int8"),
                                          _dense("scales", scales, "float32"), p, n_select, n_first, n_last,
                                          _dense("blocks", blocks, "int32"), _stream(stream)))
 
@@ -521,7 +528,7 @@ def mlkv_select_blocks(handle, layer, Q, bounds, scales, seq_lens, n_select, n_f
 def mlkv_decode_attention_blocks(handle, layer, Q, out, seq_lens, blocks, n_blocks, stream=None):
     """blocks int32 [b][g][n_blocks]."""
     a, p = _lens_ptr(seq_lens)
-    return _check(lib.mlkv_decode_attention_blocks(handle, layer, _ptr(Q), _ptr(out), p,
+    return _check(lib.mlkv_decode_attention_blocks(handle, layer, _rows("Q", Q), _rows("out", out), p,
                                                    _dense("blocks", blocks, "int32"), n_blocks,
                                                    _stream(stream)))
 
@@ -530,7 +537,7 @@ def mlkv_decode_attention_weights(handle, layer, Q, out, seq_lens, weights_in, w
     """weights fp32 [b][g][max_seq]; weights_in None: zeros."""
     a, p = _lens_ptr(seq_lens)
     w = None if weights_in is None else _dense("weights_in", weights_in, "float32")
-    return _check(lib.mlkv_decode_attention_weights(handle, layer, _ptr(Q), _ptr(out), p, w,
+    return _check(lib.mlkv_decode_attention_weights(handle, layer, _rows("Q", Q), _rows("out", out), p, w,
                                                     _dense("weights_out", weights_out, "float32"),
                                                     _stream(stream)))
 
@@ -596,9 +603,9 @@ class MLKVCache:
         return mlkv_prefill_window(self.handle, layer, Q, K, V, out, prompt_lens, int(Q.shape[1]),
                                    window, sinks, stream)
 
-    # (A step's call: one condition over a tensor's type, shape and density, one over an array's, and the library
-    # called from here: of a call with two tensors and one array 1.5 us are Python's, 2.2 through the functions
-    # of the same names.)
+    # (A step's call: one condition over the queries' and outputs' types, sizes and density, one over another tensor's,
+    # one over an array's, and the library called from here instead of through the functions of the same names. The
+    # conditions over queries and outputs take 0.4 us.)
 
     def _tensor(self, name, t, dtype, shape):
         want = _dtypes.get(dtype) or _dtype(dtype)
@@ -606,15 +613,31 @@ class MLKVCache:
             raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must be dense, {dtype} and of shape {list(shape)}")
         return t.data_ptr()
 
+    def _rows(self, name, t, n):
+        """Queries, keys, values or outputs: n numbers in all."""
+        if (t is None or t.dtype is not (_dtypes.get("bfloat16") or _dtype("bfloat16")) or t.numel() != n
+                or not t.is_contiguous()):
+            raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must be dense, bfloat16 and hold {n} numbers")
+        return t.data_ptr()
+
+    def _queries(self, Q, out):
+        """The addresses of a decode's queries and outputs, checked in one condition."""
+        bf16, n = _dtypes.get("bfloat16") or _dtype("bfloat16"), self.b * self.h * self.d
+        if (Q is None or out is None or Q.dtype is not bf16 or out.dtype is not bf16 or Q.numel() != n
+                or out.numel() != n or not Q.is_contiguous() or not out.is_contiguous()):
+            return self._rows("Q", Q, n), self._rows("out", out, n)   # (which says what is wrong)
+        return Q.data_ptr(), out.data_ptr()
+
     def _numbers(self, name, a, n):
         """n int32 numbers on the host (keep them while their address is in use) and their address."""
-        if not (type(a) is np.ndarray and a.dtype is _INT32 and a.flags.c_contiguous):
+        if type(a) is not np.ndarray or a.dtype is not _INT32:
             a = as_seq_lens(a)
         if a.shape != (n,):
             raise MLKVError(MLKV_ERR_INVALID_ARG, f"{name} must hold {n} numbers")
         try:
             return a, _address(_byte_at(a))
-        except (TypeError, ValueError):   # read-only or empty
+        except (TypeError, ValueError):   # read-only or with gaps
+            a = as_seq_lens(a)
             return a, a.ctypes.data
 
     def _blocks(self):
@@ -626,16 +649,23 @@ class MLKVCache:
         o, po = self._numbers("prefix_of", prefix_of, self.b)
         n, pn = self._numbers("prefix_lens", prefix_lens, prefix.b)
         a, p = self._numbers("seq_lens", seq_lens, self.b)
-        return _check(lib.mlkv_decode_attention_prefix(self.handle, layer, prefix.handle, po, pn, _ptr(Q),
-                                                       _ptr(out), p, _stream(stream)))
+        q, to = self._queries(Q, out)
+        return _check(lib.mlkv_decode_attention_prefix(self.handle, layer, prefix.handle, po, pn, q, to, p,
+                                                       _stream(stream)))
 
     def prefill_prefix(self, layer, prefix, prefix_of, prefix_lens, Q, K, V, out, prompt_lens, stream=None):
         """Causal prefill behind a shared beginning; Q / out [b][s_max][h][d], K / V [b][g][s_max][d]."""
         o, po = self._numbers("prefix_of", prefix_of, self.b)
         n, pn = self._numbers("prefix_lens", prefix_lens, prefix.b)
         a, p = self._numbers("prompt_lens", prompt_lens, self.b)
-        return _check(lib.mlkv_prefill_prefix(self.handle, layer, prefix.handle, po, pn, _ptr(Q), _ptr(K),
-                                              _ptr(V), _ptr(out), p, int(Q.shape[1]), _stream(stream)))
+        s_max = int(Q.shape[1]) if Q is not None and Q.dim() > 1 else 0
+        rows = self.b * s_max * self.h * self.d
+        q, to, k, v = self._rows("Q", Q, rows), self._rows("out", out, rows), None, None
+        if 0 <= layer < self.l and self.owner[layer] == layer:   # (others read the slot)
+            kv = self.b * self.g * s_max * self.d
+            k, v = self._rows("K", K, kv), self._rows("V", V, kv)
+        return _check(lib.mlkv_prefill_prefix(self.handle, layer, prefix.handle, po, pn, q, k, v, to, p, s_max,
+                                              _stream(stream)))
 
     def block_bounds(self, layer, seq_lens, bounds, scales, first=None, stream=None):
         """Bounds int8 [b][g][n_blocks][2][d] and scales fp32 [b][g][n_blocks] of the keys of every block
@@ -652,16 +682,18 @@ class MLKVCache:
         a, p = self._numbers("seq_lens", seq_lens, self.b)
         n, n_select = self._blocks(), blocks.shape[-1]
         return _check(lib.mlkv_select_blocks(
-            self.handle, layer, _ptr(Q), self._tensor("bounds", bounds, "int8", n + (2, self.d)),
-            self._tensor("scales", scales, "float32", n), p, n_select, n_first, n_last,
+            self.handle, layer, self._rows("Q", Q, self.b * self.h * self.d),
+            self._tensor("bounds", bounds, "int8", n + (2, self.d)), self._tensor("scales", scales, "float32", n), p,
+            n_select, n_first, n_last,
             self._tensor("blocks", blocks, "int32", (self.b, self.g, n_select)), _stream(stream)))
 
     def decode_attention_blocks(self, layer, Q, out, seq_lens, blocks, stream=None):
         """Decode attention over the listed blocks alone, int32 [b][g][n]."""
         a, p = self._numbers("seq_lens", seq_lens, self.b)
+        q, to = self._queries(Q, out)
         n = blocks.shape[-1]
         return _check(lib.mlkv_decode_attention_blocks(
-            self.handle, layer, _ptr(Q), _ptr(out), p,
+            self.handle, layer, q, to, p,
             self._tensor("blocks", blocks, "int32", (self.b, self.g, n)), n, _stream(stream)))
 
     def decode_attention_weights(self, layer, Q, out, seq_lens, weights_in, weights_out, stream=None):
@@ -670,8 +702,9 @@ class MLKVCache:
         a, p = self._numbers("seq_lens", seq_lens, self.b)
         n = (self.b, self.g, self.max_seq)
         w = None if weights_in is None else self._tensor("weights_in", weights_in, "float32", n)
+        q, to = self._queries(Q, out)
         return _check(lib.mlkv_decode_attention_weights(
-            self.handle, layer, _ptr(Q), _ptr(out), p, w,
+            self.handle, layer, q, to, p, w,
             self._tensor("weights_out", weights_out, "float32", n), _stream(stream)))
 
     def evict(self, layer, weights_in, weights_out, seq_lens, keep, recent, kept, to=None, stream=None):

@@ -100,7 +100,8 @@ def test_arguments_reach_the_library(lib, call):
 
 
 @pytest.mark.parametrize("numbers", [(7, 9), np.array([7, 9]), np.array([7, 9], dtype=np.int32),
-                                     np.array([7, 0, 9], dtype=np.int32)[::2], np.array([7.0, 9.0])])
+                                     np.array([7, 0, 9], dtype=np.int32)[::2], np.array([7.0, 9.0]),
+                                     np.frombuffer(np.array([7, 9], dtype=np.int32).tobytes(), dtype=np.int32)])
 def test_numbers_of_any_kind_reach_it_as_int32(lib, numbers):
     CACHE.decode_attention_blocks(1, Q, OUT, numbers, BLOCKS, stream=5)
     assert lib.calls[0][1][4] == [7, 9]
@@ -145,4 +146,79 @@ def test_refused_before_the_library(lib, call, i):
     with pytest.raises(package.MLKVError) as e:
         getattr(CACHE, call)(**kwargs, stream=5)
     assert e.value.code == BAD and "must" in str(e.value)
+    assert not lib.calls
+
+
+# Tensors that the kernels would read or write as they lie: another type, other sizes, gaps.
+DECODE = [("Q", Q), ("out", OUT)]
+PROMPT = [("Q", PQ), ("out", POUT), ("K", K), ("V", V)]
+TENSORS = {"select_blocks": DECODE[:1], "decode_attention_blocks": DECODE, "decode_attention_weights": DECODE,
+           "decode_attention_prefix": DECODE, "prefill_prefix": PROMPT}
+
+
+def _others(name, t):
+    yield dict([(name, t.float())])
+    yield dict([(name, t.half())])
+    yield dict([(name, t[..., :32])])
+    yield dict([(name, t[:1])])
+    yield dict([(name, torch.cat([t, t], 1)[:, ::2])])
+    yield dict([(name, None)])
+
+
+@pytest.mark.parametrize("call", sorted(TENSORS))
+def test_queries_and_outputs_of_another_kind_are_refused(lib, call):
+    for name, t in TENSORS[call]:
+        for change in _others(name, t):
+            with pytest.raises(package.MLKVError) as e:
+                getattr(CACHE, call)(**dict(GOOD[call][0], **change), stream=5)
+            assert e.value.code == BAD and name in str(e.value), (name, change)
+    assert not lib.calls
+
+
+def test_prompts_of_a_reading_layer_need_no_keys(lib):
+    CACHE.prefill_prefix(**dict(GOOD["prefill_prefix"][0], layer=1, K=None, V=None), stream=5)
+    assert lib.calls[0][1][6:8] == [None, None]
+
+
+def test_layers_out_of_range_are_the_library_s_to_refuse(lib):
+    for layer in (-1, 2):
+        CACHE.prefill_prefix(**dict(GOOD["prefill_prefix"][0], layer=layer), stream=5)
+    assert [c[1][1] for c in lib.calls] == [-1, 2]
+
+
+# The functions of the library's names, on handles: those take sizes as they are given.
+def _function(call):
+    kwargs = dict(GOOD[call][0])
+    for name in ("prefix",):
+        if name in kwargs:
+            kwargs[name] = kwargs[name].handle
+    if call == "select_blocks":
+        kwargs["n_select"] = 5
+    if call == "decode_attention_blocks":
+        kwargs["n_blocks"] = 5
+    if call == "evict":
+        kwargs.update(to=1001, k_max=9)
+    if call == "prefill_prefix":
+        kwargs["s_max"] = 10
+    return getattr(package, "mlkv_" + call), kwargs
+
+
+@pytest.mark.parametrize("call", sorted(GOOD))
+def test_functions_on_handles(lib, call):
+    fn, kwargs = _function(call)
+    fn(1001, **kwargs, stream=5)
+    assert lib.calls == [("mlkv_" + call, GOOD[call][1])]
+
+
+@pytest.mark.parametrize("call", sorted(GOOD))
+def test_functions_on_handles_refuse_other_types(lib, call):
+    fn, kwargs = _function(call)
+    tensors = [k for k, v in kwargs.items() if isinstance(v, torch.Tensor)]
+    assert tensors
+    for name in tensors:
+        t = kwargs[name]
+        for other in (t.to(torch.float64), torch.cat([t, t], 1)[:, ::2]):
+            with pytest.raises(package.MLKVError) as e:
+                fn(1001, **dict(kwargs, **{name: other}), stream=5)
+            assert e.value.code == BAD and name in str(e.value)
     assert not lib.calls
