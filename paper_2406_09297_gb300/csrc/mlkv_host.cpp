@@ -20,6 +20,7 @@
 #include "mlkv_cache.h"
 #include "mlkv_host.h"
 #include "mlkv_internal.h"
+#include "mlkv_plan.h"
 
 using mlkv::aligned16;
 using mlkv::check_seq_lens;
@@ -1834,18 +1835,18 @@ int mlkv::issue_prefill(const PrefillCall &a, cudaStream_t stream)
     const bool one_tile = a.d == 64;
     p.head_pairs = (!one_tile && p.G % 2 == 0) ? 1 : 0;
     const int sels = p.head_pairs ? a.h / 2 : a.h;
-    auto pre_blocks = [&](int beta) { return shared ? (over.prefix_len[beta] + 127) / 128 : 0; };
-    int max_blocks = 0;   // key blocks that some unit sees
+    static thread_local int blocks[MLKV_MAX_BATCH], pre[MLKV_MAX_BATCH];
+    for (int beta = 0; beta < a.b; ++beta)
+        blocks[beta] = (a.prompt_lens[beta] + 127) / 128;
     if (shared) {
         over.tmap_p = *a.tmap_prefix;
         over.prefix_b = a.prefix_b;
         for (int beta = 0; beta < a.b; ++beta) {
             over.prefix_of[beta] = static_cast<int16_t>(a.prefix_of[beta]);
             over.prefix_len[beta] = a.prefix_len[beta];
+            pre[beta] = static_cast<int>((static_cast<unsigned>(a.prefix_len[beta]) + 127) / 128);
         }
     }
-    for (int beta = 0; beta < a.b; ++beta)
-        max_blocks = std::max(max_blocks, pre_blocks(beta) + (a.prompt_lens[beta] + 127) / 128);
     auto issue = [&](int n) {
         p.n_units = n;
         if (a.launches != nullptr)
@@ -1854,22 +1855,22 @@ int mlkv::issue_prefill(const PrefillCall &a, cudaStream_t stream)
                       : mlkv::launch_prefill(a.d, &tmap_q, tmap_k, tmap_v, plain, stream);
     };
     int n = 0;
-    for (int seen = max_blocks - 1; seen >= 0; --seen) {
-        for (int beta = 0; beta < a.b; ++beta) {
-            const int nb = (a.prompt_lens[beta] + 127) / 128, qb = seen - pre_blocks(beta);
-            if (qb < 0 || qb >= nb || (!one_tile && !p.head_pairs && qb % 2 == 0 && qb != nb - 1))
-                continue;
-            for (int sel = 0; sel < sels; ++sel) {
-                units[n] = static_cast<uint32_t>(beta) | (static_cast<uint32_t>(qb) << 10) |
-                           (static_cast<uint32_t>(sel) << 24);
-                if (++n == most) {
-                    if ((e = issue(n)) != cudaSuccess)
-                        return fail_cuda(e, "prefill launch");
-                    n = 0;
-                }
+    const bool all = mlkv::for_query_blocks(a.b, blocks, shared ? pre : nullptr, [&](int beta, int qb) {
+        if (!one_tile && !p.head_pairs && qb % 2 == 0 && qb != blocks[beta] - 1)
+            return true;
+        for (int sel = 0; sel < sels; ++sel) {
+            units[n] = static_cast<uint32_t>(beta) | (static_cast<uint32_t>(qb) << 10) |
+                       (static_cast<uint32_t>(sel) << 24);
+            if (++n == most) {
+                if ((e = issue(n)) != cudaSuccess)
+                    return false;
+                n = 0;
             }
         }
-    }
+        return true;
+    });
+    if (!all)
+        return fail_cuda(e, "prefill launch");
     if (n > 0 && (e = issue(n)) != cudaSuccess)
         return fail_cuda(e, "prefill launch");
     return MLKV_OK;

@@ -2,7 +2,11 @@
 // tested without a GPU.  Internal.
 #pragma once
 
+#include <stdint.h>
+
 #include <algorithm>
+
+#include "mlkv.h"
 
 namespace mlkv {
 
@@ -56,6 +60,44 @@ inline PrefixPlan plan_prefix(const int *n_kt, const int *pairs, int n, int sm_c
             break;
     }
     return best;
+}
+
+// The query blocks of b prompts, those that see the most key blocks first, then by sequence: visit(beta, qb) for block
+// qb of blocks[beta], behind pre[beta] key blocks of a prefix (NULL: none anywhere).  Stops where visit returns false.
+// With prefixes the sequences enter by the last key block that they see and leave behind their first query block, so
+// that the host's work is the prompts', however far their prefixes reach (1024 prompts of two blocks behind a million
+// positions, 17 ms if every key block is walked through).
+template <typename Visit>
+inline bool for_query_blocks(int b, const int *blocks, const int *pre, const Visit &visit)
+{
+    if (pre == nullptr) {
+        const int most = *std::max_element(blocks, blocks + b);
+        for (int qb = most - 1; qb >= 0; --qb)
+            for (int beta = 0; beta < b; ++beta)
+                if (qb < blocks[beta] && !visit(beta, qb))
+                    return false;
+        return true;
+    }
+    uint16_t order[MLKV_MAX_BATCH], live[MLKV_MAX_BATCH];   // by last key block, falling; those under way, by number
+    for (int beta = 0; beta < b; ++beta)
+        order[beta] = static_cast<uint16_t>(beta);
+    const auto last = [&](int beta) { return pre[beta] + blocks[beta] - 1; };
+    std::sort(order, order + b, [&](int x, int y) { return last(x) != last(y) ? last(x) > last(y) : x < y; });
+    int n_live = 0, seen = 0;
+    for (int next = 0; next < b || n_live > 0; --seen) {
+        if (n_live == 0)
+            seen = last(order[next]);
+        const int before = n_live;
+        while (next < b && last(order[next]) == seen)
+            live[n_live++] = order[next++];
+        if (before > 0 && n_live > before)
+            std::inplace_merge(live, live + before, live + n_live);
+        for (int i = 0; i < n_live; ++i)
+            if (!visit(static_cast<int>(live[i]), seen - pre[live[i]]))
+                return false;
+        n_live = static_cast<int>(std::remove_if(live, live + n_live, [&](int x) { return pre[x] == seen; }) - live);
+    }
+    return true;
 }
 
 }  // namespace mlkv

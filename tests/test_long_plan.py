@@ -1,5 +1,4 @@
 """The launch plans of the operators for long caches, compiled from their header without CUDA."""
-import os
 import subprocess
 
 import pytest
@@ -37,7 +36,7 @@ def compiled(tmp, name, source):
     src, exe = str(tmp / f"{name}.cpp"), str(tmp / name)
     with open(src, "w") as f:
         f.write(source)
-    subprocess.run(["g++", "-std=c++17", "-O2", "-I", build.CSRC, "-o", exe, src], check=True)
+    subprocess.run(["g++", "-std=c++17", "-O2", "-I", build.CSRC, "-I", build.INCLUDE, "-o", exe, src], check=True)
     return exe
 
 
@@ -89,3 +88,85 @@ def test_one_prefix_more_takes_little_more(plans, g, G, d, tokens, per):
     for a, b, n in zip(us, us[1:], work):
         # at most the new prefix's part, and a wave of units more
         assert b <= a * (n + 1) / n + 1.2 * us[0], (n, a, b)
+
+
+BLOCKS = r"""
+#include <chrono>
+#include <cstdio>
+#include <cstring>
+#include <random>
+#include <vector>
+#include "mlkv_plan.h"
+
+using Order = std::vector<long long>;
+
+static Order blocks_of(const std::vector<int> &n, const std::vector<int> &pre, bool none)
+{
+    Order o;
+    mlkv::for_query_blocks(static_cast<int>(n.size()), n.data(), none ? nullptr : pre.data(), [&](int beta, int qb) {
+        o.push_back(beta * 1000000LL + qb);
+        return true;
+    });
+    return o;
+}
+
+// as the order is defined
+static Order plain(const std::vector<int> &n, const std::vector<int> &pre)
+{
+    Order o;
+    int most = 0;
+    for (size_t i = 0; i < n.size(); ++i)
+        most = std::max(most, n[i] + pre[i]);
+    for (int seen = most - 1; seen >= 0; --seen)
+        for (size_t i = 0; i < n.size(); ++i)
+            if (seen >= pre[i] && seen - pre[i] < n[i])
+                o.push_back(static_cast<long long>(i) * 1000000LL + seen - pre[i]);
+    return o;
+}
+
+int main()
+{
+    std::mt19937 rng(3);
+    for (int k = 0; k < 3000; ++k) {
+        const int b = 1 + rng() % (k % 50 == 0 ? 1024 : 12), most = 1 + rng() % 9, far = 1 + rng() % (k % 3 ? 5 : 400);
+        std::vector<int> n(b), pre(b);
+        for (int i = 0; i < b; ++i) {
+            n[i] = 1 + rng() % most;
+            pre[i] = rng() % 4 ? rng() % far : 0;
+        }
+        if (blocks_of(n, pre, false) != plain(n, pre))
+            return std::printf("order %d\n", k), 1;
+        if (blocks_of(n, std::vector<int>(), true) != plain(n, std::vector<int>(b, 0)))
+            return std::printf("order without prefixes %d\n", k), 1;
+    }
+    int visits = 0;   // a visit that says no is the last
+    const int n2[2] = {3, 2}, pre2[2] = {1, 7};
+    const bool all = mlkv::for_query_blocks(2, n2, pre2, [&](int, int) { return ++visits < 3; });
+    if (all || visits != 3)
+        return std::printf("stop\n"), 1;
+    // 1024 prompts of two blocks behind prefixes of one block, and of 7813 (a million positions)
+    double us[2];
+    for (int far = 0; far < 2; ++far) {
+        std::vector<int> n(1024, 2), pre(1024, far ? 7813 : 1);
+        pre[5] = 0;
+        us[far] = 1e30;
+        for (int r = 0; r < 9; ++r) {
+            const auto t0 = std::chrono::steady_clock::now();
+            long long sum = 0;
+            mlkv::for_query_blocks(1024, n.data(), pre.data(), [&](int beta, int qb) { sum += beta ^ qb; return true; });
+            const double t = std::chrono::duration<double, std::micro>(std::chrono::steady_clock::now() - t0).count();
+            us[far] = std::min(us[far], t + (sum == 42 ? 1e-9 : 0));
+        }
+    }
+    std::printf("%g %g\n", us[0], us[1]);
+    return 0;
+}
+"""
+
+
+def test_query_blocks_of_prompts(tmp_path):
+    """Their order, and that a far prefix costs the host nothing: the work is the prompts' own."""
+    out = subprocess.run([compiled(tmp_path, "blocks", BLOCKS)], capture_output=True, text=True)
+    assert out.returncode == 0, out.stdout
+    near, far = (float(x) for x in out.stdout.split())
+    assert far <= 5 * near + 50, (near, far)
