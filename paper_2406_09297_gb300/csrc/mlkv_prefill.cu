@@ -906,11 +906,11 @@ __global__ void __launch_bounds__(PrefillPlan<D, kForm>::kThreads,
                 // The reference maximum is raised to the tile's when a score exceeds it by more
                 // than 2^8 (the thread then rescales its O row in TMEM).
                 const float m_tile = max3f(mx[0], mx[1], fmaxf(mx[2], mx[3])) * scale;
-                const bool raise = (m_run == NEG_INF) || (m_tile > m_run + 8.f);
+                // (So it is by a row's first score above -infinity; without one yet the row keeps its zeros.)
+                const bool raise = m_tile > m_run + 8.f;
                 if (__any_sync(0xffffffffu, raise)) {
-                    const float m_new = raise ? fmaxf(m_run, m_tile) : m_run;
-                    // 0 while nothing is summed; a row without a score above -infinity yet keeps its zeros
-                    const float alpha = m_new == NEG_INF ? 1.f : fast_exp2(m_run - m_new);
+                    const float m_new = raise ? m_tile : m_run;
+                    const float alpha = raise ? fast_exp2(m_run - m_new) : 1.f;   // 0 while nothing is summed
                     if (t > wg) {
                         // Rescale this row of O once the previous tile's product has landed.
                         if (PL::kPSep)
