@@ -270,7 +270,9 @@ int mlkv_prefill_window(mlkv_cache_t c, int layer, const void *Q, const void *K,
  * included (keys are encoded by the caller: a sequence's own positions follow its prefix's).  A head whose scores are
  * all -infinity gets zeros.  Calls on c must be
  * ordered with those on `prefix` that store what it reads.  Scratch of c is allocated when a call needs more than
- * any before (not while cuda_stream is captured: MLKV_ERR_UNSUPPORTED); at most 255 KV heads.
+ * any before (not while cuda_stream is captured: MLKV_ERR_UNSUPPORTED), at most twice what the call needs; what it
+ * outgrew, together no more than that, lives until mlkv_cache_destroy, for captured graphs hold its address.  At most
+ * 255 KV heads.
  * Errors: as mlkv_decode_attention; MLKV_ERR_MAP (the caches' layers or heads differ), MLKV_ERR_RANGE (prefixes,
  * lengths), MLKV_ERR_OOM.
  */
@@ -349,13 +351,15 @@ int mlkv_decode_attention_blocks(mlkv_cache_t c, int layer, const void *Q, void 
 /*
  * mlkv_decode_attention_weights - mlkv_decode_attention that also adds up what each position of each KV head
  * was given: weights_out[beta][j][u] = weights_in[beta][j][u] + the sum over the group's heads of their softmax
- * weight of position u < seq_lens[beta] (Eq. 2's alpha; scores that are all -infinity give none).  The layers of an owner's block add to the owner's
- * weights one after the other.
+ * weight of position u < seq_lens[beta] (Eq. 2's alpha; scores that are all -infinity give none).  The layers of an
+ * owner's block add to the owner's weights one after the other.
  *
  *   weights_in   device fp32 [batch][g][max_seq], or NULL: zeros
  *   weights_out  device fp32 [batch][g][max_seq], written whole; weights_in itself, or apart from it
- * The other arguments and errors as for mlkv_decode_attention (its options do not apply).  Scratch of
- * batch * n_q_heads * (longest sequence) * 4 bytes, allocated as for mlkv_decode_attention_prefix.
+ * The other arguments and errors as for mlkv_decode_attention (its options do not apply).  The scores need
+ * batch * n_q_heads * (longest sequence, in whole blocks of 64) * 4 bytes of scratch, which is allocated as for
+ * mlkv_decode_attention_prefix: while sequences grow, up to twice that, and as much again of outgrown scratch.  One
+ * call with the longest lengths first makes room for all the others, captured ones among them.
  */
 int mlkv_decode_attention_weights(mlkv_cache_t c, int layer, const void *Q, void *out, const int *seq_lens,
                                   const float *weights_in, float *weights_out, void *cuda_stream);
