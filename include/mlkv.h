@@ -21,8 +21,11 @@
  *    respect to each other (one stream, or explicit events): they share the cache's merge scratch.
  *  - seq_lens (host int32[batch]) counts the token being decoded: sequence beta attends positions
  *    [0, seq_lens[beta]), 1 <= seq_lens[beta] <= max_seq.
- *  - No call allocates device memory except mlkv_cache_create; no call synchronises the device
- *    except mlkv_sync_status and mlkv_cache_destroy.
+ *  - Device memory is allocated by mlkv_cache_create and mlkv_q4_create, and as scratch of a cache, when a
+ *    call needs more than any before, by mlkv_decode_step_host (its staging), steps in the cross-layer fused form
+ *    and mlkv_decode_block_fused, mlkv_decode_attention_prefix, mlkv_prefill_prefix,
+ *    mlkv_decode_attention_weights and mlkv_evict; no other call does.  No call synchronises the device except
+ *    the ones that create, destroy or read a status (an allocation may).
  */
 #ifndef MLKV_H_
 #define MLKV_H_
@@ -284,7 +287,8 @@ int mlkv_decode_attention_prefix(mlkv_cache_t c, int layer, mlkv_cache_t prefix,
  * mlkv_prefill_prefix - mlkv_prefill of prompts that go on behind a shared beginning: prompt position t of
  * sequence beta attends to all of its prefix's positions and to positions 0 .. t of its prompt.  An owner layer
  * stores its prompt's K/V in c at positions [0, s_max); the prefix stays where it is, and mlkv_decode_attention_prefix
- * goes on from there.  (Scores that are all -infinity: zeros.)
+ * goes on from there.  (A row whose scores are all -infinity gets zeros; where no sequence has anything in front the
+ * call is mlkv_prefill, which gives NaN.)
  * prefix, prefix_of and prefix_lens as above, but prefix != c; the others and errors as for mlkv_prefill.  Short
  * prompts are taken as rows of a decode, with scratch of c as above; where that cannot be had, without.
  */

@@ -55,3 +55,36 @@ def test_the_longest_first_makes_room_for_all():
             call(n)
     graph.replay()
     cache.sync_status()
+
+
+def _bf16(*shape):
+    return torch.zeros(shape, dtype=torch.bfloat16, device="cuda")
+
+
+def test_calls_without_scratch_allocate_nothing():
+    b, h, g, d, cap, s = 8, 32, 8, 128, 3000, 2000
+    Q, out, K = _bf16(b, h, d), _bf16(b, h, d), _bf16(b, g, s, d)
+    P, pout = _bf16(b, s, h, d), _bf16(b, s, h, d)
+    new, n = _bf16(b, g, d), (cap + 63) // 64
+    bounds, scales = torch.zeros(b, g, n, 2, d, dtype=torch.int8, device="cuda"), torch.zeros(b, g, n, device="cuda")
+    blocks = torch.zeros(b, g, 9, dtype=torch.int32, device="cuda")
+    lens = [s + 1] * b
+
+    def calls(cache):
+        cache.load_prefix(0, K, K, s)
+        cache.prefill(0, P, K, K, pout, [s] * b)
+        cache.prefill_window(0, P, K, K, pout, [s] * b, 500, 4)
+        cache.append(0, new, new, lens)
+        cache.decode_attention(0, Q, out, lens)
+        cache.append_decode_attention(0, new, new, Q, out, lens)
+        cache.decode_attention_window(0, Q, out, lens, 500, 4)
+        cache.block_bounds(0, lens, bounds, scales)
+        cache.select_blocks(0, Q, bounds, scales, lens, blocks)
+        cache.decode_attention_blocks(0, Q, out, lens, blocks)
+        cache.sync_status()
+
+    calls(mlkv.MLKVCache(2, h, d, [0, 0], g, b, cap))   # (kernels are loaded when they first run)
+    cache = mlkv.MLKVCache(2, h, d, [0, 0], g, b, cap)
+    before = _used()
+    calls(cache)
+    assert _used() <= before
