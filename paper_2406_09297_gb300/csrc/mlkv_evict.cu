@@ -9,7 +9,8 @@
 // Units are handed out by a counter in rising order within a segment, so that what a unit waits for has been
 // handed out before it and is running: no wait depends on a CTA that has not started.
 // Bound by the bytes of what stays, read and written once, and by the selection's latency: 4096 positions kept of each of
-// 16 uneven sequences of up to 16,384, 8 KV heads of 128, 13.2 us to select, 72 us to move 423 MB in place, 5.9 TB/s.
+// 16 uneven sequences of up to 16,384, 8 KV heads of 128, 13.2 us to select, 72 us to move 423 MB into another cache,
+// 5.9 TB/s. In place, where units wait for those whose rows they overwrite, 106 us, 4.0 TB/s.
 #include "mlkv_device.cuh"
 #include "mlkv_long.h"
 #include "mlkv_topk.cuh"
@@ -318,9 +319,10 @@ cudaError_t launch_evict(int head_dim, const EvictParams &p, int max_len, int sm
     cfg.numAttrs = size > 1 ? 2 : 1;   // (a cluster's launch costs the host a microsecond more)
     void *args[] = {const_cast<EvictParams *>(&p)};
     // One launch where few rounds move what stays of a segment.  A round is a trip to memory and back, the second launch
-    // takes 2 to 4 us here and two of the host's.  us, one / two launches: 144 segments of 1000 positions, 250 kept,
-    // 6.8 / 9.5, 16 of 2000, 500 kept (two rounds) 8.7 / 8.1, four of 2000, 1900 kept (eight) 16.6 / 8.2; where nearly every SM has
-    // a segment, 128 of 2000, 500 kept (four) 14.8 / 16.7, of 4000, 1000 kept (eight) 26.0 / 26.5, in place 28.1 / 27.4.
+    // takes 2 to 4 us here and two of the host's.  us into another cache, one / two launches (and in place): 144 segments
+    // of 1000 positions, 250 kept, 7.7 / 9.7 (8.2 / 13.7), 16 of 2000, 500 kept (two rounds) 8.6 / 8.3 (10.2 / 12.2), 16
+    // of 2000, 1900 kept (eight) 16.8 / 8.8 (23.4 / 15.0); where nearly every SM has a segment, 128 of 2000, 500 kept
+    // (four) 17.4 / 18.2 (20.3 / 24.3), of 4000, 1000 kept (eight) 29.2 / 29.4 (36.6 / 39.8).
     const int per_round = size * (nt * kKeepVecs / (head_dim / 4)), rounds = (p.rows + per_round - 1) / per_round;
     const long long ctas = static_cast<long long>(p.b) * p.g * size;
     const bool whole = rounds <= (few || (2 * ctas > sm_count && ctas <= sm_count) ? 4 : ctas <= sm_count ? 2 : 0);

@@ -327,8 +327,9 @@ int mlkv::decode_rows(mlkv_cache *c, int layer, const mlkv_cache *prefix, const 
     // The prefixes for as many sequences at a time as have 16 heads together, beside the suffixes in their launch: read
     // from L2 again for every group of them, and merged by a launch.  us: 9, and what is longest of the bytes from HBM,
     // those through the SMs (8.5 TB/s) and a unit; half the longest suffix more where those are uneven.  Measured, us, end
-    // to end / by groups / by the prefix kernel: 4 sequences behind 16000 positions, 8 KV heads of 128, 31 / 22 / 27,
-    // 8 of them 46 / 27 / 32, 16 of them 65 / 39 / 34; 16 behind 4000, 12 KV heads of 64, 25 / 11 / 15.
+    // to end / by groups / by the prefix kernel: 4 sequences behind 16000 positions, 8 KV heads of 128, 26 / 21 / 27,
+    // 8 of them 37 / 26 / 32, 16 of them 64 / 37 / 34; 16 behind 4000, 12 KV heads of 64, 32 / 11 / 15.  (What is taken
+    // goes by the estimates: of 26 shapes it is within 3% of the best form in 22, and 8 to 29% behind in four.)
     const int S1 = 16 / c->G;
     double grouped_us = 1e30;
     int unit_tiles = 8;
